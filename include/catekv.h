@@ -12,6 +12,7 @@
  *                          (the paper is silent; implied by autoregressive decoding)
  *   catekv_decode_attn     Algorithm 1, decoding stage: Attention(q, k, v) over the
  *                          per-head lists ("all" retrieval on adaptive heads)
+ *   catekv_q8_*            the hybrid cache held in 8 bits (quantise, append, decode attention)
  *
  * Conventions
  *   - Every function returns 0 (CATEKV_OK) or a negative error code.  Arguments
@@ -531,6 +532,77 @@ int catekv_append_decode_attn(catekv_cache* cache, const void* k_new, const void
 int catekv_decode_attn_noalloc(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
                                int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
                                size_t plan_bytes, catekv_stream stream);
+
+/* ---------------------------------------------------------------- the cache in 8 bits */
+
+/*
+ * Decode attention is bound by the bytes of K and V that the hybrid cache keeps; these calls hold them in 8 bits
+ * (the paper keeps its caches in 16; this is this library's own form).  A block is CATEKV_Q8_BLOCK consecutive rows of
+ * a segment, from row 0 on; K and V each have one scale per block.  With a = the largest |x| of a block and M the
+ * type's largest number (448 for e4m3, 127 for int8):
+ *   scale = a / M (fp32),  code = x * M / a rounded to the nearest number of the type, ties to even;  the row that
+ *   attention sees is code * scale.  A block of zeros has scale 0.  A block that holds an infinity or a NaN has the scale
+ *   NaN, and so have the outputs of the heads that attend to it.
+ * Only complete blocks are held in 8 bits: the len mod 64 rows behind the last complete block stay bf16 in a tail of
+ * their own until the block is complete.  A row is thus rounded once, and the most recent rows are not rounded at all.
+ * Segments are laid out as in catekv_cache (catekv_cache_layout); an offset is a multiple of 64.
+ */
+#define CATEKV_Q8_E4M3 0
+#define CATEKV_Q8_INT8 1
+#define CATEKV_Q8_BLOCK 64
+typedef struct catekv_q8_cache {
+  int32_t B;              /* sequences */
+  int32_t Hkv;            /* KV heads */
+  int32_t d;              /* head dim, 128 */
+  int32_t dtype;          /* CATEKV_Q8_E4M3 or CATEKV_Q8_INT8 */
+  int64_t total_rows;     /* rows of each pool */
+  void* k_pool;           /* device, 8-bit codes [total_rows, d], 16-byte aligned */
+  void* v_pool;           /* device, 8-bit codes [total_rows, d], 16-byte aligned */
+  float* k_scale;         /* device [total_rows / 64]: the scale of the block that starts at pool row 64 i */
+  float* v_scale;         /* device [total_rows / 64] */
+  void* k_tail;           /* device, bf16 [B*Hkv, 64, d], 16-byte aligned: row r of the unfinished block of segment s */
+  void* v_tail;           /* device, bf16 [B*Hkv, 64, d], 16-byte aligned */
+  const int32_t* seg_off_dev; /* device [B*Hkv], first row of each segment */
+  int32_t* seg_len_dev;       /* device [B*Hkv], rows held (complete blocks and tail) */
+  const int32_t* seg_off;     /* host   [B*Hkv] */
+  const int32_t* seg_cap;     /* host   [B*Hkv] */
+  int32_t* seg_len;           /* host   [B*Hkv], mirror of seg_len_dev kept by the library's calls */
+  int32_t reserved;           /* 0; copied from the source by catekv_q8_quantize (1: seg_len holds upper bounds) */
+  int32_t reserved1;          /* 0 */
+} catekv_q8_cache;
+
+/*
+ * Every segment of `src` (no overflow pages) into the same segment of `dst`: complete blocks as codes and scales, the rows
+ * behind them into the tail; dst's lengths are set (device and host).  Rows behind a segment's length are neither read
+ * nor written.  CATEKV_ERR_CAPACITY (nothing launched) if a segment does not fit; CATEKV_ERR_INVALID_ARG if the caches
+ * differ in B or Hkv; CATEKV_ERR_UNSUPPORTED for a source with overflow pages or more than 65535 segments.
+ */
+int catekv_q8_quantize(const catekv_cache* src, catekv_q8_cache* dst, catekv_stream stream);
+
+/*
+ * Append the decoded token's key and value (device bf16 [B, Hkv, d] contiguous) to every segment.  The row goes to the
+ * tail; where it completes a block, the block's codes and scales are written in the same call.
+ * CATEKV_ERR_CAPACITY (nothing launched) if any segment is full.
+ * catekv_q8_cache_advance: host mirror only, for replayed graphs (see catekv_cache_advance).
+ */
+int catekv_q8_append(catekv_q8_cache* cache, const void* k_new, const void* v_new, catekv_stream stream);
+int catekv_q8_cache_advance(catekv_q8_cache* cache, int32_t n_tokens);
+
+/*
+ * Split-KV decode attention over the 8-bit cache: catekv_decode_attn's arguments and results (softmax(sm_scale q K^T) V
+ * with the keys and values that the codes stand for and the bf16 tails; fp32 accumulation, probabilities carried as
+ * fp16 or bf16 pairs of 16 and more bits), with a plan of its own: catekv_q8_decode_plan cuts at block borders.  Buffer
+ * sizes are those of catekv_decode_plan_bytes and catekv_decode_workspace_bytes; num_ctas comes from
+ * catekv_q8_decode_num_ctas.  A plan stays valid while the segments grow (and shrink) like one of catekv_decode_plan;
+ * a plan of the other kind is refused (CATEKV_ERR_INVALID_ARG).  The ordering note of catekv_decode_attn holds for
+ * the blocks that were complete when the plan was built.
+ */
+int catekv_q8_decode_num_ctas(void);
+int catekv_q8_decode_plan(const catekv_q8_cache* cache, int32_t num_ctas, void* plan_host, void* plan_dev,
+                          size_t plan_bytes, catekv_stream stream);
+int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
+                          int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
+                          size_t plan_bytes, void* ws, size_t ws_bytes, catekv_stream stream);
 
 #ifdef __cplusplus
 }

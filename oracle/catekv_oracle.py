@@ -37,6 +37,10 @@ What each function follows
                                       heads, with the page criterion of Quest that
                                       the paper combines with (Section 4.2.2,
                                       appendix B.2.2; chunk size 8).
+* q8_grid, q8_encode, q8_rows       : this library's own form of the cache (the paper
+                                      keeps 16 bits): blocks of 64 rows rounded to 8-bit
+                                      numbers under one scale, the unfinished block
+                                      as it is.
 
 Parity pins: every function above is pinned by tests that do not re-use it
 (pure-Python brute force, closed forms, hand-worked examples, library
@@ -544,3 +548,51 @@ def kept_fraction(r: float, eta: float, budget: int, n: int) -> float:
     tokens, consistent heads keep budget/n (Section 4.2: 2048 of 128K is 1.56 %
     and about 41 % of the cache is retained at r = 0.4, eta = 1)."""
     return r * eta + (1.0 - r) * (budget / n)
+
+
+# --------------------------------------------------------------------------
+# The cache in 8 bits
+# --------------------------------------------------------------------------
+Q8_E4M3, Q8_INT8 = 0, 1
+Q8_BLOCK = 64
+
+
+def q8_grid(dtype: int) -> np.ndarray:
+    """The non-negative numbers of the type, ascending; entry i has code i (so that even codes are even entries)."""
+    if dtype == Q8_INT8:
+        return np.arange(128, dtype=np.float64)
+    out = []
+    for code in range(127):  # 0x7f is NaN
+        e, m = code >> 3, code & 7
+        out.append(m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10))
+    return np.array(out)
+
+
+def q8_encode(block_bits: np.ndarray, dtype: int):
+    """One block [rows, d] of bf16 bits -> (numbers of the codes [rows, d], scale as fp32).
+
+    a = max |x|, M = the type's largest number; x M / a to the nearest number of the type, ties to the even code;
+    scale = a / M rounded to fp32.  M x is exact in float64 (16 bits), and the distances to the two neighbours are
+    compared multiplied out (M |x| against a times the neighbours), so no quotient is rounded before the decision."""
+    x = bf16_to_f64(block_bits)
+    M = 127.0 if dtype == Q8_INT8 else 448.0
+    a = float(np.abs(x).max())
+    if not np.isfinite(a):
+        return np.zeros_like(x), np.float32(np.nan)
+    if a == 0.0:
+        return np.zeros_like(x), np.float32(0.0)
+    grid = q8_grid(dtype)
+    y = np.abs(x) * M
+    lo = np.clip(np.searchsorted(grid * a, y, side="right") - 1, 0, len(grid) - 2)
+    twice = 2.0 * y - (grid[lo] + grid[lo + 1]) * a  # > 0: nearer to the upper neighbour
+    up = (twice > 0) | ((twice == 0) & (lo % 2 == 1))
+    return np.sign(x) * grid[lo + up], np.float32(np.float32(a) / np.float32(M))
+
+
+def q8_rows(row_bits: np.ndarray, dtype: int) -> np.ndarray:
+    """A segment's rows as attention sees them: complete blocks rounded, the rest as it is (float64)."""
+    out = bf16_to_f64(row_bits)
+    for r in range(0, len(out) // Q8_BLOCK * Q8_BLOCK, Q8_BLOCK):
+        num, s = q8_encode(row_bits[r:r + Q8_BLOCK], dtype)
+        out[r:r + Q8_BLOCK] = num * float(s)
+    return out

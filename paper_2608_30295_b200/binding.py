@@ -24,6 +24,8 @@ STATUS_WAIT_EXPIRED, STATUS_CAPACITY, STATUS_INDEX_RANGE = 1, 2, 4
 POOL_NONE, POOL_CHUNK, POOL_SLIDING = 0, 1, 2
 OUT_BF16, OUT_FP32 = 0, 1
 SEG_ALIGN = 128
+Q8_E4M3, Q8_INT8 = 0, 1
+Q8_BLOCK = 64
 
 
 class CatekvError(RuntimeError):
@@ -47,6 +49,14 @@ class CacheStruct(C.Structure):
                 ("seg_off_dev", C.c_void_p), ("seg_len_dev", C.c_void_p),
                 ("seg_off", C.c_void_p), ("seg_cap", C.c_void_p), ("seg_len", C.c_void_p),
                 ("pages", C.POINTER(PagesStruct)), ("seg_cap_dev", C.c_void_p)]
+
+
+class Q8CacheStruct(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32), ("total_rows", C.c_int64),
+                ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_tail", C.c_void_p), ("v_tail", C.c_void_p), ("seg_off_dev", C.c_void_p), ("seg_len_dev", C.c_void_p),
+                ("seg_off", C.c_void_p), ("seg_cap", C.c_void_p), ("seg_len", C.c_void_p),
+                ("reserved", C.c_int32), ("reserved1", C.c_int32)]
 
 
 class StatusStruct(C.Structure):
@@ -117,6 +127,12 @@ def _load():
         "catekv_cache_sync_lengths": (C.c_int, [C.POINTER(CacheStruct), vp]),
         "catekv_window_attn_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
         "catekv_window_attn": (C.c_int, [vp, vp, vp, i64, i64, i64, vp, i32, i32, i32, i32, i32, vp, i32, vp, vp, vp, sz, vp]),
+        "catekv_q8_quantize": (C.c_int, [C.POINTER(CacheStruct), C.POINTER(Q8CacheStruct), vp]),
+        "catekv_q8_append": (C.c_int, [C.POINTER(Q8CacheStruct), vp, vp, vp]),
+        "catekv_q8_cache_advance": (C.c_int, [C.POINTER(Q8CacheStruct), i32]),
+        "catekv_q8_decode_num_ctas": (C.c_int, []),
+        "catekv_q8_decode_plan": (C.c_int, [C.POINTER(Q8CacheStruct), i32, vp, vp, sz, vp]),
+        "catekv_q8_decode_attn": (C.c_int, [C.POINTER(Q8CacheStruct), vp, i32, f32, vp, i32, vp, vp, vp, sz, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -552,3 +568,84 @@ def catekv_classify_heads(cv, r: float) -> np.ndarray:
     mask = np.zeros(n_heads, dtype=np.uint8)
     _check(_lib.catekv_classify_heads(_np_ptr(cv), n_samples, n_heads, r, _np_ptr(mask)), "catekv_classify_heads")
     return mask
+
+
+# ---------------------------------------------------------------- the cache in 8 bits
+
+
+class Q8Cache:
+    """Device pools (8-bit codes, one fp32 scale per block of 64 rows, bf16 tails) and segment tables of one layer's
+    hybrid cache in 8 bits (memory only).  dtype: Q8_E4M3 or Q8_INT8; k_pool and v_pool are float8_e4m3fn or int8."""
+
+    def __init__(self, B: int, Hkv: int, len0, max_new: int, dtype: int = Q8_E4M3, device="cuda", d: int = 128):
+        if dtype not in (Q8_E4M3, Q8_INT8):
+            raise CatekvError(ERR_UNSUPPORTED, "Q8Cache")
+        self.B, self.Hkv, self.d, self.dtype = B, Hkv, d, dtype
+        self.seg_off, self.seg_cap, self.total_rows = catekv_cache_layout(B, Hkv, len0, max_new)
+        self.seg_len = np.zeros(B * Hkv, dtype=np.int32)
+        self.device = torch.device(device)
+        rows = max(self.total_rows, Q8_BLOCK)
+        code = torch.float8_e4m3fn if dtype == Q8_E4M3 else torch.int8
+        self.k_pool = torch.empty((rows, d), dtype=code, device=device)
+        self.v_pool = torch.empty((rows, d), dtype=code, device=device)
+        self.k_scale = torch.empty(rows // Q8_BLOCK, dtype=torch.float32, device=device)
+        self.v_scale = torch.empty_like(self.k_scale)
+        self.k_tail = torch.empty((B * Hkv, Q8_BLOCK, d), dtype=torch.bfloat16, device=device)
+        self.v_tail = torch.empty_like(self.k_tail)
+        self.seg_off_dev = torch.from_numpy(self.seg_off).to(device)
+        self.seg_len_dev = torch.zeros(B * Hkv, dtype=torch.int32, device=device)
+        self.struct = Q8CacheStruct(B, Hkv, d, dtype, self.total_rows, self.k_pool.data_ptr(), self.v_pool.data_ptr(),
+                                    self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.k_tail.data_ptr(),
+                                    self.v_tail.data_ptr(), self.seg_off_dev.data_ptr(), self.seg_len_dev.data_ptr(),
+                                    _np_ptr(self.seg_off), _np_ptr(self.seg_cap), _np_ptr(self.seg_len), 0, 0)
+
+    def set_lengths(self, lens):
+        """Set host mirror and device lengths (used when rows are written by the caller)."""
+        self.seg_len[:] = np.asarray(lens, dtype=np.int32).reshape(-1)
+        self.seg_len_dev.copy_(torch.from_numpy(self.seg_len))
+
+
+def _here(where: str, device, *tensors):
+    """The library works on the current device and stream: a buffer that lives elsewhere is refused."""
+    d = torch.device(device)
+    here = torch.cuda.current_device()
+    if d.type != "cuda" or (d.index is not None and d.index != here) or any(t is not None and t.device != torch.device("cuda", here)
+                                                                            for t in tensors):
+        raise CatekvError(ERR_INVALID_ARG, where)
+
+
+def catekv_q8_quantize(src: Cache, dst: Q8Cache):
+    _here("catekv_q8_quantize", src.device, src.k_pool, dst.k_pool)
+    _check(_lib.catekv_q8_quantize(C.byref(src.struct), C.byref(dst.struct), _stream()), "catekv_q8_quantize")
+
+
+def catekv_q8_append(cache: Q8Cache, k_new: torch.Tensor, v_new: torch.Tensor):
+    assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.dtype == v_new.dtype == torch.bfloat16
+    assert k_new.numel() == v_new.numel() == cache.B * cache.Hkv * cache.d
+    _here("catekv_q8_append", cache.device, k_new, v_new)
+    _check(_lib.catekv_q8_append(C.byref(cache.struct), k_new.data_ptr(), v_new.data_ptr(), _stream()), "catekv_q8_append")
+
+
+def catekv_q8_cache_advance(cache: Q8Cache, n_tokens: int = 1):
+    """Host mirror only: account for appends that a replayed CUDA graph performs on the device."""
+    _check(_lib.catekv_q8_cache_advance(C.byref(cache.struct), n_tokens), "catekv_q8_cache_advance")
+
+
+def catekv_q8_decode_num_ctas() -> int:
+    n = _lib.catekv_q8_decode_num_ctas()
+    if n < 0:
+        raise CatekvError(n, "catekv_q8_decode_num_ctas")
+    return n
+
+
+def catekv_q8_decode_plan(cache: Q8Cache, plan: DecodePlan):
+    _check(_lib.catekv_q8_decode_plan(C.byref(cache.struct), plan.num_ctas, plan.host.data_ptr(), plan.dev.data_ptr(),
+                                      plan.bytes, _stream()), "catekv_q8_decode_plan")
+
+
+def catekv_q8_decode_attn(cache: Q8Cache, q: torch.Tensor, plan: DecodePlan, out: torch.Tensor,
+                          lse_out: Optional[torch.Tensor] = None, sm_scale: float = 0.0):
+    assert q.shape[0] == cache.B and q.shape[2] == cache.d and out.shape == q.shape
+    assert lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and lse_out.numel() == q.shape[0] * q.shape[1])
+    _here("catekv_q8_decode_attn", cache.device, q, out, lse_out, plan.dev)
+    _decode_call(_lib.catekv_q8_decode_attn, "catekv_q8_decode_attn", cache, q, plan, out, lse_out, sm_scale)

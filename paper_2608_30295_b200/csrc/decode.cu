@@ -492,15 +492,6 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
 // ------------------------------------------------------------------------------------------
 // Combine: merge the partials of every segment that was cut into several pieces
 // ------------------------------------------------------------------------------------------
-struct CombineArgs {
-  const SegInfo* seg_info;
-  const float* part_o;
-  const float* part_lse;
-  void* out;
-  float* lse_out;
-  int32_t Hq, Hkv, G, out_fp32;
-};
-
 // One CTA of 8 warps per (segment, query head of the group).  The kernel is a chain of dependent trips to
 // memory, so it is arranged to have one: a warp loads the values and the LSEs of its eighth of the pieces at
 // once (a lane owns four consecutive d, a piece is one 512-byte row per warp-load) and merges them under a
@@ -597,6 +588,11 @@ __global__ void __launch_bounds__(kCombineWarps * 32) decode_combine_kernel(cons
     if (a.lse_out && lane == 0)
       a.lse_out[(size_t)b * a.Hq + h * a.G + hd] = W > 0.f ? (M + log2f(W)) * 0.6931471805599453f : -INFINITY;
   }
+}
+
+int launch_combine(const CombineArgs& a, int n_segs, cudaStream_t stream) {
+  CATEKV_CUDA_TRY(launch_pdl(decode_combine_kernel, dim3(n_segs, a.G), dim3(kCombineWarps * 32), 0, stream, a));
+  return CATEKV_OK;
 }
 
 }  // namespace catekv
@@ -708,7 +704,8 @@ static int decode_launch(int phases, const catekv_cache* cache, const void* k_ne
     ca.Hkv = cache->Hkv;
     ca.G = G;
     ca.out_fp32 = out_fp32;
-    CATEKV_CUDA_TRY(launch_pdl(decode_combine_kernel, dim3(n_segs, G), dim3(kCombineWarps * 32), 0, st, ca));
+    rc = launch_combine(ca, n_segs, st);
+    if (rc) return rc;
   }
   return CATEKV_OK;
 }

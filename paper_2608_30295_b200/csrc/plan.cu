@@ -13,24 +13,22 @@ extern "C" size_t catekv_decode_workspace_bytes(int32_t B, int32_t Hkv, int32_t 
   return ws_layout(B * Hkv, num_ctas, nullptr);
 }
 
-extern "C" int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, void* plan_host, void* plan_dev,
-                                  size_t plan_bytes, catekv_stream stream) {
-  CATEKV_API_RANGE();
-  int rc = check_cache(cache);
-  if (rc) return rc;
+// The schedule itself, for either kind of cache.  cut_align: a piece that does not end its segment ends at a multiple of
+// this many rows (1: wherever the CTA's share ends); end_charge: rows charged for every non-empty segment's end.
+int catekv::build_plan(const PlanSource& p, int32_t num_ctas, int32_t tile, int cut_align, int end_charge, void* plan_host,
+                       void* plan_dev, size_t plan_bytes, cudaStream_t stream) {
   if (num_ctas <= 0 || !plan_host) return CATEKV_ERR_INVALID_ARG;
-  const int n_segs = cache->B * cache->Hkv;
+  const int n_segs = p.n_segs;
   const PlanLayout L = plan_layout(n_segs, num_ctas);
   if (plan_bytes < L.bytes) return CATEKV_ERR_WORKSPACE;
   // The CTA that owns the end of a segment does more than stream rows: its last tile also takes the rows appended
   // since the plan was built, it stores the appended row, and it finishes one piece and starts the next (merge of
   // the warps, output, the next group's queries) while nothing new is issued.  Every non-empty segment's end is
-  // therefore charged kSegEndCharge rows, so that those CTAs get fewer plan-time rows and do not finish last.
+  // therefore charged end_charge rows, so that those CTAs get fewer plan-time rows and do not finish last.
   int64_t total = 0, charged = 0;
   for (int s = 0; s < n_segs; ++s) {
-    if (cache->seg_len[s] < 0 || cache->seg_len[s] > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;
-    total += cache->seg_len[s];
-    charged += cache->seg_len[s] + (cache->seg_len[s] > 0 ? kSegEndCharge : 0);
+    total += p.seg_len[s];
+    charged += p.seg_len[s] + (p.seg_len[s] > 0 ? end_charge : 0);
   }
   uint8_t* base = (uint8_t*)plan_host;
   memset(base, 0, L.bytes);
@@ -52,18 +50,19 @@ extern "C" int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, v
     ctas[c].item_begin = n_items;
     int64_t room = quota;
     while (seg < n_segs) {
-      const int32_t len = cache->seg_len[seg];
+      const int32_t len = p.seg_len[seg];
       if (len == 0) {
         // an empty segment still gets one (direct) item, so that the plan stays valid once it grows
-        items[n_items++] = WorkItem{seg, 0, 0, -1, (int64_t)cache->seg_off[seg], 1, cache->seg_cap[seg]};
+        items[n_items++] = WorkItem{seg, 0, 0, -1, (int64_t)p.seg_off[seg], 1, p.seg_cap[seg]};
         segs[seg] = SegInfo{0, 1, 0, 0};
         ++seg;
         seg_first_item = n_items;
         continue;
       }
       if (room <= 0) break;
-      const int32_t take = (int32_t)((int64_t)(len - pos) < room ? (len - pos) : room);
-      items[n_items++] = WorkItem{seg, pos, pos + take, 0, (int64_t)cache->seg_off[seg] + pos, 0, cache->seg_cap[seg]};
+      const int64_t want = (room + cut_align - 1) / cut_align * cut_align;
+      const int32_t take = (int32_t)((int64_t)(len - pos) < want ? (len - pos) : want);
+      items[n_items++] = WorkItem{seg, pos, pos + take, 0, (int64_t)p.seg_off[seg] + pos, 0, p.seg_cap[seg]};
       pos += take;
       room -= take;
       if (pos == len) {
@@ -82,7 +81,7 @@ extern "C" int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, v
         ++seg;
         pos = 0;
         seg_first_item = n_items;
-        room -= kSegEndCharge;
+        room -= end_charge;
       }
     }
     ctas[c].item_end = n_items;
@@ -95,13 +94,27 @@ extern "C" int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, v
   hdr->n_segs = n_segs;
   hdr->n_items = n_items;
   hdr->n_slots = n_slots;
-  hdr->tile = kTile;
+  hdr->tile = tile;
   hdr->total_rows = total;
   hdr->off_cta = (int32_t)L.off_cta;
   hdr->off_items = (int32_t)L.off_items;
   hdr->off_seg = (int32_t)L.off_seg;
   hdr->max_pieces = max_pieces;
   if (plan_dev)
-    CATEKV_CUDA_TRY(cudaMemcpyAsync(plan_dev, plan_host, L.bytes, cudaMemcpyHostToDevice, (cudaStream_t)stream));
+    CATEKV_CUDA_TRY(cudaMemcpyAsync(plan_dev, plan_host, L.bytes, cudaMemcpyHostToDevice, stream));
   return CATEKV_OK;
+}
+
+extern "C" int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, void* plan_host, void* plan_dev,
+                                  size_t plan_bytes, catekv_stream stream) {
+  CATEKV_API_RANGE();
+  int rc = check_cache(cache);
+  if (rc) return rc;
+  if (num_ctas <= 0 || !plan_host) return CATEKV_ERR_INVALID_ARG;
+  const int n_segs = cache->B * cache->Hkv;
+  if (plan_bytes < plan_layout(n_segs, num_ctas).bytes) return CATEKV_ERR_WORKSPACE;
+  for (int s = 0; s < n_segs; ++s)
+    if (cache->seg_len[s] < 0 || cache->seg_len[s] > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;
+  const PlanSource src = {n_segs, cache->seg_len, cache->seg_off, cache->seg_cap};
+  return build_plan(src, num_ctas, kTile, 1, kSegEndCharge, plan_host, plan_dev, plan_bytes, (cudaStream_t)stream);
 }

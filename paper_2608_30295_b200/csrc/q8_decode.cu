@@ -1,0 +1,597 @@
+// Decode attention over the 8-bit cache: split-KV partials on the tensor cores (the combine pass is decode.cu's).
+//
+// The stream is a warp's own.  A CTA owns a contiguous range of the rows of all segments laid end to end (q8 plans cut at block borders); its
+// four warps take the range's units in turn, a unit being half a block (32 rows of codes, 8 KB of K and V) or 16 rows of a bf16 tail
+// (8 KB as well).  Each warp keeps a ring of kQ8Stages units in flight with cp.async and never waits for another warp before a
+// segment's partial is merged.
+//
+// Codes are f16 numbers, so both products run on mma.m16n8k16 (f16) with the code converted in registers; tokens are M, the group's <= 8
+// query heads N.  Which token or which d a fragment slot stands for is free as long as both operands of a product agree, and is chosen so
+// that every shared-memory access is a conflict-free 16-byte load and nothing is transposed in memory:
+//   S = K Q^T   row g of A is token pi(g) = g ^ 4 (g & 1) of the 16; thread (g, c) takes the 16-byte chunks c and c + 4 of its rows, word i of
+//               chunk c + 4h is k-step 4h + i (Q's fragments are gathered to match);
+//   O^T = V^T P row g of A holds d = 16 g + 2 j (+ 1 in row g + 8) of MMA j; thread (g, c) takes chunk g of tokens 2c, (2c+1)^4 and
+//               these + 8 (the columns that P's transposed fragment has), and interleaves their bytes in registers.
+// Q enters as f16 under a power of two per head (bf16 has fewer bits than f16: exact except where an element is 2^-29 of the head's largest);
+// the scale of a block multiplies its logits.  Probabilities are formed against the running maximum times 2^12 and split into an f16
+// hi + lo pair (22 bits); the block's V scale enters through its ratio to the largest one so far, so that accumulators of different blocks share one
+// unit (vr): a growing vr rescales them exactly as a growing maximum does.
+#include <math.h>
+
+#include <atomic>
+
+#include "q8.cuh"
+
+namespace catekv {
+
+constexpr int kQ8Warps = 4;
+constexpr int kQ8DecodeThreads = kQ8Warps * 32;
+constexpr int kQ8Stages = 3;
+constexpr int kQ8Unit = 32;                              // rows of codes in a unit
+constexpr int kQ8TailUnit = 16;                          // rows of a tail in a unit
+constexpr int kQ8UnitBytes = 2 * kQ8Unit * kQ8RowBytes;  // K, then V
+static_assert(kQ8UnitBytes == 2 * kQ8TailUnit * kRowBytes, "both kinds of unit fill a stage");
+constexpr int kQ8MergeRegs = 36;  // 32 accumulators + m0, m1, l0, l1
+constexpr int kQ8MergeSlotBytes = kQ8MergeRegs * 32 * 4;
+constexpr int kQ8DecodeSmem = kQ8Warps * kQ8Stages * kQ8UnitBytes + 2 * kQ8MergeSlotBytes;
+constexpr int32_t kQ8PlanTile = kQ8Unit;   // marks a plan of this kind (decode.cu's have kTile)
+constexpr int kQ8SegEndCharge = 256;       // rows
+constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12
+constexpr float kQ8TailFloor = 7.8886090522101181e-31f;  // 2^-100
+static_assert(kQ8PlanTile != kTile, "the two kinds of plan must differ");
+
+struct Q8DecodeArgs {
+  const uint8_t* k_pool;
+  const uint8_t* v_pool;
+  const float* k_scale;
+  const float* v_scale;
+  const uint8_t* k_tail;
+  const uint8_t* v_tail;
+  const int32_t* seg_len;
+  const uint16_t* q;  // [B, Hq, d]
+  int32_t Hq, Hkv, G;
+  float scale_log2;  // sm_scale * log2(e)
+  const CtaHeader* ctas;
+  const WorkItem* items;
+  float* part_o;
+  float* part_lse;
+  void* out;
+  int32_t out_fp32;
+  float* lse_out;
+};
+
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// 4-byte global->shared copy
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src));
+}
+
+// A piece of a segment as a warp sees it: `full` units of codes starting at pool block blk0 (of which the first `live` are to be attended to: the
+// others were complete when the plan was built but no longer are), then the units of the tail.
+struct Q8Cursor {
+  int seg, slot, np, full, live, tail, units;
+  int64_t blk0;
+};
+__device__ __forceinline__ Q8Cursor q8_plan_cursor(const WorkItem& w) {
+  Q8Cursor c;
+  c.seg = w.seg;
+  c.slot = w.slot;
+  c.blk0 = w.row_base / kQ8Block;
+  c.np = (w.t1 / kQ8Block - w.t0 / kQ8Block) * (kQ8Block / kQ8Unit);  // t0 is a multiple of the block, and so is t1 of an inner piece
+  c.full = c.np;
+  c.live = c.np;
+  c.tail = 0;
+  c.units = c.np;
+  return c;
+}
+__device__ __forceinline__ void q8_live_cursor(const WorkItem& w, int len, Q8Cursor& c) {
+  int end = len / kQ8Block;
+  if (!w.last) end = min(end, w.t1 / kQ8Block);
+  c.live = max(0, end - w.t0 / kQ8Block) * (kQ8Block / kQ8Unit);
+  c.full = max(c.np, c.live);
+  c.tail = w.last ? len % kQ8Block : 0;
+  c.units = c.full + (c.tail + kQ8TailUnit - 1) / kQ8TailUnit;
+}
+__device__ __forceinline__ WorkItem q8_load_item(const WorkItem* p) {
+  const int4 x = __ldg(reinterpret_cast<const int4*>(p)), y = __ldg(reinterpret_cast<const int4*>(p) + 1);
+  WorkItem w;
+  w.seg = x.x; w.t0 = x.y; w.t1 = x.z; w.slot = x.w;
+  w.row_base = (int64_t)(((uint64_t)(uint32_t)y.y << 32) | (uint32_t)y.x);
+  w.last = y.z; w.cap = y.w;
+  return w;
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(const Q8DecodeArgs a) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ float s_scale[kQ8Warps][kQ8Stages][2];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = lane >> 2, c = lane & 3;
+  const int pi = g ^ ((g & 1) << 2);  // token of row g
+  pdl_launch_dependents();
+  int item_begin, item_end;
+  WorkItem w0;
+  {
+    // the plan was uploaded by a copy that precedes the previous kernel: it may be read before the wait
+    const int4* hp = reinterpret_cast<const int4*>(a.ctas + blockIdx.x);
+    const int4 h0 = __ldg(hp);
+    item_begin = h0.x;
+    item_end = h0.y;
+    if (item_begin >= item_end) return;
+    w0 = q8_load_item(reinterpret_cast<const WorkItem*>(hp + 1));
+  }
+  const uint32_t ring = smem_u32(smem) + warp * (kQ8Stages * kQ8UnitBytes);
+  const uint32_t ring_scale = smem_u32(&s_scale[warp][0][0]);
+  float* merge = reinterpret_cast<float*>(smem + kQ8Warps * kQ8Stages * kQ8UnitBytes);
+
+  // ---- producer side of the warp: units warp, warp + 4, ... of every item, in order
+  Q8Cursor pc = q8_plan_cursor(w0);
+  int p_item = item_begin, p_u = warp, p_seq = 0;
+  auto issue_unit = [&]() {
+    const int stage = p_seq % kQ8Stages;
+    const uint32_t sb = ring + stage * kQ8UnitBytes;
+    if (p_u < pc.full) {
+      const int64_t blk = pc.blk0 + (p_u >> 1);
+      const int64_t off = blk * kQ8BlockBytes + (p_u & 1) * (kQ8Unit * kQ8RowBytes) + lane * 16;
+      const uint8_t* kp = a.k_pool + off;
+      const uint8_t* vp = a.v_pool + off;
+      // rows of 128 bytes, chunk j of row r at place j ^ (r & 7)
+      const int r = lane >> 3, j = lane & 7;
+      const uint32_t d0 = sb + r * kQ8RowBytes + ((j ^ r) << 4), d1 = sb + (r + 4) * kQ8RowBytes + ((j ^ (r + 4)) << 4);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        cp_async16(d0 + i * 512, kp + i * 512, 16);
+        cp_async16(d1 + i * 512, kp + i * 512 + 512, 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        cp_async16(d0 + 4096 + i * 512, vp + i * 512, 16);
+        cp_async16(d1 + 4096 + i * 512, vp + i * 512 + 512, 16);
+      }
+      if (lane < 2) cp_async4(ring_scale + (stage * 2 + lane) * 4, (lane ? a.v_scale : a.k_scale) + blk);
+    } else {
+      const int r0 = (p_u - pc.full) * kQ8TailUnit;
+      const int left = pc.tail - r0;
+      const size_t off = ((size_t)pc.seg * kQ8Block + r0) * kRowBytes;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {  // rows of 256 bytes, as tile_off
+        const int r = 2 * i + (lane >> 4), j = lane & 15;
+        const int ok = r < left ? 16 : 0;
+        const size_t o = ok ? off + (size_t)r * kRowBytes + j * 16 : 0;
+        cp_async16(sb + tile_off(r, j), a.k_tail + o, ok);
+        cp_async16(sb + 4096 + tile_off(r, j), a.v_tail + o, ok);
+      }
+    }
+    ++p_seq;
+    p_u += kQ8Warps;
+  };
+  auto skip_done = [&]() {  // on to the next item that has a unit for this warp
+    while (p_item < item_end && p_u >= pc.units) {
+      p_u = warp;
+      if (++p_item < item_end) {
+        const WorkItem w = q8_load_item(a.items + p_item);
+        pc = q8_plan_cursor(w);
+        q8_live_cursor(w, *reinterpret_cast<const volatile int32_t*>(a.seg_len + w.seg), pc);
+      }
+    }
+  };
+  auto issue = [&]() {  // one unit, if any is left, = one commit group
+    if (p_item < item_end) {
+      issue_unit();
+      skip_done();
+    }
+    cp_async_commit();
+  };
+
+  // Blocks that were complete when the plan was built are older than anything the previous kernel of the stream may still be writing (an
+  // append writes behind them): the first units are requested before the wait.
+  int pre = 0;
+  for (; pre < kQ8Stages - 1 && p_u < pc.np; ++pre) {
+    issue_unit();
+    cp_async_commit();
+  }
+  pdl_wait();  // from here on: lengths, queries, and rows written by earlier kernels
+  q8_live_cursor(w0, *reinterpret_cast<const volatile int32_t*>(a.seg_len + w0.seg), pc);
+  skip_done();
+  for (; pre < kQ8Stages - 1; ++pre) issue();
+
+  int seq = 0;
+  for (int item = item_begin; item < item_end; ++item) {
+    Q8Cursor cc;
+    {
+      const WorkItem w = item == item_begin ? w0 : q8_load_item(a.items + item);
+      cc = q8_plan_cursor(w);
+      q8_live_cursor(w, *reinterpret_cast<const volatile int32_t*>(a.seg_len + w.seg), cc);
+    }
+    const int b = cc.seg / a.Hkv, h = cc.seg % a.Hkv;
+    // ---- the group's queries as B fragments: k-step 4 hh + i holds d = 16 (c + 4 hh) + 4 i + 0..3 of head g
+    const uint4* qp = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * a.G + (g < a.G ? g : 0)) * kD);
+    uint32_t qf[8][2];
+    float f0, f1;  // logits of heads 2c, 2c + 1 = accumulators times these (times the block's scale)
+    {
+      uint32_t qb[8][2];
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint4 x = g < a.G ? qp[2 * (c + 4 * hh) + e] : make_uint4(0, 0, 0, 0);
+          qb[4 * hh + 2 * e][0] = x.x;
+          qb[4 * hh + 2 * e][1] = x.y;
+          qb[4 * hh + 2 * e + 1][0] = x.z;
+          qb[4 * hh + 2 * e + 1][1] = x.w;
+        }
+      uint32_t mx = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = __vmaxu2(__vmaxu2(mx, qb[i][0] & 0x7fff7fffu), qb[i][1] & 0x7fff7fffu);
+      mx = max(mx & 0xffffu, mx >> 16);
+      mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const int E = max((int)(mx >> 7), 15);  // exponent field of the head's largest |q|: it becomes 2^14 .. 2^15
+      const float up = __int_as_float((268 - E) << 23), down = __int_as_float((E - 14) << 23);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          qf[i][r] = pack_f16(__uint_as_float(qb[i][r] << 16) * up, __uint_as_float(qb[i][r] & 0xffff0000u) * up);
+      f0 = __shfl_sync(0xffffffffu, down, 8 * c) * a.scale_log2;
+      f1 = __shfl_sync(0xffffffffu, down, 8 * c + 4) * a.scale_log2;
+    }
+    float o[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float vr = 0.f;  // largest V scale so far: the accumulators' unit
+    // new maxima and V scale: what the accumulators are multiplied with
+    auto rescale = [&](float mx0, float mx1, float vs) {
+#pragma unroll
+      for (int sh = 4; sh <= 16; sh <<= 1) {
+        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, sh));
+        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, sh));
+      }
+      const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
+      const bool grown = vs > vr;
+      if (__any_sync(0xffffffffu, mn0 > m0 || mn1 > m1 || grown)) {
+        float al0 = fast_exp2(m0 - mn0), al1 = fast_exp2(m1 - mn1);  // exp2(-inf) = 0 on the first unit
+        l0 *= al0;
+        l1 *= al1;
+        if (grown) {
+          const float rv = __fdiv_rn(vr, vs);
+          al0 *= rv;
+          al1 *= rv;
+          vr = vs;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          o[i][0] *= al0;
+          o[i][1] *= al1;
+          o[i][2] *= al0;
+          o[i][3] *= al1;
+        }
+        m0 = mn0;
+        m1 = mn1;
+      }
+    };
+
+    for (int u = warp; u < cc.units; u += kQ8Warps, ++seq) {
+      cp_async_wait<kQ8Stages - 2>();
+      __syncwarp();
+      issue();  // into the stage that the previous unit has left
+      const int stage = seq % kQ8Stages;
+      const uint32_t kb = ring + stage * kQ8UnitBytes, vb = kb + 4096;
+      if (u < cc.full) {
+        if (u >= cc.live) continue;
+        const float ks = s_scale[warp][stage][0], vs = s_scale[warp][stage][1];
+        // ---- S[32 tokens x 8 heads] = K Q^T
+        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const uint32_t ra = kb + (16 * t + pi) * kQ8RowBytes + (((c + 4 * hh) ^ (pi & 7)) << 4);
+            const uint4 lo = lds128(ra), hi = lds128(ra + 8 * kQ8RowBytes);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t a0, a1, a2, a3;
+              q8_to_f16<kType>(word(lo, i), a0, a2);
+              q8_to_f16<kType>(word(hi, i), a1, a3);
+              mma_f16_16816(s[t], a0, a1, a2, a3, qf[4 * hh + i][0], qf[4 * hh + i][1]);
+            }
+          }
+        // s[t][0], s[t][1]: token 16 t + pi(g), heads 2c, 2c + 1;  s[t][2], s[t][3]: that token + 8
+        const float k0 = f0 * ks, k1 = f1 * ks;
+        float x[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          x[t][0] = s[t][0] * k0;
+          x[t][1] = s[t][1] * k1;
+          x[t][2] = s[t][2] * k0;
+          x[t][3] = s[t][3] * k1;
+        }
+        rescale(fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3])), vs);
+        const float ratio = vr > 0.f ? __fdiv_rn(vs, vr) : vs;  // (vs is 0 or NaN where vr is 0)
+        const float r0 = kQ8PBits - m0, r1 = kQ8PBits - m1;
+        uint32_t bh[2][2], bl[2][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float p0 = fast_exp2(x[t][2 * e] + r0), p1 = fast_exp2(x[t][2 * e + 1] + r1);
+            l0 += p0;
+            l1 += p1;
+            const float w0p = p0 * ratio, w1p = p1 * ratio;
+            const uint32_t hi = pack_f16(w0p, w1p);
+            const float2 hf = unpack_f16(hi);
+            bh[t][e] = movmatrix_trans(hi);
+            bl[t][e] = movmatrix_trans(pack_f16(w0p - hf.x, w1p - hf.y));
+          }
+        // ---- O^T[128 d x 8 heads] += V^T P
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int t0 = 16 * t + 2 * c, t1 = 16 * t + ((2 * c + 1) ^ 4);
+          const uint32_t ra = vb + t0 * kQ8RowBytes + ((g ^ (t0 & 7)) << 4), rb = vb + t1 * kQ8RowBytes + ((g ^ (t1 & 7)) << 4);
+          const uint4 v0 = lds128(ra), v1 = lds128(rb), v2 = lds128(ra + 8 * kQ8RowBytes), v3 = lds128(rb + 8 * kQ8RowBytes);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t x0, x1, x2, x3, y0, y1, y2, y3;  // d = 16 g + 4 i + 0..3: tokens (t0, t1), tokens (t0 + 8, t1 + 8)
+            q8_to_f16<kType>(__byte_perm(word(v0, i), word(v1, i), 0x5140), x0, x1);
+            q8_to_f16<kType>(__byte_perm(word(v0, i), word(v1, i), 0x7362), x2, x3);
+            q8_to_f16<kType>(__byte_perm(word(v2, i), word(v3, i), 0x5140), y0, y1);
+            q8_to_f16<kType>(__byte_perm(word(v2, i), word(v3, i), 0x7362), y2, y3);
+            mma_f16_16816(o[2 * i], x0, x1, y0, y1, bh[t][0], bh[t][1]);
+            mma_f16_16816(o[2 * i], x0, x1, y0, y1, bl[t][0], bl[t][1]);
+            mma_f16_16816(o[2 * i + 1], x2, x3, y2, y3, bh[t][0], bh[t][1]);
+            mma_f16_16816(o[2 * i + 1], x2, x3, y2, y3, bl[t][0], bl[t][1]);
+          }
+        }
+      } else {
+        // ---- 16 rows of the tail: bf16 on both sides, the same fragment slots
+        const int left = cc.tail - (u - cc.full) * kQ8TailUnit;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int ch = 2 * (c + 4 * hh) + e;
+            const uint4 q4 = g < a.G ? qp[ch] : make_uint4(0, 0, 0, 0);
+            const uint4 lo = lds128(kb + tile_off(pi, ch)), hi = lds128(kb + tile_off(pi + 8, ch));
+            const uint32_t f[2][4] = {{lo.x, hi.x, lo.y, hi.y}, {lo.z, hi.z, lo.w, hi.w}};
+            mma_bf16_16816(s, f[0], q4.x, q4.y);
+            mma_bf16_16816(s, f[1], q4.z, q4.w);
+          }
+        const bool v_lo = pi < left, v_hi = pi + 8 < left;
+        const float x0 = v_lo ? s[0] * a.scale_log2 : -INFINITY, x1 = v_lo ? s[1] * a.scale_log2 : -INFINITY;
+        const float x2 = v_hi ? s[2] * a.scale_log2 : -INFINITY, x3 = v_hi ? s[3] * a.scale_log2 : -INFINITY;
+        // The tail's V has no scale: a 448th of its largest magnitude stands in for one, so that the units of blocks and tail agree whatever the
+        // magnitudes.  (The floor keeps 2^12 / vr finite.)
+        const int t0 = 2 * c, t1 = (2 * c + 1) ^ 4;
+        uint4 v[2][4];
+        uint32_t vm = 0;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int ch = 2 * g + e;
+          v[e][0] = lds128(vb + tile_off(t0, ch));
+          v[e][1] = lds128(vb + tile_off(t1, ch));
+          v[e][2] = lds128(vb + tile_off(t0 + 8, ch));
+          v[e][3] = lds128(vb + tile_off(t1 + 8, ch));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vm = __vmaxu2(vm, word(v[e][i], j) & 0x7fff7fffu);
+        }
+        vm = __reduce_max_sync(0xffffffffu, max(vm & 0xffffu, vm >> 16));
+        rescale(fmaxf(x0, x2), fmaxf(x1, x3), fmaxf(__uint_as_float(vm << 16) * (1.f / 448.f), kQ8TailFloor));
+        const float r0 = kQ8PBits - m0, r1 = kQ8PBits - m1, ratio = __fdiv_rn(1.f, vr);
+        const float p0 = fast_exp2(x0 + r0), p1 = fast_exp2(x1 + r1), p2 = fast_exp2(x2 + r0), p3 = fast_exp2(x3 + r1);
+        l0 += p0 + p2;
+        l1 += p1 + p3;
+        const float w0p = p0 * ratio, w1p = p1 * ratio, w2p = p2 * ratio, w3p = p3 * ratio;
+        const float h0 = bf16_round(w0p), h1 = bf16_round(w1p), h2 = bf16_round(w2p), h3 = bf16_round(w3p);
+        const uint32_t bh0 = movmatrix_trans(pack_bf16(h0, h1)), bh1 = movmatrix_trans(pack_bf16(h2, h3));
+        const uint32_t bl0 = movmatrix_trans(pack_bf16(w0p - h0, w1p - h1)), bl1 = movmatrix_trans(pack_bf16(w2p - h2, w3p - h3));
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {  // d = 16 g + 8 e + 2 i + 0, 1
+            const uint32_t af[4] = {__byte_perm(word(v[e][0], i), word(v[e][1], i), 0x5410), __byte_perm(word(v[e][0], i), word(v[e][1], i), 0x7632),
+                                    __byte_perm(word(v[e][2], i), word(v[e][3], i), 0x5410), __byte_perm(word(v[e][2], i), word(v[e][3], i), 0x7632)};
+            mma_bf16_16816(o[4 * e + i], af, bh0, bh1);
+            mma_bf16_16816(o[4 * e + i], af, bl0, bl1);
+          }
+        }
+      }
+    }
+
+    // ---- end of the piece: finish the row sums, put the accumulators in units of 1, merge the four warps, write the result
+#pragma unroll
+    for (int sh = 4; sh <= 16; sh <<= 1) {
+      l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
+      l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] *= vr;
+#pragma unroll
+    for (int lvl = 0; lvl < 2; ++lvl) {
+      const int stride = 1 << lvl;
+      const bool writer = (warp & (2 * stride - 1)) == stride;  // level 0: warps 1, 3; level 1: warp 2
+      const bool reader = (warp & (2 * stride - 1)) == 0;       // level 0: warps 0, 2; level 1: warp 0
+      float* mb = merge + (warp >> (lvl + 1)) * (kQ8MergeRegs * 32);
+      if (writer) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mb[(i * 4 + j) * 32 + lane] = o[i][j];
+        mb[32 * 32 + lane] = m0;
+        mb[33 * 32 + lane] = m1;
+        mb[34 * 32 + lane] = l0;
+        mb[35 * 32 + lane] = l1;
+      }
+      __syncthreads();
+      if (reader) {
+        const float om0 = mb[32 * 32 + lane], om1 = mb[33 * 32 + lane];
+        const float ol0 = mb[34 * 32 + lane], ol1 = mb[35 * 32 + lane];
+        const float mn0 = fmaxf(m0, om0), mn1 = fmaxf(m1, om1);
+        const float a0 = (m0 == -INFINITY) ? 0.f : fast_exp2(m0 - mn0);
+        const float b0 = (om0 == -INFINITY) ? 0.f : fast_exp2(om0 - mn0);
+        const float a1 = (m1 == -INFINITY) ? 0.f : fast_exp2(m1 - mn1);
+        const float b1 = (om1 == -INFINITY) ? 0.f : fast_exp2(om1 - mn1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          o[i][0] = o[i][0] * a0 + mb[(i * 4 + 0) * 32 + lane] * b0;
+          o[i][1] = o[i][1] * a1 + mb[(i * 4 + 1) * 32 + lane] * b1;
+          o[i][2] = o[i][2] * a0 + mb[(i * 4 + 2) * 32 + lane] * b0;
+          o[i][3] = o[i][3] * a1 + mb[(i * 4 + 3) * 32 + lane] * b1;
+        }
+        l0 = l0 * a0 + ol0 * b0;
+        l1 = l1 * a1 + ol1 * b1;
+        m0 = mn0;
+        m1 = mn1;
+      }
+      __syncthreads();  // slot 0 is rewritten: by warp 2 at the next level, by warp 1 at the next piece
+    }
+    if (warp == 0) {
+      // o[j][0], o[j][2]: d = 16 g + 2 j, + 1 of head 2c;  o[j][1], o[j][3]: of head 2c + 1
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int hd = 2 * c + e;
+        if (hd >= a.G) continue;
+        const float l = e ? l1 : l0, m = e ? m1 : m0;
+        const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
+        const float lse = l == 0.f ? -INFINITY : m - kQ8PBits + log2f(l);
+        float* po = cc.slot >= 0 ? a.part_o + ((size_t)cc.slot * kMaxG + hd) * kD + 16 * g
+                                 : reinterpret_cast<float*>(a.out) + (((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD + 16 * g);
+        if (cc.slot >= 0 || a.out_fp32) {
+#pragma unroll
+          for (int j = 0; j < 8; j += 2)
+            reinterpret_cast<float4*>(po)[j / 2] = make_float4(o[j][e] * inv, o[j][2 + e] * inv, o[j + 1][e] * inv, o[j + 1][2 + e] * inv);
+        } else {
+          uint4* pb = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.out) + (((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD + 16 * g));
+#pragma unroll
+          for (int j = 0; j < 8; j += 4)
+            pb[j / 4] = make_uint4(pack_bf16(o[j][e] * inv, o[j][2 + e] * inv), pack_bf16(o[j + 1][e] * inv, o[j + 1][2 + e] * inv),
+                                   pack_bf16(o[j + 2][e] * inv, o[j + 2][2 + e] * inv), pack_bf16(o[j + 3][e] * inv, o[j + 3][2 + e] * inv));
+        }
+        if (g == 0) {
+          // the combine pass takes an infinite LSE as the one partial that counts: a NaN (from a block with the scale NaN) reaches the output
+          if (cc.slot >= 0) a.part_lse[(size_t)cc.slot * kMaxG + hd] = lse == lse ? lse : INFINITY;
+          else if (a.lse_out) a.lse_out[(size_t)b * a.Hq + h * a.G + hd] = lse * 0.6931471805599453f;
+        }
+      }
+    }
+  }
+  cp_async_wait<0>();
+}
+
+}  // namespace catekv
+
+using namespace catekv;
+
+extern "C" int catekv_q8_decode_num_ctas(void) {
+  int dev = 0, sms = 0, per_sm = 0;
+  CATEKV_CUDA_TRY(cudaGetDevice(&dev));
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(q8_decode_partial_kernel<CATEKV_Q8_E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ8DecodeSmem));
+  CATEKV_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  CATEKV_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, q8_decode_partial_kernel<CATEKV_Q8_E4M3>, kQ8DecodeThreads, kQ8DecodeSmem));
+  return sms * (per_sm < 1 ? 1 : per_sm);
+}
+
+extern "C" int catekv_q8_decode_plan(const catekv_q8_cache* cache, int32_t num_ctas, void* plan_host, void* plan_dev,
+                                     size_t plan_bytes, catekv_stream stream) {
+  CATEKV_API_RANGE();
+  int rc = check_q8_cache(cache);
+  if (rc) return rc;
+  const int n_segs = cache->B * cache->Hkv;
+  for (int s = 0; s < n_segs; ++s)
+    if (cache->seg_len[s] < 0 || cache->seg_len[s] > cache->seg_cap[s]) return CATEKV_ERR_INVALID_ARG;
+  const PlanSource src = {n_segs, cache->seg_len, cache->seg_off, cache->seg_cap};
+  return build_plan(src, num_ctas, kQ8PlanTile, kQ8Block, kQ8SegEndCharge, plan_host, plan_dev, plan_bytes, (cudaStream_t)stream);
+}
+
+extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
+                                     int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
+                                     size_t plan_bytes, void* ws, size_t ws_bytes, catekv_stream stream) {
+  CATEKV_API_RANGE();
+  int rc = check_q8_cache(cache);
+  if (rc) return rc;
+  if (!q || !out || !plan_host || !plan_dev || !ws) return CATEKV_ERR_INVALID_ARG;
+  if (Hq <= 0 || Hq % cache->Hkv != 0) return CATEKV_ERR_INVALID_ARG;
+  const int G = Hq / cache->Hkv;
+  if (G > kMaxG) return CATEKV_ERR_UNSUPPORTED;
+  if (out_dtype != CATEKV_OUT_BF16 && out_dtype != CATEKV_OUT_FP32) return CATEKV_ERR_UNSUPPORTED;
+  if (!(sm_scale >= 0.f) || isinf(sm_scale)) return CATEKV_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)ws) & 15) return CATEKV_ERR_INVALID_ARG;
+  const PlanHeader* hdr = (const PlanHeader*)plan_host;
+  const int n_segs = cache->B * cache->Hkv;
+  if (plan_bytes < sizeof(PlanHeader) || hdr->magic != kPlanMagic || hdr->n_segs != n_segs || hdr->num_ctas <= 0 ||
+      hdr->tile != kQ8PlanTile)
+    return CATEKV_ERR_INVALID_ARG;
+  const PlanLayout L = plan_layout(n_segs, hdr->num_ctas);
+  if (plan_bytes < L.bytes) return CATEKV_ERR_WORKSPACE;
+  size_t off_lse = 0;
+  if (ws_bytes < ws_layout(n_segs, hdr->num_ctas, &off_lse)) return CATEKV_ERR_WORKSPACE;
+  cudaStream_t st = (cudaStream_t)stream;
+  const uint8_t* pd = (const uint8_t*)plan_dev;
+  static std::atomic<bool> attr_set[64];
+  int dev = 0;
+  CATEKV_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(q8_decode_partial_kernel<CATEKV_Q8_E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ8DecodeSmem));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(q8_decode_partial_kernel<CATEKV_Q8_INT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ8DecodeSmem));
+    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+  }
+  Q8DecodeArgs a;
+  a.k_pool = (const uint8_t*)cache->k_pool;
+  a.v_pool = (const uint8_t*)cache->v_pool;
+  a.k_scale = cache->k_scale;
+  a.v_scale = cache->v_scale;
+  a.k_tail = (const uint8_t*)cache->k_tail;
+  a.v_tail = (const uint8_t*)cache->v_tail;
+  a.seg_len = cache->seg_len_dev;
+  a.q = (const uint16_t*)q;
+  a.Hq = Hq;
+  a.Hkv = cache->Hkv;
+  a.G = G;
+  a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)kD) : sm_scale) * 1.4426950408889634f;
+  a.ctas = (const CtaHeader*)(pd + L.off_cta);
+  a.items = (const WorkItem*)(pd + L.off_items);
+  a.part_o = (float*)ws;
+  a.part_lse = (float*)((uint8_t*)ws + off_lse);
+  a.out = out;
+  a.out_fp32 = out_dtype == CATEKV_OUT_FP32;
+  a.lse_out = lse_out;
+  if (cache->dtype == CATEKV_Q8_E4M3)
+    CATEKV_CUDA_TRY(launch_pdl(q8_decode_partial_kernel<CATEKV_Q8_E4M3>, dim3(hdr->num_ctas), dim3(kQ8DecodeThreads), kQ8DecodeSmem, st, a));
+  else
+    CATEKV_CUDA_TRY(launch_pdl(q8_decode_partial_kernel<CATEKV_Q8_INT8>, dim3(hdr->num_ctas), dim3(kQ8DecodeThreads), kQ8DecodeSmem, st, a));
+  if (hdr->n_slots > 0) {
+    CombineArgs ca;
+    ca.seg_info = (const SegInfo*)(pd + L.off_seg);
+    ca.part_o = a.part_o;
+    ca.part_lse = a.part_lse;
+    ca.out = out;
+    ca.lse_out = lse_out;
+    ca.Hq = Hq;
+    ca.Hkv = cache->Hkv;
+    ca.G = G;
+    ca.out_fp32 = a.out_fp32;
+    return launch_combine(ca, n_segs, st);
+  }
+  return CATEKV_OK;
+}
