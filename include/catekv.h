@@ -13,6 +13,8 @@
  *   catekv_decode_attn     Algorithm 1, decoding stage: Attention(q, k, v) over the
  *                          per-head lists ("all" retrieval on adaptive heads)
  *   catekv_q8_*            the hybrid cache held in 8 bits (quantise, append, decode attention)
+ *   catekv_decode_attn_weighted, catekv_evict
+ *                          attention weight accumulated per cached row, and the lists cut to a budget by it
  *
  * Conventions
  *   - Every function returns 0 (CATEKV_OK) or a negative error code.  Arguments
@@ -116,7 +118,7 @@ typedef struct catekv_cache {
 
 /*
  * Device status block.  The first CATEKV_STATUS_BYTES of every workspace handed to catekv_select_compact,
- * catekv_head_cv, catekv_retrieve_compact and catekv_retrieve_select belong to it.  Kernels never trap or assert:
+ * catekv_head_cv, catekv_retrieve_compact, catekv_retrieve_select and catekv_evict belong to it.  Kernels never trap or assert:
  * a kernel that cannot do its work records why here and returns, and the context stays usable.
  *   CATEKV_STATUS_WAIT_EXPIRED  a bounded wait of the tensor-core scoring kernel ran out (the CTA freed its tensor
  *                               memory and left); scores, and everything derived from them, are invalid
@@ -125,7 +127,7 @@ typedef struct catekv_cache {
  *   CATEKV_STATUS_INDEX_RANGE   checked build only (catekv_checked_build): a device-produced row index, page or
  *                               list position was outside its segment; the access was clamped into range
  * kernel / segment / index describe the first failure recorded (kernel: 1 scoring, 2 top-k, 3 gather,
- * 4 attention, 5 retrieval metadata).
+ * 4 attention, 5 retrieval metadata, 6 eviction).
  * catekv_select_compact and catekv_head_cv clear the block when they start.  The retrieval calls never clear it
  * (a replayed CUDA graph accumulates): zero the first CATEKV_STATUS_BYTES of a retrieval workspace once after
  * allocating it, or read it with clear != 0.
@@ -532,6 +534,55 @@ int catekv_append_decode_attn(catekv_cache* cache, const void* k_new, const void
 int catekv_decode_attn_noalloc(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
                                int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
                                size_t plan_bytes, catekv_stream stream);
+
+/* ---------------------------------------------------------------- eviction by accumulated attention weight */
+
+/*
+ * Decoding lets every list grow (catekv_append); these two calls keep count of what each cached row is worth to the
+ * queries that come, and cut a list back to a budget by that count.  (The paper fixes what a consistent head keeps
+ * at the end of prefill; this is the counterpart for what is generated after it.)
+ *
+ * catekv_decode_attn_weighted is catekv_decode_attn (same arguments, outputs and plan) that also updates
+ *   weights    device float [total_rows], one per pool row:  w_r <- decay * w_r + (1/G) sum_g exp(logit_gr - lse_g)
+ * for every row r of every list (the probabilities of one step sum to 1 per list).  decay in [0, 1]; with 0 the old
+ * weights are not read.  Rows behind a list are not touched: zero the array when the cache is filled, and a row starts
+ * at 0 when it is appended.
+ *   ws  at least catekv_decode_weighted_workspace_bytes(...) with the cache's total_rows
+ * CATEKV_ERR_UNSUPPORTED for a cache with overflow pages.
+ */
+size_t catekv_decode_weighted_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_ctas, int64_t total_rows);
+int catekv_decode_attn_weighted(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
+                                int32_t out_dtype, float* lse_out, float* weights, float decay, const void* plan_host,
+                                const void* plan_dev, size_t plan_bytes, void* ws, size_t ws_bytes, catekv_stream stream);
+
+/*
+ * catekv_evict cuts every segment s with evict_mask[s] != 0 and more than max(budget, sink + local) rows to its first
+ * `sink` rows, its last `local` rows and, of those in between, the max(0, budget - sink - local) with the largest weight
+ * (ties: the lowest index; a negative weight counts as 0, a NaN as infinite), in ascending order, each with its
+ * weight.  Other segments keep all rows.
+ *   dst == src (and dst_weights == weights): in place; segments that keep all rows are not touched.  Otherwise dst is a
+ *   second cache with pools of its own, to which every segment is copied, and `src` and `weights` stay as they are.
+ *   dst_weights of the rows behind a list, up to the segment's capacity, become 0 (in place: of the segments cut).
+ *   The device lengths decide; the host mirror dst->seg_len is set by the same rule from src->seg_len, which has to be
+ *   exact (CATEKV_ERR_INVALID_ARG if src->reserved is set).  catekv_evict_lengths: that rule alone, host only (to lay
+ *   out dst).  Launch shapes follow the capacities, so the call may be captured and replayed (the mirror is then the
+ *   captured call's: catekv_cache_sync_lengths).
+ *   A decode plan of dst stays valid for catekv_decode_attn (lists that have shrunk); retrieval metadata of dst has to be
+ *   rebuilt, and catekv_append_decode_attn needs a new plan.
+ *   idx_out  device int32 [B*Hkv, idx_stride] or NULL: the rows kept of each segment
+ *   ws       device scratch of at least catekv_evict_workspace_bytes(B, Hkv, largest seg_cap of src); its first
+ *            CATEKV_STATUS_BYTES are the status block, which this call does not clear (as the retrieval calls):
+ *            CATEKV_STATUS_CAPACITY when a replayed call's list was cut at the capacity of dst.
+ * Errors: CATEKV_ERR_CAPACITY if a kept list does not fit its segment of dst (nothing launched), CATEKV_ERR_UNSUPPORTED
+ * for overflow pages or more than 2048 segments, CATEKV_ERR_INVALID_ARG if src or dst has no seg_cap_dev, if only one
+ * of cache and weights is in place, or if idx_stride is shorter than the longest kept list.
+ */
+size_t catekv_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_cap);
+int catekv_evict_lengths(const catekv_cache* src, const uint8_t* evict_mask, int32_t budget, int32_t sink, int32_t local,
+                         int32_t* lens_out);
+int catekv_evict(const catekv_cache* src, const float* weights, const uint8_t* evict_mask, int32_t budget, int32_t sink,
+                 int32_t local, catekv_cache* dst, float* dst_weights, int32_t* idx_out, int64_t idx_stride, void* ws,
+                 size_t ws_bytes, catekv_stream stream);
 
 /* ---------------------------------------------------------------- the cache in 8 bits */
 

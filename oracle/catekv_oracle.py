@@ -41,6 +41,10 @@ What each function follows
                                       keeps 16 bits): blocks of 64 rows rounded to 8-bit
                                       numbers under one scale, the unfinished block
                                       as it is.
+* group_attention_weights, evict_indices
+                                    : this library's own counterpart, for what is
+                                      generated after prefill, of what the paper keeps
+                                      of a list: rows by accumulated attention weight.
 
 Parity pins: every function above is pinned by tests that do not re-use it
 (pure-Python brute force, closed forms, hand-worked examples, library
@@ -596,3 +600,26 @@ def q8_rows(row_bits: np.ndarray, dtype: int) -> np.ndarray:
         num, s = q8_encode(row_bits[r:r + Q8_BLOCK], dtype)
         out[r:r + Q8_BLOCK] = num * float(s)
     return out
+
+
+# --------------------------------------------------------------------------
+# Eviction by accumulated attention weight
+# --------------------------------------------------------------------------
+def group_attention_weights(q_group: np.ndarray, K: np.ndarray, scale: float) -> np.ndarray:
+    """Mean over the group's query heads [G, d] of softmax(scale q K^T): what one step adds to the weights of a list's rows."""
+    if len(K) == 0:
+        return np.zeros(0)
+    return _row_softmax(scale * (q_group @ K.T)).mean(axis=0)
+
+
+def evict_indices(w: np.ndarray, sink: int, local: int, budget: int) -> np.ndarray:
+    """Rows kept of a list with weights w [n]: all, if the budget or sink + local covers them, else the first `sink`, the last
+    `local` and the budget - sink - local largest in between (ties: lowest index; negative as 0, NaN as infinite), ascending."""
+    n = len(w)
+    if budget >= n or sink + local >= n:
+        return np.arange(n)
+    c = np.array(w[sink:n - local], dtype=np.float64)
+    c = np.where(np.isnan(c), np.inf, np.maximum(c, 0.0))
+    k = max(0, budget - sink - local)
+    best = sorted(range(len(c)), key=lambda i: (-c[i], i))[:k]
+    return np.concatenate([np.arange(sink), np.array(sorted(best), dtype=np.int64) + sink, np.arange(n - local, n)]).astype(np.int64)

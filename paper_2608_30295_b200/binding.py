@@ -133,6 +133,13 @@ def _load():
         "catekv_q8_decode_num_ctas": (C.c_int, []),
         "catekv_q8_decode_plan": (C.c_int, [C.POINTER(Q8CacheStruct), i32, vp, vp, sz, vp]),
         "catekv_q8_decode_attn": (C.c_int, [C.POINTER(Q8CacheStruct), vp, i32, f32, vp, i32, vp, vp, vp, sz, vp, sz, vp]),
+        "catekv_decode_weighted_workspace_bytes": (sz, [i32, i32, i32, i32, i64]),
+        "catekv_decode_attn_weighted": (C.c_int, [C.POINTER(CacheStruct), vp, i32, f32, vp, i32, vp, vp, f32, vp, vp, sz, vp, sz,
+                                                  vp]),
+        "catekv_evict_workspace_bytes": (sz, [i32, i32, i32]),
+        "catekv_evict_lengths": (C.c_int, [C.POINTER(CacheStruct), vp, i32, i32, i32, vp]),
+        "catekv_evict": (C.c_int, [C.POINTER(CacheStruct), vp, vp, i32, i32, i32, C.POINTER(CacheStruct), vp, vp, i64, vp, sz,
+                                   vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -649,3 +656,71 @@ def catekv_q8_decode_attn(cache: Q8Cache, q: torch.Tensor, plan: DecodePlan, out
     assert lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and lse_out.numel() == q.shape[0] * q.shape[1])
     _here("catekv_q8_decode_attn", cache.device, q, out, lse_out, plan.dev)
     _decode_call(_lib.catekv_q8_decode_attn, "catekv_q8_decode_attn", cache, q, plan, out, lse_out, sm_scale)
+
+
+# ---------------------------------------------------------------- eviction by accumulated attention weight
+
+
+def decode_weighted_workspace(cache: Cache, Hq: int, plan: DecodePlan) -> torch.Tensor:
+    """A workspace for catekv_decode_attn_weighted over `cache` with this plan (memory only)."""
+    n = _lib.catekv_decode_weighted_workspace_bytes(cache.B, Hq, cache.Hkv, plan.num_ctas, cache.total_rows)
+    if n == 0:
+        raise CatekvError(ERR_INVALID_ARG, "catekv_decode_weighted_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def catekv_decode_attn_weighted(cache: Cache, q: torch.Tensor, plan: DecodePlan, out: torch.Tensor, weights: torch.Tensor,
+                                decay: float, ws: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
+                                sm_scale: float = 0.0):
+    """catekv_decode_attn that also updates `weights` (float32 [total_rows], one per pool row)."""
+    assert q.is_contiguous() and out.is_contiguous() and q.dtype == torch.bfloat16 and out.shape == q.shape
+    assert weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() >= cache.total_rows
+    assert lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and lse_out.numel() == q.shape[0] * q.shape[1])
+    if out.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("out must be bf16 or fp32")
+    _here("catekv_decode_attn_weighted", cache.device, q, out, weights, ws, lse_out)
+    _check(_lib.catekv_decode_attn_weighted(C.byref(cache.struct), q.data_ptr(), q.shape[1], sm_scale, out.data_ptr(),
+                                            OUT_BF16 if out.dtype == torch.bfloat16 else OUT_FP32, _dev_ptr(lse_out),
+                                            weights.data_ptr(), decay, plan.host.data_ptr(), plan.dev.data_ptr(), plan.bytes,
+                                            ws.data_ptr(), ws.numel(), _stream()), "catekv_decode_attn_weighted")
+
+
+def evict_workspace(cache: Cache) -> torch.Tensor:
+    """A workspace for catekv_evict from `cache` with its status block zeroed (memory only)."""
+    ws = torch.empty(_lib.catekv_evict_workspace_bytes(cache.B, cache.Hkv, int(cache.seg_cap.max())), dtype=torch.uint8,
+                     device=cache.device)
+    ws[:STATUS_BYTES].zero_()
+    return ws
+
+
+def catekv_evict_lengths(cache: Cache, evict_mask, budget: int, sink: int, local: int):
+    """Host only: rows every segment keeps under catekv_evict with these parameters."""
+    evict_mask = np.ascontiguousarray(evict_mask, dtype=np.uint8).reshape(-1)
+    assert evict_mask.size == cache.B * cache.Hkv
+    lens = np.zeros(cache.B * cache.Hkv, dtype=np.int32)
+    _check(_lib.catekv_evict_lengths(C.byref(cache.struct), _np_ptr(evict_mask), budget, sink, local, _np_ptr(lens)),
+           "catekv_evict_lengths")
+    return lens
+
+
+def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, sink: int, local: int,
+                 dst: Optional[Cache] = None, dst_weights: Optional[torch.Tensor] = None,
+                 idx_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Cut the masked segments to `budget` rows by weight, into `dst` and `dst_weights`, or in place without them."""
+    if dst is None:
+        dst, dst_weights = cache, weights
+    evict_mask = np.ascontiguousarray(evict_mask, dtype=np.uint8).reshape(-1)
+    assert evict_mask.size == cache.B * cache.Hkv
+    for w, c in ((weights, cache), (dst_weights, dst)):
+        assert w.dtype == torch.float32 and w.is_contiguous() and w.numel() >= c.total_rows
+    stride = 0
+    if idx_out is not None:
+        assert idx_out.dtype == torch.int32 and idx_out.shape[0] == cache.B * cache.Hkv and idx_out.stride(1) == 1
+        stride = idx_out.stride(0) if idx_out.shape[0] > 1 else idx_out.shape[1]
+    if ws is None:
+        ws = evict_workspace(cache)
+    _here("catekv_evict", cache.device, weights, dst_weights, dst.k_pool, idx_out, ws)
+    _check(_lib.catekv_evict(C.byref(cache.struct), weights.data_ptr(), _np_ptr(evict_mask), budget, sink, local,
+                             C.byref(dst.struct), dst_weights.data_ptr(), _dev_ptr(idx_out), stride, ws.data_ptr(), ws.numel(),
+                             _stream()), "catekv_evict")
+    return ws

@@ -48,6 +48,9 @@ struct DecodeArgs {
   void* out;
   int32_t out_fp32;
   float* lse_out;
+  // with kLogits only: logits [G][logit_stride], log2 domain; logit_stride = the pools' rows
+  float* logits;
+  int64_t logit_stride;
   int32_t n_pages;  // pages of the overflow pools (checked build: bound of a page-table entry)
   int32_t* chk;     // the checked build's status block, else null
 };
@@ -153,7 +156,8 @@ __device__ __forceinline__ void tile_rows(const ItemCursor& c, int i, int& start
   nvalid = c.live - start;
 }
 
-template <int kMode>
+// kLogits: every row's scaled logits are also left in a.logits, for the weights that catekv_decode_attn_weighted accumulates
+template <int kMode, bool kLogits = false>
 __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const DecodeArgs a) {
   constexpr bool kIndexed = kMode == kModeIndexed;
   constexpr bool kPaged = kMode == kModePaged;
@@ -353,6 +357,17 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
       const float x1 = v_lo ? (sa[1] + sb2[1]) * a.scale_log2 : -INFINITY;
       const float x2 = v_hi ? (sa[2] + sb2[2]) * a.scale_log2 : -INFINITY;
       const float x3 = v_hi ? (sa[3] + sb2[3]) * a.scale_log2 : -INFINITY;
+      if (kLogits) {  // head by head: the 8 rows of a store are one 32-byte sector
+        float* lp = a.logits + cc.row_base + (tstart - cc.t0) + row0 + g + (int64_t)(2 * t) * a.logit_stride;
+        if (2 * t < a.G) {
+          if (v_lo) lp[0] = x0;
+          if (v_hi) lp[8] = x2;
+        }
+        if (2 * t + 1 < a.G) {
+          if (v_lo) lp[a.logit_stride] = x1;
+          if (v_hi) lp[a.logit_stride + 8] = x3;
+        }
+      }
       float mx0 = fmaxf(x0, x2), mx1 = fmaxf(x1, x3);
 #pragma unroll
       for (int sh = 4; sh <= 16; sh <<= 1) {
@@ -623,7 +638,7 @@ static int decode_launch(int phases, const catekv_cache* cache, const void* k_ne
                          int32_t Hq, float sm_scale, void* out,
                          int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
                          size_t plan_bytes, void* ws, size_t ws_bytes, catekv_stream stream,
-                         const IndexList* il = nullptr) {
+                         const IndexList* il = nullptr, float* logits = nullptr) {
   int rc = check_cache(cache);
   if (rc) return rc;
   if (!q || !out || !plan_host || !plan_dev || !ws) return CATEKV_ERR_INVALID_ARG;
@@ -655,6 +670,7 @@ static int decode_launch(int phases, const catekv_cache* cache, const void* k_ne
       CATEKV_CUDA_TRY(cudaFuncSetAttribute(decode_partial_kernel<kModePlain>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDecodeSmem));
       CATEKV_CUDA_TRY(cudaFuncSetAttribute(decode_partial_kernel<kModeIndexed>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDecodeSmem));
       CATEKV_CUDA_TRY(cudaFuncSetAttribute(decode_partial_kernel<kModePaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDecodeSmem));
+      CATEKV_CUDA_TRY(cudaFuncSetAttribute(decode_partial_kernel<kModePlain, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDecodeSmem));
       if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
     DecodeArgs a;
@@ -686,7 +702,11 @@ static int decode_launch(int phases, const catekv_cache* cache, const void* k_ne
     a.max_pages = pg.max_pages;
     a.n_pages = cache->pages ? cache->pages->n_pages : 0;
     a.chk = checked_status_ptr();
-    if (il)
+    a.logits = logits;
+    a.logit_stride = cache->total_rows;
+    if (logits)
+      CATEKV_CUDA_TRY(launch_pdl(decode_partial_kernel<kModePlain, true>, dim3(hdr->num_ctas), dim3(kDecodeThreads), kDecodeSmem, st, a));
+    else if (il)
       CATEKV_CUDA_TRY(launch_pdl(decode_partial_kernel<kModeIndexed>, dim3(hdr->num_ctas), dim3(kDecodeThreads), kDecodeSmem, st, a));
     else if (cache->pages)
       CATEKV_CUDA_TRY(launch_pdl(decode_partial_kernel<kModePaged>, dim3(hdr->num_ctas), dim3(kDecodeThreads), kDecodeSmem, st, a));
@@ -728,6 +748,121 @@ extern "C" int catekv_decode_attn_indexed(const catekv_cache* cache, const int32
   const IndexList il = {idx, idx_stride, sel_len};
   return decode_launch(3, cache, nullptr, nullptr, q, Hq, sm_scale, out, out_dtype, lse_out, plan_host, plan_dev, plan_bytes, ws,
                        ws_bytes, stream, &il);
+}
+
+// ------------------------------------------------------------------------------------------
+// Attention that accumulates what every row is worth
+// ------------------------------------------------------------------------------------------
+namespace catekv {
+
+struct WeightArgs {
+  const int32_t* seg_len;
+  const CtaHeader* ctas;
+  const WorkItem* items;
+  const float* logits;  // [G][logit_stride], log2 domain
+  int64_t logit_stride;
+  const float* lse;     // [B, Hq], natural log
+  float* weights;
+  float decay;
+  int32_t Hq, Hkv, G;
+};
+
+// w <- decay w + mean over the group of exp(logit - lse), a thread per row, the rows shared out by the attention's own plan.  A row's logits
+// are G words against the 512 bytes that attention read of it, and as a rule still in L2: the pass is the price of a softmax whose
+// normaliser is known only when the last row has been seen.
+constexpr int kWeightThreads = 256;
+template <int kG>
+__global__ void __launch_bounds__(kWeightThreads) weight_kernel(const WeightArgs a) {
+  pdl_launch_dependents();
+  const int4 h0 = __ldg(reinterpret_cast<const int4*>(a.ctas + blockIdx.x));  // plan data: older than the previous kernel
+  pdl_wait();
+  for (int it = h0.x; it < h0.y; ++it) {
+    const WorkItem w = a.items[it];
+    const int len = a.seg_len[w.seg];
+    const int n = (w.last ? len : min(w.t1, len)) - w.t0;
+    float lse[kG];
+#pragma unroll
+    for (int g = 0; g < kG; ++g)
+      lse[g] = a.lse[(size_t)(w.seg / a.Hkv) * a.Hq + (size_t)(w.seg % a.Hkv) * kG + g] * 1.4426950408889634f;
+    for (int r = threadIdx.x; r < n; r += kWeightThreads) {
+      const float* lp = a.logits + w.row_base + r;
+      float* wp = a.weights + w.row_base + r;
+      float x[kG];
+#pragma unroll
+      for (int g = 0; g < kG; ++g) x[g] = lp[g * a.logit_stride];
+      const float old = a.decay != 0.f ? *wp * a.decay : 0.f;
+      float p = 0.f;
+#pragma unroll
+      for (int g = 0; g < kG; ++g) p += exp2f(x[g] - lse[g]);
+      *wp = old + p * (1.f / kG);
+    }
+  }
+}
+
+struct WeightedWs {
+  size_t off_lse, off_logits, bytes;
+};
+static WeightedWs weighted_ws_layout(int B, int Hq, int Hkv, int num_ctas, int64_t total_rows) {
+  WeightedWs w;
+  size_t o = align_up(ws_layout(B * Hkv, num_ctas, nullptr), 256);
+  w.off_lse = o; o = align_up(o + sizeof(float) * (size_t)B * Hq, 256);
+  w.off_logits = o; o = o + sizeof(float) * (size_t)(Hq / Hkv) * (size_t)total_rows;
+  w.bytes = o;
+  return w;
+}
+
+}  // namespace catekv
+
+extern "C" size_t catekv_decode_weighted_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_ctas, int64_t total_rows) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || num_ctas <= 0 || total_rows < 0) return 0;
+  return weighted_ws_layout(B, Hq, Hkv, num_ctas, total_rows).bytes;
+}
+
+extern "C" int catekv_decode_attn_weighted(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
+                                           int32_t out_dtype, float* lse_out, float* weights, float decay,
+                                           const void* plan_host, const void* plan_dev, size_t plan_bytes, void* ws,
+                                           size_t ws_bytes, catekv_stream stream) {
+  CATEKV_API_RANGE();
+  int rc = check_cache(cache);
+  if (rc) return rc;
+  if (cache->pages) return CATEKV_ERR_UNSUPPORTED;
+  if (!weights || !ws || !plan_host || !plan_dev || !(decay >= 0.f && decay <= 1.f) || Hq <= 0 || Hq % cache->Hkv) return CATEKV_ERR_INVALID_ARG;
+  const PlanHeader* hdr = (const PlanHeader*)plan_host;
+  if (plan_bytes < sizeof(PlanHeader) || hdr->magic != kPlanMagic || hdr->num_ctas <= 0) return CATEKV_ERR_INVALID_ARG;
+  const WeightedWs W = weighted_ws_layout(cache->B, Hq, cache->Hkv, hdr->num_ctas, cache->total_rows);
+  if (ws_bytes < W.bytes) return CATEKV_ERR_WORKSPACE;
+  float* lse = lse_out ? lse_out : (float*)((uint8_t*)ws + W.off_lse);
+  float* logits = (float*)((uint8_t*)ws + W.off_logits);
+  rc = decode_launch(3, cache, nullptr, nullptr, q, Hq, sm_scale, out, out_dtype, lse, plan_host, plan_dev, plan_bytes, ws, ws_bytes,
+                     stream, nullptr, logits);
+  if (rc) return rc;
+  const PlanLayout L = plan_layout(cache->B * cache->Hkv, hdr->num_ctas);
+  const uint8_t* pd = (const uint8_t*)plan_dev;
+  WeightArgs a;
+  a.seg_len = cache->seg_len_dev;
+  a.ctas = (const CtaHeader*)(pd + L.off_cta);
+  a.items = (const WorkItem*)(pd + L.off_items);
+  a.logits = logits;
+  a.logit_stride = cache->total_rows;
+  a.lse = lse;
+  a.weights = weights;
+  a.decay = decay;
+  a.Hq = Hq;
+  a.Hkv = cache->Hkv;
+  a.G = Hq / cache->Hkv;
+  const dim3 grid(hdr->num_ctas), block(kWeightThreads);
+  cudaStream_t st = (cudaStream_t)stream;
+  switch (a.G) {
+    case 1: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<1>, grid, block, 0, st, a)); break;
+    case 2: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<2>, grid, block, 0, st, a)); break;
+    case 3: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<3>, grid, block, 0, st, a)); break;
+    case 4: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<4>, grid, block, 0, st, a)); break;
+    case 5: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<5>, grid, block, 0, st, a)); break;
+    case 6: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<6>, grid, block, 0, st, a)); break;
+    case 7: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<7>, grid, block, 0, st, a)); break;
+    default: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<8>, grid, block, 0, st, a)); break;
+  }
+  return CATEKV_OK;
 }
 
 extern "C" int catekv_decode_partials(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
