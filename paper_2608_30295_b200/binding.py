@@ -156,8 +156,14 @@ def _check(rc: int, where: str):
         raise CatekvError(rc, where)
 
 
+# The current stream's handle without a Stream object around it (3 us a call); torch's own launchers take it this way.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _np_ptr(a: np.ndarray) -> int:
@@ -612,24 +618,23 @@ class Q8Cache:
         self.seg_len_dev.copy_(torch.from_numpy(self.seg_len))
 
 
-def _here(where: str, device, *tensors):
+def _here(where: str, *tensors):
     """The library works on the current device and stream: a buffer that lives elsewhere is refused."""
-    d = torch.device(device)
     here = torch.cuda.current_device()
-    if d.type != "cuda" or (d.index is not None and d.index != here) or any(t is not None and t.device != torch.device("cuda", here)
-                                                                            for t in tensors):
-        raise CatekvError(ERR_INVALID_ARG, where)
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise CatekvError(ERR_INVALID_ARG, where)
 
 
 def catekv_q8_quantize(src: Cache, dst: Q8Cache):
-    _here("catekv_q8_quantize", src.device, src.k_pool, dst.k_pool)
+    _here("catekv_q8_quantize", src.k_pool, dst.k_pool)
     _check(_lib.catekv_q8_quantize(C.byref(src.struct), C.byref(dst.struct), _stream()), "catekv_q8_quantize")
 
 
 def catekv_q8_append(cache: Q8Cache, k_new: torch.Tensor, v_new: torch.Tensor):
     assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.dtype == v_new.dtype == torch.bfloat16
     assert k_new.numel() == v_new.numel() == cache.B * cache.Hkv * cache.d
-    _here("catekv_q8_append", cache.device, k_new, v_new)
+    _here("catekv_q8_append", cache.k_pool, k_new, v_new)
     _check(_lib.catekv_q8_append(C.byref(cache.struct), k_new.data_ptr(), v_new.data_ptr(), _stream()), "catekv_q8_append")
 
 
@@ -654,7 +659,7 @@ def catekv_q8_decode_attn(cache: Q8Cache, q: torch.Tensor, plan: DecodePlan, out
                           lse_out: Optional[torch.Tensor] = None, sm_scale: float = 0.0):
     assert q.shape[0] == cache.B and q.shape[2] == cache.d and out.shape == q.shape
     assert lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and lse_out.numel() == q.shape[0] * q.shape[1])
-    _here("catekv_q8_decode_attn", cache.device, q, out, lse_out, plan.dev)
+    _here("catekv_q8_decode_attn", cache.k_pool, q, out, lse_out, plan.dev)
     _decode_call(_lib.catekv_q8_decode_attn, "catekv_q8_decode_attn", cache, q, plan, out, lse_out, sm_scale)
 
 
@@ -678,7 +683,7 @@ def catekv_decode_attn_weighted(cache: Cache, q: torch.Tensor, plan: DecodePlan,
     assert lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and lse_out.numel() == q.shape[0] * q.shape[1])
     if out.dtype not in (torch.bfloat16, torch.float32):
         raise TypeError("out must be bf16 or fp32")
-    _here("catekv_decode_attn_weighted", cache.device, q, out, weights, ws, lse_out)
+    _here("catekv_decode_attn_weighted", cache.k_pool, plan.dev, q, out, weights, ws, lse_out)
     _check(_lib.catekv_decode_attn_weighted(C.byref(cache.struct), q.data_ptr(), q.shape[1], sm_scale, out.data_ptr(),
                                             OUT_BF16 if out.dtype == torch.bfloat16 else OUT_FP32, _dev_ptr(lse_out),
                                             weights.data_ptr(), decay, plan.host.data_ptr(), plan.dev.data_ptr(), plan.bytes,
@@ -719,7 +724,7 @@ def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, s
         stride = idx_out.stride(0) if idx_out.shape[0] > 1 else idx_out.shape[1]
     if ws is None:
         ws = evict_workspace(cache)
-    _here("catekv_evict", cache.device, weights, dst_weights, dst.k_pool, idx_out, ws)
+    _here("catekv_evict", cache.k_pool, weights, dst_weights, dst.k_pool, idx_out, ws)
     _check(_lib.catekv_evict(C.byref(cache.struct), weights.data_ptr(), _np_ptr(evict_mask), budget, sink, local,
                              C.byref(dst.struct), dst_weights.data_ptr(), _dev_ptr(idx_out), stride, ws.data_ptr(), ws.numel(),
                              _stream()), "catekv_evict")

@@ -1,7 +1,13 @@
-// Eviction by accumulated attention weight: candidates' weights into the top-k's score rows, top-k (select.cu), and the
-// move of what is kept, into another cache or in place.
+// Eviction by accumulated attention weight: the selection of what a list keeps, and the move of it, into another cache or in place.
+#include <math.h>
+
+#include <atomic>
+
+#include <cooperative_groups.h>
+
 #include "decode.cuh"
-#include "select.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace catekv {
 
@@ -13,60 +19,223 @@ struct EvMask {
 struct EvParams {
   int32_t budget, sink, local;
 };
-// Sizes of a segment of n rows; the same on host and device.
-__host__ __device__ inline SelSeg evict_decide(int n, bool masked, const EvParams& p, int seg) {
-  SelSeg s = {};
+struct EvSeg {       // what becomes of a segment
+  int32_t n;         // rows it has
+  int32_t keep_all;
+  int32_t k_sel;     // rows to select among [sink, cand_end)
+  int32_t cand_end;
+  int32_t kept;      // rows it keeps
+  int32_t reserved[3];
+};
+// The same on host and device.
+__host__ __device__ inline EvSeg evict_decide(int n, bool masked, const EvParams& p) {
+  EvSeg s = {};
   s.n = n;
-  s.job = seg;
   if (!masked || p.budget >= n || p.sink + p.local >= n) {
     s.keep_all = 1;
     s.cand_end = n;
-    s.len_ub = n;
+    s.kept = n;
     return s;
   }
   const int rest = p.budget - p.sink - p.local;
   s.cand_end = n - p.local;
-  s.n_pool = s.cand_end - p.sink;
   s.k_sel = rest > 0 ? rest : 0;
-  s.len_ub = p.sink + s.k_sel + p.local;
+  s.kept = p.sink + s.k_sel + p.local;
   return s;
 }
 
-struct EvPrepArgs {
+// ------------------------------------------------------------------------------------------
+// Selection
+// ------------------------------------------------------------------------------------------
+// A cluster of CL CTAs per segment (1 where the list is short), each with a share of the candidates in shared memory as sortable patterns
+// (a non-negative float's bits order like the float).  The pattern of the k-th largest is found from the top, 11 + 11 + 9 bits, with a histogram
+// per step: weights spread over many powers of two, so the first step (exponent and three bits) already leaves a few per cent.  A histogram of its
+// own per step means one cluster barrier per step.  What is above the pattern is kept, of what equals it the first in row order; a
+// warp's votes over 32 consecutive candidates place them, so that the list is written in order and coalesced.
+constexpr int kEvThreads = 1024;
+constexpr int kEvWarps = kEvThreads / 32;
+constexpr int kEvBins = 2048;
+constexpr int kEvClusterFrom = 16384;  // candidates from which a cluster shares a list
+constexpr int kEvStageMax = 49152;  // candidates a CTA may stage (192 KB)
+__device__ __forceinline__ int ev_shift(int pass) { return pass == 0 ? 20 : pass == 1 ? 9 : 0; }
+
+struct EvSelectArgs {
   const int32_t* seg_off;
   const int32_t* seg_len;
   const float* weights;
-  SelSeg* segs;
-  float* P;
-  int64_t p_stride;
+  EvSeg* segs;
+  int32_t* idx;
+  int64_t idx_stride;
+  int32_t* chk;   // the checked build's status block, else null
+  int32_t stage;  // candidates a CTA's shared memory holds (longer shares are read from global memory)
   EvParams p;
   EvMask mask;
 };
 
-// The decision of every segment, and the weights of its candidates as the top-k wants them: non-negative patterns, NaN as infinity.
-constexpr int kEvPrepRows = 2048;
-__global__ void __launch_bounds__(256) evict_prep_kernel(const __grid_constant__ EvPrepArgs a) {
-  const int seg = blockIdx.y;
+__device__ __forceinline__ unsigned int ev_pattern(float x) {  // negative as 0, NaN as infinite
+  return x != x ? 0x7f800000u : (x > 0.f ? __float_as_uint(x) : 0u);
+}
+
+template <int CL>
+__global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_constant__ EvSelectArgs a) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int seg = blockIdx.x / CL;
+  const int rank = CL > 1 ? (int)cluster.block_rank() : 0;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  __shared__ unsigned int hist[3][kEvBins];
+  __shared__ unsigned int s_warp[kEvWarps];
+  __shared__ unsigned int s_gt[kEvWarps], s_eq[kEvWarps];
+  __shared__ unsigned int s_sel[3];
+  __shared__ unsigned int s_tot[2];  // this CTA's counts above and at the threshold, read by its peers
+  extern __shared__ __align__(16) unsigned int key[];
   pdl_launch_dependents();
+  for (int i = tid; i < 3 * kEvBins; i += kEvThreads) (&hist[0][0])[i] = 0u;
   pdl_wait();
-  const SelSeg s = evict_decide(a.seg_len[seg], (a.mask.w[seg >> 5] >> (seg & 31)) & 1u, a.p, seg);
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.segs[seg] = s;
-  if (s.keep_all || s.k_sel == 0) return;
-  const float* w = a.weights + a.seg_off[seg] + a.p.sink;
-  float* P = a.P + (int64_t)seg * a.p_stride;
-  const int c0 = blockIdx.x * kEvPrepRows + threadIdx.x;
+  const EvSeg s = evict_decide(a.seg_len[seg], (a.mask.w[seg >> 5] >> (seg & 31)) & 1u, a.p);
+  if (rank == 0 && tid == 0) a.segs[seg] = s;
+  if (s.keep_all) return;  // the whole cluster
+  auto cluster_sync = [&]() {
+    if (CL > 1) cluster.sync(); else __syncthreads();
+  };
+  int32_t* idx = a.idx + (int64_t)seg * a.idx_stride;
+  const int S = a.p.sink;
+  if (s.k_sel > 0) {
+    const int n_pool = s.cand_end - S;
+    const int per = ((n_pool + CL - 1) / CL + 31) / 32 * 32;
+    const int lo = min(n_pool, rank * per), n_loc = min(n_pool, lo + per) - lo;
+    const float* w = a.weights + (int64_t)a.seg_off[seg] + S + lo;
+    const bool staged = n_loc <= a.stage;
+    auto ld = [&](int i) { return staged ? key[i] : ev_pattern(w[i]); };
+    unsigned int prefix = 0u, pmask = 0u, need = (unsigned int)s.k_sel;
+    __syncthreads();  // the histograms are clear
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = ev_shift(pass);
+      const unsigned int dmask = pass == 2 ? 511u : 2047u;
+      unsigned int* h = hist[pass];
+      auto count = [&](bool in, unsigned int v) {
+        const bool hit = in && (v & pmask) == prefix;
+        const unsigned int d = hit ? (v >> shift) & dmask : 0xffffffffu;
+        int same;
+        __match_all_sync(0xffffffffu, d, &same);
+        if (same) {  // equal weights by the warp (rows that no query has looked at): one addition
+          if (hit && lane == 0) atomicAdd(&h[d], 32u);
+        } else if (hit) {
+          atomicAdd(&h[d], 1u);
+        }
+      };
+      if (pass == 0) {  // the first step brings the candidates in, four loads in flight
+        for (int i0 = 0; i0 < n_loc; i0 += 4 * kEvThreads) {
+          unsigned int v[4];
 #pragma unroll
-  for (int i = 0; i < kEvPrepRows / 256; ++i) {
-    const int c = c0 + i * 256;
-    if (c < s.n_pool) {
-      const float x = w[c];
-      P[c] = x != x ? INFINITY : (x > 0.f ? x : 0.f);
+          for (int e = 0; e < 4; ++e) {
+            const int i = i0 + e * kEvThreads + tid;
+            v[e] = i < n_loc ? ev_pattern(w[i]) : 0u;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = i0 + e * kEvThreads + tid;
+            if (staged && i < n_loc) key[i] = v[e];
+            count(i < n_loc, v[e]);
+          }
+        }
+      } else {
+        for (int i0 = 0; i0 < n_loc; i0 += kEvThreads) count(i0 + tid < n_loc, i0 + tid < n_loc ? ld(i0 + tid) : 0u);
+      }
+      cluster_sync();  // all histograms of this step complete
+      // thread t: bins 2047 - 2t and 2046 - 2t, larger digits first
+      unsigned int c1 = 0u, c0 = 0u;
+      const int b1 = kEvBins - 1 - 2 * tid;
+#pragma unroll
+      for (int r = 0; r < CL; ++r) {
+        const uint2 x = *reinterpret_cast<const uint2*>(CL > 1 ? cluster.map_shared_rank(&h[b1 - 1], r) : &h[b1 - 1]);
+        c0 += x.x;
+        c1 += x.y;
+      }
+      unsigned int inc = c0 + c1;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (lane == 31) s_warp[warp] = inc;
+      __syncthreads();
+      inc += __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0u);
+      const unsigned int before = inc - c0 - c1;
+      if (before < need && need <= inc) {  // one of this thread's bins holds the need-th largest
+        const bool upper = need <= before + c1;
+        s_sel[0] = (unsigned int)(upper ? b1 : b1 - 1);
+        s_sel[1] = need - before - (upper ? 0u : c1);
+        s_sel[2] = upper ? c1 : c0;
+      }
+      __syncthreads();
+      prefix |= s_sel[0] << shift;
+      pmask |= dmask << shift;
+      need = s_sel[1];
+      const bool whole = s_sel[2] == need;
+      __syncthreads();  // s_sel and s_warp are written again by the next step
+      if (whole) break;  // everything in the bin is kept: no need to look closer
     }
+    // kept: patterns above the prefix, and the first `need` of those with it
+    const unsigned int top = prefix | (~pmask & 0x7fffffffu);  // (patterns are below 2^31)
+    const int chunk = (n_loc + kEvThreads - 1) / kEvThreads * 32;  // a warp's consecutive candidates
+    const int w0 = min(n_loc, warp * chunk), w1 = min(n_loc, w0 + chunk);
+    unsigned int gt = 0u, eq = 0u;
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+      const bool in = i0 + lane < w1;
+      const unsigned int v = in ? ld(i0 + lane) : 0u;
+      gt += __popc(__ballot_sync(0xffffffffu, in && v > top));
+      eq += __popc(__ballot_sync(0xffffffffu, in && (v & pmask) == prefix));
+    }
+    if (lane == 0) {
+      s_gt[warp] = gt;
+      s_eq[warp] = eq;
+    }
+    __syncthreads();
+    const unsigned int all_gt = __reduce_add_sync(0xffffffffu, s_gt[lane]), all_eq = __reduce_add_sync(0xffffffffu, s_eq[lane]);
+    unsigned int gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_gt[lane] : 0u);
+    unsigned int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_eq[lane] : 0u);
+    if (CL > 1) {
+      if (tid == 0) {
+        s_tot[0] = all_gt;
+        s_tot[1] = all_eq;
+      }
+      cluster_sync();
+      for (int r = 0; r < rank; ++r) {
+        const unsigned int* t = cluster.map_shared_rank(&s_tot[0], r);
+        gt_before += t[0];
+        eq_before += t[1];
+      }
+    }
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+      const bool in = i0 + lane < w1;
+      const unsigned int v = in ? ld(i0 + lane) : 0u;
+      const bool g = in && v > top, q = in && (v & pmask) == prefix;
+      const unsigned int mg = __ballot_sync(0xffffffffu, g), mq = __ballot_sync(0xffffffffu, q);
+      const unsigned int low = (1u << lane) - 1u;
+      const unsigned int my_eq = eq_before + __popc(mq & low);
+      if (g || (q && my_eq < need)) {
+        int r = S + (int)(gt_before + __popc(mg & low) + min(my_eq, need));
+#ifdef CATEKV_CHECKED
+        r = checked_clamp(r, S, s.kept - a.p.local - 1, a.chk, kKidEvict, seg);
+#endif
+        idx[r] = S + lo + i0 + lane;
+      }
+      gt_before += __popc(mg);
+      eq_before += __popc(mq);
+    }
+    cluster_sync();  // no CTA leaves while a peer may still read its shared memory
+  }
+  if (rank == 0) {
+    for (int i = tid; i < S; i += kEvThreads) idx[i] = i;
+    for (int i = tid; i < a.p.local; i += kEvThreads) idx[S + s.k_sel + i] = s.cand_end + i;
   }
 }
 
+// ------------------------------------------------------------------------------------------
+// Move
+// ------------------------------------------------------------------------------------------
 struct EvMoveArgs {
-  const SelSeg* segs;
+  const EvSeg* segs;
   const int32_t* idx;
   int64_t idx_stride;
   const uint8_t* k_src;
@@ -81,11 +250,12 @@ struct EvMoveArgs {
   float* w_dst;
   int32_t* idx_out;
   int64_t idx_out_stride;
+  int32_t rows_per_cta;
   int32_t* status;
   int32_t* chk;
 };
 
-__device__ __forceinline__ int kept_row(const EvMoveArgs& a, const SelSeg& s, int seg, int r) {
+__device__ __forceinline__ int kept_row(const EvMoveArgs& a, const EvSeg& s, int seg, int r) {
   int row = s.keep_all ? r : a.idx[(int64_t)seg * a.idx_stride + r];
 #ifdef CATEKV_CHECKED
   row = checked_clamp(row, 0, s.n - 1, a.chk, kKidEvict, seg);
@@ -93,45 +263,82 @@ __device__ __forceinline__ int kept_row(const EvMoveArgs& a, const SelSeg& s, in
   return row;
 }
 
-// Into another cache: a block per 64 rows of a destination segment, a warp per row (lanes 0-15 K, 16-31 V); bound by the copy's bytes.  Rows
-// that a decode plan may cover are rewritten: plain launch, no early signal to dependents (see launch_pdl).
-constexpr int kEvRowsPerBlock = 64;
-__global__ void __launch_bounds__(256) evict_gather_kernel(const EvMoveArgs a) {
+// Into another cache; bound by the copy's bytes.  A CTA moves rows_per_cta consecutive rows of a destination segment in tiles of 32 (a warp a row: lanes 0-15
+// K, 16-31 V), three tiles ahead with cp.async; a thread reads back only what it requested itself, so nothing is synchronised, and the
+// list entries are fetched one tile before they are needed.  It rewrites rows that a decode plan may cover: it never signals its dependents
+// early (see launch_pdl).
+constexpr int kEvTile = 32;
+constexpr int kEvMoveThreads = 256;
+constexpr int kEvMoveStages = 4;
+constexpr int kEvPerThread = kEvTile * 32 / kEvMoveThreads;  // rows of a thread in a tile
+constexpr int kEvMoveSmem = kEvMoveStages * kEvTile * 2 * kRowBytes;
+__global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const EvMoveArgs a) {
+  extern __shared__ __align__(16) uint8_t stage[];
   const int seg = blockIdx.y;
-  const SelSeg s = a.segs[seg];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  const int r0 = blockIdx.x * a.rows_per_cta;
   const int cap = a.dst_cap[seg];
-  const int len = min(s.len_ub, cap);
-  const int r0 = blockIdx.x * kEvRowsPerBlock;
-  if (r0 == 0 && threadIdx.x == 0) {
+  if (r0 >= cap && r0 > 0) return;
+  const EvSeg s = a.segs[seg];
+  const int len = min(s.kept, cap);
+  if (r0 == 0 && tid == 0) {
     a.dst_len[seg] = len;
-    if (s.len_ub > cap) raise_status(a.status, CATEKV_STATUS_CAPACITY, kKidEvict, seg, s.len_ub);
+    if (s.kept > cap) raise_status(a.status, CATEKV_STATUS_CAPACITY, kKidEvict, seg, s.kept);
   }
-  if (r0 >= cap) return;
   const int64_t so = a.src_off[seg], to = a.dst_off[seg];
-  if (threadIdx.x < kEvRowsPerBlock) {
-    const int r = r0 + threadIdx.x;
-    if (r < len) {
-      const int row = kept_row(a, s, seg, r);
-      a.w_dst[to + r] = a.w_src[so + row];
-      if (a.idx_out) a.idx_out[(int64_t)seg * a.idx_out_stride + r] = row;
-    } else if (r < cap) {
-      a.w_dst[to + r] = 0.f;
-    }
-  }
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r1 = min(r0 + a.rows_per_cta, len);
   const uint8_t* src = (lane < 16 ? a.k_src : a.v_src) + so * kRowBytes + (lane & 15) * 16;
   uint8_t* dst = (lane < 16 ? a.k_dst : a.v_dst) + to * kRowBytes + (lane & 15) * 16;
-  uint4 v[8];
+  uint8_t* mine = stage + tid * 16;
+  const uint32_t mine_addr = smem_u32(mine);
+  int row[kEvPerThread];
+  auto fetch_rows = [&](int t) {  // list entries of tile t
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + warp + i * 8;
-    if (r < len) v[i] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)kept_row(a, s, seg, r) * kRowBytes));
-  }
+    for (int i = 0; i < kEvPerThread; ++i) {
+      const int r = r0 + t * kEvTile + warp + i * (kEvMoveThreads / 32);
+      row[i] = r < r1 ? kept_row(a, s, seg, r) : 0;
+    }
+  };
+  auto request = [&](int t) {  // tile t, by the entries in `row`
+    const int st = t % kEvMoveStages;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + warp + i * 8;
-    if (r < len) *reinterpret_cast<uint4*>(dst + (int64_t)r * kRowBytes) = v[i];
+    for (int i = 0; i < kEvPerThread; ++i) {
+      const int r = r0 + t * kEvTile + warp + i * (kEvMoveThreads / 32);
+      if (r < r1) cp_async16(mine_addr + (st * kEvPerThread + i) * kEvMoveThreads * 16, src + (int64_t)row[i] * kRowBytes, 16);
+    }
+    cp_async_commit();
+  };
+  const int tiles = (r1 - r0 + kEvTile - 1) / kEvTile;  // <= 0 behind the list
+  fetch_rows(0);
+  for (int t = 0; t < kEvMoveStages - 1; ++t) {
+    request(t);
+    fetch_rows(t + 1);
   }
+  // the rows' weights, and the list for the caller, while the first tiles arrive
+  for (int r = r0 + tid; r < min(r0 + a.rows_per_cta, cap); r += kEvMoveThreads) {
+    float w = 0.f;
+    if (r < len) {
+      const int from = kept_row(a, s, seg, r);
+      w = a.w_src[so + from];
+      if (a.idx_out) a.idx_out[(int64_t)seg * a.idx_out_stride + r] = from;
+    }
+    a.w_dst[to + r] = w;
+  }
+  for (int t = 0; t < tiles; ++t) {
+    request(t + kEvMoveStages - 1);
+    fetch_rows(t + kEvMoveStages);
+    cp_async_wait<kEvMoveStages - 1>();
+    const int st = t % kEvMoveStages;
+#pragma unroll
+    for (int i = 0; i < kEvPerThread; ++i) {
+      const int r = r0 + t * kEvTile + warp + i * (kEvMoveThreads / 32);
+      if (r < r1)
+        *reinterpret_cast<uint4*>(dst + (int64_t)r * kRowBytes) =
+            *reinterpret_cast<const uint4*>(mine + (st * kEvPerThread + i) * kEvMoveThreads * 16);
+    }
+  }
+  cp_async_wait<0>();
 }
 
 // In place.  Kept row j comes from row idx[j] >= j, so a tile of destination rows may be written once the tile itself has been read: nothing
@@ -142,8 +349,9 @@ constexpr int kEvInThreads = 256;
 constexpr int kEvInRows = 4;  // rows per thread and tile
 __global__ void __launch_bounds__(kEvInThreads) evict_inplace_kernel(const EvMoveArgs a) {
   const int seg = blockIdx.x / kEvSlices, slice = blockIdx.x % kEvSlices;
-  const SelSeg s = a.segs[seg];
-  const int len = s.len_ub;
+  pdl_wait();
+  const EvSeg s = a.segs[seg];
+  const int len = s.kept;
   const int tid = threadIdx.x;
   if (slice == kEvSlices - 1) {
     if (a.idx_out)
@@ -200,7 +408,7 @@ __global__ void __launch_bounds__(kEvInThreads) evict_inplace_kernel(const EvMov
 }
 
 struct EvWs {
-  size_t off_status, off_segs, off_len, off_P, off_idx, bytes;
+  size_t off_status, off_segs, off_idx, bytes;
   int64_t stride;
 };
 static EvWs ev_ws_layout(int n_segs, int max_cap) {
@@ -208,12 +416,56 @@ static EvWs ev_ws_layout(int n_segs, int max_cap) {
   w.stride = (int64_t)align_up((size_t)(max_cap > 0 ? max_cap : 1), 64);
   size_t o = 0;
   w.off_status = o; o = CATEKV_STATUS_BYTES;
-  w.off_segs = o; o = align_up(o + sizeof(SelSeg) * (size_t)n_segs, 256);
-  w.off_len = o; o = align_up(o + sizeof(int32_t) * (size_t)n_segs, 256);
-  w.off_P = o; o = align_up(o + sizeof(float) * (size_t)n_segs * w.stride, 256);
+  w.off_segs = o; o = align_up(o + sizeof(EvSeg) * (size_t)n_segs, 256);
   w.off_idx = o; o = align_up(o + sizeof(int32_t) * (size_t)n_segs * w.stride, 256);
   w.bytes = o;
   return w;
+}
+
+template <int CL>
+static int launch_evict_cluster(const EvSelectArgs& a, int n_segs, size_t smem, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n_segs * CL);
+  cfg.blockDim = dim3(kEvThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CL;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CL > 1 ? 2 : 1;
+  CATEKV_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel<CL>, a));
+  return CATEKV_OK;
+}
+
+// max_pool: bound of a masked segment's candidates
+static int launch_evict_select(EvSelectArgs a, int n_segs, int max_pool, int n_masked, cudaStream_t stream) {
+  static std::atomic<bool> attr_set[64];
+  int dev = 0;
+  CATEKV_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_gather_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvMoveSmem));
+    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+  }
+  int CL = 1;
+  if (max_pool > kEvClusterFrom)
+    for (CL = 8; CL > 1 && n_masked * CL > 2 * sm_count(); CL /= 2) {}
+  while (CL < 8 && (max_pool + CL - 1) / CL + 32 > kEvStageMax) CL *= 2;
+  const int share = ((max_pool + CL - 1) / CL + 31) / 32 * 32;
+  a.stage = share <= kEvStageMax ? share : 0;
+  const size_t smem = (size_t)a.stage * 4;
+  if (CL == 8) return launch_evict_cluster<8>(a, n_segs, smem, stream);
+  if (CL == 4) return launch_evict_cluster<4>(a, n_segs, smem, stream);
+  if (CL == 2) return launch_evict_cluster<2>(a, n_segs, smem, stream);
+  return launch_evict_cluster<1>(a, n_segs, smem, stream);
 }
 
 static int check_evict(const catekv_cache* c, const uint8_t* mask, int32_t budget, int32_t sink, int32_t local) {
@@ -242,7 +494,7 @@ extern "C" int catekv_evict_lengths(const catekv_cache* src, const uint8_t* evic
   if (rc) return rc;
   if (!lens_out) return CATEKV_ERR_INVALID_ARG;
   const EvParams p = {budget, sink, local};
-  for (int s = 0; s < src->B * src->Hkv; ++s) lens_out[s] = evict_decide(src->seg_len[s], evict_mask[s] != 0, p, s).len_ub;
+  for (int s = 0; s < src->B * src->Hkv; ++s) lens_out[s] = evict_decide(src->seg_len[s], evict_mask[s] != 0, p).kept;
   return CATEKV_OK;
 }
 
@@ -264,17 +516,20 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
     return CATEKV_ERR_INVALID_ARG;
   const int n = src->B * src->Hkv;
   if (n > kEvMaxSegs) return CATEKV_ERR_UNSUPPORTED;
-  EvPrepArgs pa = {};
-  pa.p = EvParams{budget, sink, local};
-  int max_cap = 0, max_dst_cap = 0, max_kept = 0, n_masked = 0;
+  EvSelectArgs sa = {};
+  sa.p = EvParams{budget, sink, local};
+  int max_cap = 0, max_masked = 0, max_dst_cap = 0, max_kept = 0, n_masked = 0;
+  int64_t dst_rows = 0;
   for (int s = 0; s < n; ++s) {
-    const int kept = evict_decide(src->seg_len[s], evict_mask[s] != 0, pa.p, s).len_ub;
+    const int kept = evict_decide(src->seg_len[s], evict_mask[s] != 0, sa.p).kept;
     if (kept > dst->seg_cap[s]) return CATEKV_ERR_CAPACITY;
     max_kept = kept > max_kept ? kept : max_kept;
     max_cap = src->seg_cap[s] > max_cap ? src->seg_cap[s] : max_cap;
     max_dst_cap = dst->seg_cap[s] > max_dst_cap ? dst->seg_cap[s] : max_dst_cap;
+    dst_rows += dst->seg_cap[s];
     if (evict_mask[s]) {
-      pa.mask.w[s >> 5] |= 1u << (s & 31);
+      sa.mask.w[s >> 5] |= 1u << (s & 31);
+      max_masked = src->seg_cap[s] > max_masked ? src->seg_cap[s] : max_masked;
       ++n_masked;
     }
   }
@@ -283,32 +538,18 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
   if (ws_bytes < W.bytes) return CATEKV_ERR_WORKSPACE;
   cudaStream_t st = (cudaStream_t)stream;
   uint8_t* w8 = (uint8_t*)ws;
-  pa.seg_off = src->seg_off_dev;
-  pa.seg_len = src->seg_len_dev;
-  pa.weights = weights;
-  pa.segs = (SelSeg*)(w8 + W.off_segs);
-  pa.P = (float*)(w8 + W.off_P);
-  pa.p_stride = W.stride;
-  const int gx = max_cap > 0 ? (max_cap + kEvPrepRows - 1) / kEvPrepRows : 1;
-  CATEKV_CUDA_TRY(launch_pdl(evict_prep_kernel, dim3(gx, n), dim3(256), 0, st, pa));
-  TopkArgs ta = {};
-  ta.segs = pa.segs;
-  ta.C = pa.P;
-  ta.P = pa.P;
-  ta.c_stride = W.stride;
-  ta.idx = (int32_t*)(w8 + W.off_idx);
-  ta.idx_stride = W.stride;
-  ta.seg_len_dev = (int32_t*)(w8 + W.off_len);
-  ta.sink = sink;
-  ta.pool_mode = kPoolPrescored;
-  ta.pool_param = 1;
-  ta.row_is_seg = 1;
-  ta.raw_scores = 1;
-  rc = launch_topk(ta, n, max_cap, n_masked, st);
+  sa.seg_off = src->seg_off_dev;
+  sa.seg_len = src->seg_len_dev;
+  sa.weights = weights;
+  sa.segs = (EvSeg*)(w8 + W.off_segs);
+  sa.idx = (int32_t*)(w8 + W.off_idx);
+  sa.idx_stride = W.stride;
+  sa.chk = checked_status_ptr();
+  rc = launch_evict_select(sa, n, max_masked, n_masked, st);
   if (rc) return rc;
   EvMoveArgs ma;
-  ma.segs = pa.segs;
-  ma.idx = ta.idx;
+  ma.segs = sa.segs;
+  ma.idx = sa.idx;
   ma.idx_stride = W.stride;
   ma.k_src = (const uint8_t*)src->k_pool;
   ma.v_src = (const uint8_t*)src->v_pool;
@@ -324,12 +565,17 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
   ma.idx_out_stride = idx_stride;
   ma.status = (int32_t*)(w8 + W.off_status);
   ma.chk = checked_status_ptr();
-  if (in_place)
-    evict_inplace_kernel<<<n * kEvSlices, kEvInThreads, 0, st>>>(ma);
-  else
-    evict_gather_kernel<<<dim3(max_dst_cap > 0 ? (max_dst_cap + kEvRowsPerBlock - 1) / kEvRowsPerBlock : 1, n), 256, 0, st>>>(ma);
-  CATEKV_CUDA_TRY(cudaGetLastError());
-  for (int s = 0; s < n; ++s) dst->seg_len[s] = evict_decide(src->seg_len[s], evict_mask[s] != 0, pa.p, s).len_ub;
+  ma.rows_per_cta = 0;
+  if (in_place) {
+    CATEKV_CUDA_TRY(launch_pdl(evict_inplace_kernel, dim3(n * kEvSlices), dim3(kEvInThreads), 0, st, ma));
+  } else {
+    // two CTAs and more for every SM's three places, up to 256 rows each
+    int64_t rows = dst_rows / (6 * sm_count()) / kEvTile * kEvTile;
+    ma.rows_per_cta = rows < kEvTile ? kEvTile : rows > 256 ? 256 : (int)rows;
+    const int gx = max_dst_cap > 0 ? (max_dst_cap + ma.rows_per_cta - 1) / ma.rows_per_cta : 1;
+    CATEKV_CUDA_TRY(launch_pdl(evict_gather_kernel, dim3(gx, n), dim3(kEvMoveThreads), kEvMoveSmem, st, ma));
+  }
+  for (int s = 0; s < n; ++s) dst->seg_len[s] = evict_decide(src->seg_len[s], evict_mask[s] != 0, sa.p).kept;
   if (!in_place) dst->reserved = 0;
   return CATEKV_OK;
 }

@@ -450,11 +450,7 @@ __global__ void __launch_bounds__(kTopkThreads) topk_small_kernel(const TopkArgs
       const float xmin = key_to_score(base);
       const float scale = (float)(kTsBins - 1) / (key_to_score(s_mm[1]) - xmin);
       int shift = 0;
-      // Raw scores (accumulated attention weights) spread over many powers of two: their first digits are taken linearly in
-      // the bit pattern, that is in the logarithm.
-      const int raw_shift = a.raw_scores ? max(0, 32 - __clz(range) - 10) : 0;
       auto digit = [&](unsigned int val) -> int {
-        if (linear && a.raw_scores) return min(max((int)(val - base) >> raw_shift, 0), kTsBins - 1);  // patterns are below 2^31
         if (linear) {
           // monotone in val, also when the sample's range is empty (scale infinite): a product that is not a number
           // converts to 0, an infinite or negative one is clamped

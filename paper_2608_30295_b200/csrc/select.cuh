@@ -32,7 +32,6 @@ struct TopkArgs {
   int32_t stage_entries;  // set by launch_topk: pooled entries per CTA that the dynamic shared memory holds
   int32_t* chk;           // set by launch_topk: the checked build's status block, else null
   int32_t row_is_seg;     // 1 (prescored lists only): the score row of segment s is row s, whatever its job says
-  int32_t raw_scores;     // 1 (prescored lists only): the scores are non-negative floats as they are, not monotone_key patterns
   int32_t small_pool;     // set by launch_topk for topk_small_kernel: bound of the pooled entries of a segment
 };
 
