@@ -156,6 +156,16 @@ __device__ __forceinline__ void tile_rows(const ItemCursor& c, int i, int& start
   nvalid = c.live - start;
 }
 
+// Stores whose lines L2 keeps while a stream passes through it: the logits are read again as soon as the last row has been seen.
+__device__ __forceinline__ uint64_t l2_keep_policy() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;\n" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ void store_hint(float* p, float v, uint64_t policy) {
+  asm volatile("st.global.L2::cache_hint.f32 [%0], %1, %2;\n" ::"l"(p), "f"(v), "l"(policy) : "memory");
+}
+
 // kLogits: every row's scaled logits are also left in a.logits, for the weights that catekv_decode_attn_weighted accumulates
 template <int kMode, bool kLogits = false>
 __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const DecodeArgs a) {
@@ -165,6 +175,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
   __shared__ ItemCursor s_ring[4];  // cursors of the pieces the producer has started, for the consumer
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, t = lane & 3;
+  const uint64_t keep = kLogits ? l2_keep_policy() : 0;
   pdl_launch_dependents();
   int item_begin, item_end;
   ItemCursor pc;
@@ -360,12 +371,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
       if (kLogits) {  // head by head: the 8 rows of a store are one 32-byte sector
         float* lp = a.logits + cc.row_base + (tstart - cc.t0) + row0 + g + (int64_t)(2 * t) * a.logit_stride;
         if (2 * t < a.G) {
-          if (v_lo) lp[0] = x0;
-          if (v_hi) lp[8] = x2;
+          if (v_lo) store_hint(lp, x0, keep);
+          if (v_hi) store_hint(lp + 8, x2, keep);
         }
         if (2 * t + 1 < a.G) {
-          if (v_lo) lp[a.logit_stride] = x1;
-          if (v_hi) lp[a.logit_stride + 8] = x3;
+          if (v_lo) store_hint(lp + a.logit_stride, x1, keep);
+          if (v_hi) store_hint(lp + a.logit_stride + 8, x3, keep);
         }
       }
       float mx0 = fmaxf(x0, x2), mx1 = fmaxf(x1, x3);
@@ -513,9 +524,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
 // running maximum of its own; the warps are then merged through shared memory in a fixed order.
 constexpr int kCombineWarps = 8;
 constexpr int kCombineUnroll = 16;
-__global__ void __launch_bounds__(kCombineWarps * 32) decode_combine_kernel(const CombineArgs a) {
-  const int seg = blockIdx.x, hd = blockIdx.y;
-  pdl_launch_dependents();
+__device__ __forceinline__ void combine_segment(const CombineArgs& a, int seg, int hd) {
   const SegInfo si = a.seg_info[seg];  // plan data: older than the previous kernel
   pdl_wait();
   if (si.n_pieces <= 1) return;  // written directly by the attention kernel
@@ -603,6 +612,11 @@ __global__ void __launch_bounds__(kCombineWarps * 32) decode_combine_kernel(cons
     if (a.lse_out && lane == 0)
       a.lse_out[(size_t)b * a.Hq + h * a.G + hd] = W > 0.f ? (M + log2f(W)) * 0.6931471805599453f : -INFINITY;
   }
+}
+
+__global__ void __launch_bounds__(kCombineWarps * 32) decode_combine_kernel(const CombineArgs a) {
+  pdl_launch_dependents();
+  combine_segment(a, blockIdx.x, blockIdx.y);
 }
 
 int launch_combine(const CombineArgs& a, int n_segs, cudaStream_t stream) {
@@ -756,47 +770,121 @@ extern "C" int catekv_decode_attn_indexed(const catekv_cache* cache, const int32
 namespace catekv {
 
 struct WeightArgs {
+  CombineArgs c;
+  int32_t num_ctas;  // of the plan
   const int32_t* seg_len;
   const CtaHeader* ctas;
   const WorkItem* items;
   const float* logits;  // [G][logit_stride], log2 domain
   int64_t logit_stride;
-  const float* lse;     // [B, Hq], natural log
   float* weights;
   float decay;
-  int32_t Hq, Hkv, G;
 };
 
-// w <- decay w + mean over the group of exp(logit - lse), a thread per row, the rows shared out by the attention's own plan.  A row's logits
-// are G words against the 512 bytes that attention read of it, and as a rule still in L2: the pass is the price of a softmax whose
-// normaliser is known only when the last row has been seen.
-constexpr int kWeightThreads = 256;
+// The combine pass and the weights in one launch: the first CTAs take the rows by the attention's own plan, the others merge partials:
+// w <- decay w + mean over the group of exp(logit - lse), with the LSE of a segment that was cut formed from its pieces' own
+// (a few hundred numbers), so that neither half waits for the other.  A row's logits are G words against the 512 bytes that attention read of
+// it, left in L2: they are the price of a softmax whose normaliser is known only when the last row has been seen.
+// Latency-bound: kWeightRows rows of a thread are in flight at once.
+constexpr int kWeightThreads = kCombineWarps * 32;
+constexpr int kWeightRows = 4;
 template <int kG>
-__global__ void __launch_bounds__(kWeightThreads) weight_kernel(const WeightArgs a) {
+__global__ void __launch_bounds__(kWeightThreads) combine_weight_kernel(const __grid_constant__ WeightArgs a) {
+  __shared__ float s_lse[kG];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_launch_dependents();
-  const int4 h0 = __ldg(reinterpret_cast<const int4*>(a.ctas + blockIdx.x));  // plan data: older than the previous kernel
+  const int cta = blockIdx.x;
+  if (cta >= a.num_ctas) {
+    combine_segment(a.c, (cta - a.num_ctas) / kG, (cta - a.num_ctas) % kG);
+    return;
+  }
+  // plan data (older than the previous kernel): the CTA's items and a copy of the first
+  const int4* hp = reinterpret_cast<const int4*>(a.ctas + cta);
+  const int4 h0 = __ldg(hp);
+  WorkItem w = unpack_item(__ldg(hp + 1), __ldg(hp + 2));
+  if (h0.x >= h0.y) return;
   pdl_wait();
   for (int it = h0.x; it < h0.y; ++it) {
-    const WorkItem w = a.items[it];
+    if (it > h0.x) {
+      const int4* ip = reinterpret_cast<const int4*>(a.items + it);
+      w = unpack_item(__ldg(ip), __ldg(ip + 1));
+    }
+    const SegInfo si = a.c.seg_info[w.seg];
     const int len = a.seg_len[w.seg];
-    const int n = (w.last ? len : min(w.t1, len)) - w.t0;
+    // the first rows' logits and weights are requested before the LSE is known: three trips to memory in all
+    const float* lp = a.logits + w.row_base;
+    float* wp = a.weights + w.row_base;
+    const int ahead = min(w.t1 - w.t0, kWeightThreads * kWeightRows);
+    float x[kWeightRows][kG], old[kWeightRows];
+#pragma unroll
+    for (int i = 0; i < kWeightRows; ++i) {
+      const int r = tid + i * kWeightThreads;
+#pragma unroll
+      for (int g = 0; g < kG; ++g) x[i][g] = r < ahead ? lp[g * a.logit_stride + r] : -INFINITY;
+      old[i] = r < ahead && a.decay != 0.f ? wp[r] * a.decay : 0.f;
+    }
+    __syncthreads();  // s_lse of the item before has been read
+    if (warp < kG) {
+      float l;
+      if (si.n_pieces <= 1) {
+        l = a.c.lse_out[(size_t)(w.seg / a.c.Hkv) * a.c.Hq + (size_t)(w.seg % a.c.Hkv) * kG + warp] * 1.4426950408889634f;
+      } else {
+        const float* p = a.c.part_lse + (size_t)si.slot_begin * kMaxG + warp;
+        float m = -INFINITY, sum = 0.f;
+        for (int i0 = lane; i0 < si.n_pieces; i0 += 128) {
+          float y[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = i0 + 32 * j < si.n_pieces ? p[(size_t)(i0 + 32 * j) * kMaxG] : -INFINITY;
+          const float mn = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), m);
+          if (mn > -INFINITY) {
+            sum *= exp2f(m - mn);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += exp2f(y[j] - mn);
+            m = mn;
+          }
+        }
+        float M = m;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+        sum = m > -INFINITY ? sum * exp2f(m - M) : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        l = M + log2f(sum);
+      }
+      if (lane == 0) s_lse[warp] = l;
+    }
+    __syncthreads();
     float lse[kG];
 #pragma unroll
-    for (int g = 0; g < kG; ++g)
-      lse[g] = a.lse[(size_t)(w.seg / a.Hkv) * a.Hq + (size_t)(w.seg % a.Hkv) * kG + g] * 1.4426950408889634f;
-    for (int r = threadIdx.x; r < n; r += kWeightThreads) {
-      const float* lp = a.logits + w.row_base + r;
-      float* wp = a.weights + w.row_base + r;
-      float x[kG];
+    for (int g = 0; g < kG; ++g) lse[g] = s_lse[g];
+    const int n = (w.last ? len : min(w.t1, len)) - w.t0;
+    int r0 = 0, end = min(ahead, n);  // rows [r0, end) are in x and old
+    while (true) {
 #pragma unroll
-      for (int g = 0; g < kG; ++g) x[g] = lp[g * a.logit_stride];
-      const float old = a.decay != 0.f ? *wp * a.decay : 0.f;
-      float p = 0.f;
+      for (int i = 0; i < kWeightRows; ++i) {
+        const int r = r0 + tid + i * kWeightThreads;
+        float p = 0.f;
 #pragma unroll
-      for (int g = 0; g < kG; ++g) p += exp2f(x[g] - lse[g]);
-      *wp = old + p * (1.f / kG);
+        for (int g = 0; g < kG; ++g) p += exp2f(x[i][g] - lse[g]);
+        if (r < end) wp[r] = old[i] + p * (1.f / kG);
+      }
+      r0 = end;
+      if (r0 >= n) break;
+      end = min(n, r0 + kWeightThreads * kWeightRows);
+#pragma unroll
+      for (int i = 0; i < kWeightRows; ++i) {
+        const int r = r0 + tid + i * kWeightThreads;
+#pragma unroll
+        for (int g = 0; g < kG; ++g) x[i][g] = r < end ? lp[g * a.logit_stride + r] : -INFINITY;
+        old[i] = r < end && a.decay != 0.f ? wp[r] * a.decay : 0.f;
+      }
     }
   }
+}
+
+template <int kG>
+static cudaError_t launch_weights(const WeightArgs& a, int n_segs, cudaStream_t st) {
+  return launch_pdl(combine_weight_kernel<kG>, dim3(a.num_ctas + n_segs * kG), dim3(kWeightThreads), 0, st, a);
 }
 
 struct WeightedWs {
@@ -833,34 +921,43 @@ extern "C" int catekv_decode_attn_weighted(const catekv_cache* cache, const void
   if (ws_bytes < W.bytes) return CATEKV_ERR_WORKSPACE;
   float* lse = lse_out ? lse_out : (float*)((uint8_t*)ws + W.off_lse);
   float* logits = (float*)((uint8_t*)ws + W.off_logits);
-  rc = decode_launch(3, cache, nullptr, nullptr, q, Hq, sm_scale, out, out_dtype, lse, plan_host, plan_dev, plan_bytes, ws, ws_bytes,
+  rc = decode_launch(1, cache, nullptr, nullptr, q, Hq, sm_scale, out, out_dtype, lse, plan_host, plan_dev, plan_bytes, ws, ws_bytes,
                      stream, nullptr, logits);
   if (rc) return rc;
-  const PlanLayout L = plan_layout(cache->B * cache->Hkv, hdr->num_ctas);
+  const int n_segs = cache->B * cache->Hkv;
+  const PlanLayout L = plan_layout(n_segs, hdr->num_ctas);
+  size_t off_lse = 0;
+  ws_layout(n_segs, hdr->num_ctas, &off_lse);
   const uint8_t* pd = (const uint8_t*)plan_dev;
   WeightArgs a;
+  a.c.seg_info = (const SegInfo*)(pd + L.off_seg);
+  a.c.part_o = (const float*)ws;
+  a.c.part_lse = (const float*)((const uint8_t*)ws + off_lse);
+  a.c.out = out;
+  a.c.lse_out = lse;
+  a.c.Hq = Hq;
+  a.c.Hkv = cache->Hkv;
+  a.c.G = Hq / cache->Hkv;
+  a.c.out_fp32 = out_dtype == CATEKV_OUT_FP32;
+  a.num_ctas = hdr->num_ctas;
   a.seg_len = cache->seg_len_dev;
   a.ctas = (const CtaHeader*)(pd + L.off_cta);
   a.items = (const WorkItem*)(pd + L.off_items);
   a.logits = logits;
   a.logit_stride = cache->total_rows;
-  a.lse = lse;
   a.weights = weights;
   a.decay = decay;
-  a.Hq = Hq;
-  a.Hkv = cache->Hkv;
-  a.G = Hq / cache->Hkv;
-  const dim3 grid(hdr->num_ctas), block(kWeightThreads);
   cudaStream_t st = (cudaStream_t)stream;
-  switch (a.G) {
-    case 1: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<1>, grid, block, 0, st, a)); break;
-    case 2: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<2>, grid, block, 0, st, a)); break;
-    case 3: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<3>, grid, block, 0, st, a)); break;
-    case 4: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<4>, grid, block, 0, st, a)); break;
-    case 5: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<5>, grid, block, 0, st, a)); break;
-    case 6: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<6>, grid, block, 0, st, a)); break;
-    case 7: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<7>, grid, block, 0, st, a)); break;
-    default: CATEKV_CUDA_TRY(launch_pdl(weight_kernel<8>, grid, block, 0, st, a)); break;
+  const int n = n_segs;
+  switch (a.c.G) {
+    case 1: CATEKV_CUDA_TRY(launch_weights<1>(a, n, st)); break;
+    case 2: CATEKV_CUDA_TRY(launch_weights<2>(a, n, st)); break;
+    case 3: CATEKV_CUDA_TRY(launch_weights<3>(a, n, st)); break;
+    case 4: CATEKV_CUDA_TRY(launch_weights<4>(a, n, st)); break;
+    case 5: CATEKV_CUDA_TRY(launch_weights<5>(a, n, st)); break;
+    case 6: CATEKV_CUDA_TRY(launch_weights<6>(a, n, st)); break;
+    case 7: CATEKV_CUDA_TRY(launch_weights<7>(a, n, st)); break;
+    default: CATEKV_CUDA_TRY(launch_weights<8>(a, n, st)); break;
   }
   return CATEKV_OK;
 }

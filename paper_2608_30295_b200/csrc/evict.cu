@@ -11,9 +11,12 @@ namespace cg = cooperative_groups;
 
 namespace catekv {
 
-constexpr int kEvMaxSegs = 2048;  // the mask travels in the kernel arguments
+constexpr int kEvMaxSegs = 2048;  // the masked segments travel in the kernel arguments
 struct EvMask {
   uint32_t w[kEvMaxSegs / 32];
+};
+struct EvList {
+  uint16_t seg[kEvMaxSegs];
 };
 
 struct EvParams {
@@ -47,7 +50,7 @@ __host__ __device__ inline EvSeg evict_decide(int n, bool masked, const EvParams
 // ------------------------------------------------------------------------------------------
 // Selection
 // ------------------------------------------------------------------------------------------
-// A cluster of CL CTAs per segment (1 where the list is short), each with a share of the candidates in shared memory as sortable patterns
+// A cluster of CL CTAs per masked segment (1 where the list is short), each with a share of the candidates in shared memory as sortable patterns
 // (a non-negative float's bits order like the float).  The pattern of the k-th largest is found from the top, 11 + 11 + 9 bits, with a histogram
 // per step: weights spread over many powers of two, so the first step (exponent and three bits) already leaves a few per cent.  A histogram of its
 // own per step means one cluster barrier per step.  What is above the pattern is kept, of what equals it the first in row order; a
@@ -69,7 +72,7 @@ struct EvSelectArgs {
   int32_t* chk;   // the checked build's status block, else null
   int32_t stage;  // candidates a CTA's shared memory holds (longer shares are read from global memory)
   EvParams p;
-  EvMask mask;
+  EvList list;    // a cluster each
 };
 
 __device__ __forceinline__ unsigned int ev_pattern(float x) {  // negative as 0, NaN as infinite
@@ -79,7 +82,7 @@ __device__ __forceinline__ unsigned int ev_pattern(float x) {  // negative as 0,
 template <int CL>
 __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_constant__ EvSelectArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
-  const int seg = blockIdx.x / CL;
+  const int seg = a.list.seg[blockIdx.x / CL];
   const int rank = CL > 1 ? (int)cluster.block_rank() : 0;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   __shared__ unsigned int hist[3][kEvBins];
@@ -91,7 +94,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
   pdl_launch_dependents();
   for (int i = tid; i < 3 * kEvBins; i += kEvThreads) (&hist[0][0])[i] = 0u;
   pdl_wait();
-  const EvSeg s = evict_decide(a.seg_len[seg], (a.mask.w[seg >> 5] >> (seg & 31)) & 1u, a.p);
+  const EvSeg s = evict_decide(a.seg_len[seg], true, a.p);
   if (rank == 0 && tid == 0) a.segs[seg] = s;
   if (s.keep_all) return;  // the whole cluster
   auto cluster_sync = [&]() {
@@ -235,7 +238,9 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
 // Move
 // ------------------------------------------------------------------------------------------
 struct EvMoveArgs {
-  const EvSeg* segs;
+  EvMask mask;
+  const EvSeg* segs;       // of the masked segments
+  const int32_t* src_len;  // of the others, which keep all rows
   const int32_t* idx;
   int64_t idx_stride;
   const uint8_t* k_src;
@@ -255,6 +260,10 @@ struct EvMoveArgs {
   int32_t* chk;
 };
 
+__device__ __forceinline__ EvSeg move_seg(const EvMoveArgs& a, int seg) {
+  if ((a.mask.w[seg >> 5] >> (seg & 31)) & 1u) return a.segs[seg];
+  return evict_decide(a.src_len[seg], false, EvParams{0, 0, 0});
+}
 __device__ __forceinline__ int kept_row(const EvMoveArgs& a, const EvSeg& s, int seg, int r) {
   int row = s.keep_all ? r : a.idx[(int64_t)seg * a.idx_stride + r];
 #ifdef CATEKV_CHECKED
@@ -272,7 +281,7 @@ constexpr int kEvMoveThreads = 256;
 constexpr int kEvMoveStages = 4;
 constexpr int kEvPerThread = kEvTile * 32 / kEvMoveThreads;  // rows of a thread in a tile
 constexpr int kEvMoveSmem = kEvMoveStages * kEvTile * 2 * kRowBytes;
-__global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const EvMoveArgs a) {
+__global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const __grid_constant__ EvMoveArgs a) {
   extern __shared__ __align__(16) uint8_t stage[];
   const int seg = blockIdx.y;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -280,7 +289,7 @@ __global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const EvMo
   const int r0 = blockIdx.x * a.rows_per_cta;
   const int cap = a.dst_cap[seg];
   if (r0 >= cap && r0 > 0) return;
-  const EvSeg s = a.segs[seg];
+  const EvSeg s = move_seg(a, seg);
   const int len = min(s.kept, cap);
   if (r0 == 0 && tid == 0) {
     a.dst_len[seg] = len;
@@ -347,10 +356,10 @@ __global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const EvMo
 constexpr int kEvSlices = 2 * kRowBytes / 32 + 1;
 constexpr int kEvInThreads = 256;
 constexpr int kEvInRows = 4;  // rows per thread and tile
-__global__ void __launch_bounds__(kEvInThreads) evict_inplace_kernel(const EvMoveArgs a) {
+__global__ void __launch_bounds__(kEvInThreads) evict_inplace_kernel(const __grid_constant__ EvMoveArgs a) {
   const int seg = blockIdx.x / kEvSlices, slice = blockIdx.x % kEvSlices;
   pdl_wait();
-  const EvSeg s = a.segs[seg];
+  const EvSeg s = move_seg(a, seg);
   const int len = s.kept;
   const int tid = threadIdx.x;
   if (slice == kEvSlices - 1) {
@@ -423,9 +432,9 @@ static EvWs ev_ws_layout(int n_segs, int max_cap) {
 }
 
 template <int CL>
-static int launch_evict_cluster(const EvSelectArgs& a, int n_segs, size_t smem, cudaStream_t stream) {
+static int launch_evict_cluster(const EvSelectArgs& a, int n_masked, size_t smem, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_segs * CL);
+  cfg.gridDim = dim3(n_masked * CL);
   cfg.blockDim = dim3(kEvThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -442,8 +451,8 @@ static int launch_evict_cluster(const EvSelectArgs& a, int n_segs, size_t smem, 
   return CATEKV_OK;
 }
 
-// max_pool: bound of a masked segment's candidates
-static int launch_evict_select(EvSelectArgs a, int n_segs, int max_pool, int n_masked, cudaStream_t stream) {
+// the kernels' shared-memory limits, once per device
+static int evict_attributes() {
   static std::atomic<bool> attr_set[64];
   int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
@@ -455,6 +464,10 @@ static int launch_evict_select(EvSelectArgs a, int n_segs, int max_pool, int n_m
     CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_gather_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvMoveSmem));
     if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   }
+  return CATEKV_OK;
+}
+// max_pool: bound of a masked segment's candidates
+static int launch_evict_select(EvSelectArgs& a, int n_masked, int max_pool, cudaStream_t stream) {
   int CL = 1;
   if (max_pool > kEvClusterFrom)
     for (CL = 8; CL > 1 && n_masked * CL > 2 * sm_count(); CL /= 2) {}
@@ -462,10 +475,10 @@ static int launch_evict_select(EvSelectArgs a, int n_segs, int max_pool, int n_m
   const int share = ((max_pool + CL - 1) / CL + 31) / 32 * 32;
   a.stage = share <= kEvStageMax ? share : 0;
   const size_t smem = (size_t)a.stage * 4;
-  if (CL == 8) return launch_evict_cluster<8>(a, n_segs, smem, stream);
-  if (CL == 4) return launch_evict_cluster<4>(a, n_segs, smem, stream);
-  if (CL == 2) return launch_evict_cluster<2>(a, n_segs, smem, stream);
-  return launch_evict_cluster<1>(a, n_segs, smem, stream);
+  if (CL == 8) return launch_evict_cluster<8>(a, n_masked, smem, stream);
+  if (CL == 4) return launch_evict_cluster<4>(a, n_masked, smem, stream);
+  if (CL == 2) return launch_evict_cluster<2>(a, n_masked, smem, stream);
+  return launch_evict_cluster<1>(a, n_masked, smem, stream);
 }
 
 static int check_evict(const catekv_cache* c, const uint8_t* mask, int32_t budget, int32_t sink, int32_t local) {
@@ -517,6 +530,7 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
   const int n = src->B * src->Hkv;
   if (n > kEvMaxSegs) return CATEKV_ERR_UNSUPPORTED;
   EvSelectArgs sa = {};
+  EvMoveArgs ma = {};
   sa.p = EvParams{budget, sink, local};
   int max_cap = 0, max_masked = 0, max_dst_cap = 0, max_kept = 0, n_masked = 0;
   int64_t dst_rows = 0;
@@ -528,9 +542,9 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
     max_dst_cap = dst->seg_cap[s] > max_dst_cap ? dst->seg_cap[s] : max_dst_cap;
     dst_rows += dst->seg_cap[s];
     if (evict_mask[s]) {
-      sa.mask.w[s >> 5] |= 1u << (s & 31);
+      ma.mask.w[s >> 5] |= 1u << (s & 31);
       max_masked = src->seg_cap[s] > max_masked ? src->seg_cap[s] : max_masked;
-      ++n_masked;
+      sa.list.seg[n_masked++] = (uint16_t)s;
     }
   }
   if (idx_out && idx_stride < max_kept) return CATEKV_ERR_INVALID_ARG;
@@ -545,10 +559,14 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
   sa.idx = (int32_t*)(w8 + W.off_idx);
   sa.idx_stride = W.stride;
   sa.chk = checked_status_ptr();
-  rc = launch_evict_select(sa, n, max_masked, n_masked, st);
+  rc = evict_attributes();
   if (rc) return rc;
-  EvMoveArgs ma;
+  if (n_masked > 0) {
+    rc = launch_evict_select(sa, n_masked, max_masked, st);
+    if (rc) return rc;
+  }
   ma.segs = sa.segs;
+  ma.src_len = src->seg_len_dev;
   ma.idx = sa.idx;
   ma.idx_stride = W.stride;
   ma.k_src = (const uint8_t*)src->k_pool;

@@ -35,7 +35,7 @@ constexpr int kQ8MergeRegs = 36;  // 32 accumulators + m0, m1, l0, l1
 constexpr int kQ8MergeSlotBytes = kQ8MergeRegs * 32 * 4;
 constexpr int kQ8DecodeSmem = kQ8Warps * kQ8Stages * kQ8UnitBytes + 2 * kQ8MergeSlotBytes;
 constexpr int32_t kQ8PlanTile = kQ8Unit;   // marks a plan of this kind (decode.cu's have kTile)
-constexpr int kQ8SegEndCharge = 256;       // rows
+constexpr int kQ8SegEndCharge = 512;       // rows
 constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12
 constexpr float kQ8TailFloor = 7.8886090522101181e-31f;  // 2^-100
 static_assert(kQ8PlanTile != kTile, "the two kinds of plan must differ");
@@ -82,18 +82,20 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src));
 }
 
-// A piece of a segment as a warp sees it: `full` units of codes starting at pool block blk0 (of which the first `live` are to be attended to: the
+// A piece of a segment as a warp sees it: `full` units of codes starting at unit u0 of the pool (of which the first `live` are to be attended to: the
 // others were complete when the plan was built but no longer are), then the units of the tail.
 struct Q8Cursor {
   int seg, slot, np, full, live, tail, units;
-  int64_t blk0;
+  int64_t u0;
 };
+constexpr int kUnitsPerBlock = kQ8Block / kQ8Unit;
 __device__ __forceinline__ Q8Cursor q8_plan_cursor(const WorkItem& w) {
   Q8Cursor c;
   c.seg = w.seg;
   c.slot = w.slot;
-  c.blk0 = w.row_base / kQ8Block;
-  c.np = (w.t1 / kQ8Block - w.t0 / kQ8Block) * (kQ8Block / kQ8Unit);  // t0 is a multiple of the block, and so is t1 of an inner piece
+  c.u0 = w.row_base / kQ8Unit;
+  // t0 is a multiple of the unit, and so is t1 of an inner piece; the last piece's units are those of complete blocks
+  c.np = max(0, (w.last ? w.t1 / kQ8Block * kUnitsPerBlock : w.t1 / kQ8Unit) - w.t0 / kQ8Unit);
   c.full = c.np;
   c.live = c.np;
   c.tail = 0;
@@ -101,9 +103,9 @@ __device__ __forceinline__ Q8Cursor q8_plan_cursor(const WorkItem& w) {
   return c;
 }
 __device__ __forceinline__ void q8_live_cursor(const WorkItem& w, int len, Q8Cursor& c) {
-  int end = len / kQ8Block;
-  if (!w.last) end = min(end, w.t1 / kQ8Block);
-  c.live = max(0, end - w.t0 / kQ8Block) * (kQ8Block / kQ8Unit);
+  int end = len / kQ8Block * kUnitsPerBlock;
+  if (!w.last) end = min(end, w.t1 / kQ8Unit);
+  c.live = max(0, end - w.t0 / kQ8Unit);
   c.full = max(c.np, c.live);
   c.tail = w.last ? len % kQ8Block : 0;
   c.units = c.full + (c.tail + kQ8TailUnit - 1) / kQ8TailUnit;
@@ -147,8 +149,8 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
     const int stage = p_seq % kQ8Stages;
     const uint32_t sb = ring + stage * kQ8UnitBytes;
     if (p_u < pc.full) {
-      const int64_t blk = pc.blk0 + (p_u >> 1);
-      const int64_t off = blk * kQ8BlockBytes + (p_u & 1) * (kQ8Unit * kQ8RowBytes) + lane * 16;
+      const int64_t unit = pc.u0 + p_u;
+      const int64_t off = unit * (kQ8Unit * kQ8RowBytes) + lane * 16;
       const uint8_t* kp = a.k_pool + off;
       const uint8_t* vp = a.v_pool + off;
       // rows of 128 bytes, chunk j of row r at place j ^ (r & 7)
@@ -164,7 +166,7 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
         cp_async16(d0 + 4096 + i * 512, vp + i * 512, 16);
         cp_async16(d1 + 4096 + i * 512, vp + i * 512 + 512, 16);
       }
-      if (lane < 2) cp_async4(ring_scale + (stage * 2 + lane) * 4, (lane ? a.v_scale : a.k_scale) + blk);
+      if (lane < 2) cp_async4(ring_scale + (stage * 2 + lane) * 4, (lane ? a.v_scale : a.k_scale) + unit / kUnitsPerBlock);
     } else {
       const int r0 = (p_u - pc.full) * kQ8TailUnit;
       const int left = pc.tail - r0;
@@ -499,6 +501,71 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
   cp_async_wait<0>();
 }
 
+// Combine for few (segment, head) pairs: a CTA per pair and 32 of the 128 dimensions, a warp per 32 pieces, a lane per dimension.  Small enough
+// (128 threads, at most 72 registers) to be resident beside two CTAs of the attention kernel: launched programmatically it has its plan entry and
+// waits at the dependency when the last partial is written, and the next attention kernel's CTAs find room beside it.
+constexpr int kQ8CombineThreads = 128;
+constexpr int kQ8CombineSplit = 4;
+__global__ void __launch_bounds__(kQ8CombineThreads, 7) q8_combine_kernel(const CombineArgs a) {
+  __shared__ float s_acc[kQ8CombineThreads / 32][32], s_w[kQ8CombineThreads / 32], s_m[kQ8CombineThreads / 32];
+  const int seg = blockIdx.x, hd = blockIdx.y, part = blockIdx.z;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_launch_dependents();
+  const SegInfo si = a.seg_info[seg];  // plan data: older than the previous kernel
+  pdl_wait();
+  if (si.n_pieces <= 1) return;  // written directly by the attention kernel
+  const int n = si.n_pieces;
+  const float* lse = a.part_lse + (size_t)si.slot_begin * kMaxG + hd;
+  const float* po = a.part_o + ((size_t)si.slot_begin * kMaxG + hd) * kD + part * 32 + lane;
+  float acc = 0.f, wsum = 0.f, mw = -INFINITY;
+  for (int p0 = warp * 32; p0 < n; p0 += kQ8CombineThreads) {
+    const float l = p0 + lane < n ? lse[(size_t)(p0 + lane) * kMaxG] : -INFINITY;
+    float v[32];
+#pragma unroll
+    for (int u = 0; u < 32; ++u) v[u] = p0 + u < n ? po[(size_t)(p0 + u) * (kMaxG * kD)] : 0.f;
+    float mx = l;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    mx = fmaxf(mx, mw);
+    if (mx > -INFINITY) {  // the same in every lane
+      const float sc = exp2f(mw - mx), e = exp2f(l - mx);  // 0 for an empty piece (LSE -inf) and on the first pass (mw = -inf)
+      acc *= sc;
+      wsum = wsum * sc + e;  // a lane's own pieces
+      mw = mx;
+#pragma unroll
+      for (int u = 0; u < 32; ++u) acc += __shfl_sync(0xffffffffu, e, u) * v[u];
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) wsum += __shfl_xor_sync(0xffffffffu, wsum, o);
+  s_acc[warp][lane] = acc;
+  if (lane == 0) {
+    s_w[warp] = wsum;
+    s_m[warp] = mw;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    float M = -INFINITY, W = 0.f, r = 0.f;
+#pragma unroll
+    for (int w = 0; w < kQ8CombineThreads / 32; ++w) M = fmaxf(M, s_m[w]);
+#pragma unroll
+    for (int w = 0; w < kQ8CombineThreads / 32; ++w) {
+      const float f = s_m[w] > -INFINITY ? exp2f(s_m[w] - M) : 0.f;
+      W += f * s_w[w];
+      r += f * s_acc[w][lane];
+    }
+    r *= W == 0.f ? 0.f : 1.f / W;  // (a NaN stays one)
+    const int b = seg / a.Hkv, h = seg % a.Hkv;
+    const size_t at = ((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD + part * 32 + lane;
+    if (a.out_fp32)
+      reinterpret_cast<float*>(a.out)[at] = r;
+    else
+      reinterpret_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(r);
+    if (a.lse_out && part == 0 && lane == 0)
+      a.lse_out[(size_t)b * a.Hq + h * a.G + hd] = W == 0.f ? -INFINITY : (M + log2f(W)) * 0.6931471805599453f;
+  }
+}
+
 }  // namespace catekv
 
 using namespace catekv;
@@ -591,7 +658,11 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
     ca.Hkv = cache->Hkv;
     ca.G = G;
     ca.out_fp32 = a.out_fp32;
-    return launch_combine(ca, n_segs, st);
+    // few pairs: the kernel that is resident early (one CTA per SM at most); many: decode.cu's, with a quarter of the CTAs
+    if ((int64_t)n_segs * G * kQ8CombineSplit <= sm_count())
+      CATEKV_CUDA_TRY(launch_pdl(q8_combine_kernel, dim3(n_segs, G, kQ8CombineSplit), dim3(kQ8CombineThreads), 0, st, ca));
+    else
+      return launch_combine(ca, n_segs, st);
   }
   return CATEKV_OK;
 }
