@@ -26,14 +26,17 @@ namespace catekv {
 
 constexpr int kQ8Warps = 4;
 constexpr int kQ8DecodeThreads = kQ8Warps * 32;
-constexpr int kQ8Stages = 3;
+constexpr int kQ8Regs = 224;  // a thread: leaves 8 K of an SM to the combine kernel beside two CTAs
 constexpr int kQ8Unit = 32;                              // rows of codes in a unit
 constexpr int kQ8TailUnit = 16;                          // rows of a tail in a unit
 constexpr int kQ8UnitBytes = 2 * kQ8Unit * kQ8RowBytes;  // K, then V
 static_assert(kQ8UnitBytes == 2 * kQ8TailUnit * kRowBytes, "both kinds of unit fill a stage");
-constexpr int kQ8MergeRegs = 36;  // 32 accumulators + m0, m1, l0, l1
-constexpr int kQ8MergeSlotBytes = kQ8MergeRegs * 32 * 4;
-constexpr int kQ8DecodeSmem = kQ8Warps * kQ8Stages * kQ8UnitBytes + 2 * kQ8MergeSlotBytes;
+constexpr int kQ8SlotFloats = kMaxG * kD;                // a slot of the merge: [8 heads][128 d]
+constexpr int q8_decode_smem(int stages) { return kQ8Warps * stages * kQ8UnitBytes + 2 * kQ8SlotFloats * 4; }
+// Units a warp has requested or under way: three, except that long streams of e4m3 codes (whose conversion is quicker, so that more requests are
+// outstanding at a time) run faster with two.  Measured per CTA share of 7 K and 14 K rows: e4m3 82.1 and 159 us with two, 84.7 and 168 us with
+// three; int8 83.0 and 161 with two, 80.7 and 161 with three.  Below 4 K rows three are as good or better (1.8 K rows, e4m3: 27.6 and 26.7).
+constexpr int kQ8LongShare = 4096;
 constexpr int32_t kQ8PlanTile = kQ8Unit;   // marks a plan of this kind (decode.cu's have kTile)
 constexpr int kQ8SegEndCharge = 512;       // rows
 constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12
@@ -110,6 +113,24 @@ __device__ __forceinline__ void q8_live_cursor(const WorkItem& w, int len, Q8Cur
   c.tail = w.last ? len % kQ8Block : 0;
   c.units = c.full + (c.tail + kQ8TailUnit - 1) / kQ8TailUnit;
 }
+// a load that stays where it is written (the compiler would move it down to its use, behind the requests that it is to overlap)
+__device__ __forceinline__ uint4 ldg128_here(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+// the group's queries, 4 x 16 bytes of this thread's head: d = 16 (c + 4 hh) + 8 e ... in x[2 hh + e]
+__device__ __forceinline__ void q8_load_q(const Q8DecodeArgs& a, int seg, int g, int c, uint4 (&x)[4]) {
+  const int b = seg / a.Hkv, h = seg % a.Hkv;
+  const uint4* p = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * a.G + g) * kD);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (g < a.G) x[i] = ldg128_here(p + 2 * (c + 4 * (i >> 1)) + (i & 1));
+  }
+}
+// a slot's place of (head, d): rotated by the head pair, so that a warp's 16-byte accesses fall in different banks
+__device__ __forceinline__ int q8_slot(int head, int d) { return head * kD + ((d + 4 * (head >> 1)) & (kD - 1)); }
 __device__ __forceinline__ WorkItem q8_load_item(const WorkItem* p) {
   const int4 x = __ldg(reinterpret_cast<const int4*>(p)), y = __ldg(reinterpret_cast<const int4*>(p) + 1);
   WorkItem w;
@@ -119,10 +140,11 @@ __device__ __forceinline__ WorkItem q8_load_item(const WorkItem* p) {
   return w;
 }
 
-template <int kType>
-__global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(const Q8DecodeArgs a) {
+template <int kType, int kQ8Stages>
+__global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_scale[kQ8Warps][kQ8Stages][2];
+  __shared__ float s_m[kQ8Warps][kMaxG], s_l[kQ8Warps][kMaxG];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, c = lane & 3;
   const int pi = g ^ ((g & 1) << 2);  // token of row g
@@ -140,7 +162,7 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
   }
   const uint32_t ring = smem_u32(smem) + warp * (kQ8Stages * kQ8UnitBytes);
   const uint32_t ring_scale = smem_u32(&s_scale[warp][0][0]);
-  float* merge = reinterpret_cast<float*>(smem + kQ8Warps * kQ8Stages * kQ8UnitBytes);
+  float* slots = reinterpret_cast<float*>(smem + kQ8Warps * kQ8Stages * kQ8UnitBytes);
 
   // ---- producer side of the warp: units warp, warp + 4, ... of every item, in order
   Q8Cursor pc = q8_plan_cursor(w0);
@@ -183,13 +205,29 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
     ++p_seq;
     p_u += kQ8Warps;
   };
+  // What the item behind the consumer's is made of, requested one item ahead: neither side then waits for a chain of loads at a change.
+  WorkItem nx;
+  int nx_len = 0;
+  int nx_item = item_begin;  // the item that these belong to
+  auto prefetch_item = [&](int item, int seg) {  // items after a CTA's first belong to consecutive segments
+    nx_item = item;
+    if (item < item_end) {
+      nx = q8_load_item(a.items + item);
+      nx_len = *reinterpret_cast<const volatile int32_t*>(a.seg_len + seg);
+    }
+  };
   auto skip_done = [&]() {  // on to the next item that has a unit for this warp
     while (p_item < item_end && p_u >= pc.units) {
       p_u = warp;
       if (++p_item < item_end) {
-        const WorkItem w = q8_load_item(a.items + p_item);
-        pc = q8_plan_cursor(w);
-        q8_live_cursor(w, *reinterpret_cast<const volatile int32_t*>(a.seg_len + w.seg), pc);
+        if (p_item == nx_item) {
+          pc = q8_plan_cursor(nx);
+          q8_live_cursor(nx, nx_len, pc);
+        } else {
+          const WorkItem w = q8_load_item(a.items + p_item);
+          pc = q8_plan_cursor(w);
+          q8_live_cursor(w, *reinterpret_cast<const volatile int32_t*>(a.seg_len + w.seg), pc);
+        }
       }
     }
   };
@@ -209,35 +247,35 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
     cp_async_commit();
   }
   pdl_wait();  // from here on: lengths, queries, and rows written by earlier kernels
-  q8_live_cursor(w0, *reinterpret_cast<const volatile int32_t*>(a.seg_len + w0.seg), pc);
+  uint4 q4[4];
+  q8_load_q(a, w0.seg, g, c, q4);
+  const int len0 = *reinterpret_cast<const volatile int32_t*>(a.seg_len + w0.seg);
+  prefetch_item(item_begin + 1, w0.seg + 1);
+  q8_live_cursor(w0, len0, pc);
+  Q8Cursor cc = pc;
   skip_done();
   for (; pre < kQ8Stages - 1; ++pre) issue();
 
   int seq = 0;
   for (int item = item_begin; item < item_end; ++item) {
-    Q8Cursor cc;
-    {
-      const WorkItem w = item == item_begin ? w0 : q8_load_item(a.items + item);
-      cc = q8_plan_cursor(w);
-      q8_live_cursor(w, *reinterpret_cast<const volatile int32_t*>(a.seg_len + w.seg), cc);
+    if (item > item_begin) {
+      cc = q8_plan_cursor(nx);
+      q8_live_cursor(nx, nx_len, cc);
+      prefetch_item(item + 1, cc.seg + 1);
     }
     const int b = cc.seg / a.Hkv, h = cc.seg % a.Hkv;
     // ---- the group's queries as B fragments: k-step 4 hh + i holds d = 16 (c + 4 hh) + 4 i + 0..3 of head g
-    const uint4* qp = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * a.G + (g < a.G ? g : 0)) * kD);
     uint32_t qf[8][2];
     float f0, f1;  // logits of heads 2c, 2c + 1 = accumulators times these (times the block's scale)
     {
       uint32_t qb[8][2];
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint4 x = g < a.G ? qp[2 * (c + 4 * hh) + e] : make_uint4(0, 0, 0, 0);
-          qb[4 * hh + 2 * e][0] = x.x;
-          qb[4 * hh + 2 * e][1] = x.y;
-          qb[4 * hh + 2 * e + 1][0] = x.z;
-          qb[4 * hh + 2 * e + 1][1] = x.w;
-        }
+      for (int i = 0; i < 4; ++i) {
+        qb[2 * i][0] = q4[i].x;
+        qb[2 * i][1] = q4[i].y;
+        qb[2 * i + 1][0] = q4[i].z;
+        qb[2 * i + 1][1] = q4[i].w;
+      }
       uint32_t mx = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) mx = __vmaxu2(__vmaxu2(mx, qb[i][0] & 0x7fff7fffu), qb[i][1] & 0x7fff7fffu);
@@ -362,7 +400,8 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
           }
         }
       } else {
-        // ---- 16 rows of the tail: bf16 on both sides, the same fragment slots
+        // ---- 16 rows of the tail: bf16 on both sides, the same fragment slots (the queries are read again)
+        const uint4* qp = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * a.G + g) * kD);
         const int left = cc.tail - (u - cc.full) * kQ8TailUnit;
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -370,11 +409,11 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int ch = 2 * (c + 4 * hh) + e;
-            const uint4 q4 = g < a.G ? qp[ch] : make_uint4(0, 0, 0, 0);
             const uint4 lo = lds128(kb + tile_off(pi, ch)), hi = lds128(kb + tile_off(pi + 8, ch));
             const uint32_t f[2][4] = {{lo.x, hi.x, lo.y, hi.y}, {lo.z, hi.z, lo.w, hi.w}};
-            mma_bf16_16816(s, f[0], q4.x, q4.y);
-            mma_bf16_16816(s, f[1], q4.z, q4.w);
+            const uint4 x = g < a.G ? qp[ch] : make_uint4(0, 0, 0, 0);
+            mma_bf16_16816(s, f[0], x.x, x.y);
+            mma_bf16_16816(s, f[1], x.z, x.w);
           }
         const bool v_lo = pi < left, v_hi = pi + 8 < left;
         const float x0 = v_lo ? s[0] * a.scale_log2 : -INFINITY, x1 = v_lo ? s[1] * a.scale_log2 : -INFINITY;
@@ -419,82 +458,71 @@ __global__ void __launch_bounds__(kQ8DecodeThreads, 2) q8_decode_partial_kernel(
       }
     }
 
-    // ---- end of the piece: finish the row sums, put the accumulators in units of 1, merge the four warps, write the result
+    // ---- end of the piece: merge the four warps (warps 0 and 1 fill a slot each, 2 and 3 add to them, everybody writes a part of the sum)
+    if (item + 1 < item_end) q8_load_q(a, cc.seg + 1, g, c, q4);  // on their way during the merge
 #pragma unroll
     for (int sh = 4; sh <= 16; sh <<= 1) {
       l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
       l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
     }
+    if (g == 0) {
+      s_m[warp][2 * c] = m0;
+      s_m[warp][2 * c + 1] = m1;
+      s_l[warp][2 * c] = l0;
+      s_l[warp][2 * c + 1] = l1;
+    }
+    __syncthreads();  // (and the slots of the piece before have been read)
+    float al[2];  // from this warp's unit and maximum to 1 and the CTA's maximum
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int e = 0; e < 2; ++e) {
+      float M = s_m[0][2 * c + e];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[i][j] *= vr;
+      for (int w = 1; w < kQ8Warps; ++w) M = fmaxf(M, s_m[w][2 * c + e]);
+      const float m = e ? m1 : m0;
+      al[e] = m == M ? vr : fast_exp2(m - M) * vr;
+    }
+    float* slot = slots + (warp & 1) * kQ8SlotFloats;
 #pragma unroll
-    for (int lvl = 0; lvl < 2; ++lvl) {
-      const int stride = 1 << lvl;
-      const bool writer = (warp & (2 * stride - 1)) == stride;  // level 0: warps 1, 3; level 1: warp 2
-      const bool reader = (warp & (2 * stride - 1)) == 0;       // level 0: warps 0, 2; level 1: warp 0
-      float* mb = merge + (warp >> (lvl + 1)) * (kQ8MergeRegs * 32);
-      if (writer) {
+    for (int pass = 0; pass < 2; ++pass) {
+      if ((warp >> 1) == pass) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) mb[(i * 4 + j) * 32 + lane] = o[i][j];
-        mb[32 * 32 + lane] = m0;
-        mb[33 * 32 + lane] = m1;
-        mb[34 * 32 + lane] = l0;
-        mb[35 * 32 + lane] = l1;
+          for (int j = 0; j < 8; j += 2) {  // o[j][e], o[j][2 + e]: d = 16 g + 2 j, + 1 of head 2 c + e
+            float4* p = reinterpret_cast<float4*>(slot + q8_slot(2 * c + e, 16 * g + 2 * j));
+            float4 v = make_float4(o[j][e] * al[e], o[j][2 + e] * al[e], o[j + 1][e] * al[e], o[j + 1][2 + e] * al[e]);
+            if (pass == 1) {
+              const float4 x = *p;
+              v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+            }
+            *p = v;
+          }
       }
       __syncthreads();
-      if (reader) {
-        const float om0 = mb[32 * 32 + lane], om1 = mb[33 * 32 + lane];
-        const float ol0 = mb[34 * 32 + lane], ol1 = mb[35 * 32 + lane];
-        const float mn0 = fmaxf(m0, om0), mn1 = fmaxf(m1, om1);
-        const float a0 = (m0 == -INFINITY) ? 0.f : fast_exp2(m0 - mn0);
-        const float b0 = (om0 == -INFINITY) ? 0.f : fast_exp2(om0 - mn0);
-        const float a1 = (m1 == -INFINITY) ? 0.f : fast_exp2(m1 - mn1);
-        const float b1 = (om1 == -INFINITY) ? 0.f : fast_exp2(om1 - mn1);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          o[i][0] = o[i][0] * a0 + mb[(i * 4 + 0) * 32 + lane] * b0;
-          o[i][1] = o[i][1] * a1 + mb[(i * 4 + 1) * 32 + lane] * b1;
-          o[i][2] = o[i][2] * a0 + mb[(i * 4 + 2) * 32 + lane] * b0;
-          o[i][3] = o[i][3] * a1 + mb[(i * 4 + 3) * 32 + lane] * b1;
-        }
-        l0 = l0 * a0 + ol0 * b0;
-        l1 = l1 * a1 + ol1 * b1;
-        m0 = mn0;
-        m1 = mn1;
-      }
-      __syncthreads();  // slot 0 is rewritten: by warp 2 at the next level, by warp 1 at the next piece
     }
-    if (warp == 0) {
-      // o[j][0], o[j][2]: d = 16 g + 2 j, + 1 of head 2c;  o[j][1], o[j][3]: of head 2c + 1
+    for (int hd = warp; hd < a.G; hd += kQ8Warps) {
+      float M = s_m[0][hd];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int hd = 2 * c + e;
-        if (hd >= a.G) continue;
-        const float l = e ? l1 : l0, m = e ? m1 : m0;
-        const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
-        const float lse = l == 0.f ? -INFINITY : m - kQ8PBits + log2f(l);
-        float* po = cc.slot >= 0 ? a.part_o + ((size_t)cc.slot * kMaxG + hd) * kD + 16 * g
-                                 : reinterpret_cast<float*>(a.out) + (((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD + 16 * g);
-        if (cc.slot >= 0 || a.out_fp32) {
+      for (int w = 1; w < kQ8Warps; ++w) M = fmaxf(M, s_m[w][hd]);
+      float l = 0.f;
 #pragma unroll
-          for (int j = 0; j < 8; j += 2)
-            reinterpret_cast<float4*>(po)[j / 2] = make_float4(o[j][e] * inv, o[j][2 + e] * inv, o[j + 1][e] * inv, o[j + 1][2 + e] * inv);
-        } else {
-          uint4* pb = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.out) + (((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD + 16 * g));
-#pragma unroll
-          for (int j = 0; j < 8; j += 4)
-            pb[j / 4] = make_uint4(pack_bf16(o[j][e] * inv, o[j][2 + e] * inv), pack_bf16(o[j + 1][e] * inv, o[j + 1][2 + e] * inv),
-                                   pack_bf16(o[j + 2][e] * inv, o[j + 2][2 + e] * inv), pack_bf16(o[j + 3][e] * inv, o[j + 3][2 + e] * inv));
-        }
-        if (g == 0) {
-          // the combine pass takes an infinite LSE as the one partial that counts: a NaN (from a block with the scale NaN) reaches the output
-          if (cc.slot >= 0) a.part_lse[(size_t)cc.slot * kMaxG + hd] = lse == lse ? lse : INFINITY;
-          else if (a.lse_out) a.lse_out[(size_t)b * a.Hq + h * a.G + hd] = lse * 0.6931471805599453f;
-        }
+      for (int w = 0; w < kQ8Warps; ++w) l += s_m[w][hd] == M ? s_l[w][hd] : s_l[w][hd] * fast_exp2(s_m[w][hd] - M);
+      const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
+      const float lse = l == 0.f ? -INFINITY : M - kQ8PBits + log2f(l);
+      const float4 x = *reinterpret_cast<const float4*>(slots + q8_slot(hd, 4 * lane));
+      const float4 y = *reinterpret_cast<const float4*>(slots + kQ8SlotFloats + q8_slot(hd, 4 * lane));
+      const float4 v = make_float4((x.x + y.x) * inv, (x.y + y.y) * inv, (x.z + y.z) * inv, (x.w + y.w) * inv);
+      const size_t at = ((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD;
+      if (cc.slot >= 0)
+        reinterpret_cast<float4*>(a.part_o + ((size_t)cc.slot * kMaxG + hd) * kD)[lane] = v;
+      else if (a.out_fp32)
+        reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at)[lane] = v;
+      else
+        reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + at)[lane] = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+      if (lane == 0) {
+        // the combine pass takes an infinite LSE as the one partial that counts: a NaN (from a block with the scale NaN) reaches the output
+        if (cc.slot >= 0) a.part_lse[(size_t)cc.slot * kMaxG + hd] = lse == lse ? lse : INFINITY;
+        else if (a.lse_out) a.lse_out[(size_t)b * a.Hq + h * a.G + hd] = lse * 0.6931471805599453f;
       }
     }
   }
@@ -570,13 +598,33 @@ __global__ void __launch_bounds__(kQ8CombineThreads, 7) q8_combine_kernel(const 
 
 using namespace catekv;
 
-extern "C" int catekv_q8_decode_num_ctas(void) {
-  int dev = 0, sms = 0, per_sm = 0;
+// the kernels' shared-memory limits, once per device
+template <int kType, int kStages>
+static cudaError_t q8_allow_smem() {
+  return cudaFuncSetAttribute(q8_decode_partial_kernel<kType, kStages>, cudaFuncAttributeMaxDynamicSharedMemorySize, q8_decode_smem(kStages));
+}
+static int q8_decode_attributes() {
+  static std::atomic<bool> attr_set[64];
+  int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
-  CATEKV_CUDA_TRY(cudaFuncSetAttribute(q8_decode_partial_kernel<CATEKV_Q8_E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ8DecodeSmem));
-  CATEKV_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  CATEKV_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, q8_decode_partial_kernel<CATEKV_Q8_E4M3>, kQ8DecodeThreads, kQ8DecodeSmem));
-  return sms * (per_sm < 1 ? 1 : per_sm);
+  if (dev >= 0 && dev < 64 && attr_set[dev].load(std::memory_order_acquire)) return CATEKV_OK;
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 2>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 3>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_INT8, 3>()));
+  if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+  return CATEKV_OK;
+}
+template <int kType, int kStages>
+static cudaError_t q8_launch_partials(const Q8DecodeArgs& a, int num_ctas, cudaStream_t st) {
+  return launch_pdl(q8_decode_partial_kernel<kType, kStages>, dim3(num_ctas), dim3(kQ8DecodeThreads), q8_decode_smem(kStages), st, a);
+}
+
+extern "C" int catekv_q8_decode_num_ctas(void) {
+  int rc = q8_decode_attributes();
+  if (rc) return rc;
+  int per_sm = 0;
+  CATEKV_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, q8_decode_partial_kernel<CATEKV_Q8_E4M3, 3>, kQ8DecodeThreads, q8_decode_smem(3)));
+  return sm_count() * (per_sm < 1 ? 1 : per_sm);
 }
 
 extern "C" int catekv_q8_decode_plan(const catekv_q8_cache* cache, int32_t num_ctas, void* plan_host, void* plan_dev,
@@ -615,14 +663,8 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
   if (ws_bytes < ws_layout(n_segs, hdr->num_ctas, &off_lse)) return CATEKV_ERR_WORKSPACE;
   cudaStream_t st = (cudaStream_t)stream;
   const uint8_t* pd = (const uint8_t*)plan_dev;
-  static std::atomic<bool> attr_set[64];
-  int dev = 0;
-  CATEKV_CUDA_TRY(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(q8_decode_partial_kernel<CATEKV_Q8_E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ8DecodeSmem));
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(q8_decode_partial_kernel<CATEKV_Q8_INT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQ8DecodeSmem));
-    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
-  }
+  rc = q8_decode_attributes();
+  if (rc) return rc;
   Q8DecodeArgs a;
   a.k_pool = (const uint8_t*)cache->k_pool;
   a.v_pool = (const uint8_t*)cache->v_pool;
@@ -643,10 +685,12 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
   a.out = out;
   a.out_fp32 = out_dtype == CATEKV_OUT_FP32;
   a.lse_out = lse_out;
-  if (cache->dtype == CATEKV_Q8_E4M3)
-    CATEKV_CUDA_TRY(launch_pdl(q8_decode_partial_kernel<CATEKV_Q8_E4M3>, dim3(hdr->num_ctas), dim3(kQ8DecodeThreads), kQ8DecodeSmem, st, a));
+  if (cache->dtype == CATEKV_Q8_INT8)
+    CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_INT8, 3>(a, hdr->num_ctas, st)));
+  else if (hdr->total_rows >= (int64_t)kQ8LongShare * hdr->num_ctas)
+    CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 2>(a, hdr->num_ctas, st)));
   else
-    CATEKV_CUDA_TRY(launch_pdl(q8_decode_partial_kernel<CATEKV_Q8_INT8>, dim3(hdr->num_ctas), dim3(kQ8DecodeThreads), kQ8DecodeSmem, st, a));
+    CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 3>(a, hdr->num_ctas, st)));
   if (hdr->n_slots > 0) {
     CombineArgs ca;
     ca.seg_info = (const SegInfo*)(pd + L.off_seg);
