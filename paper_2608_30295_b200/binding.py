@@ -618,24 +618,29 @@ class Q8Cache:
         self.seg_len_dev.copy_(torch.from_numpy(self.seg_len))
 
 
-def _here(where: str, *tensors):
-    """The library works on the current device and stream: a buffer that lives elsewhere is refused."""
+_OUT_CODE = {torch.bfloat16: OUT_BF16, torch.float32: OUT_FP32}
+
+
+def _stream_here(where: str, *tensors) -> int:
+    """The current stream, after a look at where the buffers live: the library works on the current device, and one that is
+    elsewhere is refused."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise CatekvError(ERR_INVALID_ARG, where)
+    return _stream() if _raw_stream is None else _raw_stream(here)
 
 
 def catekv_q8_quantize(src: Cache, dst: Q8Cache):
-    _here("catekv_q8_quantize", src.k_pool, dst.k_pool)
-    _check(_lib.catekv_q8_quantize(C.byref(src.struct), C.byref(dst.struct), _stream()), "catekv_q8_quantize")
+    st = _stream_here("catekv_q8_quantize", src.k_pool, dst.k_pool)
+    _check(_lib.catekv_q8_quantize(C.byref(src.struct), C.byref(dst.struct), st), "catekv_q8_quantize")
 
 
 def catekv_q8_append(cache: Q8Cache, k_new: torch.Tensor, v_new: torch.Tensor):
-    assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.dtype == v_new.dtype == torch.bfloat16
+    assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.dtype is v_new.dtype is torch.bfloat16
     assert k_new.numel() == v_new.numel() == cache.B * cache.Hkv * cache.d
-    _here("catekv_q8_append", cache.k_pool, k_new, v_new)
-    _check(_lib.catekv_q8_append(C.byref(cache.struct), k_new.data_ptr(), v_new.data_ptr(), _stream()), "catekv_q8_append")
+    st = _stream_here("catekv_q8_append", cache.k_pool, k_new, v_new)
+    _check(_lib.catekv_q8_append(C.byref(cache.struct), k_new.data_ptr(), v_new.data_ptr(), st), "catekv_q8_append")
 
 
 def catekv_q8_cache_advance(cache: Q8Cache, n_tokens: int = 1):
@@ -657,10 +662,18 @@ def catekv_q8_decode_plan(cache: Q8Cache, plan: DecodePlan):
 
 def catekv_q8_decode_attn(cache: Q8Cache, q: torch.Tensor, plan: DecodePlan, out: torch.Tensor,
                           lse_out: Optional[torch.Tensor] = None, sm_scale: float = 0.0):
-    assert q.shape[0] == cache.B and q.shape[2] == cache.d and out.shape == q.shape
-    assert lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and lse_out.numel() == q.shape[0] * q.shape[1])
-    _here("catekv_q8_decode_attn", cache.k_pool, q, out, lse_out, plan.dev)
-    _decode_call(_lib.catekv_q8_decode_attn, "catekv_q8_decode_attn", cache, q, plan, out, lse_out, sm_scale)
+    B, Hq, d = q.shape
+    assert B == cache.B and d == cache.d and q.dtype is torch.bfloat16 and q.is_contiguous()
+    assert out.shape == q.shape and out.is_contiguous()
+    assert lse_out is None or (lse_out.dtype is torch.float32 and lse_out.is_contiguous() and lse_out.numel() == B * Hq)
+    od = _OUT_CODE.get(out.dtype)
+    if od is None:
+        raise TypeError("out must be bf16 or fp32")
+    st = _stream_here("catekv_q8_decode_attn", cache.k_pool, q, out, lse_out, plan.dev)
+    rc = _lib.catekv_q8_decode_attn(C.byref(cache.struct), q.data_ptr(), Hq, sm_scale, out.data_ptr(), od, _dev_ptr(lse_out),
+                                    plan.host.data_ptr(), plan.dev.data_ptr(), plan.bytes, plan.ws.data_ptr(), plan.ws_bytes, st)
+    if rc != OK:
+        raise CatekvError(rc, "catekv_q8_decode_attn")
 
 
 # ---------------------------------------------------------------- eviction by accumulated attention weight
@@ -678,16 +691,20 @@ def catekv_decode_attn_weighted(cache: Cache, q: torch.Tensor, plan: DecodePlan,
                                 decay: float, ws: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
                                 sm_scale: float = 0.0):
     """catekv_decode_attn that also updates `weights` (float32 [total_rows], one per pool row)."""
-    assert q.is_contiguous() and out.is_contiguous() and q.dtype == torch.bfloat16 and out.shape == q.shape
-    assert weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() >= cache.total_rows
-    assert lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and lse_out.numel() == q.shape[0] * q.shape[1])
-    if out.dtype not in (torch.bfloat16, torch.float32):
+    B, Hq, d = q.shape
+    assert B == cache.B and d == cache.d and q.dtype is torch.bfloat16 and q.is_contiguous()
+    assert out.shape == q.shape and out.is_contiguous()
+    assert weights.dtype is torch.float32 and weights.is_contiguous() and weights.numel() >= cache.total_rows
+    assert lse_out is None or (lse_out.dtype is torch.float32 and lse_out.is_contiguous() and lse_out.numel() == B * Hq)
+    od = _OUT_CODE.get(out.dtype)
+    if od is None:
         raise TypeError("out must be bf16 or fp32")
-    _here("catekv_decode_attn_weighted", cache.k_pool, plan.dev, q, out, weights, ws, lse_out)
-    _check(_lib.catekv_decode_attn_weighted(C.byref(cache.struct), q.data_ptr(), q.shape[1], sm_scale, out.data_ptr(),
-                                            OUT_BF16 if out.dtype == torch.bfloat16 else OUT_FP32, _dev_ptr(lse_out),
-                                            weights.data_ptr(), decay, plan.host.data_ptr(), plan.dev.data_ptr(), plan.bytes,
-                                            ws.data_ptr(), ws.numel(), _stream()), "catekv_decode_attn_weighted")
+    st = _stream_here("catekv_decode_attn_weighted", cache.k_pool, plan.dev, q, out, weights, ws, lse_out)
+    rc = _lib.catekv_decode_attn_weighted(C.byref(cache.struct), q.data_ptr(), Hq, sm_scale, out.data_ptr(), od, _dev_ptr(lse_out),
+                                          weights.data_ptr(), decay, plan.host.data_ptr(), plan.dev.data_ptr(), plan.bytes,
+                                          ws.data_ptr(), ws.numel(), st)
+    if rc != OK:
+        raise CatekvError(rc, "catekv_decode_attn_weighted")
 
 
 def evict_workspace(cache: Cache) -> torch.Tensor:
@@ -715,17 +732,18 @@ def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, s
     if dst is None:
         dst, dst_weights = cache, weights
     evict_mask = np.ascontiguousarray(evict_mask, dtype=np.uint8).reshape(-1)
-    assert evict_mask.size == cache.B * cache.Hkv
-    for w, c in ((weights, cache), (dst_weights, dst)):
-        assert w.dtype == torch.float32 and w.is_contiguous() and w.numel() >= c.total_rows
+    n = cache.B * cache.Hkv
+    assert evict_mask.size == n
+    assert weights.dtype is dst_weights.dtype is torch.float32 and weights.is_contiguous() and dst_weights.is_contiguous()
+    assert weights.numel() >= cache.total_rows and dst_weights.numel() >= dst.total_rows
     stride = 0
     if idx_out is not None:
-        assert idx_out.dtype == torch.int32 and idx_out.shape[0] == cache.B * cache.Hkv and idx_out.stride(1) == 1
-        stride = idx_out.stride(0) if idx_out.shape[0] > 1 else idx_out.shape[1]
+        assert idx_out.dtype is torch.int32 and idx_out.shape[0] == n and idx_out.stride(1) == 1
+        stride = idx_out.stride(0) if n > 1 else idx_out.shape[1]
     if ws is None:
         ws = evict_workspace(cache)
-    _here("catekv_evict", cache.k_pool, weights, dst_weights, dst.k_pool, idx_out, ws)
-    _check(_lib.catekv_evict(C.byref(cache.struct), weights.data_ptr(), _np_ptr(evict_mask), budget, sink, local,
-                             C.byref(dst.struct), dst_weights.data_ptr(), _dev_ptr(idx_out), stride, ws.data_ptr(), ws.numel(),
-                             _stream()), "catekv_evict")
+    st = _stream_here("catekv_evict", cache.k_pool, weights, dst_weights, dst.k_pool, idx_out, ws)
+    _check(_lib.catekv_evict(C.byref(cache.struct), weights.data_ptr(), evict_mask.tobytes(), budget, sink, local,
+                             C.byref(dst.struct), dst_weights.data_ptr(), _dev_ptr(idx_out), stride, ws.data_ptr(), ws.numel(), st),
+           "catekv_evict")
     return ws

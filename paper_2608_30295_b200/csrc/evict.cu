@@ -50,16 +50,20 @@ __host__ __device__ inline EvSeg evict_decide(int n, bool masked, const EvParams
 // ------------------------------------------------------------------------------------------
 // Selection
 // ------------------------------------------------------------------------------------------
-// A cluster of CL CTAs per masked segment (1 where the list is short), each with a share of the candidates in shared memory as sortable patterns
-// (a non-negative float's bits order like the float).  The pattern of the k-th largest is found from the top, 11 + 11 + 9 bits, with a histogram
-// per step: weights spread over many powers of two, so the first step (exponent and three bits) already leaves a few per cent.  A histogram of its
-// own per step means one cluster barrier per step.  What is above the pattern is kept, of what equals it the first in row order; a
-// warp's votes over 32 consecutive candidates place them, so that the list is written in order and coalesced.
+// A cluster of CL CTAs per masked segment (1 where the list is short), each with a share of the candidates as sortable patterns (a non-negative
+// float's bits order like the float): in registers up to 8 per thread, else in shared memory.  The pattern of the k-th largest is found from
+// the top, 11 + 11 + 9 bits, with a histogram per step: weights spread over many powers of two, so the first step (exponent and three bits)
+// already leaves a few per cent.  The CTAs look at one another's histograms in two looks of a warp, 32 sums of 64 bins and then the 64 bins of one, and
+// as every step has a histogram of its own, with one cluster barrier.  What is above the pattern is kept, of what equals it the first in row
+// order; a warp's votes over 32 consecutive candidates place them, so that the list is written in order.
 constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBins = 2048;
-constexpr int kEvClusterFrom = 16384;  // candidates from which a cluster shares a list
-constexpr int kEvStageMax = 49152;  // candidates a CTA may stage (192 KB)
+constexpr int kEvGroup = kEvBins / 32;        // bins of a first look's sum
+constexpr int kEvRegs = 8;                    // candidates of a thread held in registers
+constexpr int kEvRegShare = kEvRegs * kEvThreads;
+constexpr int kEvStageMax = 49152;            // candidates a CTA may stage in shared memory (192 KB)
+static_assert(kEvRegs * 32 <= kEvThreads, "one thread per word of votes");
 __device__ __forceinline__ int ev_shift(int pass) { return pass == 0 ? 20 : pass == 1 ? 9 : 0; }
 
 struct EvSelectArgs {
@@ -78,23 +82,36 @@ struct EvSelectArgs {
 __device__ __forceinline__ unsigned int ev_pattern(float x) {  // negative as 0, NaN as infinite
   return x != x ? 0x7f800000u : (x > 0.f ? __float_as_uint(x) : 0u);
 }
+// inclusive sum over the warp's lanes 0 .. lane
+__device__ __forceinline__ unsigned int ev_scan(unsigned int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned int y = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
 
-template <int CL>
+template <int CL, bool kReg>
 __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_constant__ EvSelectArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
   const int seg = a.list.seg[blockIdx.x / CL];
   const int rank = CL > 1 ? (int)cluster.block_rank() : 0;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   __shared__ unsigned int hist[3][kEvBins];
-  __shared__ unsigned int s_warp[kEvWarps];
+  __shared__ unsigned int s_sum[3][32];               // sums of 64 bins over the cluster, larger ones first
   __shared__ unsigned int s_gt[kEvWarps], s_eq[kEvWarps];
+  __shared__ unsigned int s_word[kEvRegs * 32];       // votes of 32 consecutive candidates: counts above / at the threshold
   __shared__ unsigned int s_sel[3];
-  __shared__ unsigned int s_tot[2];  // this CTA's counts above and at the threshold, read by its peers
+  __shared__ unsigned int s_tot[2];                   // this CTA's counts above and at the threshold, read by its peers
   extern __shared__ __align__(16) unsigned int key[];
   pdl_launch_dependents();
   for (int i = tid; i < 3 * kEvBins; i += kEvThreads) (&hist[0][0])[i] = 0u;
+  if (tid < 96) (&s_sum[0][0])[tid] = 0u;
+  if (CL > 1) cluster.sync();  // clear everywhere before a peer adds to it
   pdl_wait();
-  const EvSeg s = evict_decide(a.seg_len[seg], true, a.p);
+  const int n_rows = a.seg_len[seg], off = a.seg_off[seg];  // (one trip to memory)
+  const EvSeg s = evict_decide(n_rows, true, a.p);
   if (rank == 0 && tid == 0) a.segs[seg] = s;
   if (s.keep_all) return;  // the whole cluster
   auto cluster_sync = [&]() {
@@ -106,27 +123,34 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
     const int n_pool = s.cand_end - S;
     const int per = ((n_pool + CL - 1) / CL + 31) / 32 * 32;
     const int lo = min(n_pool, rank * per), n_loc = min(n_pool, lo + per) - lo;
-    const float* w = a.weights + (int64_t)a.seg_off[seg] + S + lo;
+    const float* w = a.weights + (int64_t)off + S + lo;
     const bool staged = n_loc <= a.stage;
     auto ld = [&](int i) { return staged ? key[i] : ev_pattern(w[i]); };
+    unsigned int mine[kEvRegs];  // kReg: candidate e * 1024 + tid
+    if (kReg) {
+#pragma unroll
+      for (int e = 0; e < kEvRegs; ++e) mine[e] = e * kEvThreads + tid < n_loc ? ev_pattern(w[e * kEvThreads + tid]) : 0u;
+    }
     unsigned int prefix = 0u, pmask = 0u, need = (unsigned int)s.k_sel;
     __syncthreads();  // the histograms are clear
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = ev_shift(pass);
       const unsigned int dmask = pass == 2 ? 511u : 2047u;
       unsigned int* h = hist[pass];
-      auto count = [&](bool in, unsigned int v) {
+      auto count = [&](bool in, unsigned int v) {  // by whole warps
         const bool hit = in && (v & pmask) == prefix;
-        const unsigned int d = hit ? (v >> shift) & dmask : 0xffffffffu;
-        int same;
-        __match_all_sync(0xffffffffu, d, &same);
-        if (same) {  // equal weights by the warp (rows that no query has looked at): one addition
-          if (hit && lane == 0) atomicAdd(&h[d], 32u);
+        const unsigned int d = (v >> shift) & dmask, d0 = __shfl_sync(0xffffffffu, d, 0);
+        if (__all_sync(0xffffffffu, hit && d == d0)) {
+          if (lane == 0) atomicAdd(&h[d], 32u);  // equal weights (rows that no query has looked at): one addition
         } else if (hit) {
           atomicAdd(&h[d], 1u);
         }
       };
-      if (pass == 0) {  // the first step brings the candidates in, four loads in flight
+      if (kReg) {
+#pragma unroll
+        for (int e = 0; e < kEvRegs; ++e)
+          if (e * kEvThreads < n_loc) count(e * kEvThreads + tid < n_loc, mine[e]);
+      } else if (pass == 0) {  // the first step brings the candidates in, four loads in flight
         for (int i0 = 0; i0 < n_loc; i0 += 4 * kEvThreads) {
           unsigned int v[4];
 #pragma unroll
@@ -144,89 +168,147 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(const __grid_c
       } else {
         for (int i0 = 0; i0 < n_loc; i0 += kEvThreads) count(i0 + tid < n_loc, i0 + tid < n_loc ? ld(i0 + tid) : 0u);
       }
-      cluster_sync();  // all histograms of this step complete
-      // thread t: bins 2047 - 2t and 2046 - 2t, larger digits first
-      unsigned int c1 = 0u, c0 = 0u;
-      const int b1 = kEvBins - 1 - 2 * tid;
-#pragma unroll
-      for (int r = 0; r < CL; ++r) {
-        const uint2 x = *reinterpret_cast<const uint2*>(CL > 1 ? cluster.map_shared_rank(&h[b1 - 1], r) : &h[b1 - 1]);
-        c0 += x.x;
-        c1 += x.y;
-      }
-      unsigned int inc = c0 + c1;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-      }
-      if (lane == 31) s_warp[warp] = inc;
       __syncthreads();
-      inc += __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0u);
-      const unsigned int before = inc - c0 - c1;
-      if (before < need && need <= inc) {  // one of this thread's bins holds the need-th largest
-        const bool upper = need <= before + c1;
-        s_sel[0] = (unsigned int)(upper ? b1 : b1 - 1);
-        s_sel[1] = need - before - (upper ? 0u : c1);
-        s_sel[2] = upper ? c1 : c0;
+      {
+        const unsigned int* p = &h[(31 - warp) * kEvGroup + 2 * lane];
+        const unsigned int t = __reduce_add_sync(0xffffffffu, p[0] + p[1]);
+        // lane r adds it to CTA r's sum: after the barrier every CTA has the cluster's
+        if (CL > 1) {
+          if (lane < CL && t) atomicAdd(cluster.map_shared_rank(&s_sum[pass][warp], lane), t);
+        } else if (lane == 0) {
+          s_sum[pass][warp] = t;
+        }
+      }
+      cluster_sync();  // all histograms and sums of this step complete
+      if (warp == 0) {
+        const unsigned int c = s_sum[pass][lane];
+        unsigned int inc = ev_scan(c, lane);
+        const int gsel = __ffs(__ballot_sync(0xffffffffu, need <= inc)) - 1;  // the first sum that reaches `need`
+        const unsigned int before = __shfl_sync(0xffffffffu, inc - c, gsel);
+        // lane l: bins 63 - 2 l and 62 - 2 l of the group
+        const int b1 = (31 - gsel) * kEvGroup + kEvGroup - 1 - 2 * lane;
+        unsigned int c1 = 0u, c0 = 0u;
+#pragma unroll
+        for (int r = 0; r < CL; ++r) {
+          const uint2 x = *reinterpret_cast<const uint2*>(CL > 1 ? cluster.map_shared_rank(&h[b1 - 1], r) : &h[b1 - 1]);
+          c0 += x.x;
+          c1 += x.y;
+        }
+        inc = before + ev_scan(c0 + c1, lane);
+        const unsigned int ex = inc - c0 - c1;
+        if (ex < need && need <= inc) {  // one of this lane's bins holds the need-th largest
+          const bool upper = need <= ex + c1;
+          s_sel[0] = (unsigned int)(upper ? b1 : b1 - 1);
+          s_sel[1] = need - ex - (upper ? 0u : c1);
+          s_sel[2] = upper ? c1 : c0;
+        }
       }
       __syncthreads();
       prefix |= s_sel[0] << shift;
       pmask |= dmask << shift;
       need = s_sel[1];
       const bool whole = s_sel[2] == need;
-      __syncthreads();  // s_sel and s_warp are written again by the next step
       if (whole) break;  // everything in the bin is kept: no need to look closer
+      // (s_sel is written again behind the next step's barriers)
     }
     // kept: patterns above the prefix, and the first `need` of those with it
     const unsigned int top = prefix | (~pmask & 0x7fffffffu);  // (patterns are below 2^31)
-    const int chunk = (n_loc + kEvThreads - 1) / kEvThreads * 32;  // a warp's consecutive candidates
-    const int w0 = min(n_loc, warp * chunk), w1 = min(n_loc, w0 + chunk);
-    unsigned int gt = 0u, eq = 0u;
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-      const bool in = i0 + lane < w1;
-      const unsigned int v = in ? ld(i0 + lane) : 0u;
-      gt += __popc(__ballot_sync(0xffffffffu, in && v > top));
-      eq += __popc(__ballot_sync(0xffffffffu, in && (v & pmask) == prefix));
-    }
-    if (lane == 0) {
-      s_gt[warp] = gt;
-      s_eq[warp] = eq;
-    }
-    __syncthreads();
-    const unsigned int all_gt = __reduce_add_sync(0xffffffffu, s_gt[lane]), all_eq = __reduce_add_sync(0xffffffffu, s_eq[lane]);
-    unsigned int gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_gt[lane] : 0u);
-    unsigned int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_eq[lane] : 0u);
-    if (CL > 1) {
-      if (tid == 0) {
-        s_tot[0] = all_gt;
-        s_tot[1] = all_eq;
-      }
-      cluster_sync();
-      for (int r = 0; r < rank; ++r) {
-        const unsigned int* t = cluster.map_shared_rank(&s_tot[0], r);
-        gt_before += t[0];
-        eq_before += t[1];
-      }
-    }
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-      const bool in = i0 + lane < w1;
-      const unsigned int v = in ? ld(i0 + lane) : 0u;
-      const bool g = in && v > top, q = in && (v & pmask) == prefix;
-      const unsigned int mg = __ballot_sync(0xffffffffu, g), mq = __ballot_sync(0xffffffffu, q);
-      const unsigned int low = (1u << lane) - 1u;
-      const unsigned int my_eq = eq_before + __popc(mq & low);
-      if (g || (q && my_eq < need)) {
-        int r = S + (int)(gt_before + __popc(mg & low) + min(my_eq, need));
+    auto emit = [&](int c, unsigned int rnk) {  // candidate c of this share is the rnk-th kept
+      int r = S + (int)rnk;
 #ifdef CATEKV_CHECKED
-        r = checked_clamp(r, S, s.kept - a.p.local - 1, a.chk, kKidEvict, seg);
+      r = checked_clamp(r, S, s.kept - a.p.local - 1, a.chk, kKidEvict, seg);
 #endif
-        idx[r] = S + lo + i0 + lane;
+      idx[r] = S + lo + c;
+    };
+    // counts before a position of the share, and of the shares before it
+    unsigned int gt_before = 0u, eq_before = 0u;
+    auto add_peers = [&](unsigned int all_gt, unsigned int all_eq) {
+      if (CL > 1) {
+        if (tid == 0) {
+          s_tot[0] = all_gt;
+          s_tot[1] = all_eq;
+        }
+        cluster_sync();
+        unsigned int tg = 0u, te = 0u;
+        if (lane < rank) {
+          const unsigned int* t = cluster.map_shared_rank(&s_tot[0], lane);
+          tg = t[0];
+          te = t[1];
+        }
+        gt_before += __reduce_add_sync(0xffffffffu, tg);
+        eq_before += __reduce_add_sync(0xffffffffu, te);
+        // this thread's last look at a peer's shared memory lies behind it; it waits for the others' before it leaves
+        asm volatile("barrier.cluster.arrive.relaxed;\n" ::: "memory");
       }
-      gt_before += __popc(mg);
-      eq_before += __popc(mq);
+    };
+    const unsigned int low = (1u << lane) - 1u;
+    if (kReg) {
+      // word e * 32 + warp: the votes of candidates e * 1024 + 32 warp ...
+#pragma unroll
+      for (int e = 0; e < kEvRegs; ++e) {
+        unsigned int both = 0u;
+        if (e * kEvThreads < n_loc) {
+          const bool in = e * kEvThreads + tid < n_loc;
+          const unsigned int mg = __ballot_sync(0xffffffffu, in && mine[e] > top);
+          const unsigned int mq = __ballot_sync(0xffffffffu, in && (mine[e] & pmask) == prefix);
+          both = (unsigned int)__popc(mg) | ((unsigned int)__popc(mq) << 16);
+        }
+        if (lane == 0) s_word[e * 32 + warp] = both;
+      }
+      __syncthreads();
+      if (warp < kEvRegs) {  // exclusive sums within a warp's 32 words (both counts stay below 2^16), totals per warp
+        const unsigned int v = s_word[tid], inc = ev_scan(v, lane);
+        s_word[tid] = inc - v;
+        if (lane == 31) {
+          s_gt[warp] = inc & 0xffffu;
+          s_eq[warp] = inc >> 16;
+        }
+      }
+      __syncthreads();
+      const unsigned int tg = lane < kEvRegs ? s_gt[lane] : 0u, te = lane < kEvRegs ? s_eq[lane] : 0u;
+      const unsigned int ig = ev_scan(tg, lane), ie = ev_scan(te, lane);
+      add_peers(__shfl_sync(0xffffffffu, ig, 31), __shfl_sync(0xffffffffu, ie, 31));
+#pragma unroll
+      for (int e = 0; e < kEvRegs; ++e) {
+        if (e * kEvThreads >= n_loc) break;
+        const bool in = e * kEvThreads + tid < n_loc;
+        const bool g = in && mine[e] > top, q = in && (mine[e] & pmask) == prefix;
+        const unsigned int mg = __ballot_sync(0xffffffffu, g), mq = __ballot_sync(0xffffffffu, q);
+        const unsigned int word = s_word[e * 32 + warp];
+        const unsigned int gb = gt_before + __shfl_sync(0xffffffffu, ig - tg, e) + (word & 0xffffu) + __popc(mg & low);
+        const unsigned int eb = eq_before + __shfl_sync(0xffffffffu, ie - te, e) + (word >> 16) + __popc(mq & low);
+        if (g || (q && eb < need)) emit(e * kEvThreads + tid, gb + min(eb, need));
+      }
+    } else {
+      const int chunk = (n_loc + kEvThreads - 1) / kEvThreads * 32;  // a warp's consecutive candidates
+      const int w0 = min(n_loc, warp * chunk), w1 = min(n_loc, w0 + chunk);
+      unsigned int gt = 0u, eq = 0u;
+      for (int i0 = w0; i0 < w1; i0 += 32) {
+        const bool in = i0 + lane < w1;
+        const unsigned int v = in ? ld(i0 + lane) : 0u;
+        gt += __popc(__ballot_sync(0xffffffffu, in && v > top));
+        eq += __popc(__ballot_sync(0xffffffffu, in && (v & pmask) == prefix));
+      }
+      if (lane == 0) {
+        s_gt[warp] = gt;
+        s_eq[warp] = eq;
+      }
+      __syncthreads();
+      gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_gt[lane] : 0u);
+      eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? s_eq[lane] : 0u);
+      add_peers(__reduce_add_sync(0xffffffffu, s_gt[lane]), __reduce_add_sync(0xffffffffu, s_eq[lane]));
+      for (int i0 = w0; i0 < w1; i0 += 32) {
+        const bool in = i0 + lane < w1;
+        const unsigned int v = in ? ld(i0 + lane) : 0u;
+        const bool g = in && v > top, q = in && (v & pmask) == prefix;
+        const unsigned int mg = __ballot_sync(0xffffffffu, g), mq = __ballot_sync(0xffffffffu, q);
+        const unsigned int eb = eq_before + __popc(mq & low);
+        if (g || (q && eb < need)) emit(i0 + lane, gt_before + __popc(mg & low) + min(eb, need));
+        gt_before += __popc(mg);
+        eq_before += __popc(mq);
+      }
     }
-    cluster_sync();  // no CTA leaves while a peer may still read its shared memory
+    if (CL > 1) asm volatile("barrier.cluster.wait;\n" ::: "memory");
   }
   if (rank == 0) {
     for (int i = tid; i < S; i += kEvThreads) idx[i] = i;
@@ -431,12 +513,12 @@ static EvWs ev_ws_layout(int n_segs, int max_cap) {
   return w;
 }
 
-template <int CL>
-static int launch_evict_cluster(const EvSelectArgs& a, int n_masked, size_t smem, cudaStream_t stream) {
+template <int CL, bool kReg>
+static int launch_evict_cluster(const EvSelectArgs& a, int n_masked, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n_masked * CL);
   cfg.blockDim = dim3(kEvThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kReg ? 0 : (size_t)a.stage * 4;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -447,7 +529,7 @@ static int launch_evict_cluster(const EvSelectArgs& a, int n_masked, size_t smem
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL > 1 ? 2 : 1;
-  CATEKV_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel<CL>, a));
+  CATEKV_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel<CL, kReg>, a));
   return CATEKV_OK;
 }
 
@@ -456,29 +538,35 @@ static int evict_attributes() {
   static std::atomic<bool> attr_set[64];
   int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvStageMax * 4));
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_gather_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvMoveSmem));
-    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
-  }
+  if (dev >= 0 && dev < 64 && attr_set[dev].load(std::memory_order_acquire)) return CATEKV_OK;
+  const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<1, false>, at, kEvStageMax * 4));
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<2, false>, at, kEvStageMax * 4));
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<4, false>, at, kEvStageMax * 4));
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<8, false>, at, kEvStageMax * 4));
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_gather_kernel, at, kEvMoveSmem));
+  if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   return CATEKV_OK;
 }
-// max_pool: bound of a masked segment's candidates
+
+// max_pool: bound of a masked segment's candidates.  The smallest cluster whose CTAs hold their shares in registers, as long as all clusters are
+// resident at once; else fewer CTAs with longer shares in shared memory.
 static int launch_evict_select(EvSelectArgs& a, int n_masked, int max_pool, cudaStream_t stream) {
+  auto share = [&](int CL) { return ((max_pool + CL - 1) / CL + 31) / 32 * 32; };
   int CL = 1;
-  if (max_pool > kEvClusterFrom)
-    for (CL = 8; CL > 1 && n_masked * CL > 2 * sm_count(); CL /= 2) {}
-  while (CL < 8 && (max_pool + CL - 1) / CL + 32 > kEvStageMax) CL *= 2;
-  const int share = ((max_pool + CL - 1) / CL + 31) / 32 * 32;
-  a.stage = share <= kEvStageMax ? share : 0;
-  const size_t smem = (size_t)a.stage * 4;
-  if (CL == 8) return launch_evict_cluster<8>(a, n_masked, smem, stream);
-  if (CL == 4) return launch_evict_cluster<4>(a, n_masked, smem, stream);
-  if (CL == 2) return launch_evict_cluster<2>(a, n_masked, smem, stream);
-  return launch_evict_cluster<1>(a, n_masked, smem, stream);
+  while (CL < 8 && share(CL) > kEvRegShare && n_masked * CL * 2 <= 2 * sm_count()) CL *= 2;
+  while (CL < 8 && share(CL) > kEvStageMax) CL *= 2;
+  a.stage = share(CL) <= kEvStageMax ? share(CL) : 0;
+  if (share(CL) <= kEvRegShare) {
+    if (CL == 8) return launch_evict_cluster<8, true>(a, n_masked, stream);
+    if (CL == 4) return launch_evict_cluster<4, true>(a, n_masked, stream);
+    if (CL == 2) return launch_evict_cluster<2, true>(a, n_masked, stream);
+    return launch_evict_cluster<1, true>(a, n_masked, stream);
+  }
+  if (CL == 8) return launch_evict_cluster<8, false>(a, n_masked, stream);
+  if (CL == 4) return launch_evict_cluster<4, false>(a, n_masked, stream);
+  if (CL == 2) return launch_evict_cluster<2, false>(a, n_masked, stream);
+  return launch_evict_cluster<1, false>(a, n_masked, stream);
 }
 
 static int check_evict(const catekv_cache* c, const uint8_t* mask, int32_t budget, int32_t sink, int32_t local) {
