@@ -647,12 +647,15 @@ int catekv_q8_cache_advance(catekv_q8_cache* cache, int32_t n_tokens);
  * catekv_q8_decode_num_ctas.  A plan stays valid while the segments grow (and shrink) like one of catekv_decode_plan;
  * a plan of the other kind is refused (CATEKV_ERR_INVALID_ARG).  The ordering note of catekv_decode_attn holds for
  * the blocks that were complete when the plan was built.
+ * plan_dev, like ws, belongs to one call at a time: it holds the counts by which the CTA that delivers the last piece of a
+ * short segment knows that it is to merge them (they are 0 again when the call is done).  Calls of one stream may
+ * share both; calls that can overlap (two streams, two graphs) need a plan_dev and a ws each.
  */
 int catekv_q8_decode_num_ctas(void);
 int catekv_q8_decode_plan(const catekv_q8_cache* cache, int32_t num_ctas, void* plan_host, void* plan_dev,
                           size_t plan_bytes, catekv_stream stream);
 int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
-                          int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
+                          int32_t out_dtype, float* lse_out, const void* plan_host, void* plan_dev,
                           size_t plan_bytes, void* ws, size_t ws_bytes, catekv_stream stream);
 
 #ifdef __cplusplus

@@ -50,7 +50,7 @@ struct SegInfo {
   int32_t slot_begin;
   int32_t n_pieces;
   int32_t plan_len;  // rows the segment held when the plan was built
-  int32_t reserved;
+  int32_t arrived;   // 8-bit attention: pieces delivered by the running call (0 between calls)
 };
 
 struct PlanLayout {

@@ -37,6 +37,9 @@ constexpr int q8_decode_smem(int stages) { return kQ8Warps * stages * kQ8UnitByt
 // outstanding at a time) run faster with two.  Measured per CTA share of 7 K and 14 K rows: e4m3 82.1 and 159 us with two, 84.7 and 168 us with
 // three; int8 83.0 and 161 with two, 80.7 and 161 with three.  Below 4 K rows three are as good or better (1.8 K rows, e4m3: 27.6 and 26.7).
 constexpr int kQ8LongShare = 4096;
+// Segments of up to this many pieces are merged by the CTA that delivers the last one, longer ones by a combine pass (see catekv_q8_decode_attn).
+constexpr int kQ8MergePieces = 32;
+static_assert(kQ8MergePieces <= 32, "a lane per piece");
 constexpr int32_t kQ8PlanTile = kQ8Unit;   // marks a plan of this kind (decode.cu's have kTile)
 constexpr int kQ8SegEndCharge = 512;       // rows
 constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12
@@ -61,6 +64,7 @@ struct Q8DecodeArgs {
   void* out;
   int32_t out_fp32;
   float* lse_out;
+  SegInfo* merge;  // few pieces per segment: the CTA that delivers a segment's last piece merges them (counts in SegInfo::arrived); else null
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -140,11 +144,54 @@ __device__ __forceinline__ WorkItem q8_load_item(const WorkItem* p) {
   return w;
 }
 
+// One head of a segment from its pieces (at most 32), by a warp: a lane per piece for the weights, four dimensions per lane for the sum.
+__device__ __forceinline__ void q8_merge_pieces(const Q8DecodeArgs& a, int slot, int n, int b, int h, int hd, int lane) {
+  const float l = lane < n ? __ldcg(a.part_lse + (size_t)(slot + lane) * kMaxG + hd) : -INFINITY;
+  const float* po = a.part_o + ((size_t)slot * kMaxG + hd) * kD + 4 * lane;
+  constexpr int kFly = 16;  // pieces in flight
+  float4 v[kFly];
+  auto load = [&](int u0) {
+#pragma unroll
+    for (int u = 0; u < kFly; ++u)
+      v[u] = u0 + u < n ? __ldcg(reinterpret_cast<const float4*>(po + (size_t)(u0 + u) * (kMaxG * kD))) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  load(0);  // with the LSEs: one trip to memory for up to 16 pieces
+  float M = l;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  const float e = M > -INFINITY ? exp2f(l - M) : 0.f;  // an empty piece (LSE -inf) weighs 0
+  float W = e;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) W += __shfl_xor_sync(0xffffffffu, W, o);
+  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int u0 = 0; u0 < n; u0 += kFly) {
+    if (u0 > 0) load(u0);
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      const float w = __shfl_sync(0xffffffffu, e, u0 + u);
+      r.x += w * v[u].x;
+      r.y += w * v[u].y;
+      r.z += w * v[u].z;
+      r.w += w * v[u].w;
+    }
+  }
+  const float inv = W == 0.f ? 0.f : 1.f / W;  // (a NaN stays one)
+  r = make_float4(r.x * inv, r.y * inv, r.z * inv, r.w * inv);
+  const size_t at = ((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD;
+  if (a.out_fp32)
+    reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at)[lane] = r;
+  else
+    reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + at)[lane] = make_uint2(pack_bf16(r.x, r.y), pack_bf16(r.z, r.w));
+  if (a.lse_out && lane == 0)
+    a.lse_out[(size_t)b * a.Hq + (size_t)h * a.G + hd] = W == 0.f ? -INFINITY : (M + log2f(W)) * 0.6931471805599453f;
+}
+
 template <int kType, int kQ8Stages>
 __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_scale[kQ8Warps][kQ8Stages][2];
   __shared__ float s_m[kQ8Warps][kMaxG], s_l[kQ8Warps][kMaxG];
+  __shared__ int s_last;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, c = lane & 3;
   const int pi = g ^ ((g & 1) << 2);  // token of row g
@@ -460,6 +507,12 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
 
     // ---- end of the piece: merge the four warps (warps 0 and 1 fill a slot each, 2 and 3 add to them, everybody writes a part of the sum)
     if (item + 1 < item_end) q8_load_q(a, cc.seg + 1, g, c, q4);  // on their way during the merge
+    int si_slot = 0, si_pieces = 0;
+    if (a.merge && cc.slot >= 0) {
+      const int2 x = __ldg(reinterpret_cast<const int2*>(a.merge + cc.seg));
+      si_slot = x.x;
+      si_pieces = x.y;
+    }
 #pragma unroll
     for (int sh = 4; sh <= 16; sh <<= 1) {
       l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
@@ -523,6 +576,17 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
         // the combine pass takes an infinite LSE as the one partial that counts: a NaN (from a block with the scale NaN) reaches the output
         if (cc.slot >= 0) a.part_lse[(size_t)cc.slot * kMaxG + hd] = lse == lse ? lse : INFINITY;
         else if (a.lse_out) a.lse_out[(size_t)b * a.Hq + h * a.G + hd] = lse * 0.6931471805599453f;
+      }
+    }
+    if (a.merge && cc.slot >= 0) {
+      __threadfence();
+      __syncthreads();  // this CTA's piece is written
+      // the count wraps to 0 with the last piece: ready for the next call
+      if (tid == 0) s_last = atomicInc(reinterpret_cast<unsigned int*>(&a.merge[cc.seg].arrived), (unsigned int)si_pieces - 1u) == (unsigned int)si_pieces - 1u;
+      __syncthreads();
+      if (s_last) {
+        __threadfence();
+        for (int hd = warp; hd < a.G; hd += kQ8Warps) q8_merge_pieces(a, si_slot, si_pieces, b, h, hd, lane);
       }
     }
   }
@@ -640,7 +704,7 @@ extern "C" int catekv_q8_decode_plan(const catekv_q8_cache* cache, int32_t num_c
 }
 
 extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
-                                     int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
+                                     int32_t out_dtype, float* lse_out, const void* plan_host, void* plan_dev,
                                      size_t plan_bytes, void* ws, size_t ws_bytes, catekv_stream stream) {
   CATEKV_API_RANGE();
   int rc = check_q8_cache(cache);
@@ -685,13 +749,14 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
   a.out = out;
   a.out_fp32 = out_dtype == CATEKV_OUT_FP32;
   a.lse_out = lse_out;
+  a.merge = hdr->max_pieces <= kQ8MergePieces ? (SegInfo*)((uint8_t*)plan_dev + L.off_seg) : nullptr;
   if (cache->dtype == CATEKV_Q8_INT8)
     CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_INT8, 3>(a, hdr->num_ctas, st)));
   else if (hdr->total_rows >= (int64_t)kQ8LongShare * hdr->num_ctas)
     CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 2>(a, hdr->num_ctas, st)));
   else
     CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 3>(a, hdr->num_ctas, st)));
-  if (hdr->n_slots > 0) {
+  if (hdr->n_slots > 0 && !a.merge) {
     CombineArgs ca;
     ca.seg_info = (const SegInfo*)(pd + L.off_seg);
     ca.part_o = a.part_o;
