@@ -542,7 +542,7 @@ int catekv_decode_attn_noalloc(const catekv_cache* cache, const void* q, int32_t
  * queries that come, and cut a list back to a budget by that count.  (The paper fixes what a consistent head keeps
  * at the end of prefill; this is the counterpart for what is generated after it.)
  *
- * catekv_decode_attn_weighted is catekv_decode_attn (same arguments, outputs and plan) that also updates
+ * catekv_decode_attn_weighted is catekv_decode_attn (same arguments and plan, the same outputs up to fp32 rounding) that also updates
  *   weights    device float [total_rows], one per pool row:  w_r <- decay * w_r + (1/G) sum_g exp(logit_gr - lse_g)
  * for every row r of every list (the probabilities of one step sum to 1 per list).  decay in [0, 1]; with 0 the old
  * weights are not read.  Rows behind a list are not touched: zero the array when the cache is filled, and a row starts

@@ -394,6 +394,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
       const float p2 = fast_exp2(x2 - mn0), p3 = fast_exp2(x3 - mn1);
       l0 = l0 * al0 + p0 + p2;
       l1 = l1 * al1 + p1 + p3;
+      if (!kLogits)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         o[i][0] *= al0;
@@ -407,6 +408,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
       const uint32_t bh1 = movmatrix_trans(pack_bf16(h2, h3));
       const uint32_t bl0 = movmatrix_trans(pack_bf16(p0 - h0, p1 - h1));
       const uint32_t bl1 = movmatrix_trans(pack_bf16(p2 - h2, p3 - h3));
+      // kLogits: a third part, so that P has 24 bits (hi + lo have 16, which shows as 1e-6 where a few rows hold the mass)
+      uint32_t bm0 = 0, bm1 = 0;
+      if (kLogits) {
+        const float d0 = p0 - h0, d1 = p1 - h1, d2 = p2 - h2, d3 = p3 - h3;
+        bm0 = movmatrix_trans(pack_bf16(d0 - bf16_round(d0), d1 - bf16_round(d1)));
+        bm1 = movmatrix_trans(pack_bf16(d2 - bf16_round(d2), d3 - bf16_round(d3)));
+      }
       // ---- O^T[128 d x 8 heads] += V_tile^T . P
       {
         const int r = row0 + (lane & 7) + ((lane >> 4) & 1) * 8;
@@ -415,8 +423,21 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
         for (int mt = 0; mt < 8; ++mt) {
           uint32_t af[4];
           ldmatrix_x4_trans(af, vb + tile_off(r, mt * 2 + cadd));
-          mma_bf16_16816(o[mt], af, bh0, bh1);
-          mma_bf16_16816(o[mt], af, bl0, bl1);
+          if (kLogits) {
+            // The tensor cores cut their sums off instead of rounding them, which shrinks accumulators that go through hundreds of
+            // MMAs by 1e-6: here a tile's product is formed from zero and added by one rounded multiply-add.
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+            mma_bf16_16816(y, af, bm0, bm1);
+            mma_bf16_16816(y, af, bl0, bl1);
+            mma_bf16_16816(y, af, bh0, bh1);
+            o[mt][0] = fmaf(o[mt][0], al0, y[0]);
+            o[mt][1] = fmaf(o[mt][1], al1, y[1]);
+            o[mt][2] = fmaf(o[mt][2], al0, y[2]);
+            o[mt][3] = fmaf(o[mt][3], al1, y[3]);
+          } else {
+            mma_bf16_16816(o[mt], af, bh0, bh1);
+            mma_bf16_16816(o[mt], af, bl0, bl1);
+          }
         }
       }
     }

@@ -14,8 +14,8 @@
 //               these + 8 (the columns that P's transposed fragment has), and interleaves their bytes in registers.
 // Q enters as f16 under a power of two per head (bf16 has fewer bits than f16: exact except where an element is 2^-29 of the head's largest);
 // the scale of a block multiplies its logits.  Probabilities are formed against the running maximum times 2^12 and split into an f16
-// hi + lo pair (22 bits); the block's V scale enters through its ratio to the largest one so far, so that accumulators of different blocks share one
-// unit (vr): a growing vr rescales them exactly as a growing maximum does.
+// hi + lo pair (22 bits).  The tensor cores cut their fp32 sums off instead of rounding them: chains are kept short (four MMAs), a unit's P V
+// product is formed from zero and enters the accumulators by one rounded multiply-add each, which also applies the block's V scale.
 #include <math.h>
 
 #include <atomic>
@@ -42,8 +42,8 @@ constexpr int kQ8MergePieces = 32;
 static_assert(kQ8MergePieces <= 32, "a lane per piece");
 constexpr int32_t kQ8PlanTile = kQ8Unit;   // marks a plan of this kind (decode.cu's have kTile)
 constexpr int kQ8SegEndCharge = 512;       // rows
-constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12
-constexpr float kQ8TailFloor = 7.8886090522101181e-31f;  // 2^-100
+constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12 ...
+constexpr float kQ8PUnit = 1.f / 4096.f;   // ... and the accumulators in units of it
 static_assert(kQ8PlanTile != kTile, "the two kinds of plan must differ");
 
 struct Q8DecodeArgs {
@@ -343,26 +343,18 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-    float vr = 0.f;  // largest V scale so far: the accumulators' unit
-    // new maxima and V scale: what the accumulators are multiplied with
-    auto rescale = [&](float mx0, float mx1, float vs) {
+    // new maxima: what the sums so far are multiplied with
+    auto rescale = [&](float mx0, float mx1) {
 #pragma unroll
       for (int sh = 4; sh <= 16; sh <<= 1) {
         mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, sh));
         mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, sh));
       }
       const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
-      const bool grown = vs > vr;
-      if (__any_sync(0xffffffffu, mn0 > m0 || mn1 > m1 || grown)) {
-        float al0 = fast_exp2(m0 - mn0), al1 = fast_exp2(m1 - mn1);  // exp2(-inf) = 0 on the first unit
+      if (__any_sync(0xffffffffu, mn0 > m0 || mn1 > m1)) {
+        const float al0 = fast_exp2(m0 - mn0), al1 = fast_exp2(m1 - mn1);  // exp2(-inf) = 0 on the first unit
         l0 *= al0;
         l1 *= al1;
-        if (grown) {
-          const float rv = __fdiv_rn(vr, vs);
-          al0 *= rv;
-          al1 *= rv;
-          vr = vs;
-        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           o[i][0] *= al0;
@@ -383,9 +375,9 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
       const uint32_t kb = ring + stage * kQ8UnitBytes, vb = kb + 4096;
       if (u < cc.full) {
         if (u >= cc.live) continue;
-        const float ks = s_scale[warp][stage][0], vs = s_scale[warp][stage][1];
-        // ---- S[32 tokens x 8 heads] = K Q^T
-        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        const float ks = s_scale[warp][stage][0], vs = s_scale[warp][stage][1] * kQ8PUnit;
+        // ---- S[32 tokens x 8 heads] = K Q^T, the two halves of d apart
+        float sh[2][2][4];
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
@@ -393,13 +385,20 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
             const uint32_t ra = kb + (16 * t + pi) * kQ8RowBytes + (((c + 4 * hh) ^ (pi & 7)) << 4);
             const uint4 lo = lds128(ra), hi = lds128(ra + 8 * kQ8RowBytes);
 #pragma unroll
+            for (int i = 0; i < 4; ++i) sh[t][hh][i] = 0.f;
+#pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t a0, a1, a2, a3;
               q8_to_f16<kType>(word(lo, i), a0, a2);
               q8_to_f16<kType>(word(hi, i), a1, a3);
-              mma_f16_16816(s[t], a0, a1, a2, a3, qf[4 * hh + i][0], qf[4 * hh + i][1]);
+              mma_f16_16816(sh[t][hh], a0, a1, a2, a3, qf[4 * hh + i][0], qf[4 * hh + i][1]);
             }
           }
+        float s[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][i] = sh[t][0][i] + sh[t][1][i];
         // s[t][0], s[t][1]: token 16 t + pi(g), heads 2c, 2c + 1;  s[t][2], s[t][3]: that token + 8
         const float k0 = f0 * ks, k1 = f1 * ks;
         float x[2][4];
@@ -410,8 +409,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
           x[t][2] = s[t][2] * k0;
           x[t][3] = s[t][3] * k1;
         }
-        rescale(fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3])), vs);
-        const float ratio = vr > 0.f ? __fdiv_rn(vs, vr) : vs;  // (vs is 0 or NaN where vr is 0)
+        rescale(fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3])));
         const float r0 = kQ8PBits - m0, r1 = kQ8PBits - m1;
         uint32_t bh[2][2], bl[2][2];
 #pragma unroll
@@ -421,29 +419,41 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
             const float p0 = fast_exp2(x[t][2 * e] + r0), p1 = fast_exp2(x[t][2 * e + 1] + r1);
             l0 += p0;
             l1 += p1;
-            const float w0p = p0 * ratio, w1p = p1 * ratio;
-            const uint32_t hi = pack_f16(w0p, w1p);
+            const uint32_t hi = pack_f16(p0, p1);
             const float2 hf = unpack_f16(hi);
             bh[t][e] = movmatrix_trans(hi);
-            bl[t][e] = movmatrix_trans(pack_f16(w0p - hf.x, w1p - hf.y));
+            bl[t][e] = movmatrix_trans(pack_f16(p0 - hf.x, p1 - hf.y));
           }
         // ---- O^T[128 d x 8 heads] += V^T P
+        uint4 v[2][4];  // tokens 2c, (2c + 1) ^ 4, these + 8 of each half
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int t0 = 16 * t + 2 * c, t1 = 16 * t + ((2 * c + 1) ^ 4);
           const uint32_t ra = vb + t0 * kQ8RowBytes + ((g ^ (t0 & 7)) << 4), rb = vb + t1 * kQ8RowBytes + ((g ^ (t1 & 7)) << 4);
-          const uint4 v0 = lds128(ra), v1 = lds128(rb), v2 = lds128(ra + 8 * kQ8RowBytes), v3 = lds128(rb + 8 * kQ8RowBytes);
+          v[t][0] = lds128(ra);
+          v[t][1] = lds128(rb);
+          v[t][2] = lds128(ra + 8 * kQ8RowBytes);
+          v[t][3] = lds128(rb + 8 * kQ8RowBytes);
+        }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t x0, x1, x2, x3, y0, y1, y2, y3;  // d = 16 g + 4 i + 0..3: tokens (t0, t1), tokens (t0 + 8, t1 + 8)
-            q8_to_f16<kType>(__byte_perm(word(v0, i), word(v1, i), 0x5140), x0, x1);
-            q8_to_f16<kType>(__byte_perm(word(v0, i), word(v1, i), 0x7362), x2, x3);
-            q8_to_f16<kType>(__byte_perm(word(v2, i), word(v3, i), 0x5140), y0, y1);
-            q8_to_f16<kType>(__byte_perm(word(v2, i), word(v3, i), 0x7362), y2, y3);
-            mma_f16_16816(o[2 * i], x0, x1, y0, y1, bh[t][0], bh[t][1]);
-            mma_f16_16816(o[2 * i], x0, x1, y0, y1, bl[t][0], bl[t][1]);
-            mma_f16_16816(o[2 * i + 1], x2, x3, y2, y3, bh[t][0], bh[t][1]);
-            mma_f16_16816(o[2 * i + 1], x2, x3, y2, y3, bl[t][0], bl[t][1]);
+        for (int i = 0; i < 4; ++i) {
+          float y0[4] = {0.f, 0.f, 0.f, 0.f}, y1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            uint32_t x0, x1, x2, x3, z0, z1, z2, z3;  // d = 16 g + 4 i + 0..3: the first two tokens, the two + 8
+            q8_to_f16<kType>(__byte_perm(word(v[t][0], i), word(v[t][1], i), 0x5140), x0, x1);
+            q8_to_f16<kType>(__byte_perm(word(v[t][0], i), word(v[t][1], i), 0x7362), x2, x3);
+            q8_to_f16<kType>(__byte_perm(word(v[t][2], i), word(v[t][3], i), 0x5140), z0, z1);
+            q8_to_f16<kType>(__byte_perm(word(v[t][2], i), word(v[t][3], i), 0x7362), z2, z3);
+            mma_f16_16816(y0, x0, x1, z0, z1, bl[t][0], bl[t][1]);
+            mma_f16_16816(y1, x2, x3, z2, z3, bl[t][0], bl[t][1]);
+            mma_f16_16816(y0, x0, x1, z0, z1, bh[t][0], bh[t][1]);
+            mma_f16_16816(y1, x2, x3, z2, z3, bh[t][0], bh[t][1]);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            o[2 * i][r] = fmaf(y0[r], vs, o[2 * i][r]);
+            o[2 * i + 1][r] = fmaf(y1[r], vs, o[2 * i + 1][r]);
           }
         }
       } else {
@@ -465,41 +475,34 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
         const bool v_lo = pi < left, v_hi = pi + 8 < left;
         const float x0 = v_lo ? s[0] * a.scale_log2 : -INFINITY, x1 = v_lo ? s[1] * a.scale_log2 : -INFINITY;
         const float x2 = v_hi ? s[2] * a.scale_log2 : -INFINITY, x3 = v_hi ? s[3] * a.scale_log2 : -INFINITY;
-        // The tail's V has no scale: a 448th of its largest magnitude stands in for one, so that the units of blocks and tail agree whatever the
-        // magnitudes.  (The floor keeps 2^12 / vr finite.)
+        rescale(fmaxf(x0, x2), fmaxf(x1, x3));
+        const float r0 = kQ8PBits - m0, r1 = kQ8PBits - m1;
+        float p0 = fast_exp2(x0 + r0), p1 = fast_exp2(x1 + r1), p2 = fast_exp2(x2 + r0), p3 = fast_exp2(x3 + r1);
+        l0 += p0 + p2;
+        l1 += p1 + p3;
+        p0 *= kQ8PUnit;
+        p1 *= kQ8PUnit;
+        p2 *= kQ8PUnit;
+        p3 *= kQ8PUnit;
+        const float h0 = bf16_round(p0), h1 = bf16_round(p1), h2 = bf16_round(p2), h3 = bf16_round(p3);
+        const uint32_t bh0 = movmatrix_trans(pack_bf16(h0, h1)), bh1 = movmatrix_trans(pack_bf16(h2, h3));
+        const float d0 = p0 - h0, d1 = p1 - h1, d2 = p2 - h2, d3 = p3 - h3;  // three bf16 parts: 24 bits
+        const uint32_t bl0 = movmatrix_trans(pack_bf16(d0, d1)), bl1 = movmatrix_trans(pack_bf16(d2, d3));
+        const uint32_t bm0 = movmatrix_trans(pack_bf16(d0 - bf16_round(d0), d1 - bf16_round(d1)));
+        const uint32_t bm1 = movmatrix_trans(pack_bf16(d2 - bf16_round(d2), d3 - bf16_round(d3)));
         const int t0 = 2 * c, t1 = (2 * c + 1) ^ 4;
-        uint4 v[2][4];
-        uint32_t vm = 0;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int ch = 2 * g + e;
-          v[e][0] = lds128(vb + tile_off(t0, ch));
-          v[e][1] = lds128(vb + tile_off(t1, ch));
-          v[e][2] = lds128(vb + tile_off(t0 + 8, ch));
-          v[e][3] = lds128(vb + tile_off(t1 + 8, ch));
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) vm = __vmaxu2(vm, word(v[e][i], j) & 0x7fff7fffu);
-        }
-        vm = __reduce_max_sync(0xffffffffu, max(vm & 0xffffu, vm >> 16));
-        rescale(fmaxf(x0, x2), fmaxf(x1, x3), fmaxf(__uint_as_float(vm << 16) * (1.f / 448.f), kQ8TailFloor));
-        const float r0 = kQ8PBits - m0, r1 = kQ8PBits - m1, ratio = __fdiv_rn(1.f, vr);
-        const float p0 = fast_exp2(x0 + r0), p1 = fast_exp2(x1 + r1), p2 = fast_exp2(x2 + r0), p3 = fast_exp2(x3 + r1);
-        l0 += p0 + p2;
-        l1 += p1 + p3;
-        const float w0p = p0 * ratio, w1p = p1 * ratio, w2p = p2 * ratio, w3p = p3 * ratio;
-        const float h0 = bf16_round(w0p), h1 = bf16_round(w1p), h2 = bf16_round(w2p), h3 = bf16_round(w3p);
-        const uint32_t bh0 = movmatrix_trans(pack_bf16(h0, h1)), bh1 = movmatrix_trans(pack_bf16(h2, h3));
-        const uint32_t bl0 = movmatrix_trans(pack_bf16(w0p - h0, w1p - h1)), bl1 = movmatrix_trans(pack_bf16(w2p - h2, w3p - h3));
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
+          const uint4 v0 = lds128(vb + tile_off(t0, ch)), v1 = lds128(vb + tile_off(t1, ch));
+          const uint4 v2 = lds128(vb + tile_off(t0 + 8, ch)), v3 = lds128(vb + tile_off(t1 + 8, ch));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {  // d = 16 g + 8 e + 2 i + 0, 1
-            const uint32_t af[4] = {__byte_perm(word(v[e][0], i), word(v[e][1], i), 0x5410), __byte_perm(word(v[e][0], i), word(v[e][1], i), 0x7632),
-                                    __byte_perm(word(v[e][2], i), word(v[e][3], i), 0x5410), __byte_perm(word(v[e][2], i), word(v[e][3], i), 0x7632)};
-            mma_bf16_16816(o[4 * e + i], af, bh0, bh1);
+            const uint32_t af[4] = {__byte_perm(word(v0, i), word(v1, i), 0x5410), __byte_perm(word(v0, i), word(v1, i), 0x7632),
+                                    __byte_perm(word(v2, i), word(v3, i), 0x5410), __byte_perm(word(v2, i), word(v3, i), 0x7632)};
+            mma_bf16_16816(o[4 * e + i], af, bm0, bm1);
             mma_bf16_16816(o[4 * e + i], af, bl0, bl1);
+            mma_bf16_16816(o[4 * e + i], af, bh0, bh1);
           }
         }
       }
@@ -525,14 +528,14 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
       s_l[warp][2 * c + 1] = l1;
     }
     __syncthreads();  // (and the slots of the piece before have been read)
-    float al[2];  // from this warp's unit and maximum to 1 and the CTA's maximum
+    float al[2];  // from this warp's maximum to the CTA's
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float M = s_m[0][2 * c + e];
 #pragma unroll
       for (int w = 1; w < kQ8Warps; ++w) M = fmaxf(M, s_m[w][2 * c + e]);
       const float m = e ? m1 : m0;
-      al[e] = m == M ? vr : fast_exp2(m - M) * vr;
+      al[e] = m == M ? 1.f : fast_exp2(m - M);
     }
     float* slot = slots + (warp & 1) * kQ8SlotFloats;
 #pragma unroll
@@ -560,8 +563,9 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
       float l = 0.f;
 #pragma unroll
       for (int w = 0; w < kQ8Warps; ++w) l += s_m[w][hd] == M ? s_l[w][hd] : s_l[w][hd] * fast_exp2(s_m[w][hd] - M);
+      l *= kQ8PUnit;
       const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
-      const float lse = l == 0.f ? -INFINITY : M - kQ8PBits + log2f(l);
+      const float lse = l == 0.f ? -INFINITY : M + log2f(l);
       const float4 x = *reinterpret_cast<const float4*>(slots + q8_slot(hd, 4 * lane));
       const float4 y = *reinterpret_cast<const float4*>(slots + kQ8SlotFloats + q8_slot(hd, 4 * lane));
       const float4 v = make_float4((x.x + y.x) * inv, (x.y + y.y) * inv, (x.z + y.z) * inv, (x.w + y.w) * inv);
