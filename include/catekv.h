@@ -547,8 +547,9 @@ int catekv_decode_attn_noalloc(const catekv_cache* cache, const void* q, int32_t
  * for every row r of every list (the probabilities of one step sum to 1 per list).  decay in [0, 1]; with 0 the old
  * weights are not read.  Rows behind a list are not touched: zero the array when the cache is filled, and a row starts
  * at 0 when it is appended.
- *   ws  at least catekv_decode_weighted_workspace_bytes(...) with the cache's total_rows
- * CATEKV_ERR_UNSUPPORTED for a cache with overflow pages.
+ *   ws  at least catekv_decode_weighted_workspace_bytes(...) with the cache's total_rows; q, out and ws 16-byte aligned
+ * CATEKV_ERR_UNSUPPORTED for a cache with overflow pages; CATEKV_ERR_INVALID_ARG for a plan made for longer lists (the
+ * cache has been cut since).
  */
 size_t catekv_decode_weighted_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_ctas, int64_t total_rows);
 int catekv_decode_attn_weighted(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
@@ -567,8 +568,8 @@ int catekv_decode_attn_weighted(const catekv_cache* cache, const void* q, int32_
  *   exact (CATEKV_ERR_INVALID_ARG if src->reserved is set).  catekv_evict_lengths: that rule alone, host only (to lay
  *   out dst).  Launch shapes follow the capacities, so the call may be captured and replayed (the mirror is then the
  *   captured call's: catekv_cache_sync_lengths).
- *   A decode plan of dst stays valid for catekv_decode_attn (lists that have shrunk); retrieval metadata of dst has to be
- *   rebuilt, and catekv_append_decode_attn needs a new plan.
+ *   What was built for dst before has to be built anew: its decode plans (before the next append: see the ordering note
+ *   of catekv_decode_attn; catekv_decode_attn_weighted refuses a plan made for longer lists) and its retrieval metadata.
  *   idx_out  device int32 [B*Hkv, idx_stride] or NULL: the rows kept of each segment
  *   ws       device scratch of at least catekv_evict_workspace_bytes(B, Hkv, largest seg_cap of src); its first
  *            CATEKV_STATUS_BYTES are the status block, which this call does not clear (as the retrieval calls):
@@ -644,9 +645,9 @@ int catekv_q8_cache_advance(catekv_q8_cache* cache, int32_t n_tokens);
  * with the keys and values that the codes stand for and the bf16 tails; fp32 accumulation, probabilities carried as
  * fp16 or bf16 pairs of 16 and more bits), with a plan of its own: catekv_q8_decode_plan cuts at block borders.  Buffer
  * sizes are those of catekv_decode_plan_bytes and catekv_decode_workspace_bytes; num_ctas comes from
- * catekv_q8_decode_num_ctas.  A plan stays valid while the segments grow (and shrink) like one of catekv_decode_plan;
- * a plan of the other kind is refused (CATEKV_ERR_INVALID_ARG).  The ordering note of catekv_decode_attn holds for
- * the blocks that were complete when the plan was built.
+ * catekv_q8_decode_num_ctas.  A plan stays valid while the segments grow; a plan made for longer lists (the cache has been
+ * quantised anew since) and one of the other kind are refused (CATEKV_ERR_INVALID_ARG).  The ordering note of
+ * catekv_decode_attn holds for the blocks that were complete when the plan was built.
  * plan_dev, like ws, belongs to one call at a time: it holds the counts by which the CTA that delivers the last piece of a
  * short segment knows that it is to merge them (they are 0 again when the call is done).  Calls of one stream may
  * share both; calls that can overlap (two streams, two graphs) need a plan_dev and a ws each.

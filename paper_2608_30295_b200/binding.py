@@ -715,8 +715,16 @@ def evict_workspace(cache: Cache) -> torch.Tensor:
     return ws
 
 
+def _int32(where: str, *values):
+    """Counts that do not fit the C ABI's int32 are refused (ctypes would cut them off)."""
+    for v in values:
+        if not 0 <= v < 2 ** 31:
+            raise CatekvError(ERR_INVALID_ARG, where)
+
+
 def catekv_evict_lengths(cache: Cache, evict_mask, budget: int, sink: int, local: int):
     """Host only: rows every segment keeps under catekv_evict with these parameters."""
+    _int32("catekv_evict_lengths", budget, sink, local)
     evict_mask = np.ascontiguousarray(evict_mask, dtype=np.uint8).reshape(-1)
     assert evict_mask.size == cache.B * cache.Hkv
     lens = np.zeros(cache.B * cache.Hkv, dtype=np.int32)
@@ -731,6 +739,7 @@ def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, s
     """Cut the masked segments to `budget` rows by weight, into `dst` and `dst_weights`, or in place without them."""
     if dst is None:
         dst, dst_weights = cache, weights
+    _int32("catekv_evict", budget, sink, local)
     evict_mask = np.ascontiguousarray(evict_mask, dtype=np.uint8).reshape(-1)
     n = cache.B * cache.Hkv
     assert evict_mask.size == n

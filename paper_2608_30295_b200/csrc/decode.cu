@@ -936,8 +936,13 @@ extern "C" int catekv_decode_attn_weighted(const catekv_cache* cache, const void
   if (rc) return rc;
   if (cache->pages) return CATEKV_ERR_UNSUPPORTED;
   if (!weights || !ws || !plan_host || !plan_dev || !(decay >= 0.f && decay <= 1.f) || Hq <= 0 || Hq % cache->Hkv) return CATEKV_ERR_INVALID_ARG;
+  if ((((uintptr_t)q | (uintptr_t)out | (uintptr_t)ws) & 15) || ((uintptr_t)weights & 3)) return CATEKV_ERR_INVALID_ARG;
+  const int n_segs = cache->B * cache->Hkv;
   const PlanHeader* hdr = (const PlanHeader*)plan_host;
-  if (plan_bytes < sizeof(PlanHeader) || hdr->magic != kPlanMagic || hdr->num_ctas <= 0) return CATEKV_ERR_INVALID_ARG;
+  if (plan_bytes < sizeof(PlanHeader) || hdr->magic != kPlanMagic || hdr->num_ctas <= 0 || hdr->n_segs != n_segs) return CATEKV_ERR_INVALID_ARG;
+  const PlanLayout L = plan_layout(n_segs, hdr->num_ctas);
+  if (plan_bytes < L.bytes) return CATEKV_ERR_WORKSPACE;
+  if (plan_outlived(plan_host, L.off_seg, cache->seg_len, n_segs)) return CATEKV_ERR_INVALID_ARG;
   const WeightedWs W = weighted_ws_layout(cache->B, Hq, cache->Hkv, hdr->num_ctas, cache->total_rows);
   if (ws_bytes < W.bytes) return CATEKV_ERR_WORKSPACE;
   float* lse = lse_out ? lse_out : (float*)((uint8_t*)ws + W.off_lse);
@@ -945,8 +950,6 @@ extern "C" int catekv_decode_attn_weighted(const catekv_cache* cache, const void
   rc = decode_launch(1, cache, nullptr, nullptr, q, Hq, sm_scale, out, out_dtype, lse, plan_host, plan_dev, plan_bytes, ws, ws_bytes,
                      stream, nullptr, logits);
   if (rc) return rc;
-  const int n_segs = cache->B * cache->Hkv;
-  const PlanLayout L = plan_layout(n_segs, hdr->num_ctas);
   size_t off_lse = 0;
   ws_layout(n_segs, hdr->num_ctas, &off_lse);
   const uint8_t* pd = (const uint8_t*)plan_dev;

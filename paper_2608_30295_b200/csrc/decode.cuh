@@ -127,6 +127,14 @@ static int check_cache(const catekv_cache* c) {
   }
   return CATEKV_OK;
 }
+// A plan made for lists that were longer than they are now.  The attention kernels request rows that the plan knows before the preceding
+// kernel of the stream has finished: a row appended into a shortened list would be such a row.
+static bool plan_outlived(const void* plan_host, size_t off_seg, const int32_t* seg_len, int n_segs) {
+  const SegInfo* si = (const SegInfo*)((const uint8_t*)plan_host + off_seg);
+  for (int s = 0; s < n_segs; ++s)
+    if (seg_len[s] < si[s].plan_len) return true;
+  return false;
+}
 // rows segment s can hold: its own capacity plus the overflow pages it has been given
 static inline int64_t seg_capacity(const catekv_cache* c, int s) {
   return (int64_t)c->seg_cap[s] + (c->pages ? (int64_t)c->pages->seg_pages[s] * CATEKV_PAGE_ROWS : 0);

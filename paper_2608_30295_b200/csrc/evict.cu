@@ -610,6 +610,8 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
   if (dst->pages) return CATEKV_ERR_UNSUPPORTED;
   if (!weights || !dst_weights || !ws || !src->seg_cap_dev || !dst->seg_cap_dev) return CATEKV_ERR_INVALID_ARG;
   if (src->B != dst->B || src->Hkv != dst->Hkv) return CATEKV_ERR_INVALID_ARG;
+  if (((uintptr_t)src->k_pool | (uintptr_t)src->v_pool | (uintptr_t)dst->k_pool | (uintptr_t)dst->v_pool | (uintptr_t)ws) & 15) return CATEKV_ERR_INVALID_ARG;
+  if (((uintptr_t)weights | (uintptr_t)dst_weights | (uintptr_t)idx_out) & 3) return CATEKV_ERR_INVALID_ARG;
   const bool in_place = src == dst;
   if (in_place != (weights == dst_weights)) return CATEKV_ERR_INVALID_ARG;
   if (!in_place && (src->k_pool == dst->k_pool || src->v_pool == dst->v_pool || src->seg_len == dst->seg_len ||

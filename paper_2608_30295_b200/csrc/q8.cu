@@ -214,6 +214,7 @@ extern "C" int catekv_q8_quantize(const catekv_cache* src, catekv_q8_cache* dst,
   rc = check_q8_cache(dst);
   if (rc) return rc;
   if (src->pages) return CATEKV_ERR_UNSUPPORTED;
+  if (((uintptr_t)src->k_pool | (uintptr_t)src->v_pool) & 15) return CATEKV_ERR_INVALID_ARG;
   if (src->B != dst->B || src->Hkv != dst->Hkv) return CATEKV_ERR_INVALID_ARG;
   const int n = src->B * src->Hkv;
   if (n > 65535) return CATEKV_ERR_UNSUPPORTED;
@@ -251,7 +252,7 @@ extern "C" int catekv_q8_append(catekv_q8_cache* cache, const void* k_new, const
   CATEKV_API_RANGE();
   int rc = check_q8_cache(cache);
   if (rc) return rc;
-  if (!k_new || !v_new) return CATEKV_ERR_INVALID_ARG;
+  if (!k_new || !v_new || (((uintptr_t)k_new | (uintptr_t)v_new) & 15)) return CATEKV_ERR_INVALID_ARG;
   const int n = cache->B * cache->Hkv;
   for (int s = 0; s < n; ++s) {
     if (cache->seg_len[s] < 0) return CATEKV_ERR_INVALID_ARG;

@@ -729,6 +729,7 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
   if (plan_bytes < L.bytes) return CATEKV_ERR_WORKSPACE;
   size_t off_lse = 0;
   if (ws_bytes < ws_layout(n_segs, hdr->num_ctas, &off_lse)) return CATEKV_ERR_WORKSPACE;
+  if (plan_outlived(plan_host, L.off_seg, cache->seg_len, n_segs)) return CATEKV_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   const uint8_t* pd = (const uint8_t*)plan_dev;
   rc = q8_decode_attributes();

@@ -72,7 +72,7 @@ def _two(ck, lens=(100, 200), dlens=(100, 200)):
 def test_refusals_of_evict(ck):
     src, dst, keep = _two(ck)
     for kw in ({"budget": -1}, {"sink": -1}, {"local": -1}, {"sink": 2 ** 31 - 1, "local": 1}, {"w": None}, {"dw": None}, {"ws": None},
-               {"mask": False}, {"w": F, "dw": F}, {"idx": F, "stride": 9}):
+               {"mask": False}, {"w": F, "dw": F}, {"idx": F, "stride": 9}, {"w": F + 2}, {"dw": F + 1}, {"ws": F + 8}, {"idx": F + 2, "stride": 900}):
         assert _evict(ck, src, dst, **kw) == ck.ERR_INVALID_ARG, kw
     assert _evict(ck, None, dst) == ck.ERR_INVALID_ARG and _evict(ck, src, None) == ck.ERR_INVALID_ARG
     assert _evict(ck, src, src) == ck.ERR_INVALID_ARG  # in place with weights elsewhere
@@ -120,11 +120,22 @@ def test_refusals_of_weighted_attention(ck):
 
     def call(q=F, Hq=4, scale=0.0, out=F, od=0, w=F, decay=1.0, ph=plan.ctypes.data, pd=F, pb=n, wsp=F, wb=ws):
         return ck._lib.catekv_decode_attn_weighted(C.byref(st), q, Hq, scale, out, od, None, w, decay, ph, pd, pb, wsp, wb, None)
-    for kw in ({"q": None}, {"out": None}, {"w": None}, {"ph": None}, {"pd": None}, {"wsp": None}, {"Hq": 0}, {"Hq": 3}, {"decay": -0.1},
+    for kw in ({"q": F + 2}, {"out": F + 4}, {"wsp": F + 8}, {"w": F + 1}, {"q": None}, {"out": None}, {"w": None}, {"ph": None}, {"pd": None}, {"wsp": None}, {"Hq": 0}, {"Hq": 3}, {"decay": -0.1},
                {"decay": 1.5}, {"decay": float("nan")}, {"scale": -1.0}, {"pb": 10}):
         assert call(**kw) == ck.ERR_INVALID_ARG, kw
     assert call(wb=ws - 1) == ck.ERR_WORKSPACE and call(pb=n - 1) == ck.ERR_WORKSPACE
+    keep[2][1] = 199  # shorter than the plan knows it
+    assert call() == ck.ERR_INVALID_ARG
+    keep[2][1] = 200
     assert call(Hq=18, wb=1 << 40) == ck.ERR_UNSUPPORTED and call(od=7) == ck.ERR_UNSUPPORTED
     pg = ck.PagesStruct(1, 1, 0, 0, F, F, F, F, F, F)
     st.pages = C.pointer(pg)
     assert call() == ck.ERR_UNSUPPORTED
+
+
+def test_counts_past_int32_are_refused_by_the_binding(ck):
+    cache = type("C", (), {"B": 1, "Hkv": 2})()
+    for bad in ((2 ** 32, 0, 0), (5, 2 ** 31, 0), (5, 0, -1)):
+        with pytest.raises(ck.CatekvError) as e:
+            ck.catekv_evict_lengths(cache, [1, 1], *bad)
+        assert e.value.code == ck.ERR_INVALID_ARG

@@ -237,8 +237,9 @@ def test_evict_long_lists(ck, in_place, n, budget):
     _check_evicted(oc, w0, cache.seg_off, cache.seg_cap, mask, budget, 4, 64, *res, in_place, k0)
 
 
-def test_a_captured_eviction_replays_on_lists_that_have_grown(ck):
-    lens = [300, 300, 80]
+@pytest.mark.parametrize("long", [False, True])
+def test_a_captured_eviction_replays_on_lists_that_have_grown(ck, long):
+    lens = [300, 300, 80] if not long else [300, 20000, 9000]
     oc = H.random_cache(1, 3, lens, seed=330)
     cache = H.device_cache_from_oracle(ck, oc, 60)
     mask = np.array([1, 0, 1], dtype=np.uint8)
@@ -294,7 +295,7 @@ def test_a_replay_that_outgrows_the_destination_is_cut_and_reported(ck):
 @pytest.mark.parametrize("dtype", [orc.Q8_E4M3, orc.Q8_INT8])
 def test_decode_with_weights_then_evict_then_eight_bits(ck, dtype):
     """The calls as they are used together: a few decode steps that accumulate weights, the consistent heads cut back to their budget in
-    place, more steps under the old plan, the cache to 8 bits, and steps on that."""
+    place, more steps, the cache to 8 bits, and steps on that."""
     B, Hkv, G, sink, local, budget = 2, 4, 4, 4, 32, 200
     lens = [260, 1000, 190, 700, 260, 260, 900, 150]
     mask = np.array([1, 0, 1, 0, 1, 1, 0, 1], dtype=np.uint8)
@@ -327,6 +328,11 @@ def test_decode_with_weights_then_evict_then_eight_bits(ck, dtype):
                 rows = orc.evict_indices(wv[o:o + n], sink, local, budget)
                 oc.k_rows[s], oc.v_rows[s] = oc.k_rows[s][rows], oc.v_rows[s][rows]
         assert cache.seg_len.tolist() == oc.lengths().tolist()
+        if part == 0:  # the plan is for longer lists (the second time it is for lists of the budget's length: still good)
+            with pytest.raises(ck.CatekvError) as e:
+                ck.catekv_decode_attn_weighted(cache, q, plan, out, w, 0.9, ws, lse)
+            assert e.value.code == ck.ERR_INVALID_ARG
+            ck.catekv_decode_plan(cache, plan)
     q8 = ck.Q8Cache(B, Hkv, cache.seg_len, 70, dtype)
     ck.catekv_q8_quantize(cache, q8)
     p8 = ck.DecodePlan(q8, 40)

@@ -302,18 +302,37 @@ def test_append_completes_blocks_and_equals_quantize(ck, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_a_plan_follows_lists_that_have_shrunk(ck, dtype):
+def test_a_plan_for_longer_lists_is_refused(ck, dtype):
     k, v = _rows([1000, 640, 130], 90)
     c = _quantized(ck, k, v, 1, 3, dtype)
     plan = ck.DecodePlan(c, 12)
     ck.catekv_q8_decode_plan(c, plan)
     q = synth.randn_bf16((1, 6, 128), "cuda", 91, "q")
-    short = [100, 0, 64]
-    k2, v2 = _rows(short, 92)
-    src = _src(ck, k2, v2, 1, 3)
-    ck.catekv_q8_quantize(src, c)
+    k2, v2 = _rows([1000, 0, 130], 92)
+    ck.catekv_q8_quantize(_src(ck, k2, v2, 1, 3), c)
+    with pytest.raises(ck.CatekvError) as e:
+        _attend(ck, c, q, plan=plan)
+    assert e.value.code == ck.ERR_INVALID_ARG
+    ck.catekv_q8_decode_plan(c, plan)
     out, lse = _attend(ck, c, q, plan=plan)
     _check_attention(out, lse, _oracle(k2, v2, q, 1, 3, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,ctas", [(64 * 31, 31), (64 * 32, 32), (64 * 33, 33), (64 * 80, 80), (5000, 296), (64 * 32 - 1, 200)])
+def test_pieces_merged_in_the_kernel_and_by_the_combine_pass(ck, dtype, n, ctas):
+    # around the number of pieces up to which the CTA that delivers the last one merges; several calls under one plan
+    lens = [n, 100, n // 2, 0]
+    k, v = _rows(lens, 140)
+    c = _quantized(ck, k, v, 1, 4, dtype)
+    plan = ck.DecodePlan(c, ctas)
+    plan.ws.fill_(0xFF)
+    ck.catekv_q8_decode_plan(c, plan)
+    for i in range(4):
+        q = synth.randn_bf16((1, 20, 128), "cuda", 141, "q", i)
+        out, lse = _attend(ck, c, q, plan=plan)
+        _check_attention(out, lse, _oracle(k, v, q, 1, 4, dtype), (n, ctas, i))
+        assert all(torch.equal(out, _attend(ck, c, q, plan=plan)[0]) for _ in range(20))  # whoever comes last
 
 
 @pytest.mark.parametrize("dtype", TYPES)

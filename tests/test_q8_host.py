@@ -164,6 +164,10 @@ def test_refusals_of_append_and_advance(ck):
     assert ck._lib.catekv_q8_append(C.byref(st), f, f, None) == ck.ERR_CAPACITY
     assert ck._lib.catekv_q8_append(C.byref(st), None, f, None) == ck.ERR_INVALID_ARG
     assert ck._lib.catekv_q8_append(C.byref(st), f, None, None) == ck.ERR_INVALID_ARG
+    keep[2][0] = 100
+    assert ck._lib.catekv_q8_append(C.byref(st), f + 2, f, None) == ck.ERR_INVALID_ARG
+    assert ck._lib.catekv_q8_append(C.byref(st), f, f + 8, None) == ck.ERR_INVALID_ARG
+    keep[2][0] = 128
     assert list(keep[2]) == [128, 3]
     assert ck._lib.catekv_q8_cache_advance(C.byref(st), 1) == ck.ERR_CAPACITY
     assert ck._lib.catekv_q8_cache_advance(C.byref(st), -1) == ck.ERR_INVALID_ARG
@@ -201,6 +205,9 @@ def test_refusals_of_attention(ck):
         assert call(**kw) == ck.ERR_INVALID_ARG, kw
     assert call(Hq=18) == ck.ERR_UNSUPPORTED and call(od=2) == ck.ERR_UNSUPPORTED
     assert call(pb=plan.size - 1) == ck.ERR_WORKSPACE and call(wb=ws - 1) == ck.ERR_WORKSPACE
+    keep[2][0] = 99  # shorter than the plan knows it
+    assert call() == ck.ERR_INVALID_ARG
+    keep[2][0] = 100
     # the plans of the two kinds of cache are told apart
     src, keep2 = _bf16(ck, [100, 200])
     other = np.zeros_like(plan)
