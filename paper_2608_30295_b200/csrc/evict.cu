@@ -432,70 +432,99 @@ __global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const __gr
   cp_async_wait<0>();
 }
 
-// In place.  Kept row j comes from row idx[j] >= j, so a tile of destination rows may be written once the tile itself has been read: nothing
-// behind it reads there.  That makes a segment sequential in its rows, so the work is split over the columns instead: 16 CTAs
-// per segment, each moving 32 bytes of every row (a DRAM sector; eight CTAs K, eight V), and one that moves the weights.
-constexpr int kEvSlices = 2 * kRowBytes / 32 + 1;
+// In place.  Kept row j comes from row idx[j] >= j, so a tile of destination rows may be written once it has been read itself: nothing behind it
+// reads there, and what is requested ahead lies behind it.  That makes a segment sequential in its rows, so the work is split over the
+// columns instead: a CTA moves kSlice bytes of every row of K or V, three tiles ahead with cp.async and one barrier per tile (the tile has been
+// read by everybody; the writes are a thread's own).  64 bytes are two DRAM sectors; 32, where the segments are few, make twice the CTAs.
 constexpr int kEvInThreads = 256;
-constexpr int kEvInRows = 4;  // rows per thread and tile
-__global__ void __launch_bounds__(kEvInThreads) evict_inplace_kernel(const __grid_constant__ EvMoveArgs a) {
-  const int seg = blockIdx.x / kEvSlices, slice = blockIdx.x % kEvSlices;
-  pdl_wait();
-  const EvSeg s = move_seg(a, seg);
-  const int len = s.kept;
+constexpr int kEvInTileBytes = 16384;
+constexpr int kEvInStages = 4;
+constexpr int kEvInSmem = kEvInStages * kEvInTileBytes;
+constexpr int kEvInChunks = kEvInTileBytes / (16 * kEvInThreads);  // 16-byte chunks of a thread in a tile
+constexpr int kEvWRows = 8;                                        // weights of a thread in a tile
+struct EvInArgs {
+  EvMoveArgs m;
+  int32_t n_masked;
+  EvList list;
+};
+template <int kSlice>
+__global__ void __launch_bounds__(kEvInThreads) evict_inplace_kernel(const __grid_constant__ EvInArgs g) {
+  extern __shared__ __align__(16) uint8_t stage[];
+  constexpr int kSlices = 2 * kRowBytes / kSlice;
+  constexpr int kPer = kSlice / 16;  // chunks of a row
+  constexpr int kRows = kEvInTileBytes / kSlice;
+  const EvMoveArgs& a = g.m;
   const int tid = threadIdx.x;
-  if (slice == kEvSlices - 1) {
+  pdl_wait();
+  if ((int)blockIdx.x >= g.n_masked * kSlices) {  // a segment's weights, length and list for the caller
+    const int seg = blockIdx.x - g.n_masked * kSlices;
+    const EvSeg s = move_seg(a, seg);
+    const int len = s.kept;
     if (a.idx_out)
       for (int r = tid; r < len; r += kEvInThreads) a.idx_out[(int64_t)seg * a.idx_out_stride + r] = kept_row(a, s, seg, r);
     if (s.keep_all) return;
     float* w = a.w_dst + a.dst_off[seg];
     if (tid == 0) a.dst_len[seg] = len;
-    for (int t0 = 0; t0 < len; t0 += kEvInThreads * kEvInRows) {
-      float v[kEvInRows];
+    for (int t0 = 0; t0 < len; t0 += kEvInThreads * kEvWRows) {
+      float v[kEvWRows];
 #pragma unroll
-      for (int i = 0; i < kEvInRows; ++i) {
+      for (int i = 0; i < kEvWRows; ++i) {
         const int r = t0 + tid + i * kEvInThreads;
         if (r < len) v[i] = w[kept_row(a, s, seg, r)];
       }
-      __syncthreads();
+      __syncthreads();  // the tile has been read
 #pragma unroll
-      for (int i = 0; i < kEvInRows; ++i) {
+      for (int i = 0; i < kEvWRows; ++i) {
         const int r = t0 + tid + i * kEvInThreads;
         if (r < len) w[r] = v[i];
       }
-      __syncthreads();
     }
     for (int r = len + tid; r < a.dst_cap[seg]; r += kEvInThreads) w[r] = 0.f;
     return;
   }
+  const int seg = g.list.seg[blockIdx.x / kSlices], slice = blockIdx.x % kSlices;
+  const EvSeg s = move_seg(a, seg);
   if (s.keep_all) return;
-  constexpr int kHalf = (kEvSlices - 1) / 2;
-  uint8_t* base = (slice < kHalf ? a.k_dst : a.v_dst) + (int64_t)a.dst_off[seg] * kRowBytes + (slice % kHalf) * 32;
-  for (int t0 = 0; t0 < len; t0 += kEvInThreads * kEvInRows) {
-    uint4 v[kEvInRows][2];
-    int row[kEvInRows];
+  const int len = s.kept;
+  uint8_t* base = (slice < kSlices / 2 ? a.k_dst : a.v_dst) + (int64_t)a.dst_off[seg] * kRowBytes + (slice % (kSlices / 2)) * kSlice + (tid % kPer) * 16;
+  uint8_t* mine = stage + tid * 16;
+  const uint32_t mine_addr = smem_u32(mine);
+  int row[kEvInChunks];
+  auto dst_row = [&](int t, int i) { return t * kRows + (tid + i * kEvInThreads) / kPer; };
+  auto fetch_rows = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < kEvInRows; ++i) {
-      const int r = t0 + tid + i * kEvInThreads;
-      row[i] = r < len ? kept_row(a, s, seg, r) : r;
-      if (row[i] != r) {
-        const uint4* p = reinterpret_cast<const uint4*>(base + (int64_t)row[i] * kRowBytes);
-        v[i][0] = p[0];
-        v[i][1] = p[1];
-      }
+    for (int i = 0; i < kEvInChunks; ++i) {
+      const int r = dst_row(t, i);
+      row[i] = r < len ? kept_row(a, s, seg, r) : 0;
     }
-    __syncthreads();  // the tile has been read
+  };
+  auto request = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < kEvInRows; ++i) {
-      const int r = t0 + tid + i * kEvInThreads;
-      if (row[i] != r) {
-        uint4* p = reinterpret_cast<uint4*>(base + (int64_t)r * kRowBytes);
-        p[0] = v[i][0];
-        p[1] = v[i][1];
-      }
-    }
-    __syncthreads();
+    for (int i = 0; i < kEvInChunks; ++i)
+      if (dst_row(t, i) < len)
+        cp_async16(mine_addr + ((t % kEvInStages) * kEvInChunks + i) * kEvInThreads * 16, base + (int64_t)row[i] * kRowBytes, 16);
+    cp_async_commit();
+  };
+  const int tiles = (len + kRows - 1) / kRows;
+  fetch_rows(0);
+  for (int t = 0; t < kEvInStages - 1; ++t) {
+    request(t);
+    fetch_rows(t + 1);
   }
+  for (int t = 0; t < tiles; ++t) {
+    request(t + kEvInStages - 1);
+    fetch_rows(t + kEvInStages);
+    cp_async_wait<kEvInStages - 1>();
+    __syncthreads();  // the tile has been read by everybody
+#pragma unroll
+    for (int i = 0; i < kEvInChunks; ++i) {
+      const int r = dst_row(t, i);
+      if (r < len)
+        *reinterpret_cast<uint4*>(base + (int64_t)r * kRowBytes) =
+            *reinterpret_cast<const uint4*>(mine + ((t % kEvInStages) * kEvInChunks + i) * kEvInThreads * 16);
+    }
+  }
+  cp_async_wait<0>();
 }
 
 struct EvWs {
@@ -545,6 +574,8 @@ static int evict_attributes() {
   CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<4, false>, at, kEvStageMax * 4));
   CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<8, false>, at, kEvStageMax * 4));
   CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_gather_kernel, at, kEvMoveSmem));
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_inplace_kernel<32>, at, kEvInSmem));
+  CATEKV_CUDA_TRY(cudaFuncSetAttribute(evict_inplace_kernel<64>, at, kEvInSmem));
   if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   return CATEKV_OK;
 }
@@ -675,7 +706,14 @@ extern "C" int catekv_evict(const catekv_cache* src, const float* weights, const
   ma.chk = checked_status_ptr();
   ma.rows_per_cta = 0;
   if (in_place) {
-    CATEKV_CUDA_TRY(launch_pdl(evict_inplace_kernel, dim3(n * kEvSlices), dim3(kEvInThreads), 0, st, ma));
+    EvInArgs ia;
+    ia.m = ma;
+    ia.n_masked = n_masked;
+    ia.list = sa.list;
+    if (n_masked * 8 >= sm_count())
+      CATEKV_CUDA_TRY(launch_pdl(evict_inplace_kernel<64>, dim3(n_masked * 8 + n), dim3(kEvInThreads), kEvInSmem, st, ia));
+    else
+      CATEKV_CUDA_TRY(launch_pdl(evict_inplace_kernel<32>, dim3(n_masked * 16 + n), dim3(kEvInThreads), kEvInSmem, st, ia));
   } else {
     // two CTAs and more for every SM's three places, up to 256 rows each
     int64_t rows = dst_rows / (6 * sm_count()) / kEvTile * kEvTile;
