@@ -545,6 +545,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
 // running maximum of its own; the warps are then merged through shared memory in a fixed order.
 constexpr int kCombineWarps = 8;
 constexpr int kCombineUnroll = 16;
+template <int kUnroll>
 __device__ __forceinline__ void combine_segment(const CombineArgs& a, int seg, int hd) {
   const SegInfo si = a.seg_info[seg];  // plan data: older than the previous kernel
   pdl_wait();
@@ -561,11 +562,11 @@ __device__ __forceinline__ void combine_segment(const CombineArgs& a, int seg, i
   float wsum = 0.f, mw = -INFINITY;
   {
     const float* po = a.part_o + ((size_t)si.slot_begin * kMaxG + hd) * kD + lane * 4;
-    for (int p0 = warp; p0 < n; p0 += kCombineWarps * kCombineUnroll) {
-      float4 v[kCombineUnroll];
-      float w[kCombineUnroll];
+    for (int p0 = warp; p0 < n; p0 += kCombineWarps * kUnroll) {
+      float4 v[kUnroll];
+      float w[kUnroll];
 #pragma unroll
-      for (int u = 0; u < kCombineUnroll; ++u) {
+      for (int u = 0; u < kUnroll; ++u) {
         const int p = p0 + u * kCombineWarps;
         const bool ok = p < n;
         v[u] = ok ? *reinterpret_cast<const float4*>(po + (size_t)p * (kMaxG * kD)) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -573,7 +574,7 @@ __device__ __forceinline__ void combine_segment(const CombineArgs& a, int seg, i
       }
       float mx = mw;
 #pragma unroll
-      for (int u = 0; u < kCombineUnroll; ++u) mx = fmaxf(mx, w[u]);
+      for (int u = 0; u < kUnroll; ++u) mx = fmaxf(mx, w[u]);
       if (mx > -INFINITY) {
         const float sc = exp2f(mw - mx);  // 0 on the first pass (mw = -inf)
         acc.x *= sc;
@@ -583,7 +584,7 @@ __device__ __forceinline__ void combine_segment(const CombineArgs& a, int seg, i
         wsum *= sc;
         mw = mx;
 #pragma unroll
-        for (int u = 0; u < kCombineUnroll; ++u) {
+        for (int u = 0; u < kUnroll; ++u) {
           const float e = exp2f(w[u] - mx);  // an empty piece (LSE -inf) weighs 0
           acc.x += e * v[u].x;
           acc.y += e * v[u].y;
@@ -637,7 +638,7 @@ __device__ __forceinline__ void combine_segment(const CombineArgs& a, int seg, i
 
 __global__ void __launch_bounds__(kCombineWarps * 32) decode_combine_kernel(const CombineArgs a) {
   pdl_launch_dependents();
-  combine_segment(a, blockIdx.x, blockIdx.y);
+  combine_segment<kCombineUnroll>(a, blockIdx.x, blockIdx.y);
 }
 
 int launch_combine(const CombineArgs& a, int n_segs, cudaStream_t stream) {
@@ -809,14 +810,19 @@ struct WeightArgs {
 // Latency-bound: kWeightRows rows of a thread are in flight at once.
 constexpr int kWeightThreads = kCombineWarps * 32;
 constexpr int kWeightRows = 4;
-template <int kG>
+// kUnroll: pieces in flight per warp of the combine half.  With 8 the kernel has 64 registers and four CTAs per SM, with 16 (decode_combine_kernel's
+// own) 103 and two: the first is quicker while the logits are few (32K x 8 heads, G = 4, 4 MB of them: 18.8 against 19.7 us for the whole call),
+// the second where more CTAs at once mean more logits and weights passing through L2 at once (1.06 M rows, G = 7, 30 MB: 103 against 107 us;
+// 2.1 M rows, G = 8: 204 against 220); equal at 17 MB.
+constexpr int64_t kWeightFewBytes = 16 << 20;
+template <int kG, int kUnroll>
 __global__ void __launch_bounds__(kWeightThreads) combine_weight_kernel(const __grid_constant__ WeightArgs a) {
   __shared__ float s_lse[kG];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_launch_dependents();
   const int cta = blockIdx.x;
   if (cta >= a.num_ctas) {
-    combine_segment(a.c, (cta - a.num_ctas) / kG, (cta - a.num_ctas) % kG);
+    combine_segment<kUnroll>(a.c, (cta - a.num_ctas) / kG, (cta - a.num_ctas) % kG);
     return;
   }
   // plan data (older than the previous kernel): the CTA's items and a copy of the first
@@ -905,7 +911,9 @@ __global__ void __launch_bounds__(kWeightThreads) combine_weight_kernel(const __
 
 template <int kG>
 static cudaError_t launch_weights(const WeightArgs& a, int n_segs, cudaStream_t st) {
-  return launch_pdl(combine_weight_kernel<kG>, dim3(a.num_ctas + n_segs * kG), dim3(kWeightThreads), 0, st, a);
+  const dim3 grid(a.num_ctas + n_segs * kG), block(kWeightThreads);
+  if (a.logit_stride * kG * 4 <= kWeightFewBytes) return launch_pdl(combine_weight_kernel<kG, kCombineUnroll / 2>, grid, block, 0, st, a);
+  return launch_pdl(combine_weight_kernel<kG, kCombineUnroll>, grid, block, 0, st, a);
 }
 
 struct WeightedWs {
