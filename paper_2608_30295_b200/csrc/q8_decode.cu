@@ -33,9 +33,10 @@ constexpr int kQ8UnitBytes = 2 * kQ8Unit * kQ8RowBytes;  // K, then V
 static_assert(kQ8UnitBytes == 2 * kQ8TailUnit * kRowBytes, "both kinds of unit fill a stage");
 constexpr int kQ8SlotFloats = kMaxG * kD;                // a slot of the merge: [8 heads][128 d]
 constexpr int q8_decode_smem(int stages) { return kQ8Warps * stages * kQ8UnitBytes + 2 * kQ8SlotFloats * 4; }
-// Units a warp has requested or under way: three, except that long streams of e4m3 codes (whose conversion is quicker, so that more requests are
-// outstanding at a time) run faster with two.  Measured per CTA share of 7 K and 14 K rows: e4m3 82.1 and 159 us with two, 84.7 and 168 us with
-// three; int8 83.0 and 161 with two, 80.7 and 161 with three.  Below 4 K rows three are as good or better (1.8 K rows, e4m3: 27.6 and 26.7).
+// Units a warp has requested or under way: three while a CTA's share is short, where the ramp counts (1.8 K rows, G = 4: 25 us against 26), two
+// for long shares, where more requests than needed only disturb the order in which memory serves them (14 K rows, G = 4, either type:
+// 157 us against 166; 7 K rows: 83 against 86; equal at 3.5 K).  int8 codes for more than four heads are converted and multiplied slowly
+// enough for three at any length (14 K rows, G = 7: 158 us against 161; e4m3 there 171 against 158).
 constexpr int kQ8LongShare = 4096;
 // Segments of up to this many pieces are merged by the CTA that delivers the last one, longer ones by a combine pass (see catekv_q8_decode_attn).
 constexpr int kQ8MergePieces = 32;
@@ -124,7 +125,7 @@ __device__ __forceinline__ uint4 ldg128_here(const uint4* p) {
   return v;
 }
 // the group's queries, 4 x 16 bytes of this thread's head: d = 16 (c + 4 hh) + 8 e ... in x[2 hh + e]
-__device__ __forceinline__ void q8_load_q(const Q8DecodeArgs& a, int seg, int g, int c, uint4 (&x)[4]) {
+__device__ __forceinline__ void q8_load_q(const Q8DecodeArgs& a, int seg, int g, int c, uint4 (&x)[4]) {  // g: the head
   const int b = seg / a.Hkv, h = seg % a.Hkv;
   const uint4* p = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * a.G + g) * kD);
 #pragma unroll
@@ -186,7 +187,10 @@ __device__ __forceinline__ void q8_merge_pieces(const Q8DecodeArgs& a, int slot,
     a.lse_out[(size_t)b * a.Hq + (size_t)h * a.G + hd] = W == 0.f ? -INFINITY : (M + log2f(W)) * 0.6931471805599453f;
 }
 
-template <int kType, int kQ8Stages>
+// kPack (groups of up to four heads): columns 4..7 of the MMAs are the same heads again, their P the low halves: one MMA in place of two per
+// product of V (the kernel is short of MMA issue where a CTA's share is small: 128K x 3 heads, int8, 21.2 -> 19.5 us).  The two halves' sums
+// meet when a piece is merged.
+template <int kType, int kQ8Stages, bool kPack>
 __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_scale[kQ8Warps][kQ8Stages][2];
@@ -195,6 +199,8 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, c = lane & 3;
   const int pi = g ^ ((g & 1) << 2);  // token of row g
+  const int gq = kPack ? g & 3 : g;   // head of column g
+  const bool low_half = kPack && c >= 2;
   pdl_launch_dependents();
   int item_begin, item_end;
   WorkItem w0;
@@ -295,7 +301,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
   }
   pdl_wait();  // from here on: lengths, queries, and rows written by earlier kernels
   uint4 q4[4];
-  q8_load_q(a, w0.seg, g, c, q4);
+  q8_load_q(a, w0.seg, gq, c, q4);
   const int len0 = *reinterpret_cast<const volatile int32_t*>(a.seg_len + w0.seg);
   prefetch_item(item_begin + 1, w0.seg + 1);
   q8_live_cursor(w0, len0, pc);
@@ -421,8 +427,9 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
             l1 += p1;
             const uint32_t hi = pack_f16(p0, p1);
             const float2 hf = unpack_f16(hi);
-            bh[t][e] = movmatrix_trans(hi);
-            bl[t][e] = movmatrix_trans(pack_f16(p0 - hf.x, p1 - hf.y));
+            const uint32_t lo = pack_f16(p0 - hf.x, p1 - hf.y);
+            bh[t][e] = movmatrix_trans(low_half ? lo : hi);
+            if (!kPack) bl[t][e] = movmatrix_trans(lo);
           }
         // ---- O^T[128 d x 8 heads] += V^T P
         uint4 v[2][4];  // tokens 2c, (2c + 1) ^ 4, these + 8 of each half
@@ -445,8 +452,10 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
             q8_to_f16<kType>(__byte_perm(word(v[t][0], i), word(v[t][1], i), 0x7362), x2, x3);
             q8_to_f16<kType>(__byte_perm(word(v[t][2], i), word(v[t][3], i), 0x5140), z0, z1);
             q8_to_f16<kType>(__byte_perm(word(v[t][2], i), word(v[t][3], i), 0x7362), z2, z3);
-            mma_f16_16816(y0, x0, x1, z0, z1, bl[t][0], bl[t][1]);
-            mma_f16_16816(y1, x2, x3, z2, z3, bl[t][0], bl[t][1]);
+            if (!kPack) {
+              mma_f16_16816(y0, x0, x1, z0, z1, bl[t][0], bl[t][1]);
+              mma_f16_16816(y1, x2, x3, z2, z3, bl[t][0], bl[t][1]);
+            }
             mma_f16_16816(y0, x0, x1, z0, z1, bh[t][0], bh[t][1]);
             mma_f16_16816(y1, x2, x3, z2, z3, bh[t][0], bh[t][1]);
           }
@@ -458,7 +467,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
         }
       } else {
         // ---- 16 rows of the tail: bf16 on both sides, the same fragment slots (the queries are read again)
-        const uint4* qp = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * a.G + g) * kD);
+        const uint4* qp = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.Hq + h * a.G + gq) * kD);
         const int left = cc.tail - (u - cc.full) * kQ8TailUnit;
         float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -468,7 +477,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
             const int ch = 2 * (c + 4 * hh) + e;
             const uint4 lo = lds128(kb + tile_off(pi, ch)), hi = lds128(kb + tile_off(pi + 8, ch));
             const uint32_t f[2][4] = {{lo.x, hi.x, lo.y, hi.y}, {lo.z, hi.z, lo.w, hi.w}};
-            const uint4 x = g < a.G ? qp[ch] : make_uint4(0, 0, 0, 0);
+            const uint4 x = gq < a.G ? qp[ch] : make_uint4(0, 0, 0, 0);
             mma_bf16_16816(s, f[0], x.x, x.y);
             mma_bf16_16816(s, f[1], x.z, x.w);
           }
@@ -485,11 +494,12 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
         p2 *= kQ8PUnit;
         p3 *= kQ8PUnit;
         const float h0 = bf16_round(p0), h1 = bf16_round(p1), h2 = bf16_round(p2), h3 = bf16_round(p3);
-        const uint32_t bh0 = movmatrix_trans(pack_bf16(h0, h1)), bh1 = movmatrix_trans(pack_bf16(h2, h3));
         const float d0 = p0 - h0, d1 = p1 - h1, d2 = p2 - h2, d3 = p3 - h3;  // three bf16 parts: 24 bits
-        const uint32_t bl0 = movmatrix_trans(pack_bf16(d0, d1)), bl1 = movmatrix_trans(pack_bf16(d2, d3));
-        const uint32_t bm0 = movmatrix_trans(pack_bf16(d0 - bf16_round(d0), d1 - bf16_round(d1)));
-        const uint32_t bm1 = movmatrix_trans(pack_bf16(d2 - bf16_round(d2), d3 - bf16_round(d3)));
+        const uint32_t hi0 = pack_bf16(h0, h1), hi1 = pack_bf16(h2, h3), lo0 = pack_bf16(d0, d1), lo1 = pack_bf16(d2, d3);
+        const uint32_t bh0 = movmatrix_trans(low_half ? lo0 : hi0), bh1 = movmatrix_trans(low_half ? lo1 : hi1);
+        const uint32_t bl0 = kPack ? 0u : movmatrix_trans(lo0), bl1 = kPack ? 0u : movmatrix_trans(lo1);
+        const uint32_t mi0 = pack_bf16(d0 - bf16_round(d0), d1 - bf16_round(d1)), mi1 = pack_bf16(d2 - bf16_round(d2), d3 - bf16_round(d3));
+        const uint32_t bm0 = movmatrix_trans(low_half ? 0u : mi0), bm1 = movmatrix_trans(low_half ? 0u : mi1);
         const int t0 = 2 * c, t1 = (2 * c + 1) ^ 4;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -501,7 +511,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
             const uint32_t af[4] = {__byte_perm(word(v0, i), word(v1, i), 0x5410), __byte_perm(word(v0, i), word(v1, i), 0x7632),
                                     __byte_perm(word(v2, i), word(v3, i), 0x5410), __byte_perm(word(v2, i), word(v3, i), 0x7632)};
             mma_bf16_16816(o[4 * e + i], af, bm0, bm1);
-            mma_bf16_16816(o[4 * e + i], af, bl0, bl1);
+            if (!kPack) mma_bf16_16816(o[4 * e + i], af, bl0, bl1);
             mma_bf16_16816(o[4 * e + i], af, bh0, bh1);
           }
         }
@@ -509,7 +519,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
     }
 
     // ---- end of the piece: merge the four warps (warps 0 and 1 fill a slot each, 2 and 3 add to them, everybody writes a part of the sum)
-    if (item + 1 < item_end) q8_load_q(a, cc.seg + 1, g, c, q4);  // on their way during the merge
+    if (item + 1 < item_end) q8_load_q(a, cc.seg + 1, gq, c, q4);  // on their way during the merge
     int si_slot = 0, si_pieces = 0;
     if (a.merge && cc.slot >= 0) {
       const int2 x = __ldg(reinterpret_cast<const int2*>(a.merge + cc.seg));
@@ -566,9 +576,13 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
       l *= kQ8PUnit;
       const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
       const float lse = l == 0.f ? -INFINITY : M + log2f(l);
-      const float4 x = *reinterpret_cast<const float4*>(slots + q8_slot(hd, 4 * lane));
-      const float4 y = *reinterpret_cast<const float4*>(slots + kQ8SlotFloats + q8_slot(hd, 4 * lane));
-      const float4 v = make_float4((x.x + y.x) * inv, (x.y + y.y) * inv, (x.z + y.z) * inv, (x.w + y.w) * inv);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < (kPack ? 4 : 2); ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(slots + (i & 1) * kQ8SlotFloats + q8_slot(hd + 4 * (i >> 1), 4 * lane));
+        v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+      }
+      v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
       const size_t at = ((size_t)b * a.Hq + (size_t)h * a.G + hd) * kD;
       if (cc.slot >= 0)
         reinterpret_cast<float4*>(a.part_o + ((size_t)cc.slot * kMaxG + hd) * kD)[lane] = v;
@@ -667,31 +681,35 @@ __global__ void __launch_bounds__(kQ8CombineThreads, 7) q8_combine_kernel(const 
 using namespace catekv;
 
 // the kernels' shared-memory limits, once per device
-template <int kType, int kStages>
+template <int kType, int kStages, bool kPack>
 static cudaError_t q8_allow_smem() {
-  return cudaFuncSetAttribute(q8_decode_partial_kernel<kType, kStages>, cudaFuncAttributeMaxDynamicSharedMemorySize, q8_decode_smem(kStages));
+  return cudaFuncSetAttribute(q8_decode_partial_kernel<kType, kStages, kPack>, cudaFuncAttributeMaxDynamicSharedMemorySize, q8_decode_smem(kStages));
 }
 static int q8_decode_attributes() {
   static std::atomic<bool> attr_set[64];
   int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
   if (dev >= 0 && dev < 64 && attr_set[dev].load(std::memory_order_acquire)) return CATEKV_OK;
-  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 2>()));
-  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 3>()));
-  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_INT8, 3>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 2, false>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 2, true>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 3, false>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_E4M3, 3, true>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_INT8, 2, true>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_INT8, 3, false>()));
+  CATEKV_CUDA_TRY((q8_allow_smem<CATEKV_Q8_INT8, 3, true>()));
   if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   return CATEKV_OK;
 }
-template <int kType, int kStages>
+template <int kType, int kStages, bool kPack>
 static cudaError_t q8_launch_partials(const Q8DecodeArgs& a, int num_ctas, cudaStream_t st) {
-  return launch_pdl(q8_decode_partial_kernel<kType, kStages>, dim3(num_ctas), dim3(kQ8DecodeThreads), q8_decode_smem(kStages), st, a);
+  return launch_pdl(q8_decode_partial_kernel<kType, kStages, kPack>, dim3(num_ctas), dim3(kQ8DecodeThreads), q8_decode_smem(kStages), st, a);
 }
 
 extern "C" int catekv_q8_decode_num_ctas(void) {
   int rc = q8_decode_attributes();
   if (rc) return rc;
   int per_sm = 0;
-  CATEKV_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, q8_decode_partial_kernel<CATEKV_Q8_E4M3, 3>, kQ8DecodeThreads, q8_decode_smem(3)));
+  CATEKV_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, (q8_decode_partial_kernel<CATEKV_Q8_E4M3, 3, false>), kQ8DecodeThreads, q8_decode_smem(3)));
   return sm_count() * (per_sm < 1 ? 1 : per_sm);
 }
 
@@ -755,12 +773,19 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
   a.out_fp32 = out_dtype == CATEKV_OUT_FP32;
   a.lse_out = lse_out;
   a.merge = hdr->max_pieces <= kQ8MergePieces ? (SegInfo*)((uint8_t*)plan_dev + L.off_seg) : nullptr;
-  if (cache->dtype == CATEKV_Q8_INT8)
-    CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_INT8, 3>(a, hdr->num_ctas, st)));
-  else if (hdr->total_rows >= (int64_t)kQ8LongShare * hdr->num_ctas)
-    CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 2>(a, hdr->num_ctas, st)));
-  else
-    CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 3>(a, hdr->num_ctas, st)));
+  const bool longs = hdr->total_rows >= (int64_t)kQ8LongShare * hdr->num_ctas, pack = G <= 4;
+  const int n = hdr->num_ctas;
+  if (cache->dtype == CATEKV_Q8_INT8) {
+    if (!pack) CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_INT8, 3, false>(a, n, st)));
+    else if (longs) CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_INT8, 2, true>(a, n, st)));
+    else CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_INT8, 3, true>(a, n, st)));
+  } else if (longs) {
+    if (pack) CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 2, true>(a, n, st)));
+    else CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 2, false>(a, n, st)));
+  } else {
+    if (pack) CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 3, true>(a, n, st)));
+    else CATEKV_CUDA_TRY((q8_launch_partials<CATEKV_Q8_E4M3, 3, false>(a, n, st)));
+  }
   if (hdr->n_slots > 0 && !a.merge) {
     CombineArgs ca;
     ca.seg_info = (const SegInfo*)(pd + L.off_seg);

@@ -414,3 +414,17 @@ def test_refusals_leave_everything_as_it_was(ck):
     with pytest.raises(ck.CatekvError) as e:
         ck.catekv_q8_decode_attn(c, q.cpu(), plan, torch.empty(1, 4, 128, device="cuda"))
     assert e.value.code == ck.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("G", [3, 4, 5])
+def test_long_shares(ck, dtype, G):
+    # one CTA with a long share: the variant that long streams take, against the same rows shared out over many CTAs and the oracle
+    lens = [9000, 5, 4999, 64]
+    k, v = _rows(lens, 150)
+    c = _quantized(ck, k, v, 1, 4, dtype)
+    q = synth.randn_bf16((1, 4 * G, 128), "cuda", 151, "q", G)
+    ref = _oracle(k, v, q, 1, 4, dtype)
+    for ctas in (1, 2, 3, 100):
+        out, lse = _attend(ck, c, q, ctas)
+        _check_attention(out, lse, ref, ctas)
