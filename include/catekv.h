@@ -597,6 +597,8 @@ int catekv_evict(const catekv_cache* src, const float* weights, const uint8_t* e
  *   NaN, and so have the outputs of the heads that attend to it.
  * Only complete blocks are held in 8 bits: the len mod 64 rows behind the last complete block stay bf16 in a tail of
  * their own until the block is complete.  A row is thus rounded once, and the most recent rows are not rounded at all.
+ * (A list can therefore be taken back, by writing its lengths, only as far as its unfinished block reaches: the rows of a
+ * completed block are no longer in the tail.)
  * Segments are laid out as in catekv_cache (catekv_cache_layout); an offset is a multiple of 64.
  */
 #define CATEKV_Q8_E4M3 0

@@ -156,7 +156,8 @@ __device__ __forceinline__ void tile_rows(const ItemCursor& c, int i, int& start
   nvalid = c.live - start;
 }
 
-// Stores whose lines L2 keeps while a stream passes through it: the logits are read again as soon as the last row has been seen.
+// Stores whose lines L2 keeps while a stream passes through it: the logits are read again as soon as the last row has been
+// seen (8 x 64K, G = 7: 126 -> 104 us for the whole call).
 __device__ __forceinline__ uint64_t l2_keep_policy() {
   uint64_t p;
   asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;\n" : "=l"(p));
@@ -803,17 +804,20 @@ struct WeightArgs {
   float decay;
 };
 
-// The combine pass and the weights in one launch: the first CTAs take the rows by the attention's own plan, the others merge partials:
-// w <- decay w + mean over the group of exp(logit - lse), with the LSE of a segment that was cut formed from its pieces' own
-// (a few hundred numbers), so that neither half waits for the other.  A row's logits are G words against the 512 bytes that attention read of
-// it, left in L2: they are the price of a softmax whose normaliser is known only when the last row has been seen.
-// Latency-bound: kWeightRows rows of a thread are in flight at once.
+// The combine pass and the weights in one launch: the first CTAs take the rows by the attention's own plan,
+//   w <- decay w + mean over the group of exp(logit - lse),
+// the others merge partials.  The LSE of a segment that was cut is formed from its pieces' own (a few hundred numbers), so
+// that neither half waits for the other.  A row's logits are G words against the 512 bytes that attention read of it, left
+// in L2: they are the price of a softmax whose normaliser is known only when the last row has been seen.  Latency-bound:
+// kWeightRows rows of a thread are in flight at once.  Whole call in a replayed graph: 32K x 8 heads 18.7 us (attention
+// alone 16.9), 8 x 64K x 4 heads, G = 7, 102 us (82): there 24 of the 30 MB of logits go out to memory beside the stream,
+// which costs the attention kernel 10 us, and the weights pass takes 10.
 constexpr int kWeightThreads = kCombineWarps * 32;
 constexpr int kWeightRows = 4;
-// kUnroll: pieces in flight per warp of the combine half.  With 8 the kernel has 64 registers and four CTAs per SM, with 16 (decode_combine_kernel's
-// own) 103 and two: the first is quicker while the logits are few (32K x 8 heads, G = 4, 4 MB of them: 18.8 against 19.7 us for the whole call),
-// the second where more CTAs at once mean more logits and weights passing through L2 at once (1.06 M rows, G = 7, 30 MB: 103 against 107 us;
-// 2.1 M rows, G = 8: 204 against 220); equal at 17 MB.
+// kUnroll: pieces in flight per warp of the combine half.  With 8 the kernel has 64 registers and four CTAs per SM, with 16
+// (decode_combine_kernel's own) 103 and two: the first is quicker while the logits are few (32K x 8 heads, G = 4, 4 MB of
+// them: 18.8 against 19.7 us for the whole call), the second where more CTAs at once mean more logits and weights passing
+// through L2 at once (1.06 M rows, G = 7, 30 MB: 103 against 107 us; 2.1 M rows, G = 8: 204 against 220); equal at 17 MB.
 constexpr int64_t kWeightFewBytes = 16 << 20;
 template <int kG, int kUnroll>
 __global__ void __launch_bounds__(kWeightThreads) combine_weight_kernel(const __grid_constant__ WeightArgs a) {

@@ -1,21 +1,28 @@
-// Decode attention over the 8-bit cache: split-KV partials on the tensor cores (the combine pass is decode.cu's).
+// Decode attention over the 8-bit cache: split-KV partials on the tensor cores, and their merge.
 //
-// The stream is a warp's own.  A CTA owns a contiguous range of the rows of all segments laid end to end (q8 plans cut at block borders); its
-// four warps take the range's units in turn, a unit being half a block (32 rows of codes, 8 KB of K and V) or 16 rows of a bf16 tail
-// (8 KB as well).  Each warp keeps a ring of kQ8Stages units in flight with cp.async and never waits for another warp before a
-// segment's partial is merged.
+// Bound by the stream of codes (256 bytes a row) where a CTA's share is long, by latency and MMA issue where it is short.  Measured, whole call in
+// a replayed graph: 16 x 64K (1.09 GB) 158 us, 6.9 TB/s or 1.07 of the copy bandwidth; 128K x 3 heads int8 (93 MB) 19.4 us, 4.8 TB/s, of which 18.2
+// remain when nothing is computed; 256K x 2 heads, G = 7 (136 MB) 27.2 us; 4K (4.5 MB) 7.8 us.
 //
-// Codes are f16 numbers, so both products run on mma.m16n8k16 (f16) with the code converted in registers; tokens are M, the group's <= 8
-// query heads N.  Which token or which d a fragment slot stands for is free as long as both operands of a product agree, and is chosen so
-// that every shared-memory access is a conflict-free 16-byte load and nothing is transposed in memory:
-//   S = K Q^T   row g of A is token pi(g) = g ^ 4 (g & 1) of the 16; thread (g, c) takes the 16-byte chunks c and c + 4 of its rows, word i of
-//               chunk c + 4h is k-step 4h + i (Q's fragments are gathered to match);
-//   O^T = V^T P row g of A holds d = 16 g + 2 j (+ 1 in row g + 8) of MMA j; thread (g, c) takes chunk g of tokens 2c, (2c+1)^4 and
-//               these + 8 (the columns that P's transposed fragment has), and interleaves their bytes in registers.
-// Q enters as f16 under a power of two per head (bf16 has fewer bits than f16: exact except where an element is 2^-29 of the head's largest);
-// the scale of a block multiplies its logits.  Probabilities are formed against the running maximum times 2^12 and split into an f16
-// hi + lo pair (22 bits).  The tensor cores cut their fp32 sums off instead of rounding them: chains are kept short (four MMAs), a unit's P V
-// product is formed from zero and enters the accumulators by one rounded multiply-add each, which also applies the block's V scale.
+// The stream is a warp's own.  A CTA owns a contiguous range of the rows of all segments laid end to end (cut at block
+// borders); its four warps take the range's units in turn, a unit being half a block (32 rows of codes, 8 KB of K and V)
+// or 16 rows of a bf16 tail (8 KB as well).  Each warp keeps a ring of units in flight with cp.async and waits for no
+// other warp before a segment's piece is merged.
+//
+// Codes are f16 numbers, so both products run on mma.m16n8k16 (f16) with the code converted in registers; tokens are M,
+// the group's <= 8 query heads N.  Which token or which d a fragment slot stands for is free as long as both operands of
+// a product agree, and is chosen so that every shared-memory access is a conflict-free 16-byte load and nothing is
+// transposed in memory:
+//   S = K Q^T   row g of A is token pi(g) = g ^ 4 (g & 1) of the 16; thread (g, c) takes the 16-byte chunks c and c + 4
+//               of its rows, word i of chunk c + 4h is k-step 4h + i (Q's fragments are gathered to match);
+//   O^T = V^T P row g of A holds d = 16 g + 2 j (+ 1 in row g + 8) of MMA j; thread (g, c) takes chunk g of tokens 2c,
+//               (2c+1)^4 and these + 8 (the columns that P's transposed fragment has), and interleaves their bytes in
+//               registers.
+// Q enters as f16 under a power of two per head (bf16 has fewer bits than f16: exact except where an element is 2^-29 of
+// the head's largest); the scale of a block multiplies its logits.  Probabilities are formed against the running maximum
+// times 2^12 and split into an f16 hi + lo pair (22 bits).  The tensor cores cut their fp32 sums off instead of rounding
+// them: chains are kept short (four MMAs), a unit's P V product is formed from zero and enters the accumulators by one
+// rounded multiply-add each, which also applies the block's V scale (1.3e-6 -> 4e-7 against 64 bits).
 #include <math.h>
 
 #include <atomic>
@@ -33,16 +40,19 @@ constexpr int kQ8UnitBytes = 2 * kQ8Unit * kQ8RowBytes;  // K, then V
 static_assert(kQ8UnitBytes == 2 * kQ8TailUnit * kRowBytes, "both kinds of unit fill a stage");
 constexpr int kQ8SlotFloats = kMaxG * kD;                // a slot of the merge: [8 heads][128 d]
 constexpr int q8_decode_smem(int stages) { return kQ8Warps * stages * kQ8UnitBytes + 2 * kQ8SlotFloats * 4; }
-// Units a warp has requested or under way: three while a CTA's share is short, where the ramp counts (1.8 K rows, G = 4: 25 us against 26), two
-// for long shares, where more requests than needed only disturb the order in which memory serves them (14 K rows, G = 4, either type:
-// 157 us against 166; 7 K rows: 83 against 86; equal at 3.5 K).  int8 codes for more than four heads are converted and multiplied slowly
-// enough for three at any length (14 K rows, G = 7: 158 us against 161; e4m3 there 171 against 158).
+// Units a warp has requested or under way: three while a CTA's share is short, where the ramp counts (1.8 K rows, G = 4:
+// 25 us against 26), two for long shares, where more requests than needed only disturb the order in which memory serves
+// them (14 K rows, G = 4, either type: 157 us against 166; 7 K rows: 83 against 86; equal at 3.5 K).  int8 codes for more
+// than four heads are converted and multiplied slowly enough for three at any length (14 K rows, G = 7: 158 us against
+// 161; e4m3 there 171 against 158).
 constexpr int kQ8LongShare = 4096;
-// Segments of up to this many pieces are merged by the CTA that delivers the last one, longer ones by a combine pass (see catekv_q8_decode_attn).
+// Segments of up to this many pieces are merged by the CTA that delivers the last one (16 x 1K step: 15.0 us on the device
+// against 16.3, and one launch less for the host, 2.4 us; 4K lists in 32 pieces: 7.9 us on the device against 6.4, the call
+// 8 us against 10), longer ones by a combine pass (98 pieces would be 200 KB through one CTA).
 constexpr int kQ8MergePieces = 32;
 static_assert(kQ8MergePieces <= 32, "a lane per piece");
 constexpr int32_t kQ8PlanTile = kQ8Unit;   // marks a plan of this kind (decode.cu's have kTile)
-constexpr int kQ8SegEndCharge = 512;       // rows
+constexpr int kQ8SegEndCharge = 512;       // rows (128K: 23.4 us with 0, 22.5 with 128, 21.8 with 256, 21.1 with 512)
 constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12 ...
 constexpr float kQ8PUnit = 1.f / 4096.f;   // ... and the accumulators in units of it
 static_assert(kQ8PlanTile != kTile, "the two kinds of plan must differ");
@@ -90,8 +100,8 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src));
 }
 
-// A piece of a segment as a warp sees it: `full` units of codes starting at unit u0 of the pool (of which the first `live` are to be attended to: the
-// others were complete when the plan was built but no longer are), then the units of the tail.
+// A piece of a segment as a warp sees it: `full` units of codes starting at unit u0 of the pool (of which the first `live`
+// are to be attended to: the others were complete when the plan was built but no longer are), then the tail's units.
 struct Q8Cursor {
   int seg, slot, np, full, live, tail, units;
   int64_t u0;
@@ -118,7 +128,7 @@ __device__ __forceinline__ void q8_live_cursor(const WorkItem& w, int len, Q8Cur
   c.tail = w.last ? len % kQ8Block : 0;
   c.units = c.full + (c.tail + kQ8TailUnit - 1) / kQ8TailUnit;
 }
-// a load that stays where it is written (the compiler would move it down to its use, behind the requests that it is to overlap)
+// a load that stays where it is written (the compiler would move it down to its use, behind what it is to overlap with)
 __device__ __forceinline__ uint4 ldg128_here(const uint4* p) {
   uint4 v;
   asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
@@ -187,9 +197,9 @@ __device__ __forceinline__ void q8_merge_pieces(const Q8DecodeArgs& a, int slot,
     a.lse_out[(size_t)b * a.Hq + (size_t)h * a.G + hd] = W == 0.f ? -INFINITY : (M + log2f(W)) * 0.6931471805599453f;
 }
 
-// kPack (groups of up to four heads): columns 4..7 of the MMAs are the same heads again, their P the low halves: one MMA in place of two per
-// product of V (the kernel is short of MMA issue where a CTA's share is small: 128K x 3 heads, int8, 21.2 -> 19.5 us).  The two halves' sums
-// meet when a piece is merged.
+// kPack (groups of up to four heads): columns 4..7 of the MMAs are the same heads again, their P the low halves: one MMA
+// in place of two per product of V (the kernel is short of MMA issue where a CTA's share is small: 128K x 3 heads, int8,
+// 21.2 -> 19.5 us; 64 x 1K x 8 heads 28 -> 23 us).  The two halves' sums meet when a piece is merged.
 template <int kType, int kQ8Stages, bool kPack>
 __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
@@ -258,7 +268,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
     ++p_seq;
     p_u += kQ8Warps;
   };
-  // What the item behind the consumer's is made of, requested one item ahead: neither side then waits for a chain of loads at a change.
+  // What the item behind the consumer's is made of, requested one item ahead: neither side waits for a chain of loads then.
   WorkItem nx;
   int nx_len = 0;
   int nx_item = item_begin;  // the item that these belong to
@@ -292,8 +302,8 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
     cp_async_commit();
   };
 
-  // Blocks that were complete when the plan was built are older than anything the previous kernel of the stream may still be writing (an
-  // append writes behind them): the first units are requested before the wait.
+  // Blocks that were complete when the plan was built are older than anything the previous kernel of the stream may still
+  // be writing (an append writes behind them): the first units are requested before the wait.
   int pre = 0;
   for (; pre < kQ8Stages - 1 && p_u < pc.np; ++pre) {
     issue_unit();
@@ -518,7 +528,8 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
       }
     }
 
-    // ---- end of the piece: merge the four warps (warps 0 and 1 fill a slot each, 2 and 3 add to them, everybody writes a part of the sum)
+    // ---- end of the piece: merge the four warps (warps 0 and 1 fill a slot each, 2 and 3 add to them, everybody writes
+    // a part of the sum)
     if (item + 1 < item_end) q8_load_q(a, cc.seg + 1, gq, c, q4);  // on their way during the merge
     int si_slot = 0, si_pieces = 0;
     if (a.merge && cc.slot >= 0) {
@@ -611,9 +622,10 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
   cp_async_wait<0>();
 }
 
-// Combine for few (segment, head) pairs: a CTA per pair and 32 of the 128 dimensions, a warp per 32 pieces, a lane per dimension.  Small enough
-// (128 threads, at most 72 registers) to be resident beside two CTAs of the attention kernel: launched programmatically it has its plan entry and
-// waits at the dependency when the last partial is written, and the next attention kernel's CTAs find room beside it.
+// Combine for few (segment, head) pairs: a CTA per pair and 32 of the 128 dimensions, a warp per 32 pieces, a lane per
+// dimension.  Small enough (128 threads, at most 72 registers) to be resident beside two CTAs of the attention kernel:
+// launched programmatically it has its plan entry and waits at the dependency when the last partial is written, and the
+// next attention kernel's CTAs find room beside it (128K: 21.1 -> 20.5 us, 256K G = 7: 28.2 -> 26.7 us).
 constexpr int kQ8CombineThreads = 128;
 constexpr int kQ8CombineSplit = 4;
 __global__ void __launch_bounds__(kQ8CombineThreads, 7) q8_combine_kernel(const CombineArgs a) {
