@@ -737,6 +737,8 @@ def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, s
                  dst: Optional[Cache] = None, dst_weights: Optional[torch.Tensor] = None,
                  idx_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """Cut the masked segments to `budget` rows by weight, into `dst` and `dst_weights`, or in place without them."""
+    if (dst is None) != (dst_weights is None):
+        raise CatekvError(ERR_INVALID_ARG, "catekv_evict")
     if dst is None:
         dst, dst_weights = cache, weights
     _int32("catekv_evict", budget, sink, local)
