@@ -368,7 +368,8 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
       }
       const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
       if (__any_sync(0xffffffffu, mn0 > m0 || mn1 > m1)) {
-        const float al0 = fast_exp2(m0 - mn0), al1 = fast_exp2(m1 - mn1);  // exp2(-inf) = 0 on the first unit
+        // exp2(-inf) = 0 on the first unit; a head whose logits have all been -inf (an infinite key) stays as it is
+        const float al0 = mn0 > m0 ? fast_exp2(m0 - mn0) : 1.f, al1 = mn1 > m1 ? fast_exp2(m1 - mn1) : 1.f;
         l0 *= al0;
         l1 *= al1;
 #pragma unroll
@@ -426,7 +427,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
           x[t][3] = s[t][3] * k1;
         }
         rescale(fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2])), fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3])));
-        const float r0 = kQ8PBits - m0, r1 = kQ8PBits - m1;
+        const float r0 = m0 > -INFINITY ? kQ8PBits - m0 : 0.f, r1 = m1 > -INFINITY ? kQ8PBits - m1 : 0.f;
         uint32_t bh[2][2], bl[2][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -495,7 +496,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
         const float x0 = v_lo ? s[0] * a.scale_log2 : -INFINITY, x1 = v_lo ? s[1] * a.scale_log2 : -INFINITY;
         const float x2 = v_hi ? s[2] * a.scale_log2 : -INFINITY, x3 = v_hi ? s[3] * a.scale_log2 : -INFINITY;
         rescale(fmaxf(x0, x2), fmaxf(x1, x3));
-        const float r0 = kQ8PBits - m0, r1 = kQ8PBits - m1;
+        const float r0 = m0 > -INFINITY ? kQ8PBits - m0 : 0.f, r1 = m1 > -INFINITY ? kQ8PBits - m1 : 0.f;
         float p0 = fast_exp2(x0 + r0), p1 = fast_exp2(x1 + r1), p2 = fast_exp2(x2 + r0), p3 = fast_exp2(x3 + r1);
         l0 += p0 + p2;
         l1 += p1 + p3;

@@ -428,3 +428,24 @@ def test_long_shares(ck, dtype, G):
     for ctas in (1, 2, 3, 100):
         out, lse = _attend(ck, c, q, ctas)
         _check_attention(out, lse, ref, ctas)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("G", [4, 6])
+def test_infinite_keys_in_a_tail(ck, dtype, G):
+    # every tail row of a list holds an infinity: heads for which its logit is -inf see the block alone, the others NaN
+    lens = [66, 64 * 5 + 33, 65]
+    k, v = _rows(lens, 160)
+    for s, n in enumerate(lens):
+        k[s][n // 64 * 64:, 0] = float("inf")
+    c = _quantized(ck, k, v, 1, 3, dtype)
+    q = synth.randn_bf16((1, 3 * G, 128), "cuda", 161, "q", G)
+    full = [n // 64 * 64 for n in lens]
+    r, rl, vmax = _oracle([x[:n] for x, n in zip(k, full)], [x[:n] for x, n in zip(v, full)], q, 1, 3, dtype)
+    gone = (q[0, :, 0] < 0).cpu().numpy()
+    assert gone.any() and not gone.all()
+    for ctas in (1, 3, 60):
+        out, lse = _attend(ck, c, q, ctas)
+        g = out[0].double().cpu().numpy()
+        assert np.isnan(g[~gone]).any(axis=1).all()
+        assert H.rel_l2(g[gone], r[0][gone]) <= 1e-4 and np.abs(lse[0].cpu().numpy()[gone] - rl[0][gone]).max() <= 1e-4
