@@ -1,7 +1,7 @@
 // Eviction by accumulated attention weight: the selection of what a list keeps, and the move of it, into another cache or
 // in place.  Measured in a replayed graph: 64 lists of a batch (24 of 49 K cut to half, the others copied, 902 MB) 161 us,
 // 0.87 of the copy bandwidth, of which 137 are the move and 20 the selection; four lists of 1280 cut to 1024: 8.3 us (two
-// launches); the first in place 167 us (604 MB of it moved).
+// launches); the first in place 130 us (604 MB moved).
 #include <math.h>
 
 #include <atomic>
@@ -441,13 +441,14 @@ __global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const __gr
 
 // In place.  Kept row j comes from row idx[j] >= j, so a tile of destination rows may be written once it has been read
 // itself: nothing behind it reads there, and what is requested ahead lies behind it.  That makes a segment sequential in
-// its rows, so the work is split over the columns instead: a CTA moves kSlice bytes of every row of K or V, three tiles
+// its rows, so the work is split over the columns instead: a CTA moves kSlice bytes of every row of K or V, two tiles
 // ahead with cp.async and one barrier per tile (the tile has been read by everybody; the writes are a thread's own).
-// 64 bytes are two DRAM sectors; 32, where the segments are few, make twice the CTAs.  (32 bytes and a tile at a time
-// through registers took the 24 lists of 49 K 303 us instead of 167.)
-constexpr int kEvInThreads = 256;
-constexpr int kEvInTileBytes = 16384;
-constexpr int kEvInStages = 4;
+// 64 bytes are two DRAM sectors; 32, where the segments are few, make twice the CTAs.  Large tiles pay: 24 lists of 49 K,
+// selection included, take 130 us with tiles of 32 KB and three stages, 167 with 16 KB and four, 206 with 8 KB and eight
+// (303 with a tile at a time through registers).
+constexpr int kEvInThreads = 512;
+constexpr int kEvInTileBytes = 32768;
+constexpr int kEvInStages = 3;
 constexpr int kEvInSmem = kEvInStages * kEvInTileBytes;
 constexpr int kEvInChunks = kEvInTileBytes / (16 * kEvInThreads);  // 16-byte chunks of a thread in a tile
 constexpr int kEvWRows = 8;                                        // weights of a thread in a tile
