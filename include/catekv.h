@@ -549,7 +549,7 @@ int catekv_decode_attn_noalloc(const catekv_cache* cache, const void* q, int32_t
  * at 0 when it is appended.
  *   ws  at least catekv_decode_weighted_workspace_bytes(...) with the cache's total_rows; q, out and ws 16-byte aligned
  * CATEKV_ERR_UNSUPPORTED for a cache with overflow pages; CATEKV_ERR_INVALID_ARG for a plan made for longer lists (the
- * cache has been cut since).
+ * cache has been cut since) and for a cache whose lengths are upper bounds (catekv_cache_sync_lengths makes them exact).
  */
 size_t catekv_decode_weighted_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_ctas, int64_t total_rows);
 int catekv_decode_attn_weighted(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
@@ -621,7 +621,7 @@ typedef struct catekv_q8_cache {
   const int32_t* seg_off;     /* host   [B*Hkv] */
   const int32_t* seg_cap;     /* host   [B*Hkv] */
   int32_t* seg_len;           /* host   [B*Hkv], mirror of seg_len_dev kept by the library's calls */
-  int32_t reserved;           /* 0; copied from the source by catekv_q8_quantize (1: seg_len holds upper bounds) */
+  int32_t reserved;           /* 0 */
   int32_t reserved1;          /* 0 */
 } catekv_q8_cache;
 
@@ -629,7 +629,8 @@ typedef struct catekv_q8_cache {
  * Every segment of `src` (no overflow pages) into the same segment of `dst`: complete blocks as codes and scales, the rows
  * behind them into the tail; dst's lengths are set (device and host).  Rows behind a segment's length are neither read
  * nor written.  CATEKV_ERR_CAPACITY (nothing launched) if a segment does not fit; CATEKV_ERR_INVALID_ARG if the caches
- * differ in B or Hkv; CATEKV_ERR_UNSUPPORTED for a source with overflow pages or more than 65535 segments.
+ * differ in B or Hkv or src->reserved is set (catekv_cache_sync_lengths makes its lengths exact); CATEKV_ERR_UNSUPPORTED
+ * for a source with overflow pages or more than 65535 segments.
  */
 int catekv_q8_quantize(const catekv_cache* src, catekv_q8_cache* dst, catekv_stream stream);
 

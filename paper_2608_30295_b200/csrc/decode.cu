@@ -947,6 +947,7 @@ extern "C" int catekv_decode_attn_weighted(const catekv_cache* cache, const void
   int rc = check_cache(cache);
   if (rc) return rc;
   if (cache->pages) return CATEKV_ERR_UNSUPPORTED;
+  if (cache->reserved) return CATEKV_ERR_INVALID_ARG;  // lengths that are upper bounds (see plan_outlived)
   if (!weights || !ws || !plan_host || !plan_dev || !(decay >= 0.f && decay <= 1.f) || Hq <= 0 || Hq % cache->Hkv) return CATEKV_ERR_INVALID_ARG;
   if ((((uintptr_t)q | (uintptr_t)out | (uintptr_t)ws) & 15) || ((uintptr_t)weights & 3)) return CATEKV_ERR_INVALID_ARG;
   const int n_segs = cache->B * cache->Hkv;

@@ -217,6 +217,8 @@ extern "C" int catekv_q8_quantize(const catekv_cache* src, catekv_q8_cache* dst,
   rc = check_q8_cache(dst);
   if (rc) return rc;
   if (src->pages) return CATEKV_ERR_UNSUPPORTED;
+  // lengths that are upper bounds would make plans count blocks as complete that are not
+  if (src->reserved) return CATEKV_ERR_INVALID_ARG;
   if (((uintptr_t)src->k_pool | (uintptr_t)src->v_pool) & 15) return CATEKV_ERR_INVALID_ARG;
   if (src->B != dst->B || src->Hkv != dst->Hkv) return CATEKV_ERR_INVALID_ARG;
   const int n = src->B * src->Hkv;
@@ -247,7 +249,6 @@ extern "C" int catekv_q8_quantize(const catekv_cache* src, catekv_q8_cache* dst,
     q8_quantize_kernel<CATEKV_Q8_INT8><<<grid, kQ8Threads, 0, (cudaStream_t)stream>>>(a);
   CATEKV_CUDA_TRY(cudaGetLastError());
   for (int s = 0; s < n; ++s) dst->seg_len[s] = src->seg_len[s];
-  dst->reserved = src->reserved;
   return CATEKV_OK;
 }
 

@@ -46,11 +46,13 @@ constexpr int q8_decode_smem(int stages) { return kQ8Warps * stages * kQ8UnitByt
 // than four heads are converted and multiplied slowly enough for three at any length (14 K rows, G = 7: 158 us against
 // 161; e4m3 there 171 against 158).
 constexpr int kQ8LongShare = 4096;
-// Segments of up to this many pieces are merged by the CTA that delivers the last one (16 x 1K step: 15.0 us on the device
-// against 16.3, and one launch less for the host, 2.4 us; 4K lists in 32 pieces: 7.9 us on the device against 6.4, the call
-// 8 us against 10), longer ones by a combine pass (98 pieces would be 200 KB through one CTA).
-constexpr int kQ8MergePieces = 32;
-static_assert(kQ8MergePieces <= 32, "a lane per piece");
+// Segments of up to kQ8MergePieces pieces are merged by the CTA that delivers the last one (16 x 1K step: 14.3 us on the
+// device against 15.3, 16 x 64K 157.6 against 159.0, and one launch less for the host, 2.4 us); longer ones by a combine pass
+// (18 pieces, 4 x 32K: 25.9 us against 27.0 merged in the kernel; 98 would be 200 KB through one CTA).  Where a CTA's share is
+// at most kQ8MergeShare rows the call takes the host longer than the device, and the launch counts for more: up to
+// kQ8MergeMost pieces then (4K lists in 32: 7.7 us on the device against 6.2, the call 7.8 against 10).
+constexpr int kQ8MergePieces = 16, kQ8MergeMost = 32, kQ8MergeShare = 128;
+static_assert(kQ8MergeMost <= 32, "a lane per piece");
 constexpr int32_t kQ8PlanTile = kQ8Unit;   // marks a plan of this kind (decode.cu's have kTile)
 constexpr int kQ8SegEndCharge = 512;       // rows (128K: 23.4 us with 0, 22.5 with 128, 21.8 with 256, 21.1 with 512)
 constexpr float kQ8PBits = 12.f;           // probabilities are at most 2^12 ...
@@ -623,8 +625,8 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
   cp_async_wait<0>();
 }
 
-// Combine for few (segment, head) pairs: a CTA per pair and 32 of the 128 dimensions, a warp per 32 pieces, a lane per
-// dimension.  Small enough (128 threads, at most 72 registers) to be resident beside two CTAs of the attention kernel:
+// Combine: a CTA per (segment, head) pair and 32 of the 128 dimensions, a warp per 32 pieces, a lane per dimension.  Small
+// enough (128 threads, at most 72 registers) to be resident beside two CTAs of the attention kernel:
 // launched programmatically it has its plan entry and waits at the dependency when the last partial is written, and the
 // next attention kernel's CTAs find room beside it (128K: 21.1 -> 20.5 us, 256K G = 7: 28.2 -> 26.7 us).
 constexpr int kQ8CombineThreads = 128;
@@ -785,7 +787,8 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
   a.out = out;
   a.out_fp32 = out_dtype == CATEKV_OUT_FP32;
   a.lse_out = lse_out;
-  a.merge = hdr->max_pieces <= kQ8MergePieces ? (SegInfo*)((uint8_t*)plan_dev + L.off_seg) : nullptr;
+  const int most = hdr->total_rows <= (int64_t)kQ8MergeShare * hdr->num_ctas ? kQ8MergeMost : kQ8MergePieces;
+  a.merge = hdr->max_pieces <= most ? (SegInfo*)((uint8_t*)plan_dev + L.off_seg) : nullptr;
   const bool longs = hdr->total_rows >= (int64_t)kQ8LongShare * hdr->num_ctas, pack = G <= 4;
   const int n = hdr->num_ctas;
   if (cache->dtype == CATEKV_Q8_INT8) {
@@ -810,11 +813,7 @@ extern "C" int catekv_q8_decode_attn(const catekv_q8_cache* cache, const void* q
     ca.Hkv = cache->Hkv;
     ca.G = G;
     ca.out_fp32 = a.out_fp32;
-    // few pairs: the kernel that is resident early (one CTA per SM at most); many: decode.cu's, with a quarter of the CTAs
-    if ((int64_t)n_segs * G * kQ8CombineSplit <= sm_count())
-      CATEKV_CUDA_TRY(launch_pdl(q8_combine_kernel, dim3(n_segs, G, kQ8CombineSplit), dim3(kQ8CombineThreads), 0, st, ca));
-    else
-      return launch_combine(ca, n_segs, st);
+    CATEKV_CUDA_TRY(launch_pdl(q8_combine_kernel, dim3(n_segs, G, kQ8CombineSplit), dim3(kQ8CombineThreads), 0, st, ca));
   }
   return CATEKV_OK;
 }

@@ -127,6 +127,9 @@ def test_refusals_of_weighted_attention(ck):
     keep[2][1] = 199  # shorter than the plan knows it
     assert call() == ck.ERR_INVALID_ARG
     keep[2][1] = 200
+    st.reserved = 1  # lengths that are upper bounds
+    assert call() == ck.ERR_INVALID_ARG
+    st.reserved = 0
     assert call(Hq=18, wb=1 << 40) == ck.ERR_UNSUPPORTED and call(od=7) == ck.ERR_UNSUPPORTED
     pg = ck.PagesStruct(1, 1, 0, 0, F, F, F, F, F, F)
     st.pages = C.pointer(pg)

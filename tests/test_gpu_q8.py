@@ -319,7 +319,7 @@ def test_a_plan_for_longer_lists_is_refused(ck, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n,ctas", [(64 * 31, 31), (64 * 32, 32), (64 * 33, 33), (64 * 80, 80), (5000, 296), (64 * 32 - 1, 200)])
+@pytest.mark.parametrize("n,ctas", [(64 * 60, 15), (64 * 64, 16), (64 * 68, 17), (64 * 31, 31), (64 * 32, 32), (64 * 33, 33), (64 * 80, 80), (5000, 296), (64 * 32 - 1, 200)])
 def test_pieces_merged_in_the_kernel_and_by_the_combine_pass(ck, dtype, n, ctas):
     # around the number of pieces up to which the CTA that delivers the last one merges; several calls under one plan
     lens = [n, 100, n // 2, 0]

@@ -184,6 +184,9 @@ def test_refusals_of_quantize(ck):
     assert q(C.byref(big)) == ck.ERR_CAPACITY
     other, keep4 = _bf16(ck, [1, 2, 3], Hkv=3)
     assert q(C.byref(other)) == ck.ERR_INVALID_ARG
+    src.reserved = 1  # lengths that are upper bounds
+    assert q(C.byref(src)) == ck.ERR_INVALID_ARG
+    src.reserved = 0
     keep2[2][0] = 300  # longer than its own capacity
     assert q(C.byref(src)) == ck.ERR_INVALID_ARG
     pg = ck.PagesStruct(1, 1, 0, 0, 0x10000, 0x10000, 0x10000, 0x10000, 0x10000, 0x10000)
