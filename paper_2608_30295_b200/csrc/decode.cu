@@ -395,13 +395,14 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
       const float p2 = fast_exp2(x2 - mn0), p3 = fast_exp2(x3 - mn1);
       l0 = l0 * al0 + p0 + p2;
       l1 = l1 * al1 + p1 + p3;
-      if (!kLogits)
+      if (!kLogits) {  // (there the sums are scaled where the tile's product is added)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        o[i][0] *= al0;
-        o[i][1] *= al1;
-        o[i][2] *= al0;
-        o[i][3] *= al1;
+        for (int i = 0; i < 8; ++i) {
+          o[i][0] *= al0;
+          o[i][1] *= al1;
+          o[i][2] *= al0;
+          o[i][3] *= al1;
+        }
       }
       // P as bf16 hi + lo, transposed into the B-operand layout (k = token, n = head)
       const float h0 = bf16_round(p0), h1 = bf16_round(p1), h2 = bf16_round(p2), h3 = bf16_round(p3);

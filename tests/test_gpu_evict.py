@@ -350,3 +350,28 @@ def test_decode_with_weights_then_evict_then_eight_bits(ck, dtype):
                 for g in range(G):
                     o, l = orc.attention(qf[b, h * G + g], K, V, 128 ** -0.5)
                     assert H.rel_l2(out[b, h * G + g].cpu().double().numpy(), o) <= 1e-4 and abs(float(lse[b, h * G + g]) - l) <= 1e-4
+
+
+def test_two_evictions_on_two_streams(ck):
+    """Separate caches and workspaces, lists long enough for clusters of CTAs; in place and into another cache."""
+    lens = [30000, 9000, 400]
+    mask = np.ones(3, dtype=np.uint8)
+    ocs = [H.random_cache(1, 3, lens, seed=500 + i) for i in range(2)]
+    caches = [H.device_cache_from_oracle(ck, oc, 5) for oc in ocs]
+    ws = [_weights(ck, c, 510 + i) for i, c in enumerate(caches)]
+    w0 = [w.clone() for w in ws]
+    k0 = [synth.bits(c.k_pool).copy() for c in caches]
+    kept = ck.catekv_evict_lengths(caches[1], mask, 3000, 4, 64)
+    dst = ck.Cache(1, 3, kept, 0, "cuda")
+    dst.k_pool.fill_(3.0)
+    dst.v_pool.fill_(3.0)
+    dw = torch.full((dst.total_rows,), 9.0, device="cuda")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[0]):
+        ck.catekv_evict(caches[0], ws[0], mask, 3000, 4, 64)
+    with torch.cuda.stream(streams[1]):
+        ck.catekv_evict(caches[1], ws[1], mask, 3000, 4, 64, dst, dw)
+    torch.cuda.synchronize()
+    _check_evicted(ocs[0], w0[0], caches[0].seg_off, caches[0].seg_cap, mask, 3000, 4, 64, caches[0], ws[0], None, kept, True, k0[0])
+    _check_evicted(ocs[1], w0[1], caches[1].seg_off, caches[1].seg_cap, mask, 3000, 4, 64, dst, dw, None, kept, False)

@@ -449,3 +449,25 @@ def test_infinite_keys_in_a_tail(ck, dtype, G):
         g = out[0].double().cpu().numpy()
         assert np.isnan(g[~gone]).any(axis=1).all()
         assert H.rel_l2(g[gone], r[0][gone]) <= 1e-4 and np.abs(lse[0].cpu().numpy()[gone] - rl[0][gone]).max() <= 1e-4
+
+
+@pytest.mark.parametrize("ctas", [40, 296])
+def test_two_streams_with_a_plan_and_a_workspace_each(ck, ctas):
+    lens = [2000, 700, 64, 1500]
+    k, v = _rows(lens, 170)
+    c = _quantized(ck, k, v, 1, 4, orc.Q8_E4M3)
+    plans = [ck.DecodePlan(c, ctas) for _ in range(2)]
+    for p in plans:
+        ck.catekv_q8_decode_plan(c, p)
+    qs = [synth.randn_bf16((1, 16, 128), "cuda", 171, "q", i) for i in range(2)]
+    want = [_attend(ck, c, q, ctas)[0] for q in qs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty(50, 1, 16, 128, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(50):
+        for s in range(2):
+            with torch.cuda.stream(streams[s]):
+                ck.catekv_q8_decode_attn(c, qs[s], plans[s], outs[s][i])
+    torch.cuda.synchronize()
+    for s in range(2):
+        assert all(torch.equal(outs[s][i], want[s]) for i in range(50))
