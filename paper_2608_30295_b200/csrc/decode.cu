@@ -643,11 +643,6 @@ __global__ void __launch_bounds__(kCombineWarps * 32) decode_combine_kernel(cons
   combine_segment<kCombineUnroll>(a, blockIdx.x, blockIdx.y);
 }
 
-int launch_combine(const CombineArgs& a, int n_segs, cudaStream_t stream) {
-  CATEKV_CUDA_TRY(launch_pdl(decode_combine_kernel, dim3(n_segs, a.G), dim3(kCombineWarps * 32), 0, stream, a));
-  return CATEKV_OK;
-}
-
 }  // namespace catekv
 
 using namespace catekv;
@@ -762,8 +757,7 @@ static int decode_launch(int phases, const catekv_cache* cache, const void* k_ne
     ca.Hkv = cache->Hkv;
     ca.G = G;
     ca.out_fp32 = out_fp32;
-    rc = launch_combine(ca, n_segs, st);
-    if (rc) return rc;
+    CATEKV_CUDA_TRY(launch_pdl(decode_combine_kernel, dim3(n_segs, G), dim3(kCombineWarps * 32), 0, st, ca));
   }
   return CATEKV_OK;
 }

@@ -84,7 +84,7 @@ struct PlanSource {  // what a schedule is made from (host arrays)
 int build_plan(const PlanSource& p, int32_t num_ctas, int32_t tile, int cut_align, int end_charge, void* plan_host,
                void* plan_dev, size_t plan_bytes, cudaStream_t stream);
 
-struct CombineArgs {
+struct CombineArgs {  // of the passes that merge the partials of every segment that was cut into several pieces
   const SegInfo* seg_info;
   const float* part_o;
   const float* part_lse;
@@ -92,9 +92,6 @@ struct CombineArgs {
   float* lse_out;
   int32_t Hq, Hkv, G, out_fp32;
 };
-// merge the partials of every segment that was cut into several pieces
-int launch_combine(const CombineArgs& a, int n_segs, cudaStream_t stream);
-
 struct PageArgs {  // overflow pages of a cache (all null / 0 without pages)
   uint8_t* k_ovf;
   uint8_t* v_ovf;
