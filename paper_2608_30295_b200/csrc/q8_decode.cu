@@ -206,7 +206,9 @@ template <int kType, int kQ8Stages, bool kPack>
 __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_scale[kQ8Warps][kQ8Stages][2];
-  __shared__ float s_m[kQ8Warps][kMaxG], s_l[kQ8Warps][kMaxG];
+  // The warps' maxima and sums of a piece.  Two copies, taken in turn: a warp without a unit in the next piece writes that piece's
+  // while another may still be reading this one's for its last head; the barriers of the piece between order a copy's reuse.
+  __shared__ float s_ml[2][2][kQ8Warps][kMaxG];
   __shared__ int s_last;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, c = lane & 3;
@@ -533,6 +535,7 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
 
     // ---- end of the piece: merge the four warps (warps 0 and 1 fill a slot each, 2 and 3 add to them, everybody writes
     // a part of the sum)
+    float (*s_m)[kMaxG] = s_ml[(item - item_begin) & 1][0], (*s_l)[kMaxG] = s_ml[(item - item_begin) & 1][1];
     if (item + 1 < item_end) q8_load_q(a, cc.seg + 1, gq, c, q4);  // on their way during the merge
     int si_slot = 0, si_pieces = 0;
     if (a.merge && cc.slot >= 0) {
