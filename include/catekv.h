@@ -570,10 +570,12 @@ int catekv_decode_attn_weighted(const catekv_cache* cache, const void* q, int32_
  *   captured call's: catekv_cache_sync_lengths).
  *   What was built for dst before has to be built anew: its decode plans (before the next append: see the ordering note
  *   of catekv_decode_attn; catekv_decode_attn_weighted refuses a plan made for longer lists) and its retrieval metadata.
- *   idx_out  device int32 [B*Hkv, idx_stride] or NULL: the rows kept of each segment
+ *   idx_out  device int32 [B*Hkv, idx_stride] or NULL: the rows kept of each segment.  A replayed call whose list is longer
+ *            than idx_stride writes the first idx_stride of them (and evicts as it should)
  *   ws       device scratch of at least catekv_evict_workspace_bytes(B, Hkv, largest seg_cap of src); its first
  *            CATEKV_STATUS_BYTES are the status block, which this call does not clear (as the retrieval calls):
- *            CATEKV_STATUS_CAPACITY when a replayed call's list was cut at the capacity of dst.
+ *            CATEKV_STATUS_CAPACITY when a replayed call's list was cut at the capacity of dst, or what idx_out
+ *            tells of it at idx_stride.
  * Errors: CATEKV_ERR_CAPACITY if a kept list does not fit its segment of dst (nothing launched), CATEKV_ERR_UNSUPPORTED
  * for overflow pages or more than 2048 segments, CATEKV_ERR_INVALID_ARG if src or dst has no seg_cap_dev, if only one
  * of cache and weights is in place, or if idx_stride is shorter than the longest kept list.

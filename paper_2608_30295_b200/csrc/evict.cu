@@ -342,7 +342,7 @@ struct EvMoveArgs {
   int32_t* dst_len;
   float* w_dst;
   int32_t* idx_out;
-  int64_t idx_out_stride;
+  int64_t idx_out_stride;  // also the most entries of a segment: a replayed call's list may be longer than the host saw it
   int32_t rows_per_cta;
   int32_t* status;
   int32_t* chk;
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const __gr
   const int len = min(s.kept, cap);
   if (r0 == 0 && tid == 0) {
     a.dst_len[seg] = len;
-    if (s.kept > cap) raise_status(a.status, CATEKV_STATUS_CAPACITY, kKidEvict, seg, s.kept);
+    if (s.kept > cap || (a.idx_out && len > a.idx_out_stride)) raise_status(a.status, CATEKV_STATUS_CAPACITY, kKidEvict, seg, s.kept);
   }
   const int64_t so = a.src_off[seg], to = a.dst_off[seg];
   const int r1 = min(r0 + a.rows_per_cta, len);
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const __gr
     if (r < len) {
       const int from = kept_row(a, s, seg, r);
       w = a.w_src[so + from];
-      if (a.idx_out) a.idx_out[(int64_t)seg * a.idx_out_stride + r] = from;
+      if (a.idx_out && r < a.idx_out_stride) a.idx_out[(int64_t)seg * a.idx_out_stride + r] = from;
     }
     a.w_dst[to + r] = w;
   }
@@ -470,8 +470,11 @@ __global__ void __launch_bounds__(kEvInThreads) evict_inplace_kernel(const __gri
     const int seg = blockIdx.x - g.n_masked * kSlices;
     const EvSeg s = move_seg(a, seg);
     const int len = s.kept;
-    if (a.idx_out)
-      for (int r = tid; r < len; r += kEvInThreads) a.idx_out[(int64_t)seg * a.idx_out_stride + r] = kept_row(a, s, seg, r);
+    if (a.idx_out) {
+      if (tid == 0 && len > a.idx_out_stride) raise_status(a.status, CATEKV_STATUS_CAPACITY, kKidEvict, seg, len);
+      const int n_out = (int)min((int64_t)len, a.idx_out_stride);
+      for (int r = tid; r < n_out; r += kEvInThreads) a.idx_out[(int64_t)seg * a.idx_out_stride + r] = kept_row(a, s, seg, r);
+    }
     if (s.keep_all) return;
     float* w = a.w_dst + a.dst_off[seg];
     if (tid == 0) a.dst_len[seg] = len;
