@@ -736,7 +736,8 @@ def catekv_evict_lengths(cache: Cache, evict_mask, budget: int, sink: int, local
 def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, sink: int, local: int,
                  dst: Optional[Cache] = None, dst_weights: Optional[torch.Tensor] = None,
                  idx_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
-    """Cut the masked segments to `budget` rows by weight, into `dst` and `dst_weights`, or in place without them."""
+    """Cut the masked segments to `budget` rows by weight, into `dst` and `dst_weights`, or in place without them.  idx_out: int32
+    [B*Hkv, at least the longest kept list], in a captured call without gaps between its rows."""
     if (dst is None) != (dst_weights is None):
         raise CatekvError(ERR_INVALID_ARG, "catekv_evict")
     if dst is None:
@@ -750,7 +751,12 @@ def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, s
     stride = 0
     if idx_out is not None:
         assert idx_out.dtype is torch.int32 and idx_out.shape[0] == n and idx_out.stride(1) == 1
-        stride = idx_out.stride(0) if n > 1 else idx_out.shape[1]
+        width = idx_out.shape[1]
+        stride = idx_out.stride(0) if n > 1 else width
+        # rows of a wider buffer: the library bounds what it writes by the stride alone.  A capture's replays may find longer lists.
+        if width < stride and (catekv_evict_lengths(cache, evict_mask, budget, sink, local).max() > width
+                               or torch.cuda.is_current_stream_capturing()):
+            raise CatekvError(ERR_INVALID_ARG, "catekv_evict")
     if ws is None:
         ws = evict_workspace(cache)
     st = _stream_here("catekv_evict", cache.k_pool, weights, dst_weights, dst.k_pool, idx_out, ws)
