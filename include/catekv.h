@@ -630,7 +630,9 @@ typedef struct catekv_q8_cache {
 /*
  * Every segment of `src` (no overflow pages) into the same segment of `dst`: complete blocks as codes and scales, the rows
  * behind them into the tail; dst's lengths are set (device and host).  Rows behind a segment's length are neither read
- * nor written.  CATEKV_ERR_CAPACITY (nothing launched) if a segment does not fit; CATEKV_ERR_INVALID_ARG if the caches
+ * nor written.  The device lengths decide, so the call may be captured and replayed on lists that have grown; a list that
+ * no longer fits its segment of dst is cut at the segment's capacity, and dst's device length says so.  The mirror dst->seg_len
+ * is then the captured call's: copy the device lengths into it before a plan is built or a row appended.  CATEKV_ERR_CAPACITY (nothing launched) if a segment does not fit; CATEKV_ERR_INVALID_ARG if the caches
  * differ in B or Hkv or src->reserved is set (catekv_cache_sync_lengths makes its lengths exact); CATEKV_ERR_UNSUPPORTED
  * for a source with overflow pages or more than 65535 segments.
  */

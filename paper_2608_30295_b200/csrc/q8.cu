@@ -106,20 +106,25 @@ struct QuantizeArgs {
   uint8_t* v_tail;
   const int32_t* seg_off;
   int32_t* seg_len;
+  int32_t seg0;  // the launch's first segment
+};
+// The capacities of a launch's segments travel in the kernel arguments (the 8-bit cache has none on the device): the device's lengths
+// decide, which in a replayed graph may be longer than the host saw them.  Two sizes, as the longer one is 8 KB of arguments.
+constexpr int kQ8FewSegs = 128, kQ8MostSegs = 2048;
+template <int kSegs>
+struct QuantizeCaps {
+  int32_t cap[kSegs];
 };
 
 // One CTA per block of a segment (the last one takes the tail's rows), the block in registers between the maximum and the
 // codes: one pass, bound by the copy's bytes (128K, 458 MB: 74 us in a replayed graph, 6.2 TB/s, 0.96 of the copy
-// bandwidth).  It rewrites blocks that a decode plan may cover: launched without the programmatic attribute, no early
+// bandwidth).  The grid is as long as the host's longest list; where the device's is longer its CTAs go round again.
+// It rewrites blocks that a decode plan may cover: launched without the programmatic attribute, no early
 // signal to dependents (see launch_pdl).
 template <int kType>
-__global__ void __launch_bounds__(kQ8Threads) q8_quantize_kernel(const QuantizeArgs a) {
-  __shared__ uint32_t s_max[kQ8Threads / 32][2];
-  const int seg = blockIdx.y, blk = blockIdx.x, tid = threadIdx.x;
-  const int len = a.src_len[seg];
+__device__ __forceinline__ void q8_quantize_block(const QuantizeArgs& a, int seg, int blk, int len, uint32_t (*s_max)[2]) {
+  const int tid = threadIdx.x;
   const int full = len / kQ8Block;
-  if (blk == 0 && tid == 0) a.seg_len[seg] = len;
-  if (blk > full || (blk == full && len % kQ8Block == 0)) return;
   const int64_t row0 = (int64_t)a.src_off[seg] + (int64_t)blk * kQ8Block;
   const uint8_t* ks = a.k_src + row0 * kRowBytes;
   const uint8_t* vs = a.v_src + row0 * kRowBytes;
@@ -152,6 +157,37 @@ __global__ void __launch_bounds__(kQ8Threads) q8_quantize_kernel(const QuantizeA
   const int64_t dblk = a.seg_off[seg] / kQ8Block + blk;
   q8_encode_block<kType>(k, v, a.k_pool + dblk * kQ8BlockBytes, a.v_pool + dblk * kQ8BlockBytes, a.k_scale + dblk,
                          a.v_scale + dblk, s_max);
+}
+
+template <int kType, int kSegs>
+__global__ void __launch_bounds__(kQ8Threads) q8_quantize_kernel(const QuantizeArgs a, const __grid_constant__ QuantizeCaps<kSegs> caps) {
+  __shared__ uint32_t s_max[kQ8Threads / 32][2];
+  const int seg = a.seg0 + blockIdx.y;
+  const int len = min(a.src_len[seg], caps.cap[blockIdx.y]);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.seg_len[seg] = len;
+  const int end = (len + kQ8Block - 1) / kQ8Block;
+  for (int blk = blockIdx.x; blk < end; blk += gridDim.x) {
+    if (blk != (int)blockIdx.x) __syncthreads();  // s_max has been read
+    q8_quantize_block<kType>(a, seg, blk, len, s_max);
+  }
+}
+
+template <int kType, int kSegs>
+static cudaError_t q8_launch_quantize(QuantizeArgs a, const int32_t* seg_cap, int n, int gx, cudaStream_t st) {
+  for (a.seg0 = 0; a.seg0 < n; a.seg0 += kSegs) {
+    QuantizeCaps<kSegs> caps;  // (entries behind the last segment are not looked at)
+    const int m = n - a.seg0 < kSegs ? n - a.seg0 : kSegs;
+    for (int s = 0; s < m; ++s) caps.cap[s] = seg_cap[a.seg0 + s];
+    q8_quantize_kernel<kType, kSegs><<<dim3(gx, m), kQ8Threads, 0, st>>>(a, caps);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+template <int kType>
+static cudaError_t q8_launch_quantize(const QuantizeArgs& a, const int32_t* seg_cap, int n, int gx, cudaStream_t st) {
+  return n <= kQ8FewSegs ? q8_launch_quantize<kType, kQ8FewSegs>(a, seg_cap, n, gx, st)
+                         : q8_launch_quantize<kType, kQ8MostSegs>(a, seg_cap, n, gx, st);
 }
 
 struct Q8AppendArgs {
@@ -242,12 +278,12 @@ extern "C" int catekv_q8_quantize(const catekv_cache* src, catekv_q8_cache* dst,
   a.v_tail = (uint8_t*)dst->v_tail;
   a.seg_off = dst->seg_off_dev;
   a.seg_len = dst->seg_len_dev;
-  const dim3 grid(max_len > 0 ? (max_len + kQ8Block - 1) / kQ8Block : 1, n);
+  a.seg0 = 0;
+  const int gx = max_len > 0 ? (max_len + kQ8Block - 1) / kQ8Block : 1;
   if (dst->dtype == CATEKV_Q8_E4M3)
-    q8_quantize_kernel<CATEKV_Q8_E4M3><<<grid, kQ8Threads, 0, (cudaStream_t)stream>>>(a);
+    CATEKV_CUDA_TRY(q8_launch_quantize<CATEKV_Q8_E4M3>(a, dst->seg_cap, n, gx, (cudaStream_t)stream));
   else
-    q8_quantize_kernel<CATEKV_Q8_INT8><<<grid, kQ8Threads, 0, (cudaStream_t)stream>>>(a);
-  CATEKV_CUDA_TRY(cudaGetLastError());
+    CATEKV_CUDA_TRY(q8_launch_quantize<CATEKV_Q8_INT8>(a, dst->seg_cap, n, gx, (cudaStream_t)stream));
   for (int s = 0; s < n; ++s) dst->seg_len[s] = src->seg_len[s];
   return CATEKV_OK;
 }
