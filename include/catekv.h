@@ -384,6 +384,10 @@ int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, void* plan_h
  * stream before they read lengths, queries or appended rows, but they may request cache rows that
  * were valid when the plan was built while the previous kernel is still finishing.  Such rows must
  * therefore not be rewritten (by catekv_select_compact, say) between catekv_decode_plan and this call.
+ * Appends to lists that are shorter than the plan knows them (they were cut by catekv_evict, or the plan was
+ * made from upper bounds) rewrite such rows: while cache->seg_len says so, and always under a plan made from upper bounds,
+ * the kernel is launched behind the previous one's end.  That is decided when the call is made (a captured call keeps
+ * it), and no longer once the lists have grown past the plan again: build plans anew where lists are cut.
  */
 int catekv_decode_attn(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
                        int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,

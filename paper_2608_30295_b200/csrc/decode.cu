@@ -737,14 +737,15 @@ static int decode_launch(int phases, const catekv_cache* cache, const void* k_ne
     a.chk = checked_status_ptr();
     a.logits = logits;
     a.logit_stride = cache->total_rows;
-    if (logits)
-      CATEKV_CUDA_TRY(launch_pdl(decode_partial_kernel<kModePlain, true>, dim3(hdr->num_ctas), dim3(kDecodeThreads), kDecodeSmem, st, a));
-    else if (il)
-      CATEKV_CUDA_TRY(launch_pdl(decode_partial_kernel<kModeIndexed>, dim3(hdr->num_ctas), dim3(kDecodeThreads), kDecodeSmem, st, a));
-    else if (cache->pages)
-      CATEKV_CUDA_TRY(launch_pdl(decode_partial_kernel<kModePaged>, dim3(hdr->num_ctas), dim3(kDecodeThreads), kDecodeSmem, st, a));
-    else
-      CATEKV_CUDA_TRY(launch_pdl(decode_partial_kernel<kModePlain>, dim3(hdr->num_ctas), dim3(kDecodeThreads), kDecodeSmem, st, a));
+    auto* kernel = logits ? decode_partial_kernel<kModePlain, true> : il ? decode_partial_kernel<kModeIndexed>
+                   : cache->pages ? decode_partial_kernel<kModePaged> : decode_partial_kernel<kModePlain>;
+    const dim3 grid(hdr->num_ctas), block(kDecodeThreads);
+    if (!il && plan_rows_may_be_new(hdr, L.off_seg, cache)) {  // (the indexed kernel requests nothing before its wait)
+      kernel<<<grid, block, kDecodeSmem, st>>>(a);
+      CATEKV_CUDA_TRY(cudaGetLastError());
+    } else {
+      CATEKV_CUDA_TRY(launch_pdl(kernel, grid, block, kDecodeSmem, st, a));
+    }
   }
   if ((phases & 2) && hdr->n_slots > 0) {
     CombineArgs ca;

@@ -28,8 +28,10 @@ struct PlanHeader {
   int64_t total_rows;
   int32_t off_cta, off_items, off_seg;  // byte offsets of the three tables
   int32_t max_pieces;                   // most pieces any segment was cut into
+  int32_t bounds;                       // made from lengths that were upper bounds (see plan_rows_may_be_new)
+  int32_t reserved[3];
 };
-static_assert(sizeof(PlanHeader) == 48, "plan header layout");
+static_assert(sizeof(PlanHeader) == 64, "plan header layout");
 
 struct WorkItem {  // 32 bytes
   int32_t seg;
@@ -80,6 +82,7 @@ struct PlanSource {  // what a schedule is made from (host arrays)
   const int32_t* seg_len;
   const int32_t* seg_off;
   const int32_t* seg_cap;
+  int32_t bounds;  // the lengths are upper bounds
 };
 int build_plan(const PlanSource& p, int32_t num_ctas, int32_t tile, int cut_align, int end_charge, void* plan_host,
                void* plan_dev, size_t plan_bytes, cudaStream_t stream);
@@ -131,6 +134,11 @@ static bool plan_outlived(const void* plan_host, size_t off_seg, const int32_t* 
   for (int s = 0; s < n_segs; ++s)
     if (seg_len[s] < si[s].plan_len) return true;
   return false;
+}
+// Whether a row that the plan knows may be one that the preceding kernel of the stream is appending: the lists have become shorter, or the plan
+// was made from lengths that were upper bounds.  The attention kernel is then launched behind the preceding kernel's end.
+static bool plan_rows_may_be_new(const PlanHeader* hdr, size_t off_seg, const catekv_cache* c) {
+  return hdr->bounds || c->reserved || plan_outlived(hdr, off_seg, c->seg_len, hdr->n_segs);
 }
 // rows segment s can hold: its own capacity plus the overflow pages it has been given
 static inline int64_t seg_capacity(const catekv_cache* c, int s) {

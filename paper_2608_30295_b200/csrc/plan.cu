@@ -100,6 +100,7 @@ int catekv::build_plan(const PlanSource& p, int32_t num_ctas, int32_t tile, int 
   hdr->off_items = (int32_t)L.off_items;
   hdr->off_seg = (int32_t)L.off_seg;
   hdr->max_pieces = max_pieces;
+  hdr->bounds = p.bounds;
   if (plan_dev)
     CATEKV_CUDA_TRY(cudaMemcpyAsync(plan_dev, plan_host, L.bytes, cudaMemcpyHostToDevice, stream));
   return CATEKV_OK;
@@ -115,6 +116,6 @@ extern "C" int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, v
   if (plan_bytes < plan_layout(n_segs, num_ctas).bytes) return CATEKV_ERR_WORKSPACE;
   for (int s = 0; s < n_segs; ++s)
     if (cache->seg_len[s] < 0 || cache->seg_len[s] > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;
-  const PlanSource src = {n_segs, cache->seg_len, cache->seg_off, cache->seg_cap};
+  const PlanSource src = {n_segs, cache->seg_len, cache->seg_off, cache->seg_cap, cache->reserved};
   return build_plan(src, num_ctas, kTile, 1, kSegEndCharge, plan_host, plan_dev, plan_bytes, (cudaStream_t)stream);
 }

@@ -739,7 +739,7 @@ extern "C" int catekv_q8_decode_plan(const catekv_q8_cache* cache, int32_t num_c
   const int n_segs = cache->B * cache->Hkv;
   for (int s = 0; s < n_segs; ++s)
     if (cache->seg_len[s] < 0 || cache->seg_len[s] > cache->seg_cap[s]) return CATEKV_ERR_INVALID_ARG;
-  const PlanSource src = {n_segs, cache->seg_len, cache->seg_off, cache->seg_cap};
+  const PlanSource src = {n_segs, cache->seg_len, cache->seg_off, cache->seg_cap, 0};
   return build_plan(src, num_ctas, kQ8PlanTile, kQ8Block, kQ8SegEndCharge, plan_host, plan_dev, plan_bytes, (cudaStream_t)stream);
 }
 
