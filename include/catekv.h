@@ -553,7 +553,8 @@ int catekv_decode_attn_noalloc(const catekv_cache* cache, const void* q, int32_t
  * at 0 when it is appended.
  *   ws  at least catekv_decode_weighted_workspace_bytes(...) with the cache's total_rows; q, out and ws 16-byte aligned
  * CATEKV_ERR_UNSUPPORTED for a cache with overflow pages; CATEKV_ERR_INVALID_ARG for a plan made for longer lists (the
- * cache has been cut since) and for a cache whose lengths are upper bounds (catekv_cache_sync_lengths makes them exact).
+ * cache has been cut since, or the plan was made from upper bounds) and for a cache whose lengths are upper bounds:
+ * catekv_cache_sync_lengths makes them exact, and the plan is made after it.
  */
 size_t catekv_decode_weighted_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_ctas, int64_t total_rows);
 int catekv_decode_attn_weighted(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
