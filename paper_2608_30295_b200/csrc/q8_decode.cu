@@ -629,12 +629,15 @@ __global__ void __maxnreg__(kQ8Regs) q8_decode_partial_kernel(const Q8DecodeArgs
 }
 
 // Combine: a CTA per (segment, head) pair and 32 of the 128 dimensions, a warp per 32 pieces, a lane per dimension.  Small
-// enough (128 threads, at most 72 registers) to be resident beside two CTAs of the attention kernel:
+// enough (128 threads, at most 64 registers: all that two attention CTAs leave) to be resident beside two CTAs of the attention kernel:
 // launched programmatically it has its plan entry and waits at the dependency when the last partial is written, and the
 // next attention kernel's CTAs find room beside it (128K: 21.1 -> 20.5 us, 256K G = 7: 28.2 -> 26.7 us).
 constexpr int kQ8CombineThreads = 128;
 constexpr int kQ8CombineSplit = 4;
-__global__ void __launch_bounds__(kQ8CombineThreads, 7) q8_combine_kernel(const CombineArgs a) {
+constexpr int kQ8CombinePerSm = 8;  // caps its registers
+static_assert(2 * kQ8DecodeThreads * kQ8Regs + 65536 / kQ8CombinePerSm <= 65536 && kQ8CombineThreads * kQ8CombinePerSm <= 2048,
+              "a combine CTA fits beside two attention CTAs");
+__global__ void __launch_bounds__(kQ8CombineThreads, kQ8CombinePerSm) q8_combine_kernel(const CombineArgs a) {
   __shared__ float s_acc[kQ8CombineThreads / 32][32], s_w[kQ8CombineThreads / 32], s_m[kQ8CombineThreads / 32];
   const int seg = blockIdx.x, hd = blockIdx.y, part = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
