@@ -29,6 +29,8 @@
  *     caches are atomics and safe to fill from several host threads.
  *   - Kernels are enqueued on the caller's stream (a cudaStream_t passed as
  *     void*); calls do not synchronise unless stated.
+ *   - A workspace belongs to one call at a time: calls that can overlap (on two
+ *     streams, in two graphs) need one each.
  *   - bf16 values are raw 16-bit patterns.  The head dimension d is the
  *     contiguous inner dimension and must be 128.  Hq / Hkv = G <= 8; where an
  *     observation window is involved, G * L_obs <= 512.
@@ -606,6 +608,7 @@ int catekv_evict(const catekv_cache* src, const float* weights, const uint8_t* e
  * their own until the block is complete.  A row is thus rounded once, and the most recent rows are not rounded at all.
  * (A list can therefore be taken back, by writing its lengths, only as far as its unfinished block reaches: the rows of a
  * completed block are no longer in the tail.)
+ * A list in 8 bits grows up to the capacity it was laid out with and cannot be cut: catekv_evict takes the bf16 cache.
  * Segments are laid out as in catekv_cache (catekv_cache_layout); an offset is a multiple of 64.
  */
 #define CATEKV_Q8_E4M3 0
@@ -655,7 +658,7 @@ int catekv_q8_cache_advance(catekv_q8_cache* cache, int32_t n_tokens);
 /*
  * Split-KV decode attention over the 8-bit cache: catekv_decode_attn's arguments and results (softmax(sm_scale q K^T) V
  * with the keys and values that the codes stand for and the bf16 tails; fp32 accumulation, probabilities carried as
- * fp16 or bf16 pairs of 16 and more bits), with a plan of its own: catekv_q8_decode_plan cuts at block borders.  Buffer
+ * f16 pairs of 22 bits over the codes and as three bf16 parts, 24 bits, over the tails), with a plan of its own: catekv_q8_decode_plan cuts at block borders.  Buffer
  * sizes are those of catekv_decode_plan_bytes and catekv_decode_workspace_bytes; num_ctas comes from
  * catekv_q8_decode_num_ctas.  A plan stays valid while the segments grow; a plan made for longer lists (the cache has been
  * quantised anew since) and one of the other kind are refused (CATEKV_ERR_INVALID_ARG).  The ordering note of

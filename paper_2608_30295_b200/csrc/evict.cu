@@ -1,7 +1,7 @@
 // Eviction by accumulated attention weight: the selection of what a list keeps, and the move of it, into another cache or
 // in place.  Measured in a replayed graph: 64 lists of a batch (24 of 49 K cut to half, the others copied, 902 MB) 161 us,
 // 0.87 of the copy bandwidth, of which 137 are the move and 20 the selection; four lists of 1280 cut to 1024: 8.3 us (two
-// launches); the first in place 130 us (604 MB moved).
+// launches); the first in place 130 us (604 MB moved), three lists of 118 K of one sequence 122 us (75 into another cache).
 #include <math.h>
 
 #include <atomic>
@@ -443,7 +443,8 @@ __global__ void __launch_bounds__(kEvMoveThreads) evict_gather_kernel(const __gr
 // itself: nothing behind it reads there, and what is requested ahead lies behind it.  That makes a segment sequential in
 // its rows, so the work is split over the columns instead: a CTA moves kSlice bytes of every row of K or V, two tiles
 // ahead with cp.async and one barrier per tile (the tile has been read by everybody; the writes are a thread's own).
-// 64 bytes are two DRAM sectors; 32, where the segments are few, make twice the CTAs.  Large tiles pay: 24 lists of 49 K,
+// 64 bytes are two DRAM sectors; 32, where the segments are few, make twice the CTAs, 16 per list however long it is (the bound for one
+// sequence: three lists of 118 K cut to half 122 us, their floor 28).  Large tiles pay: 24 lists of 49 K,
 // selection included, take 130 us with tiles of 32 KB and three stages, 167 with 16 KB and four, 206 with 8 KB and eight
 // (303 with a tile at a time through registers).
 constexpr int kEvInThreads = 512;
@@ -594,7 +595,9 @@ static int evict_attributes() {
 }
 
 // max_pool: bound of a masked segment's candidates.  The smallest cluster whose CTAs hold their shares in registers, as
-// long as all clusters are resident at once; else fewer CTAs with longer shares in shared memory.
+// long as all clusters are resident at once with two CTAs per SM; else fewer CTAs with longer shares in shared memory.  (Above
+// about 22 K staged candidates an SM holds one such CTA: 19 to 37 lists of more than 178 K rows take two waves of clusters, which
+// wait for nothing outside their own.)
 static int launch_evict_select(EvSelectArgs& a, int n_masked, int max_pool, cudaStream_t stream) {
   auto share = [&](int CL) { return ((max_pool + CL - 1) / CL + 31) / 32 * 32; };
   int CL = 1;

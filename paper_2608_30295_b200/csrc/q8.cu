@@ -117,7 +117,7 @@ struct QuantizeCaps {
 };
 
 // One CTA per block of a segment (the last one takes the tail's rows), the block in registers between the maximum and the
-// codes: one pass, bound by the copy's bytes (128K, 458 MB: 74 us in a replayed graph, 6.2 TB/s, 0.96 of the copy
+// codes: one pass, bound by the copy's bytes (128K, 458 MB: 74 us in a replayed graph, 6.1 TB/s, 0.95 of the copy
 // bandwidth).  The grid is as long as the host's longest list; where the device's is longer its CTAs go round again.
 // It rewrites blocks that a decode plan may cover: launched without the programmatic attribute, no early
 // signal to dependents (see launch_pdl).

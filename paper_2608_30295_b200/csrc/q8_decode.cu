@@ -1,8 +1,8 @@
 // Decode attention over the 8-bit cache: split-KV partials on the tensor cores, and their merge.
 //
 // Bound by the stream of codes (256 bytes a row) where a CTA's share is long, by latency and MMA issue where it is short.  Measured, whole call in
-// a replayed graph: 16 x 64K (1.09 GB) 158 us, 6.9 TB/s or 1.07 of the copy bandwidth; 128K x 3 heads int8 (93 MB) 19.4 us, 4.8 TB/s, of which 18.2
-// remain when nothing is computed; 256K x 2 heads, G = 7 (136 MB) 27.2 us; 4K (4.5 MB) 7.8 us.
+// a replayed graph: 16 x 64K (1.09 GB) 158 us, 6.9 TB/s or 1.07 of the copy bandwidth; 128K x 3 heads int8 (93 MB) 18.9 us, 4.9 TB/s, of which 18.2
+// remain when nothing is computed; 256K x 2 heads, G = 7 (136 MB) 27.0 us; 4K (4.5 MB) 7.5 us.
 //
 // The stream is a warp's own.  A CTA owns a contiguous range of the rows of all segments laid end to end (cut at block
 // borders); its four warps take the range's units in turn, a unit being half a block (32 rows of codes, 8 KB of K and V)
