@@ -83,8 +83,8 @@ typedef void* catekv_stream; /* cudaStream_t */
 typedef struct catekv_pages {
   int32_t max_pages;   /* table entries per segment */
   int32_t n_pages;     /* pages of the overflow pools */
-  int32_t next_free;   /* host: pages handed out so far (start at 0) */
-  int32_t reserved;
+  int32_t next_free;   /* host: every page in use lies below (start at 0) */
+  int32_t released;    /* host: pages below next_free that no list holds (start at 0) */
   void* k_ovf;         /* device, bf16 [n_pages * 64, d] */
   void* v_ovf;         /* device, bf16 [n_pages * 64, d] */
   int32_t* table_dev;  /* device [B*Hkv, max_pages] */
@@ -540,6 +540,54 @@ int catekv_append_decode_attn(catekv_cache* cache, const void* k_new, const void
 int catekv_decode_attn_noalloc(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
                                int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,
                                size_t plan_bytes, catekv_stream stream);
+
+/* ---------------------------------------------------------------- chunks of new tokens */
+
+/*
+ * A chunk: n_new[b] new tokens of every sequence b (a further prompt, drafted tokens, a piece of a prompt beside sequences
+ * that decode; 0 for sequences that have none), on one token axis of n_tokens that its arrays share.  Sequence b owns the tokens
+ * [start[b], start[b] + n_new[b]); with start NULL they are packed one sequence behind the other.  No token belongs to two
+ * sequences; tokens that belong to none (a padded batch) are neither read nor written.  At most 512 sequences
+ * (CATEKV_ERR_UNSUPPORTED): the counts travel in the kernels' arguments, and a captured call keeps them.
+ */
+typedef struct catekv_chunk {
+  int32_t B;             /* sequences, the cache's */
+  int32_t n_tokens;      /* extent of the token axis */
+  const int32_t* n_new;  /* host [B] */
+  const int32_t* start;  /* host [B] or NULL */
+} catekv_chunk;
+
+/*
+ * Append a chunk's keys and values to every list: row seg_len + i of list (b, h) is written from token start[b] + i, in the
+ * segment's own rows or its overflow pages, and seg_len grows by n_new[b] on the device and in the host mirror.
+ *   k_new, v_new  device bf16 [n_tokens, Hkv, d] with element strides stride_t, stride_h (multiples of 8; d contiguous), 16-byte aligned
+ * CATEKV_ERR_CAPACITY (nothing launched) if a list cannot take its rows: catekv_pages_reserve gives it pages.
+ * CATEKV_ERR_INVALID_ARG for a cache without seg_cap_dev.  A replayed call goes by the device's lengths; rows for which a list
+ * has no room are dropped and not counted.
+ */
+int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const void* k_new, const void* v_new, int64_t stride_t,
+                        int64_t stride_h, catekv_stream stream);
+
+/*
+ * Attention of a chunk whose rows have been appended (they are the last n_new[b] rows of every list of sequence b): query i of
+ * sequence b sees the rows j < seg_len - n_new[b] + i + 1 of its lists,
+ *   out = softmax(sm_scale q K^T) V,   lse = natural-log sum of exp(logits).
+ * One token per sequence is a decode step over the same lists, without a plan.
+ *   q        device bf16 [n_tokens, Hq, d] with element strides (multiples of 8; d contiguous), 16-byte aligned
+ *   sm_scale >= 0; 0 means 1/sqrt(d)
+ *   out      device [n_tokens, Hq, d] contiguous, bf16 or float per out_dtype, 16-byte aligned; a query that sees nothing gets 0
+ *   lse_out  device float [n_tokens, Hq] or NULL; -inf where nothing is seen
+ *   ws       device scratch of at least catekv_chunk_attn_workspace_bytes(Hq, Hkv, the largest n_new[b]), 16-byte aligned; its first
+ *            CATEKV_STATUS_BYTES are the status block, which this call does not clear: zero them once
+ * fp32 accumulation; the probabilities enter the product with V as a pair of bf16 numbers, 17 significant bits.  An
+ * infinity or a NaN in a row reaches the queries that see the row and no other.
+ * The device's lengths decide, so a captured call follows lists that grow; the lengths on the host (upper bounds will do)
+ * only choose the number of CTAs.  Follows overflow pages.  Segment capacities are multiples of CATEKV_SEG_ALIGN, and the cache
+ * has seg_cap_dev (CATEKV_ERR_INVALID_ARG).
+ */
+size_t catekv_chunk_attn_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t max_new);
+int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* chunk, const void* q, int64_t q_stride_t, int64_t q_stride_h, int32_t Hq,
+                      float sm_scale, void* out, int32_t out_dtype, float* lse_out, void* ws, size_t ws_bytes, catekv_stream stream);
 
 /* ---------------------------------------------------------------- eviction by accumulated attention weight */
 

@@ -38,7 +38,7 @@ class CatekvError(RuntimeError):
 
 
 class PagesStruct(C.Structure):
-    _fields_ = [("max_pages", C.c_int32), ("n_pages", C.c_int32), ("next_free", C.c_int32), ("reserved", C.c_int32),
+    _fields_ = [("max_pages", C.c_int32), ("n_pages", C.c_int32), ("next_free", C.c_int32), ("released", C.c_int32),
                 ("k_ovf", C.c_void_p), ("v_ovf", C.c_void_p), ("table_dev", C.c_void_p), ("table", C.c_void_p),
                 ("seg_pages", C.c_void_p), ("seg_cap_dev", C.c_void_p)]
 
@@ -64,6 +64,10 @@ class StatusStruct(C.Structure):
 
 
 PAGE_ROWS = 64
+
+
+class ChunkStruct(C.Structure):
+    _fields_ = [("B", C.c_int32), ("n_tokens", C.c_int32), ("n_new", C.c_void_p), ("start", C.c_void_p)]
 
 
 class SelectParams(C.Structure):
@@ -136,6 +140,10 @@ def _load():
         "catekv_decode_weighted_workspace_bytes": (sz, [i32, i32, i32, i32, i64]),
         "catekv_decode_attn_weighted": (C.c_int, [C.POINTER(CacheStruct), vp, i32, f32, vp, i32, vp, vp, f32, vp, vp, sz, vp, sz,
                                                   vp]),
+        "catekv_append_chunk": (C.c_int, [C.POINTER(CacheStruct), C.POINTER(ChunkStruct), vp, vp, i64, i64, vp]),
+        "catekv_chunk_attn_workspace_bytes": (sz, [i32, i32, i32]),
+        "catekv_chunk_attn": (C.c_int, [C.POINTER(CacheStruct), C.POINTER(ChunkStruct), vp, i64, i64, i32, f32, vp, i32, vp, vp, sz,
+                                        vp]),
         "catekv_evict_workspace_bytes": (sz, [i32, i32, i32]),
         "catekv_evict_lengths": (C.c_int, [C.POINTER(CacheStruct), vp, i32, i32, i32, vp]),
         "catekv_evict": (C.c_int, [C.POINTER(CacheStruct), vp, vp, i32, i32, i32, C.POINTER(CacheStruct), vp, vp, i64, vp, sz,
@@ -763,4 +771,71 @@ def catekv_evict(cache: Cache, weights: torch.Tensor, evict_mask, budget: int, s
     _check(_lib.catekv_evict(C.byref(cache.struct), weights.data_ptr(), evict_mask.tobytes(), budget, sink, local,
                              C.byref(dst.struct), dst_weights.data_ptr(), _dev_ptr(idx_out), stride, ws.data_ptr(), ws.numel(), st),
            "catekv_evict")
+    return ws
+
+
+# ---------------------------------------------------------------- chunks of new tokens
+
+
+class Chunk:
+    """The new tokens of every sequence, on a token axis that queries, keys and values share (host counts only).  n_new [B]; start [B]:
+    the first token of every sequence (None: packed one behind the other); n_tokens: extent of the axis (None: as far as it is used)."""
+
+    def __init__(self, n_new, start=None, n_tokens: Optional[int] = None):
+        n_new, start = np.asarray(n_new).reshape(-1), None if start is None else np.asarray(start).reshape(-1)
+        _int32("Chunk", *(int(x) for x in n_new), *(() if start is None else (int(x) for x in start)))
+        if start is not None and start.size != n_new.size:
+            raise CatekvError(ERR_INVALID_ARG, "Chunk")
+        self.n_new = np.ascontiguousarray(n_new, dtype=np.int32)
+        self.start = None if start is None else np.ascontiguousarray(start, dtype=np.int32)
+        if n_tokens is None:
+            n_tokens = int(n_new.sum()) if start is None else max((int(s) + int(n) for s, n in zip(start, n_new)), default=0)
+        _int32("Chunk", n_tokens)
+        self.n_tokens = n_tokens
+        self.struct = ChunkStruct(self.n_new.size, n_tokens, _np_ptr(self.n_new), None if start is None else _np_ptr(self.start))
+
+
+def _token_rows(where: str, t: torch.Tensor, n_tokens: int, heads: int, d: int):
+    """Element strides (token, head) of a bf16 [n_tokens, heads, d] tensor whose d is contiguous."""
+    assert t.dtype is torch.bfloat16 and t.shape == (n_tokens, heads, d) and t.stride(2) == 1, where
+    return t.stride(0), t.stride(1)
+
+
+def catekv_append_chunk(cache: Cache, chunk: Chunk, k_new: torch.Tensor, v_new: torch.Tensor):
+    """k_new, v_new bf16 [n_tokens, Hkv, d] of the same strides (views of a wider projection will do)."""
+    st_t, st_h = _token_rows("catekv_append_chunk", k_new, chunk.n_tokens, cache.Hkv, cache.d)
+    assert v_new.dtype is torch.bfloat16 and v_new.shape == k_new.shape and v_new.stride() == k_new.stride()
+    st = _stream_here("catekv_append_chunk", cache.k_pool, k_new, v_new)
+    _check(_lib.catekv_append_chunk(C.byref(cache.struct), C.byref(chunk.struct), k_new.data_ptr(), v_new.data_ptr(), st_t, st_h, st),
+           "catekv_append_chunk")
+
+
+def chunk_attn_workspace(cache: Cache, chunk: Chunk, Hq: int) -> torch.Tensor:
+    """A workspace for catekv_chunk_attn with this chunk, or one whose longest sequence is not longer; its status block zeroed (memory only)."""
+    n = _lib.catekv_chunk_attn_workspace_bytes(Hq, cache.Hkv, int(chunk.n_new.max(initial=0)))
+    if n == 0:
+        raise CatekvError(ERR_INVALID_ARG, "catekv_chunk_attn_workspace_bytes")
+    ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
+    ws[:STATUS_BYTES].zero_()
+    return ws
+
+
+def catekv_chunk_attn(cache: Cache, chunk: Chunk, q: torch.Tensor, out: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
+                      sm_scale: float = 0.0, ws: Optional[torch.Tensor] = None):
+    """q bf16 [n_tokens, Hq, d] (token and head strides as they are); out bf16 or float32 [n_tokens, Hq, d] contiguous; lse_out float32
+    [n_tokens, Hq].  -> the workspace."""
+    Hq = q.shape[1]
+    st_t, st_h = _token_rows("catekv_chunk_attn", q, chunk.n_tokens, Hq, cache.d)
+    assert out.shape == q.shape and out.is_contiguous()
+    assert lse_out is None or (lse_out.dtype is torch.float32 and lse_out.is_contiguous() and lse_out.shape == q.shape[:2])
+    od = _OUT_CODE.get(out.dtype)
+    if od is None:
+        raise TypeError("out must be bf16 or fp32")
+    if ws is None:
+        ws = chunk_attn_workspace(cache, chunk, Hq)
+    st = _stream_here("catekv_chunk_attn", cache.k_pool, q, out, lse_out, ws)
+    rc = _lib.catekv_chunk_attn(C.byref(cache.struct), C.byref(chunk.struct), q.data_ptr(), st_t, st_h, Hq, sm_scale, out.data_ptr(), od,
+                                _dev_ptr(lse_out), ws.data_ptr(), ws.numel(), st)
+    if rc != OK:
+        raise CatekvError(rc, "catekv_chunk_attn")
     return ws

@@ -1,0 +1,1019 @@
+// Attention of a chunk of new tokens over the hybrid cache: query i of the n tokens that sequence b has just had appended
+// sees the rows j < len - n + i + 1 of every list of the sequence (its own pools, then its overflow pages),
+//   out = softmax(sm_scale q K^T) V,   lse = log sum exp(sm_scale q K^T).
+//
+// One pass over K and V with a running reference and sum per query row.  The query rows of a (sequence, KV head) are its
+// tokens' heads, row r = token * G + head, so that a K tile is read once for the whole group; a block of them is 256 rows
+// (two M = 128 tiles, template kQ2) or, where no sequence has more than 128 rows, 128 rows.  chunk_attn_kernel is persistent,
+// one CTA per SM: the 128-key tiles of all blocks of all lists, laid end to end, are cut into equal shares, from the device's lengths
+// (a captured call follows lists that grow).  A block that several CTAs share leaves partial results, which
+// chunk_combine_kernel merges in the order of the keys.
+//
+// Two streams per CTA, each with its own four softmax warps (a thread owns a query row), its own S / P slot and its own accumulator in
+// tensor memory: with two M tiles a stream is an M tile and both read the same K and V tiles; with one, the streams take
+// alternate key tiles and their accumulators are merged at the end.  While one stream's warps turn S into P, the tensor
+// pipe works for the other.  Per tile: S = Q K^T (tcgen05.mma, both operands in shared memory), the thread reads its row of S
+// (tcgen05.ld), raises its reference when the tile's maximum exceeds it by more than 2^8 (the accumulator is then scaled in tensor
+// memory: rare after the first tiles), writes P = exp2(logit - reference) over S as a bf16 pair hi + lo (both rounded to
+// nearest: 17 significant bits), and O += P_hi V + P_lo V takes P from tensor memory and V as the MN-major operand as TMA left it.
+//
+// Rows of a V tile that no query of the block sees are zeroed in shared memory before the product reads them (what lies behind a list
+// may be NaN, and 0 * NaN is not 0); an infinity or a NaN in a new row, which later tokens see and earlier ones do not, is taken
+// out there too and added to the rows that see it at the end.
+//
+// Warps: 0-3 and 4-7 softmax of the two streams, 8 tensor-core issue, 9 K / V tiles by TMA into one ring in the order of use,
+// 10 the V tiles that need a look, 11 the query block.  Every wait is bounded; a CTA whose wait runs out frees its tensor memory, records
+// CATEKV_STATUS_WAIT_EXPIRED and returns.
+#include <math.h>
+
+#include <atomic>
+
+#include "decode.cuh"
+#include "score.cuh"
+#include "tc.cuh"
+
+namespace catekv {
+
+constexpr int kChMaxSeqs = 512;  // sequences of a call: their counts travel in the kernel's arguments
+constexpr int kChThreads = 12 * 32;
+constexpr int kChTileBytes = 128 * 256;  // a [128 x 128] bf16 tile
+constexpr int kChStages = 5;
+constexpr int kChTmemCols = 512;  // S / P slots at columns 0 and 128, O at 256 and 384
+constexpr float kChTau = 8.f;
+constexpr int kChBarriers = 3 * kChStages + 12;
+template <bool kQ2>
+constexpr size_t ch_smem_bytes() {
+  return 1024 + (size_t)(kQ2 ? 2 : 1) * kChTileBytes + (size_t)kChStages * kChTileBytes + kChBarriers * 8 + 256 + (kQ2 ? 0 : 2 * 128 * 8);
+}
+static_assert(ch_smem_bytes<true>() <= 227 * 1024, "chunk_attn_kernel: one CTA's shared memory");
+
+struct ChunkSeqs {  // host counts of every sequence
+  int32_t n_new[kChMaxSeqs];
+  int32_t start[kChMaxSeqs];
+};
+struct ChunkArgs {
+  const int32_t* seg_off;
+  const int32_t* seg_len;
+  const int32_t* seg_cap;
+  const uint16_t* v_pool;
+  const uint16_t* v_ovf;
+  const int32_t* table;  // null: no pages
+  int32_t max_pages, n_pages;
+  int32_t n_segs, Hkv, G, Hq;
+  int32_t TB;  // tokens of a query block
+  int32_t slot_rows;
+  float scale_log2;
+  void* out;
+  float* lse;
+  int32_t out_fp32;
+  float* part_o;   // [2 CTAs][slot_rows][128], relative to the row's reference
+  float2* part_ml; // [2 CTAs][slot_rows]: reference (log2 domain), sum
+  int32_t* desc;   // [CTAs][8]
+  int32_t* status;
+  int32_t* checked;
+  uint32_t spin_limit;
+  int32_t idle_producer;
+};
+
+struct ChunkSeg {  // one list as the schedule sees it
+  int32_t len, n_new, n_blk;
+};
+__device__ __forceinline__ ChunkSeg ch_seg(const ChunkArgs& a, const ChunkSeqs& sq, int s) {
+  ChunkSeg g;
+  g.n_new = sq.n_new[s / a.Hkv];
+  g.n_blk = (g.n_new + a.TB - 1) / a.TB;
+  g.len = g.n_blk ? max(a.seg_len[s], 0) : 0;
+  if (g.n_blk) g.len = min(g.len, a.seg_cap[s] + CATEKV_PAGE_ROWS * a.max_pages);
+  return g;
+}
+// key tiles of a block (at least one, so that rows that see nothing get their output)
+__device__ __forceinline__ int ch_tiles(const ChunkArgs& a, const ChunkSeg& g, int blk) {
+  const int seen = g.len - g.n_new + min(g.n_new, a.TB * (blk + 1));
+  return max(1, (seen + kKeyTile - 1) / kKeyTile);
+}
+
+struct ChunkItem {
+  int32_t seg, blk, t0, t1, nt;  // tiles [t0, t1) of the block's nt
+  ChunkSeg g;
+};
+// The items of a CTA, one after the other; every role walks them by itself.
+struct ChunkWalk {
+  int32_t left, seg, blk, t;
+  ChunkSeg g;
+  __device__ __forceinline__ bool next(const ChunkArgs& a, const ChunkSeqs& sq, ChunkItem& it) {
+    if (left <= 0) return false;
+    while (blk >= g.n_blk) {
+      if (++seg >= a.n_segs) return false;
+      g = ch_seg(a, sq, seg);
+      blk = 0;
+    }
+    it.seg = seg;
+    it.blk = blk;
+    it.nt = ch_tiles(a, g, blk);
+    it.t0 = t;
+    it.t1 = min(it.nt, t + left);
+    it.g = g;
+    left -= it.t1 - it.t0;
+    t = 0;
+    ++blk;
+    return true;
+  }
+};
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ float ch_max64(const float (&x)[64]) {
+  float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]), m3 = fmax3(x[9], x[10], x[11]);
+#pragma unroll
+  for (int c = 12; c < 60; c += 8) {
+    m0 = fmax3(m0, x[c], x[c + 1]);
+    m1 = fmax3(m1, x[c + 2], x[c + 3]);
+    m2 = fmax3(m2, x[c + 4], x[c + 5]);
+    m3 = fmax3(m3, x[c + 6], x[c + 7]);
+  }
+  m0 = fmax3(m0, x[60], x[61]);
+  m1 = fmax3(m1, x[62], x[63]);
+  return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+}
+// 32 logits -> probabilities of 32 keys as bf16 pairs: hi to `hi`, what is left of them to `lo` (16 columns each); returns their sum
+template <int kParts>
+__device__ __forceinline__ float ch_probs32(const float* x, float scale, float neg_ref, uint32_t hi, uint32_t lo) {
+  float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+  uint32_t ph[16], pl[16];
+#pragma unroll
+  for (int c = 0; c < 32; c += 4) {
+    const float p0 = fast_exp2(fmaf(x[c], scale, neg_ref)), p1 = fast_exp2(fmaf(x[c + 1], scale, neg_ref));
+    const float p2 = fast_exp2(fmaf(x[c + 2], scale, neg_ref)), p3 = fast_exp2(fmaf(x[c + 3], scale, neg_ref));
+    s0 += p0;
+    s1 += p1;
+    s2 += p2;
+    s3 += p3;
+    ph[c / 2] = pack_bf16(p0, p1);
+    ph[c / 2 + 1] = pack_bf16(p2, p3);
+    if (kParts > 1) {
+      pl[c / 2] = pack_bf16(p0 - __uint_as_float(ph[c / 2] << 16), p1 - __uint_as_float(ph[c / 2] & 0xffff0000u));
+      pl[c / 2 + 1] = pack_bf16(p2 - __uint_as_float(ph[c / 2 + 1] << 16), p3 - __uint_as_float(ph[c / 2 + 1] & 0xffff0000u));
+    }
+  }
+  tmem_st16u(hi, ph);
+  if (kParts > 1) tmem_st16u(lo, pl);
+  return (s0 + s1) + (s2 + s3);
+}
+
+// pool row of row r of a list, or of its overflow pages (page < 0: not there)
+__device__ __forceinline__ int ch_page(const ChunkArgs& a, int seg, int o) {
+  const int p = o >> 6;
+  int pg = (a.table && p < a.max_pages) ? a.table[(int64_t)seg * a.max_pages + p] : -1;
+#ifdef CATEKV_CHECKED
+  pg = checked_clamp(pg, 0, a.n_pages - 1, a.checked, kKidChunk, seg);
+#endif
+  return pg < a.n_pages ? pg : -1;
+}
+
+template <bool kQ2, int kParts>
+__global__ void __launch_bounds__(kChThreads, 1)
+    chunk_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                      const __grid_constant__ CUtensorMap ko_map, const __grid_constant__ CUtensorMap vo_map,
+                      const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ChunkArgs a,
+                      const __grid_constant__ ChunkSeqs sq) {
+  constexpr int kLead = kQ2 ? 1 : 2;  // K tiles ahead of the V tile in the ring: K_0 .. K_{lead-1}, V_0, K_lead, V_1, ...
+  constexpr int kQBytes = (kQ2 ? 2 : 1) * kChTileBytes, kQBlock = kQBytes / 2;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int s_scan[12 + 4];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (s_base - smem_u32(smem_raw));
+  const uint32_t s_q = s_base, s_ring = s_base + kQBytes;
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(smem + kQBytes + kChStages * kChTileBytes);
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + kChBarriers);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+  int* s_odd = reinterpret_cast<int*>(s_tmem + 4);            // [4]: first new row with an infinity or a NaN in V, of the last blocks that had V tiles looked at
+  float2* s_ml = reinterpret_cast<float2*>(s_tmem + 8);       // one M tile: [stream][row] reference and sum
+  const uint32_t bar0 = smem_u32(s_bar);
+  auto B = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+  constexpr int kFull = 0, kEmpty = kChStages, kFixed = 2 * kChStages, kDoneS = 3 * kChStages, kPReady = kDoneS + 2, kDoneO = kPReady + 2,
+                kQFull = kDoneO + 2, kQEmpty = kQFull + 1, kXch = kQEmpty + 1;
+  static_assert(kXch + 4 <= kChBarriers, "barrier table");
+
+  pdl_launch_dependents();
+  if (tid == 0) {
+    *s_abort = 0;
+    for (int i = 0; i < kChBarriers; ++i) {
+      const int count = (i == kPReady || i == kPReady + 1) ? 4 : (i >= kXch ? 2 : 1);
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(B(i)), "r"(count));
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(s_tmem)), "r"(kChTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
+  pdl_wait();
+
+  // ---- this CTA's share of the tiles of all blocks
+  int total = 0, u0 = 0, u1 = 0;
+  {
+    int mine = 0;
+    for (int s = tid; s < a.n_segs; s += kChThreads) {
+      const ChunkSeg g = ch_seg(a, sq, s);
+      for (int j = 0; j < g.n_blk; ++j) mine += ch_tiles(a, g, j);
+    }
+    int x = mine;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (lane == 0) s_scan[warp] = x;
+    if (tid == 0) s_scan[12] = a.n_segs;  // no tile: nothing to do
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 12; ++w) total += s_scan[w];
+    const int C = gridDim.x, c = blockIdx.x, q = total / C, r = total % C;
+    u0 = c * q + min(c, r);
+    u1 = u0 + q + (c < r ? 1 : 0);
+    int before = 0;
+    for (int s0 = 0; s0 < a.n_segs; s0 += kChThreads) {
+      __syncthreads();
+      const int s = s0 + tid;
+      ChunkSeg g = {0, 0, 0};
+      int cost = 0;
+      if (s < a.n_segs) {
+        g = ch_seg(a, sq, s);
+        if (a.n_segs <= kChThreads) cost = mine;
+        else
+          for (int j = 0; j < g.n_blk; ++j) cost += ch_tiles(a, g, j);
+      }
+      int inc = cost;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (lane == 31) s_scan[warp] = inc;
+      __syncthreads();
+      int ex = before + inc - cost;
+#pragma unroll
+      for (int w = 0; w < 12; ++w) {
+        ex += w < warp ? s_scan[w] : 0;
+        before += s_scan[w];
+      }
+      if (u1 > u0 && u0 >= ex && u0 < ex + cost) {
+        int t = u0 - ex, j = 0, nt = ch_tiles(a, g, 0);
+        while (t >= nt) {
+          t -= nt;
+          nt = ch_tiles(a, g, ++j);
+        }
+        s_scan[12] = s;
+        s_scan[13] = j;
+        s_scan[14] = t;
+        int32_t* d = a.desc + blockIdx.x * 8;
+        d[0] = s;
+        d[1] = j;
+        d[2] = t;
+        d[3] = nt;
+        d[4] = g.n_new;
+        d[5] = total;
+      }
+    }
+    if (u1 <= u0 && tid == 0) a.desc[blockIdx.x * 8 + 2] = 0;  // no share: no cut at its start
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  ChunkWalk walk;
+  walk.left = u1 - u0;
+  walk.seg = s_scan[12];
+  walk.blk = s_scan[13];
+  walk.t = s_scan[14];
+  walk.g = ChunkSeg{0, 0, 0};
+  if (walk.left > 0) walk.g = ch_seg(a, sq, walk.seg);
+  ChunkItem it;
+
+  if (warp == 9) {
+    // ================= K and V tiles, in the order in which the tensor pipe uses them
+    if (lane == 0 && !a.idle_producer) {
+      uint32_t use = 0;
+      bool ok = true;
+      while (ok && walk.next(a, sq, it)) {
+        const int n = it.t1 - it.t0;
+        const int off = a.seg_off[it.seg], cap = a.seg_cap[it.seg];
+        auto load = [&](const CUtensorMap* pool, const CUtensorMap* ovf, int t) {
+          const int st = use % kChStages;
+          if (use >= kChStages && !mbar_wait(B(kEmpty + st), ((use / kChStages) - 1) & 1, s_abort, a.spin_limit)) return false;
+          ++use;
+          const int r0 = t * kKeyTile;
+          const uint32_t dst = s_ring + st * kChTileBytes, bar = B(kFull + st);
+          if (r0 < cap) {
+            mbar_expect_tx(bar, kChTileBytes);
+            tma_load_2d(dst, pool, 0, off + r0, bar);
+            tma_load_2d(dst + kKBlockBytes, pool, 64, off + r0, bar);
+          } else {
+            const int pg0 = r0 < it.g.len ? ch_page(a, it.seg, r0 - cap) : -1;
+            const int pg1 = r0 + 64 < it.g.len ? ch_page(a, it.seg, r0 + 64 - cap) : -1;
+            mbar_expect_tx(bar, (pg0 >= 0 ? kChTileBytes / 2 : 0) + (pg1 >= 0 ? kChTileBytes / 2 : 0));
+            if (pg0 >= 0) {
+              tma_load_2d(dst, ovf, 0, pg0 * 64, bar);
+              tma_load_2d(dst + kKBlockBytes, ovf, 64, pg0 * 64, bar);
+            }
+            if (pg1 >= 0) {
+              tma_load_2d(dst + 64 * 128, ovf, 0, pg1 * 64, bar);
+              tma_load_2d(dst + kKBlockBytes + 64 * 128, ovf, 64, pg1 * 64, bar);
+            }
+          }
+          return true;
+        };
+        for (int t = 0; ok && t < min(kLead, n); ++t) ok = load(&k_map, &ko_map, it.t0 + t);
+        for (int t = 0; ok && t < n; ++t) {
+          ok = load(&v_map, &vo_map, it.t0 + t);
+          if (ok && t + kLead < n) ok = load(&k_map, &ko_map, it.t0 + t + kLead);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 11) {
+    // ================= the query block of every item
+    if (lane == 0 && !a.idle_producer) {
+      uint32_t n_item = 0;
+      while (walk.next(a, sq, it)) {
+        if (n_item >= 1 && !mbar_wait(B(kQEmpty), (n_item - 1) & 1, s_abort, a.spin_limit)) break;
+        ++n_item;
+        const int h = it.seg % a.Hkv, token = sq.start[it.seg / a.Hkv] + it.blk * a.TB;
+        mbar_expect_tx(B(kQFull), 2 * 128 * a.G * a.TB);
+        tma_load_3d(s_q, &q_map, 0, h * a.G, token, B(kQFull));
+        tma_load_3d(s_q + kQBlock, &q_map, 64, h * a.G, token, B(kQFull));
+      }
+    }
+    __syncwarp();
+  } else if (warp == 10) {
+    // ================= V tiles with rows that some query of the block does not see
+    uint32_t base = 0, n_item = 0;
+    bool ok = !a.idle_producer;
+    while (ok && walk.next(a, sq, it)) {
+      const int n = it.t1 - it.t0;
+      const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;                       // rows that every query sees
+      const int last = it.g.len - it.g.n_new + min(it.g.n_new, a.TB * (it.blk + 1));     // rows that the last one sees
+      bool fresh = true;
+      for (int t = 0; ok && t < n; ++t) {
+        const int r0 = (it.t0 + t) * kKeyTile;
+        if (r0 + kKeyTile <= first) continue;
+        const uint32_t use = base + min(kLead, n) + t + min(t, max(n - kLead, 0));
+        const int st = use % kChStages;
+        ok = mbar_wait(B(kFull + st), (use / kChStages) & 1, s_abort, a.spin_limit);
+        if (!ok) break;
+        if (fresh) {
+          // four flags in turn: this block's V tile is in the ring, so the results of the block four before it are out
+          if (lane == 0) s_odd[n_item & 3] = 0x7fffffff;
+          __syncwarp();
+          fresh = false;
+        }
+        uint8_t* tile = smem + kQBytes + st * kChTileBytes;
+        int odd = 0x7fffffff;
+#pragma unroll 4
+        for (int i = 0; i < 64; ++i) {
+          const int r = i * 2 + (lane >> 4), c = lane & 15, j = r0 + r;
+          uint4* p = reinterpret_cast<uint4*>(tile + sw128_off(r, c, 128));
+          if (j >= last) {
+            *p = make_uint4(0u, 0u, 0u, 0u);
+          } else if (j >= first) {
+            uint4 v = *p;
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+            bool bad = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if ((w[k] & 0x7f80u) == 0x7f80u) bad = true, w[k] &= 0xffff0000u;
+              if ((w[k] & 0x7f800000u) == 0x7f800000u) bad = true, w[k] &= 0x0000ffffu;
+            }
+            if (bad) {
+              *p = v;
+              odd = min(odd, j);
+            }
+          }
+        }
+        if (odd != 0x7fffffff) atomicMin(&s_odd[n_item & 3], odd);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kFixed + st));
+      }
+      base += 2 * n;
+      n_item += fresh ? 0 : 1;
+    }
+    __syncwarp();
+  } else if (warp == 8) {
+    // ================= tensor-core issue
+    if (lane == 0 && !a.idle_producer) {
+      const uint32_t idesc_s = umma_idesc_bf16(128, 128), idesc_o = umma_idesc_bf16_bmn(128, 128);
+      const uint64_t dq0 = umma_desc_sw128(s_q), dk0 = umma_desc_sw128(s_ring), dv0 = umma_desc_sw128_mn(s_ring, kKBlockBytes);
+      const uint32_t dv_hi = (uint32_t)(dv0 >> 32), dv_lo0 = (uint32_t)dv0;
+      uint32_t use = 0, n_item = 0, fixed = 0;  // fixed: one bit per stage, the parity of its next look
+      uint32_t n_p[2] = {0, 0};
+      bool ok = true;
+      auto wait_tile = [&]() { return mbar_wait(B(kFull + use % kChStages), (use / kChStages) & 1, s_abort, a.spin_limit); };
+      auto issue_s = [&](int x, int st) {
+        const uint64_t dq = dq0 + (uint64_t)((kQ2 ? x : 0) * (128 * 128 >> 4)), dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4));
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+          umma_bf16(tmem + x * 128, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2),
+                    dk + (uint64_t)((kk >> 2) * (kKBlockBytes >> 4) + (kk & 3) * 2), idesc_s, kk ? 1u : 0u);
+        umma_commit(B(kDoneS + x));
+      };
+      auto issue_o = [&](int x, int st, bool fresh) {
+        const uint32_t lo = dv_lo0 + (uint32_t)(st * (kChTileBytes >> 4));
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+            umma_bf16_ta_lohi(tmem + 256 + x * 128, tmem + x * 128 + part * 64 + kk * 8, lo + (uint32_t)(kk * 128), dv_hi, idesc_o,
+                              (part | kk) ? 1u : (fresh ? 0u : 1u));
+      };
+      while (ok && walk.next(a, sq, it)) {
+        const int n = it.t1 - it.t0;
+        const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;
+        if (!(ok = mbar_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit))) break;
+        ++n_item;
+        tc_fence_after();
+        for (int t = 0; ok && t < min(kLead, n); ++t) {
+          if (!(ok = wait_tile())) break;
+          tc_fence_after();
+          const int st = use++ % kChStages;
+          issue_s(t, st);
+          if (kQ2) issue_s(1, st);
+          umma_commit(B(kEmpty + st));
+        }
+        if (ok && n <= kLead) umma_commit(B(kQEmpty));
+        for (int t = 0; ok && t < n; ++t) {
+          const bool look = (it.t0 + t + 1) * kKeyTile > first;
+          const bool more = t + kLead < n;
+          const int sv = use % kChStages, sk = (use + 1) % kChStages;
+#pragma unroll
+          for (int y = 0; y < (kQ2 ? 2 : 1); ++y) {
+            const int x = kQ2 ? y : (t & 1);
+            if (!(ok = mbar_wait(B(kPReady + x), n_p[x] & 1, s_abort, a.spin_limit))) break;
+            ++n_p[x];
+            if (y == 0) {
+              if (!(ok = wait_tile())) break;
+              if (look) {
+                if (!(ok = mbar_wait(B(kFixed + sv), (fixed >> sv) & 1, s_abort, a.spin_limit))) break;
+                fixed ^= 1u << sv;
+              }
+              ++use;
+            }
+            tc_fence_after();
+            issue_o(x, sv, t < (kQ2 ? 1 : 2));
+            if (!kQ2 || y == 1) umma_commit(B(kEmpty + sv));
+            if (more) {
+              if (y == 0) {
+                if (!(ok = wait_tile())) break;
+                tc_fence_after();
+              }
+              issue_s(x, sk);
+              if (!kQ2 || y == 1) {
+                umma_commit(B(kEmpty + sk));
+                ++use;
+                if (t + kLead + 1 == n) umma_commit(B(kQEmpty));
+              }
+            } else {
+              umma_commit(B(kDoneO + x));
+            }
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ================= softmax: warps 0-3 stream 0, warps 4-7 stream 1; a thread owns a row
+    const int x = warp >> 2, quarter = warp & 3;
+    const int lane_row = quarter * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+    const uint32_t slot = tmem + lane_base + x * 128, acc = tmem + lane_base + 256 + x * 128;
+    const int row = (kQ2 ? x * 128 : 0) + lane_row;  // row of the block
+    const int tok = row / a.G;
+    uint32_t n_s = 0, n_o = 0, n_x = 0, n_item = 0;
+    bool alive = true, first_item = true;
+    while (alive && walk.next(a, sq, it)) {
+      const int n = it.t1 - it.t0;
+      const int n_mine = kQ2 ? n : (n + 1 - x) / 2;
+      const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;
+      const int token = it.blk * a.TB + tok;
+      const bool valid = tok < a.TB && token < it.g.n_new;
+      const int sees = it.g.len - it.g.n_new + token + 1;  // rows that this thread's query sees
+      const bool idle = !__any_sync(0xffffffffu, valid);   // no row of the warp is a query: it only keeps the barriers going
+      float ref = -INFINITY, l = 0.f;
+      for (int i = 0; i < n_mine; ++i) {
+        const int t = it.t0 + (kQ2 ? i : 2 * i + x);
+        if (!(alive = mbar_wait(B(kDoneS + x), n_s & 1, s_abort, a.spin_limit))) break;
+        ++n_s;
+        if (!idle) {
+          tc_fence_after();
+          float y0[64], y1[64];
+          tmem_ld64(slot, y0);
+          tmem_ld64(slot + 64, y1);
+          tmem_wait_ld64(y0);
+          tmem_wait_ld64(y1);
+          if ((t + 1) * kKeyTile > first) {
+            const int lim = sees - t * kKeyTile;
+#pragma unroll
+            for (int c = 0; c < 64; ++c) {
+              y0[c] = c < lim ? y0[c] : -INFINITY;
+              y1[c] = c + 64 < lim ? y1[c] : -INFINITY;
+            }
+          }
+          const float mx = fmaxf(ch_max64(y0), ch_max64(y1)) * a.scale_log2;
+          const bool grow = mx > ref + kChTau;  // also the first tile with a visible key
+          const bool rescale = grow && ref > -INFINITY;
+          if (__any_sync(0xffffffffu, rescale)) {
+            // the products of the tile before are done: the tensor pipe finished them ahead of this S
+            const float f = rescale ? fast_exp2(ref - mx) : 1.f;
+            l *= f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 32) {
+              float o[32];
+              tmem_ld32(acc + c0, o);
+              tmem_wait_ld32(o);
+#pragma unroll
+              for (int c = 0; c < 32; ++c) o[c] *= f;
+              tmem_st32(acc + c0, o);
+            }
+          }
+          if (grow) ref = mx;
+          const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
+          float s = ch_probs32<kParts>(y0, a.scale_log2, neg, slot, slot + 64);
+          s += ch_probs32<kParts>(y0 + 32, a.scale_log2, neg, slot + 16, slot + 80);
+          s += ch_probs32<kParts>(y1, a.scale_log2, neg, slot + 32, slot + 96);
+          s += ch_probs32<kParts>(y1 + 32, a.scale_log2, neg, slot + 48, slot + 112);
+          l += s;
+          tmem_wait_st();
+          tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kPReady + x));
+      }
+      if (!alive) break;
+      if (n_mine > 0) {
+        if (!(alive = mbar_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
+        ++n_o;
+      }
+      tc_fence_after();
+      // ---- the item's result: the whole block, or a piece of it
+      const bool looked = it.t1 * kKeyTile > first;
+      const int odd = looked ? s_odd[n_item & 3] : 0x7fffffff;
+      n_item += looked ? 1 : 0;
+      const bool whole = n == it.nt;
+      const int b = it.seg / a.Hkv, h = it.seg - b * a.Hkv;
+      const int64_t orow = (int64_t)(sq.start[b] + token) * a.Hq + h * a.G + (row - tok * a.G);
+      const int64_t prow = (int64_t)(2 * blockIdx.x + (first_item ? 0 : 1)) * a.slot_rows + row;
+      first_item = false;
+      float f0 = 1.f, f1 = 0.f, ref_t = ref, l_t = l;
+      bool both = false;
+      if (!kQ2) {  // the two streams' halves of the keys; each stream's warps take half of d
+        s_ml[x * 128 + lane_row] = make_float2(ref, l);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kXch + quarter));
+        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
+        ++n_x;
+        tc_fence_after();
+        const float2 m0 = s_ml[lane_row], m1 = s_ml[128 + lane_row];
+        ref_t = fmaxf(m0.x, m1.x);
+        f0 = m0.x > -INFINITY ? fast_exp2(m0.x - ref_t) : 0.f;
+        f1 = m1.x > -INFINITY ? fast_exp2(m1.x - ref_t) : 0.f;
+        l_t = m0.y * f0 + m1.y * f1;
+        both = n > 1;
+      }
+      const float inv = whole ? (l_t > 0.f ? 1.f / l_t : (l_t == 0.f ? 0.f : l_t)) : 1.f;  // a NaN stays one
+      const int c_lo = kQ2 ? 0 : x * 64, c_hi = kQ2 ? 128 : c_lo + 64;
+      const uint32_t acc0 = kQ2 ? acc : tmem + lane_base + 256;
+      if (!idle) {
+#pragma unroll 1
+        for (int c0 = c_lo; c0 < c_hi; c0 += 32) {
+          float o[32];
+          tmem_ld32(acc0 + c0, o);
+          tmem_wait_ld32(o);
+          if (!kQ2) {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = f0 > 0.f ? o[c] * f0 : 0.f;
+            if (both) {
+              float o1[32];
+              tmem_ld32(acc0 + 128 + c0, o1);
+              tmem_wait_ld32(o1);
+#pragma unroll
+              for (int c = 0; c < 32; ++c) o[c] += f1 > 0.f ? o1[c] * f1 : 0.f;
+            }
+          }
+          if (odd < sees && valid) {  // infinities and NaN that were taken out of the V tiles
+            const int off = a.seg_off[it.seg], cap = a.seg_cap[it.seg];
+            for (int j = max(odd, it.t0 * kKeyTile); j < min(sees, it.t1 * kKeyTile); ++j) {
+              const uint16_t* v = a.v_pool + (int64_t)(off + j) * kD;
+              if (j >= cap) {
+                const int pg = ch_page(a, it.seg, j - cap);
+                if (pg < 0) continue;
+                v = a.v_ovf + ((int64_t)pg * 64 + ((j - cap) & 63)) * kD;
+              }
+#pragma unroll
+              for (int c = 0; c < 32; ++c) {
+                const uint32_t w = (uint32_t)v[c0 + c] << 16;
+                if ((w & 0x7f800000u) == 0x7f800000u) o[c] += __uint_as_float(w);
+              }
+            }
+          }
+          if (valid) {
+            if (!whole) {
+              float* dst = a.part_o + prow * kD + c0;
+#pragma unroll
+              for (int c = 0; c < 32; c += 4) *reinterpret_cast<float4*>(dst + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+            } else if (a.out_fp32) {
+              float* dst = reinterpret_cast<float*>(a.out) + orow * kD + c0;
+#pragma unroll
+              for (int c = 0; c < 32; c += 4)
+                *reinterpret_cast<float4*>(dst + c) = make_float4(o[c] * inv, o[c + 1] * inv, o[c + 2] * inv, o[c + 3] * inv);
+            } else {
+              uint16_t* dst = reinterpret_cast<uint16_t*>(a.out) + orow * kD + c0;
+#pragma unroll
+              for (int c = 0; c < 32; c += 8) {
+                uint4 w;
+                w.x = pack_bf16(o[c] * inv, o[c + 1] * inv);
+                w.y = pack_bf16(o[c + 2] * inv, o[c + 3] * inv);
+                w.z = pack_bf16(o[c + 4] * inv, o[c + 5] * inv);
+                w.w = pack_bf16(o[c + 6] * inv, o[c + 7] * inv);
+                *reinterpret_cast<uint4*>(dst + c) = w;
+              }
+            }
+          }
+        }
+        if (valid && (kQ2 || x == 0)) {
+          if (!whole) a.part_ml[prow] = make_float2(ref_t, l_t);
+          else if (a.lse) a.lse[orow] = l_t == 0.f ? -INFINITY : (ref_t + log2f(l_t)) * 0.6931471805599453f;
+        }
+      }
+      tc_fence_before();
+      if (!kQ2) {  // the other stream's warps have read this accumulator: its next product may overwrite it
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kXch + quarter));
+        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
+        ++n_x;
+      }
+    }
+  }
+
+  // ---- release tensor memory (after an abort: first give copies that may still be in flight time to land)
+  if (*s_abort)
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kChTmemCols) : "memory");
+  if (*s_abort && tid == 0) raise_status(a.status, CATEKV_STATUS_WAIT_EXPIRED, kKidChunk, walk.seg, (int)blockIdx.x);
+}
+
+// Merge the pieces of the blocks that several CTAs share, in the order of the keys: CTA c's descriptor says whether its share
+// begins inside a block; the first such CTA of a block has it merged.  A warp per query row; a lane owns four d.
+constexpr int kChCombineRows = 32;
+__global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq, int C) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int c = blockIdx.x;
+  const int32_t* d = a.desc + c * 8;
+  const int t0 = d[2];
+  if (t0 == 0) return;
+  const int seg = d[0], blk = d[1], nt = d[3], n_new = d[4], total = d[5];
+  const int q = total / C, r = total % C;
+  auto begin = [&](int i) { return i * q + min(i, r); };
+  const int ub = begin(c) - t0, ue = ub + nt;
+  if (begin(c - 1) > ub) return;  // an earlier CTA begins inside this block
+  int c_end = c + 1;
+  while (c_end < C && begin(c_end) < ue) ++c_end;
+  const int head = begin(c - 1) < ub ? 1 : 0;  // slot of the first piece: the last item of CTA c - 1, or its only one
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int b = seg / a.Hkv, h = seg - b * a.Hkv;
+  for (int i = warp; i < kChCombineRows; i += 8) {
+    const int row = blockIdx.y * kChCombineRows + i, tok = row / a.G, token = blk * a.TB + tok;
+    if (tok >= a.TB || token >= n_new) continue;
+    auto slot = [&](int k) { return (int64_t)(2 * k + (k == c - 1 ? head : 0)) * a.slot_rows + row; };
+    float M = -INFINITY;
+    for (int k = c - 1; k < c_end; ++k) M = fmaxf(M, a.part_ml[slot(k)].x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float L = 0.f;
+    for (int k = c - 1; k < c_end; ++k) {
+      const float2 ml = a.part_ml[slot(k)];
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;  // the row sees none of this piece's keys
+      const float w = ml.x > -INFINITY ? exp2f(ml.x - M) : 1.f;
+      const float4 v = *reinterpret_cast<const float4*>(a.part_o + slot(k) * kD + lane * 4);
+      acc.x += w * v.x;
+      acc.y += w * v.y;
+      acc.z += w * v.z;
+      acc.w += w * v.w;
+      L += w * ml.y;
+    }
+    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+    const int64_t orow = (int64_t)(sq.start[b] + token) * a.Hq + h * a.G + (row - tok * a.G);
+    if (a.out_fp32) {
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + orow * kD + lane * 4) =
+          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    } else {
+      uint2 pk;
+      pk.x = pack_bf16(acc.x * inv, acc.y * inv);
+      pk.y = pack_bf16(acc.z * inv, acc.w * inv);
+      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + orow * kD + lane * 4) = pk;
+    }
+    if (lane == 0 && a.lse) a.lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  }
+}
+
+// ---- append: the chunk's rows behind the end of every list.  A warp copies a row (lanes 0-15 K, 16-31 V), eight in flight.
+struct AppendArgs {
+  uint8_t* k_pool;
+  uint8_t* v_pool;
+  const int32_t* seg_off;
+  int32_t* seg_len;
+  const int32_t* seg_cap;
+  PageArgs pg;
+  int32_t n_pages, Hkv;
+  const uint8_t* k_new;
+  const uint8_t* v_new;
+  int64_t stride_t, stride_h;  // bytes
+  int32_t* checked;
+};
+constexpr int kApRows = 64;  // rows of a block
+// rows that fit: the capacity and the pages that the table names
+__device__ __forceinline__ uint8_t* ap_row(const AppendArgs& a, int seg, int r, bool v) {
+  const int cap = a.seg_cap[seg];
+  if (r < cap) return (v ? a.v_pool : a.k_pool) + ((int64_t)a.seg_off[seg] + r) * kRowBytes;
+  const int o = r - cap, p = o >> 6;
+  if (!a.pg.table || p >= a.pg.max_pages) return nullptr;
+  int pg = a.pg.table[(int64_t)seg * a.pg.max_pages + p];
+#ifdef CATEKV_CHECKED
+  pg = checked_clamp(pg, 0, a.n_pages - 1, a.checked, kKidChunk, seg);
+#endif
+  if (pg < 0 || pg >= a.n_pages) return nullptr;
+  return (v ? a.pg.v_ovf : a.pg.k_ovf) + ((int64_t)pg * 64 + (o & 63)) * kRowBytes;
+}
+// One block takes kApRows rows of a list.  kAlone: every list's rows fit one block, which also counts them in.
+template <bool kAlone>
+__global__ void __launch_bounds__(256) append_chunk_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ChunkSeqs sq) {
+  const int seg = blockIdx.x, b = seg / a.Hkv, h = seg - b * a.Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (lane & 15) * 16;
+  pdl_launch_dependents();
+  const int n = sq.n_new[b], r0 = blockIdx.y * kApRows;
+  if (r0 >= n) return;
+  pdl_wait();
+  const int len = a.seg_len[seg];
+  const uint8_t* src = (lane < 16 ? a.k_new : a.v_new) + (int64_t)(sq.start[b]) * a.stride_t + h * a.stride_h + c;
+  uint4 v[kApRows / 8];
+#pragma unroll
+  for (int i = 0; i < kApRows / 8; ++i) {
+    const int r = r0 + warp + 8 * i;
+    if (r < n) v[i] = __ldg(reinterpret_cast<const uint4*>(src + r * a.stride_t));
+  }
+#pragma unroll
+  for (int i = 0; i < kApRows / 8; ++i) {
+    const int r = r0 + warp + 8 * i;
+    if (r >= n) break;
+    uint8_t* dst = ap_row(a, seg, len + r, lane >= 16);
+    if (dst) *reinterpret_cast<uint4*>(dst + c) = v[i];
+  }
+  if (kAlone) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int m = n;
+      while (m > 0 && !ap_row(a, seg, len + m - 1, false)) --m;  // a replayed call that found a full list: what is there counts
+      a.seg_len[seg] = len + m;
+    }
+  }
+}
+__global__ void __launch_bounds__(128) append_count_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ChunkSeqs sq, int n_segs) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int seg = blockIdx.x * 128 + threadIdx.x;
+  if (seg >= n_segs) return;
+  const int n = sq.n_new[seg / a.Hkv], len = a.seg_len[seg];
+  int m = n;
+  while (m > 0 && !ap_row(a, seg, len + m - 1, false)) m = (m - 1) / 64 * 64;
+  if (n) a.seg_len[seg] = len + m;
+}
+
+// ---- host
+static int take_chunk(const catekv_cache* c, const catekv_chunk* ch, ChunkSeqs* sq, int* max_new, int64_t* sum) {
+  if (!ch || !ch->n_new || ch->B != c->B || ch->n_tokens < 0) return CATEKV_ERR_INVALID_ARG;
+  if (ch->B > kChMaxSeqs) return CATEKV_ERR_UNSUPPORTED;
+  int64_t at = 0;
+  *max_new = 0;
+  *sum = 0;
+  bool ascending = true;
+  int64_t end = 0;
+  for (int b = 0; b < ch->B; ++b) {
+    const int n = ch->n_new[b];
+    if (n < 0) return CATEKV_ERR_INVALID_ARG;
+    if (ch->start) at = ch->start[b];
+    if (at < 0 || at + n > ch->n_tokens) return CATEKV_ERR_INVALID_ARG;
+    sq->n_new[b] = n;
+    sq->start[b] = (int32_t)at;
+    if (n) {
+      ascending = ascending && at >= end;
+      end = at + n;
+    }
+    at += n;
+    *sum += n;
+    *max_new = n > *max_new ? n : *max_new;
+  }
+  if (!ascending)  // in another order: no token belongs to two sequences
+    for (int b = 0; b < ch->B; ++b)
+      for (int i = 0; i < b; ++i)
+        if (sq->n_new[b] && sq->n_new[i] && sq->start[b] < sq->start[i] + sq->n_new[i] && sq->start[i] < sq->start[b] + sq->n_new[b])
+          return CATEKV_ERR_INVALID_ARG;
+  return CATEKV_OK;
+}
+static const int32_t* caps_on_device(const catekv_cache* c) { return c->pages ? c->pages->seg_cap_dev : c->seg_cap_dev; }
+
+struct ChunkWs {
+  size_t off_desc, off_ml, off_o, bytes;
+  int slot_rows;
+};
+// one M tile where no sequence has more rows than it holds
+static bool ch_two_tiles(int G, int max_new) { return (int64_t)G * max_new > 128; }
+static ChunkWs chunk_ws_layout(int G, int max_new) {
+  ChunkWs w;
+  const int block = ch_two_tiles(G, max_new) ? 256 : 128;
+  const int64_t rows = (int64_t)G * max_new;
+  w.slot_rows = rows < block ? (int)rows : block;
+  const size_t ctas = (size_t)sm_count();
+  size_t o = CATEKV_STATUS_BYTES;
+  w.off_desc = o; o = align_up(o + ctas * 8 * sizeof(int32_t), 256);
+  w.off_ml = o; o = align_up(o + 2 * ctas * w.slot_rows * sizeof(float2), 256);
+  w.off_o = o; o = align_up(o + 2 * ctas * w.slot_rows * (size_t)kD * sizeof(float), 256);
+  w.bytes = o;
+  return w;
+}
+static int make_pool_map(const void* p, int64_t rows, int box_rows, CUtensorMap* map) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return CATEKV_ERR_CUDA;
+  if ((uintptr_t)p & 15) return CATEKV_ERR_INVALID_ARG;
+  const cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)(rows > 0 ? rows : 1)};
+  const cuuint64_t strides[1] = {kRowBytes};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? CATEKV_OK : CATEKV_ERR_UNSUPPORTED;
+}
+static int make_q_map(const void* q, int n_tokens, int Hq, int G, int TB, int64_t st, int64_t sh, CUtensorMap* map) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return CATEKV_ERR_CUDA;
+  const cuuint64_t dims[3] = {(cuuint64_t)kD, (cuuint64_t)Hq, (cuuint64_t)n_tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)(Hq > 1 ? sh * 2 : kRowBytes), (cuuint64_t)(n_tokens > 1 ? st * 2 : kRowBytes)};
+  const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)TB};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? CATEKV_OK : CATEKV_ERR_UNSUPPORTED;
+}
+
+template <bool kQ2, int kParts>
+static int launch_chunk(int ctas, const CUtensorMap* m, const ChunkArgs& a, const ChunkSeqs& sq, cudaStream_t st) {
+  static std::atomic<bool> attr_set[64];
+  int dev = 0;
+  CATEKV_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ch_smem_bytes<kQ2>()));
+    if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+  }
+  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts>, dim3(ctas), dim3(kChThreads), ch_smem_bytes<kQ2>(), st, m[0], m[1], m[2], m[3], m[4],
+                             a, sq));
+  return CATEKV_OK;
+}
+}  // namespace catekv
+
+using namespace catekv;
+
+extern "C" int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const void* k_new, const void* v_new, int64_t stride_t,
+                                   int64_t stride_h, catekv_stream stream) {
+  CATEKV_API_RANGE();
+  int rc = check_cache(cache);
+  if (rc) return rc;
+  ChunkSeqs sq;
+  int max_new = 0;
+  int64_t sum = 0;
+  rc = take_chunk(cache, chunk, &sq, &max_new, &sum);
+  if (rc) return rc;
+  const int n_segs = cache->B * cache->Hkv;
+  for (int s = 0; s < n_segs; ++s) {
+    const int n = sq.n_new[s / cache->Hkv];
+    if (cache->seg_len[s] < 0) return CATEKV_ERR_INVALID_ARG;
+    if (n && (int64_t)cache->seg_len[s] + n > seg_capacity(cache, s)) return CATEKV_ERR_CAPACITY;
+  }
+  if (!caps_on_device(cache)) return CATEKV_ERR_INVALID_ARG;
+  if (sum == 0) return CATEKV_OK;
+  if (!k_new || !v_new || (((uintptr_t)k_new | (uintptr_t)v_new) & 15)) return CATEKV_ERR_INVALID_ARG;
+  if (stride_t % 8 || stride_h % 8 || (stride_t < kD && chunk->n_tokens > 1) || (stride_h < kD && cache->Hkv > 1)) return CATEKV_ERR_UNSUPPORTED;
+  const int blocks = (max_new + kApRows - 1) / kApRows;
+  if (blocks > 65535) return CATEKV_ERR_UNSUPPORTED;
+  AppendArgs a = {};
+  a.k_pool = (uint8_t*)cache->k_pool;
+  a.v_pool = (uint8_t*)cache->v_pool;
+  a.seg_off = cache->seg_off_dev;
+  a.seg_len = cache->seg_len_dev;
+  a.seg_cap = caps_on_device(cache);
+  a.pg = page_args(cache);
+  a.n_pages = cache->pages ? cache->pages->n_pages : 0;
+  a.Hkv = cache->Hkv;
+  a.k_new = (const uint8_t*)k_new;
+  a.v_new = (const uint8_t*)v_new;
+  a.stride_t = stride_t * 2;
+  a.stride_h = stride_h * 2;
+  a.checked = checked_status_ptr();
+  cudaStream_t st = (cudaStream_t)stream;
+  if (blocks == 1) {
+    CATEKV_CUDA_TRY(launch_pdl(append_chunk_kernel<true>, dim3(n_segs), dim3(256), 0, st, a, sq));
+  } else {
+    CATEKV_CUDA_TRY(launch_pdl(append_chunk_kernel<false>, dim3(n_segs, blocks), dim3(256), 0, st, a, sq));
+    CATEKV_CUDA_TRY(launch_pdl(append_count_kernel, dim3((n_segs + 127) / 128), dim3(128), 0, st, a, sq, n_segs));
+  }
+  for (int s = 0; s < n_segs; ++s) cache->seg_len[s] += sq.n_new[s / cache->Hkv];
+  return CATEKV_OK;
+}
+
+extern "C" size_t catekv_chunk_attn_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t max_new) {
+  if (Hq <= 0 || Hkv <= 0 || Hq % Hkv || Hq / Hkv > kMaxG || max_new < 0) return 0;
+  return chunk_ws_layout(Hq / Hkv, max_new > 0 ? max_new : 1).bytes;
+}
+
+extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* chunk, const void* q, int64_t q_stride_t, int64_t q_stride_h,
+                                 int32_t Hq, float sm_scale, void* out, int32_t out_dtype, float* lse_out, void* ws, size_t ws_bytes,
+                                 catekv_stream stream) {
+  CATEKV_API_RANGE();
+  int rc = check_cache(cache);
+  if (rc) return rc;
+  ChunkSeqs sq;
+  int max_new = 0;
+  int64_t sum = 0;
+  rc = take_chunk(cache, chunk, &sq, &max_new, &sum);
+  if (rc) return rc;
+  if (Hq <= 0 || Hq % cache->Hkv || !(sm_scale >= 0.f && sm_scale <= 3.0e38f) || !caps_on_device(cache)) return CATEKV_ERR_INVALID_ARG;
+  const int G = Hq / cache->Hkv;
+  if (G > kMaxG || (out_dtype != CATEKV_OUT_BF16 && out_dtype != CATEKV_OUT_FP32)) return CATEKV_ERR_UNSUPPORTED;
+  const int n_segs = cache->B * cache->Hkv;
+  const bool two = ch_two_tiles(G, max_new);
+  const int TB = (two ? 256 : 128) / G;
+  int64_t units = 0;
+  for (int s = 0; s < n_segs; ++s) {
+    const int n = sq.n_new[s / cache->Hkv], len = cache->seg_len[s];
+    if (cache->seg_cap[s] < 0 || cache->seg_cap[s] % CATEKV_SEG_ALIGN || cache->seg_off[s] < 0) return CATEKV_ERR_INVALID_ARG;
+    if (len < n || len > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;  // the chunk's rows are the list's last ones
+    for (int j = 0; j < n; j += TB) units += (len - n + (n < j + TB ? n : j + TB) + kKeyTile - 1) / kKeyTile;
+  }
+  if (sum == 0) return CATEKV_OK;
+  if (units > 0x7fffffff) return CATEKV_ERR_UNSUPPORTED;
+  if (!q || !out || !ws || (((uintptr_t)q | (uintptr_t)out | (uintptr_t)ws) & 15) || ((uintptr_t)lse_out & 3)) return CATEKV_ERR_INVALID_ARG;
+  if ((Hq > 1 && (q_stride_h < kD || q_stride_h % 8)) || (chunk->n_tokens > 1 && (q_stride_t < kD || q_stride_t % 8))) return CATEKV_ERR_UNSUPPORTED;
+  const ChunkWs W = chunk_ws_layout(G, max_new);
+  if (ws_bytes < W.bytes) return CATEKV_ERR_WORKSPACE;
+  CUtensorMap m[5];
+  rc = make_pool_map(cache->k_pool, cache->total_rows, kKeyTile, &m[0]);
+  if (!rc) rc = make_pool_map(cache->v_pool, cache->total_rows, kKeyTile, &m[1]);
+  const catekv_pages* pg = cache->pages;
+  if (!rc) rc = make_pool_map(pg ? pg->k_ovf : cache->k_pool, pg ? (int64_t)pg->n_pages * CATEKV_PAGE_ROWS : cache->total_rows, CATEKV_PAGE_ROWS, &m[2]);
+  if (!rc) rc = make_pool_map(pg ? pg->v_ovf : cache->v_pool, pg ? (int64_t)pg->n_pages * CATEKV_PAGE_ROWS : cache->total_rows, CATEKV_PAGE_ROWS, &m[3]);
+  if (!rc) rc = make_q_map(q, chunk->n_tokens, Hq, G, TB, q_stride_t, q_stride_h, &m[4]);
+  if (rc) return rc;
+  uint8_t* w8 = (uint8_t*)ws;
+  ChunkArgs a = {};
+  a.seg_off = cache->seg_off_dev;
+  a.seg_len = cache->seg_len_dev;
+  a.seg_cap = caps_on_device(cache);
+  a.v_pool = (const uint16_t*)cache->v_pool;
+  if (pg) {
+    a.v_ovf = (const uint16_t*)pg->v_ovf;
+    a.table = pg->table_dev;
+    a.max_pages = pg->max_pages;
+    a.n_pages = pg->n_pages;
+  }
+  a.n_segs = n_segs;
+  a.Hkv = cache->Hkv;
+  a.G = G;
+  a.Hq = Hq;
+  a.TB = TB;
+  a.slot_rows = W.slot_rows;
+  a.scale_log2 = (sm_scale == 0.f ? 1.f / sqrtf((float)kD) : sm_scale) * 1.4426950408889634f;
+  a.out = out;
+  a.lse = lse_out;
+  a.out_fp32 = out_dtype == CATEKV_OUT_FP32;
+  a.desc = (int32_t*)(w8 + W.off_desc);
+  a.part_ml = (float2*)(w8 + W.off_ml);
+  a.part_o = (float*)(w8 + W.off_o);
+  a.status = (int32_t*)w8;
+  a.checked = checked_status_ptr();
+  a.spin_limit = kSpinLimit;
+  if (score_take_expire_launch()) {
+    a.spin_limit = 512;
+    a.idle_producer = 1;
+  }
+  const int ctas = (int)(units < sm_count() ? units : sm_count());
+  cudaStream_t st = (cudaStream_t)stream;
+  rc = two ? launch_chunk<true, 2>(ctas, m, a, sq, st) : launch_chunk<false, 2>(ctas, m, a, sq, st);
+  if (rc) return rc;
+  CATEKV_CUDA_TRY(launch_pdl(chunk_combine_kernel, dim3(ctas, (W.slot_rows + kChCombineRows - 1) / kChCombineRows), dim3(256), 0, st, a, sq, ctas));
+  return CATEKV_OK;
+}

@@ -33,7 +33,7 @@ static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; 
 int sm_count();
 
 // ---- device status block (the first CATEKV_STATUS_BYTES of a workspace, or the checked build's own block) ---
-enum KernelId { kKidScore = 1, kKidTopk = 2, kKidGather = 3, kKidAttention = 4, kKidMeta = 5, kKidEvict = 6 };
+enum KernelId { kKidScore = 1, kKidTopk = 2, kKidGather = 3, kKidAttention = 4, kKidMeta = 5, kKidEvict = 6, kKidChunk = 7 };
 // Device address of the checked build's status block; null in an unchecked library.
 int32_t* checked_status_ptr();
 
