@@ -353,20 +353,26 @@ __global__ void __launch_bounds__(kChThreads, 1)
     __syncwarp();
   } else if (warp == 10) {
     // ================= V tiles with rows that some query of the block does not see
-    uint32_t base = 0, n_item = 0;
+    uint32_t use = 0, n_item = 0;
     bool ok = !a.idle_producer;
     while (ok && walk.next(a, sq, it)) {
       const int n = it.t1 - it.t0;
       const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;                       // rows that every query sees
       const int last = it.g.len - it.g.n_new + min(it.g.n_new, a.TB * (it.blk + 1));     // rows that the last one sees
       bool fresh = true;
+      // every use of the ring is waited for in its order: a wait that skipped one could take the phase before it for its own
+      auto arrived = [&]() {
+        const uint32_t u = use++;
+        return mbar_wait(B(kFull + u % kChStages), (u / kChStages) & 1, s_abort, a.spin_limit);
+      };
+      for (int t = 0; ok && t < min(kLead, n); ++t) ok = arrived();
       for (int t = 0; ok && t < n; ++t) {
-        const int r0 = (it.t0 + t) * kKeyTile;
-        if (r0 + kKeyTile <= first) continue;
-        const uint32_t use = base + min(kLead, n) + t + min(t, max(n - kLead, 0));
-        const int st = use % kChStages;
-        ok = mbar_wait(B(kFull + st), (use / kChStages) & 1, s_abort, a.spin_limit);
-        if (!ok) break;
+        const int r0 = (it.t0 + t) * kKeyTile, st = use % kChStages;
+        if (!(ok = arrived())) break;
+        if (r0 + kKeyTile <= first) {
+          if (t + kLead < n) ok = arrived();
+          continue;
+        }
         if (fresh) {
           // four flags in turn: this block's V tile is in the ring, so the results of the block four before it are out
           if (lane == 0) s_odd[n_item & 3] = 0x7fffffff;
@@ -400,8 +406,8 @@ __global__ void __launch_bounds__(kChThreads, 1)
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kFixed + st));
+        if (t + kLead < n) ok = arrived();
       }
-      base += 2 * n;
       n_item += fresh ? 0 : 1;
     }
     __syncwarp();

@@ -131,6 +131,11 @@ CASES = [
     (3, 2, 2, [128] * 6, [700] * 6, [700, 0, 1], "padded"),
     (4, 3, 5, [0, 128, 256] * 4, [90] * 12, [90, 17, 0, 52], "packed"),
     (1, 1, 6, [0], [600], [600], "packed"),
+    # several tiles and several blocks for every CTA
+    (2, 4, 4, [3000, 2944, 1000, 384], [0, 0, 0, 0], [300, 41], "packed"),
+    (8, 8, 2, [1920], [100], [5, 1, 0, 64, 2, 3, 4, 5], "padded"),
+    (5, 8, 7, [512, 0], [1500], [400, 1, 399, 2, 77], "packed"),
+    (30, 8, 1, [384, 0, 128], [3], [1, 2, 3] * 10, "packed"),
 ]
 
 
