@@ -13,6 +13,8 @@
  *   catekv_decode_attn     Algorithm 1, decoding stage: Attention(q, k, v) over the
  *                          per-head lists ("all" retrieval on adaptive heads)
  *   catekv_q8_*            the hybrid cache held in 8 bits (quantise, append, decode attention)
+ *   catekv_append_chunk, catekv_chunk_attn, catekv_truncate, catekv_fork, catekv_pages_compact
+ *                          several new tokens per sequence over the lists, rows taken back, sequences that share rows
  *   catekv_decode_attn_weighted, catekv_evict
  *                          attention weight accumulated per cached row, and the lists cut to a budget by it
  *
@@ -77,7 +79,8 @@ typedef void* catekv_stream; /* cudaStream_t */
  * Overflow pages of a cache: room for segments to grow past the capacity they were laid out with, without moving
  * what they hold (the paper sizes its caches up front and has no counterpart).  Row r of segment s lives in the
  * cache's own pools while r < seg_cap[s]; beyond that, row seg_cap[s] + 64 p + i is row 64 table[s][p] + i of the
- * overflow pools.  Pages are handed out by catekv_pages_reserve (host bump allocator) and never move or return.
+ * overflow pools.  Pages are handed out by catekv_pages_reserve (the lowest free ones first); they come back, are shared and move by
+ * catekv_truncate, catekv_fork and catekv_pages_compact, and by no other call.  The first seg_pages[s] entries of a table row are in force.
  * All arrays are allocated by the caller; table and table_dev start out filled with -1, seg_pages with 0.
  */
 typedef struct catekv_pages {
@@ -110,7 +113,8 @@ typedef struct catekv_cache {
   catekv_pages* pages;        /* overflow pages, or NULL.  With pages a segment may hold up to
                                  seg_cap + 64 * seg_pages rows; catekv_append, catekv_cache_advance,
                                  catekv_decode_plan, catekv_decode_attn / _partials / _combine / _noalloc,
-                                 catekv_append_decode_attn and catekv_cache_regrow (as the source) follow them;
+                                 catekv_append_decode_attn, catekv_append_chunk, catekv_chunk_attn, catekv_truncate,
+                                 catekv_fork and catekv_cache_regrow (as the source) follow them;
                                  every other call refuses such a cache with CATEKV_ERR_UNSUPPORTED */
   const int32_t* seg_cap_dev; /* device [B*Hkv], copy of seg_cap, or NULL.  Kernels that write rows whose number
                                  is decided on the device (the gather of catekv_retrieve_compact) clamp to it;
@@ -120,7 +124,7 @@ typedef struct catekv_cache {
 
 /*
  * Device status block.  The first CATEKV_STATUS_BYTES of every workspace handed to catekv_select_compact,
- * catekv_head_cv, catekv_retrieve_compact, catekv_retrieve_select and catekv_evict belong to it.  Kernels never trap or assert:
+ * catekv_head_cv, catekv_retrieve_compact, catekv_retrieve_select, catekv_evict and catekv_chunk_attn belong to it.  Kernels never trap or assert:
  * a kernel that cannot do its work records why here and returns, and the context stays usable.
  *   CATEKV_STATUS_WAIT_EXPIRED  a bounded wait of the tensor-core scoring kernel ran out (the CTA freed its tensor
  *                               memory and left); scores, and everything derived from them, are invalid
@@ -129,7 +133,7 @@ typedef struct catekv_cache {
  *   CATEKV_STATUS_INDEX_RANGE   checked build only (catekv_checked_build): a device-produced row index, page or
  *                               list position was outside its segment; the access was clamped into range
  * kernel / segment / index describe the first failure recorded (kernel: 1 scoring, 2 top-k, 3 gather,
- * 4 attention, 5 retrieval metadata, 6 eviction).
+ * 4 attention, 5 retrieval metadata, 6 eviction, 7 chunks of new tokens).
  * catekv_select_compact and catekv_head_cv clear the block when they start.  The retrieval calls never clear it
  * (a replayed CUDA graph accumulates): zero the first CATEKV_STATUS_BYTES of a retrieval workspace once after
  * allocating it, or read it with clear != 0.
@@ -324,9 +328,8 @@ int catekv_cache_advance(catekv_cache* cache, int32_t n_tokens);
 
 /*
  * Paged growth.  Makes sure that every segment can take n_new more rows: segments whose capacity
- * (seg_cap + 64 * seg_pages) is short get further overflow pages, the new table entries are copied to the device
- * on `stream` (from cache->pages->table: leave it untouched until that copy has run).  Host bookkeeping only
- * besides that copy; nothing is launched.  CATEKV_ERR_CAPACITY (nothing changed) if the overflow pools or a
+ * (seg_cap + 64 * seg_pages) is short get further overflow pages, the lowest free ones in the order of the segments; the new table
+ * entries reach the device on `stream`, in a small kernel's arguments.  CATEKV_ERR_CAPACITY (nothing changed) if the overflow pools or a
  * segment's table row run out; CATEKV_ERR_INVALID_ARG if the cache has no pages.  Decode plans built before
  * stay valid.  catekv_cache_regrow with such a cache as the source gathers base rows and pages into one
  * contiguous segment again.
@@ -588,6 +591,36 @@ int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const vo
 size_t catekv_chunk_attn_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t max_new);
 int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* chunk, const void* q, int64_t q_stride_t, int64_t q_stride_h, int32_t Hq,
                       float sm_scale, void* out, int32_t out_dtype, float* lse_out, void* ws, size_t ws_bytes, catekv_stream stream);
+
+/*
+ * Rows taken back: the last n_drop[b] rows (host [B]; as many as there are, if there are fewer; 0 leaves a sequence alone) of every list
+ * of sequence b - drafted tokens that were not accepted, or a sequence that has ended.  Lengths change on the device and in the mirror.  The
+ * pages behind the new ends, reserved ones among them, are free again; their rows stay as they are until a list is given them.
+ * Where a list now ends in rows that another one reads (see catekv_fork), its rows from the last multiple of 128 (in a segment) or 64 (in a
+ * page) on are copied to pages of its own: that takes up to two free pages a list, and in a segment its seg_cap becomes that multiple.
+ * CATEKV_ERR_CAPACITY (nothing changed) if they are not there.  Decode plans are made anew after it, as after an eviction; metadata
+ * and weights of the rows taken back are the caller's.
+ *
+ * Fork: every sequence b with parent[b] != b (host [B]) becomes a continuation of sequence parent[b] as it is when the call is made:
+ * several answers to one prompt, the beams that go on.  What b held before is given up.  Nothing that can be shared is copied: b's lists read
+ * the parent's rows in place up to the last multiple of 128 and its full pages, and only the rows behind (fewer than 128 a list) are copied,
+ * to pages of b's own, where it goes on growing; parent and child grow apart.  The host and device arrays seg_off and seg_cap of b are
+ * written (the descriptor's const is for the other calls): seg_off[b's list] = the parent's, seg_cap = the rows shared in place.  b's own segment
+ * is not used again by b.  Pages that b held alone are given out again in the same call, unless another sequence continues from b.
+ * Rows that are shared must not be rewritten: catekv_evict, catekv_select_compact and the 8-bit and retrieval calls refuse caches with
+ * pages, as they always have; catekv_cache_regrow makes an unshared copy.  Decode plans made before are refused (CATEKV_ERR_INVALID_ARG).
+ * CATEKV_ERR_CAPACITY (nothing changed) if the pages or a table row run out.
+ *
+ * catekv_pages_compact moves the pages in use to the front of the overflow pools (the lowest of those that lie behind goes to the
+ * first free place, and so on), so that the rest can be handed back or the pools cut; *n_used (host, may be NULL) = pages in use.
+ * Lists and plans stay valid.
+ *
+ * All three want exact lengths (CATEKV_ERR_INVALID_ARG if cache->reserved is set), the last two a cache with pages.  They keep the host's tables,
+ * so they cannot be captured in a graph (CATEKV_ERR_UNSUPPORTED).  CATEKV_ERR_WORKSPACE if the host has no memory for their lists.
+ */
+int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catekv_stream stream);
+int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_stream stream);
+int catekv_pages_compact(catekv_cache* cache, int32_t* n_used, catekv_stream stream);
 
 /* ---------------------------------------------------------------- eviction by accumulated attention weight */
 

@@ -144,6 +144,9 @@ def _load():
         "catekv_chunk_attn_workspace_bytes": (sz, [i32, i32, i32]),
         "catekv_chunk_attn": (C.c_int, [C.POINTER(CacheStruct), C.POINTER(ChunkStruct), vp, i64, i64, i32, f32, vp, i32, vp, vp, sz,
                                         vp]),
+        "catekv_truncate": (C.c_int, [C.POINTER(CacheStruct), vp, vp]),
+        "catekv_fork": (C.c_int, [C.POINTER(CacheStruct), vp, vp]),
+        "catekv_pages_compact": (C.c_int, [C.POINTER(CacheStruct), C.POINTER(i32), vp]),
         "catekv_evict_workspace_bytes": (sz, [i32, i32, i32]),
         "catekv_evict_lengths": (C.c_int, [C.POINTER(CacheStruct), vp, i32, i32, i32, vp]),
         "catekv_evict": (C.c_int, [C.POINTER(CacheStruct), vp, vp, i32, i32, i32, C.POINTER(CacheStruct), vp, vp, i64, vp, sz,
@@ -839,3 +842,31 @@ def catekv_chunk_attn(cache: Cache, chunk: Chunk, q: torch.Tensor, out: torch.Te
     if rc != OK:
         raise CatekvError(rc, "catekv_chunk_attn")
     return ws
+
+
+def _per_sequence(where: str, cache: Cache, x) -> np.ndarray:
+    x = np.asarray(x).reshape(-1)
+    if x.size != cache.B:
+        raise CatekvError(ERR_INVALID_ARG, where)
+    _int32(where, *(int(i) for i in x))
+    return np.ascontiguousarray(x, dtype=np.int32)
+
+
+def catekv_truncate(cache: Cache, n_drop):
+    """Take the last n_drop[b] rows off every list of sequence b; pages behind the new ends are free again."""
+    n_drop = _per_sequence("catekv_truncate", cache, n_drop)
+    _check(_lib.catekv_truncate(C.byref(cache.struct), _np_ptr(n_drop), _stream_here("catekv_truncate", cache.k_pool)), "catekv_truncate")
+
+
+def catekv_fork(cache: Cache, parent):
+    """Sequence b continues from sequence parent[b] (itself: stays as it is); rows are shared as far as they can be."""
+    parent = _per_sequence("catekv_fork", cache, parent)
+    _check(_lib.catekv_fork(C.byref(cache.struct), _np_ptr(parent), _stream_here("catekv_fork", cache.k_pool)), "catekv_fork")
+
+
+def catekv_pages_compact(cache: Cache) -> int:
+    """Move the pages in use to the front of the overflow pools.  -> pages in use."""
+    n = C.c_int32(0)
+    _check(_lib.catekv_pages_compact(C.byref(cache.struct), C.byref(n), _stream_here("catekv_pages_compact", cache.k_pool)),
+           "catekv_pages_compact")
+    return n.value

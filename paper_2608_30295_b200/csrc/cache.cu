@@ -1,4 +1,4 @@
-// Growth of the per-head lists: append, the host mirror, overflow pages, the copy into a larger cache; and the
+// Growth of the per-head lists: append, the host mirror, the copy into a larger cache; and the
 // attention-recall diagnostic (Section 3.4).
 #include <math.h>
 
@@ -121,37 +121,6 @@ __global__ void __launch_bounds__(256) regrow_kernel(const uint8_t* sk, const ui
   }
 }
 }  // namespace catekv
-
-extern "C" int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_stream stream) {
-  CATEKV_API_RANGE();
-  int rc = check_cache(cache);
-  if (rc) return rc;
-  if (!cache->pages || n_new < 0) return CATEKV_ERR_INVALID_ARG;
-  catekv_pages* p = cache->pages;
-  const int n = cache->B * cache->Hkv;
-  // first pass: what is needed, nothing changed yet
-  int64_t extra = 0;
-  for (int s = 0; s < n; ++s) {
-    if (cache->seg_len[s] < 0 || cache->seg_len[s] > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;
-    const int64_t over = (int64_t)cache->seg_len[s] + n_new - cache->seg_cap[s];
-    const int64_t want = over > 0 ? (over + CATEKV_PAGE_ROWS - 1) / CATEKV_PAGE_ROWS : 0;
-    if (want > p->max_pages) return CATEKV_ERR_CAPACITY;
-    if (want > p->seg_pages[s]) extra += want - p->seg_pages[s];
-  }
-  if (extra > (int64_t)p->n_pages - p->next_free) return CATEKV_ERR_CAPACITY;
-  for (int s = 0; s < n; ++s) {
-    const int64_t over = (int64_t)cache->seg_len[s] + n_new - cache->seg_cap[s];
-    const int want = over > 0 ? (int)((over + CATEKV_PAGE_ROWS - 1) / CATEKV_PAGE_ROWS) : 0;
-    const int have = p->seg_pages[s];
-    if (want <= have) continue;
-    int32_t* row = p->table + (size_t)s * p->max_pages;
-    for (int q = have; q < want; ++q) row[q] = p->next_free++;
-    p->seg_pages[s] = want;
-    CATEKV_CUDA_TRY(cudaMemcpyAsync(p->table_dev + (size_t)s * p->max_pages + have, row + have,
-                                    sizeof(int32_t) * (size_t)(want - have), cudaMemcpyHostToDevice, (cudaStream_t)stream));
-  }
-  return CATEKV_OK;
-}
 
 extern "C" int catekv_cache_regrow(const catekv_cache* src, catekv_cache* dst, catekv_stream stream) {
   CATEKV_API_RANGE();

@@ -687,6 +687,7 @@ static int decode_launch(int phases, const catekv_cache* cache, const void* k_ne
     return CATEKV_ERR_INVALID_ARG;
   const PlanLayout L = plan_layout(n_segs, hdr->num_ctas);
   if (plan_bytes < L.bytes) return CATEKV_ERR_WORKSPACE;
+  if (cache->pages && hdr->layout != layout_stamp(cache->seg_off, cache->seg_cap, n_segs)) return CATEKV_ERR_INVALID_ARG;  // made before a fork
   size_t off_lse = 0;
   if (ws_bytes < ws_layout(n_segs, hdr->num_ctas, &off_lse)) return CATEKV_ERR_WORKSPACE;
 

@@ -29,7 +29,8 @@ struct PlanHeader {
   int32_t off_cta, off_items, off_seg;  // byte offsets of the three tables
   int32_t max_pieces;                   // most pieces any segment was cut into
   int32_t bounds;                       // made from lengths that were upper bounds (see plan_rows_may_be_new)
-  int32_t reserved[3];
+  uint32_t layout;                      // stamp of the segments' offsets and capacities (layout_stamp)
+  int32_t reserved[2];
 };
 static_assert(sizeof(PlanHeader) == 64, "plan header layout");
 
@@ -75,6 +76,13 @@ static size_t ws_layout(int n_segs, int num_ctas, size_t* off_lse) {
   size_t o = slots * kPartOBytes;
   if (off_lse) *off_lse = o;
   return o + slots * kMaxG * sizeof(float);
+}
+
+// A plan holds its segments' places: catekv_fork and catekv_truncate may change them (caches with overflow pages), and a plan made before is told by this.
+static uint32_t layout_stamp(const int32_t* seg_off, const int32_t* seg_cap, int n_segs) {
+  uint32_t h = 2166136261u;
+  for (int s = 0; s < n_segs; ++s) h = ((h ^ (uint32_t)seg_off[s]) * 16777619u ^ (uint32_t)seg_cap[s]) * 16777619u;
+  return h;
 }
 
 struct PlanSource {  // what a schedule is made from (host arrays)

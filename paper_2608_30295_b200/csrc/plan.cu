@@ -101,6 +101,7 @@ int catekv::build_plan(const PlanSource& p, int32_t num_ctas, int32_t tile, int 
   hdr->off_seg = (int32_t)L.off_seg;
   hdr->max_pieces = max_pieces;
   hdr->bounds = p.bounds;
+  hdr->layout = layout_stamp(p.seg_off, p.seg_cap, n_segs);
   if (plan_dev)
     CATEKV_CUDA_TRY(cudaMemcpyAsync(plan_dev, plan_host, L.bytes, cudaMemcpyHostToDevice, stream));
   return CATEKV_OK;
