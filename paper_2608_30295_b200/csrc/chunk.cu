@@ -10,12 +10,16 @@
 // chunk_combine_kernel merges in the order of the keys.
 //
 // Two streams per CTA, each with its own four softmax warps (a thread owns a query row), its own S / P slot and its own accumulator in
-// tensor memory: with two M tiles a stream is an M tile and both read the same K and V tiles; with one, the streams take
-// alternate key tiles and their accumulators are merged at the end.  While one stream's warps turn S into P, the tensor
-// pipe works for the other.  Per tile: S = Q K^T (tcgen05.mma, both operands in shared memory), the thread reads its row of S
-// (tcgen05.ld), raises its reference when the tile's maximum exceeds it by more than 2^8 (the accumulator is then scaled in tensor
-// memory: rare after the first tiles), writes P = exp2(logit - reference) over S as a bf16 pair hi + lo (both rounded to
-// nearest: 17 significant bits), and O += P_hi V + P_lo V takes P from tensor memory and V as the MN-major operand as TMA left it.
+// tensor memory: with two M tiles a stream is an M tile; with one, the streams take the two halves of every key tile and their
+// accumulators are merged at the end.  While one stream's warps turn S into P, the tensor pipe works for the other.  Per tile:
+// S = Q K^T (tcgen05.mma, both operands in shared memory); the thread reads its row of S (tcgen05.ld), raises its reference when the
+// tile's maximum exceeds it by more than 2^8 (the accumulator is then scaled in tensor memory: rare after the first tiles) and
+// writes P = exp2(logit - reference) over S in kParts bf16 numbers, each the rounded rest of those before it; O += P V takes P
+// from tensor memory and V as the MN-major operand as TMA left it, and starts on the first half of a row's keys while the second is at work.
+//
+// Precision.  kParts = 1: P rounded to bf16 (2^-9), as the result will be: bf16 results with two M tiles, where the products bound the kernel.
+// 2: 17 significant bits; 3: all of fp32's.  The tensor cores add with truncation, about 2^-27 of the accumulator lost per 16-key step;
+// fp32 results (kFlush) therefore have the accumulator added, with rounding, to a sum in memory every kFlush tiles, where the products start from zero.
 //
 // Rows of a V tile that no query of the block sees are zeroed in shared memory before the product reads them (what lies behind a list
 // may be NaN, and 0 * NaN is not 0); an infinity or a NaN in a new row, which later tokens see and earlier ones do not, is taken
@@ -40,10 +44,10 @@ constexpr int kChTileBytes = 128 * 256;  // a [128 x 128] bf16 tile
 constexpr int kChStages = 5;
 constexpr int kChTmemCols = 512;  // S / P slots at columns 0 and 128, O at 256 and 384
 constexpr float kChTau = 8.f;
-constexpr int kChBarriers = 3 * kChStages + 12;
+constexpr int kChBarriers = 3 * kChStages + 14;
 template <bool kQ2>
 constexpr size_t ch_smem_bytes() {
-  return 1024 + (size_t)(kQ2 ? 2 : 1) * kChTileBytes + (size_t)kChStages * kChTileBytes + kChBarriers * 8 + 256 + (kQ2 ? 0 : 2 * 128 * 8);
+  return 1024 + (size_t)(kQ2 ? 2 : 1) * kChTileBytes + (size_t)kChStages * kChTileBytes + kChBarriers * 8 + 256 + (kQ2 ? 0 : 2 * 128 * 16);
 }
 static_assert(ch_smem_bytes<true>() <= 227 * 1024, "chunk_attn_kernel: one CTA's shared memory");
 
@@ -61,13 +65,15 @@ struct ChunkArgs {
   int32_t max_pages, n_pages;
   int32_t n_segs, Hkv, G, Hq;
   int32_t TB;  // tokens of a query block
-  int32_t slot_rows;
+  int32_t R;   // rows of a tile of part_o and part_ml
   float scale_log2;
   void* out;
   float* lse;
   int32_t out_fp32;
-  float* part_o;   // [2 CTAs][slot_rows][128], relative to the row's reference
-  float2* part_ml; // [2 CTAs][slot_rows]: reference (log2 domain), sum
+  // Partial results, four tiles [32 d / 4][R rows] (float4: a warp's rows lie side by side) a CTA.  With two M tiles: tile 2 i + x, i = 0 for the CTA's
+  // first block and 1 for its last; with one: tile i, and tiles 2 and 3 for the streams' sums.  part_ml: reference (log2 domain) and sum of the rows.
+  float4* part_o;
+  float2* part_ml;
   int32_t* desc;   // [CTAs][8]
   int32_t* status;
   int32_t* checked;
@@ -130,42 +136,53 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
 }
-__device__ __forceinline__ float ch_max64(const float (&x)[64]) {
+template <int kN>
+__device__ __forceinline__ float ch_max(const float* x) {
   float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]), m3 = fmax3(x[9], x[10], x[11]);
 #pragma unroll
-  for (int c = 12; c < 60; c += 8) {
+  for (int c = 12; c < kN - 4; c += 8) {
     m0 = fmax3(m0, x[c], x[c + 1]);
     m1 = fmax3(m1, x[c + 2], x[c + 3]);
     m2 = fmax3(m2, x[c + 4], x[c + 5]);
     m3 = fmax3(m3, x[c + 6], x[c + 7]);
   }
-  m0 = fmax3(m0, x[60], x[61]);
-  m1 = fmax3(m1, x[62], x[63]);
+  m0 = fmax3(m0, x[kN - 4], x[kN - 3]);
+  m1 = fmax3(m1, x[kN - 2], x[kN - 1]);
   return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
 }
-// 32 logits -> probabilities of 32 keys as bf16 pairs: hi to `hi`, what is left of them to `lo` (16 columns each); returns their sum
+// two fp32 numbers at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+// 32 logits -> probabilities of 32 keys in kParts bf16 numbers, 16 columns each, `step` columns from part to part; returns their sum
 template <int kParts>
-__device__ __forceinline__ float ch_probs32(const float* x, float scale, float neg_ref, uint32_t hi, uint32_t lo) {
-  float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-  uint32_t ph[16], pl[16];
+__device__ __forceinline__ float ch_probs32(const float* x, float scale, float neg_ref, uint32_t to, uint32_t step) {
+  float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+  uint32_t w[kParts][16];
 #pragma unroll
-  for (int c = 0; c < 32; c += 4) {
-    const float p0 = fast_exp2(fmaf(x[c], scale, neg_ref)), p1 = fast_exp2(fmaf(x[c + 1], scale, neg_ref));
-    const float p2 = fast_exp2(fmaf(x[c + 2], scale, neg_ref)), p3 = fast_exp2(fmaf(x[c + 3], scale, neg_ref));
-    s0 += p0;
-    s1 += p1;
-    s2 += p2;
-    s3 += p3;
-    ph[c / 2] = pack_bf16(p0, p1);
-    ph[c / 2 + 1] = pack_bf16(p2, p3);
-    if (kParts > 1) {
-      pl[c / 2] = pack_bf16(p0 - __uint_as_float(ph[c / 2] << 16), p1 - __uint_as_float(ph[c / 2] & 0xffff0000u));
-      pl[c / 2 + 1] = pack_bf16(p2 - __uint_as_float(ph[c / 2 + 1] << 16), p3 - __uint_as_float(ph[c / 2 + 1] & 0xffff0000u));
+  for (int c = 0; c < 32; c += 2) {
+    float2 p = fma2(make_float2(x[c], x[c + 1]), make_float2(scale, scale), make_float2(neg_ref, neg_ref));
+    p.x = fast_exp2(p.x);
+    p.y = fast_exp2(p.y);
+    if (c & 2) s1 = add2(s1, p);
+    else s0 = add2(s0, p);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      w[k][c / 2] = pack_bf16(p.x, p.y);
+      if (k + 1 < kParts) p = add2(p, make_float2(-__uint_as_float(w[k][c / 2] << 16), -__uint_as_float(w[k][c / 2] & 0xffff0000u)));
     }
   }
-  tmem_st16u(hi, ph);
-  if (kParts > 1) tmem_st16u(lo, pl);
-  return (s0 + s1) + (s2 + s3);
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) tmem_st16u(to + k * step, w[k]);
+  s0 = add2(s0, s1);
+  return s0.x + s0.y;
 }
 
 // pool row of row r of a list, or of its overflow pages (page < 0: not there)
@@ -178,13 +195,16 @@ __device__ __forceinline__ int ch_page(const ChunkArgs& a, int seg, int o) {
   return pg < a.n_pages ? pg : -1;
 }
 
-template <bool kQ2, int kParts>
+template <bool kQ2, int kParts, int kFlush>
 __global__ void __launch_bounds__(kChThreads, 1)
     chunk_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                       const __grid_constant__ CUtensorMap ko_map, const __grid_constant__ CUtensorMap vo_map,
                       const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ChunkArgs a,
                       const __grid_constant__ ChunkSeqs sq) {
-  constexpr int kLead = kQ2 ? 1 : 2;  // K tiles ahead of the V tile in the ring: K_0 .. K_{lead-1}, V_0, K_lead, V_1, ...
+  constexpr int kKeys = kQ2 ? 128 : 64;            // keys of a tile that a stream takes
+  constexpr int kHalves = kQ2 ? 2 : 1;             // P is handed over 64 keys at a time
+  constexpr int kPartCols = kKeys / 2;             // columns of one part of P
+  static_assert(kParts * kPartCols <= 128, "P fits its slot");
   constexpr int kQBytes = (kQ2 ? 2 : 1) * kChTileBytes, kQBlock = kQBytes / 2;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_scan[12 + 4];
@@ -196,10 +216,10 @@ __global__ void __launch_bounds__(kChThreads, 1)
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + kChBarriers);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int* s_odd = reinterpret_cast<int*>(s_tmem + 4);            // [4]: first new row with an infinity or a NaN in V, of the last blocks that had V tiles looked at
-  float2* s_ml = reinterpret_cast<float2*>(s_tmem + 8);       // one M tile: [stream][row] reference and sum
+  float4* s_ml = reinterpret_cast<float4*>((reinterpret_cast<uintptr_t>(s_tmem + 8) + 15) & ~(uintptr_t)15);  // one M tile: [stream][row] reference, sum, reference of the sum in memory
   const uint32_t bar0 = smem_u32(s_bar);
   auto B = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-  constexpr int kFull = 0, kEmpty = kChStages, kFixed = 2 * kChStages, kDoneS = 3 * kChStages, kPReady = kDoneS + 2, kDoneO = kPReady + 2,
+  constexpr int kFull = 0, kEmpty = kChStages, kFixed = 2 * kChStages, kDoneS = 3 * kChStages, kPReady = kDoneS + 2, kDoneO = kPReady + 4,
                 kQFull = kDoneO + 2, kQEmpty = kQFull + 1, kXch = kQEmpty + 1;
   static_assert(kXch + 4 <= kChBarriers, "barrier table");
 
@@ -207,7 +227,7 @@ __global__ void __launch_bounds__(kChThreads, 1)
   if (tid == 0) {
     *s_abort = 0;
     for (int i = 0; i < kChBarriers; ++i) {
-      const int count = (i == kPReady || i == kPReady + 1) ? 4 : (i >= kXch ? 2 : 1);
+      const int count = (i >= kPReady && i < kPReady + 4) ? 4 : (i >= kXch ? 2 : 1);
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(B(i)), "r"(count));
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -296,6 +316,9 @@ __global__ void __launch_bounds__(kChThreads, 1)
   if (walk.left > 0) walk.g = ch_seg(a, sq, walk.seg);
   ChunkItem it;
 
+  // The softmax warps hold a row of S: registers of the other warps go to them (128 x 88 + 256 x 208 = 384 x 168, what the block was launched with).
+  if (warp >= 8) {
+    if (kQ2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
   if (warp == 9) {
     // ================= K and V tiles, in the order in which the tensor pipe uses them
     if (lane == 0 && !a.idle_producer) {
@@ -329,10 +352,10 @@ __global__ void __launch_bounds__(kChThreads, 1)
           }
           return true;
         };
-        for (int t = 0; ok && t < min(kLead, n); ++t) ok = load(&k_map, &ko_map, it.t0 + t);
-        for (int t = 0; ok && t < n; ++t) {
+        ok = load(&k_map, &ko_map, it.t0);
+        for (int t = 0; ok && t < n; ++t) {  // K_0, V_0, K_1, V_1, ...
           ok = load(&v_map, &vo_map, it.t0 + t);
-          if (ok && t + kLead < n) ok = load(&k_map, &ko_map, it.t0 + t + kLead);
+          if (ok && t + 1 < n) ok = load(&k_map, &ko_map, it.t0 + t + 1);
         }
       }
     }
@@ -365,12 +388,12 @@ __global__ void __launch_bounds__(kChThreads, 1)
         const uint32_t u = use++;
         return mbar_wait(B(kFull + u % kChStages), (u / kChStages) & 1, s_abort, a.spin_limit);
       };
-      for (int t = 0; ok && t < min(kLead, n); ++t) ok = arrived();
+      ok = arrived();
       for (int t = 0; ok && t < n; ++t) {
         const int r0 = (it.t0 + t) * kKeyTile, st = use % kChStages;
         if (!(ok = arrived())) break;
         if (r0 + kKeyTile <= first) {
-          if (t + kLead < n) ok = arrived();
+          if (t + 1 < n) ok = arrived();
           continue;
         }
         if (fresh) {
@@ -406,7 +429,7 @@ __global__ void __launch_bounds__(kChThreads, 1)
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kFixed + st));
-        if (t + kLead < n) ok = arrived();
+        if (t + 1 < n) ok = arrived();
       }
       n_item += fresh ? 0 : 1;
     }
@@ -414,85 +437,90 @@ __global__ void __launch_bounds__(kChThreads, 1)
   } else if (warp == 8) {
     // ================= tensor-core issue
     if (lane == 0 && !a.idle_producer) {
-      const uint32_t idesc_s = umma_idesc_bf16(128, 128), idesc_o = umma_idesc_bf16_bmn(128, 128);
+      const uint32_t idesc_s = umma_idesc_bf16(128, kKeys), idesc_o = umma_idesc_bf16_bmn(128, 128);
       const uint64_t dq0 = umma_desc_sw128(s_q), dk0 = umma_desc_sw128(s_ring), dv0 = umma_desc_sw128_mn(s_ring, kKBlockBytes);
       const uint32_t dv_hi = (uint32_t)(dv0 >> 32), dv_lo0 = (uint32_t)dv0;
-      uint32_t use = 0, n_item = 0, fixed = 0;  // fixed: one bit per stage, the parity of its next look
-      uint32_t n_p[2] = {0, 0};
+      uint32_t use = 0, n_item = 0, fixed = 0, n_p = 0;  // fixed: one bit per stage, the parity of its next look
       bool ok = true;
       auto wait_tile = [&]() { return mbar_wait(B(kFull + use % kChStages), (use / kChStages) & 1, s_abort, a.spin_limit); };
-      auto issue_s = [&](int x, int st) {
-        const uint64_t dq = dq0 + (uint64_t)((kQ2 ? x : 0) * (128 * 128 >> 4)), dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4));
+      auto issue_s = [&](int x, int st) {  // the stream's M tile, or its half of the keys
+        const uint64_t dq = dq0 + (uint64_t)(kQ2 ? x * (128 * 128 >> 4) : 0);
+        const uint64_t dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4) + (kQ2 ? 0 : x * (64 * 128 >> 4)));
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
           umma_bf16(tmem + x * 128, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2),
                     dk + (uint64_t)((kk >> 2) * (kKBlockBytes >> 4) + (kk & 3) * 2), idesc_s, kk ? 1u : 0u);
         umma_commit(B(kDoneS + x));
       };
-      auto issue_o = [&](int x, int st, bool fresh) {
-        const uint32_t lo = dv_lo0 + (uint32_t)(st * (kChTileBytes >> 4));
+      auto issue_o = [&](int x, int st, int half, bool fresh) {  // 64 keys
+        const uint32_t lo = dv_lo0 + (uint32_t)(st * (kChTileBytes >> 4) + (kQ2 ? half : x) * (64 * 128 >> 4));
+        const uint32_t p = tmem + x * 128 + half * 32;
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            umma_bf16_ta_lohi(tmem + 256 + x * 128, tmem + x * 128 + part * 64 + kk * 8, lo + (uint32_t)(kk * 128), dv_hi, idesc_o,
-                              (part | kk) ? 1u : (fresh ? 0u : 1u));
+          for (int kk = 0; kk < 4; ++kk)
+            umma_bf16_ta_lohi(tmem + 256 + x * 128, p + part * kPartCols + kk * 8, lo + (uint32_t)(kk * 128), dv_hi, idesc_o,
+                              (part | kk | half) ? 1u : (fresh ? 0u : 1u));
       };
       while (ok && walk.next(a, sq, it)) {
         const int n = it.t1 - it.t0;
         const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;
         if (!(ok = mbar_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit))) break;
         ++n_item;
+        if (!(ok = wait_tile())) break;
         tc_fence_after();
-        for (int t = 0; ok && t < min(kLead, n); ++t) {
-          if (!(ok = wait_tile())) break;
-          tc_fence_after();
+        {
           const int st = use++ % kChStages;
-          issue_s(t, st);
-          if (kQ2) issue_s(1, st);
+          issue_s(0, st);
+          issue_s(1, st);
           umma_commit(B(kEmpty + st));
         }
-        if (ok && n <= kLead) umma_commit(B(kQEmpty));
+        if (n == 1) umma_commit(B(kQEmpty));
         for (int t = 0; ok && t < n; ++t) {
           const bool look = (it.t0 + t + 1) * kKeyTile > first;
-          const bool more = t + kLead < n;
+          const bool more = t + 1 < n, fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
           const int sv = use % kChStages, sk = (use + 1) % kChStages;
 #pragma unroll
-          for (int y = 0; y < (kQ2 ? 2 : 1); ++y) {
-            const int x = kQ2 ? y : (t & 1);
-            if (!(ok = mbar_wait(B(kPReady + x), n_p[x] & 1, s_abort, a.spin_limit))) break;
-            ++n_p[x];
-            if (y == 0) {
-              if (!(ok = wait_tile())) break;
-              if (look) {
-                if (!(ok = mbar_wait(B(kFixed + sv), (fixed >> sv) & 1, s_abort, a.spin_limit))) break;
-                fixed ^= 1u << sv;
+          for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int half = 0; half < kHalves; ++half) {
+              if (!(ok = mbar_wait(B(kPReady + 2 * x + half), n_p & 1, s_abort, a.spin_limit))) break;
+              if (x == 0 && half == 0) {
+                if (!(ok = wait_tile())) break;
+                if (look) {
+                  if (!(ok = mbar_wait(B(kFixed + sv), (fixed >> sv) & 1, s_abort, a.spin_limit))) break;
+                  fixed ^= 1u << sv;
+                }
+                ++use;
               }
-              ++use;
+              tc_fence_after();
+              issue_o(x, sv, half, fresh);
             }
-            tc_fence_after();
-            issue_o(x, sv, t < (kQ2 ? 1 : 2));
-            if (!kQ2 || y == 1) umma_commit(B(kEmpty + sv));
+            if (!ok) break;
+            if (x == 1) umma_commit(B(kEmpty + sv));
             if (more) {
-              if (y == 0) {
+              if (x == 0) {
                 if (!(ok = wait_tile())) break;
                 tc_fence_after();
               }
               issue_s(x, sk);
-              if (!kQ2 || y == 1) {
+              if (x == 1) {
                 umma_commit(B(kEmpty + sk));
                 ++use;
-                if (t + kLead + 1 == n) umma_commit(B(kQEmpty));
+                if (t + 2 == n) umma_commit(B(kQEmpty));
               }
             } else {
               umma_commit(B(kDoneO + x));
             }
           }
+          ++n_p;
         }
       }
     }
     __syncwarp();
+    }
   } else {
+    if (kQ2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
     // ================= softmax: warps 0-3 stream 0, warps 4-7 stream 1; a thread owns a row
     const int x = warp >> 2, quarter = warp & 3;
     const int lane_row = quarter * 32 + lane;
@@ -500,43 +528,73 @@ __global__ void __launch_bounds__(kChThreads, 1)
     const uint32_t slot = tmem + lane_base + x * 128, acc = tmem + lane_base + 256 + x * 128;
     const int row = (kQ2 ? x * 128 : 0) + lane_row;  // row of the block
     const int tok = row / a.G;
-    uint32_t n_s = 0, n_o = 0, n_x = 0, n_item = 0;
+    uint32_t n_s = 0, n_o = 0, n_x = 0, n_odd = 0;
     bool alive = true, first_item = true;
     while (alive && walk.next(a, sq, it)) {
       const int n = it.t1 - it.t0;
-      const int n_mine = kQ2 ? n : (n + 1 - x) / 2;
       const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;
       const int token = it.blk * a.TB + tok;
       const bool valid = tok < a.TB && token < it.g.n_new;
       const int sees = it.g.len - it.g.n_new + token + 1;  // rows that this thread's query sees
       const bool idle = !__any_sync(0xffffffffu, valid);   // no row of the warp is a query: it only keeps the barriers going
-      float ref = -INFINITY, l = 0.f;
-      for (int i = 0; i < n_mine; ++i) {
-        const int t = it.t0 + (kQ2 ? i : 2 * i + x);
+      const int tile = blockIdx.x * 4 + (kQ2 ? 2 * (first_item ? 0 : 1) + x : (first_item ? 0 : 1));  // of partial results
+      float4* const sum = a.part_o + (int64_t)(kQ2 ? tile : blockIdx.x * 4 + 2 + x) * (32 * a.R) + lane_row;
+      first_item = false;
+      float ref = -INFINITY, l = 0.f, sum_ref = -INFINITY;
+      for (int i = 0; i < n; ++i) {
         if (!(alive = mbar_wait(B(kDoneS + x), n_s & 1, s_abort, a.spin_limit))) break;
         ++n_s;
-        if (!idle) {
-          tc_fence_after();
-          float y0[64], y1[64];
-          tmem_ld64(slot, y0);
-          tmem_ld64(slot + 64, y1);
-          tmem_wait_ld64(y0);
-          tmem_wait_ld64(y1);
-          if ((t + 1) * kKeyTile > first) {
-            const int lim = sees - t * kKeyTile;
+        if (idle) {
+          __syncwarp();
+          if (lane == 0) {
 #pragma unroll
-            for (int c = 0; c < 64; ++c) {
-              y0[c] = c < lim ? y0[c] : -INFINITY;
-              y1[c] = c + 64 < lim ? y1[c] : -INFINITY;
+            for (int half = 0; half < kHalves; ++half) mbar_arrive(B(kPReady + 2 * x + half));
+          }
+          continue;
+        }
+        tc_fence_after();
+        const bool fresh = kFlush ? i % max(kFlush, 1) == 0 : i == 0;
+        if (kFlush && fresh && i > 0) {
+          // what the tensor cores have added up since the last time goes to the sum in memory (the products of the tile before are done: the
+          // tensor pipe finished them ahead of this S)
+          const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f;
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            float o[32];
+            float4 m[8];
+            tmem_ld32(acc + c0, o);
+            if (i > kFlush) {
+#pragma unroll
+              for (int c = 0; c < 8; ++c)
+                if (valid) m[c] = sum[(c0 / 4 + c) * a.R];
+            }
+            tmem_wait_ld32(o);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              float4 y = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+              if (i > kFlush) y = make_float4(fmaf(m[c].x, f, y.x), fmaf(m[c].y, f, y.y), fmaf(m[c].z, f, y.z), fmaf(m[c].w, f, y.w));
+              if (valid) sum[(c0 / 4 + c) * a.R] = y;
             }
           }
-          const float mx = fmaxf(ch_max64(y0), ch_max64(y1)) * a.scale_log2;
-          const bool grow = mx > ref + kChTau;  // also the first tile with a visible key
-          const bool rescale = grow && ref > -INFINITY;
-          if (__any_sync(0xffffffffu, rescale)) {
-            // the products of the tile before are done: the tensor pipe finished them ahead of this S
-            const float f = rescale ? fast_exp2(ref - mx) : 1.f;
-            l *= f;
+          sum_ref = ref;
+        }
+        float y[kKeys];
+#pragma unroll
+        for (int c = 0; c < kKeys; c += 64) tmem_ld64(slot + c, *reinterpret_cast<float(*)[64]>(y + c));
+#pragma unroll
+        for (int c = 0; c < kKeys; c += 64) tmem_wait_ld64(*reinterpret_cast<float(*)[64]>(y + c));
+        if ((it.t0 + i + 1) * kKeyTile > first) {
+          const int lim = sees - (it.t0 + i) * kKeyTile - (kQ2 ? 0 : 64 * x);
+#pragma unroll
+          for (int c = 0; c < kKeys; ++c) y[c] = c < lim ? y[c] : -INFINITY;
+        }
+        const float mx = ch_max<kKeys>(y) * a.scale_log2;
+        const bool grow = mx > ref + kChTau;  // also the first tile with a visible key
+        const bool rescale = grow && ref > -INFINITY;
+        if (__any_sync(0xffffffffu, rescale)) {
+          const float f = rescale ? fast_exp2(ref - mx) : 1.f;
+          l *= f;
+          if (!fresh) {
 #pragma unroll 1
             for (int c0 = 0; c0 < 128; c0 += 32) {
               float o[32];
@@ -547,53 +605,51 @@ __global__ void __launch_bounds__(kChThreads, 1)
               tmem_st32(acc + c0, o);
             }
           }
-          if (grow) ref = mx;
-          const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
-          float s = ch_probs32<kParts>(y0, a.scale_log2, neg, slot, slot + 64);
-          s += ch_probs32<kParts>(y0 + 32, a.scale_log2, neg, slot + 16, slot + 80);
-          s += ch_probs32<kParts>(y1, a.scale_log2, neg, slot + 32, slot + 96);
-          s += ch_probs32<kParts>(y1 + 32, a.scale_log2, neg, slot + 48, slot + 112);
-          l += s;
+        }
+        if (grow) ref = mx;
+        const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
+          l += ch_probs32<kParts>(y + half * 64, a.scale_log2, neg, slot + half * 32, kPartCols);
+          l += ch_probs32<kParts>(y + half * 64 + 32, a.scale_log2, neg, slot + half * 32 + 16, kPartCols);
           tmem_wait_st();
           tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(B(kPReady + 2 * x + half));
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(B(kPReady + x));
       }
       if (!alive) break;
-      if (n_mine > 0) {
-        if (!(alive = mbar_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
-        ++n_o;
-      }
+      if (!(alive = mbar_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
+      ++n_o;
       tc_fence_after();
       // ---- the item's result: the whole block, or a piece of it
       const bool looked = it.t1 * kKeyTile > first;
-      const int odd = looked ? s_odd[n_item & 3] : 0x7fffffff;
-      n_item += looked ? 1 : 0;
-      const bool whole = n == it.nt;
+      const int odd = looked ? s_odd[n_odd & 3] : 0x7fffffff;
+      n_odd += looked ? 1 : 0;
+      const bool whole = n == it.nt, summed = kFlush && n > kFlush;
       const int b = it.seg / a.Hkv, h = it.seg - b * a.Hkv;
       const int64_t orow = (int64_t)(sq.start[b] + token) * a.Hq + h * a.G + (row - tok * a.G);
-      const int64_t prow = (int64_t)(2 * blockIdx.x + (first_item ? 0 : 1)) * a.slot_rows + row;
-      first_item = false;
-      float f0 = 1.f, f1 = 0.f, ref_t = ref, l_t = l;
-      bool both = false;
+      float f0 = 1.f, f1 = 0.f, ref_t = ref, l_t = l, fs0 = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f, fs1 = 0.f;
       if (!kQ2) {  // the two streams' halves of the keys; each stream's warps take half of d
-        s_ml[x * 128 + lane_row] = make_float2(ref, l);
+        s_ml[x * 128 + lane_row] = make_float4(ref, l, sum_ref, 0.f);
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kXch + quarter));
         if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
         ++n_x;
         tc_fence_after();
-        const float2 m0 = s_ml[lane_row], m1 = s_ml[128 + lane_row];
+        const float4 m0 = s_ml[lane_row], m1 = s_ml[128 + lane_row];
         ref_t = fmaxf(m0.x, m1.x);
         f0 = m0.x > -INFINITY ? fast_exp2(m0.x - ref_t) : 0.f;
         f1 = m1.x > -INFINITY ? fast_exp2(m1.x - ref_t) : 0.f;
-        l_t = m0.y * f0 + m1.y * f1;
-        both = n > 1;
+        fs0 = m0.z > -INFINITY ? fast_exp2(m0.z - ref_t) : 0.f;
+        fs1 = m1.z > -INFINITY ? fast_exp2(m1.z - ref_t) : 0.f;
+        // a stream whose row has seen nothing adds nothing (or the NaN that it has met)
+        l_t = (m0.x > -INFINITY ? m0.y * f0 : m0.y) + (m1.x > -INFINITY ? m1.y * f1 : m1.y);
       }
       const float inv = whole ? (l_t > 0.f ? 1.f / l_t : (l_t == 0.f ? 0.f : l_t)) : 1.f;  // a NaN stays one
       const int c_lo = kQ2 ? 0 : x * 64, c_hi = kQ2 ? 128 : c_lo + 64;
       const uint32_t acc0 = kQ2 ? acc : tmem + lane_base + 256;
+      const float4* const sum0 = kQ2 ? sum : a.part_o + (int64_t)(blockIdx.x * 4 + 2) * (32 * a.R) + lane_row;
       if (!idle) {
 #pragma unroll 1
         for (int c0 = c_lo; c0 < c_hi; c0 += 32) {
@@ -601,14 +657,27 @@ __global__ void __launch_bounds__(kChThreads, 1)
           tmem_ld32(acc0 + c0, o);
           tmem_wait_ld32(o);
           if (!kQ2) {
+            float o1[32];
+            tmem_ld32(acc0 + 128 + c0, o1);
+            tmem_wait_ld32(o1);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = f0 > 0.f ? o[c] * f0 : 0.f;
-            if (both) {
-              float o1[32];
-              tmem_ld32(acc0 + 128 + c0, o1);
-              tmem_wait_ld32(o1);
+            for (int c = 0; c < 32; ++c) o[c] = fmaf(o[c], f0, o1[c] * f1);
+          }
+          if (summed && valid) {
 #pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] += f1 > 0.f ? o1[c] * f1 : 0.f;
+            for (int c = 0; c < 8; ++c) {
+              const float4 m = sum0[(c0 / 4 + c) * a.R];
+              o[4 * c] = fmaf(m.x, fs0, o[4 * c]);
+              o[4 * c + 1] = fmaf(m.y, fs0, o[4 * c + 1]);
+              o[4 * c + 2] = fmaf(m.z, fs0, o[4 * c + 2]);
+              o[4 * c + 3] = fmaf(m.w, fs0, o[4 * c + 3]);
+              if (!kQ2) {
+                const float4 m1 = sum0[(32 + c0 / 4 + c) * a.R];
+                o[4 * c] = fmaf(m1.x, fs1, o[4 * c]);
+                o[4 * c + 1] = fmaf(m1.y, fs1, o[4 * c + 1]);
+                o[4 * c + 2] = fmaf(m1.z, fs1, o[4 * c + 2]);
+                o[4 * c + 3] = fmaf(m1.w, fs1, o[4 * c + 3]);
+              }
             }
           }
           if (odd < sees && valid) {  // infinities and NaN that were taken out of the V tiles
@@ -629,10 +698,10 @@ __global__ void __launch_bounds__(kChThreads, 1)
           }
           if (valid) {
             if (!whole) {
-              float* dst = a.part_o + prow * kD + c0;
+              float4* dst = a.part_o + (int64_t)tile * (32 * a.R) + lane_row;
 #pragma unroll
-              for (int c = 0; c < 32; c += 4) *reinterpret_cast<float4*>(dst + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
-            } else if (a.out_fp32) {
+              for (int c = 0; c < 8; ++c) dst[(c0 / 4 + c) * a.R] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+            } else if (kFlush) {
               float* dst = reinterpret_cast<float*>(a.out) + orow * kD + c0;
 #pragma unroll
               for (int c = 0; c < 32; c += 4)
@@ -652,7 +721,7 @@ __global__ void __launch_bounds__(kChThreads, 1)
           }
         }
         if (valid && (kQ2 || x == 0)) {
-          if (!whole) a.part_ml[prow] = make_float2(ref_t, l_t);
+          if (!whole) a.part_ml[(int64_t)tile * a.R + lane_row] = make_float2(ref_t, l_t);
           else if (a.lse) a.lse[orow] = l_t == 0.f ? -INFINITY : (ref_t + log2f(l_t)) * 0.6931471805599453f;
         }
       }
@@ -676,9 +745,11 @@ __global__ void __launch_bounds__(kChThreads, 1)
 }
 
 // Merge the pieces of the blocks that several CTAs share, in the order of the keys: CTA c's descriptor says whether its share
-// begins inside a block; the first such CTA of a block has it merged.  A warp per query row; a lane owns four d.
+// begins inside a block; the first such CTA of a block has it merged.  A thread block takes 32 rows (a lane a row, a warp every eighth float4 of
+// d), and writes them through shared memory row by row.
 constexpr int kChCombineRows = 32;
-__global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq, int C) {
+__global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq, int C, int two) {
+  __shared__ float s_o[kChCombineRows][kD + 4];
   pdl_launch_dependents();
   pdl_wait();
   const int c = blockIdx.x;
@@ -692,40 +763,60 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
   if (begin(c - 1) > ub) return;  // an earlier CTA begins inside this block
   int c_end = c + 1;
   while (c_end < C && begin(c_end) < ue) ++c_end;
-  const int head = begin(c - 1) < ub ? 1 : 0;  // slot of the first piece: the last item of CTA c - 1, or its only one
+  const int head = begin(c - 1) < ub ? 1 : 0;  // the first piece: the last block of CTA c - 1, or its only one
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b = seg / a.Hkv, h = seg - b * a.Hkv;
-  for (int i = warp; i < kChCombineRows; i += 8) {
-    const int row = blockIdx.y * kChCombineRows + i, tok = row / a.G, token = blk * a.TB + tok;
-    if (tok >= a.TB || token >= n_new) continue;
-    auto slot = [&](int k) { return (int64_t)(2 * k + (k == c - 1 ? head : 0)) * a.slot_rows + row; };
-    float M = -INFINITY;
-    for (int k = c - 1; k < c_end; ++k) M = fmaxf(M, a.part_ml[slot(k)].x);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float L = 0.f;
+  const int row0 = blockIdx.y * kChCombineRows, row = row0 + lane, x = row0 >> 7;  // row of the block; its M tile
+  if (blk * a.TB + row0 / a.G >= n_new) return;
+  const bool valid = row / a.G < a.TB && blk * a.TB + row / a.G < n_new;
+  auto tile = [&](int k) {
+    const int i = k == c - 1 ? head : 0;
+    return (int64_t)(k * 4 + (two ? 2 * i + x : i));
+  };
+  float M = -INFINITY, L = 0.f;
+  float4 acc[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (valid) {
+    for (int k = c - 1; k < c_end; ++k) M = fmaxf(M, a.part_ml[tile(k) * a.R + (row & 127)].x);
+#pragma unroll 2
     for (int k = c - 1; k < c_end; ++k) {
-      const float2 ml = a.part_ml[slot(k)];
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;  // the row sees none of this piece's keys
-      const float w = ml.x > -INFINITY ? exp2f(ml.x - M) : 1.f;
-      const float4 v = *reinterpret_cast<const float4*>(a.part_o + slot(k) * kD + lane * 4);
-      acc.x += w * v.x;
-      acc.y += w * v.y;
-      acc.z += w * v.z;
-      acc.w += w * v.w;
-      L += w * ml.y;
+      const float2 ml = a.part_ml[tile(k) * a.R + (row & 127)];
+      const float4* p = a.part_o + tile(k) * (32 * a.R) + (row & 127);
+      float4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = p[(warp + 8 * j) * a.R];
+      // a row that sees none of this piece's keys has nothing to add, or the NaN that it has met
+      const float w = ml.x > -INFINITY ? exp2f(ml.x - M) : (ml.y == 0.f ? 0.f : 1.f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[j].x = fmaf(w, v[j].x, acc[j].x);
+        acc[j].y = fmaf(w, v[j].y, acc[j].y);
+        acc[j].z = fmaf(w, v[j].z, acc[j].z);
+        acc[j].w = fmaf(w, v[j].w, acc[j].w);
+      }
+      L = fmaf(w, ml.y, L);
     }
     const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-    const int64_t orow = (int64_t)(sq.start[b] + token) * a.Hq + h * a.G + (row - tok * a.G);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<float4*>(&s_o[lane][(warp + 8 * j) * 4]) = make_float4(acc[j].x * inv, acc[j].y * inv, acc[j].z * inv, acc[j].w * inv);
+  }
+  auto out_row = [&](int i) { return (int64_t)(sq.start[b] + blk * a.TB + i / a.G) * a.Hq + h * a.G + i % a.G; };
+  if (valid && warp == 0 && a.lse) a.lse[out_row(row)] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  __syncthreads();
+  for (int i = warp; i < kChCombineRows; i += 8) {
+    const int tok = (row0 + i) / a.G;
+    if (tok >= a.TB || blk * a.TB + tok >= n_new) break;
+    const float4 v = *reinterpret_cast<const float4*>(&s_o[i][lane * 4]);
     if (a.out_fp32) {
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + orow * kD + lane * 4) =
-          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+      reinterpret_cast<float4*>(a.out)[out_row(row0 + i) * 32 + lane] = v;
     } else {
       uint2 pk;
-      pk.x = pack_bf16(acc.x * inv, acc.y * inv);
-      pk.y = pack_bf16(acc.z * inv, acc.w * inv);
-      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + orow * kD + lane * 4) = pk;
+      pk.x = pack_bf16(v.x, v.y);
+      pk.y = pack_bf16(v.z, v.w);
+      reinterpret_cast<uint2*>(a.out)[out_row(row0 + i) * 32 + lane] = pk;
     }
-    if (lane == 0 && a.lse) a.lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
   }
 }
 
@@ -836,20 +927,19 @@ static const int32_t* caps_on_device(const catekv_cache* c) { return c->pages ? 
 
 struct ChunkWs {
   size_t off_desc, off_ml, off_o, bytes;
-  int slot_rows;
+  int R;
 };
 // one M tile where no sequence has more rows than it holds
 static bool ch_two_tiles(int G, int max_new) { return (int64_t)G * max_new > 128; }
 static ChunkWs chunk_ws_layout(int G, int max_new) {
   ChunkWs w;
-  const int block = ch_two_tiles(G, max_new) ? 256 : 128;
   const int64_t rows = (int64_t)G * max_new;
-  w.slot_rows = rows < block ? (int)rows : block;
-  const size_t ctas = (size_t)sm_count();
+  w.R = rows < 128 ? (int)rows : 128;
+  const size_t tiles = 4 * (size_t)sm_count();
   size_t o = CATEKV_STATUS_BYTES;
-  w.off_desc = o; o = align_up(o + ctas * 8 * sizeof(int32_t), 256);
-  w.off_ml = o; o = align_up(o + 2 * ctas * w.slot_rows * sizeof(float2), 256);
-  w.off_o = o; o = align_up(o + 2 * ctas * w.slot_rows * (size_t)kD * sizeof(float), 256);
+  w.off_desc = o; o = align_up(o + (size_t)sm_count() * 8 * sizeof(int32_t), 256);
+  w.off_ml = o; o = align_up(o + tiles * w.R * sizeof(float2), 256);
+  w.off_o = o; o = align_up(o + tiles * w.R * (size_t)kD * sizeof(float), 256);
   w.bytes = o;
   return w;
 }
@@ -877,16 +967,16 @@ static int make_q_map(const void* q, int n_tokens, int Hq, int G, int TB, int64_
   return r == CUDA_SUCCESS ? CATEKV_OK : CATEKV_ERR_UNSUPPORTED;
 }
 
-template <bool kQ2, int kParts>
+template <bool kQ2, int kParts, int kFlush>
 static int launch_chunk(int ctas, const CUtensorMap* m, const ChunkArgs& a, const ChunkSeqs& sq, cudaStream_t st) {
   static std::atomic<bool> attr_set[64];
   int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ch_smem_bytes<kQ2>()));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts, kFlush>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ch_smem_bytes<kQ2>()));
     if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   }
-  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts>, dim3(ctas), dim3(kChThreads), ch_smem_bytes<kQ2>(), st, m[0], m[1], m[2], m[3], m[4],
+  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts, kFlush>, dim3(ctas), dim3(kChThreads), ch_smem_bytes<kQ2>(), st, m[0], m[1], m[2], m[3], m[4],
                              a, sq));
   return CATEKV_OK;
 }
@@ -1001,14 +1091,14 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   a.G = G;
   a.Hq = Hq;
   a.TB = TB;
-  a.slot_rows = W.slot_rows;
+  a.R = W.R;
   a.scale_log2 = (sm_scale == 0.f ? 1.f / sqrtf((float)kD) : sm_scale) * 1.4426950408889634f;
   a.out = out;
   a.lse = lse_out;
   a.out_fp32 = out_dtype == CATEKV_OUT_FP32;
   a.desc = (int32_t*)(w8 + W.off_desc);
   a.part_ml = (float2*)(w8 + W.off_ml);
-  a.part_o = (float*)(w8 + W.off_o);
+  a.part_o = (float4*)(w8 + W.off_o);
   a.status = (int32_t*)w8;
   a.checked = checked_status_ptr();
   a.spin_limit = kSpinLimit;
@@ -1018,8 +1108,10 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   }
   const int ctas = (int)(units < sm_count() ? units : sm_count());
   cudaStream_t st = (cudaStream_t)stream;
-  rc = two ? launch_chunk<true, 2>(ctas, m, a, sq, st) : launch_chunk<false, 2>(ctas, m, a, sq, st);
+  if (a.out_fp32) rc = two ? launch_chunk<true, 2, 4>(ctas, m, a, sq, st) : launch_chunk<false, 3, 8>(ctas, m, a, sq, st);
+  else rc = two ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st) : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
   if (rc) return rc;
-  CATEKV_CUDA_TRY(launch_pdl(chunk_combine_kernel, dim3(ctas, (W.slot_rows + kChCombineRows - 1) / kChCombineRows), dim3(256), 0, st, a, sq, ctas));
+  CATEKV_CUDA_TRY(launch_pdl(chunk_combine_kernel, dim3(ctas, ((two ? 256 : W.R) + kChCombineRows - 1) / kChCombineRows), dim3(256), 0, st, a, sq, ctas,
+                             two ? 1 : 0));
   return CATEKV_OK;
 }

@@ -149,7 +149,7 @@ def test_drafted_tokens_are_verified_and_taken_back(ck):
         assert ck.catekv_workspace_status(ck.catekv_chunk_attn(m.cache, chunk, q, out, lse))["flags"] == 0
         rows = [[x.double() for x in kv] for kv in m.lists]
         start = [sum(n_new[:b]) for b in range(B)]
-        check(out, *reference(rows, q, n_new, start, Hkv, D ** -0.5)[:1], lse, reference(rows, q, n_new, start, Hkv, D ** -0.5)[1], 3.0)
+        check(out, lse, reference(rows, q, n_new, start, Hkv, D ** -0.5), 3.0)
         m.truncate([n - a for n, a in zip(n_new, accepted)])
         m.verify()
     ck.catekv_pages_compact(m.cache)
@@ -159,7 +159,7 @@ def test_drafted_tokens_are_verified_and_taken_back(ck):
     out, lse = torch.zeros(q.shape, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
     ck.catekv_decode_attn(m.cache, q, plan, out, lse)
     rows = [[x.double() for x in kv] for kv in m.lists]
-    check(out, *reference(rows, q, [1] * B, list(range(B)), Hkv, D ** -0.5)[:1], lse, reference(rows, q, [1] * B, list(range(B)), Hkv, D ** -0.5)[1], 3.0)
+    check(out, lse, reference(rows, q, [1] * B, list(range(B)), Hkv, D ** -0.5), 3.0)
     m.fork([1, 1, 1])
     with pytest.raises(ck.CatekvError) as e:  # a plan holds the places of the lists that the fork has changed
         ck.catekv_decode_attn(m.cache, q, plan, out, lse)
