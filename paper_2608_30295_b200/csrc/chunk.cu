@@ -9,13 +9,13 @@
 // (a captured call follows lists that grow).  A block that several CTAs share leaves partial results, which
 // chunk_combine_kernel merges in the order of the keys.
 //
-// Two streams per CTA, each with its own four softmax warps (a thread owns a query row), its own S / P slot and its own accumulator in
-// tensor memory: with two M tiles a stream is an M tile; with one, the streams take the two halves of every key tile and their
-// accumulators are merged at the end.  While one stream's warps turn S into P, the tensor pipe works for the other.  Per tile:
-// S = Q K^T (tcgen05.mma, both operands in shared memory); the thread reads its row of S (tcgen05.ld), raises its reference when the
-// tile's maximum exceeds it by more than 2^8 (the accumulator is then scaled in tensor memory: rare after the first tiles) and
-// writes P = exp2(logit - reference) over S in kParts bf16 numbers, each the rounded rest of those before it; O += P V takes P
-// from tensor memory and V as the MN-major operand as TMA left it, and starts on the first half of a row's keys while the second is at work.
+// Per tile: S = Q K^T (tcgen05.mma, both operands in shared memory); a softmax thread owns a query row: it reads it (tcgen05.ld), raises
+// its reference when the tile's maximum exceeds it by more than 2^8 (the accumulator is then scaled in tensor memory: rare after the
+// first tiles) and writes P = exp2(logit - reference) over S in kParts bf16 numbers, each the rounded rest of those before it; O += P V
+// takes P from tensor memory and V as the MN-major operand as TMA left it, and starts on the first 64 keys while the others are at work.
+// What keeps the tensor pipe busy meanwhile: with two M tiles (bound by the products) each is a stream with softmax warps, an S / P slot and
+// an accumulator of its own, and one's products run beside the other's softmax; with one (bound by the stream of K and V)
+// there are two slots, and S of the next tile is formed ahead.
 //
 // Precision.  kParts = 1: P rounded to bf16 (2^-9), as the result will be: bf16 results with two M tiles, where the products bound the kernel.
 // 2: 17 significant bits; 3: all of fp32's.  The tensor cores add with truncation, about 2^-27 of the accumulator lost per 16-key step;
@@ -25,8 +25,8 @@
 // may be NaN, and 0 * NaN is not 0); an infinity or a NaN in a new row, which later tokens see and earlier ones do not, is taken
 // out there too and added to the rows that see it at the end.
 //
-// Warps: 0-3 and 4-7 softmax of the two streams, 8 tensor-core issue, 9 K / V tiles by TMA into one ring in the order of use,
-// 10 the V tiles that need a look, 11 the query block.  Every wait is bounded; a CTA whose wait runs out frees its tensor memory, records
+// Warps: four per M tile for the softmax; then one each for tensor-core issue, K / V tiles by TMA into one ring in the order of use,
+// the V tiles that need a look, and the query block.  Every wait is bounded; a CTA whose wait runs out frees its tensor memory, records
 // CATEKV_STATUS_WAIT_EXPIRED and returns.
 #include <math.h>
 
@@ -39,17 +39,24 @@
 namespace catekv {
 
 constexpr int kChMaxSeqs = 512;  // sequences of a call: their counts travel in the kernel's arguments
-constexpr int kChThreads = 12 * 32;
 constexpr int kChTileBytes = 128 * 256;  // a [128 x 128] bf16 tile
-constexpr int kChStages = 5;
-constexpr int kChTmemCols = 512;  // S / P slots at columns 0 and 128, O at 256 and 384
+constexpr int kChTmemCols = 512;         // two M tiles: slots of S / P at columns 0 and 128, O at 256 and 384; one: slots at 0 and 192, O at 384
 constexpr float kChTau = 8.f;
-constexpr int kChBarriers = 3 * kChStages + 14;
+constexpr int kChBarriers = 32;
 template <bool kQ2>
-constexpr size_t ch_smem_bytes() {
-  return 1024 + (size_t)(kQ2 ? 2 : 1) * kChTileBytes + (size_t)kChStages * kChTileBytes + kChBarriers * 8 + 256 + (kQ2 ? 0 : 2 * 128 * 16);
-}
-static_assert(ch_smem_bytes<true>() <= 227 * 1024, "chunk_attn_kernel: one CTA's shared memory");
+struct ChunkShape {
+  static constexpr int kTiles = kQ2 ? 2 : 1;        // M tiles
+  static constexpr int kStages = kQ2 ? 5 : 6;
+  static constexpr int kSoft = 4 * kTiles;          // softmax warps
+  static constexpr int kWarps = kSoft + 4, kThreads = kWarps * 32;
+  static constexpr int kSlots = 2, kSlotCols = kQ2 ? 128 : 192;
+  static constexpr int kLead = kQ2 ? 1 : 2;         // K tiles ahead of the V tile in the ring: K_0 .. K_{lead-1}, V_0, K_lead, V_1, ...
+  static constexpr size_t kSmem = 1024 + (size_t)(kTiles + kStages) * kChTileBytes + kChBarriers * 8 + 64;
+};
+static_assert(ChunkShape<true>::kSmem <= 226 * 1024 && ChunkShape<false>::kSmem <= 227 * 1024, "chunk_attn_kernel: one CTA's shared memory");
+// A block costs a CTA more than its tiles (its queries, a pipeline that fills and drains, its results): this many tiles are charged for it when the
+// shares are cut.
+constexpr int kChCharge = 2;
 
 struct ChunkSeqs {  // host counts of every sequence
   int32_t n_new[kChMaxSeqs];
@@ -70,8 +77,8 @@ struct ChunkArgs {
   void* out;
   float* lse;
   int32_t out_fp32;
-  // Partial results, four tiles [32 d / 4][R rows] (float4: a warp's rows lie side by side) a CTA.  With two M tiles: tile 2 i + x, i = 0 for the CTA's
-  // first block and 1 for its last; with one: tile i, and tiles 2 and 3 for the streams' sums.  part_ml: reference (log2 domain) and sum of the rows.
+  // Partial results, two tiles a stream [32 d / 4][R rows] (float4: a warp's rows lie side by side) a CTA.  With two M tiles: tile 2 i + x, i = 0 for the CTA's
+  // first block and 1 for its last; with one: tile i.  part_ml: reference (log2 domain) and sum of the rows.
   float4* part_o;
   float2* part_ml;
   int32_t* desc;   // [CTAs][8]
@@ -98,13 +105,16 @@ __device__ __forceinline__ int ch_tiles(const ChunkArgs& a, const ChunkSeg& g, i
   return max(1, (seen + kKeyTile - 1) / kKeyTile);
 }
 
+// a position among a block's units (the charge, then its tiles) -> its tile
+__device__ __forceinline__ int ch_tile_at(int p) { return max(0, p - kChCharge); }
+
 struct ChunkItem {
   int32_t seg, blk, t0, t1, nt;  // tiles [t0, t1) of the block's nt
   ChunkSeg g;
 };
 // The items of a CTA, one after the other; every role walks them by itself.
 struct ChunkWalk {
-  int32_t left, seg, blk, t;
+  int32_t left, seg, blk, p;  // units left; the next block and the position in it
   ChunkSeg g;
   __device__ __forceinline__ bool next(const ChunkArgs& a, const ChunkSeqs& sq, ChunkItem& it) {
     if (left <= 0) return false;
@@ -116,13 +126,14 @@ struct ChunkWalk {
     it.seg = seg;
     it.blk = blk;
     it.nt = ch_tiles(a, g, blk);
-    it.t0 = t;
-    it.t1 = min(it.nt, t + left);
+    const int end = min(it.nt + kChCharge, p + left);
+    it.t0 = ch_tile_at(p);
+    it.t1 = ch_tile_at(end);
     it.g = g;
-    left -= it.t1 - it.t0;
-    t = 0;
+    left -= end - p;
+    p = 0;
     ++blk;
-    return true;
+    return it.t1 > it.t0;  // (a share that ends inside a block's charge ends there)
   }
 };
 
@@ -196,43 +207,42 @@ __device__ __forceinline__ int ch_page(const ChunkArgs& a, int seg, int o) {
 }
 
 template <bool kQ2, int kParts, int kFlush>
-__global__ void __launch_bounds__(kChThreads, 1)
+__global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
     chunk_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                       const __grid_constant__ CUtensorMap ko_map, const __grid_constant__ CUtensorMap vo_map,
                       const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ChunkArgs a,
                       const __grid_constant__ ChunkSeqs sq) {
-  constexpr int kKeys = kQ2 ? 128 : 64;            // keys of a tile that a stream takes
-  constexpr int kHalves = kQ2 ? 2 : 1;             // P is handed over 64 keys at a time
-  constexpr int kPartCols = kKeys / 2;             // columns of one part of P
-  static_assert(kParts * kPartCols <= 128, "P fits its slot");
-  constexpr int kQBytes = (kQ2 ? 2 : 1) * kChTileBytes, kQBlock = kQBytes / 2;
+  using Sh = ChunkShape<kQ2>;
+  constexpr int kStages = Sh::kStages, kTiles = Sh::kTiles, kLead = Sh::kLead, kSoft = Sh::kSoft, kWarps = Sh::kWarps;
+  constexpr int kQBytes = kTiles * kChTileBytes, kQBlock = kQBytes / 2;
+  constexpr int kOCol = kQ2 ? 256 : 384;
+  static_assert(kParts * 64 <= Sh::kSlotCols, "P fits its slot");
   extern __shared__ uint8_t smem_raw[];
-  __shared__ int s_scan[12 + 4];
+  __shared__ int s_scan[kWarps + 4];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (s_base - smem_u32(smem_raw));
   const uint32_t s_q = s_base, s_ring = s_base + kQBytes;
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(smem + kQBytes + kChStages * kChTileBytes);
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(smem + kQBytes + kStages * kChTileBytes);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + kChBarriers);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  int* s_odd = reinterpret_cast<int*>(s_tmem + 4);            // [4]: first new row with an infinity or a NaN in V, of the last blocks that had V tiles looked at
-  float4* s_ml = reinterpret_cast<float4*>((reinterpret_cast<uintptr_t>(s_tmem + 8) + 15) & ~(uintptr_t)15);  // one M tile: [stream][row] reference, sum, reference of the sum in memory
+  int* s_odd = reinterpret_cast<int*>(s_tmem + 4);  // [4]: first new row with an infinity or a NaN in V, of the last blocks that had V tiles looked at
   const uint32_t bar0 = smem_u32(s_bar);
   auto B = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-  constexpr int kFull = 0, kEmpty = kChStages, kFixed = 2 * kChStages, kDoneS = 3 * kChStages, kPReady = kDoneS + 2, kDoneO = kPReady + 4,
-                kQFull = kDoneO + 2, kQEmpty = kQFull + 1, kXch = kQEmpty + 1;
-  static_assert(kXch + 4 <= kChBarriers, "barrier table");
+  constexpr int kFull = 0, kEmpty = kStages, kFixed = 2 * kStages, kDoneS = 3 * kStages, kPReady = kDoneS + 2, kDoneO = kPReady + 4,
+                kDonePV = kDoneO + 2, kQFull = kDonePV + 1, kQEmpty = kQFull + 1;
+  static_assert(kQEmpty < kChBarriers, "barrier table");
 
   pdl_launch_dependents();
   if (tid == 0) {
     *s_abort = 0;
     for (int i = 0; i < kChBarriers; ++i) {
-      const int count = (i >= kPReady && i < kPReady + 4) ? 4 : (i >= kXch ? 2 : 1);
+      const int count = (i >= kPReady && i < kPReady + 4) ? 4 : 1;
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(B(i)), "r"(count));
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == kSoft) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(s_tmem)), "r"(kChTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
@@ -241,34 +251,32 @@ __global__ void __launch_bounds__(kChThreads, 1)
   // ---- this CTA's share of the tiles of all blocks
   int total = 0, u0 = 0, u1 = 0;
   {
-    int mine = 0;
-    for (int s = tid; s < a.n_segs; s += kChThreads) {
+    auto cost_of = [&](int s) {
       const ChunkSeg g = ch_seg(a, sq, s);
-      for (int j = 0; j < g.n_blk; ++j) mine += ch_tiles(a, g, j);
-    }
+      int c = 0;
+      for (int j = 0; j < g.n_blk; ++j) c += ch_tiles(a, g, j) + kChCharge;
+      return c;
+    };
+    int mine = 0;
+    for (int s = tid; s < a.n_segs; s += Sh::kThreads) mine += cost_of(s);
     int x = mine;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     if (lane == 0) s_scan[warp] = x;
-    if (tid == 0) s_scan[12] = a.n_segs;  // no tile: nothing to do
+    if (tid == 0) s_scan[kWarps] = a.n_segs;  // no tile: nothing to do
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 12; ++w) total += s_scan[w];
+    for (int w = 0; w < kWarps; ++w) total += s_scan[w];
     const int C = gridDim.x, c = blockIdx.x, q = total / C, r = total % C;
     u0 = c * q + min(c, r);
     u1 = u0 + q + (c < r ? 1 : 0);
+    if (tid == 0) a.desc[c * 8 + 2] = 0;  // (no cut at the start of a share, unless there is one)
     int before = 0;
-    for (int s0 = 0; s0 < a.n_segs; s0 += kChThreads) {
+    for (int s0 = 0; s0 < a.n_segs; s0 += Sh::kThreads) {
       __syncthreads();
       const int s = s0 + tid;
-      ChunkSeg g = {0, 0, 0};
       int cost = 0;
-      if (s < a.n_segs) {
-        g = ch_seg(a, sq, s);
-        if (a.n_segs <= kChThreads) cost = mine;
-        else
-          for (int j = 0; j < g.n_blk; ++j) cost += ch_tiles(a, g, j);
-      }
+      if (s < a.n_segs) cost = a.n_segs <= Sh::kThreads ? mine : cost_of(s);
       int inc = cost;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -279,29 +287,29 @@ __global__ void __launch_bounds__(kChThreads, 1)
       __syncthreads();
       int ex = before + inc - cost;
 #pragma unroll
-      for (int w = 0; w < 12; ++w) {
+      for (int w = 0; w < kWarps; ++w) {
         ex += w < warp ? s_scan[w] : 0;
         before += s_scan[w];
       }
       if (u1 > u0 && u0 >= ex && u0 < ex + cost) {
-        int t = u0 - ex, j = 0, nt = ch_tiles(a, g, 0);
-        while (t >= nt) {
-          t -= nt;
+        const ChunkSeg g = ch_seg(a, sq, s);
+        int p = u0 - ex, j = 0, nt = ch_tiles(a, g, 0);
+        while (p >= nt + kChCharge) {
+          p -= nt + kChCharge;
           nt = ch_tiles(a, g, ++j);
         }
-        s_scan[12] = s;
-        s_scan[13] = j;
-        s_scan[14] = t;
-        int32_t* d = a.desc + blockIdx.x * 8;
+        s_scan[kWarps] = s;
+        s_scan[kWarps + 1] = j;
+        s_scan[kWarps + 2] = p;
+        int32_t* d = a.desc + c * 8;
         d[0] = s;
         d[1] = j;
-        d[2] = t;
+        d[2] = p;
         d[3] = nt;
         d[4] = g.n_new;
         d[5] = total;
       }
     }
-    if (u1 <= u0 && tid == 0) a.desc[blockIdx.x * 8 + 2] = 0;  // no share: no cut at its start
   }
   tc_fence_before();
   __syncthreads();
@@ -309,17 +317,17 @@ __global__ void __launch_bounds__(kChThreads, 1)
   const uint32_t tmem = *s_tmem;
   ChunkWalk walk;
   walk.left = u1 - u0;
-  walk.seg = s_scan[12];
-  walk.blk = s_scan[13];
-  walk.t = s_scan[14];
+  walk.seg = s_scan[kWarps];
+  walk.blk = s_scan[kWarps + 1];
+  walk.p = s_scan[kWarps + 2];
   walk.g = ChunkSeg{0, 0, 0};
   if (walk.left > 0) walk.g = ch_seg(a, sq, walk.seg);
   ChunkItem it;
 
   // The softmax warps hold a row of S: registers of the other warps go to them (128 x 88 + 256 x 208 = 384 x 168, what the block was launched with).
-  if (warp >= 8) {
+  if (warp >= kSoft) {
     if (kQ2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
-  if (warp == 9) {
+  if (warp == kSoft + 1) {
     // ================= K and V tiles, in the order in which the tensor pipe uses them
     if (lane == 0 && !a.idle_producer) {
       uint32_t use = 0;
@@ -328,8 +336,8 @@ __global__ void __launch_bounds__(kChThreads, 1)
         const int n = it.t1 - it.t0;
         const int off = a.seg_off[it.seg], cap = a.seg_cap[it.seg];
         auto load = [&](const CUtensorMap* pool, const CUtensorMap* ovf, int t) {
-          const int st = use % kChStages;
-          if (use >= kChStages && !mbar_wait(B(kEmpty + st), ((use / kChStages) - 1) & 1, s_abort, a.spin_limit)) return false;
+          const int st = use % kStages;
+          if (use >= kStages && !mbar_wait(B(kEmpty + st), ((use / kStages) - 1) & 1, s_abort, a.spin_limit)) return false;
           ++use;
           const int r0 = t * kKeyTile;
           const uint32_t dst = s_ring + st * kChTileBytes, bar = B(kFull + st);
@@ -352,15 +360,15 @@ __global__ void __launch_bounds__(kChThreads, 1)
           }
           return true;
         };
-        ok = load(&k_map, &ko_map, it.t0);
-        for (int t = 0; ok && t < n; ++t) {  // K_0, V_0, K_1, V_1, ...
+        for (int t = 0; ok && t < min(kLead, n); ++t) ok = load(&k_map, &ko_map, it.t0 + t);
+        for (int t = 0; ok && t < n; ++t) {
           ok = load(&v_map, &vo_map, it.t0 + t);
-          if (ok && t + 1 < n) ok = load(&k_map, &ko_map, it.t0 + t + 1);
+          if (ok && t + kLead < n) ok = load(&k_map, &ko_map, it.t0 + t + kLead);
         }
       }
     }
     __syncwarp();
-  } else if (warp == 11) {
+  } else if (warp == kSoft + 3) {
     // ================= the query block of every item
     if (lane == 0 && !a.idle_producer) {
       uint32_t n_item = 0;
@@ -374,7 +382,7 @@ __global__ void __launch_bounds__(kChThreads, 1)
       }
     }
     __syncwarp();
-  } else if (warp == 10) {
+  } else if (warp == kSoft + 2) {
     // ================= V tiles with rows that some query of the block does not see
     uint32_t use = 0, n_item = 0;
     bool ok = !a.idle_producer;
@@ -386,14 +394,14 @@ __global__ void __launch_bounds__(kChThreads, 1)
       // every use of the ring is waited for in its order: a wait that skipped one could take the phase before it for its own
       auto arrived = [&]() {
         const uint32_t u = use++;
-        return mbar_wait(B(kFull + u % kChStages), (u / kChStages) & 1, s_abort, a.spin_limit);
+        return mbar_wait(B(kFull + u % kStages), (u / kStages) & 1, s_abort, a.spin_limit);
       };
-      ok = arrived();
+      for (int t = 0; ok && t < min(kLead, n); ++t) ok = arrived();
       for (int t = 0; ok && t < n; ++t) {
-        const int r0 = (it.t0 + t) * kKeyTile, st = use % kChStages;
+        const int r0 = (it.t0 + t) * kKeyTile, st = use % kStages;
         if (!(ok = arrived())) break;
         if (r0 + kKeyTile <= first) {
-          if (t + 1 < n) ok = arrived();
+          if (t + kLead < n) ok = arrived();
           continue;
         }
         if (fresh) {
@@ -429,37 +437,36 @@ __global__ void __launch_bounds__(kChThreads, 1)
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kFixed + st));
-        if (t + 1 < n) ok = arrived();
+        if (t + kLead < n) ok = arrived();
       }
       n_item += fresh ? 0 : 1;
     }
     __syncwarp();
-  } else if (warp == 8) {
+  } else if (warp == kSoft) {
     // ================= tensor-core issue
     if (lane == 0 && !a.idle_producer) {
-      const uint32_t idesc_s = umma_idesc_bf16(128, kKeys), idesc_o = umma_idesc_bf16_bmn(128, 128);
+      const uint32_t idesc_s = umma_idesc_bf16(128, 128), idesc_o = umma_idesc_bf16_bmn(128, 128);
       const uint64_t dq0 = umma_desc_sw128(s_q), dk0 = umma_desc_sw128(s_ring), dv0 = umma_desc_sw128_mn(s_ring, kKBlockBytes);
       const uint32_t dv_hi = (uint32_t)(dv0 >> 32), dv_lo0 = (uint32_t)dv0;
-      uint32_t use = 0, n_item = 0, fixed = 0, n_p = 0;  // fixed: one bit per stage, the parity of its next look
+      uint32_t use = 0, n_item = 0, fixed = 0, n_s = 0, n_p = 0;  // fixed: one bit per stage, the parity of its next look
       bool ok = true;
-      auto wait_tile = [&]() { return mbar_wait(B(kFull + use % kChStages), (use / kChStages) & 1, s_abort, a.spin_limit); };
-      auto issue_s = [&](int x, int st) {  // the stream's M tile, or its half of the keys
-        const uint64_t dq = dq0 + (uint64_t)(kQ2 ? x * (128 * 128 >> 4) : 0);
-        const uint64_t dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4) + (kQ2 ? 0 : x * (64 * 128 >> 4)));
+      auto wait_tile = [&]() { return mbar_wait(B(kFull + use % kStages), (use / kStages) & 1, s_abort, a.spin_limit); };
+      auto issue_s = [&](int x, int slot, int st) {  // M tile x
+        const uint64_t dq = dq0 + (uint64_t)(x * (128 * 128 >> 4)), dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4));
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
-          umma_bf16(tmem + x * 128, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2),
+          umma_bf16(tmem + slot * Sh::kSlotCols, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2),
                     dk + (uint64_t)((kk >> 2) * (kKBlockBytes >> 4) + (kk & 3) * 2), idesc_s, kk ? 1u : 0u);
-        umma_commit(B(kDoneS + x));
+        umma_commit(B(kDoneS + slot));
       };
-      auto issue_o = [&](int x, int st, int half, bool fresh) {  // 64 keys
-        const uint32_t lo = dv_lo0 + (uint32_t)(st * (kChTileBytes >> 4) + (kQ2 ? half : x) * (64 * 128 >> 4));
-        const uint32_t p = tmem + x * 128 + half * 32;
+      auto issue_o = [&](int x, int slot, int st, int half, bool fresh) {  // 64 keys
+        const uint32_t lo = dv_lo0 + (uint32_t)(st * (kChTileBytes >> 4) + half * (64 * 128 >> 4));
+        const uint32_t p = tmem + slot * Sh::kSlotCols + half * 32;
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            umma_bf16_ta_lohi(tmem + 256 + x * 128, p + part * kPartCols + kk * 8, lo + (uint32_t)(kk * 128), dv_hi, idesc_o,
+            umma_bf16_ta_lohi(tmem + kOCol + x * 128, p + part * 64 + kk * 8, lo + (uint32_t)(kk * 128), dv_hi, idesc_o,
                               (part | kk | half) ? 1u : (fresh ? 0u : 1u));
       };
       while (ok && walk.next(a, sq, it)) {
@@ -467,24 +474,29 @@ __global__ void __launch_bounds__(kChThreads, 1)
         const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;
         if (!(ok = mbar_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit))) break;
         ++n_item;
-        if (!(ok = wait_tile())) break;
-        tc_fence_after();
-        {
-          const int st = use++ % kChStages;
-          issue_s(0, st);
-          issue_s(1, st);
+        for (int t = 0; t < min(kLead, n); ++t) {
+          if (!(ok = wait_tile())) break;
+          tc_fence_after();
+          const int st = use++ % kStages;
+          if (kQ2) {
+            issue_s(0, 0, st);
+            issue_s(1, 1, st);
+          } else {
+            issue_s(0, n_s++ & 1, st);
+          }
           umma_commit(B(kEmpty + st));
         }
-        if (n == 1) umma_commit(B(kQEmpty));
+        if (n <= kLead) umma_commit(B(kQEmpty));
         for (int t = 0; ok && t < n; ++t) {
           const bool look = (it.t0 + t + 1) * kKeyTile > first;
-          const bool more = t + 1 < n, fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
-          const int sv = use % kChStages, sk = (use + 1) % kChStages;
+          const bool more = t + kLead < n, fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
+          const int sv = use % kStages, sk = (use + 1) % kStages;
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
+          for (int x = 0; x < kTiles; ++x) {
+            const int slot = kQ2 ? x : (int)(n_p & 1);
 #pragma unroll
-            for (int half = 0; half < kHalves; ++half) {
-              if (!(ok = mbar_wait(B(kPReady + 2 * x + half), n_p & 1, s_abort, a.spin_limit))) break;
+            for (int half = 0; half < 2; ++half) {
+              if (!(ok = mbar_wait(B(kPReady + 2 * slot + half), (kQ2 ? n_p : n_p >> 1) & 1, s_abort, a.spin_limit))) break;
               if (x == 0 && half == 0) {
                 if (!(ok = wait_tile())) break;
                 if (look) {
@@ -494,26 +506,27 @@ __global__ void __launch_bounds__(kChThreads, 1)
                 ++use;
               }
               tc_fence_after();
-              issue_o(x, sv, half, fresh);
+              issue_o(x, slot, sv, half, fresh);
             }
             if (!ok) break;
-            if (x == 1) umma_commit(B(kEmpty + sv));
+            if (!kQ2) umma_commit(B(kDonePV));
+            if (x == kTiles - 1) umma_commit(B(kEmpty + sv));
             if (more) {
               if (x == 0) {
                 if (!(ok = wait_tile())) break;
                 tc_fence_after();
               }
-              issue_s(x, sk);
-              if (x == 1) {
+              issue_s(x, slot, sk);  // into the slot whose P has just been taken: the tensor pipe keeps issue order
+              if (x == kTiles - 1) {
                 umma_commit(B(kEmpty + sk));
                 ++use;
-                if (t + 2 == n) umma_commit(B(kQEmpty));
+                if (t + kLead + 1 == n) umma_commit(B(kQEmpty));
               }
-            } else {
-              umma_commit(B(kDoneO + x));
             }
+            if (t + 1 == n) umma_commit(B(kDoneO + x));
           }
           ++n_p;
+          if (!kQ2 && more) ++n_s;
         }
       }
     }
@@ -521,14 +534,14 @@ __global__ void __launch_bounds__(kChThreads, 1)
     }
   } else {
     if (kQ2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
-    // ================= softmax: warps 0-3 stream 0, warps 4-7 stream 1; a thread owns a row
+    // ================= softmax: four warps an M tile; a thread owns a row
     const int x = warp >> 2, quarter = warp & 3;
     const int lane_row = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-    const uint32_t slot = tmem + lane_base + x * 128, acc = tmem + lane_base + 256 + x * 128;
-    const int row = (kQ2 ? x * 128 : 0) + lane_row;  // row of the block
+    const uint32_t acc = tmem + lane_base + kOCol + x * 128;
+    const int row = x * 128 + lane_row;  // row of the block
     const int tok = row / a.G;
-    uint32_t n_s = 0, n_o = 0, n_x = 0, n_odd = 0;
+    uint32_t n_s = 0, n_o = 0, n_odd = 0;
     bool alive = true, first_item = true;
     while (alive && walk.next(a, sq, it)) {
       const int n = it.t1 - it.t0;
@@ -537,64 +550,74 @@ __global__ void __launch_bounds__(kChThreads, 1)
       const bool valid = tok < a.TB && token < it.g.n_new;
       const int sees = it.g.len - it.g.n_new + token + 1;  // rows that this thread's query sees
       const bool idle = !__any_sync(0xffffffffu, valid);   // no row of the warp is a query: it only keeps the barriers going
-      const int tile = blockIdx.x * 4 + (kQ2 ? 2 * (first_item ? 0 : 1) + x : (first_item ? 0 : 1));  // of partial results
-      float4* const sum = a.part_o + (int64_t)(kQ2 ? tile : blockIdx.x * 4 + 2 + x) * (32 * a.R) + lane_row;
+      const int tile = (blockIdx.x * 2 + (first_item ? 0 : 1)) * kTiles + x;  // of partial results
+      float4* const sum = a.part_o + (int64_t)tile * (32 * a.R) + lane_row;
       first_item = false;
       float ref = -INFINITY, l = 0.f, sum_ref = -INFINITY;
-      for (int i = 0; i < n; ++i) {
-        if (!(alive = mbar_wait(B(kDoneS + x), n_s & 1, s_abort, a.spin_limit))) break;
-        ++n_s;
+      for (int i = 0; i < n; ++i, ++n_s) {
+        const int s_slot = kQ2 ? x : (int)(n_s & 1);
+        if (!(alive = mbar_wait(B(kDoneS + s_slot), (kQ2 ? n_s : n_s >> 1) & 1, s_abort, a.spin_limit))) break;
         if (idle) {
           __syncwarp();
           if (lane == 0) {
-#pragma unroll
-            for (int half = 0; half < kHalves; ++half) mbar_arrive(B(kPReady + 2 * x + half));
+            mbar_arrive(B(kPReady + 2 * s_slot));
+            mbar_arrive(B(kPReady + 2 * s_slot + 1));
           }
           continue;
         }
         tc_fence_after();
+        const uint32_t slot = tmem + lane_base + s_slot * Sh::kSlotCols;
         const bool fresh = kFlush ? i % max(kFlush, 1) == 0 : i == 0;
-        if (kFlush && fresh && i > 0) {
-          // what the tensor cores have added up since the last time goes to the sum in memory (the products of the tile before are done: the
-          // tensor pipe finished them ahead of this S)
-          const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f;
-#pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            float o[32];
-            float4 m[8];
-            tmem_ld32(acc + c0, o);
-            if (i > kFlush) {
-#pragma unroll
-              for (int c = 0; c < 8; ++c)
-                if (valid) m[c] = sum[(c0 / 4 + c) * a.R];
-            }
-            tmem_wait_ld32(o);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              float4 y = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-              if (i > kFlush) y = make_float4(fmaf(m[c].x, f, y.x), fmaf(m[c].y, f, y.y), fmaf(m[c].z, f, y.z), fmaf(m[c].w, f, y.w));
-              if (valid) sum[(c0 / 4 + c) * a.R] = y;
-            }
-          }
-          sum_ref = ref;
-        }
-        float y[kKeys];
-#pragma unroll
-        for (int c = 0; c < kKeys; c += 64) tmem_ld64(slot + c, *reinterpret_cast<float(*)[64]>(y + c));
-#pragma unroll
-        for (int c = 0; c < kKeys; c += 64) tmem_wait_ld64(*reinterpret_cast<float(*)[64]>(y + c));
+        float y[128];
+        tmem_ld64(slot, *reinterpret_cast<float(*)[64]>(y));
+        tmem_ld64(slot + 64, *reinterpret_cast<float(*)[64]>(y + 64));
+        tmem_wait_ld64(*reinterpret_cast<float(*)[64]>(y));
+        tmem_wait_ld64(*reinterpret_cast<float(*)[64]>(y + 64));
         if ((it.t0 + i + 1) * kKeyTile > first) {
-          const int lim = sees - (it.t0 + i) * kKeyTile - (kQ2 ? 0 : 64 * x);
+          const int lim = sees - (it.t0 + i) * kKeyTile;
 #pragma unroll
-          for (int c = 0; c < kKeys; ++c) y[c] = c < lim ? y[c] : -INFINITY;
+          for (int c = 0; c < 128; ++c) y[c] = c < lim ? y[c] : -INFINITY;
         }
-        const float mx = ch_max<kKeys>(y) * a.scale_log2;
+        const float mx = ch_max<128>(y) * a.scale_log2, ref_o = ref;
         const bool grow = mx > ref + kChTau;  // also the first tile with a visible key
         const bool rescale = grow && ref > -INFINITY;
-        if (__any_sync(0xffffffffu, rescale)) {
-          const float f = rescale ? fast_exp2(ref - mx) : 1.f;
-          l *= f;
-          if (!fresh) {
+        const bool touch = (kFlush && fresh && i > 0) || (__any_sync(0xffffffffu, rescale) && !fresh);
+        // The accumulator holds the products of the tile before.  Two M tiles: the tensor pipe finished them ahead of this S.
+        if (!kQ2 && touch) {
+          if (!(alive = mbar_wait(B(kDonePV), (n_s - 1) & 1, s_abort, a.spin_limit))) break;
+          tc_fence_after();
+        }
+        if (grow) {
+          l = rescale ? l * fast_exp2(ref - mx) : l;
+          ref = mx;
+        }
+        const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
+        l += ch_probs32<kParts>(y, a.scale_log2, neg, slot, 64);
+        l += ch_probs32<kParts>(y + 32, a.scale_log2, neg, slot + 16, 64);
+        if (touch) {
+          if (kFlush && fresh) {  // what the tensor cores have added up since the last time goes to the sum in memory
+            const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref_o) : 0.f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 16) {
+              float o[16];
+              float4 m[4];
+              tmem_ld16(acc + c0, o);
+              if (i > kFlush) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                  if (valid) m[c] = sum[(c0 / 4 + c) * a.R];
+              }
+              tmem_wait_ld16(o);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                float4 z = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                if (i > kFlush) z = make_float4(fmaf(m[c].x, f, z.x), fmaf(m[c].y, f, z.y), fmaf(m[c].z, f, z.z), fmaf(m[c].w, f, z.w));
+                if (valid) sum[(c0 / 4 + c) * a.R] = z;
+              }
+            }
+            sum_ref = ref_o;
+          } else {
+            const float f = rescale ? fast_exp2(ref_o - ref) : 1.f;
 #pragma unroll 1
             for (int c0 = 0; c0 < 128; c0 += 32) {
               float o[32];
@@ -606,17 +629,16 @@ __global__ void __launch_bounds__(kChThreads, 1)
             }
           }
         }
-        if (grow) ref = mx;
-        const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
-#pragma unroll
-        for (int half = 0; half < kHalves; ++half) {
-          l += ch_probs32<kParts>(y + half * 64, a.scale_log2, neg, slot + half * 32, kPartCols);
-          l += ch_probs32<kParts>(y + half * 64 + 32, a.scale_log2, neg, slot + half * 32 + 16, kPartCols);
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(B(kPReady + 2 * x + half));
-        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kPReady + 2 * s_slot));
+        l += ch_probs32<kParts>(y + 64, a.scale_log2, neg, slot + 32, 64);
+        l += ch_probs32<kParts>(y + 96, a.scale_log2, neg, slot + 48, 64);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kPReady + 2 * s_slot + 1));
       }
       if (!alive) break;
       if (!(alive = mbar_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
@@ -629,55 +651,22 @@ __global__ void __launch_bounds__(kChThreads, 1)
       const bool whole = n == it.nt, summed = kFlush && n > kFlush;
       const int b = it.seg / a.Hkv, h = it.seg - b * a.Hkv;
       const int64_t orow = (int64_t)(sq.start[b] + token) * a.Hq + h * a.G + (row - tok * a.G);
-      float f0 = 1.f, f1 = 0.f, ref_t = ref, l_t = l, fs0 = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f, fs1 = 0.f;
-      if (!kQ2) {  // the two streams' halves of the keys; each stream's warps take half of d
-        s_ml[x * 128 + lane_row] = make_float4(ref, l, sum_ref, 0.f);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(B(kXch + quarter));
-        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
-        ++n_x;
-        tc_fence_after();
-        const float4 m0 = s_ml[lane_row], m1 = s_ml[128 + lane_row];
-        ref_t = fmaxf(m0.x, m1.x);
-        f0 = m0.x > -INFINITY ? fast_exp2(m0.x - ref_t) : 0.f;
-        f1 = m1.x > -INFINITY ? fast_exp2(m1.x - ref_t) : 0.f;
-        fs0 = m0.z > -INFINITY ? fast_exp2(m0.z - ref_t) : 0.f;
-        fs1 = m1.z > -INFINITY ? fast_exp2(m1.z - ref_t) : 0.f;
-        // a stream whose row has seen nothing adds nothing (or the NaN that it has met)
-        l_t = (m0.x > -INFINITY ? m0.y * f0 : m0.y) + (m1.x > -INFINITY ? m1.y * f1 : m1.y);
-      }
-      const float inv = whole ? (l_t > 0.f ? 1.f / l_t : (l_t == 0.f ? 0.f : l_t)) : 1.f;  // a NaN stays one
-      const int c_lo = kQ2 ? 0 : x * 64, c_hi = kQ2 ? 128 : c_lo + 64;
-      const uint32_t acc0 = kQ2 ? acc : tmem + lane_base + 256;
-      const float4* const sum0 = kQ2 ? sum : a.part_o + (int64_t)(blockIdx.x * 4 + 2) * (32 * a.R) + lane_row;
+      const float fs = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f;
+      const float inv = whole ? (l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l)) : 1.f;  // a NaN stays one
       if (!idle) {
 #pragma unroll 1
-        for (int c0 = c_lo; c0 < c_hi; c0 += 32) {
+        for (int c0 = 0; c0 < 128; c0 += 32) {
           float o[32];
-          tmem_ld32(acc0 + c0, o);
+          tmem_ld32(acc + c0, o);
           tmem_wait_ld32(o);
-          if (!kQ2) {
-            float o1[32];
-            tmem_ld32(acc0 + 128 + c0, o1);
-            tmem_wait_ld32(o1);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = fmaf(o[c], f0, o1[c] * f1);
-          }
           if (summed && valid) {
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-              const float4 m = sum0[(c0 / 4 + c) * a.R];
-              o[4 * c] = fmaf(m.x, fs0, o[4 * c]);
-              o[4 * c + 1] = fmaf(m.y, fs0, o[4 * c + 1]);
-              o[4 * c + 2] = fmaf(m.z, fs0, o[4 * c + 2]);
-              o[4 * c + 3] = fmaf(m.w, fs0, o[4 * c + 3]);
-              if (!kQ2) {
-                const float4 m1 = sum0[(32 + c0 / 4 + c) * a.R];
-                o[4 * c] = fmaf(m1.x, fs1, o[4 * c]);
-                o[4 * c + 1] = fmaf(m1.y, fs1, o[4 * c + 1]);
-                o[4 * c + 2] = fmaf(m1.z, fs1, o[4 * c + 2]);
-                o[4 * c + 3] = fmaf(m1.w, fs1, o[4 * c + 3]);
-              }
+              const float4 m = sum[(c0 / 4 + c) * a.R];
+              o[4 * c] = fmaf(m.x, fs, o[4 * c]);
+              o[4 * c + 1] = fmaf(m.y, fs, o[4 * c + 1]);
+              o[4 * c + 2] = fmaf(m.z, fs, o[4 * c + 2]);
+              o[4 * c + 3] = fmaf(m.w, fs, o[4 * c + 3]);
             }
           }
           if (odd < sees && valid) {  // infinities and NaN that were taken out of the V tiles
@@ -698,9 +687,8 @@ __global__ void __launch_bounds__(kChThreads, 1)
           }
           if (valid) {
             if (!whole) {
-              float4* dst = a.part_o + (int64_t)tile * (32 * a.R) + lane_row;
 #pragma unroll
-              for (int c = 0; c < 8; ++c) dst[(c0 / 4 + c) * a.R] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+              for (int c = 0; c < 8; ++c) sum[(c0 / 4 + c) * a.R] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
             } else if (kFlush) {
               float* dst = reinterpret_cast<float*>(a.out) + orow * kD + c0;
 #pragma unroll
@@ -720,18 +708,12 @@ __global__ void __launch_bounds__(kChThreads, 1)
             }
           }
         }
-        if (valid && (kQ2 || x == 0)) {
-          if (!whole) a.part_ml[(int64_t)tile * a.R + lane_row] = make_float2(ref_t, l_t);
-          else if (a.lse) a.lse[orow] = l_t == 0.f ? -INFINITY : (ref_t + log2f(l_t)) * 0.6931471805599453f;
+        if (valid) {
+          if (!whole) a.part_ml[(int64_t)tile * a.R + lane_row] = make_float2(ref, l);
+          else if (a.lse) a.lse[orow] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
         }
       }
       tc_fence_before();
-      if (!kQ2) {  // the other stream's warps have read this accumulator: its next product may overwrite it
-        __syncwarp();
-        if (lane == 0) mbar_arrive(B(kXch + quarter));
-        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
-        ++n_x;
-      }
     }
   }
 
@@ -740,7 +722,7 @@ __global__ void __launch_bounds__(kChThreads, 1)
     for (int i = 0; i < 200; ++i) __nanosleep(1000);
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kChTmemCols) : "memory");
+  if (warp == kSoft) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kChTmemCols) : "memory");
   if (*s_abort && tid == 0) raise_status(a.status, CATEKV_STATUS_WAIT_EXPIRED, kKidChunk, walk.seg, (int)blockIdx.x);
 }
 
@@ -754,13 +736,13 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
   pdl_wait();
   const int c = blockIdx.x;
   const int32_t* d = a.desc + c * 8;
-  const int t0 = d[2];
-  if (t0 == 0) return;
+  const int p0 = d[2];
+  if (ch_tile_at(p0) == 0) return;
   const int seg = d[0], blk = d[1], nt = d[3], n_new = d[4], total = d[5];
   const int q = total / C, r = total % C;
   auto begin = [&](int i) { return i * q + min(i, r); };
-  const int ub = begin(c) - t0, ue = ub + nt;
-  if (begin(c - 1) > ub) return;  // an earlier CTA begins inside this block
+  const int ub = begin(c) - p0, ue = ub + nt + kChCharge;  // the block's units
+  if (ch_tile_at(begin(c - 1) - ub) > 0) return;  // an earlier CTA begins inside this block
   int c_end = c + 1;
   while (c_end < C && begin(c_end) < ue) ++c_end;
   const int head = begin(c - 1) < ub ? 1 : 0;  // the first piece: the last block of CTA c - 1, or its only one
@@ -771,7 +753,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
   const bool valid = row / a.G < a.TB && blk * a.TB + row / a.G < n_new;
   auto tile = [&](int k) {
     const int i = k == c - 1 ? head : 0;
-    return (int64_t)(k * 4 + (two ? 2 * i + x : i));
+    return (int64_t)(two ? (k * 2 + i) * 2 + x : k * 2 + i);
   };
   float M = -INFINITY, L = 0.f;
   float4 acc[4];
@@ -935,7 +917,7 @@ static ChunkWs chunk_ws_layout(int G, int max_new) {
   ChunkWs w;
   const int64_t rows = (int64_t)G * max_new;
   w.R = rows < 128 ? (int)rows : 128;
-  const size_t tiles = 4 * (size_t)sm_count();
+  const size_t tiles = (ch_two_tiles(G, max_new) ? 4 : 2) * (size_t)sm_count();
   size_t o = CATEKV_STATUS_BYTES;
   w.off_desc = o; o = align_up(o + (size_t)sm_count() * 8 * sizeof(int32_t), 256);
   w.off_ml = o; o = align_up(o + tiles * w.R * sizeof(float2), 256);
@@ -973,10 +955,10 @@ static int launch_chunk(int ctas, const CUtensorMap* m, const ChunkArgs& a, cons
   int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts, kFlush>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ch_smem_bytes<kQ2>()));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts, kFlush>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ChunkShape<kQ2>::kSmem));
     if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   }
-  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts, kFlush>, dim3(ctas), dim3(kChThreads), ch_smem_bytes<kQ2>(), st, m[0], m[1], m[2], m[3], m[4],
+  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts, kFlush>, dim3(ctas), dim3(ChunkShape<kQ2>::kThreads), ChunkShape<kQ2>::kSmem, st, m[0], m[1], m[2], m[3], m[4],
                              a, sq));
   return CATEKV_OK;
 }
@@ -1108,7 +1090,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   }
   const int ctas = (int)(units < sm_count() ? units : sm_count());
   cudaStream_t st = (cudaStream_t)stream;
-  if (a.out_fp32) rc = two ? launch_chunk<true, 2, 4>(ctas, m, a, sq, st) : launch_chunk<false, 3, 8>(ctas, m, a, sq, st);
+  if (a.out_fp32) rc = two ? launch_chunk<true, 2, 4>(ctas, m, a, sq, st) : launch_chunk<false, 3, 4>(ctas, m, a, sq, st);
   else rc = two ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st) : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
   if (rc) return rc;
   CATEKV_CUDA_TRY(launch_pdl(chunk_combine_kernel, dim3(ctas, ((two ? 256 : W.R) + kChCombineRows - 1) / kChCombineRows), dim3(256), 0, st, a, sq, ctas,
