@@ -9,13 +9,13 @@
 // (a captured call follows lists that grow).  A block that several CTAs share leaves partial results, which
 // chunk_combine_kernel merges in the order of the keys.
 //
-// Per tile: S = Q K^T (tcgen05.mma, both operands in shared memory); a softmax thread owns a query row: it reads it (tcgen05.ld), raises
-// its reference when the tile's maximum exceeds it by more than 2^8 (the accumulator is then scaled in tensor memory: rare after the
-// first tiles) and writes P = exp2(logit - reference) over S in kParts bf16 numbers, each the rounded rest of those before it; O += P V
-// takes P from tensor memory and V as the MN-major operand as TMA left it, and starts on the first 64 keys while the others are at work.
-// What keeps the tensor pipe busy meanwhile: with two M tiles (bound by the products) each is a stream with softmax warps, an S / P slot and
-// an accumulator of its own, and one's products run beside the other's softmax; with one (bound by the stream of K and V)
-// there are two slots, and S of the next tile is formed ahead.
+// A tile is worked on in two steps of 64 keys.  Per step: S = Q K^T (tcgen05.mma, both operands in shared memory); a softmax thread owns a
+// query row: it reads it (tcgen05.ld), raises its reference when the step's maximum exceeds it by more than 2^8 (the accumulator is then
+// scaled in tensor memory: rare after the first tiles) and writes P = exp2(logit - reference) over S in kParts bf16 numbers, each the
+// rounded rest of those before it; O += P V takes P from tensor memory and V as the MN-major operand as TMA left it.  Every M tile has softmax
+// warps of its own, an accumulator, and two slots of S / P, so that S of the next step is formed while the softmax is at this one.
+// (Steps of 128 keys have room for one slot only beside two accumulators: softmax and products of an M tile took turns, 4100
+// cycles a tile for two M tiles where the products need 2050; S with 64 keys reads its Q operand twice as often.)
 //
 // Precision.  kParts = 1: P rounded to bf16 (2^-9), as the result will be: bf16 results with two M tiles, where the products bound the kernel.
 // 2: 17 significant bits; 3: all of fp32's.  The tensor cores add with truncation, about 2^-27 of the accumulator lost per 16-key step;
@@ -40,7 +40,7 @@ namespace catekv {
 
 constexpr int kChMaxSeqs = 512;  // sequences of a call: their counts travel in the kernel's arguments
 constexpr int kChTileBytes = 128 * 256;  // a [128 x 128] bf16 tile
-constexpr int kChTmemCols = 512;         // two M tiles: slots of S / P at columns 0 and 128, O at 256 and 384; one: slots at 0 and 192, O at 384
+constexpr int kChTmemCols = 512;         // slots of S / P in columns 0-255, the M tiles' accumulators at 256 and 384
 constexpr float kChTau = 8.f;
 constexpr int kChBarriers = 32;
 template <bool kQ2>
@@ -49,8 +49,7 @@ struct ChunkShape {
   static constexpr int kStages = kQ2 ? 5 : 6;
   static constexpr int kSoft = 4 * kTiles;          // softmax warps
   static constexpr int kWarps = kSoft + 4, kThreads = kWarps * 32;
-  static constexpr int kSlots = 2, kSlotCols = kQ2 ? 128 : 192;
-  static constexpr int kLead = kQ2 ? 1 : 2;         // K tiles ahead of the V tile in the ring: K_0 .. K_{lead-1}, V_0, K_lead, V_1, ...
+  static constexpr int kSlotCols = kQ2 ? 64 : 128;  // slot h of M tile x: columns (2 x + h) kSlotCols; step h of a tile takes slot h
   static constexpr size_t kSmem = 1024 + (size_t)(kTiles + kStages) * kChTileBytes + kChBarriers * 8 + 64;
 };
 static_assert(ChunkShape<true>::kSmem <= 226 * 1024 && ChunkShape<false>::kSmem <= 227 * 1024, "chunk_attn_kernel: one CTA's shared memory");
@@ -137,6 +136,19 @@ struct ChunkWalk {
   }
 };
 
+// One lane of a converged warp issues for all of it.  The warp that feeds the tensor cores runs converged, so that descriptors, addresses and counters
+// live in uniform registers: with one lane on a branch of its own every tcgen05.mma moved its operands there first, 70 cycles an
+// instruction, and the products were bound by that.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ int uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(bar)
@@ -213,13 +225,12 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
                       const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ChunkArgs a,
                       const __grid_constant__ ChunkSeqs sq) {
   using Sh = ChunkShape<kQ2>;
-  constexpr int kStages = Sh::kStages, kTiles = Sh::kTiles, kLead = Sh::kLead, kSoft = Sh::kSoft, kWarps = Sh::kWarps;
+  constexpr int kStages = Sh::kStages, kTiles = Sh::kTiles, kSoft = Sh::kSoft, kWarps = Sh::kWarps;
   constexpr int kQBytes = kTiles * kChTileBytes, kQBlock = kQBytes / 2;
-  constexpr int kOCol = kQ2 ? 256 : 384;
-  static_assert(kParts * 64 <= Sh::kSlotCols, "P fits its slot");
+  static_assert(kParts * 32 <= Sh::kSlotCols, "P fits its slot");
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_scan[kWarps + 4];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uni(tid >> 5), lane = tid & 31;
   const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (s_base - smem_u32(smem_raw));
   const uint32_t s_q = s_base, s_ring = s_base + kQBytes;
@@ -229,8 +240,8 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
   int* s_odd = reinterpret_cast<int*>(s_tmem + 4);  // [4]: first new row with an infinity or a NaN in V, of the last blocks that had V tiles looked at
   const uint32_t bar0 = smem_u32(s_bar);
   auto B = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-  constexpr int kFull = 0, kEmpty = kStages, kFixed = 2 * kStages, kDoneS = 3 * kStages, kPReady = kDoneS + 2, kDoneO = kPReady + 4,
-                kDonePV = kDoneO + 2, kQFull = kDonePV + 1, kQEmpty = kQFull + 1;
+  constexpr int kFull = 0, kEmpty = kStages, kFixed = 2 * kStages, kDoneS = 3 * kStages, kPReady = kDoneS + 4, kDoneO = kPReady + 4,
+                kDonePV = kDoneO + 2, kQFull = kDonePV + 2, kQEmpty = kQFull + 1;
   static_assert(kQEmpty < kChBarriers, "barrier table");
 
   pdl_launch_dependents();
@@ -324,9 +335,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
   if (walk.left > 0) walk.g = ch_seg(a, sq, walk.seg);
   ChunkItem it;
 
-  // The softmax warps hold a row of S: registers of the other warps go to them (128 x 88 + 256 x 208 = 384 x 168, what the block was launched with).
   if (warp >= kSoft) {
-    if (kQ2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
   if (warp == kSoft + 1) {
     // ================= K and V tiles, in the order in which the tensor pipe uses them
     if (lane == 0 && !a.idle_producer) {
@@ -360,10 +369,10 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
           }
           return true;
         };
-        for (int t = 0; ok && t < min(kLead, n); ++t) ok = load(&k_map, &ko_map, it.t0 + t);
-        for (int t = 0; ok && t < n; ++t) {
+        ok = load(&k_map, &ko_map, it.t0);
+        for (int t = 0; ok && t < n; ++t) {  // K_0, V_0, K_1, V_1, ...
           ok = load(&v_map, &vo_map, it.t0 + t);
-          if (ok && t + kLead < n) ok = load(&k_map, &ko_map, it.t0 + t + kLead);
+          if (ok && t + 1 < n) ok = load(&k_map, &ko_map, it.t0 + t + 1);
         }
       }
     }
@@ -396,12 +405,12 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
         const uint32_t u = use++;
         return mbar_wait(B(kFull + u % kStages), (u / kStages) & 1, s_abort, a.spin_limit);
       };
-      for (int t = 0; ok && t < min(kLead, n); ++t) ok = arrived();
+      ok = arrived();
       for (int t = 0; ok && t < n; ++t) {
         const int r0 = (it.t0 + t) * kKeyTile, st = use % kStages;
         if (!(ok = arrived())) break;
         if (r0 + kKeyTile <= first) {
-          if (t + kLead < n) ok = arrived();
+          if (t + 1 < n) ok = arrived();
           continue;
         }
         if (fresh) {
@@ -437,108 +446,110 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kFixed + st));
-        if (t + kLead < n) ok = arrived();
+        if (t + 1 < n) ok = arrived();
       }
       n_item += fresh ? 0 : 1;
     }
     __syncwarp();
   } else if (warp == kSoft) {
-    // ================= tensor-core issue
-    if (lane == 0 && !a.idle_producer) {
-      const uint32_t idesc_s = umma_idesc_bf16(128, 128), idesc_o = umma_idesc_bf16_bmn(128, 128);
+    // ================= tensor-core issue (the whole warp, converged)
+    if (!a.idle_producer) {
+      const uint32_t idesc_s = umma_idesc_bf16(128, 64), idesc_o = umma_idesc_bf16_bmn(128, 128);
       const uint64_t dq0 = umma_desc_sw128(s_q), dk0 = umma_desc_sw128(s_ring), dv0 = umma_desc_sw128_mn(s_ring, kKBlockBytes);
-      const uint32_t dv_hi = (uint32_t)(dv0 >> 32), dv_lo0 = (uint32_t)dv0;
-      uint32_t use = 0, n_item = 0, fixed = 0, n_s = 0, n_p = 0;  // fixed: one bit per stage, the parity of its next look
+      const uint32_t tm = (uint32_t)uni((int)tmem);
+      uint32_t use = 0, n_item = 0, fixed = 0, n_p = 0;  // fixed: one bit per stage, the parity of its next look; n_p: tiles
       bool ok = true;
-      auto wait_tile = [&]() { return mbar_wait(B(kFull + use % kStages), (use / kStages) & 1, s_abort, a.spin_limit); };
-      auto issue_s = [&](int x, int slot, int st) {  // M tile x
-        const uint64_t dq = dq0 + (uint64_t)(x * (128 * 128 >> 4)), dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4));
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk)
-          umma_bf16(tmem + slot * Sh::kSlotCols, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2),
-                    dk + (uint64_t)((kk >> 2) * (kKBlockBytes >> 4) + (kk & 3) * 2), idesc_s, kk ? 1u : 0u);
-        umma_commit(B(kDoneS + slot));
+      auto wait_tile = [&]() { return warp_wait(B(kFull + use % kStages), (use / kStages) & 1, s_abort, a.spin_limit); };
+      auto commit = [&](int i) {
+        if (elect_one()) umma_commit(B(i));
       };
-      auto issue_o = [&](int x, int slot, int st, int half, bool fresh) {  // 64 keys
-        const uint32_t lo = dv_lo0 + (uint32_t)(st * (kChTileBytes >> 4) + half * (64 * 128 >> 4));
-        const uint32_t p = tmem + slot * Sh::kSlotCols + half * 32;
+      auto issue_s = [&](int x, int h, int st) {
+        const uint64_t dq = dq0 + (uint64_t)(x * (128 * 128 >> 4)), dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4) + h * (64 * 128 >> 4));
+        const uint32_t d = tm + (2 * x + h) * Sh::kSlotCols;
+        if (elect_one()) {
 #pragma unroll
-        for (int part = 0; part < kParts; ++part)
+          for (int kk = 0; kk < 8; ++kk)
+            umma_bf16(d, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2), dk + (uint64_t)((kk >> 2) * (kKBlockBytes >> 4) + (kk & 3) * 2),
+                      idesc_s, kk ? 1u : 0u);
+          umma_commit(B(kDoneS + 2 * x + h));
+        }
+      };
+      auto issue_o = [&](int x, int h, int st, bool fresh) {
+        const uint64_t dv = dv0 + (uint64_t)(st * (kChTileBytes >> 4) + h * (64 * 128 >> 4));
+        const uint32_t d = tm + 256 + x * 128, p = tm + (2 * x + h) * Sh::kSlotCols;
+        if (elect_one()) {
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            umma_bf16_ta_lohi(tmem + kOCol + x * 128, p + part * 64 + kk * 8, lo + (uint32_t)(kk * 128), dv_hi, idesc_o,
-                              (part | kk | half) ? 1u : (fresh ? 0u : 1u));
+          for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              umma_bf16_ta(d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc_o, (part | kk) ? 1u : (fresh ? 0u : 1u));
+          umma_commit(B(kDonePV + x));
+        }
       };
       while (ok && walk.next(a, sq, it)) {
-        const int n = it.t1 - it.t0;
-        const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;
-        if (!(ok = mbar_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit))) break;
+        const int t0 = uni(it.t0), n = uni(it.t1) - t0;
+        const int first = uni(it.g.len - it.g.n_new + it.blk * a.TB + 1);
+        if (!(ok = warp_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit))) break;
         ++n_item;
-        for (int t = 0; t < min(kLead, n); ++t) {
-          if (!(ok = wait_tile())) break;
-          tc_fence_after();
+        if (!(ok = wait_tile())) break;
+        tc_fence_after();
+        {
           const int st = use++ % kStages;
-          if (kQ2) {
-            issue_s(0, 0, st);
-            issue_s(1, 1, st);
-          } else {
-            issue_s(0, n_s++ & 1, st);
-          }
-          umma_commit(B(kEmpty + st));
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < kTiles; ++x) issue_s(x, h, st);
+          commit(kEmpty + st);
         }
-        if (n <= kLead) umma_commit(B(kQEmpty));
-        for (int t = 0; ok && t < n; ++t) {
-          const bool look = (it.t0 + t + 1) * kKeyTile > first;
-          const bool more = t + kLead < n, fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
+        if (n == 1) commit(kQEmpty);
+        for (int t = 0; ok && t < n; ++t, ++n_p) {
+          const bool look = (t0 + t + 1) * kKeyTile > first, more = t + 1 < n;
+          const bool fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
           const int sv = use % kStages, sk = (use + 1) % kStages;
 #pragma unroll
-          for (int x = 0; x < kTiles; ++x) {
-            const int slot = kQ2 ? x : (int)(n_p & 1);
+          for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              if (!(ok = mbar_wait(B(kPReady + 2 * slot + half), (kQ2 ? n_p : n_p >> 1) & 1, s_abort, a.spin_limit))) break;
-              if (x == 0 && half == 0) {
-                if (!(ok = wait_tile())) break;
-                if (look) {
-                  if (!(ok = mbar_wait(B(kFixed + sv), (fixed >> sv) & 1, s_abort, a.spin_limit))) break;
+            for (int x = 0; x < kTiles; ++x) {
+              if (ok) ok = warp_wait(B(kPReady + 2 * x + h), n_p & 1, s_abort, a.spin_limit);
+              if (h == 0 && x == 0) {
+                if (ok) ok = wait_tile();
+                ++use;
+                if (ok && look) {
+                  ok = warp_wait(B(kFixed + sv), (fixed >> sv) & 1, s_abort, a.spin_limit);
                   fixed ^= 1u << sv;
                 }
-                ++use;
               }
+              if (!ok) break;
               tc_fence_after();
-              issue_o(x, slot, sv, half, fresh);
-            }
-            if (!ok) break;
-            if (!kQ2) umma_commit(B(kDonePV));
-            if (x == kTiles - 1) umma_commit(B(kEmpty + sv));
-            if (more) {
-              if (x == 0) {
-                if (!(ok = wait_tile())) break;
-                tc_fence_after();
+              issue_o(x, h, sv, fresh && h == 0);
+              if (h == 1 && x == kTiles - 1) commit(kEmpty + sv);
+              if (more) {  // the next tile's S into the slot whose P has just been taken: the tensor pipe keeps issue order
+                if (h == 0 && x == 0) {
+                  if (!(ok = wait_tile())) break;
+                  ++use;
+                  tc_fence_after();
+                }
+                issue_s(x, h, sk);
+                if (h == 1 && x == kTiles - 1) {
+                  commit(kEmpty + sk);
+                  if (t + 2 == n) commit(kQEmpty);
+                }
+              } else if (h == 1) {
+                commit(kDoneO + x);
               }
-              issue_s(x, slot, sk);  // into the slot whose P has just been taken: the tensor pipe keeps issue order
-              if (x == kTiles - 1) {
-                umma_commit(B(kEmpty + sk));
-                ++use;
-                if (t + kLead + 1 == n) umma_commit(B(kQEmpty));
-              }
             }
-            if (t + 1 == n) umma_commit(B(kDoneO + x));
           }
-          ++n_p;
-          if (!kQ2 && more) ++n_s;
         }
       }
     }
     __syncwarp();
     }
   } else {
-    if (kQ2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
     // ================= softmax: four warps an M tile; a thread owns a row
     const int x = warp >> 2, quarter = warp & 3;
     const int lane_row = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-    const uint32_t acc = tmem + lane_base + kOCol + x * 128;
+    const uint32_t acc = tmem + lane_base + 256 + x * 128;
     const int row = x * 128 + lane_row;  // row of the block
     const int tok = row / a.G;
     uint32_t n_s = 0, n_o = 0, n_odd = 0;
@@ -554,91 +565,81 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
       float4* const sum = a.part_o + (int64_t)tile * (32 * a.R) + lane_row;
       first_item = false;
       float ref = -INFINITY, l = 0.f, sum_ref = -INFINITY;
-      for (int i = 0; i < n; ++i, ++n_s) {
-        const int s_slot = kQ2 ? x : (int)(n_s & 1);
-        if (!(alive = mbar_wait(B(kDoneS + s_slot), (kQ2 ? n_s : n_s >> 1) & 1, s_abort, a.spin_limit))) break;
-        if (idle) {
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(B(kPReady + 2 * s_slot));
-            mbar_arrive(B(kPReady + 2 * s_slot + 1));
-          }
-          continue;
-        }
-        tc_fence_after();
-        const uint32_t slot = tmem + lane_base + s_slot * Sh::kSlotCols;
+      for (int i = 0; alive && i < n; ++i, ++n_s) {
         const bool fresh = kFlush ? i % max(kFlush, 1) == 0 : i == 0;
-        float y[128];
-        tmem_ld64(slot, *reinterpret_cast<float(*)[64]>(y));
-        tmem_ld64(slot + 64, *reinterpret_cast<float(*)[64]>(y + 64));
-        tmem_wait_ld64(*reinterpret_cast<float(*)[64]>(y));
-        tmem_wait_ld64(*reinterpret_cast<float(*)[64]>(y + 64));
-        if ((it.t0 + i + 1) * kKeyTile > first) {
-          const int lim = sees - (it.t0 + i) * kKeyTile;
-#pragma unroll
-          for (int c = 0; c < 128; ++c) y[c] = c < lim ? y[c] : -INFINITY;
-        }
-        const float mx = ch_max<128>(y) * a.scale_log2, ref_o = ref;
-        const bool grow = mx > ref + kChTau;  // also the first tile with a visible key
-        const bool rescale = grow && ref > -INFINITY;
-        const bool touch = (kFlush && fresh && i > 0) || (__any_sync(0xffffffffu, rescale) && !fresh);
-        // The accumulator holds the products of the tile before.  Two M tiles: the tensor pipe finished them ahead of this S.
-        if (!kQ2 && touch) {
-          if (!(alive = mbar_wait(B(kDonePV), (n_s - 1) & 1, s_abort, a.spin_limit))) break;
-          tc_fence_after();
-        }
-        if (grow) {
-          l = rescale ? l * fast_exp2(ref - mx) : l;
-          ref = mx;
-        }
-        const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
-        l += ch_probs32<kParts>(y, a.scale_log2, neg, slot, 64);
-        l += ch_probs32<kParts>(y + 32, a.scale_log2, neg, slot + 16, 64);
-        if (touch) {
-          if (kFlush && fresh) {  // what the tensor cores have added up since the last time goes to the sum in memory
-            const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref_o) : 0.f;
+        if (kFlush && fresh && i > 0 && !idle) {
+          // what the tensor cores have added up since the last time goes to the sum in memory, which is requested before the products are waited for
+          const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f;
+          bool done = false;
 #pragma unroll 1
-            for (int c0 = 0; c0 < 128; c0 += 16) {
-              float o[16];
-              float4 m[4];
-              tmem_ld16(acc + c0, o);
-              if (i > kFlush) {
+          for (int c0 = 0; c0 < 128; c0 += 64) {
+            float4 m[16];
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                  if (valid) m[c] = sum[(c0 / 4 + c) * a.R];
-              }
-              tmem_wait_ld16(o);
+            for (int c = 0; c < 16; ++c) m[c] = i > kFlush && valid ? sum[(c0 / 4 + c) * a.R] : make_float4(0.f, 0.f, 0.f, 0.f);
+            // (this step's S was issued behind the products of the step but one before: behind it, the parity tells the last step's)
+            if (!done && !(alive = mbar_wait(B(kDoneS + 2 * x), n_s & 1, s_abort, a.spin_limit) && mbar_wait(B(kDonePV + x), 1, s_abort, a.spin_limit))) break;
+            done = true;
+            tc_fence_after();
+            float o[64];
+            tmem_ld64(acc + c0, o);
+            tmem_wait_ld64(o);
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                float4 z = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-                if (i > kFlush) z = make_float4(fmaf(m[c].x, f, z.x), fmaf(m[c].y, f, z.y), fmaf(m[c].z, f, z.z), fmaf(m[c].w, f, z.w));
-                if (valid) sum[(c0 / 4 + c) * a.R] = z;
-              }
-            }
-            sum_ref = ref_o;
-          } else {
-            const float f = rescale ? fast_exp2(ref_o - ref) : 1.f;
-#pragma unroll 1
-            for (int c0 = 0; c0 < 128; c0 += 32) {
-              float o[32];
-              tmem_ld32(acc + c0, o);
-              tmem_wait_ld32(o);
-#pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] *= f;
-              tmem_st32(acc + c0, o);
-            }
+            for (int c = 0; c < 16; ++c)
+              if (valid)
+                sum[(c0 / 4 + c) * a.R] = make_float4(fmaf(m[c].x, f, o[4 * c]), fmaf(m[c].y, f, o[4 * c + 1]), fmaf(m[c].z, f, o[4 * c + 2]),
+                                                      fmaf(m[c].w, f, o[4 * c + 3]));
           }
+          if (!alive) break;
+          sum_ref = ref;
+          tc_fence_before();
         }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(B(kPReady + 2 * s_slot));
-        l += ch_probs32<kParts>(y + 64, a.scale_log2, neg, slot + 32, 64);
-        l += ch_probs32<kParts>(y + 96, a.scale_log2, neg, slot + 48, 64);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(B(kPReady + 2 * s_slot + 1));
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          if (!(alive = mbar_wait(B(kDoneS + 2 * x + h), n_s & 1, s_abort, a.spin_limit))) break;
+          if (idle) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(B(kPReady + 2 * x + h));
+            continue;
+          }
+          tc_fence_after();
+          const uint32_t slot = tmem + lane_base + (2 * x + h) * Sh::kSlotCols;
+          const int k0 = (it.t0 + i) * kKeyTile + 64 * h;
+          float y[64];
+          tmem_ld64(slot, y);
+          tmem_wait_ld64(y);
+          if (k0 + 64 > first) {
+            const int lim = sees - k0;
+#pragma unroll
+            for (int c = 0; c < 64; ++c) y[c] = c < lim ? y[c] : -INFINITY;
+          }
+          const float mx = ch_max<64>(y) * a.scale_log2;
+          const bool grow = mx > ref + kChTau;  // also the first step with a visible key
+          if (__any_sync(0xffffffffu, grow)) {
+            const float f = grow && ref > -INFINITY ? fast_exp2(ref - mx) : 1.f;
+            l *= f;
+            if ((h == 1 || !fresh) && __any_sync(0xffffffffu, f != 1.f)) {  // the accumulator follows, behind the products of the step before
+              if (!(alive = mbar_wait(B(kDonePV + x), h ^ 1, s_abort, a.spin_limit))) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c0 = 0; c0 < 128; c0 += 32) {
+                float o[32];
+                tmem_ld32(acc + c0, o);
+                tmem_wait_ld32(o);
+#pragma unroll
+                for (int c = 0; c < 32; ++c) o[c] *= f;
+                tmem_st32(acc + c0, o);
+              }
+            }
+            if (grow) ref = mx;
+          }
+          const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
+          l += ch_probs32<kParts>(y, a.scale_log2, neg, slot, 32);
+          l += ch_probs32<kParts>(y + 32, a.scale_log2, neg, slot + 16, 32);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(B(kPReady + 2 * x + h));
+        }
       }
       if (!alive) break;
       if (!(alive = mbar_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
