@@ -149,6 +149,16 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
 }
 
+// Whether a phase has completed, without waiting.
+__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(done)
+               : "r"(bar), "r"(parity)
+               : "memory");
+  return __all_sync(0xffffffffu, done != 0);
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(bar)
@@ -502,15 +512,17 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
           commit(kEmpty + st);
         }
         if (n == 1) commit(kQEmpty);
+        bool p_there = false;  // the next P was seen ready before the last S was issued: its products follow without a look at a barrier
         for (int t = 0; ok && t < n; ++t, ++n_p) {
           const bool look = (t0 + t + 1) * kKeyTile > first, more = t + 1 < n;
           const bool fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
           const int sv = use % kStages, sk = (use + 1) % kStages;
+          bool k_there = false;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int x = 0; x < kTiles; ++x) {
-              if (ok) ok = warp_wait(B(kPReady + 2 * x + h), n_p & 1, s_abort, a.spin_limit);
+              if (!p_there) ok = warp_wait(B(kPReady + 2 * x + h), n_p & 1, s_abort, a.spin_limit);
               if (h == 0 && x == 0) {
                 if (ok) ok = wait_tile();
                 ++use;
@@ -518,19 +530,23 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
                   ok = warp_wait(B(kFixed + sv), (fixed >> sv) & 1, s_abort, a.spin_limit);
                   fixed ^= 1u << sv;
                 }
+                if (ok && more) k_there = warp_test(B(kFull + sk), (use / kStages) & 1);
               }
               if (!ok) break;
               tc_fence_after();
               issue_o(x, h, sv, fresh && h == 0);
               if (h == 1 && x == kTiles - 1) commit(kEmpty + sv);
+              const bool last = h == 1 && x == kTiles - 1;  // of the tile
+              const int xn = x + 1 < kTiles ? x + 1 : 0, hn = x + 1 < kTiles ? h : h ^ 1;
+              p_there = (!last || more) && warp_test(B(kPReady + 2 * xn + hn), (last ? n_p + 1 : n_p) & 1);
               if (more) {  // the next tile's S into the slot whose P has just been taken: the tensor pipe keeps issue order
                 if (h == 0 && x == 0) {
-                  if (!(ok = wait_tile())) break;
+                  if (!k_there && !(ok = wait_tile())) break;
                   ++use;
                   tc_fence_after();
                 }
                 issue_s(x, h, sk);
-                if (h == 1 && x == kTiles - 1) {
+                if (last) {
                   commit(kEmpty + sk);
                   if (t + 2 == n) commit(kQEmpty);
                 }
@@ -538,6 +554,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
                 commit(kDoneO + x);
               }
             }
+            if (!ok) break;
           }
         }
       }
