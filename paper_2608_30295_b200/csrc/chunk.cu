@@ -18,8 +18,10 @@
 // cycles a tile for two M tiles where the products need 2050; S with 64 keys reads its Q operand twice as often.)
 //
 // Precision.  kParts = 1: P rounded to bf16 (2^-9), as the result will be: bf16 results with two M tiles, where the products bound the kernel.
-// 2: 17 significant bits; 3: all of fp32's.  The tensor cores add with truncation, about 2^-27 of the accumulator lost per 16-key step;
-// fp32 results (kFlush) therefore have the accumulator added, with rounding, to a sum in memory every kFlush tiles, where the products start from zero.
+// 2 (bf16 results, one M tile): 17 significant bits.  3 (fp32 results): all of fp32's.  The tensor cores add with truncation, and what that loses
+// goes by the accumulator's size and the number of instructions.  For fp32 results the parts behind the first therefore have an accumulator of their
+// own, 2^-9 as large, and both are added, with rounding, to a sum in the thread's registers every kFlush tiles, where the products start from zero
+// (relative error of 64K rows: 5e-6 with one accumulator and a flush every 16 tiles).  That takes one M tile, whatever the number of rows.
 //
 // Rows of a V tile that no query of the block sees are zeroed in shared memory before the product reads them (what lies behind a list
 // may be NaN, and 0 * NaN is not 0); an infinity or a NaN in a new row, which later tokens see and earlier ones do not, is taken
@@ -76,8 +78,8 @@ struct ChunkArgs {
   void* out;
   float* lse;
   int32_t out_fp32;
-  // Partial results, two tiles a stream [32 d / 4][R rows] (float4: a warp's rows lie side by side) a CTA.  With two M tiles: tile 2 i + x, i = 0 for the CTA's
-  // first block and 1 for its last; with one: tile i.  part_ml: reference (log2 domain) and sum of the rows.
+  // Partial results, two tiles [32 d / 4][R rows] (float4: a warp's rows lie side by side) for every M tile of a CTA: of its first block, and
+  // of its last.  part_ml: reference (log2 domain) and sum of the rows.
   float4* part_o;
   float2* part_ml;
   int32_t* desc;   // [CTAs][8]
@@ -347,40 +349,51 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
 
   if (warp >= kSoft) {
   if (warp == kSoft + 1) {
-    // ================= K and V tiles, in the order in which the tensor pipe uses them
-    if (lane == 0 && !a.idle_producer) {
+    // ================= K and V tiles, in the order in which the tensor pipe uses them: K_0, V_0, K_1, V_1, ...
+    // The entries of the page table are fetched 32 at a time, a lane each (one by one, a trip to memory for every tile, they were slower than the products).
+    if (!a.idle_producer) {
       uint32_t use = 0;
       bool ok = true;
       while (ok && walk.next(a, sq, it)) {
         const int n = it.t1 - it.t0;
         const int off = a.seg_off[it.seg], cap = a.seg_cap[it.seg];
+        int window = -64, entry = -1;  // lane i holds the list's page window + i
         auto load = [&](const CUtensorMap* pool, const CUtensorMap* ovf, int t) {
           const int st = use % kStages;
-          if (use >= kStages && !mbar_wait(B(kEmpty + st), ((use / kStages) - 1) & 1, s_abort, a.spin_limit)) return false;
+          if (use >= kStages && !warp_wait(B(kEmpty + st), ((use / kStages) - 1) & 1, s_abort, a.spin_limit)) return false;
           ++use;
           const int r0 = t * kKeyTile;
           const uint32_t dst = s_ring + st * kChTileBytes, bar = B(kFull + st);
           if (r0 < cap) {
-            mbar_expect_tx(bar, kChTileBytes);
-            tma_load_2d(dst, pool, 0, off + r0, bar);
-            tma_load_2d(dst + kKBlockBytes, pool, 64, off + r0, bar);
-          } else {
-            const int pg0 = r0 < it.g.len ? ch_page(a, it.seg, r0 - cap) : -1;
-            const int pg1 = r0 + 64 < it.g.len ? ch_page(a, it.seg, r0 + 64 - cap) : -1;
-            mbar_expect_tx(bar, (pg0 >= 0 ? kChTileBytes / 2 : 0) + (pg1 >= 0 ? kChTileBytes / 2 : 0));
-            if (pg0 >= 0) {
-              tma_load_2d(dst, ovf, 0, pg0 * 64, bar);
-              tma_load_2d(dst + kKBlockBytes, ovf, 64, pg0 * 64, bar);
+            if (lane == 0) {
+              mbar_expect_tx(bar, kChTileBytes);
+              tma_load_2d(dst, pool, 0, off + r0, bar);
+              tma_load_2d(dst + kKBlockBytes, pool, 64, off + r0, bar);
             }
-            if (pg1 >= 0) {
-              tma_load_2d(dst + 64 * 128, ovf, 0, pg1 * 64, bar);
-              tma_load_2d(dst + kKBlockBytes + 64 * 128, ovf, 64, pg1 * 64, bar);
+          } else {
+            const int p = (r0 - cap) >> 6;
+            if (p < window || p + 1 >= window + 32) {  // the V tile before comes after this K tile
+              window = max(p - 2, 0);
+              entry = cap + (window + lane) * 64 < it.g.len ? ch_page(a, it.seg, (window + lane) * 64) : -1;
+            }
+            const int pg0 = __shfl_sync(0xffffffffu, entry, p - window), pg1 = __shfl_sync(0xffffffffu, entry, p + 1 - window);
+            if (lane == 0) {
+              mbar_expect_tx(bar, (pg0 >= 0 ? kChTileBytes / 2 : 0) + (pg1 >= 0 ? kChTileBytes / 2 : 0));
+              if (pg0 >= 0) {
+                tma_load_2d(dst, ovf, 0, pg0 * 64, bar);
+                tma_load_2d(dst + kKBlockBytes, ovf, 64, pg0 * 64, bar);
+              }
+              if (pg1 >= 0) {
+                tma_load_2d(dst + 64 * 128, ovf, 0, pg1 * 64, bar);
+                tma_load_2d(dst + kKBlockBytes + 64 * 128, ovf, 64, pg1 * 64, bar);
+              }
             }
           }
+          __syncwarp();
           return true;
         };
         ok = load(&k_map, &ko_map, it.t0);
-        for (int t = 0; ok && t < n; ++t) {  // K_0, V_0, K_1, V_1, ...
+        for (int t = 0; ok && t < n; ++t) {
           ok = load(&v_map, &vo_map, it.t0 + t);
           if (ok && t + 1 < n) ok = load(&k_map, &ko_map, it.t0 + t + 1);
         }
@@ -492,7 +505,8 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
           for (int part = 0; part < kParts; ++part)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              umma_bf16_ta(d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc_o, (part | kk) ? 1u : (fresh ? 0u : 1u));
+              umma_bf16_ta(kFlush && part ? d + 128 : d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc_o,
+                           kk || part > (kFlush ? 1 : 0) ? 1u : (fresh ? 0u : 1u));
           umma_commit(B(kDonePV + x));
         }
       };
@@ -579,37 +593,11 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
       const int sees = it.g.len - it.g.n_new + token + 1;  // rows that this thread's query sees
       const bool idle = !__any_sync(0xffffffffu, valid);   // no row of the warp is a query: it only keeps the barriers going
       const int tile = (blockIdx.x * 2 + (first_item ? 0 : 1)) * kTiles + x;  // of partial results
-      float4* const sum = a.part_o + (int64_t)tile * (32 * a.R) + lane_row;
       first_item = false;
       float ref = -INFINITY, l = 0.f, sum_ref = -INFINITY;
+      float sum[kFlush ? 128 : 1];
       for (int i = 0; alive && i < n; ++i, ++n_s) {
         const bool fresh = kFlush ? i % max(kFlush, 1) == 0 : i == 0;
-        if (kFlush && fresh && i > 0 && !idle) {
-          // what the tensor cores have added up since the last time goes to the sum in memory, which is requested before the products are waited for
-          const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f;
-          bool done = false;
-#pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 64) {
-            float4 m[16];
-#pragma unroll
-            for (int c = 0; c < 16; ++c) m[c] = i > kFlush && valid ? sum[(c0 / 4 + c) * a.R] : make_float4(0.f, 0.f, 0.f, 0.f);
-            // (this step's S was issued behind the products of the step but one before: behind it, the parity tells the last step's)
-            if (!done && !(alive = mbar_wait(B(kDoneS + 2 * x), n_s & 1, s_abort, a.spin_limit) && mbar_wait(B(kDonePV + x), 1, s_abort, a.spin_limit))) break;
-            done = true;
-            tc_fence_after();
-            float o[64];
-            tmem_ld64(acc + c0, o);
-            tmem_wait_ld64(o);
-#pragma unroll
-            for (int c = 0; c < 16; ++c)
-              if (valid)
-                sum[(c0 / 4 + c) * a.R] = make_float4(fmaf(m[c].x, f, o[4 * c]), fmaf(m[c].y, f, o[4 * c + 1]), fmaf(m[c].z, f, o[4 * c + 2]),
-                                                      fmaf(m[c].w, f, o[4 * c + 3]));
-          }
-          if (!alive) break;
-          sum_ref = ref;
-          tc_fence_before();
-        }
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
           if (!(alive = mbar_wait(B(kDoneS + 2 * x + h), n_s & 1, s_abort, a.spin_limit))) break;
@@ -629,7 +617,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
 #pragma unroll
             for (int c = 0; c < 64; ++c) y[c] = c < lim ? y[c] : -INFINITY;
           }
-          const float mx = ch_max<64>(y) * a.scale_log2;
+          const float mx = ch_max<64>(y) * a.scale_log2, ref_o = ref;
           const bool grow = mx > ref + kChTau;  // also the first step with a visible key
           if (__any_sync(0xffffffffu, grow)) {
             const float f = grow && ref > -INFINITY ? fast_exp2(ref - mx) : 1.f;
@@ -638,7 +626,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
               if (!(alive = mbar_wait(B(kDonePV + x), h ^ 1, s_abort, a.spin_limit))) break;
               tc_fence_after();
 #pragma unroll 1
-              for (int c0 = 0; c0 < 128; c0 += 32) {
+              for (int c0 = 0; c0 < (kFlush ? 256 : 128); c0 += 32) {
                 float o[32];
                 tmem_ld32(acc + c0, o);
                 tmem_wait_ld32(o);
@@ -652,6 +640,26 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
           const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
           l += ch_probs32<kParts>(y, a.scale_log2, neg, slot, 32);
           l += ch_probs32<kParts>(y + 32, a.scale_log2, neg, slot + 16, 32);
+          if (kFlush && h == 0 && fresh && i > 0) {  // what the tensor cores have added up since the last time
+            // (this step's S was issued behind the products of the step but one before: behind it, the parity tells the last step's)
+            if (!(alive = mbar_wait(B(kDonePV + x), 1, s_abort, a.spin_limit))) break;
+            tc_fence_after();
+            const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref_o) : 0.f;
+#pragma unroll
+            for (int c0 = 0; c0 < 128; c0 += 16) {
+              float o[16], o1[16];
+              tmem_ld16(acc + c0, o);
+              tmem_ld16(acc + 128 + c0, o1);
+              tmem_wait_ld16(o);
+              tmem_wait_ld16(o1);
+#pragma unroll
+              for (int c = 0; c < 16; ++c) {
+                const float z = o[c] + o1[c];
+                if constexpr (kFlush > 0) sum[c0 + c] = i > kFlush ? fmaf(sum[c0 + c], f, z) : z;
+              }
+            }
+            sum_ref = ref_o;
+          }
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -670,22 +678,20 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
       const int b = it.seg / a.Hkv, h = it.seg - b * a.Hkv;
       const int64_t orow = (int64_t)(sq.start[b] + token) * a.Hq + h * a.G + (row - tok * a.G);
       const float fs = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f;
+      float4* const part = a.part_o + (int64_t)tile * (32 * a.R) + lane_row;
       const float inv = whole ? (l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l)) : 1.f;  // a NaN stays one
       if (!idle) {
-#pragma unroll 1
+#pragma unroll(kFlush ? 4 : 1)
         for (int c0 = 0; c0 < 128; c0 += 32) {
           float o[32];
           tmem_ld32(acc + c0, o);
           tmem_wait_ld32(o);
-          if (summed && valid) {
+          if constexpr (kFlush > 0) {
+            float o1[32];
+            tmem_ld32(acc + 128 + c0, o1);
+            tmem_wait_ld32(o1);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              const float4 m = sum[(c0 / 4 + c) * a.R];
-              o[4 * c] = fmaf(m.x, fs, o[4 * c]);
-              o[4 * c + 1] = fmaf(m.y, fs, o[4 * c + 1]);
-              o[4 * c + 2] = fmaf(m.z, fs, o[4 * c + 2]);
-              o[4 * c + 3] = fmaf(m.w, fs, o[4 * c + 3]);
-            }
+            for (int c = 0; c < 32; ++c) o[c] = summed ? fmaf(sum[c0 + c], fs, o[c] + o1[c]) : o[c] + o1[c];
           }
           if (odd < sees && valid) {  // infinities and NaN that were taken out of the V tiles
             const int off = a.seg_off[it.seg], cap = a.seg_cap[it.seg];
@@ -706,7 +712,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
           if (valid) {
             if (!whole) {
 #pragma unroll
-              for (int c = 0; c < 8; ++c) sum[(c0 / 4 + c) * a.R] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+              for (int c = 0; c < 8; ++c) part[(c0 / 4 + c) * a.R] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
             } else if (kFlush) {
               float* dst = reinterpret_cast<float*>(a.out) + orow * kD + c0;
 #pragma unroll
@@ -1051,7 +1057,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   const int G = Hq / cache->Hkv;
   if (G > kMaxG || (out_dtype != CATEKV_OUT_BF16 && out_dtype != CATEKV_OUT_FP32)) return CATEKV_ERR_UNSUPPORTED;
   const int n_segs = cache->B * cache->Hkv;
-  const bool two = ch_two_tiles(G, max_new);
+  const bool two = out_dtype == CATEKV_OUT_BF16 && ch_two_tiles(G, max_new);
   const int TB = (two ? 256 : 128) / G;
   int64_t units = 0;
   for (int s = 0; s < n_segs; ++s) {
@@ -1108,8 +1114,9 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   }
   const int ctas = (int)(units < sm_count() ? units : sm_count());
   cudaStream_t st = (cudaStream_t)stream;
-  if (a.out_fp32) rc = two ? launch_chunk<true, 2, 4>(ctas, m, a, sq, st) : launch_chunk<false, 3, 4>(ctas, m, a, sq, st);
-  else rc = two ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st) : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
+  rc = a.out_fp32 ? launch_chunk<false, 3, 3>(ctas, m, a, sq, st)
+       : two      ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st)
+                  : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
   if (rc) return rc;
   CATEKV_CUDA_TRY(launch_pdl(chunk_combine_kernel, dim3(ctas, ((two ? 256 : W.R) + kChCombineRows - 1) / kChCombineRows), dim3(256), 0, st, a, sq, ctas,
                              two ? 1 : 0));
