@@ -751,11 +751,17 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
 }
 
 // Merge the pieces of the blocks that several CTAs share, in the order of the keys: CTA c's descriptor says whether its share
-// begins inside a block; the first such CTA of a block has it merged.  A thread block takes 32 rows (a lane a row, a warp every eighth float4 of
-// d), and writes them through shared memory row by row.
-constexpr int kChCombineRows = 32;
-__global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq, int C, int two) {
-  __shared__ float s_o[kChCombineRows][kD + 4];
+// begins inside a block; the first such CTA of a block has it merged.  A thread block takes kRows rows and 32 float4 of d; what threads are left
+// share out the pieces (few rows of one long list come in up to 148), and the groups' sums are added in their order.  Bound by its
+// trips to memory: descriptor, references and sums of all pieces, the pieces.
+constexpr int kChCombineThreads = 1024;
+template <int kRows>
+__global__ void __launch_bounds__(kChCombineThreads) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq,
+                                                                          int C, int two) {
+  constexpr int kGroups = kChCombineThreads / (kRows * 32);
+  __shared__ float4 s_o[kGroups][kRows][33];
+  __shared__ float s_l[kGroups][kRows];
+  __shared__ float s_m[32][kRows];
   pdl_launch_dependents();
   pdl_wait();
   const int c = blockIdx.x;
@@ -767,63 +773,91 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
   auto begin = [&](int i) { return i * q + min(i, r); };
   const int ub = begin(c) - p0, ue = ub + nt + kChCharge;  // the block's units
   if (ch_tile_at(begin(c - 1) - ub) > 0) return;  // an earlier CTA begins inside this block
-  int c_end = c + 1;
-  while (c_end < C && begin(c_end) < ue) ++c_end;
+  // the CTAs that begin before its end: begin(k) < ue
+  int c_end = q ? (ue > r * (q + 1) ? r + (ue - r * (q + 1) + q - 1) / q : (ue + q) / (q + 1)) : min(ue, C);
+  c_end = min(c_end, C);
   const int head = begin(c - 1) < ub ? 1 : 0;  // the first piece: the last block of CTA c - 1, or its only one
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b = seg / a.Hkv, h = seg - b * a.Hkv;
-  const int row0 = blockIdx.y * kChCombineRows, row = row0 + lane, x = row0 >> 7;  // row of the block; its M tile
+  const int row0 = blockIdx.y * kRows, x = row0 >> 7;  // row of the block; its M tile
   if (blk * a.TB + row0 / a.G >= n_new) return;
-  const bool valid = row / a.G < a.TB && blk * a.TB + row / a.G < n_new;
   auto tile = [&](int k) {
     const int i = k == c - 1 ? head : 0;
     return (int64_t)(two ? (k * 2 + i) * 2 + x : k * 2 + i);
   };
-  float M = -INFINITY, L = 0.f;
-  float4 acc[4];
+  const int i_row = threadIdx.x % kRows, c4 = threadIdx.x / kRows % 32, group = threadIdx.x / (kRows * 32);
+  const int row = row0 + i_row, in_tile = row & 127, n = c_end - (c - 1);
+  const bool valid = row / a.G < a.TB && blk * a.TB + row / a.G < n_new;
+  // the rows' largest reference
+  float M = -INFINITY;
+  if (valid)
+    for (int k = group * 32 + c4; k < n; k += kGroups * 32) M = fmaxf(M, a.part_ml[tile(c - 1 + k) * a.R + in_tile].x);
+  if (kGroups > 1) {
+    if (group == 0) s_m[c4][i_row] = M;
+    for (int g = 1; g < kGroups; ++g) {
+      __syncthreads();
+      if (group == g) s_m[c4][i_row] = fmaxf(s_m[c4][i_row], M);
+    }
+  } else {
+    s_m[c4][i_row] = M;
+  }
+  __syncthreads();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][i_row]);
+  float L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int k_lo = n * group / kGroups, k_hi = n * (group + 1) / kGroups;
   if (valid) {
-    for (int k = c - 1; k < c_end; ++k) M = fmaxf(M, a.part_ml[tile(k) * a.R + (row & 127)].x);
-#pragma unroll 2
-    for (int k = c - 1; k < c_end; ++k) {
-      const float2 ml = a.part_ml[tile(k) * a.R + (row & 127)];
-      const float4* p = a.part_o + tile(k) * (32 * a.R) + (row & 127);
-      float4 v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = p[(warp + 8 * j) * a.R];
+#pragma unroll 4
+    for (int k = k_lo; k < k_hi; ++k) {
+      const int64_t t = tile(c - 1 + k);
+      const float2 ml = a.part_ml[t * a.R + in_tile];
+      const float4 v = a.part_o[t * (32 * a.R) + c4 * a.R + in_tile];
       // a row that sees none of this piece's keys has nothing to add, or the NaN that it has met
       const float w = ml.x > -INFINITY ? exp2f(ml.x - M) : (ml.y == 0.f ? 0.f : 1.f);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        acc[j].x = fmaf(w, v[j].x, acc[j].x);
-        acc[j].y = fmaf(w, v[j].y, acc[j].y);
-        acc[j].z = fmaf(w, v[j].z, acc[j].z);
-        acc[j].w = fmaf(w, v[j].w, acc[j].w);
-      }
+      acc.x = fmaf(w, v.x, acc.x);
+      acc.y = fmaf(w, v.y, acc.y);
+      acc.z = fmaf(w, v.z, acc.z);
+      acc.w = fmaf(w, v.w, acc.w);
       L = fmaf(w, ml.y, L);
     }
-    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<float4*>(&s_o[lane][(warp + 8 * j) * 4]) = make_float4(acc[j].x * inv, acc[j].y * inv, acc[j].z * inv, acc[j].w * inv);
   }
-  auto out_row = [&](int i) { return (int64_t)(sq.start[b] + blk * a.TB + i / a.G) * a.Hq + h * a.G + i % a.G; };
-  if (valid && warp == 0 && a.lse) a.lse[out_row(row)] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  s_o[group][i_row][c4] = acc;
+  if (c4 == 0) s_l[group][i_row] = L;
   __syncthreads();
-  for (int i = warp; i < kChCombineRows; i += 8) {
+  // a warp a row now: its lanes write it side by side
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = warp; i < kRows; i += kChCombineThreads / 32) {
     const int tok = (row0 + i) / a.G;
-    if (tok >= a.TB || blk * a.TB + tok >= n_new) break;
-    const float4 v = *reinterpret_cast<const float4*>(&s_o[i][lane * 4]);
+    if (tok >= a.TB || blk * a.TB + tok >= n_new) continue;
+    float4 v = s_o[0][i][lane];
+    L = s_l[0][i];
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) {
+      const float4 y = s_o[g][i][lane];
+      v = make_float4(v.x + y.x, v.y + y.y, v.z + y.z, v.w + y.w);
+      L += s_l[g][i];
+    }
+    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+    const int64_t orow = (int64_t)(sq.start[b] + blk * a.TB + tok) * a.Hq + h * a.G + (row0 + i) % a.G;
     if (a.out_fp32) {
-      reinterpret_cast<float4*>(a.out)[out_row(row0 + i) * 32 + lane] = v;
+      reinterpret_cast<float4*>(a.out)[orow * 32 + lane] = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
     } else {
       uint2 pk;
-      pk.x = pack_bf16(v.x, v.y);
-      pk.y = pack_bf16(v.z, v.w);
-      reinterpret_cast<uint2*>(a.out)[out_row(row0 + i) * 32 + lane] = pk;
+      pk.x = pack_bf16(v.x * inv, v.y * inv);
+      pk.y = pack_bf16(v.z * inv, v.w * inv);
+      reinterpret_cast<uint2*>(a.out)[orow * 32 + lane] = pk;
+    }
+    if (lane == 0 && a.lse) {
+      float m = s_m[0][i];
+      for (int k = 1; k < 32; ++k) m = fmaxf(m, s_m[k][i]);
+      a.lse[orow] = L == 0.f ? -INFINITY : (m + log2f(L)) * 0.6931471805599453f;
     }
   }
+}
+template <int kRows>
+static cudaError_t launch_combine(const ChunkArgs& a, const ChunkSeqs& sq, int ctas, bool two, cudaStream_t st) {
+  return launch_pdl(chunk_combine_kernel<kRows>, dim3(ctas, ((two ? 256 : a.R) + kRows - 1) / kRows), dim3(kChCombineThreads), 0, st, a, sq, ctas,
+                    two ? 1 : 0);
 }
 
 // ---- append: the chunk's rows behind the end of every list.  A warp copies a row (lanes 0-15 K, 16-31 V), eight in flight.
@@ -1118,7 +1152,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
        : two      ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st)
                   : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
   if (rc) return rc;
-  CATEKV_CUDA_TRY(launch_pdl(chunk_combine_kernel, dim3(ctas, ((two ? 256 : W.R) + kChCombineRows - 1) / kChCombineRows), dim3(256), 0, st, a, sq, ctas,
-                             two ? 1 : 0));
+  CATEKV_CUDA_TRY(a.R <= 4 ? launch_combine<4>(a, sq, ctas, two, st) : a.R <= 8 ? launch_combine<8>(a, sq, ctas, two, st)
+                                                                               : launch_combine<32>(a, sq, ctas, two, st));
   return CATEKV_OK;
 }
