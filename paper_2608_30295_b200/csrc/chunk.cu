@@ -23,8 +23,8 @@
 // own, 2^-9 as large, and both are added, with rounding, to a sum in the thread's registers every kFlush tiles, where the products start from zero
 // (relative error of 64K rows: 5e-6 with one accumulator and a flush every 16 tiles).  That takes one M tile, whatever the number of rows.
 //
-// Rows of a V tile that no query of the block sees are zeroed in shared memory before the product reads them (what lies behind a list
-// may be NaN, and 0 * NaN is not 0); an infinity or a NaN in a new row, which later tokens see and earlier ones do not, is taken
+// The product with V stops at the 16 keys that hold the last row that a query of the block sees; of these, rows behind it are zeroed in shared
+// memory (what lies behind a list may be NaN, and 0 * NaN is not 0); an infinity or a NaN in a new row, which later tokens see and earlier ones do not, is taken
 // out there too and added to the rows that see it at the end.
 //
 // Warps: four per M tile for the softmax; then one each for tensor-core issue, K / V tiles by TMA into one ring in the order of use,
@@ -90,14 +90,19 @@ struct ChunkArgs {
 };
 
 struct ChunkSeg {  // one list as the schedule sees it
-  int32_t len, n_new, n_blk;
+  int32_t len, n_new, n_blk, off, cap;
 };
-__device__ __forceinline__ ChunkSeg ch_seg(const ChunkArgs& a, const ChunkSeqs& sq, int s) {
-  ChunkSeg g;
-  g.n_new = sq.n_new[s / a.Hkv];
+__device__ __forceinline__ void ch_set_len(const ChunkArgs& a, ChunkSeg& g, int s) {
+  g.len = min(max(a.seg_len[s], 0), g.cap + CATEKV_PAGE_ROWS * a.max_pages);
+}
+__device__ __forceinline__ ChunkSeg ch_seg(const ChunkArgs& a, const ChunkSeqs& sq, int s, bool with_len) {
+  ChunkSeg g = {0, sq.n_new[s / a.Hkv], 0, 0, 0};
   g.n_blk = (g.n_new + a.TB - 1) / a.TB;
-  g.len = g.n_blk ? max(a.seg_len[s], 0) : 0;
-  if (g.n_blk) g.len = min(g.len, a.seg_cap[s] + CATEKV_PAGE_ROWS * a.max_pages);
+  if (g.n_blk) {
+    g.off = a.seg_off[s];
+    g.cap = a.seg_cap[s];
+    if (with_len) ch_set_len(a, g, s);
+  }
   return g;
 }
 // key tiles of a block (at least one, so that rows that see nothing get their output)
@@ -121,7 +126,7 @@ struct ChunkWalk {
     if (left <= 0) return false;
     while (blk >= g.n_blk) {
       if (++seg >= a.n_segs) return false;
-      g = ch_seg(a, sq, seg);
+      g = ch_seg(a, sq, seg, true);
       blk = 0;
     }
     it.seg = seg;
@@ -220,6 +225,8 @@ __device__ __forceinline__ float ch_probs32(const float* x, float scale, float n
   return s0.x + s0.y;
 }
 
+// rows of a V tile that the product takes, where `seen` rows from its first on are seen (at least one step, so that the accumulator is written)
+__device__ __forceinline__ int ch_v_rows(int seen) { return min(max((seen + 15) & ~15, 16), kKeyTile); }
 // pool row of row r of a list, or of its overflow pages (page < 0: not there)
 __device__ __forceinline__ int ch_page(const ChunkArgs& a, int seg, int o) {
   const int p = o >> 6;
@@ -241,7 +248,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
   constexpr int kQBytes = kTiles * kChTileBytes, kQBlock = kQBytes / 2;
   static_assert(kParts * 32 <= Sh::kSlotCols, "P fits its slot");
   extern __shared__ uint8_t smem_raw[];
-  __shared__ int s_scan[kWarps + 4];
+  __shared__ int s_scan[kWarps], s_first[8];
   const int tid = threadIdx.x, warp = uni(tid >> 5), lane = tid & 31;
   const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (s_base - smem_u32(smem_raw));
@@ -269,37 +276,47 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(s_tmem)), "r"(kChTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
+  if (tid == kSoft * 32 + 32) {
+    const CUtensorMap* maps[5] = {&k_map, &v_map, &q_map, &ko_map, &vo_map};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) asm volatile("prefetch.tensormap [%0];\n" ::"l"(maps[i]) : "memory");
+  }
+  // The list of this thread: all but its length is there before the kernels ahead have finished.
+  ChunkSeg mine = {0, 0, 0, 0, 0};
+  if (tid < a.n_segs) mine = ch_seg(a, sq, tid, false);
   pdl_wait();
 
   // ---- this CTA's share of the tiles of all blocks
   int total = 0, u0 = 0, u1 = 0;
   {
-    auto cost_of = [&](int s) {
-      const ChunkSeg g = ch_seg(a, sq, s);
+    auto cost_of = [&](const ChunkSeg& g) {
       int c = 0;
       for (int j = 0; j < g.n_blk; ++j) c += ch_tiles(a, g, j) + kChCharge;
       return c;
     };
-    int mine = 0;
-    for (int s = tid; s < a.n_segs; s += Sh::kThreads) mine += cost_of(s);
-    int x = mine;
+    if (mine.n_blk) ch_set_len(a, mine, tid);
+    const int cost0 = cost_of(mine);
+    int x = cost0;
+    for (int s = tid + Sh::kThreads; s < a.n_segs; s += Sh::kThreads) x += cost_of(ch_seg(a, sq, s, true));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     if (lane == 0) s_scan[warp] = x;
-    if (tid == 0) s_scan[kWarps] = a.n_segs;  // no tile: nothing to do
+    if (tid == 0) {
+      s_first[0] = a.n_segs;               // no tile: nothing to do
+      a.desc[blockIdx.x * 8 + 2] = 0;      // (no cut at the start of a share, unless there is one)
+    }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) total += s_scan[w];
-    const int C = gridDim.x, c = blockIdx.x, q = total / C, r = total % C;
+    const int C = gridDim.x, c = blockIdx.x, q = total / C, r = total - q * C;
     u0 = c * q + min(c, r);
     u1 = u0 + q + (c < r ? 1 : 0);
-    if (tid == 0) a.desc[c * 8 + 2] = 0;  // (no cut at the start of a share, unless there is one)
     int before = 0;
     for (int s0 = 0; s0 < a.n_segs; s0 += Sh::kThreads) {
       __syncthreads();
       const int s = s0 + tid;
-      int cost = 0;
-      if (s < a.n_segs) cost = a.n_segs <= Sh::kThreads ? mine : cost_of(s);
+      if (s0 > 0) mine = s < a.n_segs ? ch_seg(a, sq, s, true) : ChunkSeg{0, 0, 0, 0, 0};
+      const int cost = s0 > 0 ? cost_of(mine) : cost0;
       int inc = cost;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -315,22 +332,22 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
         before += s_scan[w];
       }
       if (u1 > u0 && u0 >= ex && u0 < ex + cost) {
-        const ChunkSeg g = ch_seg(a, sq, s);
-        int p = u0 - ex, j = 0, nt = ch_tiles(a, g, 0);
+        int p = u0 - ex, j = 0, nt = ch_tiles(a, mine, 0);
         while (p >= nt + kChCharge) {
           p -= nt + kChCharge;
-          nt = ch_tiles(a, g, ++j);
+          nt = ch_tiles(a, mine, ++j);
         }
-        s_scan[kWarps] = s;
-        s_scan[kWarps + 1] = j;
-        s_scan[kWarps + 2] = p;
-        int32_t* d = a.desc + c * 8;
-        d[0] = s;
-        d[1] = j;
-        d[2] = p;
-        d[3] = nt;
-        d[4] = g.n_new;
-        d[5] = total;
+        s_first[0] = s;
+        s_first[1] = j;
+        s_first[2] = p;
+        s_first[3] = mine.len;
+        s_first[4] = mine.n_new;
+        s_first[5] = mine.n_blk;
+        s_first[6] = mine.off;
+        s_first[7] = mine.cap;
+        int4* d = reinterpret_cast<int4*>(a.desc + c * 8);
+        d[0] = make_int4(s, j, p, nt);
+        d[1] = make_int4(mine.n_new, total, 0, 0);
       }
     }
   }
@@ -340,11 +357,10 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
   const uint32_t tmem = *s_tmem;
   ChunkWalk walk;
   walk.left = u1 - u0;
-  walk.seg = s_scan[kWarps];
-  walk.blk = s_scan[kWarps + 1];
-  walk.p = s_scan[kWarps + 2];
-  walk.g = ChunkSeg{0, 0, 0};
-  if (walk.left > 0) walk.g = ch_seg(a, sq, walk.seg);
+  walk.seg = s_first[0];
+  walk.blk = s_first[1];
+  walk.p = s_first[2];
+  walk.g = ChunkSeg{s_first[3], s_first[4], s_first[5], s_first[6], s_first[7]};
   ChunkItem it;
 
   if (warp >= kSoft) {
@@ -356,7 +372,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
       bool ok = true;
       while (ok && walk.next(a, sq, it)) {
         const int n = it.t1 - it.t0;
-        const int off = a.seg_off[it.seg], cap = a.seg_cap[it.seg];
+        const int off = it.g.off, cap = it.g.cap;
         int window = -64, entry = -1;  // lane i holds the list's page window + i
         auto load = [&](const CUtensorMap* pool, const CUtensorMap* ovf, int t) {
           const int st = use % kStages;
@@ -444,9 +460,10 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
         }
         uint8_t* tile = smem + kQBytes + st * kChTileBytes;
         int odd = 0x7fffffff;
+        const int end = ch_v_rows(last - r0);
 #pragma unroll 4
-        for (int i = 0; i < 64; ++i) {
-          const int r = i * 2 + (lane >> 4), c = lane & 15, j = r0 + r;
+        for (int r = max(first - r0, 0) + (lane >> 4); r < end; r += 2) {
+          const int c = lane & 15, j = r0 + r;
           uint4* p = reinterpret_cast<uint4*>(tile + sw128_off(r, c, 128));
           if (j >= last) {
             *p = make_uint4(0u, 0u, 0u, 0u);
@@ -497,7 +514,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
           umma_commit(B(kDoneS + 2 * x + h));
         }
       };
-      auto issue_o = [&](int x, int h, int st, bool fresh) {
+      auto issue_o = [&](int x, int h, int st, bool fresh, int rows) {
         const uint64_t dv = dv0 + (uint64_t)(st * (kChTileBytes >> 4) + h * (64 * 128 >> 4));
         const uint32_t d = tm + 256 + x * 128, p = tm + (2 * x + h) * Sh::kSlotCols;
         if (elect_one()) {
@@ -505,7 +522,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
           for (int part = 0; part < kParts; ++part)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              umma_bf16_ta(kFlush && part ? d + 128 : d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc_o,
+              if (64 * h + 16 * kk < rows) umma_bf16_ta(kFlush && part ? d + 128 : d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc_o,
                            kk || part > (kFlush ? 1 : 0) ? 1u : (fresh ? 0u : 1u));
           umma_commit(B(kDonePV + x));
         }
@@ -513,6 +530,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
       while (ok && walk.next(a, sq, it)) {
         const int t0 = uni(it.t0), n = uni(it.t1) - t0;
         const int first = uni(it.g.len - it.g.n_new + it.blk * a.TB + 1);
+        const int last = uni(it.g.len - it.g.n_new + min(it.g.n_new, a.TB * (it.blk + 1)));
         if (!(ok = warp_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit))) break;
         ++n_item;
         if (!(ok = wait_tile())) break;
@@ -530,7 +548,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
         for (int t = 0; ok && t < n; ++t, ++n_p) {
           const bool look = (t0 + t + 1) * kKeyTile > first, more = t + 1 < n;
           const bool fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
-          const int sv = use % kStages, sk = (use + 1) % kStages;
+          const int sv = use % kStages, sk = (use + 1) % kStages, rows = ch_v_rows(last - (t0 + t) * kKeyTile);
           bool k_there = false;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -548,7 +566,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
               }
               if (!ok) break;
               tc_fence_after();
-              issue_o(x, h, sv, fresh && h == 0);
+              issue_o(x, h, sv, fresh && h == 0, rows);
               if (h == 1 && x == kTiles - 1) commit(kEmpty + sv);
               const bool last = h == 1 && x == kTiles - 1;  // of the tile
               const int xn = x + 1 < kTiles ? x + 1 : 0, hn = x + 1 < kTiles ? h : h ^ 1;
@@ -694,7 +712,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
             for (int c = 0; c < 32; ++c) o[c] = summed ? fmaf(sum[c0 + c], fs, o[c] + o1[c]) : o[c] + o1[c];
           }
           if (odd < sees && valid) {  // infinities and NaN that were taken out of the V tiles
-            const int off = a.seg_off[it.seg], cap = a.seg_cap[it.seg];
+            const int off = it.g.off, cap = it.g.cap;
             for (int j = max(odd, it.t0 * kKeyTile); j < min(sees, it.t1 * kKeyTile); ++j) {
               const uint16_t* v = a.v_pool + (int64_t)(off + j) * kD;
               if (j >= cap) {
