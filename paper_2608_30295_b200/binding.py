@@ -846,9 +846,8 @@ def catekv_chunk_attn(cache: Cache, chunk: Chunk, q: torch.Tensor, out: torch.Te
 
 def _per_sequence(where: str, cache: Cache, x) -> np.ndarray:
     x = np.asarray(x).reshape(-1)
-    if x.size != cache.B:
+    if x.size != cache.B or x.min() < 0 or x.max() >= 2 ** 31:  # (the C ABI's int32)
         raise CatekvError(ERR_INVALID_ARG, where)
-    _int32(where, *(int(i) for i in x))
     return np.ascontiguousarray(x, dtype=np.int32)
 
 

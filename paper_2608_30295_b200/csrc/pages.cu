@@ -25,8 +25,10 @@ struct PageOp {  // kind | count << 3, and what the kind says
 enum PageOpKind {
   kOpSegment = 0,   // segment `count`: off = a, cap = b, len = c (c < 0: as it is)
   kOpTable = 1,     // `count` (1 or 2) table entries from index a on: b, c
-  kOpCopyPool = 2,  // `count` rows from pool row a to overflow row b
-  kOpCopyPage = 3,  // `count` rows from overflow row a to overflow row b; c >= 0: table entry c names the page of b
+  kOpCopyPool = 2,  // `count` rows from pool row a to overflow row b; table entry c names the page of b
+  kOpCopyPage = 3,  // `count` rows from overflow row a to overflow row b; table entry c names the page of b
+  kOpTableCopy = 4, // `count` table entries from index a on are those from index b on
+  kOpTableRun = 5,  // `count` table entries from index a on are the pages b, b + 1, ...
 };
 struct PageTargets {
   uint8_t *k_pool, *v_pool, *k_ovf, *v_ovf;
@@ -38,7 +40,9 @@ struct PageOps {
   int32_t n_copy, n_set;  // the copies come first
   PageOp op[kN];
 };
-constexpr int kFewOps = 224, kManyOps = 1984;  // arguments of 3.7 KB, or as many as a launch takes (32 KB)
+// Arguments of up to 3.6 KB, or as many as a launch takes (32 KB: 5 us more of the host's time).
+constexpr int kFewBytes = 3584, kManyBytes = 31744;
+constexpr int kFewOps = kFewBytes / 16, kManyOps = kManyBytes / 16;
 
 // A block copies up to 64 rows of K and V, or 256 threads set one thing each.
 template <int kN>
@@ -62,7 +66,7 @@ __global__ void __launch_bounds__(256) page_ops_kernel(const __grid_constant__ P
       const int r = (tid >> 5) + 8 * i;
       if (r < rows) *reinterpret_cast<uint4*>(dst + (int64_t)r * kRowBytes) = v[i];
     }
-    if (tid == 0 && (o.kind & 7) == kOpCopyPage && o.c >= 0) t.table[o.c] = o.b / CATEKV_PAGE_ROWS;
+    if (tid == 0) t.table[o.c] = o.b / CATEKV_PAGE_ROWS;
     return;
   }
   const int i = ((int)blockIdx.x - ops.n_copy) * 256 + tid;
@@ -74,10 +78,45 @@ __global__ void __launch_bounds__(256) page_ops_kernel(const __grid_constant__ P
     t.seg_cap[n] = o.b;
     if (t.seg_cap2) t.seg_cap2[n] = o.b;
     if (o.c >= 0) t.seg_len[n] = o.c;
-  } else {
+  } else if ((o.kind & 7) == kOpTable) {
     t.table[o.a] = o.b;
     if (n > 1) t.table[o.a + 1] = o.c;
+  } else {
+    for (int j = 0; j < n; ++j) t.table[o.a + j] = (o.kind & 7) == kOpTableRun ? o.b + j : t.table[o.b + j];
   }
+}
+
+// Pages that move: page src[i] -> dst[i], src ascending, every dst below every src.  A block copies a page; the blocks behind those
+// look every table entry up among the sources.
+template <class T, int kBytes>
+struct PageMoves {
+  static constexpr int kRoom = kBytes / (2 * (int)sizeof(T));
+  int32_t n, n_entries;
+  T src[kRoom], dst[kRoom];
+};
+template <class T, int kBytes>
+__global__ void __launch_bounds__(256) page_moves_kernel(const __grid_constant__ PageTargets t, const __grid_constant__ PageMoves<T, kBytes> m) {
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x < m.n) {
+    constexpr int kChunks = CATEKV_PAGE_ROWS * kRowBytes / 16;  // of K, and of V
+    const int64_t src = (int64_t)m.src[blockIdx.x] * kChunks, dst = (int64_t)m.dst[blockIdx.x] * kChunks;
+    uint4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = reinterpret_cast<const uint4*>(i < 4 ? t.k_ovf : t.v_ovf)[src + tid + (i & 3) * 256];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(i < 4 ? t.k_ovf : t.v_ovf)[dst + tid + (i & 3) * 256] = v[i];
+    return;
+  }
+  const int e = ((int)blockIdx.x - m.n) * 256 + tid;
+  if (e >= m.n_entries) return;
+  const int page = t.table[e];
+  int lo = 0, hi = m.n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if ((int)m.src[mid] < page) lo = mid + 1;
+    else hi = mid;
+  }
+  if (lo < m.n && (int)m.src[lo] == page) t.table[e] = (int)m.dst[lo];
 }
 
 constexpr int kDropSeqs = 512;
@@ -122,11 +161,18 @@ struct HostList {
 
 struct PageOrders {
   HostList<PageOp> copies, sets;
-  bool copy_rows(bool pool, int64_t src, int64_t dst, int rows, int entry) {
-    return copies.push(PageOp{(pool ? kOpCopyPool : kOpCopyPage) | rows << 3, (int32_t)src, (int32_t)dst, entry});
+  // `rows` rows to the start of a page, which table entry `entry` names from now on
+  bool copy_rows(bool pool, int64_t src, int page, int rows, int64_t entry) {
+    return copies.push(PageOp{(pool ? kOpCopyPool : kOpCopyPage) | rows << 3, (int32_t)src, page * CATEKV_PAGE_ROWS, (int32_t)entry});
   }
   bool segment(int s, int off, int cap, int len) { return sets.push(PageOp{kOpSegment | s << 3, off, cap, len}); }
+  bool entries_of(int64_t at, int64_t from, int n) {  // as the device's table has them
+    return n == 0 || sets.push(PageOp{kOpTableCopy | n << 3, (int32_t)at, (int32_t)from, 0});
+  }
   bool entries(int64_t at, const int32_t* v, int n) {
+    int run = 1;
+    while (run < n && v[run] == v[0] + run) ++run;
+    if (run == n && n > 2) return sets.push(PageOp{kOpTableRun | n << 3, (int32_t)at, v[0], 0});
     for (int i = 0; i < n; i += 2)
       if (!sets.push(PageOp{kOpTable | (i + 1 < n ? 2 : 1) << 3, (int32_t)(at + i), v[i], i + 1 < n ? v[i + 1] : 0})) return false;
     return true;
@@ -143,7 +189,7 @@ static int send_batch(const PageTargets& t, const PageOp* copies, int nc, const 
   CATEKV_CUDA_TRY(cudaGetLastError());
   return CATEKV_OK;
 }
-static int send(const catekv_cache* c, PageOrders& o, cudaStream_t st) {
+static PageTargets targets(const catekv_cache* c) {
   const catekv_pages* p = c->pages;
   PageTargets t = {};
   t.k_pool = (uint8_t*)c->k_pool;
@@ -155,6 +201,10 @@ static int send(const catekv_cache* c, PageOrders& o, cudaStream_t st) {
   t.seg_cap = const_cast<int32_t*>(p->seg_cap_dev);
   t.seg_cap2 = c->seg_cap_dev != p->seg_cap_dev ? const_cast<int32_t*>(c->seg_cap_dev) : nullptr;
   t.seg_len = c->seg_len_dev;
+  return t;
+}
+static int send(const catekv_cache* c, PageOrders& o, cudaStream_t st) {
+  const PageTargets t = targets(c);
   size_t ic = 0, is = 0;
   while (ic < o.copies.n || is < o.sets.n) {
     const size_t left = o.copies.n - ic + o.sets.n - is, room = left <= kFewOps ? kFewOps : kManyOps;
@@ -193,6 +243,21 @@ static void settle(catekv_pages* p, const HostList<int32_t>& count) {
     }
   p->next_free = top;
   p->released = top - live;
+}
+template <class T, int kBytes>
+static int send_moves(const catekv_cache* c, const int32_t* src, const int32_t* dst, size_t n, cudaStream_t st) {
+  PageMoves<T, kBytes> m;
+  m.n_entries = c->B * c->Hkv * c->pages->max_pages;
+  for (size_t i0 = 0; i0 < n; i0 += m.kRoom) {
+    m.n = (int32_t)std::min(n - i0, (size_t)m.kRoom);
+    for (int i = 0; i < m.n; ++i) {
+      m.src[i] = (T)src[i0 + i];
+      m.dst[i] = (T)dst[i0 + i];
+    }
+    page_moves_kernel<T, kBytes><<<m.n + (m.n_entries + 255) / 256, 256, 0, st>>>(targets(c), m);
+    CATEKV_CUDA_TRY(cudaGetLastError());
+  }
+  return CATEKV_OK;
 }
 struct FreePages {  // the lowest pages that no list held when the call began, one after the other
   const HostList<int32_t>& count;
@@ -310,34 +375,40 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
   if (rc) return rc;
   FreePages free_pages{count};
   struct Child {
-    int32_t seg, off, cap, len, pages, at;  // its table entries: entries[at, at + pages)
+    int32_t seg, off, cap, len, full, fresh, page[2];  // shares `full` pages, then has `fresh` ones of its own
   };
   HostList<Child> children;
-  HostList<int32_t> entries;
+  HostList<int32_t> entries;  // of children whose parent is replaced itself: its row of the tables as it was
   PageOrders orders;
-  bool ok = true;
+  if (!children.reserve((size_t)replaced * Hkv) || !orders.copies.reserve((size_t)replaced * Hkv) || !orders.sets.reserve((size_t)replaced * Hkv * 2))
+    return CATEKV_ERR_WORKSPACE;
   for (int b = 0; b < B; ++b) {
     if (parent[b] == b) continue;
+    const bool moving = parent[parent[b]] != parent[b];
     for (int h = 0; h < Hkv; ++h) {
       const int s = b * Hkv + h, f = parent[b] * Hkv + h;
       const int len = cache->seg_len[f], cap = cache->seg_cap[f], off = cache->seg_off[f];
-      const int32_t* row = p->table + (size_t)f * p->max_pages;
-      Child c = {s, off, len <= cap ? len / CATEKV_SEG_ALIGN * CATEKV_SEG_ALIGN : cap, len, 0, (int32_t)entries.n};
-      const int full = len <= cap ? 0 : (len - cap) / CATEKV_PAGE_ROWS;  // pages of the parent that are full: read by both
-      for (int q = 0; q < full; ++q) ok = ok && entries.push(row[q]);
-      const int done = c.cap + full * CATEKV_PAGE_ROWS;
-      c.pages = full + div_up(len - done, CATEKV_PAGE_ROWS);
-      if (c.pages > p->max_pages) return CATEKV_ERR_CAPACITY;
-      for (int r = done; r < len; r += CATEKV_PAGE_ROWS) {
-        const int page = free_pages.take();
-        if (page < 0) return CATEKV_ERR_CAPACITY;
-        const bool pool = len <= cap;
-        ok = ok && entries.push(page) &&
-             orders.copy_rows(pool, pool ? (int64_t)off + r : (int64_t)row[full] * CATEKV_PAGE_ROWS, (int64_t)page * CATEKV_PAGE_ROWS,
-                              std::min(CATEKV_PAGE_ROWS, len - r), -1);
+      const bool pool = len <= cap;  // nothing in pages
+      const int64_t row = (int64_t)f * p->max_pages, to = (int64_t)s * p->max_pages;
+      Child c = {s, off, pool ? len / CATEKV_SEG_ALIGN * CATEKV_SEG_ALIGN : cap, len, pool ? 0 : (len - cap) / CATEKV_PAGE_ROWS, 0, {0, 0}};
+      const int done = c.cap + c.full * CATEKV_PAGE_ROWS;
+      c.fresh = div_up(len - done, CATEKV_PAGE_ROWS);
+      if (c.full + c.fresh > p->max_pages) return CATEKV_ERR_CAPACITY;
+      bool ok = true;
+      for (int i = 0; i < c.fresh; ++i) {
+        c.page[i] = free_pages.take();
+        if (c.page[i] < 0) return CATEKV_ERR_CAPACITY;
+        const int r = done + i * CATEKV_PAGE_ROWS;
+        ok = ok && orders.copy_rows(pool, pool ? (int64_t)off + r : (int64_t)p->table[row + c.full] * CATEKV_PAGE_ROWS, c.page[i],
+                                    std::min(CATEKV_PAGE_ROWS, len - r), to + c.full + i);
       }
-      ok = ok && children.push(c) && orders.segment(s, c.off, c.cap, c.len) &&
-           orders.entries((int64_t)s * p->max_pages, entries.p + c.at, c.pages);
+      ok = ok && children.push(c) && orders.segment(s, c.off, c.cap, c.len);
+      if (moving) {
+        ok = ok && orders.entries(to, p->table + row, c.full);
+        for (int q = 0; q < c.full; ++q) ok = ok && entries.push(p->table[row + q]);
+      } else {
+        ok = ok && orders.entries_of(to, row, c.full);
+      }
       if (!ok) return CATEKV_ERR_WORKSPACE;
     }
   }
@@ -346,16 +417,27 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
   if (!rc) rc = send(cache, orders, st);
   if (rc) return rc;
   int32_t *seg_off = const_cast<int32_t*>(cache->seg_off), *seg_cap = const_cast<int32_t*>(cache->seg_cap);
+  size_t at = 0;
+  for (int s = 0; s < n; ++s)  // what replaced parents held; the others' pages are not counted
+    if (parent[s / Hkv] != s / Hkv && !gone[s])
+      for (int q = 0; q < p->seg_pages[s]; ++q) --count[p->table[(size_t)s * p->max_pages + q]];
   for (size_t i = 0; i < children.n; ++i) {
     const Child& c = children[i];
+    const int b = c.seg / Hkv, from = parent[b] * Hkv + c.seg % Hkv;
+    int32_t* row = p->table + (size_t)c.seg * p->max_pages;
+    if (parent[parent[b]] != parent[b]) {
+      if (c.full) memcpy(row, entries.p + at, sizeof(int32_t) * (size_t)c.full);
+      at += (size_t)c.full;
+    } else if (c.full) {
+      memcpy(row, p->table + (size_t)from * p->max_pages, sizeof(int32_t) * (size_t)c.full);
+    }
+    for (int q = 0; q < c.fresh; ++q) row[c.full + q] = c.page[q];
     seg_off[c.seg] = c.off;
     seg_cap[c.seg] = c.cap;
     cache->seg_len[c.seg] = c.len;
-    p->seg_pages[c.seg] = c.pages;
-    if (c.pages) memcpy(p->table + (size_t)c.seg * p->max_pages, entries.p + c.at, sizeof(int32_t) * (size_t)c.pages);
+    p->seg_pages[c.seg] = c.full + c.fresh;
+    for (int q = 0; q < c.full + c.fresh; ++q) ++count[row[q]];
   }
-  rc = count_pages(cache, nullptr, count);
-  if (rc) return rc;
   settle(p, count);
   return CATEKV_OK;
 }
@@ -425,7 +507,7 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
           if (page < 0) return CATEKV_ERR_CAPACITY;
           c.entry[q] = page;
           ++count[page];
-          if (!orders.copy_rows(true, (int64_t)cache->seg_off[s] + r, (int64_t)page * CATEKV_PAGE_ROWS, std::min(CATEKV_PAGE_ROWS, len - r), -1))
+          if (!orders.copy_rows(true, (int64_t)cache->seg_off[s] + r, page, std::min(CATEKV_PAGE_ROWS, len - r), (int64_t)s * p->max_pages + q))
             return CATEKV_ERR_WORKSPACE;
         }
         cap[s] = c.cap;
@@ -438,10 +520,10 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
         c.first = kept - 1;
         c.n_entries = 1;
         c.entry[0] = page;
-        if (!orders.copy_rows(false, (int64_t)row[kept - 1] * CATEKV_PAGE_ROWS, (int64_t)page * CATEKV_PAGE_ROWS, (len - cap[s]) % CATEKV_PAGE_ROWS, -1))
+        if (!orders.copy_rows(false, (int64_t)row[kept - 1] * CATEKV_PAGE_ROWS, page, (len - cap[s]) % CATEKV_PAGE_ROWS,
+                              (int64_t)s * p->max_pages + kept - 1))
           return CATEKV_ERR_WORKSPACE;
       }
-      if (c.n_entries && !orders.entries((int64_t)s * p->max_pages + c.first, c.entry, c.n_entries)) return CATEKV_ERR_WORKSPACE;
       if (!changes.push(c)) return CATEKV_ERR_WORKSPACE;
     }
   }
@@ -480,41 +562,32 @@ extern "C" int catekv_pages_compact(catekv_cache* cache, int32_t* n_used, catekv
   if (rc) return rc;
   const int n = cache->B * cache->Hkv;
   catekv_pages* p = cache->pages;
-  HostList<int32_t> count, to;  // to: the copy that moves a page, or -1
+  HostList<int32_t> count, src, dst, to;  // to: where a page is afterwards
   rc = count_pages(cache, nullptr, count);
   if (rc) return rc;
   int live = 0;
   for (int q = 0; q < p->n_pages; ++q) live += count[q] > 0;
-  PageOrders orders;
-  if (!to.fill((size_t)p->n_pages, -1)) return CATEKV_ERR_WORKSPACE;
+  if (!to.reserve((size_t)p->n_pages) || !src.reserve((size_t)live) || !dst.reserve((size_t)live)) return CATEKV_ERR_WORKSPACE;
   int hole = 0;
-  for (int q = live; q < p->n_pages; ++q) {
-    if (!count[q]) continue;
+  for (int q = 0; q < p->n_pages; ++q) {
+    to.p[q] = q;
+    if (q < live || !count[q]) continue;
     while (count[hole]) ++hole;
-    to[q] = (int32_t)orders.copies.n;
-    if (!orders.copy_rows(false, (int64_t)q * CATEKV_PAGE_ROWS, (int64_t)hole * CATEKV_PAGE_ROWS, CATEKV_PAGE_ROWS, -1)) return CATEKV_ERR_WORKSPACE;
-    ++hole;
+    src.push(q);
+    dst.push(hole);
+    to.p[q] = hole++;
   }
   cudaStream_t st = (cudaStream_t)stream;
-  if (orders.copies.n) {
-    for (int s = 0; s < n; ++s) {
-      const int32_t* row = p->table + (size_t)s * p->max_pages;
-      for (int q = 0; q < p->seg_pages[s]; ++q) {
-        const int i = to[row[q]];
-        if (i < 0) continue;
-        const int32_t page = orders.copies[i].b / CATEKV_PAGE_ROWS;
-        const int64_t at = (int64_t)s * p->max_pages + q;
-        if (count[row[q]] == 1) orders.copies[i].c = (int32_t)at;
-        else if (!orders.entries(at, &page, 1)) return CATEKV_ERR_WORKSPACE;
-      }
-    }
+  if (src.n) {
     rc = check_not_captured(st);
-    if (!rc) rc = send(cache, orders, st);
+    if (!rc)
+      rc = p->n_pages > 65536 ? send_moves<int32_t, kManyBytes>(cache, src.p, dst.p, src.n, st)
+           : src.n * 4 > kFewBytes ? send_moves<uint16_t, kManyBytes>(cache, src.p, dst.p, src.n, st)
+                                   : send_moves<uint16_t, kFewBytes>(cache, src.p, dst.p, src.n, st);
     if (rc) return rc;
     for (int s = 0; s < n; ++s) {
       int32_t* row = p->table + (size_t)s * p->max_pages;
-      for (int q = 0; q < p->seg_pages[s]; ++q)
-        if (to[row[q]] >= 0) row[q] = orders.copies[to[row[q]]].b / CATEKV_PAGE_ROWS;
+      for (int q = 0; q < p->seg_pages[s]; ++q) row[q] = to.p[row[q]];
     }
   }
   p->next_free = live;
