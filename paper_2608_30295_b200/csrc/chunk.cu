@@ -27,8 +27,8 @@
 // memory (what lies behind a list may be NaN, and 0 * NaN is not 0); an infinity or a NaN in a new row, which later tokens see and earlier ones do not, is taken
 // out there too and added to the rows that see it at the end.
 //
-// Warps: four per M tile for the softmax; then one each for tensor-core issue, K / V tiles by TMA into one ring in the order of use,
-// the V tiles that need a look, and the query block.  Every wait is bounded; a CTA whose wait runs out frees its tensor memory, records
+// Warps: those of the softmax; then one each for the query block and the logits' instructions, the K and V tiles by TMA into a ring each, the V
+// tiles that need a look, and the products' instructions.  Every wait is bounded; a CTA whose wait runs out frees its tensor memory, records
 // CATEKV_STATUS_WAIT_EXPIRED and returns.
 #include <math.h>
 
@@ -44,17 +44,20 @@ constexpr int kChMaxSeqs = 512;  // sequences of a call: their counts travel in 
 constexpr int kChTileBytes = 128 * 256;  // a [128 x 128] bf16 tile
 constexpr int kChTmemCols = 512;         // slots of S / P in columns 0-255, the M tiles' accumulators at 256 and 384
 constexpr float kChTau = 8.f;
-constexpr int kChBarriers = 32;
-template <bool kQ2>
+constexpr int kChBarriers = 44;
+template <bool kQ2, int kFlush>
 struct ChunkShape {
+  static constexpr bool kSplit = !kQ2 && !kFlush;   // one M tile, bf16 results: the steps of a tile have softmax warps of their own
   static constexpr int kTiles = kQ2 ? 2 : 1;        // M tiles
-  static constexpr int kStages = kQ2 ? 5 : 6;
-  static constexpr int kSoft = 4 * kTiles;          // softmax warps
+  static constexpr int kStagesK = kFlush ? 3 : 2, kStagesV = 3;  // of the two rings
+  static constexpr int kSoft = kQ2 || kSplit ? 8 : 4;  // softmax warps
   static constexpr int kWarps = kSoft + 4, kThreads = kWarps * 32;
-  static constexpr int kSlotCols = kQ2 ? 64 : 128;  // slot h of M tile x: columns (2 x + h) kSlotCols; step h of a tile takes slot h
-  static constexpr size_t kSmem = 1024 + (size_t)(kTiles + kStages) * kChTileBytes + kChBarriers * 8 + 64;
+  // Slot of step h of a tile: 2 x + h for M tile x; kSplit: four slots, 2 (tile mod 2) + h, so that S is formed two tiles ahead.
+  static constexpr int kSlotCols = kFlush ? 128 : 64;
+  static constexpr int kLead = kSplit ? 2 : 1;      // K tiles loaded ahead of the V tile: K_0 .. K_{lead-1}, V_0, K_lead, V_1, ...
+  static constexpr size_t kSmem = 1024 + (size_t)(kTiles + kStagesK + kStagesV) * kChTileBytes + kChBarriers * 8 + 64 + (kSplit ? 4 * 128 * sizeof(float) : 0);
+  static_assert(kSmem <= 226 * 1024, "chunk_attn_kernel: one CTA's shared memory");
 };
-static_assert(ChunkShape<true>::kSmem <= 226 * 1024 && ChunkShape<false>::kSmem <= 227 * 1024, "chunk_attn_kernel: one CTA's shared memory");
 // A block costs a CTA more than its tiles (its queries, a pipeline that fills and drains, its results): this many tiles are charged for it when the
 // shares are cut.
 constexpr int kChCharge = 2;
@@ -156,16 +159,6 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
 }
 
-// Whether a phase has completed, without waiting.
-__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-               : "=r"(done)
-               : "r"(bar), "r"(parity)
-               : "memory");
-  return __all_sync(0xffffffffu, done != 0);
-}
-
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(bar)
@@ -201,13 +194,19 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
   return d;
 }
-// 32 logits -> probabilities of 32 keys in kParts bf16 numbers, 16 columns each, `step` columns from part to part; returns their sum
-template <int kParts>
-__device__ __forceinline__ float ch_probs32(const float* x, float scale, float neg_ref, uint32_t to, uint32_t step) {
+__device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n"
+               :
+               : "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+// kN logits -> probabilities of kN keys in kParts bf16 numbers, kN / 2 columns each, `step` columns from part to part; returns their sum
+template <int kN, int kParts>
+__device__ __forceinline__ float ch_probs(const float* x, float scale, float neg_ref, uint32_t to, uint32_t step) {
   float2 s0 = make_float2(0.f, 0.f), s1 = s0;
-  uint32_t w[kParts][16];
+  uint32_t w[kParts][kN / 2];
 #pragma unroll
-  for (int c = 0; c < 32; c += 2) {
+  for (int c = 0; c < kN; c += 2) {
     float2 p = fma2(make_float2(x[c], x[c + 1]), make_float2(scale, scale), make_float2(neg_ref, neg_ref));
     p.x = fast_exp2(p.x);
     p.y = fast_exp2(p.y);
@@ -220,7 +219,10 @@ __device__ __forceinline__ float ch_probs32(const float* x, float scale, float n
     }
   }
 #pragma unroll
-  for (int k = 0; k < kParts; ++k) tmem_st16u(to + k * step, w[k]);
+  for (int k = 0; k < kParts; ++k) {
+    if constexpr (kN == 32) tmem_st16u(to + k * step, w[k]);
+    else tmem_st8u(to + k * step, w[k]);
+  }
   s0 = add2(s0, s1);
   return s0.x + s0.y;
 }
@@ -238,36 +240,42 @@ __device__ __forceinline__ int ch_page(const ChunkArgs& a, int seg, int o) {
 }
 
 template <bool kQ2, int kParts, int kFlush>
-__global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
+__global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
     chunk_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                       const __grid_constant__ CUtensorMap ko_map, const __grid_constant__ CUtensorMap vo_map,
                       const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ChunkArgs a,
                       const __grid_constant__ ChunkSeqs sq) {
-  using Sh = ChunkShape<kQ2>;
-  constexpr int kStages = Sh::kStages, kTiles = Sh::kTiles, kSoft = Sh::kSoft, kWarps = Sh::kWarps;
+  using Sh = ChunkShape<kQ2, kFlush>;
+  constexpr int kStagesK = Sh::kStagesK, kStagesV = Sh::kStagesV, kTiles = Sh::kTiles, kLead = Sh::kLead, kSoft = Sh::kSoft, kWarps = Sh::kWarps;
   constexpr int kQBytes = kTiles * kChTileBytes, kQBlock = kQBytes / 2;
+  constexpr bool kSplit = Sh::kSplit;
   static_assert(kParts * 32 <= Sh::kSlotCols, "P fits its slot");
+  // tile number n (of the CTA): the slot of M tile x and step h, and the parity of its barriers
+  auto slot_of = [](uint32_t n, int x, int h) { return kSplit ? (int)(2 * (n & 1)) + h : 2 * x + h; };
+  auto phase_of = [](uint32_t n) { return (kSplit ? n >> 1 : n) & 1; };
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_scan[kWarps], s_first[8];
   const int tid = threadIdx.x, warp = uni(tid >> 5), lane = tid & 31;
   const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (s_base - smem_u32(smem_raw));
-  const uint32_t s_q = s_base, s_ring = s_base + kQBytes;
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(smem + kQBytes + kStages * kChTileBytes);
+  const uint32_t s_q = s_base, s_k = s_base + kQBytes, s_v = s_k + kStagesK * kChTileBytes;
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(smem + kQBytes + (kStagesK + kStagesV) * kChTileBytes);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + kChBarriers);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int* s_odd = reinterpret_cast<int*>(s_tmem + 4);  // [4]: first new row with an infinity or a NaN in V, of the last blocks that had V tiles looked at
+  float* s_ref = reinterpret_cast<float*>(s_tmem + 16);  // kSplit: [step][row] the rows' references, then their sums
   const uint32_t bar0 = smem_u32(s_bar);
   auto B = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-  constexpr int kFull = 0, kEmpty = kStages, kFixed = 2 * kStages, kDoneS = 3 * kStages, kPReady = kDoneS + 4, kDoneO = kPReady + 4,
-                kDonePV = kDoneO + 2, kQFull = kDonePV + 2, kQEmpty = kQFull + 1;
-  static_assert(kQEmpty < kChBarriers, "barrier table");
+  constexpr int kFullK = 0, kEmptyK = kFullK + kStagesK, kFullV = kEmptyK + kStagesK, kEmptyV = kFullV + kStagesV, kFixed = kEmptyV + kStagesV,
+                kDoneS = kFixed + kStagesV, kPReady = kDoneS + 4, kDonePV = kPReady + 4, kDoneO = kDonePV + 4, kQFull = kDoneO + 2, kQEmpty = kQFull + 1,
+                kDec = kQEmpty + 1, kXch = kDec + 4;
+  static_assert(kXch + 4 <= kChBarriers, "barrier table");
 
   pdl_launch_dependents();
   if (tid == 0) {
     *s_abort = 0;
     for (int i = 0; i < kChBarriers; ++i) {
-      const int count = (i >= kPReady && i < kPReady + 4) ? 4 : 1;
+      const int count = (i >= kPReady && i < kPReady + 4) ? 4 : (i >= kXch && i < kXch + 4) ? 2 : 1;
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(B(i)), "r"(count));
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -365,21 +373,17 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
 
   if (warp >= kSoft) {
   if (warp == kSoft + 1) {
-    // ================= K and V tiles, in the order in which the tensor pipe uses them: K_0, V_0, K_1, V_1, ...
+    // ================= K and V tiles, in the order of their use
     // The entries of the page table are fetched 32 at a time, a lane each (one by one, a trip to memory for every tile, they were slower than the products).
     if (!a.idle_producer) {
-      uint32_t use = 0;
+      uint32_t n_k = 0, n_v = 0;
       bool ok = true;
       while (ok && walk.next(a, sq, it)) {
         const int n = it.t1 - it.t0;
         const int off = it.g.off, cap = it.g.cap;
         int window = -64, entry = -1;  // lane i holds the list's page window + i
-        auto load = [&](const CUtensorMap* pool, const CUtensorMap* ovf, int t) {
-          const int st = use % kStages;
-          if (use >= kStages && !warp_wait(B(kEmpty + st), ((use / kStages) - 1) & 1, s_abort, a.spin_limit)) return false;
-          ++use;
+        auto load = [&](const CUtensorMap* pool, const CUtensorMap* ovf, uint32_t dst, uint32_t bar, int t) {
           const int r0 = t * kKeyTile;
-          const uint32_t dst = s_ring + st * kChTileBytes, bar = B(kFull + st);
           if (r0 < cap) {
             if (lane == 0) {
               mbar_expect_tx(bar, kChTileBytes);
@@ -388,8 +392,8 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
             }
           } else {
             const int p = (r0 - cap) >> 6;
-            if (p < window || p + 1 >= window + 32) {  // the V tile before comes after this K tile
-              window = max(p - 2, 0);
+            if (p < window || p + 1 >= window + 32) {  // V tiles before come after this K tile
+              window = max(p - 2 * kLead, 0);
               entry = cap + (window + lane) * 64 < it.g.len ? ch_page(a, it.seg, (window + lane) * 64) : -1;
             }
             const int pg0 = __shfl_sync(0xffffffffu, entry, p - window), pg1 = __shfl_sync(0xffffffffu, entry, p + 1 - window);
@@ -406,59 +410,92 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
             }
           }
           __syncwarp();
-          return true;
         };
-        ok = load(&k_map, &ko_map, it.t0);
-        for (int t = 0; ok && t < n; ++t) {
-          ok = load(&v_map, &vo_map, it.t0 + t);
-          if (ok && t + 1 < n) ok = load(&k_map, &ko_map, it.t0 + t + 1);
+        for (int t = -kLead; ok && t < n; ++t) {
+          if (t >= 0) {
+            const int st = n_v % kStagesV;
+            if (n_v >= kStagesV && !(ok = warp_wait(B(kEmptyV + st), ((n_v / kStagesV) - 1) & 1, s_abort, a.spin_limit))) break;
+            ++n_v;
+            load(&v_map, &vo_map, s_v + st * kChTileBytes, B(kFullV + st), it.t0 + t);
+          }
+          if (t + kLead < n) {
+            const int st = n_k % kStagesK;
+            if (n_k >= kStagesK && !(ok = warp_wait(B(kEmptyK + st), ((n_k / kStagesK) - 1) & 1, s_abort, a.spin_limit))) break;
+            ++n_k;
+            load(&k_map, &ko_map, s_k + st * kChTileBytes, B(kFullK + st), it.t0 + t + kLead);
+          }
         }
       }
     }
     __syncwarp();
   } else if (warp == kSoft + 3) {
-    // ================= the query block of every item
-    if (lane == 0 && !a.idle_producer) {
-      uint32_t n_item = 0;
-      while (walk.next(a, sq, it)) {
-        if (n_item >= 1 && !mbar_wait(B(kQEmpty), (n_item - 1) & 1, s_abort, a.spin_limit)) break;
-        ++n_item;
-        const int h = it.seg % a.Hkv, token = sq.start[it.seg / a.Hkv] + it.blk * a.TB;
-        mbar_expect_tx(B(kQFull), 2 * 128 * a.G * a.TB);
-        tma_load_3d(s_q, &q_map, 0, h * a.G, token, B(kQFull));
-        tma_load_3d(s_q + kQBlock, &q_map, 64, h * a.G, token, B(kQFull));
+    // ================= products with V (the whole warp, converged)
+    if (!a.idle_producer) {
+      const uint32_t idesc = umma_idesc_bf16_bmn(128, 128), tm = (uint32_t)uni((int)tmem);
+      const uint64_t dv0 = umma_desc_sw128_mn(s_v, kKBlockBytes);
+      uint32_t n_t = 0, fixed = 0;  // tiles; one bit per stage, the parity of its next look
+      bool ok = true;
+      while (ok && walk.next(a, sq, it)) {
+        const int t0 = uni(it.t0), n = uni(it.t1) - t0;
+        const int first = uni(it.g.len - it.g.n_new + it.blk * a.TB + 1);
+        const int last = uni(it.g.len - it.g.n_new + min(it.g.n_new, a.TB * (it.blk + 1)));
+        for (int t = 0; ok && t < n; ++t, ++n_t) {
+          const bool look = (t0 + t + 1) * kKeyTile > first, fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
+          const int st = n_t % kStagesV, rows = ch_v_rows(last - (t0 + t) * kKeyTile);
+          ok = warp_wait(B(kFullV + st), (n_t / kStagesV) & 1, s_abort, a.spin_limit);
+          if (ok && look) {
+            ok = warp_wait(B(kFixed + st), (fixed >> st) & 1, s_abort, a.spin_limit);
+            fixed ^= 1u << st;
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int x = 0; x < kTiles; ++x) {
+              const int slot = slot_of(n_t, x, h);
+              if (!ok || !(ok = warp_wait(B(kPReady + slot), phase_of(n_t), s_abort, a.spin_limit))) break;
+              tc_fence_after();
+              const uint64_t dv = dv0 + (uint64_t)(st * (kChTileBytes >> 4) + h * (64 * 128 >> 4));
+              const uint32_t d = tm + 256 + x * 128, p = tm + slot * Sh::kSlotCols;
+              const bool begin = fresh && h == 0;
+              if (elect_one()) {
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                  for (int kk = 0; kk < 4; ++kk)
+                    if (64 * h + 16 * kk < rows)
+                      umma_bf16_ta(kFlush && part ? d + 128 : d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc,
+                                   kk || part > (kFlush ? 1 : 0) ? 1u : (begin ? 0u : 1u));
+                umma_commit(B(kDonePV + slot));
+                if (h == 1 && x == kTiles - 1) umma_commit(B(kEmptyV + st));
+                if (h == 1 && t + 1 == n) umma_commit(B(kDoneO + x));
+              }
+            }
+          }
+        }
       }
     }
     __syncwarp();
   } else if (warp == kSoft + 2) {
     // ================= V tiles with rows that some query of the block does not see
-    uint32_t use = 0, n_item = 0;
+    uint32_t n_v = 0, n_item = 0;
     bool ok = !a.idle_producer;
     while (ok && walk.next(a, sq, it)) {
       const int n = it.t1 - it.t0;
       const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;                       // rows that every query sees
       const int last = it.g.len - it.g.n_new + min(it.g.n_new, a.TB * (it.blk + 1));     // rows that the last one sees
       bool fresh = true;
-      // every use of the ring is waited for in its order: a wait that skipped one could take the phase before it for its own
-      auto arrived = [&]() {
-        const uint32_t u = use++;
-        return mbar_wait(B(kFull + u % kStages), (u / kStages) & 1, s_abort, a.spin_limit);
-      };
-      ok = arrived();
-      for (int t = 0; ok && t < n; ++t) {
-        const int r0 = (it.t0 + t) * kKeyTile, st = use % kStages;
-        if (!(ok = arrived())) break;
-        if (r0 + kKeyTile <= first) {
-          if (t + 1 < n) ok = arrived();
-          continue;
-        }
+      // (every tile is waited for in its order: a wait that skipped one could take the phase before it for its own)
+      for (int t = 0; ok && t < n; ++t, ++n_v) {
+        const int r0 = (it.t0 + t) * kKeyTile, st = n_v % kStagesV;
+        if (!(ok = mbar_wait(B(kFullV + st), (n_v / kStagesV) & 1, s_abort, a.spin_limit))) break;
+        if (r0 + kKeyTile <= first) continue;
         if (fresh) {
           // four flags in turn: this block's V tile is in the ring, so the results of the block four before it are out
           if (lane == 0) s_odd[n_item & 3] = 0x7fffffff;
           __syncwarp();
           fresh = false;
         }
-        uint8_t* tile = smem + kQBytes + st * kChTileBytes;
+        uint8_t* tile = smem + kQBytes + (kStagesK + st) * kChTileBytes;
         int odd = 0x7fffffff;
         const int end = ch_v_rows(last - r0);
 #pragma unroll 4
@@ -486,107 +523,56 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kFixed + st));
-        if (t + 1 < n) ok = arrived();
       }
       n_item += fresh ? 0 : 1;
     }
     __syncwarp();
   } else if (warp == kSoft) {
-    // ================= tensor-core issue (the whole warp, converged)
+    // ================= the query block of every item, and its logits (the whole warp, converged)
+    // Logits and products are issued by a warp each: while one looks at its barriers the other keeps the tensor pipe fed.
     if (!a.idle_producer) {
-      const uint32_t idesc_s = umma_idesc_bf16(128, 64), idesc_o = umma_idesc_bf16_bmn(128, 128);
-      const uint64_t dq0 = umma_desc_sw128(s_q), dk0 = umma_desc_sw128(s_ring), dv0 = umma_desc_sw128_mn(s_ring, kKBlockBytes);
-      const uint32_t tm = (uint32_t)uni((int)tmem);
-      uint32_t use = 0, n_item = 0, fixed = 0, n_p = 0;  // fixed: one bit per stage, the parity of its next look; n_p: tiles
+      const uint32_t idesc = umma_idesc_bf16(128, 64), tm = (uint32_t)uni((int)tmem);
+      const uint64_t dq0 = umma_desc_sw128(s_q), dk0 = umma_desc_sw128(s_k);
+      uint32_t n_item = 0, n_t = 0;
       bool ok = true;
-      auto wait_tile = [&]() { return warp_wait(B(kFull + use % kStages), (use / kStages) & 1, s_abort, a.spin_limit); };
-      auto commit = [&](int i) {
-        if (elect_one()) umma_commit(B(i));
-      };
-      auto issue_s = [&](int x, int h, int st) {
-        const uint64_t dq = dq0 + (uint64_t)(x * (128 * 128 >> 4)), dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4) + h * (64 * 128 >> 4));
-        const uint32_t d = tm + (2 * x + h) * Sh::kSlotCols;
-        if (elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            umma_bf16(d, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2), dk + (uint64_t)((kk >> 2) * (kKBlockBytes >> 4) + (kk & 3) * 2),
-                      idesc_s, kk ? 1u : 0u);
-          umma_commit(B(kDoneS + 2 * x + h));
-        }
-      };
-      auto issue_o = [&](int x, int h, int st, bool fresh, int rows) {
-        const uint64_t dv = dv0 + (uint64_t)(st * (kChTileBytes >> 4) + h * (64 * 128 >> 4));
-        const uint32_t d = tm + 256 + x * 128, p = tm + (2 * x + h) * Sh::kSlotCols;
-        if (elect_one()) {
-#pragma unroll
-          for (int part = 0; part < kParts; ++part)
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              if (64 * h + 16 * kk < rows) umma_bf16_ta(kFlush && part ? d + 128 : d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc_o,
-                           kk || part > (kFlush ? 1 : 0) ? 1u : (fresh ? 0u : 1u));
-          umma_commit(B(kDonePV + x));
-        }
-      };
       while (ok && walk.next(a, sq, it)) {
-        const int t0 = uni(it.t0), n = uni(it.t1) - t0;
-        const int first = uni(it.g.len - it.g.n_new + it.blk * a.TB + 1);
-        const int last = uni(it.g.len - it.g.n_new + min(it.g.n_new, a.TB * (it.blk + 1)));
-        if (!(ok = warp_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit))) break;
-        ++n_item;
-        if (!(ok = wait_tile())) break;
-        tc_fence_after();
-        {
-          const int st = use++ % kStages;
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int x = 0; x < kTiles; ++x) issue_s(x, h, st);
-          commit(kEmpty + st);
+        const int n = uni(it.t1 - it.t0);
+        if (n_item >= 1 && !(ok = warp_wait(B(kQEmpty), (n_item - 1) & 1, s_abort, a.spin_limit))) break;
+        if (lane == 0) {
+          const int hd = it.seg % a.Hkv * a.G, token = sq.start[it.seg / a.Hkv] + it.blk * a.TB;
+          mbar_expect_tx(B(kQFull), 2 * 128 * a.G * a.TB);
+          tma_load_3d(s_q, &q_map, 0, hd, token, B(kQFull));
+          tma_load_3d(s_q + kQBlock, &q_map, 64, hd, token, B(kQFull));
         }
-        if (n == 1) commit(kQEmpty);
-        bool p_there = false;  // the next P was seen ready before the last S was issued: its products follow without a look at a barrier
-        for (int t = 0; ok && t < n; ++t, ++n_p) {
-          const bool look = (t0 + t + 1) * kKeyTile > first, more = t + 1 < n;
-          const bool fresh = kFlush ? t % max(kFlush, 1) == 0 : t == 0;
-          const int sv = use % kStages, sk = (use + 1) % kStages, rows = ch_v_rows(last - (t0 + t) * kKeyTile);
-          bool k_there = false;
+        __syncwarp();
+        ok = warp_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit);
+        ++n_item;
+        for (int t = 0; ok && t < n; ++t, ++n_t) {
+          const int st = n_t % kStagesK;
+          ok = warp_wait(B(kFullK + st), (n_t / kStagesK) & 1, s_abort, a.spin_limit);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int x = 0; x < kTiles; ++x) {
-              if (!p_there) ok = warp_wait(B(kPReady + 2 * x + h), n_p & 1, s_abort, a.spin_limit);
-              if (h == 0 && x == 0) {
-                if (ok) ok = wait_tile();
-                ++use;
-                if (ok && look) {
-                  ok = warp_wait(B(kFixed + sv), (fixed >> sv) & 1, s_abort, a.spin_limit);
-                  fixed ^= 1u << sv;
-                }
-                if (ok && more) k_there = warp_test(B(kFull + sk), (use / kStages) & 1);
-              }
+              const int slot = slot_of(n_t, x, h);
+              // the slot's last P has been taken
+              if (ok && n_t >= (kSplit ? 2 : 1)) ok = warp_wait(B(kDonePV + slot), phase_of(n_t) ^ 1, s_abort, a.spin_limit);
               if (!ok) break;
               tc_fence_after();
-              issue_o(x, h, sv, fresh && h == 0, rows);
-              if (h == 1 && x == kTiles - 1) commit(kEmpty + sv);
-              const bool last = h == 1 && x == kTiles - 1;  // of the tile
-              const int xn = x + 1 < kTiles ? x + 1 : 0, hn = x + 1 < kTiles ? h : h ^ 1;
-              p_there = (!last || more) && warp_test(B(kPReady + 2 * xn + hn), (last ? n_p + 1 : n_p) & 1);
-              if (more) {  // the next tile's S into the slot whose P has just been taken: the tensor pipe keeps issue order
-                if (h == 0 && x == 0) {
-                  if (!k_there && !(ok = wait_tile())) break;
-                  ++use;
-                  tc_fence_after();
+              const uint64_t dq = dq0 + (uint64_t)(x * (128 * 128 >> 4)), dk = dk0 + (uint64_t)(st * (kChTileBytes >> 4) + h * (64 * 128 >> 4));
+              const uint32_t d = tm + slot * Sh::kSlotCols;
+              if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                  umma_bf16(d, dq + (uint64_t)((kk >> 2) * (kQBlock >> 4) + (kk & 3) * 2),
+                            dk + (uint64_t)((kk >> 2) * (kKBlockBytes >> 4) + (kk & 3) * 2), idesc, kk ? 1u : 0u);
+                umma_commit(B(kDoneS + slot));
+                if (h == 1 && x == kTiles - 1) {
+                  umma_commit(B(kEmptyK + st));
+                  if (t + 1 == n) umma_commit(B(kQEmpty));
                 }
-                issue_s(x, h, sk);
-                if (last) {
-                  commit(kEmpty + sk);
-                  if (t + 2 == n) commit(kQEmpty);
-                }
-              } else if (h == 1) {
-                commit(kDoneO + x);
               }
             }
-            if (!ok) break;
           }
         }
       }
@@ -594,14 +580,15 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
     __syncwarp();
     }
   } else {
-    // ================= softmax: four warps an M tile; a thread owns a row
-    const int x = warp >> 2, quarter = warp & 3;
+    // ================= softmax; a thread owns a row of its warps' M tile, or (kSplit) the row's share of one step of every tile
+    const int g = kSplit ? warp >> 2 : 0, x = kQ2 ? warp >> 2 : 0, quarter = warp & 3;
     const int lane_row = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
     const uint32_t acc = tmem + lane_base + 256 + x * 128;
     const int row = x * 128 + lane_row;  // row of the block
     const int tok = row / a.G;
-    uint32_t n_s = 0, n_o = 0, n_odd = 0;
+    float* const s_l = s_ref + 256;
+    uint32_t n_s = 0, n_o = 0, n_odd = 0, n_dec = 0, n_x = 0;
     bool alive = true, first_item = true;
     while (alive && walk.next(a, sq, it)) {
       const int n = it.t1 - it.t0;
@@ -617,15 +604,19 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
       for (int i = 0; alive && i < n; ++i, ++n_s) {
         const bool fresh = kFlush ? i % max(kFlush, 1) == 0 : i == 0;
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          if (!(alive = mbar_wait(B(kDoneS + 2 * x + h), n_s & 1, s_abort, a.spin_limit))) break;
+        for (int h = kSplit ? g : 0; h < (kSplit ? g + 1 : 2); ++h) {
+          const int s_slot = slot_of(n_s, x, h);
+          if (!(alive = mbar_wait(B(kDoneS + s_slot), phase_of(n_s), s_abort, a.spin_limit))) break;
           if (idle) {
             __syncwarp();
-            if (lane == 0) mbar_arrive(B(kPReady + 2 * x + h));
+            if (lane == 0) mbar_arrive(B(kPReady + s_slot));
             continue;
           }
           tc_fence_after();
-          const uint32_t slot = tmem + lane_base + (2 * x + h) * Sh::kSlotCols;
+          const uint32_t slot = tmem + lane_base + s_slot * Sh::kSlotCols;
+          // the products of the step before (whose slot's earlier phases are behind us: its own S has been read)
+          const uint32_t n_b = h == 0 ? n_s - 1 : n_s;
+          auto wait_products = [&]() { return mbar_wait(B(kDonePV + slot_of(n_b, x, h ^ 1)), phase_of(n_b), s_abort, a.spin_limit); };
           const int k0 = (it.t0 + i) * kKeyTile + 64 * h;
           float y[64];
           tmem_ld64(slot, y);
@@ -635,13 +626,25 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
 #pragma unroll
             for (int c = 0; c < 64; ++c) y[c] = c < lim ? y[c] : -INFINITY;
           }
-          const float mx = ch_max<64>(y) * a.scale_log2, ref_o = ref;
-          const bool grow = mx > ref + kChTau;  // also the first step with a visible key
-          if (__any_sync(0xffffffffu, grow)) {
-            const float f = grow && ref > -INFINITY ? fast_exp2(ref - mx) : 1.f;
-            l *= f;
+          const float mx = ch_max<64>(y) * a.scale_log2;
+          float ref_o = ref;  // the accumulator's reference
+          if (kSplit) {
+            // The two steps' threads of a row share its reference: each decides after the other has decided for the step before.  Only that is serial.
+            if (n_dec + g > 0 && !(alive = mbar_wait(B(kDec + quarter), (n_dec + g - 1) & 1, s_abort, a.spin_limit))) break;
+            ref_o = i + g > 0 ? s_ref[(g ^ 1) * 128 + lane_row] : -INFINITY;
+          }
+          const bool grow = mx > ref_o + kChTau;  // also the first step with a visible key
+          const float ref_n = grow ? mx : ref_o;
+          if (kSplit) {
+            s_ref[g * 128 + lane_row] = ref_n;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(B(kDec + quarter));
+          }
+          if (__any_sync(0xffffffffu, ref_n > ref)) {
+            if (ref_n > ref) l = ref > -INFINITY ? l * fast_exp2(ref - ref_n) : l;
+            const float f = grow && ref_o > -INFINITY ? fast_exp2(ref_o - ref_n) : 1.f;
             if ((h == 1 || !fresh) && __any_sync(0xffffffffu, f != 1.f)) {  // the accumulator follows, behind the products of the step before
-              if (!(alive = mbar_wait(B(kDonePV + x), h ^ 1, s_abort, a.spin_limit))) break;
+              if (!(alive = wait_products())) break;
               tc_fence_after();
 #pragma unroll 1
               for (int c0 = 0; c0 < (kFlush ? 256 : 128); c0 += 32) {
@@ -653,14 +656,18 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
                 tmem_st32(acc + c0, o);
               }
             }
-            if (grow) ref = mx;
+            ref = ref_n;
           }
           const float neg = ref > -INFINITY ? -ref : 0.f;  // nothing seen yet: every P is exp2(-inf) = 0
-          l += ch_probs32<kParts>(y, a.scale_log2, neg, slot, 32);
-          l += ch_probs32<kParts>(y + 32, a.scale_log2, neg, slot + 16, 32);
+          if (kFlush) {
+#pragma unroll
+            for (int c = 0; c < 64; c += 16) l += ch_probs<16, kParts>(y + c, a.scale_log2, neg, slot + c / 2, 32);
+          } else {
+            l += ch_probs<32, kParts>(y, a.scale_log2, neg, slot, 32);
+            l += ch_probs<32, kParts>(y + 32, a.scale_log2, neg, slot + 16, 32);
+          }
           if (kFlush && h == 0 && fresh && i > 0) {  // what the tensor cores have added up since the last time
-            // (this step's S was issued behind the products of the step but one before: behind it, the parity tells the last step's)
-            if (!(alive = mbar_wait(B(kDonePV + x), 1, s_abort, a.spin_limit))) break;
+            if (!(alive = wait_products())) break;
             tc_fence_after();
             const float f = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref_o) : 0.f;
 #pragma unroll
@@ -671,24 +678,39 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
               tmem_wait_ld16(o);
               tmem_wait_ld16(o1);
 #pragma unroll
-              for (int c = 0; c < 16; ++c) {
-                const float z = o[c] + o1[c];
-                if constexpr (kFlush > 0) sum[c0 + c] = i > kFlush ? fmaf(sum[c0 + c], f, z) : z;
-              }
+              for (int c = 0; c < 16; ++c)
+                if constexpr (kFlush > 0) sum[c0 + c] = i > kFlush ? fmaf(sum[c0 + c], f, o[c] + o1[c]) : o[c] + o1[c];
             }
             sum_ref = ref_o;
           }
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(B(kPReady + 2 * x + h));
+          if (lane == 0) mbar_arrive(B(kPReady + s_slot));
         }
+        n_dec += idle ? 0 : 2;
       }
       if (!alive) break;
+      if (kSplit) {  // the row's sums of both steps, relative to the last decision (the second step's)
+        if (!idle) {
+          if (!(alive = mbar_wait(B(kDec + quarter), (n_dec - 1) & 1, s_abort, a.spin_limit))) break;
+          const float ref_end = s_ref[128 + lane_row];
+          if (ref_end > ref) {
+            l = ref > -INFINITY ? l * fast_exp2(ref - ref_end) : l;
+            ref = ref_end;
+          }
+        }
+        s_l[g * 128 + lane_row] = l;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kXch + quarter));
+        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
+        ++n_x;
+        l = s_l[lane_row] + s_l[128 + lane_row];
+      }
       if (!(alive = mbar_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
       ++n_o;
       tc_fence_after();
-      // ---- the item's result: the whole block, or a piece of it
+      // ---- the item's result: the whole block, or a piece of it (kSplit: each step's threads write half of d)
       const bool looked = it.t1 * kKeyTile > first;
       const int odd = looked ? s_odd[n_odd & 3] : 0x7fffffff;
       n_odd += looked ? 1 : 0;
@@ -700,7 +722,8 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
       const float inv = whole ? (l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l)) : 1.f;  // a NaN stays one
       if (!idle) {
 #pragma unroll(kFlush ? 4 : 1)
-        for (int c0 = 0; c0 < 128; c0 += 32) {
+        for (int cc = 0; cc < (kSplit ? 64 : 128); cc += 32) {
+          const int c0 = g * 64 + cc;
           float o[32];
           tmem_ld32(acc + c0, o);
           tmem_wait_ld32(o);
@@ -709,7 +732,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
             tmem_ld32(acc + 128 + c0, o1);
             tmem_wait_ld32(o1);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = summed ? fmaf(sum[c0 + c], fs, o[c] + o1[c]) : o[c] + o1[c];
+            for (int c = 0; c < 32; ++c) o[c] = summed ? fmaf(sum[cc + c], fs, o[c] + o1[c]) : o[c] + o1[c];
           }
           if (odd < sees && valid) {  // infinities and NaN that were taken out of the V tiles
             const int off = it.g.off, cap = it.g.cap;
@@ -750,12 +773,18 @@ __global__ void __launch_bounds__(ChunkShape<kQ2>::kThreads, 1)
             }
           }
         }
-        if (valid) {
+        if (valid && g == 0) {
           if (!whole) a.part_ml[(int64_t)tile * a.R + lane_row] = make_float2(ref, l);
           else if (a.lse) a.lse[orow] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
         }
       }
       tc_fence_before();
+      if (kSplit) {  // the other step's threads have read the accumulator too: the next block's products may overwrite it
+        __syncwarp();
+        if (lane == 0) mbar_arrive(B(kXch + quarter));
+        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
+        ++n_x;
+      }
     }
   }
 
@@ -1031,10 +1060,10 @@ static int launch_chunk(int ctas, const CUtensorMap* m, const ChunkArgs& a, cons
   int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts, kFlush>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ChunkShape<kQ2>::kSmem));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts, kFlush>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ChunkShape<kQ2, kFlush>::kSmem));
     if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   }
-  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts, kFlush>, dim3(ctas), dim3(ChunkShape<kQ2>::kThreads), ChunkShape<kQ2>::kSmem, st, m[0], m[1], m[2], m[3], m[4],
+  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts, kFlush>, dim3(ctas), dim3(ChunkShape<kQ2, kFlush>::kThreads), ChunkShape<kQ2, kFlush>::kSmem, st, m[0], m[1], m[2], m[3], m[4],
                              a, sq));
   return CATEKV_OK;
 }
