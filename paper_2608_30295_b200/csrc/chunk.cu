@@ -60,7 +60,7 @@ struct ChunkShape {
 };
 // A block costs a CTA more than its tiles (its queries, a pipeline that fills and drains, its results): this many tiles are charged for it when the
 // shares are cut.
-constexpr int kChCharge = 2;
+constexpr int kChCharge = 3;
 
 struct ChunkSeqs {  // host counts of every sequence
   int32_t n_new[kChMaxSeqs];
@@ -168,6 +168,17 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
+}
+// 32 bytes of this thread's row; `whole`: the address is a multiple of 32, and one store writes a sector
+__device__ __forceinline__ void st_row32(void* p, const uint32_t (&w)[8], bool whole) {
+  if (whole) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                 "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
 }
 template <int kN>
 __device__ __forceinline__ float ch_max(const float* x) {
@@ -496,17 +507,27 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
           fresh = false;
         }
         uint8_t* tile = smem + kQBytes + (kStagesK + st) * kChTileBytes;
+        auto chunk = [&](int r) { return reinterpret_cast<uint4*>(tile + sw128_off(r, lane & 15, 128)); };  // 16 lanes a row
         int odd = 0x7fffffff;
-        const int end = ch_v_rows(last - r0);
-#pragma unroll 4
-        for (int r = max(first - r0, 0) + (lane >> 4); r < end; r += 2) {
-          const int c = lane & 15, j = r0 + r;
-          uint4* p = reinterpret_cast<uint4*>(tile + sw128_off(r, c, 128));
-          if (j >= last) {
-            *p = make_uint4(0u, 0u, 0u, 0u);
-          } else if (j >= first) {
-            uint4 v = *p;
-            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+        const int lo = max(first - r0, 0), hi = min(last - r0, kKeyTile);
+        for (int rb = lo; rb < hi; rb += 16) {
+          uint4 v[8];
+          uint32_t ones = 0;  // sign bits of halves whose exponent is all ones
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = rb + 2 * i + (lane >> 4);
+            v[i] = r < hi ? *chunk(r) : make_uint4(0u, 0u, 0u, 0u);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            ones |= ((v[i].x & 0x7f807f80u) + 0x00800080u) | ((v[i].y & 0x7f807f80u) + 0x00800080u) | ((v[i].z & 0x7f807f80u) + 0x00800080u) |
+                    ((v[i].w & 0x7f807f80u) + 0x00800080u);
+          if (!__any_sync(0xffffffffu, (ones & 0x80008000u) != 0)) continue;
+          for (int i = 0; i < 8; ++i) {
+            const int r = rb + 2 * i + (lane >> 4);
+            if (r >= hi) break;
+            uint4 y = *chunk(r);
+            uint32_t* w = reinterpret_cast<uint32_t*>(&y);
             bool bad = false;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -514,11 +535,14 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
               if ((w[k] & 0x7f800000u) == 0x7f800000u) bad = true, w[k] &= 0x0000ffffu;
             }
             if (bad) {
-              *p = v;
-              odd = min(odd, j);
+              *chunk(r) = y;
+              odd = min(odd, r0 + r);
             }
           }
+          __syncwarp();
         }
+        const int end = ch_v_rows(last - r0);
+        for (int r = max(last - r0, 0) + (lane >> 4); r < end; r += 2) *chunk(r) = make_uint4(0u, 0u, 0u, 0u);
         if (odd != 0x7fffffff) atomicMin(&s_odd[n_item & 3], odd);
         fence_async_smem();
         __syncwarp();
@@ -754,21 +778,16 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
             if (!whole) {
 #pragma unroll
               for (int c = 0; c < 8; ++c) part[(c0 / 4 + c) * a.R] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-            } else if (kFlush) {
-              float* dst = reinterpret_cast<float*>(a.out) + orow * kD + c0;
-#pragma unroll
-              for (int c = 0; c < 32; c += 4)
-                *reinterpret_cast<float4*>(dst + c) = make_float4(o[c] * inv, o[c + 1] * inv, o[c + 2] * inv, o[c + 3] * inv);
             } else {
-              uint16_t* dst = reinterpret_cast<uint16_t*>(a.out) + orow * kD + c0;
+              uint8_t* dst = reinterpret_cast<uint8_t*>(a.out) + (orow * kD + c0) * (kFlush ? 4 : 2);
+              const bool sector = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
 #pragma unroll
-              for (int c = 0; c < 32; c += 8) {
-                uint4 w;
-                w.x = pack_bf16(o[c] * inv, o[c + 1] * inv);
-                w.y = pack_bf16(o[c + 2] * inv, o[c + 3] * inv);
-                w.z = pack_bf16(o[c + 4] * inv, o[c + 5] * inv);
-                w.w = pack_bf16(o[c + 6] * inv, o[c + 7] * inv);
-                *reinterpret_cast<uint4*>(dst + c) = w;
+              for (int c = 0; c < 32; c += kFlush ? 8 : 16) {
+                uint32_t w[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                  w[k] = kFlush ? __float_as_uint(o[c + k] * inv) : pack_bf16(o[(c + 2 * k) & 31] * inv, o[(c + 2 * k + 1) & 31] * inv);
+                st_row32(dst + c * (kFlush ? 4 : 2), w, sector);
               }
             }
           }
