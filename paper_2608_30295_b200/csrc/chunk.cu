@@ -1159,11 +1159,12 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   const int n_segs = cache->B * cache->Hkv;
   const bool two = out_dtype == CATEKV_OUT_BF16 && ch_two_tiles(G, max_new);
   const int TB = (two ? 256 : 128) / G;
-  int64_t units = 0;
+  int64_t units = 0, blocks = 0;
   for (int s = 0; s < n_segs; ++s) {
     const int n = sq.n_new[s / cache->Hkv], len = cache->seg_len[s];
     if (cache->seg_cap[s] < 0 || cache->seg_cap[s] % CATEKV_SEG_ALIGN || cache->seg_off[s] < 0) return CATEKV_ERR_INVALID_ARG;
     if (len < n || len > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;  // the chunk's rows are the list's last ones
+    blocks += (n + TB - 1) / TB;
     for (int j = 0; j < n; j += TB) units += (len - n + (n < j + TB ? n : j + TB) + kKeyTile - 1) / kKeyTile;
   }
   if (sum == 0) return CATEKV_OK;
@@ -1212,13 +1213,16 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
     a.spin_limit = 512;
     a.idle_producer = 1;
   }
-  const int ctas = (int)(units < sm_count() ? units : sm_count());
+  // As many shares as there are tiles, up to one a CTA; lists of one or two tiles stay whole (a second tile costs 1.5 us, a merge 4: 8.4 against 12.5 us
+  // for a token over 8 lists of 128 rows, while lists of 500 rows gain by being cut, 12.5 against 14.7).
+  const int64_t shares = units <= 2 * blocks ? blocks : units;
+  const int ctas = (int)(shares < sm_count() ? shares : sm_count());
   cudaStream_t st = (cudaStream_t)stream;
   rc = a.out_fp32 ? launch_chunk<false, 3, 3>(ctas, m, a, sq, st)
        : two      ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st)
                   : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
   if (rc) return rc;
-  CATEKV_CUDA_TRY(a.R <= 4 ? launch_combine<4>(a, sq, ctas, two, st) : a.R <= 8 ? launch_combine<8>(a, sq, ctas, two, st)
-                                                                               : launch_combine<32>(a, sq, ctas, two, st));
+  CATEKV_CUDA_TRY(two ? launch_combine<32>(a, sq, ctas, two, st) : a.R <= 4 ? launch_combine<4>(a, sq, ctas, two, st)
+                                                                            : launch_combine<8>(a, sq, ctas, two, st));
   return CATEKV_OK;
 }
