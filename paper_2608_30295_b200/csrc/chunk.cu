@@ -1157,16 +1157,22 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   const int G = Hq / cache->Hkv;
   if (G > kMaxG || (out_dtype != CATEKV_OUT_BF16 && out_dtype != CATEKV_OUT_FP32)) return CATEKV_ERR_UNSUPPORTED;
   const int n_segs = cache->B * cache->Hkv;
-  const bool two = out_dtype == CATEKV_OUT_BF16 && ch_two_tiles(G, max_new);
-  const int TB = (two ? 256 : 128) / G;
-  int64_t units = 0, blocks = 0;
+  int64_t units_of[2] = {0, 0}, blocks_of[2] = {0, 0};  // tiles and blocks with one M tile, with two
   for (int s = 0; s < n_segs; ++s) {
     const int n = sq.n_new[s / cache->Hkv], len = cache->seg_len[s];
     if (cache->seg_cap[s] < 0 || cache->seg_cap[s] % CATEKV_SEG_ALIGN || cache->seg_off[s] < 0) return CATEKV_ERR_INVALID_ARG;
     if (len < n || len > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;  // the chunk's rows are the list's last ones
-    blocks += (n + TB - 1) / TB;
-    for (int j = 0; j < n; j += TB) units += (len - n + (n < j + TB ? n : j + TB) + kKeyTile - 1) / kKeyTile;
+    for (int w = 0; w < 2; ++w) {
+      const int TB = (w ? 256 : 128) / G;
+      blocks_of[w] += (n + TB - 1) / TB;
+      for (int j = 0; j < n; j += TB) units_of[w] += (len - n + (n < j + TB ? n : j + TB) + kKeyTile - 1) / kKeyTile;
+    }
   }
+  // A tile takes 2400 cycles for one M tile (the stream of K and V bounds it) and 3400 for two (the products do): two, unless so many sequences have a
+  // few tokens only that their blocks would be half empty (512 tokens beside 31 single ones over 8 x 8000 rows each: 285 us with two, 257 with one).
+  const bool two = out_dtype == CATEKV_OUT_BF16 && units_of[1] * 7 < units_of[0] * 5;
+  const int TB = (two ? 256 : 128) / G;
+  const int64_t units = units_of[two], blocks = blocks_of[two];
   if (sum == 0) return CATEKV_OK;
   if (units > 0x7fffffff) return CATEKV_ERR_UNSUPPORTED;
   if (!q || !out || !ws || (((uintptr_t)q | (uintptr_t)out | (uintptr_t)ws) & 15) || ((uintptr_t)lse_out & 3)) return CATEKV_ERR_INVALID_ARG;
