@@ -565,8 +565,9 @@ typedef struct catekv_chunk {
  * segment's own rows or its overflow pages, and seg_len grows by n_new[b] on the device and in the host mirror.
  *   k_new, v_new  device bf16 [n_tokens, Hkv, d] with element strides stride_t, stride_h (multiples of 8; d contiguous), 16-byte aligned
  * CATEKV_ERR_CAPACITY (nothing launched) if a list cannot take its rows: catekv_pages_reserve gives it pages.
- * CATEKV_ERR_INVALID_ARG for a cache without seg_cap_dev.  A replayed call goes by the device's lengths; rows for which a list
- * has no room are dropped and not counted.
+ * CATEKV_ERR_INVALID_ARG for a cache without seg_cap_dev.  A replayed call goes by the device's lengths, so its lists are given room before
+ * it, as for a replayed catekv_append (the mirror: catekv_cache_sync_lengths, or catekv_cache_advance where all sequences grow alike).  Rows
+ * behind the last entry of a list's page table are dropped and not counted; a page that a list has given back may still be an entry.
  */
 int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const void* k_new, const void* v_new, int64_t stride_t,
                         int64_t stride_h, catekv_stream stream);
@@ -582,8 +583,9 @@ int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const vo
  *   lse_out  device float [n_tokens, Hq] or NULL; -inf where nothing is seen
  *   ws       device scratch of at least catekv_chunk_attn_workspace_bytes(Hq, Hkv, the largest n_new[b]), 16-byte aligned; its first
  *            CATEKV_STATUS_BYTES are the status block, which this call does not clear: zero them once
- * fp32 accumulation; the probabilities enter the product with V as a pair of bf16 numbers, 17 significant bits.  An
- * infinity or a NaN in a row reaches the queries that see the row and no other.
+ * fp32 accumulation.  With out_dtype fp32 the probabilities enter the product with V as three bf16 numbers (all their bits), with bf16
+ * as two (17 bits) or, where the queries fill larger blocks, as one (rounded to bf16, as the results are).  An infinity or a NaN in a row
+ * leaves the results of the queries that see the row not finite (in its column, where it is in V) and touches no other.
  * The device's lengths decide, so a captured call follows lists that grow; the lengths on the host (upper bounds will do)
  * only choose the number of CTAs.  Follows overflow pages.  Segment capacities are multiples of CATEKV_SEG_ALIGN, and the cache
  * has seg_cap_dev (CATEKV_ERR_INVALID_ARG).

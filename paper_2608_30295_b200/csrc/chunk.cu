@@ -954,6 +954,11 @@ __device__ __forceinline__ uint8_t* ap_row(const AppendArgs& a, int seg, int r, 
   if (pg < 0 || pg >= a.n_pages) return nullptr;
   return (v ? a.pg.v_ovf : a.pg.k_ovf) + ((int64_t)pg * 64 + (o & 63)) * kRowBytes;
 }
+// How many of n rows behind the list's len fit: all of them, unless a replayed call has found the list full.
+__device__ __forceinline__ int ap_fitting(const AppendArgs& a, int seg, int len, int n) {
+  while (n > 0 && !ap_row(a, seg, len + n - 1, false)) n = max(0, a.seg_cap[seg] + (len + n - 1 - a.seg_cap[seg]) / 64 * 64 - len);
+  return n;
+}
 // One block takes kApRows rows of a list.  kAlone: every list's rows fit one block, which also counts them in.
 template <bool kAlone>
 __global__ void __launch_bounds__(256) append_chunk_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ChunkSeqs sq) {
@@ -981,9 +986,7 @@ __global__ void __launch_bounds__(256) append_chunk_kernel(const __grid_constant
   if (kAlone) {
     __syncthreads();
     if (threadIdx.x == 0) {
-      int m = n;
-      while (m > 0 && !ap_row(a, seg, len + m - 1, false)) --m;  // a replayed call that found a full list: what is there counts
-      a.seg_len[seg] = len + m;
+      a.seg_len[seg] = len + ap_fitting(a, seg, len, n);
     }
   }
 }
@@ -993,9 +996,7 @@ __global__ void __launch_bounds__(128) append_count_kernel(const __grid_constant
   const int seg = blockIdx.x * 128 + threadIdx.x;
   if (seg >= n_segs) return;
   const int n = sq.n_new[seg / a.Hkv], len = a.seg_len[seg];
-  int m = n;
-  while (m > 0 && !ap_row(a, seg, len + m - 1, false)) m = (m - 1) / 64 * 64;
-  if (n) a.seg_len[seg] = len + m;
+  if (n) a.seg_len[seg] = len + ap_fitting(a, seg, len, n);
 }
 
 // ---- host
