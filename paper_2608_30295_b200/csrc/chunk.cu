@@ -243,9 +243,9 @@ __device__ __forceinline__ int ch_v_rows(int seen) { return min(max((seen + 15) 
 // pool row of row r of a list, or of its overflow pages (page < 0: not there)
 __device__ __forceinline__ int ch_page(const ChunkArgs& a, int seg, int o) {
   const int p = o >> 6;
-  int pg = (a.table && p < a.max_pages) ? a.table[(int64_t)seg * a.max_pages + p] : -1;
+  const int pg = (a.table && p < a.max_pages) ? a.table[(int64_t)seg * a.max_pages + p] : -1;
 #ifdef CATEKV_CHECKED
-  pg = checked_clamp(pg, 0, a.n_pages - 1, a.checked, kKidChunk, seg);
+  if (pg < 0 || pg >= a.n_pages) raise_status(a.checked, CATEKV_STATUS_INDEX_RANGE, kKidChunk, seg, pg);
 #endif
   return pg < a.n_pages ? pg : -1;
 }
@@ -947,9 +947,9 @@ __device__ __forceinline__ uint8_t* ap_row(const AppendArgs& a, int seg, int r, 
   if (r < cap) return (v ? a.v_pool : a.k_pool) + ((int64_t)a.seg_off[seg] + r) * kRowBytes;
   const int o = r - cap, p = o >> 6;
   if (!a.pg.table || p >= a.pg.max_pages) return nullptr;
-  int pg = a.pg.table[(int64_t)seg * a.pg.max_pages + p];
+  const int pg = a.pg.table[(int64_t)seg * a.pg.max_pages + p];
 #ifdef CATEKV_CHECKED
-  pg = checked_clamp(pg, 0, a.n_pages - 1, a.checked, kKidChunk, seg);
+  if (pg >= a.n_pages) raise_status(a.checked, CATEKV_STATUS_INDEX_RANGE, kKidChunk, seg, pg);  // (-1: where the list's room ends)
 #endif
   if (pg < 0 || pg >= a.n_pages) return nullptr;
   return (v ? a.pg.v_ovf : a.pg.k_ovf) + ((int64_t)pg * 64 + (o & 63)) * kRowBytes;
