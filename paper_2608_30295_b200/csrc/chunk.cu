@@ -226,7 +226,8 @@ __device__ __forceinline__ float ch_probs(const float* x, float scale, float neg
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
       w[k][c / 2] = pack_bf16(p.x, p.y);
-      if (k + 1 < kParts) p = add2(p, make_float2(-__uint_as_float(w[k][c / 2] << 16), -__uint_as_float(w[k][c / 2] & 0xffff0000u)));
+      if (k + 1 < kParts)  // what is left of it (exact)
+        p = fma2(make_float2(__uint_as_float(w[k][c / 2] << 16), __uint_as_float(w[k][c / 2] & 0xffff0000u)), make_float2(-1.f, -1.f), p);
     }
   }
 #pragma unroll
@@ -1154,7 +1155,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   int64_t sum = 0;
   rc = take_chunk(cache, chunk, &sq, &max_new, &sum);
   if (rc) return rc;
-  if (Hq <= 0 || Hq % cache->Hkv || !(sm_scale >= 0.f && sm_scale <= 3.0e38f) || !caps_on_device(cache)) return CATEKV_ERR_INVALID_ARG;
+  if (Hq <= 0 || Hq % cache->Hkv || !(sm_scale >= 0.f && sm_scale <= 2.0e38f) || !caps_on_device(cache)) return CATEKV_ERR_INVALID_ARG;
   const int G = Hq / cache->Hkv;
   if (G > kMaxG || (out_dtype != CATEKV_OUT_BF16 && out_dtype != CATEKV_OUT_FP32)) return CATEKV_ERR_UNSUPPORTED;
   const int n_segs = cache->B * cache->Hkv;
