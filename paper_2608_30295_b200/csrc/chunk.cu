@@ -821,14 +821,13 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
 // begins inside a block; the first such CTA of a block has it merged.  A thread block takes kRows rows and 32 float4 of d; what threads are left
 // share out the pieces (few rows of one long list come in up to 148), and the groups' sums are added in their order.  Bound by its
 // trips to memory: descriptor, references and sums of all pieces, the pieces.
-constexpr int kChCombineThreads = 1024;
-template <int kRows>
-__global__ void __launch_bounds__(kChCombineThreads) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq,
+template <int kRows, int kThreads>
+__global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq,
                                                                           int C, int two) {
-  constexpr int kGroups = kChCombineThreads / (kRows * 32);
+  constexpr int kGroups = kThreads / (kRows * 32);
   __shared__ float4 s_o[kGroups][kRows][33];
   __shared__ float s_l[kGroups][kRows];
-  __shared__ float s_m[32][kRows];
+  __shared__ float s_m[32][kRows], s_top[kRows];
   pdl_launch_dependents();
   pdl_wait();
   const int c = blockIdx.x;
@@ -854,22 +853,21 @@ __global__ void __launch_bounds__(kChCombineThreads) chunk_combine_kernel(const 
   const int i_row = threadIdx.x % kRows, c4 = threadIdx.x / kRows % 32, group = threadIdx.x / (kRows * 32);
   const int row = row0 + i_row, in_tile = row & 127, n = c_end - (c - 1);
   const bool valid = row / a.G < a.TB && blk * a.TB + row / a.G < n_new;
-  // the rows' largest reference
+  // the rows' largest reference: of few pieces every thread looks at them all, many are shared out
   float M = -INFINITY;
-  if (valid)
-    for (int k = group * 32 + c4; k < n; k += kGroups * 32) M = fmaxf(M, a.part_ml[tile(c - 1 + k) * a.R + in_tile].x);
-  if (kGroups > 1) {
-    if (group == 0) s_m[c4][i_row] = M;
-    for (int g = 1; g < kGroups; ++g) {
-      __syncthreads();
-      if (group == g) s_m[c4][i_row] = fmaxf(s_m[c4][i_row], M);
-    }
+  if (n <= 8) {
+    if (valid)
+      for (int k = 0; k < n; ++k) M = fmaxf(M, a.part_ml[tile(c - 1 + k) * a.R + in_tile].x);
   } else {
-    s_m[c4][i_row] = M;
-  }
-  __syncthreads();
+    if (valid)
+      for (int k = group * 32 + c4; k < n; k += kGroups * 32) M = fmaxf(M, a.part_ml[tile(c - 1 + k) * a.R + in_tile].x);
+    for (int g = 0; g < kGroups; ++g) {
+      if (group == g) s_m[c4][i_row] = g == 0 ? M : fmaxf(s_m[c4][i_row], M);
+      __syncthreads();
+    }
 #pragma unroll
-  for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][i_row]);
+    for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][i_row]);
+  }
   float L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   const int k_lo = n * group / kGroups, k_hi = n * (group + 1) / kGroups;
@@ -880,7 +878,7 @@ __global__ void __launch_bounds__(kChCombineThreads) chunk_combine_kernel(const 
       const float2 ml = a.part_ml[t * a.R + in_tile];
       const float4 v = a.part_o[t * (32 * a.R) + c4 * a.R + in_tile];
       // a row that sees none of this piece's keys has nothing to add, or the NaN that it has met
-      const float w = ml.x > -INFINITY ? exp2f(ml.x - M) : (ml.y == 0.f ? 0.f : 1.f);
+      const float w = ml.x > -INFINITY ? fast_exp2(ml.x - M) : (ml.y == 0.f ? 0.f : 1.f);
       acc.x = fmaf(w, v.x, acc.x);
       acc.y = fmaf(w, v.y, acc.y);
       acc.z = fmaf(w, v.z, acc.z);
@@ -889,11 +887,14 @@ __global__ void __launch_bounds__(kChCombineThreads) chunk_combine_kernel(const 
     }
   }
   s_o[group][i_row][c4] = acc;
-  if (c4 == 0) s_l[group][i_row] = L;
+  if (c4 == 0) {
+    s_l[group][i_row] = L;
+    if (group == 0) s_top[i_row] = M;
+  }
   __syncthreads();
   // a warp a row now: its lanes write it side by side
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = warp; i < kRows; i += kChCombineThreads / 32) {
+  for (int i = warp; i < kRows; i += kThreads / 32) {
     const int tok = (row0 + i) / a.G;
     if (tok >= a.TB || blk * a.TB + tok >= n_new) continue;
     float4 v = s_o[0][i][lane];
@@ -914,16 +915,12 @@ __global__ void __launch_bounds__(kChCombineThreads) chunk_combine_kernel(const 
       pk.y = pack_bf16(v.z * inv, v.w * inv);
       reinterpret_cast<uint2*>(a.out)[orow * 32 + lane] = pk;
     }
-    if (lane == 0 && a.lse) {
-      float m = s_m[0][i];
-      for (int k = 1; k < 32; ++k) m = fmaxf(m, s_m[k][i]);
-      a.lse[orow] = L == 0.f ? -INFINITY : (m + log2f(L)) * 0.6931471805599453f;
-    }
+    if (lane == 0 && a.lse) a.lse[orow] = L == 0.f ? -INFINITY : (s_top[i] + log2f(L)) * 0.6931471805599453f;
   }
 }
-template <int kRows>
+template <int kRows, int kThreads>
 static cudaError_t launch_combine(const ChunkArgs& a, const ChunkSeqs& sq, int ctas, bool two, cudaStream_t st) {
-  return launch_pdl(chunk_combine_kernel<kRows>, dim3(ctas, ((two ? 256 : a.R) + kRows - 1) / kRows), dim3(kChCombineThreads), 0, st, a, sq, ctas,
+  return launch_pdl(chunk_combine_kernel<kRows, kThreads>, dim3(ctas, ((two ? 256 : a.R) + kRows - 1) / kRows), dim3(kThreads), 0, st, a, sq, ctas,
                     two ? 1 : 0);
 }
 
@@ -1230,7 +1227,9 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
        : two      ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st)
                   : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
   if (rc) return rc;
-  CATEKV_CUDA_TRY(two ? launch_combine<32>(a, sq, ctas, two, st) : a.R <= 4 ? launch_combine<4>(a, sq, ctas, two, st)
-                                                                            : launch_combine<8>(a, sq, ctas, two, st));
+  const cudaError_t e = two        ? launch_combine<8, 256>(a, sq, ctas, two, st)
+                        : a.R <= 4 ? launch_combine<4, 1024>(a, sq, ctas, two, st)
+                                   : launch_combine<8, 1024>(a, sq, ctas, two, st);
+  CATEKV_CUDA_TRY(e);
   return CATEKV_OK;
 }
