@@ -292,3 +292,49 @@ def test_a_call_that_is_refused_changes_nothing(ck):
         ck.catekv_chunk_attn(m.cache, ck.Chunk([101, 0]), queries(101, 4), torch.zeros(101, 4, D, device="cuda"))
     assert e.value.code == ck.ERR_INVALID_ARG
     m.verify()
+
+
+@pytest.mark.parametrize("G,m", [(4, 5), (4, 100)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_queries_that_see_nothing(ck, G, m, dtype):
+    """A replayed call may find a list with fewer rows than the chunk has tokens: the first queries then see none of them."""
+    for n in (0, 1, 3, 64):
+        cache, rows = make_cache(ck, 1, 2, [200, 256], [0, 0], seed=9)
+        cache.seg_len_dev.copy_(torch.tensor([n, 256], dtype=torch.int32))
+        for pool in (cache.k_pool, cache.v_pool):
+            pool[int(cache.seg_off[0]) + n:int(cache.seg_off[0]) + 200] = float("nan")
+        q = queries(m, 2 * G)
+        out, lse = run(ck, cache, [m], q, dtype=dtype)
+        none = max(0, m - n)
+        assert (out[:none, :G] == 0).all() and (lse[:none, :G] == float("-inf")).all()
+        # (the other list's results too: where blocks are cut between CTAs, and so the order of the sums, goes by all lists' lengths)
+        for h, length, kv in ((0, n, [x[:n] for x in rows[0]]), (1, 256, rows[1])):
+            at = slice(h * G, (h + 1) * G)
+            for i in range(none if h == 0 else 0, m):
+                see = length - m + i + 1
+                z = q[i, at].double() @ kv[0][:see].T * D ** -0.5
+                assert float((lse[i, at].double() - torch.logsumexp(z, 1)).abs().max()) <= 1e-5
+                p = torch.softmax(z, 1)
+                o = p @ kv[1][:see]
+                # a bf16 result and its probabilities are off by half a step each (2^-8), an fp32 result by 1e-5 of the row
+                tol = 4e-5 if dtype == torch.float32 else 2.0 ** -8
+                bound = tol * (o.abs() + p @ kv[1][:see].abs()) + 4e-5 * o.abs().amax()
+                assert ((out[i, at].double() - o).abs() <= bound).all()
+
+
+def test_the_chunk_steps_of_the_readme(ck):
+    import os
+    import re
+    import paper_2608_30295_b200 as pkg
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        block, = re.findall(r"```py\n(.*?)```", f.read(), flags=re.S)
+    cache = ck.Cache(3, 2, [300] * 6, 0)
+    cache.k_pool.normal_(), cache.v_pool.normal_()
+    cache.set_lengths([300] * 6)
+    names = {"ck": pkg, "cache": cache, "n_pages": 40, "max_pages": 6, "n_new": [5, 1, 80], "Hq": 8, "k_new": queries(86, 2), "v_new": queries(86, 2, 9),
+             "q": queries(86, 8), "out": torch.full((86, 8, D), float("nan"), device="cuda"), "lse": torch.zeros(86, 8, device="cuda"),
+             "n_rejected": [3, 0, 20], "parent": [0, 1, 1]}
+    exec(block, names)
+    assert torch.isfinite(names["out"]).all()
+    assert cache.seg_len.tolist() == cache.seg_len_dev.tolist() == [302, 302, 301, 301, 301, 301]
+    assert names["pages_in_use"] == int(cache.pages.seg_pages.sum())
