@@ -93,13 +93,14 @@ struct ChunkArgs {
 };
 
 struct ChunkSeg {  // one list as the schedule sees it
-  int32_t len, n_new, n_blk, off, cap;
+  int32_t len, n_new, n_blk, off, cap, start, head;  // start: the sequence's first token; head: the list's first query head
 };
 __device__ __forceinline__ void ch_set_len(const ChunkArgs& a, ChunkSeg& g, int s) {
   g.len = min(max(a.seg_len[s], 0), g.cap + CATEKV_PAGE_ROWS * a.max_pages);
 }
 __device__ __forceinline__ ChunkSeg ch_seg(const ChunkArgs& a, const ChunkSeqs& sq, int s, bool with_len) {
-  ChunkSeg g = {0, sq.n_new[s / a.Hkv], 0, 0, 0};
+  const int b = s / a.Hkv;
+  ChunkSeg g = {0, sq.n_new[b], 0, 0, 0, sq.start[b], (s - b * a.Hkv) * a.G};
   g.n_blk = (g.n_new + a.TB - 1) / a.TB;
   if (g.n_blk) {
     g.off = a.seg_off[s];
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
   auto slot_of = [](uint32_t n, int x, int h) { return kSplit ? (int)(2 * (n & 1)) + h : 2 * x + h; };
   auto phase_of = [](uint32_t n) { return (kSplit ? n >> 1 : n) & 1; };
   extern __shared__ uint8_t smem_raw[];
-  __shared__ int s_scan[kWarps], s_first[8];
+  __shared__ int s_scan[kWarps], s_first[10];
   const int tid = threadIdx.x, warp = uni(tid >> 5), lane = tid & 31;
   const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (s_base - smem_u32(smem_raw));
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
     for (int i = 0; i < 5; ++i) asm volatile("prefetch.tensormap [%0];\n" ::"l"(maps[i]) : "memory");
   }
   // The list of this thread: all but its length is there before the kernels ahead have finished.
-  ChunkSeg mine = {0, 0, 0, 0, 0};
+  ChunkSeg mine = {0, 0, 0, 0, 0, 0, 0};
   if (tid < a.n_segs) mine = ch_seg(a, sq, tid, false);
   pdl_wait();
 
@@ -316,41 +317,54 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
     };
     if (mine.n_blk) ch_set_len(a, mine, tid);
     const int cost0 = cost_of(mine);
-    int x = cost0;
-    for (int s = tid + Sh::kThreads; s < a.n_segs; s += Sh::kThreads) x += cost_of(ch_seg(a, sq, s, true));
+    const bool one_pass = a.n_segs <= Sh::kThreads;
+    int inc = cost0;  // of the lists up to this thread's, within the warp
+    if (!one_pass)
+      for (int s = tid + Sh::kThreads; s < a.n_segs; s += Sh::kThreads) inc += cost_of(ch_seg(a, sq, s, true));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    if (lane == 0) s_scan[warp] = x;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 31) s_scan[warp] = inc;
     if (tid == 0) {
-      s_first[0] = a.n_segs;               // no tile: nothing to do
-      a.desc[blockIdx.x * 8 + 2] = 0;      // (no cut at the start of a share, unless there is one)
+      s_first[0] = a.n_segs;           // no tile: nothing to do
+      a.desc[blockIdx.x * 8 + 2] = 0;  // (no cut at the start of a share, unless there is one)
     }
     __syncthreads();
+    int before = 0;  // of the warps before this one
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) total += s_scan[w];
+    for (int w = 0; w < kWarps; ++w) {
+      before += w < warp ? s_scan[w] : 0;
+      total += s_scan[w];
+    }
     const int C = gridDim.x, c = blockIdx.x, q = total / C, r = total - q * C;
     u0 = c * q + min(c, r);
     u1 = u0 + q + (c < r ? 1 : 0);
-    int before = 0;
+    int passed = 0;  // of the lists of earlier rounds
     for (int s0 = 0; s0 < a.n_segs; s0 += Sh::kThreads) {
-      __syncthreads();
       const int s = s0 + tid;
-      if (s0 > 0) mine = s < a.n_segs ? ch_seg(a, sq, s, true) : ChunkSeg{0, 0, 0, 0, 0};
-      const int cost = s0 > 0 ? cost_of(mine) : cost0;
-      int inc = cost;
+      int cost = cost0;
+      if (!one_pass) {
+        __syncthreads();
+        if (s0 > 0) mine = s < a.n_segs ? ch_seg(a, sq, s, true) : ChunkSeg{0, 0, 0, 0, 0, 0, 0};
+        cost = s0 > 0 ? cost_of(mine) : cost0;
+        inc = cost;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-      }
-      if (lane == 31) s_scan[warp] = inc;
-      __syncthreads();
-      int ex = before + inc - cost;
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += y;
+        }
+        if (lane == 31) s_scan[warp] = inc;
+        __syncthreads();
+        before = passed;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        ex += w < warp ? s_scan[w] : 0;
-        before += s_scan[w];
+        for (int w = 0; w < kWarps; ++w) {
+          before += w < warp ? s_scan[w] : 0;
+          passed += s_scan[w];
+        }
       }
+      const int ex = before + inc - cost;
       if (u1 > u0 && u0 >= ex && u0 < ex + cost) {
         int p = u0 - ex, j = 0, nt = ch_tiles(a, mine, 0);
         while (p >= nt + kChCharge) {
@@ -365,6 +379,8 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
         s_first[5] = mine.n_blk;
         s_first[6] = mine.off;
         s_first[7] = mine.cap;
+        s_first[8] = mine.start;
+        s_first[9] = mine.head;
         int4* d = reinterpret_cast<int4*>(a.desc + c * 8);
         d[0] = make_int4(s, j, p, nt);
         d[1] = make_int4(mine.n_new, total, 0, 0);
@@ -380,7 +396,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
   walk.seg = s_first[0];
   walk.blk = s_first[1];
   walk.p = s_first[2];
-  walk.g = ChunkSeg{s_first[3], s_first[4], s_first[5], s_first[6], s_first[7]};
+  walk.g = ChunkSeg{s_first[3], s_first[4], s_first[5], s_first[6], s_first[7], s_first[8], s_first[9]};
   ChunkItem it;
 
   if (warp >= kSoft) {
@@ -477,9 +493,9 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
                     if (64 * h + 16 * kk < rows)
                       umma_bf16_ta(kFlush && part ? d + 128 : d, p + part * 32 + kk * 8, dv + (uint64_t)(kk * 128), idesc,
                                    kk || part > (kFlush ? 1 : 0) ? 1u : (begin ? 0u : 1u));
+                if (h == 1 && t + 1 == n) umma_commit(B(kDoneO + x));  // (the one that is waited for comes first)
                 umma_commit(B(kDonePV + slot));
                 if (h == 1 && x == kTiles - 1) umma_commit(B(kEmptyV + st));
-                if (h == 1 && t + 1 == n) umma_commit(B(kDoneO + x));
               }
             }
           }
@@ -564,7 +580,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
         const int n = uni(it.t1 - it.t0);
         if (n_item >= 1 && !(ok = warp_wait(B(kQEmpty), (n_item - 1) & 1, s_abort, a.spin_limit))) break;
         if (lane == 0) {
-          const int hd = it.seg % a.Hkv * a.G, token = sq.start[it.seg / a.Hkv] + it.blk * a.TB;
+          const int hd = it.g.head, token = it.g.start + it.blk * a.TB;
           mbar_expect_tx(B(kQFull), 2 * 128 * a.G * a.TB);
           tma_load_3d(s_q, &q_map, 0, hd, token, B(kQFull));
           tma_load_3d(s_q + kQBlock, &q_map, 64, hd, token, B(kQFull));
@@ -740,8 +756,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
       const int odd = looked ? s_odd[n_odd & 3] : 0x7fffffff;
       n_odd += looked ? 1 : 0;
       const bool whole = n == it.nt, summed = kFlush && n > kFlush;
-      const int b = it.seg / a.Hkv, h = it.seg - b * a.Hkv;
-      const int64_t orow = (int64_t)(sq.start[b] + token) * a.Hq + h * a.G + (row - tok * a.G);
+      const int64_t orow = (int64_t)(it.g.start + token) * a.Hq + it.g.head + (row - tok * a.G);
       const float fs = sum_ref > -INFINITY ? fast_exp2(sum_ref - ref) : 0.f;
       float4* const part = a.part_o + (int64_t)tile * (32 * a.R) + lane_row;
       const float inv = whole ? (l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l)) : 1.f;  // a NaN stays one
