@@ -1172,6 +1172,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   if (G > kMaxG || (out_dtype != CATEKV_OUT_BF16 && out_dtype != CATEKV_OUT_FP32)) return CATEKV_ERR_UNSUPPORTED;
   const int n_segs = cache->B * cache->Hkv;
   int64_t units_of[2] = {0, 0}, blocks_of[2] = {0, 0};  // tiles and blocks with one M tile, with two
+  int64_t most = 0;  // what the schedule could count up to, if a replayed call found the lists full
   for (int s = 0; s < n_segs; ++s) {
     const int n = sq.n_new[s / cache->Hkv], len = cache->seg_len[s];
     if (cache->seg_cap[s] < 0 || cache->seg_cap[s] % CATEKV_SEG_ALIGN || cache->seg_off[s] < 0) return CATEKV_ERR_INVALID_ARG;
@@ -1179,6 +1180,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
     for (int w = 0; w < 2; ++w) {
       const int TB = (w ? 256 : 128) / G;
       blocks_of[w] += (n + TB - 1) / TB;
+      if (w == 0) most += (int64_t)((n + TB - 1) / TB) * (seg_capacity(cache, s) / kKeyTile + 1 + kChCharge);
       for (int j = 0; j < n; j += TB) units_of[w] += (len - n + (n < j + TB ? n : j + TB) + kKeyTile - 1) / kKeyTile;
     }
   }
@@ -1188,7 +1190,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   const int TB = (two ? 256 : 128) / G;
   const int64_t units = units_of[two], blocks = blocks_of[two];
   if (sum == 0) return CATEKV_OK;
-  if (units > 0x7fffffff) return CATEKV_ERR_UNSUPPORTED;
+  if (most > 0x7fffffff) return CATEKV_ERR_UNSUPPORTED;  // (a minute's work: such a chunk is brought in by parts)
   if (!q || !out || !ws || (((uintptr_t)q | (uintptr_t)out | (uintptr_t)ws) & 15) || ((uintptr_t)lse_out & 3)) return CATEKV_ERR_INVALID_ARG;
   if ((Hq > 1 && (q_stride_h < kD || q_stride_h % 8)) || (chunk->n_tokens > 1 && (q_stride_t < kD || q_stride_t % 8))) return CATEKV_ERR_UNSUPPORTED;
   const ChunkWs W = chunk_ws_layout(G, max_new);

@@ -221,3 +221,14 @@ def test_binding_refuses(ck):
         with pytest.raises(ck.CatekvError) as e:
             ck._per_sequence("x", Cache, x)
         assert e.value.code == ck.ERR_INVALID_ARG
+
+
+def test_chunks_beyond_the_schedules_count_are_refused(ck):
+    """The schedule counts blocks times tiles in 32 bits, and a replayed call may find lists as long as their capacities."""
+    n = 1 << 20
+    big = Fake(ck, [n] * 64)
+    assert attend(ck, big, chunk(ck, [n]), Hq=64, st_t=64 * 128) == ck.ERR_UNSUPPORTED
+    roomy = Fake(ck, [2048] * 64, max_new=4 * n)  # 16 blocks of a list, 32 K tiles each once it is full
+    assert attend(ck, roomy, chunk(ck, [2048]), Hq=64, st_t=64 * 128, ws=None) == ck.ERR_INVALID_ARG  # fits the count: the next check speaks
+    roomy = Fake(ck, [8192] * 512, B=8, max_new=2 * n)  # 512 lists x 512 blocks x 16 K tiles once they are full
+    assert attend(ck, roomy, chunk(ck, [8192] * 8), Hq=512, st_t=512 * 128) == ck.ERR_UNSUPPORTED
