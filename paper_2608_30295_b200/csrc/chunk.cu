@@ -76,6 +76,7 @@ struct ChunkArgs {
   int32_t max_pages, n_pages;
   int32_t n_segs, Hkv, G, Hq;
   int32_t TB;  // tokens of a query block
+  int32_t TQ;  // tokens of a load
   int32_t R;   // rows of a tile of part_o and part_ml
   float scale_log2;
   void* out;
@@ -302,6 +303,10 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
 #pragma unroll
     for (int i = 0; i < 5; ++i) asm volatile("prefetch.tensormap [%0];\n" ::"l"(maps[i]) : "memory");
   }
+  // Rows of the block without a query are zeros, and so are their S and P: the tensor cores draw less for them, and calls back to back run at
+  // the power limit (4 tokens of 16 x 32K rows for 0.3 s: 385 us a call with whatever lay there, 355 with zeros; a single call 346).
+  for (int i = tid; i < kQBytes / 16; i += Sh::kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+  fence_async_smem();
   // The list of this thread: all but its length is there before the kernels ahead have finished.
   ChunkSeg mine = {0, 0, 0, 0, 0, 0, 0};
   if (tid < a.n_segs) mine = ch_seg(a, sq, tid, false);
@@ -575,15 +580,25 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
       const uint32_t idesc = umma_idesc_bf16(128, 64), tm = (uint32_t)uni((int)tmem);
       const uint64_t dq0 = umma_desc_sw128(s_q), dk0 = umma_desc_sw128(s_k);
       uint32_t n_item = 0, n_t = 0;
+      int q_rows = 0;  // rows of the query block that are not zeros
       bool ok = true;
       while (ok && walk.next(a, sq, it)) {
         const int n = uni(it.t1 - it.t0);
         if (n_item >= 1 && !(ok = warp_wait(B(kQEmpty), (n_item - 1) & 1, s_abort, a.spin_limit))) break;
-        if (lane == 0) {
-          const int hd = it.g.head, token = it.g.start + it.blk * a.TB;
-          mbar_expect_tx(B(kQFull), 2 * 128 * a.G * a.TB);
-          tma_load_3d(s_q, &q_map, 0, hd, token, B(kQFull));
-          tma_load_3d(s_q + kQBlock, &q_map, 64, hd, token, B(kQFull));
+        const int loads = (min(it.g.n_new - it.blk * a.TB, a.TB) + a.TQ - 1) / a.TQ, rows = loads * a.TQ * a.G;
+        for (int r = rows + (lane >> 3); r < q_rows; r += 4) {  // rows that the block before had
+          *reinterpret_cast<uint4*>(smem + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          *reinterpret_cast<uint4*>(smem + kQBlock + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        if (rows < q_rows) fence_async_smem();
+        q_rows = rows;
+        if (lane == 0) mbar_expect_tx(B(kQFull), 256 * rows);
+        __syncwarp();
+        if (lane < loads) {  // (at most eight)
+          const uint32_t dst = s_q + lane * a.TQ * a.G * 128;
+          const int token = it.g.start + it.blk * a.TB + lane * a.TQ;
+          tma_load_3d(dst, &q_map, 0, it.g.head, token, B(kQFull));
+          tma_load_3d(dst + kQBlock, &q_map, 64, it.g.head, token, B(kQFull));
         }
         __syncwarp();
         ok = warp_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit);
@@ -640,7 +655,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
       const bool idle = !__any_sync(0xffffffffu, valid);   // no row of the warp is a query: it only keeps the barriers going
       const int tile = (blockIdx.x * 2 + (first_item ? 0 : 1)) * kTiles + x;  // of partial results
       first_item = false;
-      float ref = -INFINITY, l = 0.f, sum_ref = -INFINITY;
+      float ref = valid ? -INFINITY : INFINITY, l = 0.f, sum_ref = -INFINITY;  // (no query: every P is 0)
       float sum[kFlush ? 128 : 1];
       for (int i = 0; alive && i < n; ++i, ++n_s) {
         const bool fresh = kFlush ? i % max(kFlush, 1) == 0 : i == 0;
@@ -672,7 +687,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
           if (kSplit) {
             // The two steps' threads of a row share its reference: each decides after the other has decided for the step before.  Only that is serial.
             if (n_dec + g > 0 && !(alive = mbar_wait(B(kDec + quarter), (n_dec + g - 1) & 1, s_abort, a.spin_limit))) break;
-            ref_o = i + g > 0 ? s_ref[(g ^ 1) * 128 + lane_row] : -INFINITY;
+            ref_o = i + g > 0 ? s_ref[(g ^ 1) * 128 + lane_row] : ref;
           }
           const bool grow = mx > ref_o + kChTau;  // also the first step with a visible key
           const float ref_n = grow ? mx : ref_o;
@@ -1188,6 +1203,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   // few tokens only that their blocks would be half empty (512 tokens beside 31 single ones over 8 x 8000 rows each: 285 us with two, 257 with one).
   const bool two = out_dtype == CATEKV_OUT_BF16 && units_of[1] * 7 < units_of[0] * 5;
   const int TB = (two ? 256 : 128) / G;
+  const int box = 32 % G == 0 ? 32 / G : TB, TQ = max_new < box ? max_new : box;  // loads of 32 rows, where tokens come to that
   const int64_t units = units_of[two], blocks = blocks_of[two];
   if (sum == 0) return CATEKV_OK;
   if (most > 0x7fffffff) return CATEKV_ERR_UNSUPPORTED;  // (a minute's work: such a chunk is brought in by parts)
@@ -1201,7 +1217,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   const catekv_pages* pg = cache->pages;
   if (!rc) rc = make_pool_map(pg ? pg->k_ovf : cache->k_pool, pg ? (int64_t)pg->n_pages * CATEKV_PAGE_ROWS : cache->total_rows, CATEKV_PAGE_ROWS, &m[2]);
   if (!rc) rc = make_pool_map(pg ? pg->v_ovf : cache->v_pool, pg ? (int64_t)pg->n_pages * CATEKV_PAGE_ROWS : cache->total_rows, CATEKV_PAGE_ROWS, &m[3]);
-  if (!rc) rc = make_q_map(q, chunk->n_tokens, Hq, G, TB, q_stride_t, q_stride_h, &m[4]);
+  if (!rc) rc = make_q_map(q, chunk->n_tokens, Hq, G, TQ, q_stride_t, q_stride_h, &m[4]);
   if (rc) return rc;
   uint8_t* w8 = (uint8_t*)ws;
   ChunkArgs a = {};
@@ -1220,6 +1236,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   a.G = G;
   a.Hq = Hq;
   a.TB = TB;
+  a.TQ = TQ;
   a.R = W.R;
   a.scale_log2 = (sm_scale == 0.f ? 1.f / sqrtf((float)kD) : sm_scale) * 1.4426950408889634f;
   a.out = out;
