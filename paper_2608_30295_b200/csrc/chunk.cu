@@ -41,6 +41,7 @@
 namespace catekv {
 
 constexpr int kChMaxSeqs = 512;  // sequences of a call: their counts travel in the kernel's arguments
+constexpr int kChMaxCtas = 256;
 constexpr int kChTileBytes = 128 * 256;  // a [128 x 128] bf16 tile
 constexpr int kChTmemCols = 512;         // slots of S / P in columns 0-255, the M tiles' accumulators at 256 and 384
 constexpr float kChTau = 8.f;
@@ -848,27 +849,73 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
 }
 
 // Merge the pieces of the blocks that several CTAs share, in the order of the keys: CTA c's descriptor says whether its share
-// begins inside a block; the first such CTA of a block has it merged.  A thread block takes kRows rows and 32 float4 of d; what threads are left
-// share out the pieces (few rows of one long list come in up to 148), and the groups' sums are added in their order.  Bound by its
-// trips to memory: descriptor, references and sums of all pieces, the pieces.
-template <int kRows, int kThreads>
+// begins inside a block; the first such CTA of a block has it merged.  A thread block takes kRows rows, a thread kVec float4 of a row; what threads are
+// left share out the pieces (few rows of one long list come in up to 148), and the groups' sums are merged in their order.  Bound by its trips
+// to memory: descriptor, pieces; so references are not looked through first, the sums follow them piece by piece.
+struct ChunkSum {
+  float m, l;  // reference (log2 domain), sum
+  // the weights of what is there and of what comes; a part that sees no key has nothing to add, or the NaN that it has met
+  __device__ __forceinline__ float2 add(float m2, float l2) {
+    float f = 1.f, w = l2 == 0.f ? 0.f : 1.f;
+    if (m2 > -INFINITY) {
+      const float top = fmaxf(m, m2);
+      f = m > -INFINITY ? fast_exp2(m - top) : 1.f;
+      w = fast_exp2(m2 - top);
+      m = top;
+    }
+    l = fmaf(w, l2, l * f);
+    return make_float2(f, w);
+  }
+};
+__device__ __forceinline__ void ch_blend(float4& acc, const float4& v, float2 fw) {
+  acc.x = fmaf(fw.y, v.x, acc.x * fw.x);
+  acc.y = fmaf(fw.y, v.y, acc.y * fw.x);
+  acc.z = fmaf(fw.y, v.z, acc.z * fw.x);
+  acc.w = fmaf(fw.y, v.w, acc.w * fw.x);
+}
+template <int kRows, int kThreads, int kVec>
 __global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkSeqs sq,
                                                                           int C, int two) {
-  constexpr int kGroups = kThreads / (kRows * 32);
+  constexpr int kCols = 32 / kVec, kGroups = kThreads / (kRows * kCols), kAtOnce = 4;
   __shared__ float4 s_o[kGroups][kRows][33];
-  __shared__ float s_l[kGroups][kRows];
-  __shared__ float s_m[32][kRows], s_top[kRows];
+  __shared__ float2 s_ml[kGroups][kRows];
   pdl_launch_dependents();
   pdl_wait();
-  const int c = blockIdx.x;
-  const int32_t* d = a.desc + c * 8;
-  const int p0 = d[2];
-  if (ch_tile_at(p0) == 0) return;
-  const int seg = d[0], blk = d[1], nt = d[3], n_new = d[4], total = d[5];
+  // the blockIdx.x-th CTA that has a block merged (launched for all CTAs, most thread blocks would find nothing to do, at 5 ns each)
+  __shared__ int s_flags[kThreads / 32], s_pick;
+  __shared__ int4 s_desc[2];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  {
+    const int c = threadIdx.x;
+    bool merges = false;
+    int4 d0, d1;
+    if (c > 0 && c < C) {
+      d0 = reinterpret_cast<const int4*>(a.desc)[c * 2];
+      d1 = reinterpret_cast<const int4*>(a.desc)[c * 2 + 1];
+      const int total = d1.y, q = total / C, r = total - q * C;
+      const int ub = c * q + min(c, r) - d0.z;
+      merges = ch_tile_at(d0.z) > 0 && ch_tile_at((c - 1) * q + min(c - 1, r) - ub) == 0;  // (no earlier CTA begins inside the block)
+    }
+    const uint32_t flags = __ballot_sync(0xffffffffu, merges);
+    if (lane == 0) s_flags[warp] = __popc(flags);
+    if (threadIdx.x == 0) s_pick = 0;
+    __syncthreads();
+    int rank = __popc(flags & ((1u << lane) - 1));
+    for (int w = 0; w < warp; ++w) rank += s_flags[w];
+    if (merges && rank == (int)blockIdx.x) {
+      s_pick = c;
+      s_desc[0] = d0;
+      s_desc[1] = d1;
+    }
+    __syncthreads();
+  }
+  const int c = s_pick;
+  if (c == 0) return;
+  const int4 d0 = s_desc[0], d1 = s_desc[1];
+  const int seg = d0.x, blk = d0.y, nt = d0.w, n_new = d1.x, total = d1.y;
   const int q = total / C, r = total % C;
   auto begin = [&](int i) { return i * q + min(i, r); };
-  const int ub = begin(c) - p0, ue = ub + nt + kChCharge;  // the block's units
-  if (ch_tile_at(begin(c - 1) - ub) > 0) return;  // an earlier CTA begins inside this block
+  const int ub = begin(c) - d0.z, ue = ub + nt + kChCharge;  // the block's units
   // the CTAs that begin before its end: begin(k) < ue
   int c_end = q ? (ue > r * (q + 1) ? r + (ue - r * (q + 1) + q - 1) / q : (ue + q) / (q + 1)) : min(ue, C);
   c_end = min(c_end, C);
@@ -880,62 +927,48 @@ __global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_co
     const int i = k == c - 1 ? head : 0;
     return (int64_t)(two ? (k * 2 + i) * 2 + x : k * 2 + i);
   };
-  const int i_row = threadIdx.x % kRows, c4 = threadIdx.x / kRows % 32, group = threadIdx.x / (kRows * 32);
+  const int i_row = threadIdx.x % kRows, c4 = threadIdx.x / kRows % kCols, group = threadIdx.x / (kRows * kCols);
   const int row = row0 + i_row, in_tile = row & 127, n = c_end - (c - 1);
   const bool valid = row / a.G < a.TB && blk * a.TB + row / a.G < n_new;
-  // the rows' largest reference: of few pieces every thread looks at them all, many are shared out
-  float M = -INFINITY;
-  if (n <= 8) {
-    if (valid)
-      for (int k = 0; k < n; ++k) M = fmaxf(M, a.part_ml[tile(c - 1 + k) * a.R + in_tile].x);
-  } else {
-    if (valid)
-      for (int k = group * 32 + c4; k < n; k += kGroups * 32) M = fmaxf(M, a.part_ml[tile(c - 1 + k) * a.R + in_tile].x);
-    for (int g = 0; g < kGroups; ++g) {
-      if (group == g) s_m[c4][i_row] = g == 0 ? M : fmaxf(s_m[c4][i_row], M);
-      __syncthreads();
-    }
+  ChunkSum sum = {-INFINITY, 0.f};
+  float4 acc[kVec];
 #pragma unroll
-    for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][i_row]);
-  }
-  float L = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int k_lo = n * group / kGroups, k_hi = n * (group + 1) / kGroups;
+  for (int j = 0; j < kVec; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (valid) {
-#pragma unroll 4
-    for (int k = k_lo; k < k_hi; ++k) {
-      const int64_t t = tile(c - 1 + k);
-      const float2 ml = a.part_ml[t * a.R + in_tile];
-      const float4 v = a.part_o[t * (32 * a.R) + c4 * a.R + in_tile];
-      // a row that sees none of this piece's keys has nothing to add, or the NaN that it has met
-      const float w = ml.x > -INFINITY ? fast_exp2(ml.x - M) : (ml.y == 0.f ? 0.f : 1.f);
-      acc.x = fmaf(w, v.x, acc.x);
-      acc.y = fmaf(w, v.y, acc.y);
-      acc.z = fmaf(w, v.z, acc.z);
-      acc.w = fmaf(w, v.w, acc.w);
-      L = fmaf(w, ml.y, L);
+    const int k_hi = c - 1 + n * (group + 1) / kGroups;
+    for (int k0 = c - 1 + n * group / kGroups; k0 < k_hi; k0 += kAtOnce) {
+      float2 ml[kAtOnce];
+      float4 v[kAtOnce][kVec];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        if (k0 + u < k_hi) {
+          const int64_t t = tile(k0 + u);
+          ml[u] = a.part_ml[t * a.R + in_tile];
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) v[u][j] = a.part_o[t * (32 * a.R) + (c4 + j * kCols) * a.R + in_tile];
+        }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        if (k0 + u < k_hi) {
+          const float2 fw = sum.add(ml[u].x, ml[u].y);
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) ch_blend(acc[j], v[u][j], fw);
+        }
     }
   }
-  s_o[group][i_row][c4] = acc;
-  if (c4 == 0) {
-    s_l[group][i_row] = L;
-    if (group == 0) s_top[i_row] = M;
-  }
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) s_o[group][i_row][c4 + j * kCols] = acc[j];
+  if (c4 == 0) s_ml[group][i_row] = make_float2(sum.m, sum.l);
   __syncthreads();
   // a warp a row now: its lanes write it side by side
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = warp; i < kRows; i += kThreads / 32) {
     const int tok = (row0 + i) / a.G;
     if (tok >= a.TB || blk * a.TB + tok >= n_new) continue;
     float4 v = s_o[0][i][lane];
-    L = s_l[0][i];
-#pragma unroll
-    for (int g = 1; g < kGroups; ++g) {
-      const float4 y = s_o[g][i][lane];
-      v = make_float4(v.x + y.x, v.y + y.y, v.z + y.z, v.w + y.w);
-      L += s_l[g][i];
-    }
-    const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+    sum = ChunkSum{s_ml[0][i].x, s_ml[0][i].y};
+#pragma unroll 4
+    for (int g = 1; g < kGroups; ++g) ch_blend(v, s_o[g][i][lane], sum.add(s_ml[g][i].x, s_ml[g][i].y));
+    const float inv = sum.l > 0.f ? 1.f / sum.l : (sum.l == 0.f ? 0.f : sum.l);
     const int64_t orow = (int64_t)(sq.start[b] + blk * a.TB + tok) * a.Hq + h * a.G + (row0 + i) % a.G;
     if (a.out_fp32) {
       reinterpret_cast<float4*>(a.out)[orow * 32 + lane] = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
@@ -945,13 +978,14 @@ __global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_co
       pk.y = pack_bf16(v.z * inv, v.w * inv);
       reinterpret_cast<uint2*>(a.out)[orow * 32 + lane] = pk;
     }
-    if (lane == 0 && a.lse) a.lse[orow] = L == 0.f ? -INFINITY : (s_top[i] + log2f(L)) * 0.6931471805599453f;
+    if (lane == 0 && a.lse) a.lse[orow] = sum.l == 0.f ? -INFINITY : (sum.m + log2f(sum.l)) * 0.6931471805599453f;
   }
 }
-template <int kRows, int kThreads>
-static cudaError_t launch_combine(const ChunkArgs& a, const ChunkSeqs& sq, int ctas, bool two, cudaStream_t st) {
-  return launch_pdl(chunk_combine_kernel<kRows, kThreads>, dim3(ctas, ((two ? 256 : a.R) + kRows - 1) / kRows), dim3(kThreads), 0, st, a, sq, ctas,
-                    two ? 1 : 0);
+template <int kRows, int kThreads, int kVec>
+static cudaError_t launch_combine(const ChunkArgs& a, const ChunkSeqs& sq, int blocks, int ctas, bool two, cudaStream_t st) {
+  static_assert(kThreads >= kChMaxCtas, "a thread looks at a CTA");
+  return launch_pdl(chunk_combine_kernel<kRows, kThreads, kVec>, dim3(blocks, ((two ? 256 : a.R) + kRows - 1) / kRows), dim3(kThreads), 0, st, a, sq,
+                    ctas, two ? 1 : 0);
 }
 
 // ---- append: the chunk's rows behind the end of every list.  A warp copies a row (lanes 0-15 K, 16-31 V), eight in flight.
@@ -1255,15 +1289,22 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   // As many shares as there are tiles, up to one a CTA; lists of one or two tiles stay whole (a second tile costs 1.5 us, a merge 4: 8.4 against 12.5 us
   // for a token over 8 lists of 128 rows, while lists of 500 rows gain by being cut, 12.5 against 14.7).
   const int64_t shares = units <= 2 * blocks ? blocks : units;
-  const int ctas = (int)(shares < sm_count() ? shares : sm_count());
+  const int most_ctas = sm_count() < kChMaxCtas ? sm_count() : kChMaxCtas, ctas = (int)(shares < most_ctas ? shares : most_ctas);
   cudaStream_t st = (cudaStream_t)stream;
   rc = a.out_fp32 ? launch_chunk<false, 3, 3>(ctas, m, a, sq, st)
        : two      ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st)
                   : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
   if (rc) return rc;
-  const cudaError_t e = two        ? launch_combine<8, 256>(a, sq, ctas, two, st)
-                        : a.R <= 4 ? launch_combine<4, 1024>(a, sq, ctas, two, st)
-                                   : launch_combine<8, 1024>(a, sq, ctas, two, st);
+  if (ctas == 1) return CATEKV_OK;
+  const int merged = (int)(blocks < ctas - 1 ? blocks : ctas - 1);  // blocks that may be cut
+  // Threads to share out the pieces where a block of queries is cut into many (one list of 60 K rows, 149 pieces: 9.3 us with one row a thread block, 11
+  // with 4, 20 with 8; 8 lists of 2 K, 19 pieces of 4 rows: 5.5 with 4, 7.9 with 32), more rows where it is into few (3 lists of 118 K and 512
+  // tokens, 7 pieces of 256 rows: 8.6 us with 32, 13.7 with 8; 32 lists of 16 K, 5 pieces of 16 rows: 6.8 and 5.5).
+  const int pieces = ctas / merged + 1;
+  const cudaError_t e = pieces > 96   ? launch_combine<1, 1024, 1>(a, sq, merged, ctas, two, st)
+                        : pieces > 12 ? launch_combine<4, 1024, 1>(a, sq, merged, ctas, two, st)
+                        : a.R <= 16   ? launch_combine<8, 512, 1>(a, sq, merged, ctas, two, st)
+                                      : launch_combine<32, 256, 4>(a, sq, merged, ctas, two, st);
   CATEKV_CUDA_TRY(e);
   return CATEKV_OK;
 }
