@@ -898,10 +898,14 @@ __global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_co
     }
     const uint32_t flags = __ballot_sync(0xffffffffu, merges);
     if (lane == 0) s_flags[warp] = __popc(flags);
-    if (threadIdx.x == 0) s_pick = 0;
     __syncthreads();
-    int rank = __popc(flags & ((1u << lane) - 1));
-    for (int w = 0; w < warp; ++w) rank += s_flags[w];
+    int rank = __popc(flags & ((1u << lane) - 1)), all = 0;
+#pragma unroll
+    for (int w = 0; w < (kThreads < kChMaxCtas ? kThreads : kChMaxCtas) / 32; ++w) {
+      rank += w < warp ? s_flags[w] : 0;
+      all += s_flags[w];
+    }
+    if ((int)blockIdx.x >= all) return;
     if (merges && rank == (int)blockIdx.x) {
       s_pick = c;
       s_desc[0] = d0;
@@ -910,7 +914,6 @@ __global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_co
     __syncthreads();
   }
   const int c = s_pick;
-  if (c == 0) return;
   const int4 d0 = s_desc[0], d1 = s_desc[1];
   const int seg = d0.x, blk = d0.y, nt = d0.w, n_new = d1.x, total = d1.y;
   const int q = total / C, r = total % C;
