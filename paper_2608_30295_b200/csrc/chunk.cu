@@ -59,9 +59,9 @@ struct ChunkShape {
   static constexpr size_t kSmem = 1024 + (size_t)(kTiles + kStagesK + kStagesV) * kChTileBytes + kChBarriers * 8 + 64 + (kSplit ? 4 * 128 * sizeof(float) : 0);
   static_assert(kSmem <= 226 * 1024, "chunk_attn_kernel: one CTA's shared memory");
 };
-// A block costs a CTA more than its tiles (its queries, a pipeline that fills and drains, its results): this many tiles are charged for it when the
-// shares are cut.
-constexpr int kChCharge = 3;
+// Tiles that a block is charged (ChunkArgs::charge), with one M tile and with two.  One M tile: 64 x 300 rows of 8 heads, 4 tokens, 31.8 us with 3, 34.7
+// with 2, 34.2 with 4; two: 4096 tokens alone 142.3 with 2, 148 with 3, 148.5 with 1.
+constexpr int kChCharge = 3, kChChargeTwo = 2;
 
 struct ChunkSeqs {  // host counts of every sequence
   int32_t n_new[kChMaxSeqs];
@@ -79,6 +79,7 @@ struct ChunkArgs {
   int32_t TB;  // tokens of a query block
   int32_t TQ;  // tokens of a load
   int32_t R;   // rows of a tile of part_o and part_ml
+  int32_t charge;  // tiles that a block is charged beyond its own when the shares are cut: its queries, a pipeline that fills and drains, its results
   float scale_log2;
   void* out;
   float* lse;
@@ -118,7 +119,7 @@ __device__ __forceinline__ int ch_tiles(const ChunkArgs& a, const ChunkSeg& g, i
 }
 
 // a position among a block's units (the charge, then its tiles) -> its tile
-__device__ __forceinline__ int ch_tile_at(int p) { return max(0, p - kChCharge); }
+__device__ __forceinline__ int ch_tile_at(const ChunkArgs& a, int p) { return max(0, p - a.charge); }
 
 struct ChunkItem {
   int32_t seg, blk, t0, t1, nt;  // tiles [t0, t1) of the block's nt
@@ -138,9 +139,9 @@ struct ChunkWalk {
     it.seg = seg;
     it.blk = blk;
     it.nt = ch_tiles(a, g, blk);
-    const int end = min(it.nt + kChCharge, p + left);
-    it.t0 = ch_tile_at(p);
-    it.t1 = ch_tile_at(end);
+    const int end = min(it.nt + a.charge, p + left);
+    it.t0 = ch_tile_at(a, p);
+    it.t1 = ch_tile_at(a, end);
     it.g = g;
     left -= end - p;
     p = 0;
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
   {
     auto cost_of = [&](const ChunkSeg& g) {
       int c = 0;
-      for (int j = 0; j < g.n_blk; ++j) c += ch_tiles(a, g, j) + kChCharge;
+      for (int j = 0; j < g.n_blk; ++j) c += ch_tiles(a, g, j) + a.charge;
       return c;
     };
     if (mine.n_blk) ch_set_len(a, mine, tid);
@@ -373,8 +374,8 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
       const int ex = before + inc - cost;
       if (u1 > u0 && u0 >= ex && u0 < ex + cost) {
         int p = u0 - ex, j = 0, nt = ch_tiles(a, mine, 0);
-        while (p >= nt + kChCharge) {
-          p -= nt + kChCharge;
+        while (p >= nt + a.charge) {
+          p -= nt + a.charge;
           nt = ch_tiles(a, mine, ++j);
         }
         s_first[0] = s;
@@ -894,7 +895,7 @@ __global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_co
       d1 = reinterpret_cast<const int4*>(a.desc)[c * 2 + 1];
       const int total = d1.y, q = total / C, r = total - q * C;
       const int ub = c * q + min(c, r) - d0.z;
-      merges = ch_tile_at(d0.z) > 0 && ch_tile_at((c - 1) * q + min(c - 1, r) - ub) == 0;  // (no earlier CTA begins inside the block)
+      merges = ch_tile_at(a, d0.z) > 0 && ch_tile_at(a, (c - 1) * q + min(c - 1, r) - ub) == 0;  // (no earlier CTA begins inside the block)
     }
     const uint32_t flags = __ballot_sync(0xffffffffu, merges);
     if (lane == 0) s_flags[warp] = __popc(flags);
@@ -918,7 +919,7 @@ __global__ void __launch_bounds__(kThreads) chunk_combine_kernel(const __grid_co
   const int seg = d0.x, blk = d0.y, nt = d0.w, n_new = d1.x, total = d1.y;
   const int q = total / C, r = total % C;
   auto begin = [&](int i) { return i * q + min(i, r); };
-  const int ub = begin(c) - d0.z, ue = ub + nt + kChCharge;  // the block's units
+  const int ub = begin(c) - d0.z, ue = ub + nt + a.charge;  // the block's units
   // the CTAs that begin before its end: begin(k) < ue
   int c_end = q ? (ue > r * (q + 1) ? r + (ue - r * (q + 1) + q - 1) / q : (ue + q) / (q + 1)) : min(ue, C);
   c_end = min(c_end, C);
@@ -1275,6 +1276,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   a.TB = TB;
   a.TQ = TQ;
   a.R = W.R;
+  a.charge = two ? kChChargeTwo : kChCharge;
   a.scale_log2 = (sm_scale == 0.f ? 1.f / sqrtf((float)kD) : sm_scale) * 1.4426950408889634f;
   a.out = out;
   a.lse = lse_out;
@@ -1289,9 +1291,9 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
     a.spin_limit = 512;
     a.idle_producer = 1;
   }
-  // As many shares as there are tiles, up to one a CTA; lists of one or two tiles stay whole (a second tile costs 1.5 us, a merge 4: 8.4 against 12.5 us
-  // for a token over 8 lists of 128 rows, while lists of 500 rows gain by being cut, 12.5 against 14.7).
-  const int64_t shares = units <= 2 * blocks ? blocks : units;
+  // As many shares as there are tiles, up to one a CTA; short lists stay whole (a merge costs 2 us, a further tile 0.8, in fp32 1.2: a token over 8 lists of
+  // 200 rows 7.8 against 10.1 us, 4 x 500 rows of 8 heads 10.4 against 11.7; but 8 lists of 600 rows 11 whole, 10.3 cut, and in fp32 of 500 rows 16.7 and 14.2).
+  const int64_t shares = units <= (a.out_fp32 ? 3 : 4) * blocks ? blocks : units;
   const int most_ctas = sm_count() < kChMaxCtas ? sm_count() : kChMaxCtas, ctas = (int)(shares < most_ctas ? shares : most_ctas);
   cudaStream_t st = (cudaStream_t)stream;
   rc = a.out_fp32 ? launch_chunk<false, 3, 3>(ctas, m, a, sq, st)
