@@ -2,7 +2,8 @@
 //
 // Host bookkeeping over the mirrors, and one kernel that carries its orders in its arguments (no copy from host memory that a caller would
 // have to keep, nothing to wait for): 64 rows of K and V copied to a page, entries of the page table and segment descriptions set.
-// Bound by the copied rows (1 KB a row, K and V, read and written) where there are many, by the launch where there are few.  The kernels do
+// Bound by the copied rows (1 KB a row, K and V, read and written) where there are many, by the launch where there are few
+// (64 lists, 40 rows each copied: 5 us with cold caches; 466 pages moved, 30 MB: 7 us).  The kernels do
 // not signal their dependents early: they write rows and table entries that a decode plan may know.
 //
 // Rows are shared, not copied, where that is possible.  A list that continues from another one (fork) reads the parent's rows in place up to the

@@ -1,6 +1,6 @@
 """Chunks of new tokens: append and attention against the definition in 64 bits.
 
-Tolerances.  fp32 results: a logit carries an error of about 2^-23 of its size, a probability 2^-18 (two bf16 parts, rounded to nearest) and the
+Tolerances.  fp32 results: a logit carries an error of about 2^-23 of its size, a probability 2^-22 (exp2; its three bf16 parts have all bits) and the
 accumulators 2^-24 a step; relative L2 1e-5 leaves a factor of a few over the sum of these.  bf16 results are off by half a step of the type
 more, 2^-8 of the value at most, and so is every probability on its way into the product (it is rounded to bf16 where the blocks are large): with
 p (1 + e), |e| <= 2^-8, the result moves by at most 2^-8 sum p |v|.  Element by element.  lse: 1e-5 of its size."""
