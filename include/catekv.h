@@ -582,7 +582,8 @@ int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const vo
  *   out      device [n_tokens, Hq, d] contiguous, bf16 or float per out_dtype, 16-byte aligned; a query that sees nothing gets 0
  *   lse_out  device float [n_tokens, Hq] or NULL; -inf where nothing is seen
  *   ws       device scratch of at least catekv_chunk_attn_workspace_bytes(Hq, Hkv, the largest n_new[b]), 16-byte aligned; its first
- *            CATEKV_STATUS_BYTES are the status block, which this call does not clear: zero them once
+ *            CATEKV_STATUS_BYTES are the status block, which this call does not clear: zero them once.  Calls that may run at the same time
+ *            (streams, replayed graphs) need a workspace each
  * fp32 accumulation.  With out_dtype fp32 the probabilities enter the product with V as three bf16 numbers (all their bits), with bf16
  * as two (17 bits) or, where the queries fill larger blocks, as one (rounded to bf16, as the results are).  An infinity or a NaN in a row
  * leaves the results of the queries that see the row not finite (in its column, where it is in V) and touches no other.
