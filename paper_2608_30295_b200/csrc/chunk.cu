@@ -25,7 +25,8 @@
 // 2 lists of 65 K rows in 296 us.
 //
 // Precision.  kParts = 1: P rounded to bf16 (2^-9), as the result will be: bf16 results with two M tiles, where the products bound the kernel.
-// 2 (bf16 results, one M tile): 17 significant bits.  3 (fp32 results): all of fp32's.  The tensor cores add with truncation, and what that loses
+// 2 (bf16 results, one M tile): 17 significant bits; where the block has at most 64 rows they may lie in the M tile twice (kDup): the copies' softmax comes out
+// the same, their warps write the second part, one instruction multiplies both, and the results are added at the end.  3 (fp32 results): all of fp32's.  The tensor cores add with truncation, and what that loses
 // goes by the accumulator's size and the number of instructions.  For fp32 results the parts behind the first therefore have an accumulator of their
 // own, 2^-9 as large, and both are added, with rounding, to a sum in the thread's registers every kFlush tiles, where the products start from zero
 // (relative error of 64K rows: 5e-6 with one accumulator and a flush every 16 tiles).  That takes one M tile, whatever the number of rows.
@@ -52,8 +53,9 @@ constexpr int kChMaxCtas = 256;
 constexpr int kChTileBytes = 128 * 256;  // a [128 x 128] bf16 tile
 constexpr int kChTmemCols = 512;         // slots of S / P in columns 0-255, the M tiles' accumulators at 256 and 384
 constexpr float kChTau = 8.f;
-constexpr int kChBarriers = 44;
-template <bool kQ2, int kFlush>
+constexpr int kChBarriers = 52;
+constexpr int kLowStride = 36;  // floats: rows of 32 columns handed over in shared memory
+template <bool kQ2, int kFlush, bool kDup>
 struct ChunkShape {
   static constexpr bool kSplit = !kQ2 && !kFlush;   // one M tile, bf16 results: the steps of a tile have softmax warps of their own
   static constexpr int kTiles = kQ2 ? 2 : 1;        // M tiles
@@ -63,7 +65,8 @@ struct ChunkShape {
   // Slot of step h of a tile: 2 x + h for M tile x; kSplit: four slots, 2 (tile mod 2) + h, so that S is formed two tiles ahead.
   static constexpr int kSlotCols = kFlush ? 128 : 64;
   static constexpr int kLead = kSplit ? 2 : 1;      // K tiles loaded ahead of the V tile: K_0 .. K_{lead-1}, V_0, K_lead, V_1, ...
-  static constexpr size_t kSmem = 1024 + (size_t)(kTiles + kStagesK + kStagesV) * kChTileBytes + kChBarriers * 8 + 64 + (kSplit ? 4 * 128 * sizeof(float) : 0);
+  static constexpr size_t kSmem = 1024 + (size_t)(kTiles + kStagesK + kStagesV) * kChTileBytes + kChBarriers * 8 + 64 + (kSplit ? 4 * 128 * sizeof(float) : 0) +
+                                  (kDup ? 2 * 64 * kLowStride * sizeof(float) : 0);
   static_assert(kSmem <= 226 * 1024, "chunk_attn_kernel: one CTA's shared memory");
 };
 // Tiles that a block is charged (ChunkArgs::charge), with one M tile and with two.  One M tile: 64 x 300 rows of 8 heads, 4 tokens, 31.8 us with 3, 34.7
@@ -222,8 +225,9 @@ __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t (&v)[8]
                : "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-// kN logits -> probabilities of kN keys in kParts bf16 numbers, kN / 2 columns each, `step` columns from part to part; returns their sum
-template <int kN, int kParts>
+// kN logits -> probabilities of kN keys in kParts bf16 numbers, kN / 2 columns each, `step` columns from part to part; returns their sum.
+// kLastOnly: the last of the parts alone, at step 0.
+template <int kN, int kParts, bool kLastOnly = false>
 __device__ __forceinline__ float ch_probs(const float* x, float scale, float neg_ref, uint32_t to, uint32_t step) {
   float2 s0 = make_float2(0.f, 0.f), s1 = s0;
   uint32_t w[kParts][kN / 2];
@@ -242,7 +246,7 @@ __device__ __forceinline__ float ch_probs(const float* x, float scale, float neg
     }
   }
 #pragma unroll
-  for (int k = 0; k < kParts; ++k) {
+  for (int k = kLastOnly ? kParts - 1 : 0; k < kParts; ++k) {
     if constexpr (kN == 32) tmem_st16u(to + k * step, w[k]);
     else tmem_st8u(to + k * step, w[k]);
   }
@@ -262,13 +266,13 @@ __device__ __forceinline__ int ch_page(const ChunkArgs& a, int seg, int o) {
   return pg < a.n_pages ? pg : -1;
 }
 
-template <bool kQ2, int kParts, int kFlush>
-__global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
+template <bool kQ2, int kParts, int kFlush, bool kDup>
+__global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
     chunk_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                       const __grid_constant__ CUtensorMap ko_map, const __grid_constant__ CUtensorMap vo_map,
                       const __grid_constant__ CUtensorMap q_map, const __grid_constant__ ChunkArgs a,
                       const __grid_constant__ ChunkSeqs sq) {
-  using Sh = ChunkShape<kQ2, kFlush>;
+  using Sh = ChunkShape<kQ2, kFlush, kDup>;
   constexpr int kStagesK = Sh::kStagesK, kStagesV = Sh::kStagesV, kTiles = Sh::kTiles, kLead = Sh::kLead, kSoft = Sh::kSoft, kWarps = Sh::kWarps;
   constexpr int kQBytes = kTiles * kChTileBytes, kQBlock = kQBytes / 2;
   constexpr bool kSplit = Sh::kSplit;
@@ -287,12 +291,13 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int* s_odd = reinterpret_cast<int*>(s_tmem + 4);  // [4]: first new row with an infinity or a NaN in V, of the last blocks that had V tiles looked at
   float* s_ref = reinterpret_cast<float*>(s_tmem + 16);  // kSplit: [step][row] the rows' references, then their sums
+  float* s_low = s_ref + 4 * 128;  // kDup: [step][64 rows][kLowStride]
   const uint32_t bar0 = smem_u32(s_bar);
   auto B = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   constexpr int kFullK = 0, kEmptyK = kFullK + kStagesK, kFullV = kEmptyK + kStagesK, kEmptyV = kFullV + kStagesV, kFixed = kEmptyV + kStagesV,
                 kDoneS = kFixed + kStagesV, kPReady = kDoneS + 4, kDonePV = kPReady + 4, kDoneO = kDonePV + 4, kQFull = kDoneO + 2, kQEmpty = kQFull + 1,
-                kDec = kQEmpty + 1, kXch = kDec + 4;
-  static_assert(kXch + 4 <= kChBarriers, "barrier table");
+                kDec = kQEmpty + 1, kXch = kDec + 4, kLowFull = kXch + 4, kLowEmpty = kLowFull + 4;
+  static_assert(kLowEmpty + 4 <= kChBarriers, "barrier table");
 
   pdl_launch_dependents();
   if (tid == 0) {
@@ -598,16 +603,24 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
         for (int r = rows + (lane >> 3); r < q_rows; r += 4) {  // rows that the block before had
           *reinterpret_cast<uint4*>(smem + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           *reinterpret_cast<uint4*>(smem + kQBlock + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          if constexpr (kDup) {
+            *reinterpret_cast<uint4*>(smem + (64 + r) * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(smem + kQBlock + (64 + r) * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
         }
         if (rows < q_rows) fence_async_smem();
         q_rows = rows;
-        if (lane == 0) mbar_expect_tx(B(kQFull), 256 * rows);
+        if (lane == 0) mbar_expect_tx(B(kQFull), (kDup ? 512 : 256) * rows);
         __syncwarp();
         if (lane < loads) {  // (at most eight)
           const uint32_t dst = s_q + lane * a.TQ * a.G * 128;
           const int token = it.g.start + it.blk * a.TB + lane * a.TQ;
           tma_load_3d(dst, &q_map, 0, it.g.head, token, B(kQFull));
           tma_load_3d(dst + kQBlock, &q_map, 64, it.g.head, token, B(kQFull));
+          if constexpr (kDup) {
+            tma_load_3d(dst + 64 * 128, &q_map, 0, it.g.head, token, B(kQFull));
+            tma_load_3d(dst + kQBlock + 64 * 128, &q_map, 64, it.g.head, token, B(kQFull));
+          }
         }
         __syncwarp();
         ok = warp_wait(B(kQFull), n_item & 1, s_abort, a.spin_limit);
@@ -650,10 +663,11 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
     const int lane_row = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
     const uint32_t acc = tmem + lane_base + 256 + x * 128;
-    const int row = x * 128 + lane_row;  // row of the block
+    const int row = kDup ? lane_row & 63 : x * 128 + lane_row;  // row of the block
+    const bool low = kDup && quarter >= 2;  // of the copies, whose warps write the low parts
     const int tok = row / a.G;
     float* const s_l = s_ref + 256;
-    uint32_t n_s = 0, n_o = 0, n_odd = 0, n_dec = 0, n_x = 0;
+    uint32_t n_s = 0, n_o = 0, n_odd = 0, n_dec = 0, n_x = 0, n_low = 0;
     bool alive = true, first_item = true;
     while (alive && walk.next(a, sq, it)) {
       const int n = it.t1 - it.t0;
@@ -727,6 +741,9 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
           if (kFlush) {
 #pragma unroll
             for (int c = 0; c < 64; c += 16) l += ch_probs<16, kParts>(y + c, a.scale_log2, neg, slot + c / 2, 32);
+          } else if (low) {
+            l += ch_probs<32, 2, true>(y, a.scale_log2, neg, slot, 0);
+            l += ch_probs<32, 2, true>(y + 32, a.scale_log2, neg, slot + 16, 0);
           } else {
             l += ch_probs<32, kParts>(y, a.scale_log2, neg, slot, 32);
             l += ch_probs<32, kParts>(y + 32, a.scale_log2, neg, slot + 16, 32);
@@ -798,6 +815,26 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
 #pragma unroll
             for (int c = 0; c < 32; ++c) o[c] = summed ? fmaf(sum[cc + c], fs, o[c] + o1[c]) : o[c] + o1[c];
           }
+          if constexpr (kDup) {  // the low parts' products, from the copy's warp
+            float4* const z = reinterpret_cast<float4*>(s_low + (g * 64 + row) * kLowStride);
+            const uint32_t pair = g * 2 + (quarter & 1);
+            if (low) {
+              if (n_low > 0 && !(alive = mbar_wait(B(kLowEmpty + pair), (n_low - 1) & 1, s_abort, a.spin_limit))) break;
+#pragma unroll
+              for (int c = 0; c < 8; ++c) z[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+            } else {
+              if (!(alive = mbar_wait(B(kLowFull + pair), n_low & 1, s_abort, a.spin_limit))) break;
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                const float4 w = z[c];
+                o[4 * c] += w.x, o[4 * c + 1] += w.y, o[4 * c + 2] += w.z, o[4 * c + 3] += w.w;
+              }
+            }
+            ++n_low;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(B((low ? kLowFull : kLowEmpty) + pair));
+            if (low) continue;
+          }
           if (odd < sees && valid) {  // infinities and NaN that were taken out of the V tiles
             const int off = it.g.off, cap = it.g.cap;
             for (int j = max(odd, it.t0 * kKeyTile); j < min(sees, it.t1 * kKeyTile); ++j) {
@@ -832,7 +869,8 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush>::kThreads, 1)
             }
           }
         }
-        if (valid && g == 0) {
+        if (!alive) break;
+        if (valid && g == 0 && !low) {
           if (!whole) a.part_ml[(int64_t)tile * a.R + lane_row] = make_float2(ref, l);
           else if (a.lse) a.lse[orow] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
         }
@@ -1149,16 +1187,16 @@ static int make_q_map(const void* q, int n_tokens, int Hq, int G, int TB, int64_
   return r == CUDA_SUCCESS ? CATEKV_OK : CATEKV_ERR_UNSUPPORTED;
 }
 
-template <bool kQ2, int kParts, int kFlush>
+template <bool kQ2, int kParts, int kFlush, bool kDup>
 static int launch_chunk(int ctas, const CUtensorMap* m, const ChunkArgs& a, const ChunkSeqs& sq, cudaStream_t st) {
   static std::atomic<bool> attr_set[64];
   int dev = 0;
   CATEKV_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts, kFlush>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ChunkShape<kQ2, kFlush>::kSmem));
+    CATEKV_CUDA_TRY(cudaFuncSetAttribute(chunk_attn_kernel<kQ2, kParts, kFlush, kDup>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ChunkShape<kQ2, kFlush, kDup>::kSmem));
     if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
   }
-  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts, kFlush>, dim3(ctas), dim3(ChunkShape<kQ2, kFlush>::kThreads), ChunkShape<kQ2, kFlush>::kSmem, st, m[0], m[1], m[2], m[3], m[4],
+  CATEKV_CUDA_TRY(launch_pdl(chunk_attn_kernel<kQ2, kParts, kFlush, kDup>, dim3(ctas), dim3(ChunkShape<kQ2, kFlush, kDup>::kThreads), ChunkShape<kQ2, kFlush, kDup>::kSmem, st, m[0], m[1], m[2], m[3], m[4],
                              a, sq));
   return CATEKV_OK;
 }
@@ -1304,10 +1342,15 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   // 200 rows 7.8 against 10.1 us, 4 x 500 rows of 8 heads 10.4 against 11.7; but 8 lists of 600 rows 11 whole, 10.3 cut, and in fp32 of 500 rows 16.7 and 14.2).
   const int64_t shares = units <= (a.out_fp32 ? 3 : 4) * blocks ? blocks : units;
   const int most_ctas = sm_count() < kChMaxCtas ? sm_count() : kChMaxCtas, ctas = (int)(shares < most_ctas ? shares : most_ctas);
+  // Low parts of P in rows of their own, where at most half of the M tile's rows are queries and the stream is long: half the products, and at the power
+  // limit that is time (4 tokens of 16 x 32 K rows back to back 400 us without, 367 with; a token over 8 x 32 K rows, 14 tiles a CTA, 31.1 and 30.5; 4 tokens of
+  // 16 x 1 K rows, 7 tiles, 19.4 and 20.3: results are handed from warp to warp).
+  const bool dup = (int64_t)G * max_new <= 64 && units >= 12 * (int64_t)sm_count();
   cudaStream_t st = (cudaStream_t)stream;
-  rc = a.out_fp32 ? launch_chunk<false, 3, 3>(ctas, m, a, sq, st)
-       : two      ? launch_chunk<true, 1, 0>(ctas, m, a, sq, st)
-                  : launch_chunk<false, 2, 0>(ctas, m, a, sq, st);
+  rc = a.out_fp32 ? launch_chunk<false, 3, 3, false>(ctas, m, a, sq, st)
+       : two      ? launch_chunk<true, 1, 0, false>(ctas, m, a, sq, st)
+       : dup      ? launch_chunk<false, 1, 0, true>(ctas, m, a, sq, st)
+                  : launch_chunk<false, 2, 0, false>(ctas, m, a, sq, st);
   if (rc) return rc;
   if (ctas == 1) return CATEKV_OK;
   const int merged = (int)(blocks < ctas - 1 ? blocks : ctas - 1);  // blocks that may be cut

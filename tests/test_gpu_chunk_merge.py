@@ -94,3 +94,41 @@ def test_pieces_that_see_nothing_or_meet_an_infinity(ck, n_new):
         out, _ = run(ck, cache, [n_new], q, dtype=dtype)
         bad = ~torch.isfinite(out)
         assert bad[..., 9].all() and not bad[..., :7].any() and not bad[..., 10:].any()
+
+
+@pytest.mark.parametrize("G,n_new", [(4, [4, 0, 16, 1]), (7, [9, 2, 1, 9]), (1, [64, 1, 33, 32]), (8, [1, 1, 1, 1]), (3, [21, 20, 1, 0])])
+def test_few_rows_over_long_lists(ck, G, n_new):
+    """bf16 results, at most 64 query rows a block, more than 1776 tiles in all: the form whose low parts have rows of their own."""
+    B, Hkv = 4, 8
+    base = [9000, 8192, 7000 + 61, 10000] * 8
+    cache, rows = make_cache(ck, B, Hkv, base, [70, 0, 5, 200] * 8, seed=G)
+    q = queries(sum(n_new), Hkv * G)
+    start = [sum(n_new[:b]) for b in range(B)]
+    want = reference(rows, q, n_new, start, Hkv, D ** -0.5)
+    out, lse = run(ck, cache, n_new, q, dtype=torch.bfloat16)
+    check(out, lse, want, 3.0)
+    # the two parts of P carry 17 bits: what is left is the rounding of the result
+    there = ~torch.isnan(want[1])
+    w, g = want[0][there], out[there].double()
+    assert ((g - w).abs() <= w.abs() * 2.0 ** -8 + 1e-5 * w.abs().amax(dim=-1, keepdim=True) * 4).all()
+    again, lse2 = run(ck, cache, n_new, q, dtype=torch.bfloat16)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_few_rows_over_long_lists_with_numbers_that_are_not_finite(ck):
+    n_new, Hkv, G = [5, 3], 8, 4
+    cache, rows = make_cache(ck, 2, Hkv, [16000] * 16, [40] * 16, seed=8)
+    q = queries(8, Hkv * G)
+    want = reference(rows, q, n_new, [0, 5], Hkv, D ** -0.5)
+    n = 16040
+    poke(cache, 0, n - 3, 11, float("inf"), "v")    # the third of five new rows: tokens 2, 3 and 4 see it
+    poke(cache, 9, n - 1, 12, float("nan"), "k")    # list (1, 1): the last token alone
+    poke(cache, 2, 77, 5, float("-inf"), "v")       # an old row: every token of the list
+    out, lse = run(ck, cache, n_new, q, dtype=torch.bfloat16)
+    bad = ~torch.isfinite(out)
+    assert bad[2:5, 0:G, 11].all() and bad[7, G:2 * G].all() and bad[:5, 2 * G:3 * G, 5].all()
+    bad[2:5, 0:G, 11] = bad[7, G:2 * G] = bad[:5, 2 * G:3 * G, 5] = False
+    assert not bad.any()
+    fine = torch.isfinite(out)
+    tol = (want[0].abs() + want[2]) * 2.0 ** -8 + 1e-5 * want[0].abs().amax(dim=-1, keepdim=True) * 4
+    assert ((out.double() - want[0]).abs() <= tol)[fine].all()
