@@ -1285,7 +1285,8 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
     }
   }
   // A tile takes 2400 cycles for one M tile (the stream of K and V bounds it) and 3400 for two (the products do): two, unless so many sequences have a
-  // few tokens only that their blocks would be half empty (512 tokens beside 31 single ones over 8 x 8000 rows each: 285 us with two, 257 with one).
+  // few tokens only that their blocks would be half empty (over 8 x 8000 rows each: 512 tokens beside 31 single ones 277 us with two, 242 with one; 8 sequences of
+  // 40 tokens 73 and 91; 4 of 128 beside 16 single ones, where the rule is at its border, 184 and 185).
   const bool two = out_dtype == CATEKV_OUT_BF16 && units_of[1] * 7 < units_of[0] * 5;
   const int TB = (two ? 256 : 128) / G;
   const int box = 32 % G == 0 ? 32 / G : TB, TQ = max_new < box ? max_new : box;  // loads of 32 rows, where tokens come to that
