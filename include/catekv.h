@@ -585,7 +585,7 @@ int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const vo
  *            CATEKV_STATUS_BYTES are the status block, which this call does not clear: zero them once.  Calls that may run at the same time
  *            (streams, replayed graphs) need a workspace each
  * fp32 accumulation.  With out_dtype fp32 the probabilities enter the product with V as three bf16 numbers (all their bits), with bf16
- * as two (17 bits) or, where the queries fill larger blocks, as one (rounded to bf16, as the results are).  An infinity or a NaN in a row
+ * as two (17 bits).  An infinity or a NaN in a row
  * leaves the results of the queries that see the row not finite (in its column, where it is in V) and touches no other.
  * The device's lengths decide, so a captured call follows lists that grow; the lengths on the host (upper bounds will do)
  * only choose the number of CTAs.  Follows overflow pages.  Segment capacities are multiples of CATEKV_SEG_ALIGN, and the cache

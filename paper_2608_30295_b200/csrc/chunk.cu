@@ -3,8 +3,8 @@
 //   out = softmax(sm_scale q K^T) V,   lse = log sum exp(sm_scale q K^T).
 //
 // One pass over K and V with a running reference and sum per query row.  The query rows of a (sequence, KV head) are its
-// tokens' heads, row r = token * G + head, so that a K tile is read once for the whole group; a block of them is 256 rows
-// (two M = 128 tiles, template kQ2) or, where no sequence has more than 128 rows, 128 rows.  chunk_attn_kernel is persistent,
+// tokens' heads, row r = token * G + head, so that a K tile is read once for the whole group; a block of them is 128 rows (an M = 128 tile) or,
+// where K and V are more than L2 holds, 256 (two, template kQ2).  chunk_attn_kernel is persistent,
 // one CTA per SM: the 128-key tiles of all blocks of all lists, laid end to end, are cut into equal shares, from the device's lengths
 // (a captured call follows lists that grow).  A block that several CTAs share leaves partial results, which
 // chunk_combine_kernel merges in the order of the keys.
@@ -15,17 +15,18 @@
 // rounded rest of those before it; O += P V takes P from tensor memory and V as the MN-major operand as TMA left it.  Every M tile has softmax
 // warps of its own, an accumulator, and two slots of S / P, so that S of the next step is formed while the softmax is at this one.
 // (Steps of 128 keys have room for one slot only beside two accumulators: softmax and products of an M tile took turns, 4100
-// cycles a tile for two M tiles, 3400 with steps of 64, where the products need 2050; S with 64 keys reads its Q operand twice as often.)  One M tile with
+// cycles a tile for two M tiles and P in one part, 3400 with steps of 64, where the products need 2050; S with 64 keys reads its Q operand twice as often.)  One M tile with
 // bf16 results (kSplit) has four slots and softmax warps for either step of a tile: S is formed two tiles ahead, as few rows are a chain of waits otherwise.
 //
-// Bounds and measures (B200, single runs).  Two M tiles: the products; 4096 tokens over 8 lists of 16 K rows, G = 4, in 1030 to 1080 us, 1100 to 1200
-// TFLOP/s at a power-limited 1.6 to 1.75 GHz; 4096 tokens alone in 142 us.  One M tile: K and V once through DRAM; 4 tokens of 16 x 32 K rows in 311 to
-// 346 us, 6.2 to 6.9 TB/s; a token over 8 lists of 128 rows in 7.9 us, which are waits one behind the other (schedule 1 us, loads 1, S, softmax and product 2.5,
+// Bounds and measures (B200, single runs).  Full blocks: the products, three for the formula's two; 4096 tokens over 8 lists of 16 K rows, G = 4, in 1300 us
+// with either form (950 TFLOP/s of the formula's, 1400 of the three products); 4096 tokens alone in 179 us; two M tiles, 512 tokens over 3 lists of 117 K
+// rows, in 417 us.  Few rows: K and V once through DRAM; 4 tokens of 16 x 32 K rows in 311 to 346 us, 6.2 to 6.9 TB/s; a token over 8 lists of 128 rows in 7.9 us, which are waits one behind the other (schedule 1 us, loads 1, S, softmax and product 2.5,
 // results 0.7, the merge's launch).  fp32 results: three products for one, and the softmax's conversions; 333 tokens of 7 heads a group over
 // 2 lists of 65 K rows in 296 us.
 //
-// Precision.  kParts = 1: P rounded to bf16 (2^-9), as the result will be: bf16 results with two M tiles, where the products bound the kernel.
-// 2 (bf16 results, one M tile): 17 significant bits; where the block has at most 64 rows they may lie in the M tile twice (kDup): the copies' softmax comes out
+// Precision.  kParts = 2 (bf16 results): P with 17 significant bits in every form, so that the result's own rounding is what is seen of it (with P in one bf16
+// number, 2^-9, 512 tokens over 117 K rows take 341 us for 417, and the error of results in the norm is 2.3e-3 for 1.65e-3; which form runs
+// goes by the other sequences of the batch too).  Where the block has at most 64 rows they may lie in the M tile twice (kDup, kParts = 1): the copies' softmax comes out
 // the same, their warps write the second part, one instruction multiplies both, and the results are added at the end.  3 (fp32 results): all of fp32's.  The tensor cores add with truncation, and what that loses
 // goes by the accumulator's size and the number of instructions.  For fp32 results the parts behind the first therefore have an accumulator of their
 // own, 2^-9 as large, and both are added, with rounding, to a sum in the thread's registers every kFlush tiles, where the products start from zero
@@ -70,8 +71,9 @@ struct ChunkShape {
   static_assert(kSmem <= 226 * 1024, "chunk_attn_kernel: one CTA's shared memory");
 };
 // Tiles that a block is charged (ChunkArgs::charge), with one M tile and with two.  One M tile: 64 x 300 rows of 8 heads, 4 tokens, 31.8 us with 3, 34.7
-// with 2, 34.2 with 4; two: 4096 tokens alone 142.3 with 2, 148 with 3, 148.5 with 1.
+// with 2, 34.2 with 4; two: 64 tokens of 16 x 2500 rows of 8 heads 81.8 us with 2, 89.2 with 3, 86.4 with 1.
 constexpr int kChCharge = 3, kChChargeTwo = 2;
+constexpr int64_t kChL2Rows = (int64_t)120e6 / (2 * kRowBytes);  // rows whose K and V fill L2 (126 MB)
 
 struct ChunkSeqs {  // host counts of every sequence
   int32_t n_new[kChMaxSeqs];
@@ -1273,10 +1275,12 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   const int n_segs = cache->B * cache->Hkv;
   int64_t units_of[2] = {0, 0}, blocks_of[2] = {0, 0};  // tiles and blocks with one M tile, with two
   int64_t most = 0;  // what the schedule could count up to, if a replayed call found the lists full
+  int64_t rows = 0;  // of the lists that have queries
   for (int s = 0; s < n_segs; ++s) {
     const int n = sq.n_new[s / cache->Hkv], len = cache->seg_len[s];
     if (cache->seg_cap[s] < 0 || cache->seg_cap[s] % CATEKV_SEG_ALIGN || cache->seg_off[s] < 0) return CATEKV_ERR_INVALID_ARG;
     if (len < n || len > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;  // the chunk's rows are the list's last ones
+    if (n) rows += len;
     for (int w = 0; w < 2; ++w) {
       const int TB = (w ? 256 : 128) / G;
       blocks_of[w] += (n + TB - 1) / TB;
@@ -1284,10 +1288,12 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
       for (int j = 0; j < n; j += TB) units_of[w] += (len - n + (n < j + TB ? n : j + TB) + kKeyTile - 1) / kKeyTile;
     }
   }
-  // A tile takes 2400 cycles for one M tile (the stream of K and V bounds it) and 3400 for two (the products do): two, unless so many sequences have a
-  // few tokens only that their blocks would be half empty (over 8 x 8000 rows each: 512 tokens beside 31 single ones 277 us with two, 242 with one; 8 sequences of
-  // 40 tokens 73 and 91; 4 of 128 beside 16 single ones, where the rule is at its border, 184 and 185).
-  const bool two = out_dtype == CATEKV_OUT_BF16 && units_of[1] * 7 < units_of[0] * 5;
+  // Two M tiles read K and V half as often.  Where L2 holds them that is no gain, and one M tile, whose steps have warps of their own, is faster (512 tokens over
+  // 8 x 16 K rows 155 us with one, 165 with two; 4096 alone 179 and 185; 8 x 100 tokens over 2000 rows 63 and 71); where it does not, the second reading
+  // comes from DRAM (512 tokens over 8 x 32 K rows 340 and 308, 8 x 48 K 532 and 463, 3 x 117 K 466 and 417).  Unless so many sequences have a few tokens only
+  // that the blocks would be half empty (over 8 x 65 K rows each: 512 tokens beside two single ones, 0.56 of the tiles, 790 and 771; beside four, 0.6, 897
+  // and 904; 512 beside 31 over 8 x 8000 rows 229 and 371).
+  const bool two = out_dtype == CATEKV_OUT_BF16 && rows > kChL2Rows && units_of[1] * 5 < units_of[0] * 3;
   const int TB = (two ? 256 : 128) / G;
   const int box = 32 % G == 0 ? 32 / G : TB, TQ = max_new < box ? max_new : box;  // loads of 32 rows, where tokens come to that
   const int64_t units = units_of[two], blocks = blocks_of[two];
@@ -1349,7 +1355,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   const bool dup = (int64_t)G * max_new <= 64 && units >= 12 * (int64_t)sm_count();
   cudaStream_t st = (cudaStream_t)stream;
   rc = a.out_fp32 ? launch_chunk<false, 3, 3, false>(ctas, m, a, sq, st)
-       : two      ? launch_chunk<true, 1, 0, false>(ctas, m, a, sq, st)
+       : two      ? launch_chunk<true, 2, 0, false>(ctas, m, a, sq, st)
        : dup      ? launch_chunk<false, 1, 0, true>(ctas, m, a, sq, st)
                   : launch_chunk<false, 2, 0, false>(ctas, m, a, sq, st);
   if (rc) return rc;
