@@ -329,7 +329,8 @@ int catekv_cache_advance(catekv_cache* cache, int32_t n_tokens);
 /*
  * Paged growth.  Makes sure that every segment can take n_new more rows: segments whose capacity
  * (seg_cap + 64 * seg_pages) is short get further overflow pages, the lowest free ones in the order of the segments; the new table
- * entries reach the device on `stream`, in a small kernel's arguments.  CATEKV_ERR_CAPACITY (nothing changed) if the overflow pools or a
+ * entries reach the device on `stream`, in a small kernel's arguments: a call that hands out pages cannot be captured in a graph
+ * (CATEKV_ERR_UNSUPPORTED, nothing changed), where they would be the same pages at every replay.  CATEKV_ERR_CAPACITY (nothing changed) if the overflow pools or a
  * segment's table row run out; CATEKV_ERR_INVALID_ARG if the cache has no pages.  Decode plans built before
  * stay valid.  catekv_cache_regrow with such a cache as the source gathers base rows and pages into one
  * contiguous segment again.

@@ -281,7 +281,7 @@ static int check_paged(const catekv_cache* c) {
   }
   return CATEKV_OK;
 }
-// The calls below change the host's tables: one that is captured would be replayed without that.
+// The calls below change the host's tables: one that is captured would be replayed without that, and name pages again that are other lists' by then.
 static int check_not_captured(cudaStream_t st) {
   cudaStreamCaptureStatus s = cudaStreamCaptureStatusNone;
   CATEKV_CUDA_TRY(cudaStreamIsCapturing(st, &s));
@@ -333,7 +333,8 @@ extern "C" int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_s
     }
     if (want > have && !orders.entries((int64_t)s * p->max_pages + have, given.p + g0, want - have)) return CATEKV_ERR_WORKSPACE;
   }
-  rc = send(cache, orders, (cudaStream_t)stream);
+  rc = check_not_captured((cudaStream_t)stream);
+  if (!rc) rc = send(cache, orders, (cudaStream_t)stream);
   if (rc) return rc;
   size_t g = 0;
   int top = p->next_free;
