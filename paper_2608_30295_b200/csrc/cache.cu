@@ -18,7 +18,9 @@ __global__ void __launch_bounds__(128) append_kernel(uint8_t* k_pool, uint8_t* v
   int64_t row = (int64_t)seg_off[seg] + len;
   if (pg.table && len >= pg.seg_cap[seg]) {  // the row goes to an overflow page
     const int o = len - pg.seg_cap[seg];
-    row = (int64_t)pg.table[(int64_t)seg * pg.max_pages + (o >> 6)] * 64 + (o & 63);
+    const int page = (o >> 6) < pg.max_pages ? pg.table[(int64_t)seg * pg.max_pages + (o >> 6)] : -1;
+    if (page < 0) return;  // a replayed call whose list was not given room: the row is dropped and not counted
+    row = (int64_t)page * 64 + (o & 63);
     k_pool = pg.k_ovf;
     v_pool = pg.v_ovf;
   }

@@ -197,6 +197,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
   // ---- producer
   int p_item = item_begin, p_tile = 0, p_seq = 0;
   int ix[(kTile * 16) / kDecodeThreads];  // indexed variant: see load_idx
+#ifdef CATEKV_CHECKED
+  bool waited = false;
+#endif
   auto issue_tile = [&]() {  // tile p_tile of the producer's item into stage p_seq % kStages
     const uint32_t sb = s_stage + (p_seq % kStages) * kStageBytes;
     int start, rows_left;
@@ -211,16 +214,17 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
       page0 = __ldg(row + min(pg0, a.max_pages - 1));
       page1 = __ldg(row + min(pg0 + 1, a.max_pages - 1));
 #ifdef CATEKV_CHECKED
-      // a page the tile's valid rows reach must have been handed out (an entry behind them may still be -1)
-      if (start + rows_left > pc.cap + pg0 * 64) page0 = checked_clamp(page0, 0, a.n_pages - 1, a.chk, kKidAttention, pc.seg);
-      if (start + rows_left > pc.cap + (pg0 + 1) * 64) page1 = checked_clamp(page1, 0, a.n_pages - 1, a.chk, kKidAttention, pc.seg);
+      // a page the tile's valid rows reach must have been handed out (an entry behind them may be -1; before the wait these are the plan's rows)
+      const int none = waited ? 0 : -1;
+      if (start + rows_left > pc.cap + pg0 * 64) page0 = checked_clamp(page0, none, a.n_pages - 1, a.chk, kKidAttention, pc.seg);
+      if (start + rows_left > pc.cap + (pg0 + 1) * 64) page1 = checked_clamp(page1, none, a.n_pages - 1, a.chk, kKidAttention, pc.seg);
 #endif
     }
 #pragma unroll
     for (int i = 0; i < (kTile * 16) / kDecodeThreads; ++i) {
       const int id = tid + i * kDecodeThreads;
       const int r = id >> 4, c = id & 15;
-      const int ok = r < rows_left ? 16 : 0;
+      int ok = r < rows_left ? 16 : 0;
       int64_t grow = ok ? row0 + r : 0;  // padding rows read nothing
       uint8_t* kp = a.k_pool;
       uint8_t* vp = a.v_pool;
@@ -230,8 +234,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
 #endif
       if (kIndexed && pc.indexed && ok) grow = (pc.row_base - pc.t0) + ix[i];
       if (kPaged && ok && start + r >= pc.cap) {  // the row lives in an overflow page
-        const int o = start + r - pc.cap;
-        grow = (int64_t)((o >> 6) == pg0 ? page0 : page1) * 64 + (o & 63);
+        const int o = start + r - pc.cap, page = (o >> 6) == pg0 ? page0 : page1;
+        if (page < 0) ok = 0;  // given back since the plan was made: no row of the list lies there
+        grow = ok ? (int64_t)page * 64 + (o & 63) : 0;
         kp = a.k_ovf;
         vp = a.v_ovf;
       }
@@ -309,6 +314,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
     cp_async_commit();
   }
   pdl_wait();  // from here on: lengths, queries and rows written by earlier kernels
+#ifdef CATEKV_CHECKED
+  waited = true;
+#endif
   live_cursor<kMode>(a, pc);
   const ItemCursor first = pc;
   if (item_begin + 1 < item_end) fetch_next<kMode>(a, item_begin + 1, pc.seg + 1, nxt);

@@ -30,6 +30,7 @@ enum PageOpKind {
   kOpCopyPage = 3,  // `count` rows from overflow row a to overflow row b; table entry c names the page of b
   kOpTableCopy = 4, // `count` table entries from index a on are those from index b on
   kOpTableRun = 5,  // `count` table entries from index a on are the pages b, b + 1, ...
+  kOpTableClear = 6, // `count` table entries from index a on name no page any more
 };
 struct PageTargets {
   uint8_t *k_pool, *v_pool, *k_ovf, *v_ovf;
@@ -83,7 +84,8 @@ __global__ void __launch_bounds__(256) page_ops_kernel(const __grid_constant__ P
     t.table[o.a] = o.b;
     if (n > 1) t.table[o.a + 1] = o.c;
   } else {
-    for (int j = 0; j < n; ++j) t.table[o.a + j] = (o.kind & 7) == kOpTableRun ? o.b + j : t.table[o.b + j];
+    const int kind = o.kind & 7;
+    for (int j = 0; j < n; ++j) t.table[o.a + j] = kind == kOpTableRun ? o.b + j : kind == kOpTableClear ? -1 : t.table[o.b + j];
   }
 }
 
@@ -124,11 +126,19 @@ constexpr int kDropSeqs = 512;
 struct Drops {
   int32_t n[kDropSeqs];
 };
-__global__ void __launch_bounds__(128) truncate_kernel(int32_t* seg_len, const __grid_constant__ Drops d, int Hkv, int seg0, int n) {
-  const int i = blockIdx.x * 128 + threadIdx.x;
+// A warp a list: its new length, and -1 for the table entries (up to `most`) of pages that it has given back.  They may be another list's soon: a replayed
+// append that finds its list full, and an attention under a plan made for the longer list, must not follow them.
+__global__ void __launch_bounds__(128) truncate_kernel(int32_t* seg_len, const __grid_constant__ Drops d, int Hkv, int seg0, int n, int32_t* table,
+                                                       const int32_t* seg_cap, int max_pages, int most) {
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (i >= n) return;
-  const int drop = d.n[i / Hkv];
-  if (drop > 0) seg_len[seg0 + i] = max(0, seg_len[seg0 + i] - drop);
+  const int drop = d.n[i / Hkv], seg = seg0 + i;
+  if (drop <= 0) return;
+  const int len = max(0, seg_len[seg] - drop);
+  __syncwarp();
+  if (lane == 0) seg_len[seg] = len;
+  if (!table) return;
+  for (int q = (max(0, len - seg_cap[seg]) + CATEKV_PAGE_ROWS - 1) / CATEKV_PAGE_ROWS + lane; q < most; q += 32) table[(int64_t)seg * max_pages + q] = -1;
 }
 
 // a growing array of host memory that does not throw
@@ -170,6 +180,7 @@ struct PageOrders {
   bool entries_of(int64_t at, int64_t from, int n) {  // as the device's table has them
     return n == 0 || sets.push(PageOp{kOpTableCopy | n << 3, (int32_t)at, (int32_t)from, 0});
   }
+  bool clear(int64_t at, int n) { return n <= 0 || sets.push(PageOp{kOpTableClear | n << 3, (int32_t)at, 0, 0}); }
   bool entries(int64_t at, const int32_t* v, int n) {
     int run = 1;
     while (run < n && v[run] == v[0] + run) ++run;
@@ -382,7 +393,7 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
   HostList<Child> children;
   HostList<int32_t> entries;  // of children whose parent is replaced itself: its row of the tables as it was
   PageOrders orders;
-  if (!children.reserve((size_t)replaced * Hkv) || !orders.copies.reserve((size_t)replaced * Hkv) || !orders.sets.reserve((size_t)replaced * Hkv * 2))
+  if (!children.reserve((size_t)replaced * Hkv) || !orders.copies.reserve((size_t)replaced * Hkv) || !orders.sets.reserve((size_t)replaced * Hkv * 3))
     return CATEKV_ERR_WORKSPACE;
   for (int b = 0; b < B; ++b) {
     if (parent[b] == b) continue;
@@ -405,6 +416,7 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
                                     std::min(CATEKV_PAGE_ROWS, len - r), to + c.full + i);
       }
       ok = ok && children.push(c) && orders.segment(s, c.off, c.cap, c.len);
+      ok = ok && orders.clear(to + c.full + c.fresh, p->seg_pages[s] - (c.full + c.fresh));
       if (moving) {
         ok = ok && orders.entries(to, p->table + row, c.full);
         for (int q = 0; q < c.full; ++q) ok = ok && entries.push(p->table[row + q]);
@@ -437,6 +449,7 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
     seg_off[c.seg] = c.off;
     seg_cap[c.seg] = c.cap;
     cache->seg_len[c.seg] = c.len;
+    for (int q = c.full + c.fresh; q < p->seg_pages[c.seg]; ++q) row[q] = -1;
     p->seg_pages[c.seg] = c.full + c.fresh;
     for (int q = 0; q < c.full + c.fresh; ++q) ++count[row[q]];
   }
@@ -536,11 +549,16 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
     rc = send(cache, orders, st);
     if (rc) return rc;
   }
+  int most = 0;  // entries in force, of the list with most of them
+  if (p)
+    for (int s = 0; s < n; ++s)
+      if (n_drop[s / Hkv] > 0) most = std::max(most, p->seg_pages[s]);
   for (int b0 = 0; b0 < B; b0 += kDropSeqs) {
     Drops d;
     const int nb = std::min(kDropSeqs, B - b0);
     memcpy(d.n, n_drop + b0, sizeof(int32_t) * (size_t)nb);
-    truncate_kernel<<<div_up((int64_t)nb * Hkv, 128), 128, 0, st>>>(cache->seg_len_dev, d, Hkv, b0 * Hkv, nb * Hkv);
+    truncate_kernel<<<div_up((int64_t)nb * Hkv, 4), 128, 0, st>>>(cache->seg_len_dev, d, Hkv, b0 * Hkv, nb * Hkv, p ? p->table_dev : nullptr,
+                                                                   p ? p->seg_cap_dev : nullptr, p ? p->max_pages : 0, most);
     CATEKV_CUDA_TRY(cudaGetLastError());
   }
   for (int s = 0; s < n; ++s)
@@ -549,9 +567,11 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
     int32_t* seg_cap = const_cast<int32_t*>(cache->seg_cap);
     for (size_t i = 0; i < changes.n; ++i) {
       const Change& c = changes[i];
+      int32_t* row = p->table + (size_t)c.seg * p->max_pages;
       seg_cap[c.seg] = c.cap;
+      for (int q = c.pages; q < p->seg_pages[c.seg]; ++q) row[q] = -1;
       p->seg_pages[c.seg] = c.pages;
-      for (int q = 0; q < c.n_entries; ++q) p->table[(size_t)c.seg * p->max_pages + c.first + q] = c.entry[q];
+      for (int q = 0; q < c.n_entries; ++q) row[c.first + q] = c.entry[q];
     }
     settle(p, count);
   }

@@ -43,3 +43,94 @@ def test_pages_are_not_handed_out_or_moved_in_a_capture(ck):
     ck.catekv_pages_reserve(m.cache, 100)
     m.append([100, 100])
     m.verify()
+
+
+def check_tables(m):
+    """Host and device agree on every entry, and those behind the pages in force name none."""
+    p = m.cache.pages
+    torch.cuda.synchronize()
+    assert p.table_dev.tolist() == p.table.tolist()
+    for s in range(m.S):
+        assert (p.table[s, int(p.seg_pages[s]):] == -1).all()
+
+
+def test_tables_name_no_page_that_was_given_back(ck):
+    m = Model(ck, 4, 2, [300] * 8, 80, 12, 5)
+    for step in (lambda: ck.catekv_pages_reserve(m.cache, 400), lambda: m.append([400, 10, 130, 0]), lambda: m.truncate([250, 0, 1, 300]),
+                 lambda: m.fork([0, 0, 2, 2]), lambda: ck.catekv_pages_reserve(m.cache, 70), lambda: m.append([3, 70, 64, 1]), lambda: m.fork([2, 3, 0, 1]),
+                 lambda: ck.catekv_pages_compact(m.cache), lambda: m.truncate([5000, 200, 130, 129]), lambda: m.fork([3, 1, 1, 3])):
+        step()
+        m.verify()
+        check_tables(m)
+
+
+def given_back(ck, n_new, append):
+    """A captured append whose list 0 has room for 20 rows more and whose former pages list 1 has got."""
+    m = Model(ck, 2, 1, [128, 128], 8, 4, 1)
+    ck.catekv_pages_reserve(m.cache, n_new)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        append(m.cache)
+    ck.catekv_cache_sync_lengths(m.cache)  # (nothing has run)
+    mine = m.cache.pages.table[0, :int(m.cache.pages.seg_pages[0])].tolist()
+    m.append([n_new, 64 * len(mine)])
+    m.truncate([n_new + 20, 0])
+    ck.catekv_pages_reserve(m.cache, 20)
+    m.append([0, 20])
+    assert m.cache.pages.seg_pages.tolist() == [0, len(mine) + 1] and m.cache.pages.table[1, len(mine)] == mine[0]
+    m.verify()
+    return m, g
+
+
+@pytest.mark.parametrize("n_new", [30, 100])  # one launch, and two
+def test_a_replayed_append_does_not_follow_a_page_that_was_given_back(ck, n_new):
+    k, v = (torch.randn(n_new, 1, D, device="cuda").bfloat16() for _ in range(2))
+    m, g = given_back(ck, n_new, lambda cache: ck.catekv_append_chunk(cache, ck.Chunk([n_new, 0]), k, v))
+    for _ in range(2):
+        g.replay()
+    ck.catekv_cache_sync_lengths(m.cache)
+    assert m.cache.seg_len.tolist() == [128, m.lists[1][0].shape[0]]
+    m.lists[0] = [torch.cat([x, new[:20, 0]]) for x, new in zip(m.lists[0], (k, v))]
+    m.verify()
+
+
+@pytest.mark.parametrize("steps", [25, 60])  # the second one: list 1 has no room left either
+def test_a_replayed_token_does_not_follow_a_page_that_was_given_back(ck, steps):
+    k, v = (torch.randn(2, 1, D, device="cuda").bfloat16() for _ in range(2))
+    m, g = given_back(ck, 30, lambda cache: ck.catekv_append(cache, k, v))
+    for _ in range(steps):
+        g.replay()
+    ck.catekv_cache_sync_lengths(m.cache)
+    for s, n in ((0, 20), (1, min(steps, 44))):
+        m.lists[s] = [torch.cat([x, *[new[s]] * n]) for x, new in zip(m.lists[s], (k, v))]
+    m.verify()
+
+
+def test_a_plan_made_before_rows_were_taken_back(ck):
+    """It knows rows in pages that the list has given back: they are left out, whoever has the pages now."""
+    B, Hkv, G = 2, 1, 4
+    m = Model(ck, B, Hkv, [100, 100], 12, 8, 3)
+    ck.catekv_pages_reserve(m.cache, 300)
+    m.append([300, 300])
+    plan = ck.DecodePlan(m.cache, 7)
+    ck.catekv_decode_plan(m.cache, plan)
+    q = torch.randn(B, Hkv * G, D, device="cuda").bfloat16()
+    out, lse = torch.zeros(q.shape, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
+    for drop, add in (([250, 0], [0, 0]), ([0, 20], [0, 0]), ([90, 200], [0, 0]), ([0, 0], [7, 5])):
+        m.truncate(drop)
+        free = sorted(set(range(12)) - {int(x) for s in range(2) for x in m.cache.pages.table[s, :int(m.cache.pages.seg_pages[s])]})
+        for page in free:  # what another list may have there
+            m.cache.pages.k_ovf[page * 64:page * 64 + 64] = float("nan")
+            m.cache.pages.v_ovf[page * 64:page * 64 + 64] = float("inf")
+        if any(add):
+            ck.catekv_pages_reserve(m.cache, max(add))
+            m.append(add)
+        ck.catekv_decode_attn(m.cache, q, plan, out, lse)
+        for b in range(B):
+            kk, vv = (x.double() for x in m.lists[b])
+            z = q[b].double() @ kk.T * D ** -0.5
+            o = torch.softmax(z, 1) @ vv
+            assert float((out[b].double() - o).norm() / o.norm()) <= 1e-5
+            assert float((lse[b].double() - torch.logsumexp(z, 1)).abs().max()) <= 1e-5
+        check_tables(m)
