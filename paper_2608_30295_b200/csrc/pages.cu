@@ -482,19 +482,25 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
   };
   HostList<Change> changes;
   HostList<int32_t> count, at_start, cap;
+  // Lists that read the same segment's rows (sequences that were forked), a group by offset, ascending: where a list's group begins, the largest
+  // capacity of those behind the list, and by group that of those already passed (as this call leaves them).
+  HostList<int64_t> by_off;
+  HostList<int32_t> group, behind, passed;
+  bool shared = false;
   PageOrders orders;
   if (p) {
-    // whether any two lists read the same segment's rows (sequences that were forked)
-    bool shared = false;
     if (!cap.fill(n, 0)) return CATEKV_ERR_WORKSPACE;
-    {
-      HostList<int32_t> offs;
-      for (int s = 0; s < n; ++s) {
-        cap[s] = cache->seg_cap[s];
-        if (cap[s] > 0 && !offs.push(cache->seg_off[s])) return CATEKV_ERR_WORKSPACE;
-      }
-      std::sort(offs.p, offs.p + offs.n);
-      for (size_t i = 1; i < offs.n; ++i) shared = shared || offs[i] == offs[i - 1];
+    for (int s = 0; s < n; ++s) {
+      cap[s] = cache->seg_cap[s];
+      if (cap[s] > 0 && !by_off.push((int64_t)cache->seg_off[s] << 32 | s)) return CATEKV_ERR_WORKSPACE;
+    }
+    std::sort(by_off.p, by_off.p + by_off.n);
+    for (size_t i = 1; i < by_off.n; ++i) shared = shared || by_off[i] >> 32 == by_off[i - 1] >> 32;
+    if (shared) {
+      if (!group.fill(n, 0) || !behind.fill(n, 0) || !passed.fill(by_off.n, 0)) return CATEKV_ERR_WORKSPACE;
+      for (size_t i = 1; i < by_off.n; ++i) group[(int32_t)by_off[i]] = by_off[i] >> 32 == by_off[i - 1] >> 32 ? group[(int32_t)by_off[i - 1]] : (int32_t)i;
+      for (size_t i = by_off.n; i-- > 1;)
+        if (by_off[i] >> 32 == by_off[i - 1] >> 32) behind[(int32_t)by_off[i - 1]] = std::max(behind[(int32_t)by_off[i]], cap[(int32_t)by_off[i]]);
     }
     rc = count_pages(cache, nullptr, count);
     if (rc) return rc;
@@ -504,13 +510,15 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
     FreePages free_pages{at_start};  // (a page released by this call may still be the source of one of its copies)
     for (int s = 0; s < n; ++s) {
       const int drop = n_drop[s / Hkv];
-      if (drop == 0) continue;
+      const bool member = shared && cap[s] > 0;
+      if (drop == 0) {
+        if (member) passed[group[s]] = std::max(passed[group[s]], cap[s]);
+        continue;
+      }
       const int len = std::max(0, cache->seg_len[s] - drop);
       int32_t* row = p->table + (size_t)s * p->max_pages;
       Change c = {s, cap[s], len > cap[s] ? div_up(len - cap[s], CATEKV_PAGE_ROWS) : 0, 0, 0, {0, 0}};
-      bool read = false;  // another list reads the segment's rows behind the new end
-      if (shared && len < cap[s])
-        for (int o = 0; o < n && !read; ++o) read = o != s && cache->seg_off[o] == cache->seg_off[s] && cap[o] > len;
+      const bool read = member && len < cap[s] && std::max(passed[group[s]], behind[s]) > len;  // another list reads the segment's rows behind the new end
       const int kept = read ? 0 : c.pages;
       for (int q = kept; q < p->seg_pages[s]; ++q) --count[row[q]];
       if (read) {
@@ -539,6 +547,7 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
                               (int64_t)s * p->max_pages + kept - 1))
           return CATEKV_ERR_WORKSPACE;
       }
+      if (member) passed[group[s]] = std::max(passed[group[s]], cap[s]);
       if (!changes.push(c)) return CATEKV_ERR_WORKSPACE;
     }
   }

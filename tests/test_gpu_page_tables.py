@@ -134,3 +134,18 @@ def test_a_plan_made_before_rows_were_taken_back(ck):
             assert float((out[b].double() - o).norm() / o.norm()) <= 1e-5
             assert float((lse[b].double() - torch.logsumexp(z, 1)).abs().max()) <= 1e-5
         check_tables(m)
+
+
+def test_many_sequences_leave_shared_rows_in_turn(ck):
+    """Who still reads a segment's rows behind a new end goes by the lists before it in the same call as they are left, and by those after it as they were."""
+    B = 24
+    m = Model(ck, B, 2, [700] * (B * 2), 40 * B, 24, 6)
+    m.fork([b % 3 for b in range(B)])
+    m.verify()
+    for drop in ([60] + [0] * 23, [300] * 4 + [100] * 4 + [0] * 16, [0] * 12 + [400] * 6 + [5] * 6, [130] * 24, [0, 10, 500] * 8, [5000] * 20 + [1] * 4):
+        m.truncate(drop)
+        m.verify()
+        ck.catekv_pages_reserve(m.cache, 70)
+        m.append([70 - 3 * b if b % 4 else 0 for b in range(B)])
+        m.verify()
+        check_tables(m)
