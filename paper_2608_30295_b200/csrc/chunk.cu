@@ -171,6 +171,8 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 __device__ __forceinline__ int uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+// Every wait of the kernel: the warp goes on, or leaves, as a whole (its lanes may see a wait run out at different times, and what follows are
+// collectives of the warp).
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
 }
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
       // (every tile is waited for in its order: a wait that skipped one could take the phase before it for its own)
       for (int t = 0; ok && t < n; ++t, ++n_v) {
         const int r0 = (it.t0 + t) * kKeyTile, st = n_v % kStagesV;
-        if (!(ok = mbar_wait(B(kFullV + st), (n_v / kStagesV) & 1, s_abort, a.spin_limit))) break;
+        if (!(ok = warp_wait(B(kFullV + st), (n_v / kStagesV) & 1, s_abort, a.spin_limit))) break;
         if (r0 + kKeyTile <= first) continue;
         if (fresh) {
           // four flags in turn: this block's V tile is in the ring, so the results of the block four before it are out
@@ -687,7 +689,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
 #pragma unroll 1
         for (int h = kSplit ? g : 0; h < (kSplit ? g + 1 : 2); ++h) {
           const int s_slot = slot_of(n_s, x, h);
-          if (!(alive = mbar_wait(B(kDoneS + s_slot), phase_of(n_s), s_abort, a.spin_limit))) break;
+          if (!(alive = warp_wait(B(kDoneS + s_slot), phase_of(n_s), s_abort, a.spin_limit))) break;
           if (idle) {
             __syncwarp();
             if (lane == 0) mbar_arrive(B(kPReady + s_slot));
@@ -697,7 +699,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
           const uint32_t slot = tmem + lane_base + s_slot * Sh::kSlotCols;
           // the products of the step before (whose slot's earlier phases are behind us: its own S has been read)
           const uint32_t n_b = h == 0 ? n_s - 1 : n_s;
-          auto wait_products = [&]() { return mbar_wait(B(kDonePV + slot_of(n_b, x, h ^ 1)), phase_of(n_b), s_abort, a.spin_limit); };
+          auto wait_products = [&]() { return warp_wait(B(kDonePV + slot_of(n_b, x, h ^ 1)), phase_of(n_b), s_abort, a.spin_limit); };
           const int k0 = (it.t0 + i) * kKeyTile + 64 * h;
           float y[64];
           tmem_ld64(slot, y);
@@ -711,7 +713,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
           float ref_o = ref;  // the accumulator's reference
           if (kSplit) {
             // The two steps' threads of a row share its reference: each decides after the other has decided for the step before.  Only that is serial.
-            if (n_dec + g > 0 && !(alive = mbar_wait(B(kDec + quarter), (n_dec + g - 1) & 1, s_abort, a.spin_limit))) break;
+            if (n_dec + g > 0 && !(alive = warp_wait(B(kDec + quarter), (n_dec + g - 1) & 1, s_abort, a.spin_limit))) break;
             ref_o = i + g > 0 ? s_ref[(g ^ 1) * 128 + lane_row] : ref;
           }
           const bool grow = mx > ref_o + kChTau;  // also the first step with a visible key
@@ -777,7 +779,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
       if (!alive) break;
       if (kSplit) {  // the row's sums of both steps, relative to the last decision (the second step's)
         if (!idle) {
-          if (!(alive = mbar_wait(B(kDec + quarter), (n_dec - 1) & 1, s_abort, a.spin_limit))) break;
+          if (!(alive = warp_wait(B(kDec + quarter), (n_dec - 1) & 1, s_abort, a.spin_limit))) break;
           const float ref_end = s_ref[128 + lane_row];
           if (ref_end > ref) {
             l = ref > -INFINITY ? l * fast_exp2(ref - ref_end) : l;
@@ -787,11 +789,11 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
         s_l[g * 128 + lane_row] = l;
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kXch + quarter));
-        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
+        if (!(alive = warp_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
         ++n_x;
         l = s_l[lane_row] + s_l[128 + lane_row];
       }
-      if (!(alive = mbar_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
+      if (!(alive = warp_wait(B(kDoneO + x), n_o & 1, s_abort, a.spin_limit))) break;
       ++n_o;
       tc_fence_after();
       // ---- the item's result: the whole block, or a piece of it (kSplit: each step's threads write half of d)
@@ -821,11 +823,11 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
             float4* const z = reinterpret_cast<float4*>(s_low + (g * 64 + row) * kLowStride);
             const uint32_t pair = g * 2 + (quarter & 1);
             if (low) {
-              if (n_low > 0 && !(alive = mbar_wait(B(kLowEmpty + pair), (n_low - 1) & 1, s_abort, a.spin_limit))) break;
+              if (n_low > 0 && !(alive = warp_wait(B(kLowEmpty + pair), (n_low - 1) & 1, s_abort, a.spin_limit))) break;
 #pragma unroll
               for (int c = 0; c < 8; ++c) z[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
             } else {
-              if (!(alive = mbar_wait(B(kLowFull + pair), n_low & 1, s_abort, a.spin_limit))) break;
+              if (!(alive = warp_wait(B(kLowFull + pair), n_low & 1, s_abort, a.spin_limit))) break;
 #pragma unroll
               for (int c = 0; c < 8; ++c) {
                 const float4 w = z[c];
@@ -881,7 +883,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
       if (kSplit) {  // the other step's threads have read the accumulator too: the next block's products may overwrite it
         __syncwarp();
         if (lane == 0) mbar_arrive(B(kXch + quarter));
-        if (!(alive = mbar_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
+        if (!(alive = warp_wait(B(kXch + quarter), n_x & 1, s_abort, a.spin_limit))) break;
         ++n_x;
       }
     }

@@ -123,3 +123,20 @@ def test_two_tiles_whose_waits_run_out(ck):
     ck.catekv_chunk_attn(cache, chunk, q, out, lse, ws=ws)
     assert ck.catekv_workspace_status(ws)["flags"] == 0
     check_rounded_once(out, lse, reference(rows, q, n_new, starts(n_new), 8, D ** -0.5))
+
+
+def test_doubled_rows_whose_waits_run_out(ck):
+    """Few query rows over long lists: the warps also wait for one another's results."""
+    cache, rows = make_cache(ck, 2, 8, [16000] * 16, [40] * 16, seed=8)
+    n_new, q = [5, 3], queries(8, 32)
+    out, lse = torch.full(q.shape, 3.0, device="cuda", dtype=torch.bfloat16), torch.full(q.shape[:2], 3.0, device="cuda")
+    chunk = ck.Chunk(n_new)
+    ws = ck.chunk_attn_workspace(cache, chunk, 32)
+    for _ in range(3):
+        ck.catekv_test_expire_score_waits(1)
+        ck.catekv_chunk_attn(cache, chunk, q, out, lse, ws=ws)
+        st = ck.catekv_workspace_status(ws, clear=True, raise_on_error=False)
+        assert st["flags"] == ck.STATUS_WAIT_EXPIRED and st["kernel"] == 7
+        ck.catekv_chunk_attn(cache, chunk, q, out, lse, ws=ws)
+        assert ck.catekv_workspace_status(ws)["flags"] == 0
+        check_rounded_once(out, lse, reference(rows, q, n_new, [0, 5], 8, D ** -0.5))
