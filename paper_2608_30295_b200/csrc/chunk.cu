@@ -306,8 +306,9 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
   pdl_launch_dependents();
   if (tid == 0) {
     *s_abort = 0;
+#pragma unroll
     for (int i = 0; i < kChBarriers; ++i) {
-      const int count = (i >= kPReady && i < kPReady + 4) ? 4 : (i >= kXch && i < kXch + 4) ? 2 : 1;
+      const int count = (i >= kPReady && i < kPReady + 4) ? 4 : (i >= kXch && i < kXch + 4) || (i >= kEmptyV && i < kEmptyV + kStagesV) ? 2 : 1;
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(B(i)), "r"(count));
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -535,11 +536,15 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
       const int first = it.g.len - it.g.n_new + it.blk * a.TB + 1;                       // rows that every query sees
       const int last = it.g.len - it.g.n_new + min(it.g.n_new, a.TB * (it.blk + 1));     // rows that the last one sees
       bool fresh = true;
-      // (every tile is waited for in its order: a wait that skipped one could take the phase before it for its own)
+      // Every tile is waited for in its order, and its place in the ring is free when this warp has passed it too: a warp that skipped a tile, or fell two
+      // uses of a place behind, could take another phase for its own.
       for (int t = 0; ok && t < n; ++t, ++n_v) {
         const int r0 = (it.t0 + t) * kKeyTile, st = n_v % kStagesV;
         if (!(ok = warp_wait(B(kFullV + st), (n_v / kStagesV) & 1, s_abort, a.spin_limit))) break;
-        if (r0 + kKeyTile <= first) continue;
+        if (r0 + kKeyTile <= first) {
+          if (lane == 0) mbar_arrive(B(kEmptyV + st));
+          continue;
+        }
         if (fresh) {
           // four flags in turn: this block's V tile is in the ring, so the results of the block four before it are out
           if (lane == 0) s_odd[n_item & 3] = 0x7fffffff;
@@ -586,7 +591,10 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
         if (odd != 0x7fffffff) atomicMin(&s_odd[n_item & 3], odd);
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(B(kFixed + st));
+        if (lane == 0) {
+          mbar_arrive(B(kFixed + st));
+          mbar_arrive(B(kEmptyV + st));
+        }
       }
       n_item += fresh ? 0 : 1;
     }

@@ -13,3 +13,35 @@ def test_every_wait_is_the_warps():
         text = re.sub(r"//[^\n]*", "", f.read())
     assert re.findall(r"[^\n]*\bmbar_wait\([^\n]*", text) == ["  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));"]
     assert len(re.findall(r"\bwarp_wait\(", text)) > 15
+
+
+def parity_ring(counted, uses=40, places=3, seed=0):
+    """The V ring as its barriers see it, roles scheduled at random with the looking warp rarely: does that warp get through?  A wait for a use of a place
+    passes when the parity of the place's completed phases says so, whichever phase that is."""
+    import random
+    rng = random.Random(seed)
+    full, free = [0] * places, [0] * places  # completed phases; of `free`, arrivals
+    need = 2 if counted else 1
+    loaded = multiplied = looked = 0
+    for _ in range(200 * uses):
+        role = rng.choices(("load", "multiply", "look"), (8, 8, 1))[0]
+        if role == "load" and loaded < uses:
+            if loaded < places or free[loaded % places] >= need * (loaded // places):
+                full[loaded % places] += 1
+                loaded += 1
+        elif role == "multiply" and multiplied < loaded:
+            free[multiplied % places] += 1
+            multiplied += 1
+        elif role == "look" and looked < uses and full[looked % places] % 2 != (looked // places) % 2:
+            if counted:
+                free[looked % places] += 1
+            looked += 1
+    return looked == uses
+
+
+def test_a_place_of_the_ring_is_free_when_the_looking_warp_has_passed_it_too():
+    assert all(parity_ring(True, seed=i) for i in range(20)) and not all(parity_ring(False, seed=i) for i in range(20))
+    with open(SOURCE) as f:
+        text = re.sub(r"//[^\n]*", "", f.read())
+    assert re.search(r"\(i >= kEmptyV && i < kEmptyV \+ kStagesV\) \? 2", text)  # arrivals: the products' commit, and the warp that looks
+    assert len(re.findall(r"mbar_arrive\(B\(kEmptyV \+ st\)\)", text)) == 2 and len(re.findall(r"umma_commit\(B\(kEmptyV \+ st\)\)", text)) == 1
