@@ -361,7 +361,8 @@ int catekv_cache_regrow(const catekv_cache* src, catekv_cache* dst, catekv_strea
  * their capacities: every item reads the current length on the device, the last
  * item of a segment follows rows appended since (append), and rows behind a length
  * that has shrunk (a per-step cache refilled by catekv_retrieve_compact) are left
- * out; rebuild it now and then to restore balance.  catekv_append_decode_attn
+ * out; rebuild it now and then to restore balance, and where lists have been cut
+ * (catekv_evict, catekv_truncate: see the ordering note below) or forked.  catekv_append_decode_attn
  * alone needs lengths that are not below the plan's (ERR_INVALID_ARG otherwise).
  *
  * catekv_decode_num_ctas: SM count * resident CTAs per SM of the decode kernel
@@ -390,10 +391,11 @@ int catekv_decode_plan(const catekv_cache* cache, int32_t num_ctas, void* plan_h
  * stream before they read lengths, queries or appended rows, but they may request cache rows that
  * were valid when the plan was built while the previous kernel is still finishing.  Such rows must
  * therefore not be rewritten (by catekv_select_compact, say) between catekv_decode_plan and this call.
- * Appends to lists that are shorter than the plan knows them (they were cut by catekv_evict, or the plan was
+ * Appends to lists that are shorter than the plan knows them (they were cut by catekv_evict or catekv_truncate, or the plan was
  * made from upper bounds) rewrite such rows: while cache->seg_len says so, and always under a plan made from upper bounds,
  * the kernel is launched behind the previous one's end.  That is decided when the call is made (a captured call keeps
- * it), and no longer once the lists have grown past the plan again: build plans anew where lists are cut.
+ * it), and no longer once the lists have grown past the plan again: build plans anew where lists are cut.  (catekv_append_chunk may bring them
+ * there in one call; no kernel overlaps with its writing.  catekv_append's last step up to the plan's length does overlap.)
  */
 int catekv_decode_attn(const catekv_cache* cache, const void* q, int32_t Hq, float sm_scale, void* out,
                        int32_t out_dtype, float* lse_out, const void* plan_host, const void* plan_dev,

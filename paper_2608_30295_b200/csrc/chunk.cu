@@ -1084,12 +1084,12 @@ __device__ __forceinline__ int ap_fitting(const AppendArgs& a, int seg, int len,
   while (n > 0 && !ap_row(a, seg, len + n - 1, false)) n = max(0, a.seg_cap[seg] + (len + n - 1 - a.seg_cap[seg]) / 64 * 64 - len);
   return n;
 }
-// One block takes kApRows rows of a list.  kAlone: every list's rows fit one block, which also counts them in.
+// One block takes kApRows rows of a list.  kAlone: every list's rows fit one block, which also counts them in.  The kernel does not signal its dependents
+// early: rows that were taken back (catekv_truncate) and come anew may be rows that a decode plan knows, which attention under it requests at its start.
 template <bool kAlone>
 __global__ void __launch_bounds__(256) append_chunk_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ChunkSeqs sq) {
   const int seg = blockIdx.x, b = seg / a.Hkv, h = seg - b * a.Hkv;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = (lane & 15) * 16;
-  pdl_launch_dependents();
   const int n = sq.n_new[b], r0 = blockIdx.y * kApRows;
   if (r0 >= n) return;
   pdl_wait();

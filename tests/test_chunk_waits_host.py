@@ -45,3 +45,11 @@ def test_a_place_of_the_ring_is_free_when_the_looking_warp_has_passed_it_too():
         text = re.sub(r"//[^\n]*", "", f.read())
     assert re.search(r"\(i >= kEmptyV && i < kEmptyV \+ kStagesV\) \? 2", text)  # arrivals: the products' commit, and the warp that looks
     assert len(re.findall(r"mbar_arrive\(B\(kEmptyV \+ st\)\)", text)) == 2 and len(re.findall(r"umma_commit\(B\(kEmptyV \+ st\)\)", text)) == 1
+
+
+def test_the_append_of_a_chunk_does_not_signal_early():
+    """Attention under a plan from before rows were taken back requests, at its start, rows that the plan knows: the append may be writing them."""
+    with open(SOURCE) as f:
+        text = f.read()
+    body = text[text.index(" append_chunk_kernel("):text.index(" append_count_kernel(")]
+    assert "pdl_wait();" in body and "pdl_launch_dependents" not in body

@@ -149,3 +149,28 @@ def test_many_sequences_leave_shared_rows_in_turn(ck):
         m.append([70 - 3 * b if b % 4 else 0 for b in range(B)])
         m.verify()
         check_tables(m)
+
+
+def test_rows_taken_back_and_appended_anew_under_one_plan(ck):
+    """The plan knows the places of the new rows: attention that follows the append at once must not read them before they are written."""
+    B, Hkv, G = 8, 4, 4
+    m = Model(ck, B, Hkv, [500] * (B * Hkv), 200, 8, 3)
+    ck.catekv_pages_reserve(m.cache, 200)
+    m.append([120] * B)
+    plan = ck.DecodePlan(m.cache, ck.catekv_decode_num_ctas())
+    ck.catekv_decode_plan(m.cache, plan)
+    out, lse = torch.zeros((B, Hkv * G, D), device="cuda"), torch.zeros((B, Hkv * G), device="cuda")
+    for step in range(12):
+        n = 100 + 3 * step
+        m.truncate([n] * B)
+        ck.catekv_pages_reserve(m.cache, n)
+        q = torch.randn(B, Hkv * G, D, device="cuda").bfloat16()
+        m.append([n] * B)
+        ck.catekv_decode_attn(m.cache, q, plan, out, lse)
+        for s in range(m.S):
+            b, h = divmod(s, Hkv)
+            k, v = (x.double() for x in m.lists[s])
+            z = q[b, h * G:h * G + G].double() @ k.T * D ** -0.5
+            o = torch.softmax(z, 1) @ v
+            assert float((out[b, h * G:h * G + G].double() - o).norm() / o.norm()) <= 1e-5
+            assert float((lse[b, h * G:h * G + G].double() - torch.logsumexp(z, 1)).abs().max()) <= 1e-5
