@@ -593,7 +593,7 @@ int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const vo
  * The device's lengths decide, so a captured call follows lists that grow; the lengths on the host (upper bounds will do)
  * only choose the number of CTAs.  Follows overflow pages.  Segment capacities are multiples of CATEKV_SEG_ALIGN, and the cache
  * has seg_cap_dev (CATEKV_ERR_INVALID_ARG).  CATEKV_ERR_UNSUPPORTED if blocks of 128 query rows times blocks of 128 rows of their lists' capacities
- * come to more than 2^31: a chunk of that size is brought in by parts.
+ * (with all the pages that a list may be given) come to more than 2^31: a chunk of that size is brought in by parts.
  */
 size_t catekv_chunk_attn_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t max_new);
 int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* chunk, const void* q, int64_t q_stride_t, int64_t q_stride_h, int32_t Hq,

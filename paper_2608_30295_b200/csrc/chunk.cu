@@ -1284,7 +1284,8 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
   if (G > kMaxG || (out_dtype != CATEKV_OUT_BF16 && out_dtype != CATEKV_OUT_FP32)) return CATEKV_ERR_UNSUPPORTED;
   const int n_segs = cache->B * cache->Hkv;
   int64_t units_of[2] = {0, 0}, blocks_of[2] = {0, 0};  // tiles and blocks with one M tile, with two
-  int64_t most = 0;  // what the schedule could count up to, if a replayed call found the lists full
+  int64_t most = 0;  // what the schedule could count up to, if a replayed call found the lists full, with all the pages that they may be given by then
+  const int64_t page_rows = cache->pages ? (int64_t)CATEKV_PAGE_ROWS * (cache->pages->max_pages < cache->pages->n_pages ? cache->pages->max_pages : cache->pages->n_pages) : 0;
   int64_t rows = 0;  // of the lists that have queries
   for (int s = 0; s < n_segs; ++s) {
     const int n = sq.n_new[s / cache->Hkv], len = cache->seg_len[s];
@@ -1294,7 +1295,7 @@ extern "C" int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* 
     for (int w = 0; w < 2; ++w) {
       const int TB = (w ? 256 : 128) / G;
       blocks_of[w] += (n + TB - 1) / TB;
-      if (w == 0) most += (int64_t)((n + TB - 1) / TB) * (seg_capacity(cache, s) / kKeyTile + 1 + kChCharge);
+      if (w == 0) most += (int64_t)((n + TB - 1) / TB) * ((cache->seg_cap[s] + page_rows) / kKeyTile + 1 + kChCharge);
       for (int j = 0; j < n; j += TB) units_of[w] += (len - n + (n < j + TB ? n : j + TB) + kKeyTile - 1) / kKeyTile;
     }
   }
