@@ -1,5 +1,6 @@
 """What the page calls leave in the host's and the device's tables, and when they may be captured."""
 import numpy as np
+import numpy as np
 import pytest
 import torch
 
@@ -174,3 +175,34 @@ def test_rows_taken_back_and_appended_anew_under_one_plan(ck):
             o = torch.softmax(z, 1) @ v
             assert float((out[b, h * G:h * G + G].double() - o).norm() / o.norm()) <= 1e-5
             assert float((lse[b, h * G:h * G + G].double() - torch.logsumexp(z, 1)).abs().max()) <= 1e-5
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_next_free_follows_the_pages_in_use(ck, seed):
+    """Pages are handed out from next_free on while none below it is free: it lies behind every page in use, and after a call that counts them right behind."""
+    rng = np.random.default_rng(100 + seed)
+    B, Hkv = int(rng.integers(2, 6)), int(rng.integers(1, 4))
+    m = Model(ck, B, Hkv, [200] * (B * Hkv), 40 * B * Hkv, 60, seed)
+    p = m.cache.pages
+    for _ in range(20):
+        what, counted = rng.integers(0, 5), False
+        if what <= 1 and max(x[0].shape[0] for x in m.lists) < 2000:
+            n_new = [int(rng.choice([0, 1, 64, 100])) for _ in range(B)]
+            ck.catekv_pages_reserve(m.cache, max(n_new))
+            m.append(n_new)
+        elif what == 2:
+            parent = [int(rng.integers(0, B)) for _ in range(B)]
+            counted = parent != list(range(B))
+            m.fork(parent)
+        elif what == 3:
+            drop = [int(rng.choice([0, 1, 64, 130, 5000])) for _ in range(B)]
+            counted = any(drop)
+            m.truncate(drop)
+        else:
+            counted = ck.catekv_pages_compact(m.cache) >= 0
+        m.verify()
+        used = {int(x) for s in range(m.S) for x in p.table[s, :int(p.seg_pages[s])]}
+        top = max(used) + 1 if used else 0
+        assert p.struct.next_free == top if counted else p.struct.next_free >= top
+        assert p.struct.released == p.struct.next_free - len(used)
+        assert p.struct.next_free <= p.struct.n_pages
