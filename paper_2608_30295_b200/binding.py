@@ -305,7 +305,8 @@ def catekv_cache_advance(cache: Cache, n_tokens: int = 1):
 
 def catekv_pages_reserve(cache: Cache, n_new: int):
     """Make sure every segment can take n_new more rows (hands out overflow pages where the capacity is short)."""
-    _check(_lib.catekv_pages_reserve(C.byref(cache.struct), n_new, _stream()), "catekv_pages_reserve")
+    st = _stream_here("catekv_pages_reserve", cache.k_pool)
+    _check(_lib.catekv_pages_reserve(C.byref(cache.struct), n_new, st), "catekv_pages_reserve")
 
 
 def catekv_cache_regrow(src: Cache, max_new: int) -> Cache:
