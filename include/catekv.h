@@ -79,7 +79,7 @@ typedef void* catekv_stream; /* cudaStream_t */
  * Overflow pages of a cache: room for segments to grow past the capacity they were laid out with, without moving
  * what they hold (the paper sizes its caches up front and has no counterpart).  Row r of segment s lives in the
  * cache's own pools while r < seg_cap[s]; beyond that, row seg_cap[s] + 64 p + i is row 64 table[s][p] + i of the
- * overflow pools.  Pages are handed out by catekv_pages_reserve (the lowest free ones first); they come back, are shared and move by
+ * overflow pools.  Pages are handed out by catekv_pages_reserve and catekv_pages_reserve_each (the lowest free ones first); they come back, are shared and move by
  * catekv_truncate, catekv_fork and catekv_pages_compact, and by no other call.  The first seg_pages[s] entries of a table row are in force,
  * those behind them are -1.  All arrays are allocated by the caller; table and table_dev start out filled with -1, seg_pages with 0.
  */
@@ -336,6 +336,8 @@ int catekv_cache_advance(catekv_cache* cache, int32_t n_tokens);
  * contiguous segment again.
  */
 int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_stream stream);
+/* The same with a number for the lists of every sequence, n_new[b] (host [B]): a piece of a prompt beside sequences that decode. */
+int catekv_pages_reserve_each(catekv_cache* cache, const int32_t* n_new, catekv_stream stream);
 
 /*
  * Growth beyond the capacity a cache was laid out with (Section 4.4.3 keeps generating for as long as the
@@ -567,7 +569,7 @@ typedef struct catekv_chunk {
  * Append a chunk's keys and values to every list: row seg_len + i of list (b, h) is written from token start[b] + i, in the
  * segment's own rows or its overflow pages, and seg_len grows by n_new[b] on the device and in the host mirror.
  *   k_new, v_new  device bf16 [n_tokens, Hkv, d] with element strides stride_t, stride_h (multiples of 8; d contiguous), 16-byte aligned
- * CATEKV_ERR_CAPACITY (nothing launched) if a list cannot take its rows: catekv_pages_reserve gives it pages.
+ * CATEKV_ERR_CAPACITY (nothing launched) if a list cannot take its rows: catekv_pages_reserve_each gives it pages.
  * CATEKV_ERR_INVALID_ARG for a cache without seg_cap_dev.  A replayed call goes by the device's lengths, so its lists are given room before
  * it, as for a replayed catekv_append (the mirror: catekv_cache_sync_lengths, or catekv_cache_advance where all sequences grow alike).  Rows
  * for which a list has no room are dropped and not counted.

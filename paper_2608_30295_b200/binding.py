@@ -101,6 +101,7 @@ def _load():
         "catekv_cache_advance": (C.c_int, [C.POINTER(CacheStruct), i32]),
         "catekv_cache_regrow": (C.c_int, [C.POINTER(CacheStruct), C.POINTER(CacheStruct), vp]),
         "catekv_pages_reserve": (C.c_int, [C.POINTER(CacheStruct), i32, vp]),
+        "catekv_pages_reserve_each": (C.c_int, [C.POINTER(CacheStruct), vp, vp]),
         "catekv_decode_num_ctas": (C.c_int, []),
         "catekv_decode_plan_bytes": (sz, [i32, i32, i32]),
         "catekv_decode_workspace_bytes": (sz, [i32, i32, i32]),
@@ -307,6 +308,13 @@ def catekv_pages_reserve(cache: Cache, n_new: int):
     """Make sure every segment can take n_new more rows (hands out overflow pages where the capacity is short)."""
     st = _stream_here("catekv_pages_reserve", cache.k_pool)
     _check(_lib.catekv_pages_reserve(C.byref(cache.struct), n_new, st), "catekv_pages_reserve")
+
+
+def catekv_pages_reserve_each(cache: Cache, n_new):
+    """The same for n_new[b] more rows in the lists of sequence b."""
+    n_new = _per_sequence("catekv_pages_reserve_each", cache, n_new)
+    st = _stream_here("catekv_pages_reserve_each", cache.k_pool)
+    _check(_lib.catekv_pages_reserve_each(C.byref(cache.struct), _np_ptr(n_new), st), "catekv_pages_reserve_each")
 
 
 def catekv_cache_regrow(src: Cache, max_new: int) -> Cache:

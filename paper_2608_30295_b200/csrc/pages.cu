@@ -300,22 +300,21 @@ static int check_not_captured(cudaStream_t st) {
 }
 static inline int div_up(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
-}  // namespace catekv
-
-using namespace catekv;
-
-extern "C" int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_stream stream) {
-  CATEKV_API_RANGE();
+// Room for all_new rows in every list, or for each[b] in those of sequence b.
+static int reserve(catekv_cache* cache, int32_t all_new, const int32_t* each, catekv_stream stream) {
   int rc = check_cache(cache);
   if (rc) return rc;
-  if (!cache->pages || n_new < 0) return CATEKV_ERR_INVALID_ARG;
+  if (!cache->pages || all_new < 0) return CATEKV_ERR_INVALID_ARG;
+  for (int b = 0; each && b < cache->B; ++b)
+    if (each[b] < 0) return CATEKV_ERR_INVALID_ARG;
   catekv_pages* p = cache->pages;
   const int n = cache->B * cache->Hkv;
+  auto rows_over = [&](int s) { return (int64_t)cache->seg_len[s] + (each ? each[s / cache->Hkv] : all_new) - cache->seg_cap[s]; };
   // first pass: what is needed, nothing changed yet
   int64_t extra = 0;
   for (int s = 0; s < n; ++s) {
     if (cache->seg_len[s] < 0 || cache->seg_len[s] > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;
-    const int64_t over = (int64_t)cache->seg_len[s] + n_new - cache->seg_cap[s];
+    const int64_t over = rows_over(s);
     const int64_t want = over > 0 ? (over + CATEKV_PAGE_ROWS - 1) / CATEKV_PAGE_ROWS : 0;
     if (want > p->max_pages) return CATEKV_ERR_CAPACITY;
     if (want > p->seg_pages[s]) extra += want - p->seg_pages[s];
@@ -334,7 +333,7 @@ extern "C" int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_s
   PageOrders orders;
   int next = p->next_free;
   for (int s = 0; s < n; ++s) {
-    const int64_t over = (int64_t)cache->seg_len[s] + n_new - cache->seg_cap[s];
+    const int64_t over = rows_over(s);
     const int want = over > 0 ? div_up(over, CATEKV_PAGE_ROWS) : 0, have = p->seg_pages[s];
     const size_t g0 = given.n;
     for (int q = have; q < want; ++q) {
@@ -350,7 +349,7 @@ extern "C" int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_s
   size_t g = 0;
   int top = p->next_free;
   for (int s = 0; s < n; ++s) {
-    const int64_t over = (int64_t)cache->seg_len[s] + n_new - cache->seg_cap[s];
+    const int64_t over = rows_over(s);
     const int want = over > 0 ? div_up(over, CATEKV_PAGE_ROWS) : 0;
     for (int q = p->seg_pages[s]; q < want; ++q) {
       top = std::max(top, given[g] + 1);
@@ -361,6 +360,20 @@ extern "C" int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_s
   p->released += top - p->next_free - (int)extra;
   p->next_free = top;
   return CATEKV_OK;
+}
+
+}  // namespace catekv
+
+using namespace catekv;
+
+extern "C" int catekv_pages_reserve(catekv_cache* cache, int32_t n_new, catekv_stream stream) {
+  CATEKV_API_RANGE();
+  return reserve(cache, n_new, nullptr, stream);
+}
+
+extern "C" int catekv_pages_reserve_each(catekv_cache* cache, const int32_t* n_new, catekv_stream stream) {
+  CATEKV_API_RANGE();
+  return n_new ? reserve(cache, 0, n_new, stream) : CATEKV_ERR_INVALID_ARG;
 }
 
 extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_stream stream) {

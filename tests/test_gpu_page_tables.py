@@ -206,3 +206,31 @@ def test_next_free_follows_the_pages_in_use(ck, seed):
         assert p.struct.next_free == top if counted else p.struct.next_free >= top
         assert p.struct.released == p.struct.next_free - len(used)
         assert p.struct.next_free <= p.struct.n_pages
+
+
+def test_a_mixed_batch_gets_the_pages_it_needs(ck):
+    """A piece of a prompt beside sequences that decode: pages for the piece in its sequence's lists alone."""
+    B, Hkv = 8, 2
+    m = Model(ck, B, Hkv, [128] * (B * Hkv), 40, 12, 4)
+    n_new = [0, 1, 600, 1, 0, 1, 70, 1]
+    with pytest.raises(ck.CatekvError) as e:
+        ck.catekv_pages_reserve(m.cache, max(n_new))  # 10 pages for each of the 16 lists
+    assert e.value.code == ck.ERR_CAPACITY
+    ck.catekv_pages_reserve_each(m.cache, n_new)
+    assert m.cache.pages.seg_pages.tolist() == [-(-n // 64) for n in n_new for _ in range(Hkv)]
+    m.append(n_new)
+    m.verify()
+    check_tables(m)
+    ck.catekv_pages_reserve_each(m.cache, [0] * B)  # nothing to do
+    m.truncate([0, 0, 300, 0, 0, 0, 70, 0])
+    ck.catekv_pages_reserve_each(m.cache, [300, 0, 0, 0, 100, 0, 0, 0])
+    m.append([300, 63, 20, 0, 100, 0, 0, 0])
+    m.verify()
+    check_tables(m)
+    before = state(m)
+    for n in ([1] * (B - 1), [-1] + [0] * (B - 1), None):
+        with pytest.raises((ck.CatekvError, TypeError)):
+            ck.catekv_pages_reserve_each(m.cache, n)
+    with pytest.raises(ck.CatekvError) as e:
+        ck.catekv_pages_reserve_each(m.cache, [5000] + [0] * (B - 1))  # more than a table row holds
+    assert e.value.code == ck.ERR_CAPACITY and state(m) == before

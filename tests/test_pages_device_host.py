@@ -22,3 +22,19 @@ def test_a_cache_on_another_device_is_refused(ck, monkeypatch):  # noqa: F811
             call()
         assert e.value.code == ck.ERR_INVALID_ARG
     assert f.state() == before
+
+
+def test_reserving_by_sequence_is_refused(ck):  # noqa: F811
+    import ctypes as C
+    f = Fake(ck, [128, 128], B=2, pages=(3, 4))
+    before = f.state()
+    call = lambda *n: ck._lib.catekv_pages_reserve_each(C.byref(f.st), np.array(n, dtype=np.int32).ctypes.data_as(C.c_void_p), None)
+    assert ck._lib.catekv_pages_reserve_each(C.byref(f.st), None, None) == ck.ERR_INVALID_ARG
+    assert ck._lib.catekv_pages_reserve_each(None, None, None) == ck.ERR_INVALID_ARG
+    assert call(-1, 0) == call(0, -1) == ck.ERR_INVALID_ARG
+    assert call(0, 0) == ck.OK
+    assert call(200, 1) == ck.ERR_CAPACITY            # five pages, three are there
+    assert call(257, 0) == call(2 ** 31 - 1, 0) == ck.ERR_CAPACITY  # a table row of four pages
+    g = Fake(ck, [128, 128], B=2)
+    assert ck._lib.catekv_pages_reserve_each(C.byref(g.st), np.zeros(2, dtype=np.int32).ctypes.data_as(C.c_void_p), None) == ck.ERR_INVALID_ARG  # no pages
+    assert f.state() == before
