@@ -171,7 +171,7 @@ int catekv_checked_status(catekv_status* out, int32_t clear);
 
 /*
  * Test hook, host side: the next n_launches launches of the tensor-core kernels (window scoring, window
- * attention) run with their producer lanes idle
+ * attention, chunk attention) run with their producer lanes idle
  * (no copy and no tensor-core instruction is issued) and a wait limit of 512 polls, so that every wait runs out
  * with nothing in flight and the CATEKV_STATUS_WAIT_EXPIRED path executes.  Process-wide counter; 0 switches
  * it off.  Nothing faults or hangs: the CTAs free their tensor memory and return.
@@ -572,7 +572,8 @@ typedef struct catekv_chunk {
  * CATEKV_ERR_CAPACITY (nothing launched) if a list cannot take its rows: catekv_pages_reserve_each gives it pages.
  * CATEKV_ERR_INVALID_ARG for a cache without seg_cap_dev.  A replayed call goes by the device's lengths, so its lists are given room before
  * it, as for a replayed catekv_append (the mirror: catekv_cache_sync_lengths, or catekv_cache_advance where all sequences grow alike).  Rows
- * for which a list has no room are dropped and not counted.
+ * for which a list has no room are dropped and not counted.  Retrieval metadata does not follow: a caller who keeps it builds it anew
+ * (catekv_retrieval_build) before the next retrieval.
  */
 int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const void* k_new, const void* v_new, int64_t stride_t,
                         int64_t stride_h, catekv_stream stream);
@@ -591,7 +592,8 @@ int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const vo
  *            (streams, replayed graphs) need a workspace each
  * fp32 accumulation.  With out_dtype fp32 the probabilities enter the product with V as three bf16 numbers (all their bits), with bf16
  * as two (17 bits).  An infinity or a NaN in a row
- * leaves the results of the queries that see the row not finite (in its column, where it is in V) and touches no other.
+ * of V leaves the results of the queries that see the row not finite in its column; in a row of K those of the queries that see it and whose logit it
+ * makes NaN or +infinity (a logit of -infinity weighs 0).  No other result is touched.
  * The device's lengths decide, so a captured call follows lists that grow; the lengths on the host (upper bounds will do)
  * only choose the number of CTAs.  Follows overflow pages.  Segment capacities are multiples of CATEKV_SEG_ALIGN, and the cache
  * has seg_cap_dev (CATEKV_ERR_INVALID_ARG).  CATEKV_ERR_UNSUPPORTED if blocks of 128 query rows times blocks of 128 rows of their lists' capacities
@@ -617,7 +619,8 @@ int catekv_chunk_attn(const catekv_cache* cache, const catekv_chunk* chunk, cons
  * written (the descriptor's const is for the other calls): seg_off[b's list] = the parent's, seg_cap = the rows shared in place.  b's own segment
  * is not used again by b.  Pages that b held alone are given out again in the same call, unless another sequence continues from b.
  * Rows that are shared must not be rewritten: catekv_evict, catekv_select_compact and the 8-bit and retrieval calls refuse caches with
- * pages, as they always have; catekv_cache_regrow makes an unshared copy.  Decode plans made before are refused (CATEKV_ERR_INVALID_ARG).
+ * pages, as they always have; catekv_cache_regrow makes an unshared copy.  Decode plans are made anew after it; one made before is
+ * refused (CATEKV_ERR_INVALID_ARG) where a list's place has changed by it.
  * CATEKV_ERR_CAPACITY (nothing changed) if the pages or a table row run out.
  *
  * catekv_pages_compact moves the pages in use to the front of the overflow pools (the lowest of those that lie behind goes to the
