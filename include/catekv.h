@@ -80,8 +80,8 @@ typedef void* catekv_stream; /* cudaStream_t */
  * what they hold (the paper sizes its caches up front and has no counterpart).  Row r of segment s lives in the
  * cache's own pools while r < seg_cap[s]; beyond that, row seg_cap[s] + 64 p + i is row 64 table[s][p] + i of the
  * overflow pools.  Pages are handed out by catekv_pages_reserve and catekv_pages_reserve_each (the lowest free ones first); they come back, are shared and move by
- * catekv_truncate, catekv_fork and catekv_pages_compact, and by no other call.  The first seg_pages[s] entries of a table row are in force,
- * those behind them are -1.  All arrays are allocated by the caller; table and table_dev start out filled with -1, seg_pages with 0.
+ * catekv_truncate, catekv_fork and catekv_pages_compact, and by no other call.  The first seg_pages[s] entries of a table row are in force;
+ * behind them lie entries of pages that the list has given back, which become -1 before such a page is handed out or moved to, and -1.  All arrays are allocated by the caller; table and table_dev start out filled with -1, seg_pages with 0.
  */
 typedef struct catekv_pages {
   int32_t max_pages;   /* table entries per segment */
@@ -572,7 +572,8 @@ typedef struct catekv_chunk {
  * CATEKV_ERR_CAPACITY (nothing launched) if a list cannot take its rows: catekv_pages_reserve_each gives it pages.
  * CATEKV_ERR_INVALID_ARG for a cache without seg_cap_dev.  A replayed call goes by the device's lengths, so its lists are given room before
  * it, as for a replayed catekv_append (the mirror: catekv_cache_sync_lengths, or catekv_cache_advance where all sequences grow alike).  Rows
- * for which a list has no room are dropped and not counted.  Retrieval metadata does not follow: a caller who keeps it builds it anew
+ * for which a list has no room are dropped and not counted, except that a list takes a page again that it has given back while that is free: the host's
+ * calls then refuse the cache (CATEKV_ERR_INVALID_ARG: longer than its capacity).  Retrieval metadata does not follow: a caller who keeps it builds it anew
  * (catekv_retrieval_build) before the next retrieval.
  */
 int catekv_append_chunk(catekv_cache* cache, const catekv_chunk* chunk, const void* k_new, const void* v_new, int64_t stride_t,

@@ -126,19 +126,11 @@ constexpr int kDropSeqs = 512;
 struct Drops {
   int32_t n[kDropSeqs];
 };
-// A warp a list: its new length, and -1 for the table entries (up to `most`) of pages that it has given back.  They may be another list's soon: a replayed
-// append that finds its list full, and an attention under a plan made for the longer list, must not follow them.
-__global__ void __launch_bounds__(128) truncate_kernel(int32_t* seg_len, const __grid_constant__ Drops d, int Hkv, int seg0, int n, int32_t* table,
-                                                       const int32_t* seg_cap, int max_pages, int most) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(128) truncate_kernel(int32_t* seg_len, const __grid_constant__ Drops d, int Hkv, int seg0, int n) {
+  const int i = blockIdx.x * 128 + threadIdx.x;
   if (i >= n) return;
-  const int drop = d.n[i / Hkv], seg = seg0 + i;
-  if (drop <= 0) return;
-  const int len = max(0, seg_len[seg] - drop);
-  __syncwarp();
-  if (lane == 0) seg_len[seg] = len;
-  if (!table) return;
-  for (int q = (max(0, len - seg_cap[seg]) + CATEKV_PAGE_ROWS - 1) / CATEKV_PAGE_ROWS + lane; q < most; q += 32) table[(int64_t)seg * max_pages + q] = -1;
+  const int drop = d.n[i / Hkv];
+  if (drop > 0) seg_len[seg0 + i] = max(0, seg_len[seg0 + i] - drop);
 }
 
 // a growing array of host memory that does not throw
@@ -271,6 +263,29 @@ static int send_moves(const catekv_cache* c, const int32_t* src, const int32_t* 
   }
   return CATEKV_OK;
 }
+// Table entries behind those in force.  A list that gives pages back keeps their entries while the pages are free and were its own: it is likely to be given
+// them again, and catekv_truncate then needs no order (drafted tokens).  Before a page is handed out or moved to, every such entry becomes -1, so
+// that no list's row names a page of another one, which a replayed append without room, or attention under a plan made for a longer list, would follow.
+// Host and device hold the same entries; they lie directly behind those in force.
+static int entries_end(const catekv_pages* p, int s) {
+  const int32_t* row = p->table + (size_t)s * p->max_pages;
+  int q = p->seg_pages[s];
+  while (q < p->max_pages && row[q] >= 0) ++q;
+  return q;
+}
+// Orders that clear them, of all lists, from entry from(s) on; forget: the same on the host.
+template <class From>
+static bool clear_behind(const catekv_cache* c, PageOrders& orders, From from) {
+  for (int s = 0; s < c->B * c->Hkv; ++s) {
+    const int at = from(s), end = entries_end(c->pages, s);
+    if (at < end && !orders.clear((int64_t)s * c->pages->max_pages + at, end - at)) return false;
+  }
+  return true;
+}
+static void forget(catekv_pages* p, int s, int at) {
+  int32_t* row = p->table + (size_t)s * p->max_pages;
+  for (int q = at; q < p->max_pages && (q < p->seg_pages[s] || row[q] >= 0); ++q) row[q] = -1;
+}
 struct FreePages {  // the lowest pages that no list held when the call began, one after the other
   const HostList<int32_t>& count;
   int at = 0;
@@ -309,10 +324,11 @@ static int reserve(catekv_cache* cache, int32_t all_new, const int32_t* each, ca
     if (each[b] < 0) return CATEKV_ERR_INVALID_ARG;
   catekv_pages* p = cache->pages;
   const int n = cache->B * cache->Hkv;
-  auto rows_over = [&](int s) { return (int64_t)cache->seg_len[s] + (each ? each[s / cache->Hkv] : all_new) - cache->seg_cap[s]; };
+  auto rows_over = [&](int s) -> int64_t { return (int64_t)cache->seg_len[s] + (each ? each[s / cache->Hkv] : all_new) - cache->seg_cap[s]; };
   // first pass: what is needed, nothing changed yet
   int64_t extra = 0;
   for (int s = 0; s < n; ++s) {
+    if (p->seg_pages[s] < 0 || p->seg_pages[s] > p->max_pages) return CATEKV_ERR_INVALID_ARG;
     if (cache->seg_len[s] < 0 || cache->seg_len[s] > seg_capacity(cache, s)) return CATEKV_ERR_INVALID_ARG;
     const int64_t over = rows_over(s);
     const int64_t want = over > 0 ? (over + CATEKV_PAGE_ROWS - 1) / CATEKV_PAGE_ROWS : 0;
@@ -343,9 +359,12 @@ static int reserve(catekv_cache* cache, int32_t all_new, const int32_t* each, ca
     }
     if (want > have && !orders.entries((int64_t)s * p->max_pages + have, given.p + g0, want - have)) return CATEKV_ERR_WORKSPACE;
   }
+  auto pages_then = [&](int s) { return std::max(p->seg_pages[s], (int)std::max<int64_t>(0, (rows_over(s) + CATEKV_PAGE_ROWS - 1) / CATEKV_PAGE_ROWS)); };
+  if (!clear_behind(cache, orders, pages_then)) return CATEKV_ERR_WORKSPACE;
   rc = check_not_captured((cudaStream_t)stream);
   if (!rc) rc = send(cache, orders, (cudaStream_t)stream);
   if (rc) return rc;
+  for (int s = 0; s < n; ++s) forget(p, s, pages_then(s));
   size_t g = 0;
   int top = p->next_free;
   for (int s = 0; s < n; ++s) {
@@ -429,7 +448,6 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
                                     std::min(CATEKV_PAGE_ROWS, len - r), to + c.full + i);
       }
       ok = ok && children.push(c) && orders.segment(s, c.off, c.cap, c.len);
-      ok = ok && orders.clear(to + c.full + c.fresh, p->seg_pages[s] - (c.full + c.fresh));
       if (moving) {
         ok = ok && orders.entries(to, p->table + row, c.full);
         for (int q = 0; q < c.full; ++q) ok = ok && entries.push(p->table[row + q]);
@@ -439,12 +457,19 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
       if (!ok) return CATEKV_ERR_WORKSPACE;
     }
   }
+  HostList<int32_t> pages_then;
+  if (!pages_then.fill(n, 0)) return CATEKV_ERR_WORKSPACE;
+  for (int s = 0; s < n; ++s) pages_then[s] = p->seg_pages[s];
+  for (size_t i = 0; i < children.n; ++i) pages_then[children[i].seg] = children[i].full + children[i].fresh;
+  if (!clear_behind(cache, orders, [&](int s) { return pages_then[s]; })) return CATEKV_ERR_WORKSPACE;
   cudaStream_t st = (cudaStream_t)stream;
   rc = check_not_captured(st);
   if (!rc) rc = send(cache, orders, st);
   if (rc) return rc;
   int32_t *seg_off = const_cast<int32_t*>(cache->seg_off), *seg_cap = const_cast<int32_t*>(cache->seg_cap);
   size_t at = 0;
+  for (int s = 0; s < n; ++s)
+    if (parent[s / Hkv] == s / Hkv) forget(p, s, p->seg_pages[s]);
   for (int s = 0; s < n; ++s)  // what replaced parents held; the others' pages are not counted
     if (parent[s / Hkv] != s / Hkv && !gone[s])
       for (int q = 0; q < p->seg_pages[s]; ++q) --count[p->table[(size_t)s * p->max_pages + q]];
@@ -462,7 +487,7 @@ extern "C" int catekv_fork(catekv_cache* cache, const int32_t* parent, catekv_st
     seg_off[c.seg] = c.off;
     seg_cap[c.seg] = c.cap;
     cache->seg_len[c.seg] = c.len;
-    for (int q = c.full + c.fresh; q < p->seg_pages[c.seg]; ++q) row[q] = -1;
+    forget(p, c.seg, c.full + c.fresh);
     p->seg_pages[c.seg] = c.full + c.fresh;
     for (int q = 0; q < c.full + c.fresh; ++q) ++count[row[q]];
   }
@@ -492,6 +517,7 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
 
   struct Change {
     int32_t seg, cap, pages, n_entries, first, entry[2];  // new capacity and page count; table entries [first, first + n_entries) that change
+    bool clear;                                           // the entries behind them are cleared at once
   };
   HostList<Change> changes;
   HostList<int32_t> count, at_start, cap;
@@ -530,10 +556,13 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
       }
       const int len = std::max(0, cache->seg_len[s] - drop);
       int32_t* row = p->table + (size_t)s * p->max_pages;
-      Change c = {s, cap[s], len > cap[s] ? div_up(len - cap[s], CATEKV_PAGE_ROWS) : 0, 0, 0, {0, 0}};
+      Change c = {s, cap[s], len > cap[s] ? div_up(len - cap[s], CATEKV_PAGE_ROWS) : 0, 0, 0, {0, 0}, len == 0};
       const bool read = member && len < cap[s] && std::max(passed[group[s]], behind[s]) > len;  // another list reads the segment's rows behind the new end
       const int kept = read ? 0 : c.pages;
-      for (int q = kept; q < p->seg_pages[s]; ++q) --count[row[q]];
+      for (int q = kept; q < p->seg_pages[s]; ++q) {
+        --count[row[q]];
+        c.clear = c.clear || at_start[row[q]] > 1;  // another list's entry too: they would both be given it
+      }
       if (read) {
         c.cap = len / CATEKV_SEG_ALIGN * CATEKV_SEG_ALIGN;
         c.pages = c.n_entries = div_up(len - c.cap, CATEKV_PAGE_ROWS);
@@ -564,6 +593,18 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
       if (!changes.push(c)) return CATEKV_ERR_WORKSPACE;
     }
   }
+  HostList<int32_t> pages_then;
+  const bool hands_out = orders.copies.n > 0;
+  if (p) {
+    if (!pages_then.fill(n, 0)) return CATEKV_ERR_WORKSPACE;
+    for (int s = 0; s < n; ++s) pages_then[s] = hands_out ? p->seg_pages[s] : p->max_pages;  // (what is given back by this call is not handed out by it)
+    for (size_t i = 0; i < changes.n; ++i) {
+      const Change& c = changes[i];
+      if (c.clear) pages_then[c.seg] = c.pages;
+      else if (hands_out) pages_then[c.seg] = std::max(c.pages, p->seg_pages[c.seg]);
+    }
+    if (!clear_behind(cache, orders, [&](int s) { return pages_then[s]; })) return CATEKV_ERR_WORKSPACE;
+  }
   cudaStream_t st = (cudaStream_t)stream;
   rc = check_not_captured(st);
   if (rc) return rc;
@@ -571,27 +612,22 @@ extern "C" int catekv_truncate(catekv_cache* cache, const int32_t* n_drop, catek
     rc = send(cache, orders, st);
     if (rc) return rc;
   }
-  int most = 0;  // entries in force, of the list with most of them
-  if (p)
-    for (int s = 0; s < n; ++s)
-      if (n_drop[s / Hkv] > 0) most = std::max(most, p->seg_pages[s]);
   for (int b0 = 0; b0 < B; b0 += kDropSeqs) {
     Drops d;
     const int nb = std::min(kDropSeqs, B - b0);
     memcpy(d.n, n_drop + b0, sizeof(int32_t) * (size_t)nb);
-    truncate_kernel<<<div_up((int64_t)nb * Hkv, 4), 128, 0, st>>>(cache->seg_len_dev, d, Hkv, b0 * Hkv, nb * Hkv, p ? p->table_dev : nullptr,
-                                                                   p ? p->seg_cap_dev : nullptr, p ? p->max_pages : 0, most);
+    truncate_kernel<<<div_up((int64_t)nb * Hkv, 128), 128, 0, st>>>(cache->seg_len_dev, d, Hkv, b0 * Hkv, nb * Hkv);
     CATEKV_CUDA_TRY(cudaGetLastError());
   }
   for (int s = 0; s < n; ++s)
     if (n_drop[s / Hkv] > 0) cache->seg_len[s] = std::max(0, cache->seg_len[s] - n_drop[s / Hkv]);
   if (p) {
     int32_t* seg_cap = const_cast<int32_t*>(cache->seg_cap);
+    for (int s = 0; s < n; ++s) forget(p, s, pages_then[s]);
     for (size_t i = 0; i < changes.n; ++i) {
       const Change& c = changes[i];
       int32_t* row = p->table + (size_t)c.seg * p->max_pages;
       seg_cap[c.seg] = c.cap;
-      for (int q = c.pages; q < p->seg_pages[c.seg]; ++q) row[q] = -1;
       p->seg_pages[c.seg] = c.pages;
       for (int q = 0; q < c.n_entries; ++q) row[c.first + q] = c.entry[q];
     }
@@ -623,9 +659,13 @@ extern "C" int catekv_pages_compact(catekv_cache* cache, int32_t* n_used, catekv
   }
   cudaStream_t st = (cudaStream_t)stream;
   if (src.n) {
+    PageOrders orders;
+    if (!clear_behind(cache, orders, [&](int s) { return p->seg_pages[s]; })) return CATEKV_ERR_WORKSPACE;
     rc = check_not_captured(st);
-    if (!rc)
-      rc = p->n_pages > 65536 ? send_moves<int32_t, kManyBytes>(cache, src.p, dst.p, src.n, st)
+    if (!rc) rc = send(cache, orders, st);
+    if (rc) return rc;
+    for (int s = 0; s < n; ++s) forget(p, s, p->seg_pages[s]);
+    rc = p->n_pages > 65536 ? send_moves<int32_t, kManyBytes>(cache, src.p, dst.p, src.n, st)
            : src.n * 4 > kFewBytes ? send_moves<uint16_t, kManyBytes>(cache, src.p, dst.p, src.n, st)
                                    : send_moves<uint16_t, kFewBytes>(cache, src.p, dst.p, src.n, st);
     if (rc) return rc;

@@ -47,15 +47,16 @@ def test_pages_are_not_handed_out_or_moved_in_a_capture(ck):
 
 
 def check_tables(m):
-    """Host and device agree on every entry, and those behind the pages in force name none."""
+    """Host and device agree on every entry; those behind the pages in force are -1, or name a page that is free and no other list's row names."""
     p = m.cache.pages
     torch.cuda.synchronize()
     assert p.table_dev.tolist() == p.table.tolist()
-    for s in range(m.S):
-        assert (p.table[s, int(p.seg_pages[s]):] == -1).all()
+    used = {int(x) for s in range(m.S) for x in p.table[s, :int(p.seg_pages[s])]}
+    behind = [int(x) for s in range(m.S) for x in p.table[s, int(p.seg_pages[s]):] if x >= 0]
+    assert len(set(behind)) == len(behind) and not used & set(behind)
 
 
-def test_tables_name_no_page_that_was_given_back(ck):
+def test_tables_name_no_page_of_another_list(ck):
     m = Model(ck, 4, 2, [300] * 8, 80, 12, 5)
     for step in (lambda: ck.catekv_pages_reserve(m.cache, 400), lambda: m.append([400, 10, 130, 0]), lambda: m.truncate([250, 0, 1, 300]),
                  lambda: m.fork([0, 0, 2, 2]), lambda: ck.catekv_pages_reserve(m.cache, 70), lambda: m.append([3, 70, 64, 1]), lambda: m.fork([2, 3, 0, 1]),
@@ -110,31 +111,48 @@ def test_a_replayed_token_does_not_follow_a_page_that_was_given_back(ck, steps):
 
 def test_a_plan_made_before_rows_were_taken_back(ck):
     """It knows rows in pages that the list has given back: they are left out, whoever has the pages now."""
-    B, Hkv, G = 2, 1, 4
-    m = Model(ck, B, Hkv, [100, 100], 12, 8, 3)
-    ck.catekv_pages_reserve(m.cache, 300)
-    m.append([300, 300])
+    G = 4
+    m = Model(ck, 3, 1, [100] * 3, 14, 12, 3)
+    ck.catekv_pages_reserve_each(m.cache, [300, 300, 0])
+    m.append([300, 300, 0])
     plan = ck.DecodePlan(m.cache, 7)
     ck.catekv_decode_plan(m.cache, plan)
-    q = torch.randn(B, Hkv * G, D, device="cuda").bfloat16()
+    q = torch.randn(3, G, D, device="cuda").bfloat16()
     out, lse = torch.zeros(q.shape, device="cuda"), torch.zeros(q.shape[:2], device="cuda")
-    for drop, add in (([250, 0], [0, 0]), ([0, 20], [0, 0]), ([90, 200], [0, 0]), ([0, 0], [7, 5])):
+    odd = torch.full((400, 1, D), float("inf"), device="cuda", dtype=torch.bfloat16)
+    for drop, add in (([250, 0, 0], [0, 0, 150]), ([0, 20, 0], [0, 0, 60]), ([90, 200, 0], [0, 0, 250]), ([0, 0, 0], [7, 5, 0])):
         m.truncate(drop)
-        free = sorted(set(range(12)) - {int(x) for s in range(2) for x in m.cache.pages.table[s, :int(m.cache.pages.seg_pages[s])]})
-        for page in free:  # what another list may have there
-            m.cache.pages.k_ovf[page * 64:page * 64 + 64] = float("nan")
-            m.cache.pages.v_ovf[page * 64:page * 64 + 64] = float("inf")
-        if any(add):
-            ck.catekv_pages_reserve(m.cache, max(add))
+        check_tables(m)
+        ck.catekv_pages_reserve_each(m.cache, add)
+        check_tables(m)
+        if add[2]:  # the third sequence gets the pages, and rows of infinities
+            ck.catekv_append_chunk(m.cache, ck.Chunk(add), odd[:add[2]], odd[:add[2]])
+            m.lists[2] = [torch.cat([x, odd[:add[2], 0]]) for x in m.lists[2]]
+        else:
             m.append(add)
+        m.verify()
         ck.catekv_decode_attn(m.cache, q, plan, out, lse)
-        for b in range(B):
+        for b in range(2):
             kk, vv = (x.double() for x in m.lists[b])
             z = q[b].double() @ kk.T * D ** -0.5
             o = torch.softmax(z, 1) @ vv
             assert float((out[b].double() - o).norm() / o.norm()) <= 1e-5
             assert float((lse[b].double() - torch.logsumexp(z, 1)).abs().max()) <= 1e-5
+
+
+def test_drafts_keep_the_tables_entries(ck):
+    """Pages given back and reserved again by the same lists: the same entries, and no order for the device in between."""
+    m = Model(ck, 3, 2, [200] * 6, 60, 8, 5)
+    ck.catekv_pages_reserve(m.cache, 150)
+    first = m.cache.pages.table.copy()
+    for _ in range(3):
+        m.append([150, 100, 3])
+        m.truncate([150, 100, 3])
+        torch.cuda.synchronize()
+        assert (m.cache.pages.table == first).all() and m.cache.pages.table_dev.tolist() == first.tolist()
+        m.verify()
         check_tables(m)
+        ck.catekv_pages_reserve(m.cache, 150)
 
 
 def test_many_sequences_leave_shared_rows_in_turn(ck):
