@@ -219,12 +219,14 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
       if (start + rows_left > pc.cap + pg0 * 64) page0 = checked_clamp(page0, none, a.n_pages - 1, a.chk, kKidAttention, pc.seg);
       if (start + rows_left > pc.cap + (pg0 + 1) * 64) page1 = checked_clamp(page1, none, a.n_pages - 1, a.chk, kKidAttention, pc.seg);
 #endif
+      // a page that has been given back since the plan was made: no row of the list lies there, nor behind it
+      if ((page0 | page1) < 0) rows_left = min(rows_left, pc.cap - start + (page0 < 0 ? pg0 : pg0 + 1) * 64);
     }
 #pragma unroll
     for (int i = 0; i < (kTile * 16) / kDecodeThreads; ++i) {
       const int id = tid + i * kDecodeThreads;
       const int r = id >> 4, c = id & 15;
-      int ok = r < rows_left ? 16 : 0;
+      const int ok = r < rows_left ? 16 : 0;
       int64_t grow = ok ? row0 + r : 0;  // padding rows read nothing
       uint8_t* kp = a.k_pool;
       uint8_t* vp = a.v_pool;
@@ -234,9 +236,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) decode_partial_kernel(const
 #endif
       if (kIndexed && pc.indexed && ok) grow = (pc.row_base - pc.t0) + ix[i];
       if (kPaged && ok && start + r >= pc.cap) {  // the row lives in an overflow page
-        const int o = start + r - pc.cap, page = (o >> 6) == pg0 ? page0 : page1;
-        if (page < 0) ok = 0;  // given back since the plan was made: no row of the list lies there
-        grow = ok ? (int64_t)page * 64 + (o & 63) : 0;
+        const int o = start + r - pc.cap;
+        grow = (int64_t)((o >> 6) == pg0 ? page0 : page1) * 64 + (o & 63);
         kp = a.k_ovf;
         vp = a.v_ovf;
       }
