@@ -18,11 +18,11 @@
 // cycles a tile for two M tiles and P in one part, 3400 with steps of 64, where the products need 2050; S with 64 keys reads its Q operand twice as often.)  One M tile with
 // bf16 results (kSplit) has four slots and softmax warps for either step of a tile: S is formed two tiles ahead, as few rows are a chain of waits otherwise.
 //
-// Bounds and measures (B200, single runs).  Full blocks: the products, three for the formula's two; 4096 tokens over 8 lists of 16 K rows, G = 4, in 1300 us
-// with either form (950 TFLOP/s of the formula's, 1400 of the three products); 4096 tokens alone in 179 us; two M tiles, 512 tokens over 3 lists of 117 K
+// Bounds and measures (B200, single runs).  Full blocks: the products, three for the formula's two; 4096 tokens over 8 lists of 16 K rows, G = 4, in 1220 to
+// 1300 us with either form (950 to 1020 TFLOP/s of the formula's two products, half as much again in all); 4096 tokens alone in 173 to 186 us; two M tiles, 512 tokens over 3 lists of 117 K
 // rows, in 417 us.  Few rows: K and V once through DRAM; 4 tokens of 16 x 32 K rows in 311 to 346 us, 6.2 to 6.9 TB/s; a token over 8 lists of 128 rows in 7.9 us, which are waits one behind the other (schedule 1 us, loads 1, S, softmax and product 2.5,
 // results 0.7, the merge's launch).  fp32 results: three products for one, and the softmax's conversions; 333 tokens of 7 heads a group over
-// 2 lists of 65 K rows in 296 us.
+// 2 lists of 65 K rows in 280 to 316 us.
 //
 // Precision.  kParts = 2 (bf16 results): P with 17 significant bits in every form, so that the result's own rounding is what is seen of it (with P in one bf16
 // number, 2^-9, 512 tokens over 117 K rows take 341 us for 417, and the error of results in the norm is 2.3e-3 for 1.65e-3; which form runs
@@ -910,7 +910,7 @@ __global__ void __launch_bounds__(ChunkShape<kQ2, kFlush, kDup>::kThreads, 1)
 // begins inside a block; the first such CTA of a block has it merged.  A thread block takes kRows rows, a thread kVec float4 of a row; what threads are
 // left share out the pieces (few rows of one long list come in up to 148), and the groups' sums are merged in their order.  Bound by its trips
 // to memory: descriptors, pieces; so references are not looked through first, the sums follow them piece by piece (24 blocks of 126 rows in 7 pieces:
-// 7.1 us; 147 blocks of 256 rows in 2 pieces, 57 MB, 18 us; one list of 60 K rows in 148 pieces 9.3 us).
+// 7.1 us; 147 blocks of 128 rows in 2 pieces 10 us; one list of 60 K rows in 148 pieces 9.3 us).
 struct ChunkSum {
   float m, l;  // reference (log2 domain), sum
   // the weights of what is there and of what comes; a part that sees no key has nothing to add, or the NaN that it has met
